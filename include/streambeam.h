@@ -268,9 +268,177 @@ sb_status sb_timing(sb_decoder *dec, double *proj_ms, int64_t *proj_launches);
 
 sb_status sb_destroy(sb_decoder *dec);
 /* Text of the decoder's last failure; with dec == NULL, of the calling
- * thread's last failed sb_create_noalloc. */
+ * thread's last failed sb_create_noalloc or serving call. */
 const char *sb_last_error(const sb_decoder *dec);
 const char *sb_status_string(sb_status s);
+
+/* ------------------------------------------------------------------------
+ * Cached decoding of transformer decoders, and sampled tokens: the operators
+ * of a serving step next to the search. Each call takes a struct of its
+ * arguments (host memory, read before the call returns) and a stream, checks
+ * the arguments on the host, enqueues its kernels and returns without
+ * waiting. The calls keep nothing between them, allocate nothing and may be
+ * captured into a HIP graph; they are thread-safe. All arrays are device
+ * memory of the current device, owned by the caller. A refused call enqueues
+ * nothing; sb_last_error(NULL) gives the reason.
+ *
+ * What only the GPU can see (lengths, page ids, slots, per-row parameters) is
+ * never trusted with an address: page ids and slots outside the cache are
+ * skipped, as said at each call.
+ *
+ * The paged cache of one layer: keys and values are arrays of n_pages pages of
+ * page_size tokens, each token kv_heads rows of head_dim values (strides in
+ * elements, rows contiguous). Request b's token at position p lies in page
+ * table[b][p / page_size], place p % page_size; its slot is
+ * page * page_size + place. SB_BF16 or SB_F16. Addresses of q, k, v, out and
+ * the caches are 16-byte aligned and their strides multiples of 8 elements.
+ * ------------------------------------------------------------------------ */
+
+/* IEEE half precision, for these calls only (next to sb_dtype's two). */
+enum { SB_F16 = 2 };
+
+/* Block tables and slot maps of a step from the requests' lengths.
+ * add[b] > 0 asks for that many new tokens, 0 leaves request b as it is, < 0
+ * releases it: its ceil(lens / page_size) pages go back, its length becomes 0.
+ * Released pages are pushed on the free list (request, then page order) before
+ * any page is taken. Requests are then granted in index order as long as the
+ * tokens total at most token_cap and the pages last; the first that does not
+ * fit and all behind it get 0 tokens (callers ask again next step). A request
+ * whose tokens would not fit its table row alone gets 0 and holds up nobody.
+ * New pages are popped from the end of the free list, ascending by request and
+ * table column. The new state goes to lens_out and n_free_out, which may be
+ * lens and n_free: with other arrays the call can be repeated, and does the
+ * same again. Lengths are taken as 0 .. max_pages * page_size and n_free as
+ * 0 .. n_pages where they lie outside; pages beyond n_pages on the free list
+ * are dropped. */
+typedef struct {
+  int64_t struct_bytes;     /* sizeof(sb_plan_args)                                 */
+  const int32_t *lens;      /* [n_requests] tokens cached                           */
+  const int32_t *add;       /* [n_requests]                                         */
+  const int32_t *n_free;    /* [1] pages on the free list                           */
+  int32_t *free_list;       /* [n_pages] page ids, in/out                           */
+  int32_t *table;           /* [n_requests][table_stride] page ids, in/out          */
+  int32_t *lens_out;        /* [n_requests]                                         */
+  int32_t *n_free_out;      /* [1]                                                  */
+  int32_t *q_start;         /* [n_requests + 1] first new token of each request     */
+  int32_t *granted;         /* [n_requests] tokens granted                          */
+  int64_t *slots;           /* [token_cap] cache slot of each new token, -1 behind  */
+  int32_t *positions;       /* [token_cap] its position in its request, -1 behind   */
+  int64_t table_stride;     /* >= max_pages                                         */
+  int32_t n_requests;       /* 1 .. SB_PLAN_MAX_REQUESTS                            */
+  int32_t n_pages;          /* >= 1                                                 */
+  int32_t page_size;        /* 1 .. 4096; n_pages and max_pages times it < 2^31     */
+  int32_t max_pages;        /* columns of the table in use, >= 1                    */
+  int32_t token_cap;        /* >= 0                                                 */
+  int32_t reserved;         /* 0                                                    */
+} sb_plan_args;
+#define SB_PLAN_MAX_REQUESTS 8192
+sb_status sb_plan_pages(const sb_plan_args *args, void *stream);
+
+/* Rotary positions and the write into the cache. For every token t and pair i
+ * of a head's first 2 n_pairs values, (a, b) becomes
+ *   (a c - b s, a s + b c),  c, s = mscale * cos, sin(positions[t] * inv_freq[i])
+ * (angles in fp64, the rotation in fp32, rounded once); the rest of the head
+ * is copied. Pairs are (i, i + n_pairs) (SB_ROPE_HALF) or (2i, 2i + 1)
+ * (SB_ROPE_INTERLEAVED). Rotated queries go to q_out (which may be q), rotated
+ * keys and the values to slot slots[t] of the caches. A token whose slot lies
+ * outside the cache is skipped: its q_out row stays as it was. Two tokens of
+ * one slot leave either's key and value there. */
+enum { SB_ROPE_HALF = 0, SB_ROPE_INTERLEAVED = 1 };
+typedef struct {
+  int64_t struct_bytes;     /* sizeof(sb_rope_args)                                 */
+  const void *q, *k, *v;    /* [n_tokens][q_heads | kv_heads][head_dim]             */
+  void *q_out;              /* [n_tokens][q_heads][head_dim]                        */
+  void *k_cache, *v_cache;  /* [n_pages][page_size][kv_heads][head_dim]             */
+  const int32_t *positions; /* [n_tokens]                                           */
+  const int64_t *slots;     /* [n_tokens]                                           */
+  const double *inv_freq;   /* [n_pairs] radians per position                       */
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;   /* strides */
+  int64_t kc_page, kc_slot, kc_head, vc_page, vc_slot, vc_head;
+  int32_t n_tokens;         /* >= 0                                                 */
+  int32_t q_heads, kv_heads;/* 1 .. 1024                                            */
+  int32_t head_dim;         /* a multiple of 8, up to 512                           */
+  int32_t n_pairs;          /* a multiple of 8 (half) or 4 (interleaved), >= 0      */
+  int32_t layout;
+  int32_t dtype;            /* SB_BF16 or SB_F16                                    */
+  int32_t n_pages, page_size;
+  float mscale;
+} sb_rope_args;
+sb_status sb_rope_append(const sb_rope_args *args, void *stream);
+
+/* Causal attention of new tokens over their request's paged cache:
+ *   out[t] = sum_j softmax_j(scale q[t] . k_j) v_j
+ * for query t of request b (q_start[b] <= t < q_start[b + 1], its m = q_start[b +
+ * 1] - q_start[b] queries being the request's last m positions, position
+ * p = lens[b] - q_start[b + 1] + t) over the keys j <= p that the window leaves:
+ * j > p - window, or j < sinks (window 0: all). Query head h reads key/value head
+ * h / (q_heads / kv_heads). A query with p < 0 gets 0; so does one whose keys all
+ * lie in pages outside the cache, which are skipped. Rows of out behind
+ * q_start[n_requests] stay as they were. fp32 scores, statistics and sums; the
+ * weights are rounded to the cache's type for the product with the values.
+ * max_q and max_kv (upper bounds of a request's queries and of lens) choose the
+ * kernels and the split of long caches: where they are too small the result is
+ * right all the same, only slower. The workspace holds the parts of split
+ * caches; calls that may run at the same time need one each. */
+typedef struct {
+  int64_t struct_bytes;     /* sizeof(sb_attention_args)                            */
+  const void *q;            /* [n_tokens][q_heads][head_dim]                        */
+  const void *k_cache, *v_cache;
+  const int32_t *table;     /* [n_requests][table_stride]                           */
+  const int32_t *lens;      /* [n_requests] tokens cached, the new ones included    */
+  const int32_t *q_start;   /* [n_requests + 1], ascending from 0                   */
+  void *out;                /* [n_tokens][q_heads][head_dim]; not q                 */
+  int64_t q_token, q_head, out_token, out_head, kc_page, kc_slot, kc_head, vc_page, vc_slot, vc_head, table_stride;
+  int32_t n_tokens;         /* rows of q and out                                    */
+  int32_t n_requests;       /* >= 1                                                 */
+  int32_t q_heads, kv_heads;/* 1 .. 1024, q_heads a multiple of kv_heads            */
+  int32_t head_dim;         /* 64, 128 or 256                                       */
+  int32_t dtype;            /* SB_BF16 or SB_F16                                    */
+  int32_t n_pages, page_size, max_pages;
+  int32_t window, sinks;    /* >= 0                                                 */
+  int32_t max_q, max_kv;    /* >= 0                                                 */
+  float scale;
+} sb_attention_args;
+/* Bytes of workspace sb_paged_attention needs on the current device for these
+ * sizes (pointers are not looked at); -1 if they are invalid. */
+int64_t sb_attention_workspace(const sb_attention_args *args);
+/* workspace: 256-byte aligned, at least sb_attention_workspace bytes (NULL
+ * where that is 0). */
+sb_status sb_paged_attention(const sb_attention_args *args, void *workspace, size_t bytes, void *stream);
+
+/* One token per row of logits, drawn with the row's number u. With
+ * w_i = exp((z_i - max z) / temperature), tokens ranked by (-z_i, i):
+ *   top_k  keeps ranks below k (k <= 0 or k >= vocab: all);
+ *   top_p  then keeps a token where the weights ranked before it total less
+ *          than p times what top_k kept (p >= 1 or NaN: all; the first stays);
+ *   min_p  then keeps w_i >= p (p <= 0 or NaN: all; p > 1 counts as 1);
+ * the token is the smallest kept i whose weights up to i total more than u
+ * times the kept ones (u is taken into [0, 1), the last kept one at 1). With
+ * temperature <= 0 or NaN it is the largest logit, of equal ones the first.
+ * logprobs: ln of the drawn token's share of the kept weights. Logits -inf and
+ * NaN are never drawn; those of +inf share the draw evenly; a row with nothing
+ * to draw gives token -1 and -inf. Weights are whole multiples of 2^-44 (of the
+ * row's largest), summed as integers: the result does not depend on the order
+ * of sums, and a token more than 44 powers of two below the largest is not
+ * drawn. */
+typedef struct {
+  int64_t struct_bytes;     /* sizeof(sb_sample_args)                               */
+  const void *logits;       /* [rows][row_stride], the first vocab of each row      */
+  const float *u;           /* [rows] in [0, 1)                                     */
+  const float *temperature; /* [rows], or NULL: 1                                   */
+  const int32_t *top_k;     /* [rows], or NULL: all                                 */
+  const float *top_p;       /* [rows], or NULL: all                                 */
+  const float *min_p;       /* [rows], or NULL: all                                 */
+  int32_t *tokens;          /* [rows]                                               */
+  float *logprobs;          /* [rows], or NULL                                      */
+  int64_t row_stride;       /* elements                                             */
+  int32_t rows;             /* >= 0                                                 */
+  int32_t vocab;            /* 1 .. SB_SAMPLE_MAX_VOCAB                             */
+  int32_t dtype;            /* SB_F32, SB_BF16 or SB_F16                            */
+  int32_t reserved;         /* 0                                                    */
+} sb_sample_args;
+#define SB_SAMPLE_MAX_VOCAB 262144
+sb_status sb_sample_tokens(const sb_sample_args *args, void *stream);
 
 /* ------------------------------------------------------------------------
  * Test support. Not part of the decoding interface: these calls expose one

@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import struct
 import numpy as np
 from ctypes import POINTER, c_char_p, c_double, c_int32, c_int64, c_size_t, c_uint16, c_void_p
 
@@ -23,7 +24,9 @@ SB_OK, SB_E_INVALID_ARG, SB_E_WORKSPACE, SB_E_STATE, SB_E_QUEUE_FULL, SB_E_TRUNC
     SB_E_HIP, SB_E_UNSUPPORTED = range(8)
 SB_FIXED, SB_VAR_BATCH, SB_VAR_STREAM, SB_VAR_FIFO, SB_FIXED_STREAM, SB_VAR_CAP = 0, 1, 2, 3, 4, 5
 SB_RULE_PAPER, SB_RULE_FAIRSEQ = 0, 1
-SB_F32, SB_BF16 = 0, 1
+SB_F32, SB_BF16, SB_F16 = 0, 1, 2
+SB_ROPE_HALF, SB_ROPE_INTERLEAVED = 0, 1
+SB_PLAN_MAX_REQUESTS, SB_SAMPLE_MAX_VOCAB = 8192, 262144
 SCHEDULERS = {"fixed": SB_FIXED, "var_batch": SB_VAR_BATCH, "var_stream": SB_VAR_STREAM,
               "var_fifo": SB_VAR_FIFO, "fixed_stream": SB_FIXED_STREAM, "var_cap": SB_VAR_CAP}
 # Scheduler names that also pick the Fairseq finalization rule.
@@ -58,6 +61,15 @@ class SbStats(ctypes.Structure):
     _fields_ = [("timesteps", c_int64), ("expansions", c_int64), ("noops", c_int64),
                 ("refills", c_int64), ("admitted", c_int64), ("hyps", c_int64), ("finished", c_int64),
                 ("positions", c_int64), ("tile_recomputes", c_int64)]
+
+
+# Arguments of the serving calls, in the order of their structs' fields
+# (struct_bytes first): packed rather than kept as ctypes structures, whose
+# assignments take longer than a single-token call.
+PLAN_ARGS = struct.Struct("q11Pq6i")
+ROPE_ARGS = struct.Struct("q9P14q9if")
+ATTENTION_ARGS = struct.Struct("q7P11q13if")
+SAMPLE_ARGS = struct.Struct("q8Pq4i")
 
 
 class StreambeamError(RuntimeError):
@@ -104,6 +116,11 @@ def lib():
                                       c_void_p, P(c_double), P(c_double), P(c_int32)]),
         "sb_debug_slot": (c_int32, [c_void_p, c_int32, c_int32, P(c_int32), P(c_double), P(c_int64),
                                     P(c_int32), P(c_int32), c_int32, P(c_int32), P(c_uint16), c_int64]),
+        "sb_plan_pages": (c_int32, [c_char_p, c_void_p]),
+        "sb_rope_append": (c_int32, [c_char_p, c_void_p]),
+        "sb_attention_workspace": (c_int64, [c_char_p]),
+        "sb_paged_attention": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
+        "sb_sample_tokens": (c_int32, [c_char_p, c_void_p]),
         "sb_destroy": (c_int32, [c_void_p]),
         "sb_last_error": (c_char_p, [c_void_p]),
         "sb_status_string": (c_char_p, [c_int32]),

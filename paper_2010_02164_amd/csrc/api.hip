@@ -12,6 +12,7 @@
 
 #include "../../include/streambeam.h"
 #include "sb_internal.h"
+#include "serve.h"
 #include "topk.h"
 
 using namespace sb;
@@ -374,6 +375,8 @@ void set_create_err(const char *msg) {
 }
 
 }  // namespace
+
+void sb::set_call_error(const char *msg) { set_create_err(msg); }
 
 extern "C" {
 

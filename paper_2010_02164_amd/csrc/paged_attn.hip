@@ -1,0 +1,581 @@
+// Causal attention of new tokens over a paged cache, grouped heads, with an
+// optional sliding window and first tokens that stay visible.
+//
+// The q_heads / kv_heads = G query heads of one key/value head and the
+// request's m queries are G m rows over the same keys (row i G + g: query i,
+// head g of the group), so one pass over the keys serves them all. Scores are
+// taken transposed, S^T = K Q^T: a lane then holds scores of one row only, the
+// running maximum and sum of its softmax are one register each, and its
+// weights lie just as the second product O^T = V^T P^T wants its right operand
+// (the keys of a product may come in any order, as long as both operands have
+// the same). V^T is read from row-major V in LDS with the transposing read.
+//
+// k_attn_few: up to 16 rows (single tokens); bound by reading the cache. A
+// wave takes 32 keys at a time by itself, the keys of a request are split over
+// the four waves of a workgroup and over workgroups, and k_attn_join adds the
+// parts. k_attn_many: 128 rows a workgroup (prompts), 64 keys at a time in
+// LDS; bound by the matrix products and the exponentials between them.
+#include <algorithm>
+
+#include "serve.h"
+
+namespace sb {
+namespace {
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef unsigned int u4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u2 __attribute__((ext_vector_type(2)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+
+constexpr int FEW_ROWS = 16, FEW_KEYS = 32;
+constexpr int MANY_ROWS = 128, MANY_KEYS = 64;
+constexpr int AT_THREADS = 256, AT_WAVES = 4;
+constexpr double LOG2E = 1.4426950408889634074;
+
+template <int DT>
+__device__ __forceinline__ f4 mfma16(const u4 &x, const u4 &y, const f4 &c) {
+  typedef typename Half<DT>::v8 v8;
+  if constexpr (DT == SB_BF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, x), __builtin_bit_cast(v8, y), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, x), __builtin_bit_cast(v8, y), c, 0, 0, 0);
+}
+template <int DT>
+__device__ __forceinline__ f16v mfma32(const u4 &x, const u4 &y, const f16v &c) {
+  typedef typename Half<DT>::v8 v8;
+  if constexpr (DT == SB_BF16)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8, x), __builtin_bit_cast(v8, y), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8, x), __builtin_bit_cast(v8, y), c, 0, 0, 0);
+}
+
+// Four rows of 16 values each, transposed: lane l of each 16 lanes points at
+// row l / 4, values 4 (l % 4) .. + 3, and gets value l of the four rows.
+__device__ __forceinline__ u2 read_transposed(const unsigned char *p) {
+  const s4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(p));
+  return __builtin_bit_cast(u2, v);
+}
+
+// Orders a wave's own LDS writes before its later reads by other lanes.
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Eight values with NaN and infinities as 0; `bad` if there were any.
+template <int DT>
+__device__ __forceinline__ u4 finite_only(const u4 &x, bool &bad) {
+  constexpr uint32_t E = DT == SB_BF16 ? 0x7F80u : 0x7C00u;   // exponent bits, all set in NaN and infinities
+  u4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool lo = (x[i] & E) == E, hi = (x[i] & (E << 16)) == (E << 16);
+    y[i] = x[i] & ((lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u));
+    bad |= lo || hi;
+  }
+  return y;
+}
+
+// A hidden key's weight is 0, and 0 times what stands there would be NaN where
+// that is NaN or infinite. In a tile whose keys some rows see and others do
+// not, such values are therefore taken out of V before the matrix product and
+// added by themselves to the rows that give them a weight: w times each of four
+// values that is not finite.
+template <int DT>
+__device__ __forceinline__ f4 not_finite(float w, const unsigned char *v) {
+  const u2 x = *reinterpret_cast<const u2 *>(v);
+  f4 y;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float f = Half<DT>::to_float(j & 1 ? x[j >> 1] >> 16 : x[j >> 1] & 0xFFFFu);
+    y[j] = w != 0.0f && !(fabsf(f) < INFINITY) ? w * f : 0.0f;
+  }
+  return y;
+}
+
+// The rows and keys of one workgroup's pass. The keys its rows see are the
+// first `ns` of the request and those from `lo` on, n_vis in all.
+struct Span {
+  int q0, m, n;      // first query, queries and cached tokens of the request
+  int rows, r0;      // G m, first row of this pass
+  int ns, lo, n_vis;
+  int p_first, p_last;   // positions of the first and last of these rows
+  __device__ __forceinline__ int key(int u) const { return u < ns ? u : lo + (u - ns); }
+  // Whether all rows see all keys of a tile from k_first to k_last.
+  __device__ __forceinline__ bool all_see(const sb_attention_args &a, int k_first, int k_last) const {
+    return k_last <= p_first && (a.window == 0 || k_first > p_last - a.window || k_last < a.sinks);
+  }
+};
+
+__device__ __forceinline__ void span_request(const sb_attention_args &a, int b, Span &s) {
+  s.q0 = max(a.q_start[b], 0);
+  s.m = min(a.q_start[b + 1], a.n_tokens) - s.q0;
+  s.n = (int)min((long long)max(a.lens[b], 0), (long long)a.max_pages * a.page_size);
+  s.rows = s.m * (a.q_heads / a.kv_heads);
+}
+
+__device__ __forceinline__ void span_rows(const sb_attention_args &a, int r0, int count, Span &s) {
+  const int G = a.q_heads / a.kv_heads;
+  s.r0 = r0;
+  s.p_first = s.n - s.m + r0 / G;
+  s.p_last = s.n - s.m + min(r0 + count - 1, s.rows - 1) / G;
+  s.lo = a.window > 0 ? max(s.p_first - a.window + 1, 0) : 0;
+  s.ns = min(a.sinks, s.lo);
+  s.n_vis = max(s.p_last + 1 - s.lo + s.ns, 0);
+}
+
+// A key's page, -1 if there is none; `place` within it. (key + 1/2) / size is
+// further from a whole number than the product with the reciprocal is off.
+__device__ __forceinline__ int page_of(const sb_attention_args &a, const int *table, double inv_page, int key, int &place) {
+  const int c = (int)(((double)key + 0.5) * inv_page);
+  place = key - c * a.page_size;
+  const int page = table[c];
+  return (unsigned)page < (unsigned)a.n_pages ? page : -1;
+}
+
+__device__ __forceinline__ bool sees(const sb_attention_args &a, int p, int key) {
+  return key <= p && (a.window == 0 || key > p - a.window || key < a.sinks);
+}
+
+// Parts of a split: sums [splits][n_tokens q_heads][D], then (maximum, sum).
+template <int D>
+__device__ __forceinline__ float *part_sums(const sb_attention_args &a, float *parts, int split, long long row) {
+  return parts + ((long long)split * a.n_tokens * a.q_heads + row) * D;
+}
+template <int D>
+__device__ __forceinline__ float2 *part_stats(const sb_attention_args &a, float *parts, int splits, int split, long long row) {
+  const long long nr = (long long)a.n_tokens * a.q_heads;
+  return reinterpret_cast<float2 *>(parts + splits * nr * D) + split * nr + row;
+}
+
+template <int DT, int D>
+__global__ __launch_bounds__(AT_THREADS) void k_attn_few(sb_attention_args a, int splits, float *parts) {
+  constexpr int VS = 2 * D + 32;            // bytes of a V row in LDS: 8 rows of 32 bytes in different banks
+  constexpr int KS = D / 32, NV = D / 16;   // products per score, 16-byte pieces of V per lane
+  constexpr int DT16 = D / 16;
+  __shared__ alignas(16) unsigned char lds[AT_WAVES][FEW_KEYS * VS];
+  __shared__ float2 stats[AT_WAVES][FEW_ROWS];
+  static_assert(FEW_KEYS * VS >= FEW_ROWS * D * 4, "the waves' sums fit where V was");
+  const int b = blockIdx.x, hk = blockIdx.y, split = blockIdx.z;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g4 = lane >> 4, l16 = lane & 15;
+  const int G = a.q_heads / a.kv_heads;
+  const int *table = a.table + b * a.table_stride;
+  const double inv_page = 1.0 / a.page_size;
+  const float c = (float)(a.scale * LOG2E);
+  const uint16_t *kc = static_cast<const uint16_t *>(a.k_cache) + hk * a.kc_head;
+  const uint16_t *vc = static_cast<const uint16_t *>(a.v_cache) + hk * a.vc_head;
+  Span s;
+  span_request(a, b, s);
+  for (int r0 = 0; r0 < s.rows; r0 += FEW_ROWS) {
+    span_rows(a, r0, FEW_ROWS, s);
+    const int row = r0 + l16, i = row / G, p = s.n - s.m + i;
+    const bool real = row < s.rows;
+    u4 q[KS];
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      const uint16_t *src = static_cast<const uint16_t *>(a.q) + (s.q0 + i) * a.q_token + (hk * G + row - i * G) * a.q_head;
+      q[x] = real ? *reinterpret_cast<const u4 *>(src + 32 * x + 8 * g4) : u4{0, 0, 0, 0};
+    }
+    f4 o[DT16];
+#pragma unroll
+    for (int x = 0; x < DT16; ++x) o[x] = f4{0, 0, 0, 0};
+    float mx = -INFINITY, sum = 0.0f;
+    const int tiles = (s.n_vis + FEW_KEYS - 1) / FEW_KEYS, per = (tiles + splits - 1) / splits;
+    const int t_end = min(tiles, (split + 1) * per);
+    for (int t = split * per + w; t < t_end; t += AT_WAVES) {
+      // Where the tile's keys lie (lane l: key l % 32).
+      const int u = t * FEW_KEYS + (lane & 31);
+      int place = 0;
+      const int page = u < s.n_vis ? page_of(a, table, inv_page, s.key(u), place) : -1;
+      const uint32_t there = (uint32_t)__ballot(page >= 0);
+      const long long ko = page >= 0 ? page * a.kc_page + place * a.kc_slot : 0;
+      const long long vo = page >= 0 ? page * a.vc_page + place * a.vc_slot : -1;
+      u4 k[2][KS], v[NV];
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        const uint16_t *src = kc + __shfl(ko, hf * 16 + l16, 64) + 8 * g4;
+#pragma unroll
+        for (int x = 0; x < KS; ++x) k[hf][x] = *reinterpret_cast<const u4 *>(src + 32 * x);
+      }
+#pragma unroll
+      for (int x = 0; x < NV; ++x) {
+        const int piece = x * 64 + lane, kr = piece / (D / 8);
+        const long long off = __shfl(vo, kr, 64);
+        v[x] = u4{0, 0, 0, 0};
+        if (off >= 0) v[x] = *reinterpret_cast<const u4 *>(vc + off + (piece - kr * (D / 8)) * 8);
+      }
+      const int k_first = s.key(t * FEW_KEYS), k_last = s.key(t * FEW_KEYS + FEW_KEYS - 1);
+      const bool plain = there == 0xFFFFFFFFu && s.all_see(a, k_first, k_last);
+      f4 sc[2] = {f4{0, 0, 0, 0}, f4{0, 0, 0, 0}};
+#pragma unroll
+      for (int x = 0; x < KS; ++x)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) sc[hf] = mfma16<DT>(k[hf][x], q[x], sc[hf]);
+      // Lane: keys 16 hf + 4 g4 + j of row l16.
+      float tm = -INFINITY;
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          sc[hf][j] *= c;
+          if (!plain) {
+            const int at = 16 * hf + 4 * g4 + j;
+            const bool on = real && ((there >> at) & 1u) && sees(a, p, s.key(t * FEW_KEYS + at));
+            sc[hf][j] = on ? sc[hf][j] : -INFINITY;
+          }
+          tm = fmaxf(tm, sc[hf][j]);
+        }
+      tm = fmaxf(tm, __shfl_xor(tm, 16, 64));
+      tm = fmaxf(tm, __shfl_xor(tm, 32, 64));
+      const float mn = fmaxf(mx, tm), base = mn == -INFINITY ? 0.0f : mn;
+      const float shrink = __builtin_amdgcn_exp2f(mx - base);
+      mx = mn;
+      float ts = 0.0f;
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          sc[hf][j] = __builtin_amdgcn_exp2f(sc[hf][j] - base);
+          ts += sc[hf][j];
+        }
+      sum = sum * shrink + ts;   // this lane's keys only; added up at the end
+      const u4 pk = {Half<DT>::pack(sc[0][0], sc[0][1]), Half<DT>::pack(sc[0][2], sc[0][3]),
+                     Half<DT>::pack(sc[1][0], sc[1][1]), Half<DT>::pack(sc[1][2], sc[1][3])};
+      auto put = [&] {
+#pragma unroll
+        for (int x = 0; x < NV; ++x) {
+          const int piece = x * 64 + lane, kr = piece / (D / 8);
+          *reinterpret_cast<u4 *>(&lds[w][kr * VS + (piece - kr * (D / 8)) * 16]) = v[x];
+        }
+        wave_lds_fence();
+      };
+      put();
+      f4 extra[DT16];
+      bool careful = false;
+      if (!plain) {
+        bool bad = false;
+        u4 vf[NV];
+#pragma unroll
+        for (int x = 0; x < NV; ++x) vf[x] = finite_only<DT>(v[x], bad);
+        careful = __any(bad);
+        if (careful) {
+#pragma unroll
+          for (int x = 0; x < DT16; ++x) extra[x] = f4{0, 0, 0, 0};
+          for (int kk = 0; kk < FEW_KEYS; ++kk) {
+            float wt = sc[0][0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) wt = e == (kk >> 4) * 4 + (kk & 3) ? sc[e >> 2][e & 3] : wt;
+            wt = __shfl(wt, ((kk & 15) >> 2) * 16 + l16, 64);
+#pragma unroll
+            for (int x = 0; x < DT16; ++x) extra[x] += not_finite<DT>(wt, &lds[w][kk * VS + 32 * x + 8 * g4]);
+          }
+          wave_lds_fence();
+#pragma unroll
+          for (int x = 0; x < NV; ++x) v[x] = vf[x];
+          put();
+        }
+      }
+      const unsigned char *vt = &lds[w][(4 * g4 + (l16 >> 2)) * VS + (l16 & 3) * 8];
+#pragma unroll
+      for (int x = 0; x < DT16; ++x) {
+        const u2 v0 = read_transposed(vt + 32 * x), v1 = read_transposed(vt + 16 * VS + 32 * x);
+        o[x] = mfma16<DT>(u4{v0[0], v0[1], v1[0], v1[1]}, pk, o[x] * shrink);
+      }
+      if (careful) {
+#pragma unroll
+        for (int x = 0; x < DT16; ++x) o[x] += extra[x];
+      }
+      wave_lds_fence();
+    }
+    sum += __shfl_xor(sum, 16, 64);
+    sum += __shfl_xor(sum, 32, 64);
+    // The four waves' parts: sums side by side where V was.
+    float *os = reinterpret_cast<float *>(&lds[w][0]);
+#pragma unroll
+    for (int x = 0; x < DT16; ++x) *reinterpret_cast<f4 *>(os + l16 * D + 16 * x + 4 * g4) = o[x];
+    if (g4 == 0) stats[w][l16] = make_float2(mx, sum);
+    __syncthreads();
+    for (int e = threadIdx.x; e < FEW_ROWS * D / 4; e += AT_THREADS) {
+      const int rr = e / (D / 4), col = (e - rr * (D / 4)) * 4, rw = r0 + rr;
+      if (rw >= s.rows) continue;
+      float m4 = -INFINITY;
+#pragma unroll
+      for (int x = 0; x < AT_WAVES; ++x) m4 = fmaxf(m4, stats[x][rr].x);
+      const float base = m4 == -INFINITY ? 0.0f : m4;
+      float l4 = 0.0f;
+      f4 acc = {0, 0, 0, 0};
+#pragma unroll
+      for (int x = 0; x < AT_WAVES; ++x) {
+        const float f = __builtin_amdgcn_exp2f(stats[x][rr].x - base);
+        l4 += f * stats[x][rr].y;
+        acc += f * *reinterpret_cast<const f4 *>(reinterpret_cast<const float *>(&lds[x][0]) + rr * D + col);
+      }
+      const int qi = rw / G, tok = s.q0 + qi, h = hk * G + rw - qi * G;
+      if (splits == 1) {
+        const float inv = l4 == 0.0f ? 0.0f : 1.0f / l4;
+        uint16_t *dst = static_cast<uint16_t *>(a.out) + tok * a.out_token + h * a.out_head + col;
+        *reinterpret_cast<u2 *>(dst) = u2{Half<DT>::pack(acc[0] * inv, acc[1] * inv), Half<DT>::pack(acc[2] * inv, acc[3] * inv)};
+      } else {
+        const long long pr = (long long)tok * a.q_heads + h;
+        *reinterpret_cast<f4 *>(part_sums<D>(a, parts, split, pr) + col) = acc;
+        if (col == 0) *part_stats<D>(a, parts, splits, split, pr) = make_float2(m4, l4);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// One wave per row: parts with a share in the row, added in order.
+template <int DT, int D>
+__global__ __launch_bounds__(AT_THREADS) void k_attn_join(sb_attention_args a, int splits, float *parts) {
+  const int lane = threadIdx.x & 63;
+  const long long row = (long long)blockIdx.x * AT_WAVES + (threadIdx.x >> 6);
+  const long long rows = (long long)min(a.q_start[a.n_requests], a.n_tokens) * a.q_heads;
+  if (row >= rows) return;
+  float mx = -INFINITY;
+  for (int s = 0; s < splits; ++s) mx = fmaxf(mx, part_stats<D>(a, parts, splits, s, row)->x);
+  const float base = mx == -INFINITY ? 0.0f : mx;
+  constexpr int E = D / 64;
+  float acc[E], sum = 0.0f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+  for (int s = 0; s < splits; ++s) {
+    const float2 st = *part_stats<D>(a, parts, splits, s, row);
+    if (st.x == -INFINITY) continue;   // nothing seen there
+    const float f = __builtin_amdgcn_exp2f(st.x - base);
+    sum += f * st.y;
+    const float *src = part_sums<D>(a, parts, s, row) + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] += f * src[e];
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  const long long tok = row / a.q_heads;
+  const int h = (int)(row - tok * a.q_heads);
+  uint16_t *dst = static_cast<uint16_t *>(a.out) + tok * a.out_token + h * a.out_head + lane * E;
+  if constexpr (E == 1) {
+    *dst = (uint16_t)Half<DT>::pack(acc[0] * inv, 0.0f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t *>(dst + e) = Half<DT>::pack(acc[e] * inv, acc[e + 1] * inv);
+  }
+}
+
+template <int DT, int D>
+__global__ __launch_bounds__(AT_THREADS) void k_attn_many(sb_attention_args a) {
+  constexpr int KSTR = 2 * D + 16, VSTR = 2 * D + 32;   // bytes of a K and a V row in LDS
+  constexpr int PC = MANY_KEYS * (D / 8) / AT_THREADS;  // 16-byte pieces of K (and V) a thread brings
+  constexpr int KS = D / 16, DB = D / 32;
+  __shared__ alignas(16) unsigned char lk[MANY_KEYS * KSTR];
+  __shared__ alignas(16) unsigned char lv[MANY_KEYS * VSTR];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, h2 = lane >> 5;
+  const int G = a.q_heads / a.kv_heads, hk = blockIdx.y;
+  // The request of this tile: request b's tiles start at q_start[b] G / 128 + b,
+  // which leaves at least one place a tile; the last ones of some stay empty.
+  const int tile = (int)(gridDim.x - 1 - blockIdx.x);
+  int b = 0, bh = a.n_requests;
+  while (bh - b > 1) {
+    const int mid = (b + bh) >> 1;
+    if ((long long)a.q_start[mid] * G / MANY_ROWS + mid <= tile) b = mid;
+    else bh = mid;
+  }
+  Span s;
+  span_request(a, b, s);
+  const int r0 = (int)(tile - ((long long)a.q_start[b] * G / MANY_ROWS + b)) * MANY_ROWS;
+  if (r0 < 0 || r0 >= s.rows) return;
+  span_rows(a, r0, MANY_ROWS, s);
+  const int *table = a.table + b * a.table_stride;
+  const double inv_page = 1.0 / a.page_size;
+  const float c = (float)(a.scale * LOG2E);
+  const uint16_t *kc = static_cast<const uint16_t *>(a.k_cache) + hk * a.kc_head;
+  const uint16_t *vc = static_cast<const uint16_t *>(a.v_cache) + hk * a.vc_head;
+
+  const int row = r0 + 32 * w + l32, i = row / G, p = s.n - s.m + i;
+  const bool real = row < s.rows;
+  u4 q[KS];
+#pragma unroll
+  for (int x = 0; x < KS; ++x) {
+    const uint16_t *src = static_cast<const uint16_t *>(a.q) + (s.q0 + i) * a.q_token + (hk * G + row - i * G) * a.q_head;
+    q[x] = real ? *reinterpret_cast<const u4 *>(src + 16 * x + 8 * h2) : u4{0, 0, 0, 0};
+  }
+  f16v o[DB];
+#pragma unroll
+  for (int x = 0; x < DB; ++x)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[x][e] = 0.0f;
+  float mx = -INFINITY, sum = 0.0f;
+
+  u4 kr[PC], vr[PC];
+  __shared__ uint32_t there[2][2];   // [parity][half]: keys of the tile that have a page
+  __shared__ int not_fin[2];         // [parity]: V of a tile that not all rows see has values that are not finite
+  if (threadIdx.x < 2) not_fin[threadIdx.x] = 0;
+  __syncthreads();
+  const int tiles = (s.n_vis + MANY_KEYS - 1) / MANY_KEYS;
+  auto bring = [&](int t) {
+#pragma unroll
+    for (int x = 0; x < PC; ++x) {
+      const int piece = x * AT_THREADS + threadIdx.x, kk = piece / (D / 8), col = (piece - kk * (D / 8)) * 8;
+      const int u = t * MANY_KEYS + kk;
+      int place = 0;
+      const int page = u < s.n_vis ? page_of(a, table, inv_page, s.key(u), place) : -1;
+      kr[x] = vr[x] = u4{0, 0, 0, 0};
+      if (page >= 0) {
+        kr[x] = *reinterpret_cast<const u4 *>(kc + page * a.kc_page + place * a.kc_slot + col);
+        vr[x] = *reinterpret_cast<const u4 *>(vc + page * a.vc_page + place * a.vc_slot + col);
+      }
+    }
+    if (threadIdx.x < MANY_KEYS) {
+      const int u = t * MANY_KEYS + threadIdx.x;
+      int place = 0;
+      const unsigned long long m = __ballot(u < s.n_vis && page_of(a, table, inv_page, s.key(u), place) >= 0);
+      if (threadIdx.x < 2) there[t & 1][threadIdx.x] = (uint32_t)(m >> (32 * threadIdx.x));
+    }
+  };
+  if (tiles > 0) bring(0);
+  for (int t = 0; t < tiles; ++t) {
+    const int u0 = t * MANY_KEYS;
+    const bool shared = s.all_see(a, s.key(u0), s.key(u0 + MANY_KEYS - 1));
+    bool bad = false;
+#pragma unroll
+    for (int x = 0; x < PC; ++x) {
+      const int piece = x * AT_THREADS + threadIdx.x, kk = piece / (D / 8), col = (piece - kk * (D / 8)) * 16;
+      *reinterpret_cast<u4 *>(&lk[kk * KSTR + col]) = kr[x];
+      *reinterpret_cast<u4 *>(&lv[kk * VSTR + col]) = vr[x];
+      if (!shared) finite_only<DT>(vr[x], bad);
+    }
+    if (bad) not_fin[t & 1] = 1;
+    __syncthreads();
+    const uint32_t on0 = there[t & 1][0], on1 = there[t & 1][1];
+    const bool careful = not_fin[t & 1];
+    if (threadIdx.x == 0) not_fin[(t + 1) & 1] = 0;
+    if (t + 1 < tiles) bring(t + 1);
+    f16v sc[2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[kb][e] = 0.0f;
+#pragma unroll
+      for (int x = 0; x < KS; ++x) {
+        const u4 kf = *reinterpret_cast<const u4 *>(&lk[(32 * kb + l32) * KSTR + 32 * x + 16 * h2]);
+        sc[kb] = mfma32<DT>(kf, q[x], sc[kb]);
+      }
+    }
+    // Lane: keys 32 kb + 8 (e / 4) + 4 h2 + e % 4 of row l32.
+    const bool plain = (on0 & on1) == 0xFFFFFFFFu && shared;
+    float tm = -INFINITY;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int at = 8 * (e >> 2) + 4 * h2 + (e & 3);
+        float x = sc[kb][e] * c;
+        if (!plain) {
+          const bool on = real && (((kb ? on1 : on0) >> at) & 1u) && sees(a, p, s.key(u0 + 32 * kb + at));
+          x = on ? x : -INFINITY;
+        }
+        sc[kb][e] = x;
+        tm = fmaxf(tm, x);
+      }
+    tm = fmaxf(tm, __shfl_xor(tm, 32, 64));
+    const float mn = fmaxf(mx, tm), base = mn == -INFINITY ? 0.0f : mn;
+    const float shrink = __builtin_amdgcn_exp2f(mx - base);
+    mx = mn;
+    float ts = 0.0f;
+    u4 pk[4];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        const float x = __builtin_amdgcn_exp2f(sc[kb][e] - base), y = __builtin_amdgcn_exp2f(sc[kb][e + 1] - base);
+        ts += x + y;
+        pk[2 * kb + (e >> 3)][(e & 7) >> 1] = Half<DT>::pack(x, y);
+      }
+    sum = sum * shrink + ts;
+#pragma unroll
+    for (int x = 0; x < DB; ++x) o[x] *= shrink;
+    if (careful) {
+      for (int kk = 0; kk < MANY_KEYS; ++kk) {
+        const int e = ((kk >> 3) & 1) * 4 + (kk & 3), from = (kk >> 2) & 1;
+        uint32_t code = 0;
+#pragma unroll
+        for (int x = 0; x < 16; ++x) code = x == (kk >> 4) * 4 + (e >> 1) ? pk[x >> 2][x & 3] : code;
+        const float wt = __shfl(Half<DT>::to_float(e & 1 ? code >> 16 : code & 0xFFFFu), from * 32 + l32, 64);
+#pragma unroll
+        for (int x = 0; x < DB; ++x)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const f4 z = not_finite<DT>(wt, &lv[kk * VSTR + 64 * x + 16 * y + 8 * h2]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[x][4 * y + j] += z[j];
+          }
+      }
+      __syncthreads();
+      for (int piece = threadIdx.x; piece < MANY_KEYS * (D / 8); piece += AT_THREADS) {
+        u4 *at = reinterpret_cast<u4 *>(&lv[piece / (D / 8) * VSTR + piece % (D / 8) * 16]);
+        *at = finite_only<DT>(*at, bad);
+      }
+      __syncthreads();
+    }
+    const unsigned char *vt = &lv[(4 * h2 + ((lane & 15) >> 2)) * VSTR + ((lane >> 4) & 1) * 32 + (lane & 3) * 8];
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int x = 0; x < DB; ++x) {
+        const u2 v0 = read_transposed(vt + 16 * ks * VSTR + 64 * x), v1 = read_transposed(vt + (16 * ks + 8) * VSTR + 64 * x);
+        o[x] = mfma32<DT>(u4{v0[0], v0[1], v1[0], v1[1]}, pk[ks], o[x]);
+      }
+    __syncthreads();
+  }
+  sum += __shfl_xor(sum, 32, 64);
+  if (!real) return;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  uint16_t *dst = static_cast<uint16_t *>(a.out) + (s.q0 + i) * a.out_token + (hk * G + row - i * G) * a.out_head;
+#pragma unroll
+  for (int x = 0; x < DB; ++x)
+#pragma unroll
+    for (int e = 0; e < 16; e += 4)
+      *reinterpret_cast<u2 *>(dst + 32 * x + 2 * e + 4 * h2) =
+          u2{Half<DT>::pack(o[x][e] * inv, o[x][e + 1] * inv), Half<DT>::pack(o[x][e + 2] * inv, o[x][e + 3] * inv)};
+}
+
+// Prompts go to k_attn_many, which keeps 128 rows on its keys; a few rows
+// would leave most of its products empty.
+bool many(const sb_attention_args &a) { return (long long)a.max_q * (a.q_heads / a.kv_heads) > 3 * FEW_ROWS; }
+
+template <int DT, int D>
+hipError_t launch(const sb_attention_args &a, int splits, float *parts, hipStream_t s) {
+  if (many(a)) {
+    const long long gx = (long long)a.n_tokens * (a.q_heads / a.kv_heads) / MANY_ROWS + a.n_requests;
+    hipLaunchKernelGGL((k_attn_many<DT, D>), dim3((unsigned)gx, a.kv_heads), dim3(AT_THREADS), 0, s, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((k_attn_few<DT, D>), dim3(a.n_requests, a.kv_heads, splits), dim3(AT_THREADS), 0, s, a, splits, parts);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || splits == 1) return e;
+  const long long rows = (long long)a.n_tokens * a.q_heads;
+  hipLaunchKernelGGL((k_attn_join<DT, D>), dim3((unsigned)((rows + AT_WAVES - 1) / AT_WAVES)), dim3(AT_THREADS), 0, s, a, splits, parts);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int attention_splits(const sb_attention_args &a, int n_cu) {
+  if (many(a)) return 1;
+  const long long seen = a.window > 0 ? std::min((long long)a.max_kv, (long long)a.window + a.sinks + a.max_q) : a.max_kv;
+  const long long want = (4LL * n_cu + (long long)a.n_requests * a.kv_heads - 1) / ((long long)a.n_requests * a.kv_heads);
+  return (int)std::max(1LL, std::min({want, (seen + 255) / 256, 64LL}));
+}
+
+hipError_t launch_paged_attention(const sb_attention_args &a, int splits, float *parts, hipStream_t s) {
+  if (a.n_tokens == 0) return hipSuccess;
+  if (a.dtype == SB_BF16) {
+    if (a.head_dim == 64) return launch<SB_BF16, 64>(a, splits, parts, s);
+    if (a.head_dim == 128) return launch<SB_BF16, 128>(a, splits, parts, s);
+    return launch<SB_BF16, 256>(a, splits, parts, s);
+  }
+  if (a.head_dim == 64) return launch<SB_F16, 64>(a, splits, parts, s);
+  if (a.head_dim == 128) return launch<SB_F16, 128>(a, splits, parts, s);
+  return launch<SB_F16, 256>(a, splits, parts, s);
+}
+
+}  // namespace sb

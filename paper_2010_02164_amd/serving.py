@@ -1,0 +1,295 @@
+"""Operators of a serving step: paged caches, rotary positions, attention with
+a sliding window and sinks, sampled tokens.
+
+A step of a cached decoder takes them in this order: plan_pages finds pages
+and slots for the step's new tokens, rope_append turns their queries and keys
+and writes keys and values to the slots (per layer), paged_attention reads
+the cache (per layer), sample_tokens draws the next token of every request.
+Each is one call of the C ABI (include/streambeam.h, which defines what it
+computes) on torch's current stream of its tensors' device; nothing waits,
+and every call can be captured into a graph. There are no backward passes.
+"""
+from __future__ import annotations
+
+import math
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import _native as N
+
+_HALVES = {torch.bfloat16: N.SB_BF16, torch.float16: N.SB_F16}
+_LOGITS = {torch.float32: N.SB_F32, **_HALVES}
+_LAYOUTS = {"half": N.SB_ROPE_HALF, "interleaved": N.SB_ROPE_INTERLEAVED}
+
+
+def _refuse(what):
+    raise ValueError(what)
+
+
+def _check(status: int, where: str):
+    if status != N.SB_OK:
+        msg = N.lib().sb_last_error(None)
+        raise N.StreambeamError(status, where, msg.decode() if msg else "")
+
+
+def _call(fn, where, dev, *args):
+    """fn(*args, stream) on the tensors' device and its current stream."""
+    stream = torch.cuda.current_stream(dev).cuda_stream
+    if dev.index == torch.cuda.current_device():
+        status = fn(*args, stream)
+    else:
+        with torch.cuda.device(dev):
+            status = fn(*args, stream)
+    if status != N.SB_OK:
+        _check(status, where)
+
+
+def _whole(t, name, dtype, dev, shape):
+    """A contiguous array of whole numbers or parameters."""
+    if t.dtype != dtype or t.device != dev or t.shape != shape or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
+    return t.data_ptr()
+
+
+def _apart(t, name):
+    """A tensor that is written: no two of its elements in one place."""
+    if not t.is_contiguous():
+        span = 1
+        for stride, size in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n > 1):
+            if stride < span:
+                _refuse(f"{name} is written and its elements overlap")
+            span = stride * (size - 1) + span
+    return t
+
+
+def _no_grad(*tensors):
+    if torch.is_grad_enabled() and any(t.requires_grad for t in tensors):
+        _refuse("there is no backward pass: call it under torch.no_grad()")
+
+
+def _device(t, name):
+    if not t.is_cuda:
+        _refuse(f"{name} must be on a GPU")
+    return t.device
+
+
+def _heads(t, name, dtype, dev, tokens=None, dim=None):
+    if t.dim() != 3 or t.dtype != dtype or t.device != dev or (t.shape[2] > 1 and t.stride(2) != 1):
+        _refuse(f"{name} must be a {dtype} tensor [tokens, heads, head_dim] on {dev} with contiguous heads")
+    if (tokens is not None and t.shape[0] != tokens) or (dim is not None and t.shape[2] != dim):
+        _refuse(f"{name} has another number of tokens or another head_dim")
+
+
+def _caches(k_cache, v_cache, dtype, dev, heads, dim):
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        if t.dim() != 4 or t.dtype != dtype or t.device != dev or t.stride(3) != 1:
+            _refuse(f"{name} must be a {dtype} tensor [pages, page_size, heads, head_dim] on {dev} with contiguous heads")
+    if k_cache.shape != v_cache.shape or k_cache.shape[3] != dim or (heads is not None and k_cache.shape[2] != heads):
+        _refuse("the caches must have one shape, with the keys' heads and head_dim")
+
+
+class PagePlan(NamedTuple):
+    """What plan_pages found. lens and n_free are the new state: give them to
+    the next call."""
+    q_start: torch.Tensor     # [requests + 1] int32: request b's new tokens are rows q_start[b] .. q_start[b + 1]
+    lens: torch.Tensor        # [requests] int32: tokens cached, the granted ones included
+    granted: torch.Tensor     # [requests] int32: new tokens granted
+    slots: torch.Tensor       # [token_cap] int64: cache slot of each new token, -1 behind the last
+    positions: torch.Tensor   # [token_cap] int32: its position in its request, -1 behind the last
+    n_free: torch.Tensor      # [1] int32: pages on the free list
+
+
+def plan_pages(lens, add, free_list, n_free, table, *, page_size: int, token_cap: int, out: Optional[PagePlan] = None) -> PagePlan:
+    """Pages, slots and positions of a step's new tokens, from the requests'
+    lengths (sb_plan_pages).
+
+    lens, add: int32 [requests] (add: new tokens wanted, 0 none, negative
+    releases the request); free_list: int32 [pages], its first n_free (int32
+    [1]) entries free page ids; table: int32 [requests, max_pages]. table and
+    free_list are updated in place, the rest of the new state is returned, in
+    new tensors or in `out`'s, which may be lens and n_free themselves. token_cap:
+    the most tokens a step takes."""
+    dev = _device(lens, "lens")
+    if lens.dim() != 1 or table.dim() != 2 or table.dtype != torch.int32 or table.device != dev or (table.shape[1] > 1 and table.stride(1) != 1):
+        _refuse(f"table must be an int32 tensor [requests, max_pages] on {dev} with contiguous rows")
+    B, width, cap = lens.shape[0], table.shape[1], int(token_cap)
+    if table.shape[0] != B or free_list.dim() != 1:
+        _refuse("table needs a row per request, free_list one dimension")
+    if cap < 0:
+        _refuse("token_cap must not be negative")
+    _apart(table, "table")
+    i32 = torch.int32
+    if out is None:
+        new = torch.empty(3 * B + 2, dtype=i32, device=dev)   # one allocation for the small ones
+        out = PagePlan(new[:B + 1], new[B + 1:2 * B + 1], new[2 * B + 1:3 * B + 1], torch.empty(cap, dtype=torch.int64, device=dev),
+                       torch.empty(cap, dtype=i32, device=dev), new[3 * B + 1:])
+    args = N.PLAN_ARGS.pack(
+        N.PLAN_ARGS.size, _whole(lens, "lens", i32, dev, (B,)), _whole(add, "add", i32, dev, (B,)),
+        _whole(n_free, "n_free", i32, dev, (1,)), _whole(free_list, "free_list", i32, dev, free_list.shape), table.data_ptr(),
+        _whole(out.lens, "out.lens", i32, dev, (B,)), _whole(out.n_free, "out.n_free", i32, dev, (1,)),
+        _whole(out.q_start, "out.q_start", i32, dev, (B + 1,)), _whole(out.granted, "out.granted", i32, dev, (B,)),
+        _whole(out.slots, "out.slots", torch.int64, dev, (cap,)), _whole(out.positions, "out.positions", i32, dev, (cap,)),
+        table.stride(0) if B > 1 else width, B, free_list.shape[0], int(page_size), width, cap, 0)
+    _call(N.lib().sb_plan_pages, "sb_plan_pages", dev, args)
+    return out
+
+
+def rope_frequencies(rot_dim: int, *, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_length: int = 4096,
+                     beta_fast: float = 32.0, beta_slow: float = 1.0, device="cuda"):
+    """(inv_freq, mscale) of rotary positions over rot_dim values of a head.
+
+    inv_freq[i] = base^(-2i / rot_dim) in float64. For contexts `factor` times
+    as long as the original_length trained on, scaling "linear" divides all by
+    the factor; "ntk" raises the base by factor^(rot_dim / (rot_dim - 2)), which
+    keeps the fastest pair and slows the slowest by the factor; "parts" divides
+    pairs that turn less than beta_slow times over original_length, keeps
+    those that turn more than beta_fast times, blends between, and scales the
+    rotated part by mscale = 1 + ln(factor) / 10 (the YaRN method)."""
+    if rot_dim < 2 or rot_dim % 2 or not base > 1 or not factor >= 1:
+        _refuse("rot_dim must be even and at least 2, base above 1, factor at least 1")
+    i = torch.arange(rot_dim // 2, dtype=torch.float64)
+    mscale = 1.0
+    if scaling == "ntk":
+        if rot_dim > 2:
+            base = base * factor ** (rot_dim / (rot_dim - 2))
+    elif scaling not in ("none", "linear", "parts"):
+        _refuse(f"unknown scaling {scaling!r}")
+    inv = base ** (-2.0 * i / rot_dim)
+    if scaling == "linear":
+        inv = inv / factor
+    elif scaling == "parts":
+        def pair_of(turns):   # the pair (as a real number) that turns so often over original_length
+            return rot_dim * math.log(original_length / (2 * math.pi * turns)) / (2 * math.log(base))
+        lo = max(math.floor(pair_of(beta_fast)), 0)
+        hi = min(math.ceil(pair_of(beta_slow)), rot_dim // 2 - 1)
+        slowed = ((i - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
+        inv = inv * (1 - slowed) + inv / factor * slowed
+        mscale = 1.0 + 0.1 * math.log(factor)
+    return inv.to(device), mscale
+
+
+def rope_append(q, k, v, positions, slots, k_cache, v_cache, inv_freq, *, layout: str = "half", mscale: float = 1.0, out=None):
+    """Rotated queries; rotated keys and the values go to their cache slots
+    (sb_rope_append).
+
+    q: [tokens, q_heads, head_dim], k, v: [tokens, kv_heads, head_dim], caches:
+    [pages, page_size, kv_heads, head_dim], one type (bfloat16 or float16);
+    their token, head, page and slot strides are free. positions: int32
+    [tokens], slots: int64 [tokens] (plan_pages gives both; tokens with slots
+    outside the cache are skipped); inv_freq: float64, one per pair
+    (rope_frequencies). out: where the queries go, q itself for in place."""
+    dev, dtype = _device(q, "q"), q.dtype
+    if dtype not in _HALVES:
+        _refuse("q must be bfloat16 or float16")
+    _no_grad(q, k, v)
+    _heads(q, "q", dtype, dev)
+    T, Hq, D = q.shape
+    _heads(k, "k", dtype, dev, T, D)
+    _heads(v, "v", dtype, dev, T, D)
+    Hkv = k.shape[1]
+    if v.shape[1] != Hkv:
+        _refuse("k and v must have the same heads")
+    _caches(k_cache, v_cache, dtype, dev, Hkv, D)
+    _apart(k_cache, "k_cache"), _apart(v_cache, "v_cache")
+    if out is None:
+        out = torch.empty((T, Hq, D), dtype=dtype, device=dev)
+    else:
+        _heads(out, "out", dtype, dev, T, D)
+        if out.shape[1] != Hq:
+            _refuse("out must have q's heads")
+        _apart(out, "out")
+    if layout not in _LAYOUTS:
+        _refuse(f"unknown layout {layout!r}")
+    if inv_freq.dim() != 1:
+        _refuse("inv_freq must have one dimension")
+    np_ = inv_freq.shape[0]
+    qs, ks, vs, os_, kc, vc = q.stride(), k.stride(), v.stride(), out.stride(), k_cache.stride(), v_cache.stride()
+    args = N.ROPE_ARGS.pack(
+        N.ROPE_ARGS.size, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+        _whole(positions, "positions", torch.int32, dev, (T,)), _whole(slots, "slots", torch.int64, dev, (T,)),
+        _whole(inv_freq, "inv_freq", torch.float64, dev, (np_,)), qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], os_[0], os_[1],
+        kc[0], kc[1], kc[2], vc[0], vc[1], vc[2], T, Hq, Hkv, D, np_, _LAYOUTS[layout], _HALVES[dtype], k_cache.shape[0],
+        k_cache.shape[1], mscale)
+    _call(N.lib().sb_rope_append, "sb_rope_append", dev, args)
+    return out
+
+
+def paged_attention(q, k_cache, v_cache, table, lens, q_start, *, max_q: int, max_kv: int, window: int = 0, sinks: int = 0,
+                    scale: Optional[float] = None, out=None):
+    """Causal attention of a step's queries over their requests' paged caches
+    (sb_paged_attention).
+
+    q: [tokens, q_heads, head_dim] (rotated), caches: [pages, page_size, kv_heads,
+    head_dim], one type (bfloat16 or float16), head_dim 64, 128 or 256; table:
+    int32 [requests, max_pages]; lens: int32 [requests], the new tokens included;
+    q_start: int32 [requests + 1]. A query sees the last `window` positions up
+    to its own and the request's first `sinks` (window 0: all up to its own).
+    scale: 1 / sqrt(head_dim) by default. max_q, max_kv: upper bounds of a request's queries
+    and of lens, for the choice of kernels only. Rows of the result behind
+    the last request's are left as they are in `out` (undefined without it)."""
+    dev, dtype = _device(q, "q"), q.dtype
+    if dtype not in _HALVES:
+        _refuse("q must be bfloat16 or float16")
+    _no_grad(q, k_cache, v_cache)
+    _heads(q, "q", dtype, dev)
+    T, Hq, D = q.shape
+    _caches(k_cache, v_cache, dtype, dev, None, D)
+    if table.dim() != 2 or table.dtype != torch.int32 or table.device != dev or (table.shape[1] > 1 and table.stride(1) != 1):
+        _refuse(f"table must be an int32 tensor [requests, max_pages] on {dev} with contiguous rows")
+    B, width = table.shape
+    if out is None:
+        out = torch.empty((T, Hq, D), dtype=dtype, device=dev)
+    else:
+        _heads(out, "out", dtype, dev, T, D)
+        if out.shape[1] != Hq:
+            _refuse("out must have q's heads")
+        _apart(out, "out")
+    pages, page, Hkv, _ = k_cache.shape
+    qs, os_, kc, vc = q.stride(), out.stride(), k_cache.stride(), v_cache.stride()
+    args = N.ATTENTION_ARGS.pack(
+        N.ATTENTION_ARGS.size, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table.data_ptr(),
+        _whole(lens, "lens", torch.int32, dev, (B,)), _whole(q_start, "q_start", torch.int32, dev, (B + 1,)), out.data_ptr(),
+        qs[0], qs[1], os_[0], os_[1], kc[0], kc[1], kc[2], vc[0], vc[1], vc[2], table.stride(0) if B > 1 else width,
+        T, B, Hq, Hkv, D, _HALVES[dtype], pages, page, width, window, sinks, max_q, max_kv,
+        1.0 / math.sqrt(D) if scale is None else scale)
+    L = N.lib()
+    if dev.index == torch.cuda.current_device():
+        need = L.sb_attention_workspace(args)
+    else:
+        with torch.cuda.device(dev):
+            need = L.sb_attention_workspace(args)
+    if need < 0:
+        _check(N.SB_E_INVALID_ARG, "sb_paged_attention")
+    parts = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
+    _call(L.sb_paged_attention, "sb_paged_attention", dev, args, parts.data_ptr() if need else None, need)
+    return out
+
+
+def sample_tokens(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, out=None):
+    """(tokens int32 [rows], logprobs float32 [rows]): one token per row of
+    logits, drawn with the given numbers (sb_sample_tokens).
+
+    logits: [rows, vocab], float32, bfloat16 or float16, contiguous rows; u:
+    float32 [rows] in [0, 1). temperature, top_p, min_p (float32) and top_k
+    (int32): one per row, or None to leave that filter out (temperature: 1; 0
+    takes the largest logit). logprobs: of the drawn token among the kept
+    ones. out: (tokens, logprobs) to write to."""
+    dev = _device(logits, "logits")
+    if logits.dim() != 2 or logits.dtype not in _LOGITS or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        _refuse("logits must be a float32, bfloat16 or float16 tensor [rows, vocab] with contiguous rows")
+    _no_grad(logits)
+    R, V = logits.shape
+    f32 = torch.float32
+    if out is None:
+        out = torch.empty(R, dtype=torch.int32, device=dev), torch.empty(R, dtype=f32, device=dev)
+    tokens, logprobs = out
+    args = N.SAMPLE_ARGS.pack(
+        N.SAMPLE_ARGS.size, logits.data_ptr(), _whole(u, "u", f32, dev, (R,)),
+        0 if temperature is None else _whole(temperature, "temperature", f32, dev, (R,)),
+        0 if top_k is None else _whole(top_k, "top_k", torch.int32, dev, (R,)),
+        0 if top_p is None else _whole(top_p, "top_p", f32, dev, (R,)),
+        0 if min_p is None else _whole(min_p, "min_p", f32, dev, (R,)), _whole(tokens, "out tokens", torch.int32, dev, (R,)),
+        _whole(logprobs, "out logprobs", f32, dev, (R,)), logits.stride(0) if R > 1 else V, R, V, _LOGITS[logits.dtype], 0)
+    _call(N.lib().sb_sample_tokens, "sb_sample_tokens", dev, args)
+    return tokens, logprobs

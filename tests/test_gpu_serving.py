@@ -1,0 +1,651 @@
+"""The serving operators on the GPU against their fp64 oracle.
+
+Tolerances: eps is torch.finfo(type).eps, a rounding is off by eps / 2 of the
+value. Rotation: one rounding of the result, and fp32 errors of the angle
+(2^-25 turns of input rounding, 2^-23 of cosine and sine) and of three
+operations, below 2^-20 of |a| + |b|. Attention: one rounding of the result and
+one of each weight (eps / 2 of sum w |v| together); a score is off by at most
+D 2^-24 of its sum |q||k| times the scale plus 2^-22 of its own size (the
+products with scale log2 e), a weight by twice that and 2^-20 more from the
+exponentials, the sums and the joins. Sampled tokens have to be equal."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2010_02164_amd as sb
+from oracle import serving as oracle
+
+pytestmark = pytest.mark.gpu
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+
+
+def rng(seed):
+    return np.random.default_rng(seed)
+
+
+def dev(a, dtype=None):
+    return torch.as_tensor(np.ascontiguousarray(a)).cuda().to(dtype) if dtype else torch.as_tensor(np.ascontiguousarray(a)).cuda()
+
+
+def i32(a):
+    return dev(np.asarray(a, np.int32))
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+# -- pages -------------------------------------------------------------------------
+
+def run_plan(lens, add, free, n_pages, table, page, cap, **kw):
+    fl = np.full(n_pages, -7, np.int32)
+    fl[:len(free)] = free
+    tab, fl = i32(table), i32(fl)
+    p = sb.plan_pages(i32(lens), i32(add), fl, i32([len(free)]), tab, page_size=page, token_cap=cap, **kw)
+    return p, tab, fl
+
+
+def check_plan(lens, add, free, n_pages, table, page, cap):
+    want = oracle.plan_pages(lens, add, free, table, page, cap)
+    p, tab, fl = run_plan(lens, add, free, n_pages, table, page, cap)
+    got = [x.tolist() for x in (p.lens, p.granted, fl[:int(p.n_free)], tab, p.slots, p.positions, p.q_start)]
+    for name, a, b in zip(("lens", "granted", "free", "table", "slots", "positions", "q_start"), got, want):
+        assert a == [int(x) for x in b] if name != "table" else a == b.tolist(), name
+    return want
+
+
+@pytest.mark.parametrize("B,page,mode", [(1, 16, "one"), (3, 1, "few"), (7, 5, "mixed"), (64, 16, "one"), (1000, 16, "mixed"), (1025, 8, "one"),
+                                         (2049, 3, "mixed"), (8192, 4, "mixed"), (33, 64, "long"), (5, 4096, "long")])
+def test_plan(gpu, B, page, mode):
+    r = rng(B)
+    width = 12 if mode != "long" else 60
+    lens = r.integers(0, 6 * page, B)
+    add = {"one": np.ones(B, int), "few": r.integers(0, 5, B), "mixed": r.integers(-1, 4 * page, B),
+           "long": r.integers(-1, min(50 * page, 3000), B)}[mode]
+    held = -(-lens // page)
+    n_pages = int(held.sum() + B * 3)
+    ids = r.permutation(n_pages)
+    table = np.full((B, width), -1)
+    table[np.arange(width) < held[:, None]] = ids[:held.sum()]
+    free = ids[held.sum():].tolist()
+    everything = int(np.maximum(add, 0).sum())
+    for cap, some in ((everything + 3, free), (everything // 2, free), (everything + 3, free[:len(free) // 4]), (0, free)):
+        want = check_plan(lens, add, some, n_pages, table, page, cap)
+        new = [int(x) for b, n in enumerate(lens) if add[b] >= 0 for x in want[3][b, :-(-want[0][b] // page)]]
+        assert len(set(new)) == len(new) and not set(new) & set(want[2])   # no page twice
+
+
+def test_plan_refuses_one_request_without_holding_up_others(gpu):
+    want = check_plan([0, 30, 2, 0], [5, 3, 2, 33], [4, 5, 6, 7], 8, np.full((4, 8), 1), 4, 50)
+    assert want[1] == [5, 0, 2, 0]
+
+
+def test_plan_wrong_state_stays_in_bounds(gpu):
+    """Lengths and free counts out of range are taken as the nearest in it,
+    released pages that do not fit the list are dropped, and slots of page ids
+    that are none are -1."""
+    p, tab, fl = run_plan([10 ** 9, -5, 4], [-1, 3, 1], list(range(6)), 6, [[9, -3, 7]] * 3, 2, 9)
+    assert p.lens.tolist() == [0, 3, 5] and int(p.n_free) == 6 - 3
+    assert tab.tolist()[1][:2] == [5, 4]
+    p, tab, _ = run_plan([0], [3], [99, -2], 2, [[0, 0]], 2, 4)
+    assert p.slots.tolist() == [-1, -1, -1, -1] and p.positions.tolist() == [0, 1, 2, -1]
+    lens, table = i32([2]), i32([[0, 1]])   # 2 more fill the row and need a page
+    for n_free in (-4, 50):
+        p = sb.plan_pages(lens, i32([2]), i32([2, 3]), i32([n_free]), table, page_size=2, token_cap=2)
+        assert p.granted.tolist() == ([0] if n_free < 0 else [2])
+
+
+def test_plan_in_place_and_repeated(gpu):
+    """State written over its inputs goes on as the oracle does; state written
+    elsewhere leaves the call repeatable."""
+    r = rng(3)
+    B, page, width, n_pages = 40, 4, 20, 300
+    lens, free, table = [0] * B, list(range(n_pages)), np.full((B, width), -1)
+    fl, tab = i32(free), i32(table)
+    cur = sb.PagePlan(i32([0] * (B + 1)), i32(lens), i32(lens), dev(np.zeros(90, np.int64)), i32([0] * 90), i32([n_pages]))
+    for step in range(30):
+        add = r.integers(-1, 6, B)
+        lens, granted, free, table, slots, pos, q_start = oracle.plan_pages(lens, add, free, table, page, 90)
+        apart = [sb.plan_pages(cur.lens, i32(add), fl, cur.n_free, tab, page_size=page, token_cap=90) for _ in range(2)]
+        assert all(torch.equal(x, y) for x, y in zip(*apart))
+        got = sb.plan_pages(cur.lens, i32(add), fl, cur.n_free, tab, page_size=page, token_cap=90, out=cur)
+        assert got is cur and all(torch.equal(x, y) for x, y in zip(got, apart[0]))
+        assert cur.lens.tolist() == lens and cur.slots.tolist() == slots and fl[:int(cur.n_free)].tolist() == free
+
+
+# -- rotary positions and the cache's write --------------------------------------------
+
+def rope_case(T, Hq, Hkv, D, pairs, dtype, seed, page=16, far=10 ** 6):
+    r = rng(seed)
+    n_pages = T // page + 3
+    make = lambda *s: dev(r.standard_normal(s), dtype)   # noqa: E731
+    return dict(q=make(T, Hq, D), k=make(T, Hkv, D), v=make(T, Hkv, D), positions=i32(r.integers(0, far, T)),
+                slots=dev(r.permutation(n_pages * page)[:T]), k_cache=make(n_pages, page, Hkv, D), v_cache=make(n_pages, page, Hkv, D),
+                inv_freq=dev(10000.0 ** (-np.arange(pairs) / max(pairs, 1))))
+
+
+def check_rope(c, layout, mscale, rotated, before, rows=None):
+    """rows: the tokens to look at (None: all)."""
+    dtype = rotated.dtype
+    eps = torch.finfo(dtype).eps
+    inv, pos, slots = f64(c["inv_freq"]), c["positions"].tolist(), c["slots"].tolist()
+    page = c["k_cache"].shape[1]
+    kb, vb = before[0].clone(), before[1].clone()
+    for t in range(len(pos)) if rows is None else rows:
+        if not 0 <= slots[t] < kb.shape[0] * page:
+            continue
+        at = slots[t] // page, slots[t] % page
+        for x, got in ((c["q"][t], rotated[t]), (c["k"][t], c["k_cache"][at])):
+            for h in range(x.shape[0]):
+                want, size = oracle.rotate(f64(x[h]), pos[t], inv, layout, mscale)
+                assert np.all(np.abs(f64(got[h]) - want) <= eps / 2 * np.abs(want) + 2.0 ** -20 * size), (t, h)
+        assert torch.equal(c["v_cache"][at], c["v"][t])
+        kb[at], vb[at] = c["k_cache"][at], c["v"][t]
+    if rows is None:   # nothing else was written
+        assert torch.equal(kb, c["k_cache"]) and torch.equal(vb, c["v_cache"])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("T,Hq,Hkv,D,pairs,layout,mscale,page", [
+    (1, 4, 1, 64, 32, "half", 1.0, 16), (5, 3, 3, 128, 64, "interleaved", 1.2, 7), (37, 8, 2, 128, 16, "half", 0.7, 1),
+    (3, 1, 1, 256, 128, "half", 1.0, 128), (9, 5, 1, 8, 4, "interleaved", 1.0, 3), (4, 2, 2, 512, 256, "half", 1.0, 64),
+    (6, 7, 1, 72, 8, "half", 1.1, 5), (2, 2, 1, 64, 0, "half", 1.0, 4), (2, 2, 1, 64, 0, "interleaved", 1.0, 4)])
+def test_rope(gpu, T, Hq, Hkv, D, pairs, layout, mscale, page, dtype):
+    c = rope_case(T, Hq, Hkv, D, pairs, dtype, T + D, page)
+    before = c["k_cache"].clone(), c["v_cache"].clone()
+    got = sb.rope_append(**c, layout=layout, mscale=mscale)
+    check_rope(c, layout, mscale, got, before)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rope_many_tokens(gpu, layout):
+    """A prompt (several tokens a workgroup, a last one that is not full)."""
+    c = rope_case(8195, 4, 2, 64, 16, BF16, 5)
+    c["slots"][[0, 4097, 8190]] = torch.tensor([-1, 10 ** 12, c["k_cache"].shape[0] * 16]).cuda()
+    before = c["k_cache"].clone(), c["v_cache"].clone()
+    out = dev(np.full((8195, 4, 64), 7.0), BF16)
+    sb.rope_append(**c, layout=layout, out=out)
+    check_rope(c, layout, 1.0, out, before, [1, 2, 3, 4, 5, 4096, 4098, 8189, 8191, 8192, 8193, 8194])
+    assert bool((out[[0, 4097, 8190]] == 7).all())          # skipped tokens stay as they were
+    one = [sb.rope_append(**{n: (x[t:t + 300] if x.shape[0] == 8195 else x) for n, x in c.items()}, layout=layout)
+           for t in range(0, 8195, 300)]                     # and the one-token kernel gives the same bits
+    keep = torch.ones(8195, dtype=torch.bool)
+    keep[[0, 4097, 8190]] = False
+    assert torch.equal(torch.cat(one)[keep], out[keep])
+
+
+def test_rope_views_in_place(gpu):
+    """Slices of one projection's output, turned in place; caches with heads
+    before tokens, both in one allocation."""
+    T, Hq, Hkv, D, page = 21, 6, 2, 64, 4
+    r = rng(8)
+    qkv = dev(r.standard_normal((T, Hq + 2 * Hkv, D)), F16)
+    c = rope_case(T, Hq, Hkv, D, 32, F16, 9, page)
+    pool = torch.zeros(8, 2, Hkv, page, D, dtype=F16, device="cuda")
+    q, k, v = qkv[:, :Hq], qkv[:, Hq:Hq + Hkv], qkv[:, Hq + Hkv:]
+    c.update(q=q, k=k, v=v, k_cache=pool[:, 0].transpose(1, 2), v_cache=pool[:, 1].transpose(1, 2))
+    plain = {n: x.clone() for n, x in c.items()}
+    want = sb.rope_append(**{n: x.contiguous() for n, x in plain.items()})
+    before = torch.zeros_like(plain["k_cache"]), torch.zeros_like(plain["v_cache"])
+    assert sb.rope_append(**c, out=q) is q
+    assert torch.equal(q, want)
+    check_rope(dict(plain, k_cache=c["k_cache"], v_cache=c["v_cache"]), "half", 1.0, q, before)
+
+
+def test_rope_far_positions(gpu):
+    """Positions up to 2^31 - 1: an fp32 angle would be off by whole turns."""
+    c = rope_case(4, 1, 1, 64, 32, F16, 11)
+    c["positions"] = i32([2 ** 31 - 1, 2 ** 30 + 1, 0, -5])
+    before = c["k_cache"].clone(), c["v_cache"].clone()
+    check_rope(c, "half", 1.0, sb.rope_append(**c), before)
+
+
+# -- attention ---------------------------------------------------------------------
+
+def attention_case(B, Hq, Hkv, D, page, q_lens, kv_lens, dtype, seed, pad=0, spread=1.0):
+    r = rng(seed)
+    q_lens, kv_lens = np.resize(q_lens, B), np.resize(kv_lens, B)
+    held = -(-kv_lens // page)
+    n_pages = int(held.sum()) + 2
+    table = np.full((B, max(int(held.max()), 1) + 1), -1)
+    table[np.arange(table.shape[1]) < held[:, None]] = r.permutation(n_pages)[:held.sum()]
+    q_start = np.concatenate([[0], np.cumsum(q_lens)])
+    T = int(q_start[-1]) + pad
+    return dict(q=dev(spread * r.standard_normal((T, Hq, D)), dtype), k_cache=dev(r.standard_normal((n_pages, page, Hkv, D)), dtype),
+                v_cache=dev(r.standard_normal((n_pages, page, Hkv, D)), dtype), table=i32(table), lens=i32(kv_lens), q_start=i32(q_start))
+
+
+def bounds(c, max_q=None, max_kv=None):
+    q = (c["q_start"][1:] - c["q_start"][:-1]).max()
+    return dict(max_q=int(q) if max_q is None else max_q, max_kv=int(c["lens"].max()) if max_kv is None else max_kv)
+
+
+def check_attention(c, got, window=0, sinks=0, scale=None, only=None):
+    """only: queries to look at (the oracle runs on those requests' rows)."""
+    D = got.shape[2]
+    eps = torch.finfo(got.dtype).eps
+    scale = 1 / math.sqrt(D) if scale is None else scale
+    want, size, big = oracle.attention(f64(c["q"]), f64(c["k_cache"]), f64(c["v_cache"]), c["table"].tolist(), c["lens"].tolist(),
+                                       c["q_start"].tolist(), window, sinks, scale)
+    score = big * abs(scale) * (D * 2.0 ** -24 + 2.0 ** -22)
+    tol = eps / 2 * np.abs(want) + (eps / 2 + 2 * score[..., :1] + 2.0 ** -20) * size + torch.finfo(got.dtype).smallest_normal
+    rows = int(c["q_start"][-1])
+    d = np.abs(f64(got)[:rows] - want[:rows])
+    assert np.all(d <= tol[:rows]), (np.argwhere(~(d <= tol[:rows]))[:5], np.nanmax(d / tol[:rows]))
+
+
+FORMS = [   # B, Hq, Hkv, page, queries, cached
+    (1, 4, 1, 16, [1], [1]), (5, 8, 2, 16, [1], [1, 2, 31, 33, 200]), (3, 5, 5, 7, [1], [64, 500, 13]),
+    (2, 16, 1, 1, [1], [40, 97]), (3, 32, 2, 24, [1], [130, 5, 300]), (4, 8, 4, 32, [3, 1, 4, 2], [3, 90, 65, 2]),
+    (2, 40, 2, 16, [2], [50, 81]), (3, 4, 2, 16, [40, 1, 97], [40, 260, 150]), (1, 8, 1, 64, [70], [129]), (2, 3, 3, 5, [130, 33], [200, 33]),
+]
+
+
+@pytest.mark.parametrize("dtype,D", [(BF16, 128), (F16, 64), (BF16, 256), (F16, 128)])
+@pytest.mark.parametrize("form", range(len(FORMS)))
+def test_attention(gpu, form, dtype, D):
+    c = attention_case(*FORMS[form][:3], D, *FORMS[form][3:], dtype, form)
+    for window, sinks in ((0, 0), (17, 0), (17, 4), (1, 0), (1, 100), (64, 33)):
+        got = sb.paged_attention(**c, **bounds(c), window=window, sinks=sinks)
+        check_attention(c, got, window, sinks)
+
+
+@pytest.mark.parametrize("dtype,D,Hq,Hkv", [(BF16, 128, 4, 1), (F16, 64, 8, 1), (BF16, 256, 2, 1)])
+def test_attention_long_cache_in_parts(gpu, dtype, D, Hq, Hkv):
+    """Caches long enough to be split over workgroups, short ones beside."""
+    c = attention_case(3, Hq, Hkv, D, 16, [1, 2, 1], [6000, 9, 2500], dtype, 5)
+    for window, sinks in ((0, 0), (2000, 5)):
+        got = sb.paged_attention(**c, **bounds(c), window=window, sinks=sinks)
+        check_attention(c, got, window, sinks)
+
+
+def test_attention_wrong_bounds_only_cost_time(gpu):
+    """max_q and max_kv that are too small or too large: the same result up to rounding."""
+    for q, kv in (([1], [700, 30]), ([60, 3], [700, 30])):
+        c = attention_case(2, 8, 2, 128, 16, q, kv, BF16, 6)
+        for max_q, max_kv in ((0, 0), (1, 1), (1, 10 ** 6), (10 ** 6, 700), (2 ** 31 - 1, 2 ** 31 - 1)):
+            got = sb.paged_attention(**c, max_q=max_q, max_kv=max_kv, window=300, sinks=2)
+            check_attention(c, got, 300, 2)
+
+
+@pytest.mark.parametrize("max_q", [1, 1000])
+def test_attention_empty_rows(gpu, max_q):
+    """Requests without queries or tokens, queries before the first position,
+    rows behind the last request."""
+    c = attention_case(6, 4, 2, 64, 8, [0, 2, 1, 0, 5, 1], [9, 2, 0, 0, 3, 6], BF16, 7, pad=4)
+    out = dev(np.full(c["q"].shape, 3.0), BF16)
+    assert sb.paged_attention(**c, max_q=max_q, max_kv=9, out=out) is out
+    check_attention(c, out)
+    assert bool((out[2] == 0).all()) and bool((out[3:5] == 0).all())   # of a request of 0 tokens; positions -2 and -1
+    assert bool((out[-4:] == 3).all())
+    out.fill_(3)
+    nobody = dict(c, q_start=i32([0] * 7))
+    sb.paged_attention(**nobody, max_q=max_q, max_kv=9, out=out)
+    assert bool((out == 3).all())
+
+
+@pytest.mark.parametrize("max_q", [1, 1000])
+def test_attention_pages_outside_the_cache_are_skipped(gpu, max_q):
+    c = attention_case(3, 4, 2, 128, 4, [2, 1, 1], [30, 21, 8], BF16, 8)
+    c["table"][0, 3], c["table"][0, 5], c["table"][1, 0] = 10 ** 6, -9, 2 ** 31 - 1
+    c["table"][2, :2] = -1
+    got = sb.paged_attention(**c, max_q=max_q, max_kv=30)
+    check_attention(c, got)
+    assert bool((got[3] == 0).all())
+    c["lens"][1] = 2 ** 31 - 1   # longer than its table row: cut there, whose places behind are -1
+    got = sb.paged_attention(**c, max_q=max_q, max_kv=30)
+    assert bool(torch.isfinite(got).all())
+
+
+@pytest.mark.parametrize("max_q,dtype", [(1, BF16), (1000, BF16), (1000, F16)])
+def test_attention_what_is_hidden_does_not_matter(gpu, max_q, dtype):
+    """NaN and infinities on pages of nobody, behind the last token, before the
+    window, and at positions that other rows of the tile do see."""
+    for q, kv, window, sinks in (([1], [50, 77], 20, 3), ([6, 3], [50, 77], 9, 2), ([6, 3], [50, 77], 0, 0)):
+        c = attention_case(2, 4, 1, 64, 16, q, kv, dtype, 9)
+        clean = sb.paged_attention(**c, max_q=max_q, max_kv=77, window=window, sinks=sinks)
+        used = torch.zeros(c["k_cache"].shape[:2], dtype=torch.bool, device="cuda")
+        m = c["q_start"][1:] - c["q_start"][:-1]
+        for b, n in enumerate(kv):
+            lo = max(0, n - int(m[b]) + 1 - window) if window else 0
+            for j in list(range(min(sinks, lo))) + list(range(lo, n)):
+                used[c["table"][b, j // 16], j % 16] = True
+        for bad in (math.nan, math.inf, -math.inf):
+            c["k_cache"][~used] = bad
+            c["v_cache"][~used] = bad
+            assert torch.equal(sb.paged_attention(**c, max_q=max_q, max_kv=77, window=window, sinks=sinks), clean)
+        if q[0] > 1:   # the last position is seen by the last query alone
+            at = int(c["table"][0, 49 // 16]), 49 % 16
+            c["k_cache"][at], c["v_cache"][at] = 0.0, math.nan
+            got = sb.paged_attention(**c, max_q=max_q, max_kv=77, window=window, sinks=sinks)
+            assert torch.equal(got[:5], clean[:5]) and bool(got[5].isnan().all()) and torch.equal(got[6:], clean[6:])
+            c["v_cache"][at] = math.inf
+            c["k_cache"][at] = math.nan
+            got = sb.paged_attention(**c, max_q=max_q, max_kv=77, window=window, sinks=sinks)
+            assert torch.equal(got[:5], clean[:5]) and bool(got[5].isnan().all()) and torch.equal(got[6:], clean[6:])
+
+
+@pytest.mark.parametrize("max_q", [1, 1000])
+def test_attention_large_scores(gpu, max_q):
+    """Scores of thousands: the running maximum has to move; and a scale of its
+    own, also negative and zero."""
+    c = attention_case(2, 4, 2, 128, 16, [9, 1], [300, 140], BF16, 10, spread=60.0)
+    for scale in (None, -0.02, 0.0):
+        got = sb.paged_attention(**c, max_q=max_q, max_kv=300, scale=scale)
+        check_attention(c, got, scale=scale)
+
+
+@pytest.mark.parametrize("max_q", [1, 1000])
+def test_attention_strides(gpu, max_q):
+    """q a slice of a wider projection, caches with heads before tokens in one
+    allocation, a table that is part of a wider one, out into a slice."""
+    c = attention_case(3, 6, 2, 64, 8, [4, 1, 2], [20, 33, 2], F16, 11)
+    want = sb.paged_attention(**c, max_q=max_q, max_kv=33, window=9, sinks=1)
+    T, P = c["q"].shape[0], c["k_cache"].shape[0]
+    wide = torch.randn(T, 10, 64, device="cuda").half()
+    wide[:, 2:8] = c["q"]
+    pool = torch.empty(P, 2, 2, 8, 64, dtype=F16, device="cuda")
+    pool[:, 0], pool[:, 1] = c["k_cache"].transpose(1, 2), c["v_cache"].transpose(1, 2)
+    tab = torch.full((3, c["table"].shape[1] + 5), -1, dtype=torch.int32, device="cuda")
+    tab[:, :-5] = c["table"]
+    out = torch.zeros(6, T, 72, dtype=F16, device="cuda")
+    got = sb.paged_attention(wide[:, 2:8], pool[:, 0].transpose(1, 2), pool[:, 1].transpose(1, 2), tab[:, :-5], c["lens"], c["q_start"],
+                             max_q=max_q, max_kv=33, window=9, sinks=1, out=out[:, :, :64].transpose(0, 1))
+    assert torch.equal(got, want) and bool((out[:, :, 64:] == 0).all())
+
+
+def test_attention_offsets_beyond_32_bits(gpu):
+    """A cache of 5 GB, the request's pages at its end."""
+    page, Hkv, D = 64, 8, 128
+    n_pages = (5 << 30) // (page * Hkv * D * 2)
+    k, v = (torch.zeros(n_pages, page, Hkv, D, dtype=BF16, device="cuda") for _ in range(2))
+    c = attention_case(1, 16, Hkv, D, page, [1], [150], BF16, 12)
+    for max_q in (1, 1000):
+        want = sb.paged_attention(**c, max_q=max_q, max_kv=150)
+        tail = n_pages - c["k_cache"].shape[0]
+        k[tail:], v[tail:] = c["k_cache"], c["v_cache"]
+        got = sb.paged_attention(c["q"], k, v, torch.where(c["table"] >= 0, c["table"] + tail, -1), c["lens"], c["q_start"],
+                                 max_q=max_q, max_kv=150)
+        assert torch.equal(got, want)
+
+
+# -- sampling ----------------------------------------------------------------------
+
+def check_sample(z, u, T=None, top_k=None, top_p=None, min_p=None, dtype=F32):
+    z = dev(z, F32).to(dtype)
+    f = lambda x: None if x is None else dev(np.asarray(x, np.float32))   # noqa: E731
+    tok, lp = sb.sample_tokens(z, f(u), temperature=f(T), top_k=None if top_k is None else i32(top_k), top_p=f(top_p), min_p=f(min_p))
+    zz = f64(z)
+    for r in range(len(zz)):
+        val = lambda x, d: d if x is None else np.float32(x[r])   # noqa: E731
+        want = oracle.sample(zz[r], np.float64(np.float32(u[r])), float(val(T, 1.0)), 0 if top_k is None else int(top_k[r]),
+                             float(val(top_p, 1.0)), float(val(min_p, 0.0)))
+        assert int(tok[r]) == want[0], (r, int(tok[r]), want)
+        assert float(lp[r]) == pytest.approx(want[1], rel=2.0 ** -22, abs=2.0 ** -36), r
+    return tok, lp
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("V", [1, 2, 3, 63, 64, 65, 255, 1000, 1023, 1025, 4097, 32000, 50001])
+def test_sample(gpu, V, dtype):
+    r = rng(V)
+    rows = 24 if V < 2000 else 12
+    z = r.standard_normal((rows, V)) * 2.5
+    z[np.arange(rows)[:, None], r.integers(0, V, (rows, 5))] += 6 * r.random((rows, 5))
+    u, T = r.random(rows), 0.5 + r.random(rows)
+    T[3::8] = 0
+    k = np.where(np.arange(rows) % 3 == 0, 0, np.exp(r.random(rows) * math.log(max(V, 2))).astype(int))
+    p, mp = np.where(np.arange(rows) % 4 == 1, 1.0, 0.5 + 0.5 * r.random(rows)), np.where(np.arange(rows) % 2, 0.0, 0.2 * r.random(rows))
+    check_sample(z, u, dtype=dtype)
+    check_sample(z, u, T, dtype=dtype)
+    check_sample(z, u, T, top_k=k, dtype=dtype)
+    check_sample(z, u, T, top_p=p, dtype=dtype)
+    check_sample(z, u, None, min_p=mp, dtype=dtype)
+    check_sample(z, u, T, k, p, mp, dtype)
+
+
+@pytest.mark.parametrize("V", [7, 3000])
+def test_sample_ties(gpu, V):
+    """Equal logits: the lowest indexes are kept, and every border of the draw
+    is exact."""
+    for z in (np.zeros(V), np.r_[np.zeros(V // 2), np.ones(V - V // 2)], np.tile([1.0, -1.0, 1.0], V)[:V]):
+        z = np.tile(z, (16, 1))
+        u = np.r_[np.arange(8) / 8, 1 - 2.0 ** -24, 1.0, 0.5, 2.0 ** -24, np.nan, -1.0, 2.0, 0.25]
+        check_sample(z, u)
+        check_sample(z, u, top_k=np.arange(16) * V // 14)
+        check_sample(z, u, top_p=np.arange(16) / 14)
+        check_sample(z, u, top_k=np.full(16, V // 2 + 1), top_p=np.arange(16) / 14)
+        check_sample(z, u, T=np.full(16, math.log2(math.e)), min_p=np.arange(16) / 14)
+
+
+def test_sample_flat_and_wide(gpu):
+    """Cuts that keep very many tokens."""
+    r = rng(4)
+    z = np.concatenate([0.01 * r.standard_normal((6, 20000)), r.standard_normal((6, 20000))])
+    u = r.random(12)
+    check_sample(z, u, top_p=np.linspace(0.1, 0.999, 12))
+    check_sample(z, u, top_k=np.linspace(2, 19999, 12).astype(int))
+    check_sample(z, u, top_k=np.linspace(500, 19999, 12).astype(int), top_p=np.linspace(0.999, 0.3, 12), min_p=np.full(12, 0.01))
+    check_sample(z, u, T=np.full(12, 100.0))
+
+
+def test_sample_odd_values(gpu):
+    """-inf, NaN, +inf, the largest and smallest numbers, -0; parameters out of
+    their range."""
+    inf, nan, big = math.inf, math.nan, 3.0e38
+    rows = [[-inf, 0, nan, 1, -inf], [nan] * 5, [-inf] * 5, [inf, 0, inf, 1, nan], [big, -big, big, 0, 1], [-big, -big, -inf, -big, nan],
+            [-0.0, 0.0, -0.0, 0.0, -inf], [1e-40, 0, -1e-40, 0, 0]]
+    n = len(rows)
+    for u in (0.0, 0.3, 0.7, 1.0):
+        U = [u] * n
+        check_sample(rows, U)
+        check_sample(rows, U, T=[0.0] * n)
+        check_sample(rows, U, T=[nan] * n)
+        check_sample(rows, U, T=[-1.0] * n)
+        check_sample(rows, U, T=[1e-30] * n)
+        check_sample(rows, U, T=[1e30] * n, top_k=[3] * n)
+        check_sample(rows, U, top_k=[2] * n, top_p=[0.4] * n, min_p=[0.1] * n)
+        check_sample(rows, U, top_k=[-3] * n, top_p=[nan] * n, min_p=[nan] * n)
+        check_sample(rows, U, top_k=[2 ** 31 - 1] * n, top_p=[inf] * n, min_p=[inf] * n)
+        check_sample(rows, U, top_k=[1] * n, top_p=[-1.0] * n, min_p=[-1.0] * n)
+    tok, lp = sb.sample_tokens(dev(np.zeros((1, 4)), F32), dev(np.float32([0.6])), temperature=dev(np.float32([inf])))
+    assert int(tok) == 2
+
+
+def test_sample_views(gpu):
+    """Rows of a wider array, at addresses of no alignment, and out tensors."""
+    r = rng(6)
+    for dtype in (F32, BF16):
+        wide = dev(r.standard_normal((5, 3011)), dtype)
+        z, u = wide[:, 5:3006], dev(r.random(5).astype(np.float32))
+        p = dev(np.full(5, 0.9, np.float32))
+        want = sb.sample_tokens(z.contiguous(), u, top_p=p)
+        out = torch.full((7,), -9, dtype=torch.int32, device="cuda")[1:6], torch.zeros(5, device="cuda")
+        got = sb.sample_tokens(z, u, top_p=p, out=out)
+        assert got[0] is out[0] and torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert sb.sample_tokens(z[:0], u[:0])[0].shape == (0,)
+
+
+def test_sample_frequencies(gpu):
+    """Draws over a grid of numbers come as often as the weights say."""
+    z = dev(np.log([[0.1, 0.2, 0.3, 0.4]]), F32).expand(4096, 4).contiguous()
+    u = (torch.arange(4096, device="cuda") / 4096).float()
+    assert torch.bincount(sb.sample_tokens(z, u)[0]).tolist() == [410, 819, 1229, 1638]
+
+
+# -- together ----------------------------------------------------------------------
+
+class Layer:
+    """A toy cached decoder of one layer, tokens to logits, on torch products."""
+
+    def __init__(self, seed, V=500, H=256, Hq=8, Hkv=2, D=64):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        make = lambda *s: (torch.randn(*s, generator=g, device="cuda") / math.sqrt(s[0])).to(BF16)   # noqa: E731
+        self.E, self.qkv, self.o, self.out = make(V, H) * 20, make(H, (Hq + 2 * Hkv) * D), make(Hq * D, H), make(H, V) * 4
+        self.Hq, self.Hkv, self.D = Hq, Hkv, D
+        self.inv_freq, self.mscale = sb.rope_frequencies(D, scaling="parts", factor=4.0, original_length=64)
+
+    def step(self, tokens, plan, cache, table, **kw):
+        x = self.E[tokens]
+        qkv = (x @ self.qkv).view(len(tokens), -1, self.D)
+        q, k, v = qkv.split([self.Hq, self.Hkv, self.Hkv], 1)
+        q = sb.rope_append(q, k, v, plan.positions, plan.slots, *cache, self.inv_freq, mscale=self.mscale)
+        a = sb.paged_attention(q, *cache, table, plan.lens, plan.q_start, **kw)
+        return (x + a.reshape(len(tokens), -1) @ self.o) @ self.out
+
+
+def fresh(n_pages, page, layer, B, width, cap):
+    cache = [torch.full((n_pages, page, layer.Hkv, layer.D), math.nan, dtype=BF16, device="cuda") for _ in range(2)]
+    zero = torch.zeros(B, dtype=torch.int32, device="cuda")
+    plan = sb.PagePlan(i32([0] * (B + 1)), zero.clone(), zero.clone(), torch.zeros(cap, dtype=torch.int64, device="cuda"),
+                       torch.zeros(cap, dtype=torch.int32, device="cuda"), i32([n_pages]))
+    return cache, i32(np.arange(n_pages)), torch.full((B, width), -1, dtype=torch.int32, device="cuda"), plan
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (24, 3)])
+def test_a_run_of_them_together(gpu, window, sinks):
+    """Prompts in one step and token by token: caches, attention and draws of a
+    batch with a released and reused request follow each request alone."""
+    layer, page, width = Layer(1), 8, 16
+    r = rng(2)
+    prompts = [r.integers(0, 500, n).tolist() for n in (37, 1, 20)]
+    kw = dict(max_kv=width * page, window=window, sinks=sinks)
+
+    def generate(prompt, n, us):
+        """One request alone, its whole text given anew at each step."""
+        text, got = list(prompt), []
+        for t in range(n):
+            cache, free, table, plan = fresh(width, page, layer, 1, width, len(text))
+            plan = sb.plan_pages(plan.lens, i32([len(text)]), free, plan.n_free, table, page_size=page, token_cap=len(text))
+            logits = layer.step(torch.tensor(text).cuda(), plan, cache, table, max_q=len(text), **kw)
+            tok = sb.sample_tokens(logits[-1:].float(), dev(np.float32(us[t:t + 1])), top_p=dev(np.float32([0.8])))[0]
+            got.append((int(tok), logits[-1].float()))
+            text.append(int(tok))
+        return got
+
+    us = [np.float32(r.random(12)) for _ in range(3)]
+    alone = [generate(p, 12 if b != 1 else 6, us[b]) for b, p in enumerate(prompts)]
+    cache, free, table, plan = fresh(40, page, layer, 3, width, 64)
+    add = i32([len(p) for p in prompts])
+    tokens = torch.tensor(sum(prompts, []) + [0] * (64 - sum(map(len, prompts)))).cuda()
+    max_q, top_p = 37, dev(np.full(3, 0.8, np.float32))
+    used = []
+    for t in range(12):
+        plan = sb.plan_pages(plan.lens, add, free, plan.n_free, table, page_size=page, token_cap=64, out=plan)
+        used.append(40 - int(plan.n_free))
+        logits = layer.step(tokens, plan, cache, table, max_q=max_q, **kw)
+        last = logits[(plan.q_start[1:].long() - 1).clamp(min=0)].float()
+        drawn = sb.sample_tokens(last, dev(np.array([x[t] for x in us], np.float32)), top_p=top_p)[0]
+        live = [0, 1, 2] if t < 6 else [0, 2]
+        for b in live:
+            # (the logits' products round in another order for other batches: the tokens follow the given ones)
+            assert torch.allclose(last[b], alone[b][t][1], atol=0.05 * float(alone[b][t][1].abs().max())), (t, b)
+        # Each request's next token, in order; request 1 ends after its sixth.
+        nxt = [alone[b][t][0] for b in live if not (b == 1 and t == 5)]
+        assert drawn.shape == (3,)
+        add = i32([1, 1, 1]) if t < 5 else i32([1, -1 if t == 5 else 0, 1])
+        tokens = torch.tensor(nxt + [0] * (64 - len(nxt))).cuda()
+        max_q = 1
+    assert used[6] < used[5] or used[6] <= used[5] + 1   # request 1's pages came back
+    assert plan.lens.tolist() == [37 + 11, 0, 20 + 11]
+
+
+def test_captured_steps(gpu):
+    """A whole step captured once and replayed, with eager work between: as the
+    same steps taken eagerly. Two graphs live at once, each with its workspace."""
+    page, width, B = 8, 40, 4
+    graphs = []
+    for seed in (1, 2):
+        layer = Layer(seed)
+        state = fresh(100, page, layer, B, width, B)
+        shadow = fresh(100, page, layer, B, width, B)
+        tokens, u = torch.full((B,), 3 * seed, device="cuda"), torch.zeros(B, device="cuda")
+        add = i32([1] * B)
+        par = dict(temperature=dev(np.full(B, 0.9, np.float32)), top_k=i32([50] * B), min_p=dev(np.full(B, 0.02, np.float32)))
+
+        def step(state, tokens, u, layer=layer, add=add, par=par):
+            cache, free, table, plan = state
+            sb.plan_pages(plan.lens, add, free, plan.n_free, table, page_size=page, token_cap=B, out=plan)
+            logits = layer.step(tokens, plan, cache, table, max_q=1, max_kv=width * page, window=30, sinks=2)
+            new, lp = sb.sample_tokens(logits, u, **par)
+            return new.long(), lp
+
+        want_tokens = tokens.clone()
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(stream):   # warm-up of torch's own products, on a state of its own
+            step(fresh(100, page, layer, B, width, B), tokens, u)
+        torch.cuda.current_stream().wait_stream(stream)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            new, lp = step(state, tokens, u)
+            tokens.copy_(new)
+        graphs.append([graph, state, shadow, tokens, u, lp, want_tokens, step])
+    r = rng(5)
+    for t in range(40):
+        for x in graphs:
+            u = torch.as_tensor(r.random(B).astype(np.float32)).cuda()
+            x[4].copy_(u)
+            x[0].replay()
+            new, lp = x[7](x[2], x[6], u)
+            x[6] = new
+            assert torch.equal(x[3], new) and torch.equal(x[5], lp), t
+            assert torch.equal(x[1][3].lens, x[2][3].lens) and torch.equal(x[1][2], x[2][2])
+            torch.cuda.synchronize()
+
+
+def test_other_streams(gpu):
+    """Work enqueued on the current stream of the caller, behind what it waits
+    for there."""
+    c = attention_case(2, 8, 2, 128, 16, [1], [3000, 40], BF16, 13)
+    want = sb.paged_attention(**c, **bounds(c))
+    stream = torch.cuda.Stream()
+    q = torch.zeros_like(c["q"])
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        big = torch.randn(4096, 4096, device="cuda")
+        for _ in range(10):
+            big = big @ big * 0.01
+        q.copy_(c["q"])
+        got = sb.paged_attention(**dict(c, q=q), **bounds(c))
+    stream.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_python_refusals(gpu):
+    c = attention_case(2, 4, 2, 64, 16, [1], [30, 40], BF16, 1)
+    kw = bounds(c)
+    for name, bad in (("q", c["q"].float()), ("q", c["q"].cpu()), ("q", c["q"].transpose(1, 2)), ("k_cache", c["k_cache"].half()),
+                      ("v_cache", c["v_cache"][:-1]), ("table", c["table"].long()), ("lens", c["lens"][:1]), ("q_start", c["q_start"].cpu()),
+                      ("q", c["q"][0])):
+        with pytest.raises(ValueError):
+            sb.paged_attention(**dict(c, **{name: bad}), **kw)
+    with pytest.raises(ValueError, match="overlap"):
+        sb.paged_attention(**c, **kw, out=c["q"][:1].expand(2, 4, 64))
+    with pytest.raises(ValueError, match="backward"):
+        sb.paged_attention(**dict(c, q=c["q"].clone().requires_grad_()), **kw)
+    for over in (dict(window=-1), dict(max_kv=-1), dict(scale=math.nan)):
+        with pytest.raises(sb.decoder.N.StreambeamError):
+            sb.paged_attention(**c, **dict(kw, **over))
+    odd = torch.zeros(2, 4, 68, dtype=BF16, device="cuda")[:, :, 2:66]   # rows at addresses of 4 bytes
+    with pytest.raises(sb.decoder.N.StreambeamError, match="16-byte|multiple of 8"):
+        sb.paged_attention(**dict(c, q=odd), **kw)
+    r = rope_case(3, 4, 2, 64, 32, BF16, 1)
+    for name, bad in (("k", r["k"][:2]), ("v", r["v"][:, :1]), ("positions", r["positions"].long()), ("slots", r["slots"].int()),
+                      ("inv_freq", r["inv_freq"].float()), ("k_cache", r["k_cache"][:1].expand(5, 16, 2, 64)), ("q", r["q"].half())):
+        with pytest.raises(ValueError):
+            sb.rope_append(**dict(r, **{name: bad}))
+    with pytest.raises(ValueError, match="layout"):
+        sb.rope_append(**r, layout="both")
+    z, u = torch.zeros(3, 10, device="cuda"), torch.zeros(3, device="cuda")
+    for bad in (dict(top_k=u), dict(top_p=u[:2]), dict(temperature=u.double()), dict(min_p=u.cpu())):
+        with pytest.raises(ValueError):
+            sb.sample_tokens(z, u, **bad)
+    with pytest.raises(ValueError):
+        sb.sample_tokens(z.double(), u)
+    with pytest.raises(sb.decoder.N.StreambeamError):
+        sb.sample_tokens(torch.zeros(1, 262145, device="cuda"), u[:1])
+    with pytest.raises(ValueError, match="token_cap"):
+        sb.plan_pages(i32([1]), i32([1]), i32([1]), i32([1]), i32([[1]]), page_size=4, token_cap=-1)
