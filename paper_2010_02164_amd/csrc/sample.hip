@@ -1,11 +1,20 @@
 // One token per row of logits under temperature, top-k, top-p and min-p,
-// drawn with a given number.
+// drawn with a given number. One workgroup per row.
 //
 // Every filter keeps a prefix of the tokens ranked by (-z, index), so the kept
 // tokens are those above one cut (a logit and, among its equals, an index),
-// and nothing has to be sorted: a radix search over the ordered bits of the
-// logits finds where a sum of counts (top-k) or of weights (top-p) passes its
-// limit. The draw then runs over the kept tokens in index order.
+// and nothing is sorted: a radix search over the ordered bits of the logits
+// finds where a sum of counts (top-k) or of weights (top-p) passes its limit,
+// and the draw is the same search over the kept tokens' indexes.
+//
+// Most rows are read once: a sample of the row (four 16-byte pieces a thread)
+// gives a bound that the k-th largest logit cannot be below - the k-th largest
+// of the threads' largest -, the pass over the row lists the tokens from that
+// bound on (about k times the row's share in the sample, some hundreds), and
+// all searches run on the list in registers and LDS. min-p alone bounds them
+// likewise by the sample's largest. top-p without top-k needs every weight: a
+// second pass adds them up into bins of equal ratio, which names the bin that
+// the cut is in, a third lists that bin, a fourth draws; they read caches.
 //
 // Weights are whole multiples of 2^-44 in 64-bit integers: up to 2^18 of them
 // add up without rounding or overflow, in any order, so that partial sums of
@@ -18,16 +27,19 @@ namespace sb {
 namespace {
 
 typedef unsigned long long u64;
+typedef unsigned int u4 __attribute__((ext_vector_type(4)));
 
 constexpr int SM_THREADS = 1024;
 constexpr int SM_WAVES = SM_THREADS / 64;
-constexpr double ONE = 0x1p44;   // the weight of the largest logit
-
-template <int DT>
-__device__ __forceinline__ float load_logit(const void *row, int i) {
-  if constexpr (DT == SB_F32) return static_cast<const float *>(row)[i];
-  else return Half<DT>::to_float(static_cast<const uint16_t *>(row)[i]);
-}
+constexpr double ONE = 0x1p44;        // the weight of the largest logit
+constexpr int LIST_PER = 4, LIST_MAX = LIST_PER * SM_THREADS;
+constexpr int BIN_BITS = 9, BINS = 1 << BIN_BITS;
+constexpr int TAB_BITS = 9;           // 2^x by a table of 2^(i / 512) and a cubic
+// The largest top-k that is read off the sample: of a row eight times the
+// sample (the largest fp32 ones of common vocabularies) the list then holds
+// about 8 times as many tokens, at most what it has room for.
+constexpr int SAMPLED_K = 512;
+constexpr int BATCH = 4;              // 16-byte pieces a thread loads at once
 
 // The bits of z in an order that ascends with it; NaN counts as -inf.
 __device__ __forceinline__ uint32_t order_bits(float z) {
@@ -35,14 +47,97 @@ __device__ __forceinline__ uint32_t order_bits(float z) {
   const uint32_t b = __float_as_uint(z + 0.0f);   // -0 is 0
   return b ^ (b >> 31 ? 0xFFFFFFFFu : 0x80000000u);
 }
+__device__ __forceinline__ float from_order(uint32_t b) { return __uint_as_float(b ^ (b >> 31 ? 0x80000000u : 0xFFFFFFFFu)); }
+constexpr uint32_t LOWEST = 0x007FFFFFu;   // order_bits(-inf)
+
+// A row: elements before the first 16-byte address, whole pieces, the rest.
+template <int DT>
+struct Row {
+  static constexpr int VEC = DT == SB_F32 ? 4 : 8, ES = DT == SB_F32 ? 4 : 2;
+  const unsigned char *at;
+  int V, head, pieces;
+  __device__ __forceinline__ Row(const void *row, int n) : at(static_cast<const unsigned char *>(row)), V(n) {
+    head = min((int)((16 - (reinterpret_cast<uintptr_t>(at) & 15)) & 15) / ES, V);
+    pieces = (V - head) / VEC;
+  }
+  __device__ __forceinline__ float one(int i) const {
+    if constexpr (DT == SB_F32) return reinterpret_cast<const float *>(at)[i];
+    else return Half<DT>::to_float(reinterpret_cast<const uint16_t *>(at)[i]);
+  }
+  __device__ __forceinline__ u4 piece(int j) const { return *reinterpret_cast<const u4 *>(at + head * ES + (size_t)j * 16); }
+  static __device__ __forceinline__ void unpack(const u4 &x, float (&z)[VEC]) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      if constexpr (DT == SB_F32) z[i] = __uint_as_float(x[i]);
+      else z[i] = Half<DT>::to_float(i & 1 ? x[i >> 1] >> 16 : x[i >> 1] & 0xFFFFu);
+    }
+  }
+  // f(z, i0) for pieces first, first + step, ... of [first, end): values i0 .. i0 + VEC - 1.
+  template <typename F>
+  __device__ __forceinline__ void each_piece(int first, int end, int step, F f) const {
+    for (int j0 = first; j0 < end; j0 += BATCH * step) {
+      u4 x[BATCH];
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b)
+        if (j0 + b * step < end) x[b] = piece(j0 + b * step);
+#pragma unroll
+      for (int b = 0; b < BATCH; ++b) {
+        if (j0 + b * step >= end) break;
+        float z[VEC];
+        unpack(x[b], z);
+        f(z, head + (j0 + b * step) * VEC);
+      }
+    }
+  }
+  // The elements outside the pieces, one a thread, -inf in the other places.
+  template <typename F>
+  __device__ __forceinline__ void each_end(F f) const {
+    const int rest = V - pieces * VEC;
+    if ((int)threadIdx.x < rest) {
+      const int i = (int)threadIdx.x < head ? (int)threadIdx.x : pieces * VEC + (int)threadIdx.x;
+      float z[VEC];
+      z[0] = one(i);
+#pragma unroll
+      for (int e = 1; e < VEC; ++e) z[e] = -INFINITY;
+      f(z, i);
+    }
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(F f) const {
+    each_piece(threadIdx.x, pieces, SM_THREADS, f);
+    each_end(f);
+  }
+};
+
+struct Shared {
+  double tab[1 << TAB_BITS];   // 2^(i / 512)
+  u64 hist[BINS];
+  u64 part[SM_WAVES];
+  uint32_t key[LIST_MAX];      // listed tokens: order bits
+  int idx[LIST_MAX];           // and indexes
+  u64 rest, at_cut;
+  uint32_t digit;
+  int n, token;
+};
 
 // A row's weights: 2^44 exp((z - top) / T), rounded.
 struct Weigher {
+  const double *tab;
   double top, c;   // c = log2(e) / T
-  __device__ __forceinline__ u64 operator()(float z) const {
-    const double x = fmin(fmax(((double)z - top) * c, -64.0), 0.0);   // NaN, and -inf with T = inf: -64
-    return (u64)rint(exp2(x) * ONE);
+  // log2 of the weight (of the largest: 0). NaN, and -inf with T = inf: -64.
+  __device__ __forceinline__ double log2w(float z) const { return fmin(fmax(((double)z - top) * c, -64.0), 0.0); }
+  // x = n / 512 + r with |r| <= 2^-10: 2^x = 2^(n / 512) (1 + r ln 2 + ...);
+  // the cubic leaves out (2^-10 ln 2)^4 / 24 = 2^-46.7.
+  __device__ __forceinline__ u64 of(double x) const {
+    constexpr double MAGIC = 0x1.8p43;   // its last bit is worth 2^-9
+    const double t = x + MAGIC;
+    const int n = (int)__double2loint(t);
+    const double r = x - (t - MAGIC);
+    const double y = fma(fma(fma(r, 0.055504108664821580, 0.24022650695910071), r, 0.69314718055994531), r, 1.0);
+    const double w = ldexp(tab[n & ((1 << TAB_BITS) - 1)] * y, 44 + (n >> TAB_BITS));
+    return (u64)__double_as_longlong(w + 0x1p52) & 0xFFFFFFFFFFFFFull;   // w <= 2^44, rounded to a whole number
   }
+  __device__ __forceinline__ u64 operator()(float z) const { return of(log2w(z)); }
 };
 
 __device__ __forceinline__ u64 wave_scan(u64 v) {   // inclusive
@@ -53,18 +148,13 @@ __device__ __forceinline__ u64 wave_scan(u64 v) {   // inclusive
   }
   return v;
 }
-
-struct Shared {
-  u64 hist[256];
-  u64 part[SM_WAVES];
-  u64 rest;          // search: what of the limit is left within the digit
-  uint32_t digit;
-  int token;
-};
-
-__device__ __forceinline__ u64 block_sum(u64 v, Shared &sh) {
+__device__ __forceinline__ u64 wave_sum(u64 v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+__device__ __forceinline__ u64 block_sum(u64 v, Shared &sh) {
+  v = wave_sum(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = v;
   __syncthreads();
@@ -73,168 +163,420 @@ __device__ __forceinline__ u64 block_sum(u64 v, Shared &sh) {
   for (int i = 0; i < SM_WAVES; ++i) s += sh.part[i];
   return s;
 }
-
-// The logit (as order bits) at which the weights, added from the largest logit
-// down, first total more than `limit`, which they do; `rest`: limit less what
-// lies above that logit. weight(bits, z) is a token's weight.
-template <int DT, typename F>
-__device__ __forceinline__ uint32_t radix_search(const void *row, int V, u64 limit, F weight, u64 &rest, Shared &sh) {
-  uint32_t prefix = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < 256; i += SM_THREADS) sh.hist[i] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < V; i += SM_THREADS) {
-      const float z = load_logit<DT>(row, i);
-      const uint32_t b = order_bits(z);
-      if (shift == 24 || (b >> (shift + 8)) == prefix) {
-        const u64 w = weight(b, z);
-        if (w) atomicAdd(&sh.hist[(b >> shift) & 255u], w);
-      }
-    }
-    __syncthreads();
-    if (threadIdx.x < 64) {   // four digits a lane, from 255 down
-      const int d0 = 255 - 4 * (int)threadIdx.x;
-      u64 s = 0;
-      for (int j = 0; j < 4; ++j) s += sh.hist[d0 - j];
-      u64 before = wave_scan(s) - s;
-      for (int j = 0; j < 4; ++j) {
-        const u64 h = sh.hist[d0 - j];
-        if (before <= limit && limit < before + h) {
-          sh.digit = (uint32_t)(d0 - j);
-          sh.rest = limit - before;
-        }
-        before += h;
-      }
-    }
-    __syncthreads();
-    prefix = (prefix << 8) | sh.digit;
-    limit = sh.rest;
-  }
-  rest = limit;
-  return prefix;
+__device__ __forceinline__ uint32_t block_max(uint32_t v, Shared &sh) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = v;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < SM_WAVES; ++i) v = max(v, (uint32_t)sh.part[i]);
+  return v;
 }
 
-// The smallest index up to which the weights total more than `limit`, which
-// they do. Each wave adds up a stretch of the row; the one that passes the
-// limit walks its stretch again.
-template <int DT, typename F>
-__device__ __forceinline__ int locate(const void *row, int V, u64 limit, F weight, Shared &sh) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int len = (V + SM_THREADS - 1) / SM_THREADS * 64;
-  const int lo = min(w * len, V), hi = min(lo + len, V);
-  u64 s = 0;
-  for (int i = lo + lane; i < hi; i += 64) s += weight(i, load_logit<DT>(row, i));
+__device__ __forceinline__ void clear_bins(Shared &sh) {
+  __syncthreads();
+  if (threadIdx.x < BINS) sh.hist[threadIdx.x] = 0;
+  __syncthreads();
+}
+// The bin at which the bins' sum, from bin 0 up, first passes `limit`; the last
+// one where it never does. rest: limit less what lies before the bin; at: what
+// is in it.
+__device__ __forceinline__ uint32_t find_bin(u64 limit, u64 &rest, u64 &at, Shared &sh) {
+  constexpr int PER = BINS / 64;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    u64 h[PER], s = 0;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    for (int j = 0; j < PER; ++j) s += h[j] = sh.hist[threadIdx.x * PER + j];
+    u64 before = wave_scan(s) - s;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const bool last = threadIdx.x == 63 && j == PER - 1;
+      if (before <= limit && (limit < before + h[j] || last)) {
+        sh.digit = threadIdx.x * PER + j;
+        sh.rest = limit - before;
+        sh.at_cut = h[j];
+      }
+      before += h[j];
+    }
+  }
+  __syncthreads();
+  rest = sh.rest;
+  at = sh.at_cut;
+  return sh.digit;
+}
+
+// Each thread's share of a list, in registers.
+struct Items {
+  uint32_t key[LIST_PER];
+  int idx[LIST_PER];
+  u64 w[LIST_PER];   // 0: not there, or not kept
+};
+
+// The key at which the items' weights, in ascending order of their keys, first
+// total more than `limit`, which they do. keys < 2^bits; `drop` low bits are
+// left out of the search (and of the result).
+template <typename K>
+__device__ __forceinline__ uint32_t list_search(const Items &it, K key, int bits, int drop, u64 limit, u64 &rest, u64 &at, Shared &sh) {
+  uint32_t prefix = 0;
+  int shift = bits;
+  do {
+    const int take = min(BIN_BITS, shift - drop);
+    shift -= take;
+    clear_bins(sh);
+#pragma unroll
+    for (int j = 0; j < LIST_PER; ++j) {
+      const uint32_t k = key(j);
+      if (it.w[j] && (shift + take >= 32 || (k >> (shift + take)) == prefix)) atomicAdd(&sh.hist[(k >> shift) & ((1u << take) - 1)], it.w[j]);
+    }
+    prefix = (prefix << take) | find_bin(limit, rest, at, sh);
+    limit = rest;
+  } while (shift > drop);
+  return prefix << drop;
+}
+
+// Likewise over the row's tokens, from the largest logit down, 8 bits a pass;
+// weight(bits, z) is a token's weight. For rows whose cut lies among more equal
+// or nearly equal logits than the list holds.
+template <int DT, typename F>
+__device__ __noinline__ uint32_t row_search(const Row<DT> &row, u64 limit, F weight, u64 &rest, Shared &sh) {
+  uint32_t prefix = 0;
+  for (int shift = 24; shift >= 0; shift -= 8) {
+    clear_bins(sh);
+    row.each([&](const float (&z)[Row<DT>::VEC], int) {
+#pragma unroll
+      for (int e = 0; e < Row<DT>::VEC; ++e) {
+        const uint32_t b = order_bits(z[e]), d = ~b;
+        if (shift == 24 || (d >> (shift + 8)) == prefix) {
+          const u64 w = weight(b, z[e]);
+          if (w) atomicAdd(&sh.hist[(d >> shift) & 255u], w);
+        }
+      }
+    });
+    u64 at;
+    prefix = (prefix << 8) | find_bin(limit, rest, at, sh);
+    limit = rest;
+  }
+  return ~prefix;
+}
+
+// The smallest index up to which the weights total more than limit(total),
+// which they do. Each wave adds up a stretch of the row, then all threads
+// share the stretch that passes the limit.
+template <int DT, typename F, typename L>
+__device__ __forceinline__ int locate(const Row<DT> &row, F weight, L limit_of, u64 &total, Shared &sh) {
+  constexpr int VEC = Row<DT>::VEC;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int len = (row.pieces + SM_WAVES - 1) / SM_WAVES;   // pieces a wave
+  u64 s = 0;
+  auto add = [&](const float (&z)[VEC], int i0) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) s += weight(i0 + e, z[e]);
+  };
+  row.each_piece(min(w * len, row.pieces) + lane, min((w + 1) * len, row.pieces), 64, add);
+  // The row's ends belong to the first and the last stretch.
+  if (w == 0 && lane < row.head) s += weight(lane, row.one(lane));
+  const int tail0 = row.head + row.pieces * VEC;
+  if (w == SM_WAVES - 1 && tail0 + lane < row.V) s += weight(tail0 + lane, row.one(tail0 + lane));
+  s = wave_sum(s);
   __syncthreads();
   if (lane == 0) sh.part[w] = s;
   __syncthreads();
-  u64 before = 0;
-  for (int i = 0; i < w; ++i) before += sh.part[i];
-  if (before <= limit && limit < before + s) {
-    for (int i0 = lo; i0 < hi; i0 += 64) {
-      const int i = i0 + lane;
-      const u64 x = wave_scan(i < hi ? weight(i, load_logit<DT>(row, i)) : 0);
-      const u64 m = __ballot(before + x > limit);
-      if (m) {
-        if (lane == 0) sh.token = i0 + __builtin_ctzll(m);
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < SM_WAVES; ++i) total += sh.part[i];
+  u64 limit = limit_of(total), before = 0;
+  int x = 0;
+  while (x < SM_WAVES - 1 && before + sh.part[x] <= limit) before += sh.part[x++];
+  limit -= before;
+  const int lo = x == 0 ? 0 : row.head + min(x * len, row.pieces) * VEC;
+  const int hi = x == SM_WAVES - 1 ? row.V : row.head + min((x + 1) * len, row.pieces) * VEC;
+  const int per = (hi - lo + SM_THREADS - 1) / SM_THREADS, a0 = min(lo + (int)threadIdx.x * per, hi), a1 = min(a0 + per, hi);
+  u64 mine = 0;
+  for (int i = a0; i < a1; ++i) mine += weight(i, row.one(i));
+  u64 upto = wave_scan(mine);
+  __syncthreads();
+  if (lane == 63) sh.part[w] = upto;
+  __syncthreads();
+  for (int i = 0; i < w; ++i) upto += sh.part[i];
+  if (upto - mine <= limit && limit < upto) {
+    u64 run = upto - mine;
+    for (int i = a0; i < a1; ++i) {
+      run += weight(i, row.one(i));
+      if (run > limit) {
+        sh.token = i;
         break;
       }
-      before += __shfl(x, 63, 64);
     }
   }
   __syncthreads();
   return sh.token;
 }
 
-template <int DT>
-__global__ __launch_bounds__(SM_THREADS) void k_sample(sb_sample_args a) {
-  __shared__ Shared sh;
-  const int r = blockIdx.x, V = a.vocab;
-  const size_t es = DT == SB_F32 ? 4 : 2;
-  const void *row = static_cast<const unsigned char *>(a.logits) + (size_t)r * a.row_stride * es;
-
-  uint32_t best = 0;
-  for (int i = threadIdx.x; i < V; i += SM_THREADS) best = max(best, order_bits(load_logit<DT>(row, i)));
+// Takes this thread's share of the list; weight(bits).
+template <typename F>
+__device__ __forceinline__ void take_list(Items &it, int n, F weight, const Shared &sh) {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) best = max(best, (uint32_t)__shfl_xor((int)best, o, 64));
-  if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = best;
-  __syncthreads();
-  for (int i = 0; i < SM_WAVES; ++i) best = max(best, (uint32_t)sh.part[i]);
-  const uint32_t lowest = order_bits(-INFINITY);
-  if (best == lowest) {
-    if (threadIdx.x == 0) {
+  for (int j = 0; j < LIST_PER; ++j) {
+    const int at = j * SM_THREADS + threadIdx.x;
+    const bool on = at < n;
+    it.key[j] = on ? sh.key[at] : 0;
+    it.idx[j] = on ? sh.idx[at] : 0;
+    it.w[j] = on ? weight(it.key[j]) : 0;
+  }
+}
+
+__device__ __forceinline__ void list_token(uint32_t bits, int i, Shared &sh) {
+  const int at = atomicAdd(&sh.n, 1);
+  if (at < LIST_MAX) {
+    sh.key[at] = bits;
+    sh.idx[at] = i;
+  }
+}
+
+__device__ __forceinline__ int bits_of(uint32_t x) { return 32 - __clz((int)x); }   // x < 2^bits; 0 for 0
+
+template <int DT>
+__global__ __launch_bounds__(SM_THREADS, 8) void k_sample(sb_sample_args a) {
+  constexpr int VEC = Row<DT>::VEC;
+  __shared__ Shared sh;
+  const int r = blockIdx.x, V = a.vocab, tid = threadIdx.x;
+  const Row<DT> row(static_cast<const unsigned char *>(a.logits) + (size_t)r * a.row_stride * Row<DT>::ES, V);
+  const float T = a.temperature ? a.temperature[r] : 1.0f;
+  const int k = a.top_k && a.top_k[r] > 0 && a.top_k[r] < V ? a.top_k[r] : 0;
+  const float p = a.top_p && a.top_p[r] < 1.0f ? a.top_p[r] : 1.0f;
+  const float mp = a.min_p && a.min_p[r] > 0.0f ? fminf(a.min_p[r], 1.0f) : 0.0f;
+  const float u = a.u[r];
+  const bool greedy = !(T > 0.0f);
+  if (tid < (1 << TAB_BITS)) sh.tab[tid] = exp2(tid * (1.0 / (1 << TAB_BITS)));
+  if (tid == 0) sh.n = 0;
+
+  // The sample: BATCH pieces a thread, from as many places of the row.
+  const int apart = max((row.pieces + BATCH - 1) / BATCH, SM_THREADS);
+  u4 x[BATCH];
+  float zm = -INFINITY;
+#pragma unroll
+  for (int b = 0; b < BATCH; ++b) {
+    const int j = b * apart + tid;
+    if (j < row.pieces) {
+      x[b] = row.piece(j);
+      float z[VEC];
+      Row<DT>::unpack(x[b], z);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) zm = fmaxf(zm, z[e]);
+    }
+  }
+  const uint32_t seen = block_max(order_bits(zm), sh);   // (its barriers also publish tab and n)
+  // Whether the tokens that matter are read off the sample, and from which on.
+  const bool sampled = greedy || (k > 0 && k <= SAMPLED_K) || (k == 0 && p == 1.0f && mp > 0.0f);
+  float bound = -INFINITY;
+  if (greedy) {
+    bound = from_order(seen);
+  } else if (sampled) {
+    if (k > 0) {
+      Items it;
+      it.key[0] = seen - order_bits(zm);
+      it.w[0] = 1;
+#pragma unroll
+      for (int j = 1; j < LIST_PER; ++j) it.w[j] = 0, it.key[j] = 0;
+      // 18 bits of it: rounded away from the largest, which keeps it a bound.
+      u64 rest, at;
+      const uint32_t d = list_search(it, [&](int j) { return it.key[j]; }, 32, 14, (u64)(k - 1), rest, at, sh) | 0x3FFFu;
+      bound = from_order(seen - min(d, seen - LOWEST));
+    }
+    // min-p keeps z >= top + T ln(min_p), top at least the sample's (less a
+    // little for the rounding here).
+    if (p == 1.0f && mp > 0.0f && from_order(seen) < INFINITY) {
+      const double b = (double)from_order(seen) + (double)T * log((double)mp);
+      bound = fmaxf(bound, (float)(b - 1e-6 * fabs(b) - 1e-30));
+    }
+  }
+
+  // The pass over the row: its largest logit, its smallest finite one, and
+  // the tokens from the bound on.
+  zm = -INFINITY;
+  float zl = INFINITY;
+  auto look = [&](const float (&z)[VEC], int i0) {
+    float m = z[0];
+#pragma unroll
+    for (int e = 1; e < VEC; ++e) m = fmaxf(m, z[e]);
+    zm = fmaxf(zm, m);
+    if (sampled) {
+      if (m >= bound && m > -INFINITY) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (z[e] >= bound && z[e] > -INFINITY) list_token(order_bits(z[e]), i0 + e, sh);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) zl = fminf(zl, z[e] > -INFINITY ? z[e] : INFINITY);
+    }
+  };
+#pragma unroll
+  for (int b = 0; b < BATCH; ++b) {
+    const int j = b * apart + tid;
+    if (j < row.pieces) {
+      float z[VEC];
+      Row<DT>::unpack(x[b], z);
+      look(z, row.head + j * VEC);
+    }
+  }
+  if (apart > SM_THREADS)
+    for (int b = 0; b < BATCH; ++b) row.each_piece(b * apart + SM_THREADS + tid, min((b + 1) * apart, row.pieces), SM_THREADS, look);
+  row.each_end(look);
+  const uint32_t best = block_max(order_bits(zm), sh);
+  if (best == LOWEST) {
+    if (tid == 0) {
       a.tokens[r] = -1;
       if (a.logprobs) a.logprobs[r] = -INFINITY;
     }
     return;
   }
-  const float top = __uint_as_float(best ^ (best >> 31 ? 0x80000000u : 0xFFFFFFFFu));
-  const float T = a.temperature ? a.temperature[r] : 1.0f;
+  const float top = from_order(best);
+  // (The largest logit +inf: 10^300 instead, below which all others weigh nothing.)
+  const Weigher weigh{sh.tab, top == INFINITY ? 1e300 : (double)top, 1.4426950408889634074 / (double)T};
+  const u64 floor_w = mp > 0.0f ? (u64)ceil((double)mp * ONE) : 0;
+  const float uc = u > 0.0f ? fminf(u, 1.0f) : 0.0f;
+  auto draw_limit = [=](u64 total) { return min((u64)((double)uc * (double)total), total - 1); };
+  // Kept where the weights ranked before total less than p z_k, so at most
+  // this: the cut is where they first total more.
+  auto top_p_limit = [=](u64 z_k) { return (u64)fmax(ceil((double)p * (double)z_k), 1.0) - 1; };
 
-  // Kept: order bits above `cut`, or equal to it with an index up to `cut_i`.
-  uint32_t cut = 0;
-  int cut_i = V;
-  double total = 1.0, x_tok = 0.0;
   int token;
-  if (!(T > 0.0f)) {
-    token = locate<DT>(row, V, 0, [=](int, float z) { return (u64)(order_bits(z) == best); }, sh);
+  u64 total;
+  const int n = sh.n;
+  if (sampled && n <= LIST_MAX) {
+    Items it;
+    take_list(it, n, [&](uint32_t b) { return greedy ? (u64)(b == best) : weigh(from_order(b)); }, sh);
+    if (!greedy) {
+      const int bits = bits_of(best - order_bits(bound));
+      // Leaves the weights of those up to the cut, of its equals the first
+      // `rest` / (what each adds) + 1.
+      auto cut_at = [&](uint32_t d, u64 before, u64 each, u64 at) {
+        int last = V;
+        if (at > before + each) {   // not all of its equals stay
+          Items eq = it;
+#pragma unroll
+          for (int j = 0; j < LIST_PER; ++j) eq.w[j] = it.w[j] && best - it.key[j] == d;
+          u64 rest, a2;
+          last = (int)list_search(eq, [&](int j) { return (uint32_t)eq.idx[j]; }, bits_of(V - 1), 0, before / each, rest, a2, sh);
+        }
+#pragma unroll
+        for (int j = 0; j < LIST_PER; ++j) {
+          const uint32_t dj = best - it.key[j];
+          if (dj > d || (dj == d && it.idx[j] > last)) it.w[j] = 0;
+        }
+      };
+      if (k > 0 && k < n) {
+        Items count = it;
+#pragma unroll
+        for (int j = 0; j < LIST_PER; ++j) count.w[j] = j * SM_THREADS + tid < n;
+        u64 rest, at;
+        const uint32_t d = list_search(count, [&](int j) { return best - count.key[j]; }, bits, 0, (u64)(k - 1), rest, at, sh);
+        cut_at(d, rest, 1, at);
+      }
+      if (p < 1.0f) {
+        u64 s = 0;
+#pragma unroll
+        for (int j = 0; j < LIST_PER; ++j) s += it.w[j];
+        const u64 z_k = block_sum(s, sh), limit = top_p_limit(z_k);
+        if (limit < z_k) {
+          u64 rest, at;
+          const uint32_t d = list_search(it, [&](int j) { return best - it.key[j]; }, bits, 0, limit, rest, at, sh);
+          cut_at(d, rest, weigh(from_order(best - d)), at);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < LIST_PER; ++j)
+        if (it.w[j] < floor_w) it.w[j] = 0;
+    }
+    u64 s = 0, rest, at;
+#pragma unroll
+    for (int j = 0; j < LIST_PER; ++j) s += it.w[j];
+    total = block_sum(s, sh);
+    token = (int)list_search(it, [&](int j) { return (uint32_t)it.idx[j]; }, bits_of(V - 1), 0, greedy ? 0 : draw_limit(total), rest, at, sh);
+    if (greedy) total = (u64)ONE;
   } else {
-    // (The largest logit +inf: 10^300 instead, below which all others weigh nothing.)
-    const Weigher weigh{top == INFINITY ? 1e300 : (double)top, 1.4426950408889634074 / (double)T};
-    const int k = a.top_k ? a.top_k[r] : 0;
-    const float p = a.top_p ? a.top_p[r] : 1.0f, mp = a.min_p ? a.min_p[r] : 0.0f;
+    // Kept: order bits above `cut`, or equal to it with an index up to `cut_i`.
+    uint32_t cut = 0;
+    int cut_i = V;
     auto kept = [&](int i, uint32_t b) { return b > cut || (b == cut && i <= cut_i); };
-    // Of the tokens equal to the cut the first `rest` + 1 stay.
-    auto cut_at = [&](uint32_t bits, u64 rest) {
-      const int last = locate<DT>(row, V, rest, [=](int, float z) { return (u64)(order_bits(z) == bits); }, sh);
+    auto cut_row = [&](uint32_t bits, u64 nth) {
+      u64 t;
+      const int last = locate<DT>(row, [=](int, float z) { return (u64)(order_bits(z) == bits); }, [=](u64) { return nth; }, t, sh);
       if (bits > cut) cut_i = last;
       else if (bits == cut) cut_i = min(cut_i, last);
       cut = max(cut, bits);
     };
-    if (k > 0 && k < V) {
-      u64 rest;
-      const uint32_t bits = radix_search<DT>(row, V, (u64)(k - 1), [](uint32_t, float) { return (u64)1; }, rest, sh);
-      cut_at(bits, rest);
-    }
-    if (p < 1.0f) {
-      u64 z_k = 0;
-      for (int i = threadIdx.x; i < V; i += SM_THREADS) {
-        const float z = load_logit<DT>(row, i);
-        z_k += kept(i, order_bits(z)) ? weigh(z) : 0;
+    // Bins of equal ratio, BINS - 1 from the largest weight down to the
+    // smallest one there is (or that can matter), what is below in the last.
+    const float low = sampled ? -INFINITY : -from_order(block_max(order_bits(-zl), sh));   // (the full list: not looked for)
+    auto cut_by = [&](bool count, double reach, auto limit_of) {
+      const double range = fmin(fmax(-weigh.log2w(low), 1e-9), reach), scale = (BINS - 1) / range * (1 - 1e-9);
+      auto bin = [&](double x) { return (int)fmin(-x * scale, (double)(BINS - 1)); };
+      clear_bins(sh);
+      u64 below = 0, all = 0;
+      row.each([&](const float (&z)[VEC], int i0) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const uint32_t b = order_bits(z[e]);
+          if (b == LOWEST || !kept(i0 + e, b)) continue;
+          const double xw = weigh.log2w(z[e]);
+          const u64 w = count ? 1 : weigh.of(xw);
+          all += w;
+          const int at = bin(xw);
+          if (at < BINS - 1) atomicAdd(&sh.hist[at], w);
+          else below += w;
+        }
+      });
+      below = block_sum(below, sh);
+      all = block_sum(all, sh);
+      if (tid == 0) sh.hist[BINS - 1] = below;
+      const u64 limit = limit_of(all);
+      if (limit >= all) return;
+      u64 rest, at;
+      const int target = (int)find_bin(limit, rest, at, sh);
+      if (tid == 0) sh.n = 0;
+      __syncthreads();
+      row.each([&](const float (&z)[VEC], int i0) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const uint32_t b = order_bits(z[e]);
+          if (b != LOWEST && bin(weigh.log2w(z[e])) == target && kept(i0 + e, b)) list_token(b, i0 + e, sh);
+        }
+      });
+      __syncthreads();
+      const int m = sh.n;
+      uint32_t bits;
+      if (m <= LIST_MAX) {
+        Items it;
+        take_list(it, m, [&](uint32_t b) { return count ? (u64)1 : weigh(from_order(b)); }, sh);
+        bits = best - list_search(it, [&](int j) { return best - it.key[j]; }, 32, 0, rest, rest, at, sh);
+      } else {
+        bits = row_search<DT>(row, limit, [=](uint32_t b, float z) { return b == LOWEST || b < cut ? 0 : count ? (u64)1 : weigh(z); }, rest, sh);
       }
-      z_k = block_sum(z_k, sh);
-      // Kept where the weights ranked before total less than p z_k, so at
-      // most `limit`: the cut is where they first total more.
-      const u64 limit = (u64)fmax(ceil((double)p * (double)z_k), 1.0) - 1;
-      if (limit < z_k) {
-        // (Ties at the top-k cut weigh the same, so leaving out the kept ones'
-        // equals behind cut_i changes no sum before the last kept one.)
-        u64 rest;
-        const uint32_t bits = radix_search<DT>(row, V, limit, [=](uint32_t b, float z) { return b >= cut ? weigh(z) : 0; }, rest, sh);
-        const float z = __uint_as_float(bits ^ (bits >> 31 ? 0x80000000u : 0xFFFFFFFFu));
-        cut_at(bits, rest / weigh(z));
-      }
-    }
-    const u64 floor_w = mp > 0.0f ? (u64)ceil((double)fminf(mp, 1.0f) * ONE) : 0;
-    auto weight = [&](int i, float z) {
-      const u64 w = weigh(z);
-      return kept(i, order_bits(z)) && w >= floor_w ? w : 0;
+      cut_row(bits, count ? rest : rest / weigh(from_order(bits)));
     };
-    u64 z_all = 0;
-    for (int i = threadIdx.x; i < V; i += SM_THREADS) z_all += weight(i, load_logit<DT>(row, i));
-    z_all = block_sum(z_all, sh);
-    const float u = a.u[r];
-    const u64 limit = min((u64)((double)(u > 0.0f ? fminf(u, 1.0f) : 0.0f) * (double)z_all), z_all - 1);
-    token = locate<DT>(row, V, limit, weight, sh);
-    total = (double)z_all / ONE;
-    const float z = load_logit<DT>(row, token);
-    x_tok = top == INFINITY ? 0.0 : ((double)z - (double)top) / (double)T;
+    if (!greedy && k > 0) cut_by(true, 64.0, [=](u64) { return (u64)(k - 1); });
+    // Weights below (1 - p) / V of the largest total less than 1 - p of all:
+    // the cut is not among them (one octave and more to spare for rounding).
+    if (!greedy && p < 1.0f) cut_by(false, fmin(2.0 + log2((double)V / fmax(1.0 - (double)p, 1e-9)), 64.0), top_p_limit);
+    auto weight = [&](int i, float z) -> u64 {
+      const uint32_t b = order_bits(z);
+      if (greedy) return b == best;
+      if (!kept(i, b)) return 0;
+      const u64 w = weigh(z);
+      return w >= floor_w ? w : 0;
+    };
+    token = locate<DT>(row, weight, [=](u64 t) { return greedy ? (u64)0 : draw_limit(t); }, total, sh);
+    if (greedy) total = (u64)ONE;
   }
-  if (threadIdx.x == 0) {
+  if (tid == 0) {
     a.tokens[r] = token;
-    if (a.logprobs) a.logprobs[r] = (float)(x_tok - log(total));
+    const double z = row.one(token);
+    const double xt = greedy || top == INFINITY ? 0.0 : (z - (double)top) / (double)T;
+    if (a.logprobs) a.logprobs[r] = (float)(xt - log((double)total / ONE));
   }
 }
 
