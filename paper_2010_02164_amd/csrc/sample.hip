@@ -8,13 +8,13 @@
 // and the draw is the same search over the kept tokens' indexes.
 //
 // Most rows are read once: a sample of the row (four 16-byte pieces a thread)
-// gives a bound that the k-th largest logit cannot be below - the k-th largest
-// of the threads' largest -, the pass over the row lists the tokens from that
-// bound on (about k times the row's share in the sample, some hundreds), and
-// all searches run on the list in registers and LDS. min-p alone bounds them
-// likewise by the sample's largest. top-p without top-k needs every weight: a
-// second pass adds them up into bins of equal ratio, which names the bin that
-// the cut is in, a third lists that bin, a fourth draws; they read caches.
+// gives a bound that the k-th largest logit hardly ever is below, the pass over
+// the row lists the tokens from that bound on, a few hundred, and all searches
+// run on the list in registers and LDS; a list of fewer than k tokens sends the
+// row the other way. min-p alone bounds the tokens by the sample's largest.
+// top-p without top-k needs every weight: a second pass adds them up into bins
+// of equal ratio, which names the bin that the cut is in, a third lists that
+// bin, a fourth draws; they read caches.
 //
 // Weights are whole multiples of 2^-44 in 64-bit integers: up to 2^18 of them
 // add up without rounding or overflow, in any order, so that partial sums of
@@ -35,11 +35,12 @@ constexpr double ONE = 0x1p44;        // the weight of the largest logit
 constexpr int LIST_PER = 4, LIST_MAX = LIST_PER * SM_THREADS;
 constexpr int BIN_BITS = 9, BINS = 1 << BIN_BITS;
 constexpr int TAB_BITS = 9;           // 2^x by a table of 2^(i / 512) and a cubic
-// The largest top-k that is read off the sample: of a row eight times the
-// sample (the largest fp32 ones of common vocabularies) the list then holds
-// about 8 times as many tokens, at most what it has room for.
-constexpr int SAMPLED_K = 512;
-constexpr int BATCH = 4;              // 16-byte pieces a thread loads at once
+// The largest top-k that is read off the sample: the list then aims at twice
+// as many tokens, and 256 more.
+constexpr int SAMPLED_K = 1536;
+// 16-byte pieces a thread loads at once: of the sample, and of a pass (4 there
+// made the code of the passes larger than the instruction cache).
+constexpr int SAMPLE = 4, BATCH = 2;
 
 // The bits of z in an order that ascends with it; NaN counts as -inf.
 __device__ __forceinline__ uint32_t order_bits(float z) {
@@ -75,6 +76,7 @@ struct Row {
   // f(z, i0) for pieces first, first + step, ... of [first, end): values i0 .. i0 + VEC - 1.
   template <typename F>
   __device__ __forceinline__ void each_piece(int first, int end, int step, F f) const {
+#pragma unroll 1
     for (int j0 = first; j0 < end; j0 += BATCH * step) {
       u4 x[BATCH];
 #pragma unroll
@@ -112,7 +114,7 @@ struct Row {
 struct Shared {
   double tab[1 << TAB_BITS];   // 2^(i / 512)
   u64 hist[BINS];
-  u64 part[SM_WAVES];
+  u64 part[SM_WAVES], ends[2][8];
   uint32_t key[LIST_MAX];      // listed tokens: order bits
   int idx[LIST_MAX];           // and indexes
   u64 rest, at_cut;
@@ -123,7 +125,9 @@ struct Shared {
 // A row's weights: 2^44 exp((z - top) / T), rounded.
 struct Weigher {
   const double *tab;
-  double top, c;   // c = log2(e) / T
+  double top, c;   // c = log2(e) / T. With a largest logit of +inf: 2^128 and 1, far from all others
+  __device__ __forceinline__ Weigher(const double *t, float largest, float T)
+      : tab(t), top(largest == INFINITY ? 0x1p128 : (double)largest), c(largest == INFINITY ? 1.0 : 1.4426950408889634074 / (double)T) {}
   // log2 of the weight (of the largest: 0). NaN, and -inf with T = inf: -64.
   __device__ __forceinline__ double log2w(float z) const { return fmin(fmax(((double)z - top) * c, -64.0), 0.0); }
   // x = n / 512 + r with |r| <= 2^-10: 2^x = 2^(n / 512) (1 + r ln 2 + ...);
@@ -131,14 +135,24 @@ struct Weigher {
   __device__ __forceinline__ u64 of(double x) const {
     constexpr double MAGIC = 0x1.8p43;   // its last bit is worth 2^-9
     const double t = x + MAGIC;
-    const int n = (int)__double2loint(t);
+    const int n = __double2loint(t);
     const double r = x - (t - MAGIC);
     const double y = fma(fma(fma(r, 0.055504108664821580, 0.24022650695910071), r, 0.69314718055994531), r, 1.0);
-    const double w = ldexp(tab[n & ((1 << TAB_BITS) - 1)] * y, 44 + (n >> TAB_BITS));
+    const double v = tab[n & ((1 << TAB_BITS) - 1)] * y;
+    // Its exponent raised by 44 + n / 512, between -20 and 44.
+    const double w = __hiloint2double(__double2hiint(v) + ((44 + (n >> TAB_BITS)) << 20), __double2loint(v));
     return (u64)__double_as_longlong(w + 0x1p52) & 0xFFFFFFFFFFFFFull;   // w <= 2^44, rounded to a whole number
   }
   __device__ __forceinline__ u64 operator()(float z) const { return of(log2w(z)); }
 };
+
+// x or 0, by a mask that the compiler does not turn into a branch around x:
+// the chains of operations of a piece's tokens are to run side by side.
+__device__ __forceinline__ u64 only_if(bool on, u64 x) {
+  uint32_t m = on ? 0xFFFFFFFFu : 0u;
+  asm("" : "+v"(m));
+  return (u64)((uint32_t)x & m) | ((u64)((uint32_t)(x >> 32) & m) << 32);
+}
 
 __device__ __forceinline__ u64 wave_scan(u64 v) {   // inclusive
 #pragma unroll
@@ -237,11 +251,12 @@ __device__ __forceinline__ uint32_t list_search(const Items &it, K key, int bits
 }
 
 // Likewise over the row's tokens, from the largest logit down, 8 bits a pass;
-// weight(bits, z) is a token's weight. For rows whose cut lies among more equal
+// weight(z) is a token's weight. For rows whose cut lies among more equal
 // or nearly equal logits than the list holds.
 template <int DT, typename F>
-__device__ __noinline__ uint32_t row_search(const Row<DT> &row, u64 limit, F weight, u64 &rest, Shared &sh) {
+__device__ __forceinline__ uint32_t row_search(const Row<DT> &row, u64 limit, F weight, u64 &rest, u64 &at, Shared &sh) {
   uint32_t prefix = 0;
+#pragma unroll 1
   for (int shift = 24; shift >= 0; shift -= 8) {
     clear_bins(sh);
     row.each([&](const float (&z)[Row<DT>::VEC], int) {
@@ -249,12 +264,11 @@ __device__ __noinline__ uint32_t row_search(const Row<DT> &row, u64 limit, F wei
       for (int e = 0; e < Row<DT>::VEC; ++e) {
         const uint32_t b = order_bits(z[e]), d = ~b;
         if (shift == 24 || (d >> (shift + 8)) == prefix) {
-          const u64 w = weight(b, z[e]);
+          const u64 w = weight(z[e]);
           if (w) atomicAdd(&sh.hist[(d >> shift) & 255u], w);
         }
       }
     });
-    u64 at;
     prefix = (prefix << 8) | find_bin(limit, rest, at, sh);
     limit = rest;
   }
@@ -262,53 +276,81 @@ __device__ __noinline__ uint32_t row_search(const Row<DT> &row, u64 limit, F wei
 }
 
 // The smallest index up to which the weights total more than limit(total),
-// which they do. Each wave adds up a stretch of the row, then all threads
-// share the stretch that passes the limit.
+// which they do; weights(z, i0, w) gives those of a piece. Each wave adds up a
+// stretch of pieces (the row's ends are stretches of their own), then all
+// threads share the stretch that passes the limit.
 template <int DT, typename F, typename L>
-__device__ __forceinline__ int locate(const Row<DT> &row, F weight, L limit_of, u64 &total, Shared &sh) {
+__device__ __forceinline__ int locate(const Row<DT> &row, F weights, L limit_of, u64 &total, Shared &sh) {
   constexpr int VEC = Row<DT>::VEC;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int len = (row.pieces + SM_WAVES - 1) / SM_WAVES;   // pieces a wave
   u64 s = 0;
-  auto add = [&](const float (&z)[VEC], int i0) {
+  row.each_piece(min(w * len, row.pieces) + lane, min((w + 1) * len, row.pieces), 64, [&](const float (&z)[VEC], int i0) {
+    u64 x[VEC];
+    weights(z, i0, x);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) s += weight(i0 + e, z[e]);
-  };
-  row.each_piece(min(w * len, row.pieces) + lane, min((w + 1) * len, row.pieces), 64, add);
-  // The row's ends belong to the first and the last stretch.
-  if (w == 0 && lane < row.head) s += weight(lane, row.one(lane));
-  const int tail0 = row.head + row.pieces * VEC;
-  if (w == SM_WAVES - 1 && tail0 + lane < row.V) s += weight(tail0 + lane, row.one(tail0 + lane));
+    for (int e = 0; e < VEC; ++e) s += x[e];
+  });
   s = wave_sum(s);
   __syncthreads();
   if (lane == 0) sh.part[w] = s;
+  // Ends: a wave each, one token a lane.
+  if (w < 2) {
+    const int i0 = w == 0 ? 0 : row.head + row.pieces * VEC, count = w == 0 ? row.head : row.V - i0;
+    u64 x[VEC];
+    float z[VEC];
+    z[0] = lane < count ? row.one(i0 + lane) : -INFINITY;
+#pragma unroll
+    for (int e = 1; e < VEC; ++e) z[e] = -INFINITY;
+    weights(z, i0 + lane, x);
+    x[0] = wave_scan(x[0]);
+    if (lane < 8) sh.ends[w][lane] = x[0];   // (up to 7 tokens)
+  }
   __syncthreads();
-  total = 0;
+  const u64 first = sh.ends[0][7], last = sh.ends[1][7];
+  total = first + last;
 #pragma unroll
   for (int i = 0; i < SM_WAVES; ++i) total += sh.part[i];
-  u64 limit = limit_of(total), before = 0;
+  u64 limit = limit_of(total), before = first;
+  if (limit < first || limit >= total - last) {
+    const int e = limit < first ? 0 : 1;
+    if (e == 1) limit -= total - last;
+    int i = 0;
+    while (i < 7 && sh.ends[e][i] <= limit) ++i;
+    return (e == 0 ? 0 : row.head + row.pieces * VEC) + i;
+  }
   int x = 0;
   while (x < SM_WAVES - 1 && before + sh.part[x] <= limit) before += sh.part[x++];
   limit -= before;
-  const int lo = x == 0 ? 0 : row.head + min(x * len, row.pieces) * VEC;
-  const int hi = x == SM_WAVES - 1 ? row.V : row.head + min((x + 1) * len, row.pieces) * VEC;
-  const int per = (hi - lo + SM_THREADS - 1) / SM_THREADS, a0 = min(lo + (int)threadIdx.x * per, hi), a1 = min(a0 + per, hi);
-  u64 mine = 0;
-  for (int i = a0; i < a1; ++i) mine += weight(i, row.one(i));
-  u64 upto = wave_scan(mine);
-  __syncthreads();
-  if (lane == 63) sh.part[w] = upto;
-  __syncthreads();
-  for (int i = 0; i < w; ++i) upto += sh.part[i];
-  if (upto - mine <= limit && limit < upto) {
-    u64 run = upto - mine;
-    for (int i = a0; i < a1; ++i) {
-      run += weight(i, row.one(i));
-      if (run > limit) {
-        sh.token = i;
-        break;
+  // The stretch in threads' shares of neighbouring pieces, walked twice: for
+  // their sums, then by the thread that passes the limit.
+  const int lo = min(x * len, row.pieces), hi = min(lo + len, row.pieces), per = (hi - lo + SM_THREADS - 1) / SM_THREADS;
+  const int a0 = min(lo + (int)threadIdx.x * per, hi);
+  int a1 = min(a0 + per, hi);
+  u64 run = 0, mine = 0;
+#pragma unroll 1
+  for (int turn = 0; turn < 2; ++turn) {
+#pragma unroll 1
+    for (int j = a0; j < a1; ++j) {
+      float z[VEC];
+      u64 y[VEC];
+      Row<DT>::unpack(row.piece(j), z);
+      weights(z, row.head + j * VEC, y);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        if (turn == 1 && run <= limit && limit < run + y[e]) sh.token = row.head + j * VEC + e;
+        run += y[e];
       }
     }
+    if (turn == 1) break;
+    mine = run;
+    u64 upto = wave_scan(mine);
+    __syncthreads();
+    if (lane == 63) sh.part[w] = upto;
+    __syncthreads();
+    for (int i = 0; i < w; ++i) upto += sh.part[i];
+    run = upto - mine;
+    if (run > limit || limit >= upto) a1 = a0;
   }
   __syncthreads();
   return sh.token;
@@ -338,7 +380,7 @@ __device__ __forceinline__ void list_token(uint32_t bits, int i, Shared &sh) {
 __device__ __forceinline__ int bits_of(uint32_t x) { return 32 - __clz((int)x); }   // x < 2^bits; 0 for 0
 
 template <int DT>
-__global__ __launch_bounds__(SM_THREADS, 8) void k_sample(sb_sample_args a) {
+__global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a) {
   constexpr int VEC = Row<DT>::VEC;
   __shared__ Shared sh;
   const int r = blockIdx.x, V = a.vocab, tid = threadIdx.x;
@@ -352,12 +394,12 @@ __global__ __launch_bounds__(SM_THREADS, 8) void k_sample(sb_sample_args a) {
   if (tid < (1 << TAB_BITS)) sh.tab[tid] = exp2(tid * (1.0 / (1 << TAB_BITS)));
   if (tid == 0) sh.n = 0;
 
-  // The sample: BATCH pieces a thread, from as many places of the row.
-  const int apart = max((row.pieces + BATCH - 1) / BATCH, SM_THREADS);
-  u4 x[BATCH];
+  // The sample: SAMPLE pieces a thread, from as many places of the row.
+  const int apart = max((row.pieces + SAMPLE - 1) / SAMPLE, SM_THREADS);
+  u4 x[SAMPLE];
   float zm = -INFINITY;
 #pragma unroll
-  for (int b = 0; b < BATCH; ++b) {
+  for (int b = 0; b < SAMPLE; ++b) {
     const int j = b * apart + tid;
     if (j < row.pieces) {
       x[b] = row.piece(j);
@@ -371,6 +413,7 @@ __global__ __launch_bounds__(SM_THREADS, 8) void k_sample(sb_sample_args a) {
   // Whether the tokens that matter are read off the sample, and from which on.
   const bool sampled = greedy || (k > 0 && k <= SAMPLED_K) || (k == 0 && p == 1.0f && mp > 0.0f);
   float bound = -INFINITY;
+  bool sure = true;   // nothing that matters lies below the bound
   if (greedy) {
     bound = from_order(seen);
   } else if (sampled) {
@@ -380,16 +423,23 @@ __global__ __launch_bounds__(SM_THREADS, 8) void k_sample(sb_sample_args a) {
       it.w[0] = 1;
 #pragma unroll
       for (int j = 1; j < LIST_PER; ++j) it.w[j] = 0, it.key[j] = 0;
+      // Read off the sample as the k-th largest is off the row, or a lower
+      // one than that (2 k + 256 tokens in the row by the sample's share) where
+      // that lists fewer: no bound in itself, so the list is counted.
+      const int want = min(k, (int)((float)(2 * k + 256) * (float)(min(SAMPLE * SM_THREADS, row.pieces) * VEC) / (float)V) + 1);
+      sure = want == k;
       // 18 bits of it: rounded away from the largest, which keeps it a bound.
       u64 rest, at;
-      const uint32_t d = list_search(it, [&](int j) { return it.key[j]; }, 32, 14, (u64)(k - 1), rest, at, sh) | 0x3FFFu;
+      const uint32_t d = list_search(it, [&](int j) { return it.key[j]; }, 32, 14, (u64)(want - 1), rest, at, sh) | 0x3FFFu;
       bound = from_order(seen - min(d, seen - LOWEST));
     }
     // min-p keeps z >= top + T ln(min_p), top at least the sample's (less a
     // little for the rounding here).
     if (p == 1.0f && mp > 0.0f && from_order(seen) < INFINITY) {
       const double b = (double)from_order(seen) + (double)T * log((double)mp);
-      bound = fmaxf(bound, (float)(b - 1e-6 * fabs(b) - 1e-30));
+      const float bf = (float)(b - 1e-6 * fabs(b) - 1e-30);
+      sure |= bf >= bound;
+      bound = fmaxf(bound, bf);
     }
   }
 
@@ -414,7 +464,7 @@ __global__ __launch_bounds__(SM_THREADS, 8) void k_sample(sb_sample_args a) {
     }
   };
 #pragma unroll
-  for (int b = 0; b < BATCH; ++b) {
+  for (int b = 0; b < SAMPLE; ++b) {
     const int j = b * apart + tid;
     if (j < row.pieces) {
       float z[VEC];
@@ -423,7 +473,8 @@ __global__ __launch_bounds__(SM_THREADS, 8) void k_sample(sb_sample_args a) {
     }
   }
   if (apart > SM_THREADS)
-    for (int b = 0; b < BATCH; ++b) row.each_piece(b * apart + SM_THREADS + tid, min((b + 1) * apart, row.pieces), SM_THREADS, look);
+#pragma unroll 1
+    for (int b = 0; b < SAMPLE; ++b) row.each_piece(b * apart + SM_THREADS + tid, min((b + 1) * apart, row.pieces), SM_THREADS, look);
   row.each_end(look);
   const uint32_t best = block_max(order_bits(zm), sh);
   if (best == LOWEST) {
@@ -434,8 +485,7 @@ __global__ __launch_bounds__(SM_THREADS, 8) void k_sample(sb_sample_args a) {
     return;
   }
   const float top = from_order(best);
-  // (The largest logit +inf: 10^300 instead, below which all others weigh nothing.)
-  const Weigher weigh{sh.tab, top == INFINITY ? 1e300 : (double)top, 1.4426950408889634074 / (double)T};
+  const Weigher weigh(sh.tab, top, T);
   const u64 floor_w = mp > 0.0f ? (u64)ceil((double)mp * ONE) : 0;
   const float uc = u > 0.0f ? fminf(u, 1.0f) : 0.0f;
   auto draw_limit = [=](u64 total) { return min((u64)((double)uc * (double)total), total - 1); };
@@ -443,10 +493,10 @@ __global__ __launch_bounds__(SM_THREADS, 8) void k_sample(sb_sample_args a) {
   // this: the cut is where they first total more.
   auto top_p_limit = [=](u64 z_k) { return (u64)fmax(ceil((double)p * (double)z_k), 1.0) - 1; };
 
-  int token;
-  u64 total;
+  int token = 0;
+  u64 total = 1;
   const int n = sh.n;
-  if (sampled && n <= LIST_MAX) {
+  if (sampled && n <= LIST_MAX && (sure || n >= k)) {
     Items it;
     take_list(it, n, [&](uint32_t b) { return greedy ? (u64)(b == best) : weigh(from_order(b)); }, sh);
     if (!greedy) {
@@ -499,77 +549,122 @@ __global__ __launch_bounds__(SM_THREADS, 8) void k_sample(sb_sample_args a) {
     if (greedy) total = (u64)ONE;
   } else {
     // Kept: order bits above `cut`, or equal to it with an index up to `cut_i`.
-    uint32_t cut = 0;
-    int cut_i = V;
-    auto kept = [&](int i, uint32_t b) { return b > cut || (b == cut && i <= cut_i); };
-    auto cut_row = [&](uint32_t bits, u64 nth) {
-      u64 t;
-      const int last = locate<DT>(row, [=](int, float z) { return (u64)(order_bits(z) == bits); }, [=](u64) { return nth; }, t, sh);
-      if (bits > cut) cut_i = last;
-      else if (bits == cut) cut_i = min(cut_i, last);
-      cut = max(cut, bits);
-    };
-    // Bins of equal ratio, BINS - 1 from the largest weight down to the
-    // smallest one there is (or that can matter), what is below in the last.
+    uint32_t cut = LOWEST;
+    float cut_z = -INFINITY;
+    int cut_i = -1;
     const float low = sampled ? -INFINITY : -from_order(block_max(order_bits(-zl), sh));   // (the full list: not looked for)
-    auto cut_by = [&](bool count, double reach, auto limit_of) {
-      const double range = fmin(fmax(-weigh.log2w(low), 1e-9), reach), scale = (BINS - 1) / range * (1 - 1e-9);
-      auto bin = [&](double x) { return (int)fmin(-x * scale, (double)(BINS - 1)); };
-      clear_bins(sh);
-      u64 below = 0, all = 0;
-      row.each([&](const float (&z)[VEC], int i0) {
+    auto kept = [&](int i, float z) { return (z > cut_z) | ((z == cut_z) & (i <= cut_i)); };   // (NaN: no)
+    // Top-k by counts, top-p by weights, then the draw: one code for all, its
+    // passes being much of the kernel's.
+#pragma unroll 1
+    for (int stage = greedy ? 2 : 0; stage < 3; ++stage) {
+      const bool count = stage == 0;
+      uint32_t bits = 0;
+      u64 limit = 0;
+      if (stage < 2) {
+        if (count ? k == 0 : p == 1.0f) continue;
+        // Bins of equal ratio, from the largest weight down to the smallest
+        // one there is, or that can matter; what is below in the last. Weights
+        // below (1 - p) / V of the largest total less than 1 - p of all: the
+        // cut is not among them (two octaves to spare for rounding).
+        const double reach = count ? 64.0 : fmin(2.0 + log2((double)V / fmax(1.0 - (double)p, 1e-9)), 64.0);
+        const double range = fmin(fmax(-weigh.log2w(low), 1e-4), reach), scale = (BINS - 2) / range;
+        auto bin = [&](double x) { return min(__double2loint(fma(x, -scale, 0x1.8p52)), BINS - 1); };   // to the nearest
+        clear_bins(sh);
+        u64 below = 0, all = 0;
+        row.each([&](const float (&z)[VEC], int i0) {
+          u64 w[VEC];
+          int at[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const uint32_t b = order_bits(z[e]);
-          if (b == LOWEST || !kept(i0 + e, b)) continue;
-          const double xw = weigh.log2w(z[e]);
-          const u64 w = count ? 1 : weigh.of(xw);
-          all += w;
-          const int at = bin(xw);
-          if (at < BINS - 1) atomicAdd(&sh.hist[at], w);
-          else below += w;
-        }
-      });
-      below = block_sum(below, sh);
-      all = block_sum(all, sh);
-      if (tid == 0) sh.hist[BINS - 1] = below;
-      const u64 limit = limit_of(all);
-      if (limit >= all) return;
-      u64 rest, at;
-      const int target = (int)find_bin(limit, rest, at, sh);
-      if (tid == 0) sh.n = 0;
-      __syncthreads();
-      row.each([&](const float (&z)[VEC], int i0) {
+          for (int e = 0; e < VEC; ++e) {   // no branches here: the tokens' chains of operations run side by side
+            const double xw = weigh.log2w(z[e]);
+            w[e] = only_if(kept(i0 + e, z[e]), count ? 1 : weigh.of(xw));
+            at[e] = bin(xw);
+          }
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          const uint32_t b = order_bits(z[e]);
-          if (b != LOWEST && bin(weigh.log2w(z[e])) == target && kept(i0 + e, b)) list_token(b, i0 + e, sh);
+          for (int e = 0; e < VEC; ++e) {
+            all += w[e];
+            if (at[e] < BINS - 1) {
+              if (w[e]) atomicAdd(&sh.hist[at[e]], w[e]);
+            } else {
+              below += w[e];
+            }
+          }
+        });
+        below = block_sum(below, sh);
+        all = block_sum(all, sh);
+        if (tid == 0) sh.hist[BINS - 1] = below;
+        limit = count ? (u64)(k - 1) : top_p_limit(all);
+        if (limit >= all) continue;
+        u64 rest, at;
+        const int target = (int)find_bin(limit, rest, at, sh);
+        if (tid == 0) sh.n = 0;
+        // The bin's logits: bins fall as logits rise, so each end is bisected.
+        auto first_in = [&](int most) {   // the lowest order bits with a bin up to `most`
+          uint32_t lo = LOWEST, hi = best;   // (best is in bin 0)
+          while (lo < hi) {
+            const uint32_t mid = lo + (hi - lo) / 2;
+            if (bin(weigh.log2w(from_order(mid))) <= most) hi = mid;
+            else lo = mid + 1;
+          }
+          return hi;
+        };
+        const float z_lo = from_order(max(first_in(target), max(cut, LOWEST + 1)));
+        const float z_hi = target > 0 ? from_order(first_in(target - 1) - 1) : top;
+        __syncthreads();
+        row.each([&](const float (&z)[VEC], int i0) {
+          float m = z[0];
+#pragma unroll
+          for (int e = 1; e < VEC; ++e) m = fmaxf(m, z[e]);
+          if (!(m >= z_lo)) return;
+#pragma unroll
+          for (int e = 0; e < VEC; ++e)
+            if (z[e] >= z_lo && z[e] <= z_hi && (z[e] != cut_z || i0 + e <= cut_i)) list_token(order_bits(z[e]), i0 + e, sh);
+        });
+        __syncthreads();
+        const int m = sh.n;
+        if (m <= LIST_MAX) {
+          Items it;
+          take_list(it, m, [&](uint32_t b) { return count ? (u64)1 : weigh(from_order(b)); }, sh);
+          bits = best - list_search(it, [&](int j) { return best - it.key[j]; }, 32, 0, rest, rest, at, sh);
+        } else {
+          bits = row_search<DT>(row, limit, [&](float z) { return z >= cut_z && z > -INFINITY ? count ? (u64)1 : weigh(z) : 0; }, rest, at, sh);
         }
-      });
-      __syncthreads();
-      const int m = sh.n;
-      uint32_t bits;
-      if (m <= LIST_MAX) {
-        Items it;
-        take_list(it, m, [&](uint32_t b) { return count ? (u64)1 : weigh(from_order(b)); }, sh);
-        bits = best - list_search(it, [&](int j) { return best - it.key[j]; }, 32, 0, rest, rest, at, sh);
-      } else {
-        bits = row_search<DT>(row, limit, [=](uint32_t b, float z) { return b == LOWEST || b < cut ? 0 : count ? (u64)1 : weigh(z); }, rest, sh);
+        const u64 each = count ? 1 : weigh(from_order(bits));
+        if (at <= rest + each) {   // all of the cut's equals stay
+          if (bits > cut) cut_i = V;
+          cut = bits;
+          cut_z = from_order(cut);
+          continue;
+        }
+        limit = rest / each;   // the first so many of them, and one
+      } else if (greedy) {
+        bits = best;
       }
-      cut_row(bits, count ? rest : rest / weigh(from_order(bits)));
-    };
-    if (!greedy && k > 0) cut_by(true, 64.0, [=](u64) { return (u64)(k - 1); });
-    // Weights below (1 - p) / V of the largest total less than 1 - p of all:
-    // the cut is not among them (one octave and more to spare for rounding).
-    if (!greedy && p < 1.0f) cut_by(false, fmin(2.0 + log2((double)V / fmax(1.0 - (double)p, 1e-9)), 64.0), top_p_limit);
-    auto weight = [&](int i, float z) -> u64 {
-      const uint32_t b = order_bits(z);
-      if (greedy) return b == best;
-      if (!kept(i, b)) return 0;
-      const u64 w = weigh(z);
-      return w >= floor_w ? w : 0;
-    };
-    token = locate<DT>(row, weight, [=](u64 t) { return greedy ? (u64)0 : draw_limit(t); }, total, sh);
+      const int found = locate<DT>(
+          row,
+          [&](const float (&z)[VEC], int i0, u64 (&w)[VEC]) {
+            float m = z[0];
+#pragma unroll
+            for (int e = 1; e < VEC; ++e) m = fmaxf(m, z[e]);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) w[e] = bits && order_bits(z[e]) == bits;
+            if (bits || m < cut_z) return;   // a wave without kept tokens takes no weights
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+              const u64 x = weigh(z[e]);
+              w[e] = only_if(kept(i0 + e, z[e]) & (x >= floor_w), x);
+            }
+          },
+          [&](u64 t) { return bits ? limit : draw_limit(t); }, total, sh);
+      if (stage == 2) {
+        token = found;
+      } else {
+        cut_i = bits > cut ? found : min(cut_i, found);
+        cut = bits;
+        cut_z = from_order(cut);
+      }
+    }
     if (greedy) total = (u64)ONE;
   }
   if (tid == 0) {
