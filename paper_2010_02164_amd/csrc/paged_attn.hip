@@ -79,18 +79,29 @@ __device__ __forceinline__ u4 finite_only(const u4 &x, bool &bad) {
 
 // A hidden key's weight is 0, and 0 times what stands there would be NaN where
 // that is NaN or infinite. In a tile whose keys some rows see and others do
-// not, such values are therefore taken out of V before the matrix product and
-// added by themselves to the rows that give them a weight: w times each of four
-// values that is not finite.
+// not, such values are therefore taken out of V, and a product of two
+// indicators (ones where V is not finite, ones where a weight is not 0) says
+// which results become NaN instead. That code is apart: the loops over the
+// keys stop at such a tile and are run again with it from the start, so that
+// it takes no registers from them.
 template <int DT>
-__device__ __forceinline__ f4 not_finite(float w, const unsigned char *v) {
-  const u2 x = *reinterpret_cast<const u2 *>(v);
-  f4 y;
+__device__ __forceinline__ uint32_t ones_where(bool lo, bool hi) {
+  constexpr uint32_t ONE16 = DT == SB_BF16 ? 0x3F80u : 0x3C00u;
+  return (lo ? ONE16 : 0u) | (hi ? ONE16 << 16 : 0u);
+}
+template <int DT>
+__device__ __forceinline__ u4 not_finite(const u4 &x) {
+  constexpr uint32_t E = DT == SB_BF16 ? 0x7F80u : 0x7C00u;
+  u4 y;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float f = Half<DT>::to_float(j & 1 ? x[j >> 1] >> 16 : x[j >> 1] & 0xFFFFu);
-    y[j] = w != 0.0f && !(fabsf(f) < INFINITY) ? w * f : 0.0f;
-  }
+  for (int i = 0; i < 4; ++i) y[i] = ones_where<DT>((x[i] & E) == E, (x[i] & (E << 16)) == (E << 16));
+  return y;
+}
+template <int DT>
+__device__ __forceinline__ u4 not_zero(const u4 &x) {
+  u4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = ones_where<DT>((x[i] & 0xFFFFu) != 0, (x[i] >> 16) != 0);
   return y;
 }
 
@@ -149,11 +160,128 @@ __device__ __forceinline__ float2 *part_stats(const sb_attention_args &a, float 
   return reinterpret_cast<float2 *>(parts + splits * nr * D) + split * nr + row;
 }
 
-template <int DT, int D>
-__global__ __launch_bounds__(AT_THREADS) void k_attn_few(sb_attention_args a, int splits, float *parts) {
+// One wave's pass over its tiles t0, t0 + 4, ... < t_end: the 16 rows' sums, their
+// maxima and this lane's share of the weights' sums. False where it stopped.
+template <int DT, int D, bool CAREFUL>
+__device__ __forceinline__ bool few_keys(const sb_attention_args &a, const Span &s, const int *table, const uint16_t *kc, const uint16_t *vc,
+                                         const u4 (&q)[D / 32], int p, bool real, int t0, int t_end, unsigned char *lds, f4 (&o)[D / 16],
+                                         float &mx, float &sum) {
   constexpr int VS = 2 * D + 32;            // bytes of a V row in LDS: 8 rows of 32 bytes in different banks
   constexpr int KS = D / 32, NV = D / 16;   // products per score, 16-byte pieces of V per lane
   constexpr int DT16 = D / 16;
+  const int lane = threadIdx.x & 63, g4 = lane >> 4, l16 = lane & 15;
+  const double inv_page = 1.0 / a.page_size;
+  const float c = (float)(a.scale * LOG2E);
+  mx = -INFINITY;
+  sum = 0.0f;
+#pragma unroll
+  for (int x = 0; x < DT16; ++x) o[x] = f4{0, 0, 0, 0};
+  // Where a tile's keys lie (lane l: key l % 32), looked up a tile ahead.
+  auto find = [&](int t, int &place) {
+    const int u = t * FEW_KEYS + (lane & 31);
+    return t < t_end && u < s.n_vis ? page_of(a, table, inv_page, s.key(u), place) : -1;
+  };
+  int next_place = 0, next = find(t0, next_place);
+  for (int t = t0; t < t_end; t += AT_WAVES) {
+    const int page = next, place = next_place;
+    const uint32_t there = (uint32_t)__ballot(page >= 0);
+    const long long ko = page >= 0 ? page * a.kc_page + place * a.kc_slot : 0;   // (keys that are not there: any that is)
+    const long long vo = page >= 0 ? page * a.vc_page + place * a.vc_slot : 0;
+    u4 k[2][KS], v[NV];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      const uint16_t *src = kc + __shfl(ko, hf * 16 + l16, 64) + 8 * g4;
+#pragma unroll
+      for (int x = 0; x < KS; ++x) k[hf][x] = *reinterpret_cast<const u4 *>(src + 32 * x);
+    }
+#pragma unroll
+    for (int x = 0; x < NV; ++x) {
+      const int piece = x * 64 + lane, kr = piece / (D / 8);
+      v[x] = *reinterpret_cast<const u4 *>(vc + __shfl(vo, kr, 64) + (piece - kr * (D / 8)) * 8);
+    }
+    next = find(t + AT_WAVES, next_place);
+    const bool plain = there == 0xFFFFFFFFu && s.all_see(a, s.key(t * FEW_KEYS), s.key(t * FEW_KEYS + FEW_KEYS - 1));
+    f4 sc[2] = {f4{0, 0, 0, 0}, f4{0, 0, 0, 0}};
+#pragma unroll
+    for (int x = 0; x < KS; ++x)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) sc[hf] = mfma16<DT>(k[hf][x], q[x], sc[hf]);
+    // Lane: keys 16 hf + 4 g4 + j of row l16.
+    float tm = -INFINITY;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sc[hf][j] *= c;
+        if (!plain) {
+          const int at = 16 * hf + 4 * g4 + j;
+          const bool on = real && ((there >> at) & 1u) && sees(a, p, s.key(t * FEW_KEYS + at));
+          sc[hf][j] = on ? sc[hf][j] : -INFINITY;
+        }
+        tm = fmaxf(tm, sc[hf][j]);
+      }
+    tm = fmaxf(tm, __shfl_xor(tm, 16, 64));
+    tm = fmaxf(tm, __shfl_xor(tm, 32, 64));
+    const float mn = fmaxf(mx, tm), base = mn == -INFINITY ? 0.0f : mn;
+    const float shrink = __builtin_amdgcn_exp2f(mx - base);
+    mx = mn;
+    float ts = 0.0f;
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sc[hf][j] = __builtin_amdgcn_exp2f(sc[hf][j] - base);
+        ts += sc[hf][j];
+      }
+    sum = sum * shrink + ts;
+    const u4 pk = {Half<DT>::pack(sc[0][0], sc[0][1]), Half<DT>::pack(sc[0][2], sc[0][3]),
+                   Half<DT>::pack(sc[1][0], sc[1][1]), Half<DT>::pack(sc[1][2], sc[1][3])};
+    bool bad = false;
+#pragma unroll
+    for (int x = 0; x < NV; ++x) {
+      const int piece = x * 64 + lane, kr = piece / (D / 8);
+      if (!plain) {
+        if (!((there >> kr) & 1u)) v[x] = u4{0, 0, 0, 0};
+        finite_only<DT>(v[x], bad);
+      }
+      *reinterpret_cast<u4 *>(lds + kr * VS + (piece - kr * (D / 8)) * 16) = v[x];
+    }
+    if (!CAREFUL && __any(bad)) return false;
+    wave_lds_fence();
+    const unsigned char *vt = lds + (4 * g4 + (l16 >> 2)) * VS + (l16 & 3) * 8;
+    if (CAREFUL && !plain) {
+      const u4 pn = not_zero<DT>(pk);
+#pragma unroll
+      for (int x = 0; x < DT16; ++x) {
+        const u2 v0 = read_transposed(vt + 32 * x), v1 = read_transposed(vt + 16 * VS + 32 * x);
+        const f4 hit = mfma16<DT>(not_finite<DT>(u4{v0[0], v0[1], v1[0], v1[1]}), pn, f4{0, 0, 0, 0});
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[x][j] = hit[j] > 0.0f ? NAN : o[x][j];
+      }
+      wave_lds_fence();
+      for (int piece = lane; piece < FEW_KEYS * (D / 8); piece += 64) {
+        u4 *at = reinterpret_cast<u4 *>(lds + piece / (D / 8) * VS + piece % (D / 8) * 16);
+        *at = finite_only<DT>(*at, bad);
+      }
+      wave_lds_fence();
+    }
+#pragma unroll
+    for (int x = 0; x < DT16; ++x) {
+      const u2 v0 = read_transposed(vt + 32 * x), v1 = read_transposed(vt + 16 * VS + 32 * x);
+      o[x] = mfma16<DT>(u4{v0[0], v0[1], v1[0], v1[1]}, pk, o[x] * shrink);
+    }
+    wave_lds_fence();
+  }
+  return true;
+}
+
+// Workgroups of k_attn_few that a compute unit is to hold at once, for loads in
+// flight: as many as the registers of a wave's tile allow.
+constexpr int few_groups(int D) { return D == 64 ? 3 : D == 128 ? 2 : 1; }
+
+template <int DT, int D>
+__global__ __launch_bounds__(AT_THREADS, few_groups(D)) void k_attn_few(sb_attention_args a, int splits, int chunk, float *parts) {
+  constexpr int VS = 2 * D + 32, DT16 = D / 16, KS = D / 32;
   __shared__ alignas(16) unsigned char lds[AT_WAVES][FEW_KEYS * VS];
   __shared__ float2 stats[AT_WAVES][FEW_ROWS];
   static_assert(FEW_KEYS * VS >= FEW_ROWS * D * 4, "the waves' sums fit where V was");
@@ -161,8 +289,6 @@ __global__ __launch_bounds__(AT_THREADS) void k_attn_few(sb_attention_args a, in
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g4 = lane >> 4, l16 = lane & 15;
   const int G = a.q_heads / a.kv_heads;
   const int *table = a.table + b * a.table_stride;
-  const double inv_page = 1.0 / a.page_size;
-  const float c = (float)(a.scale * LOG2E);
   const uint16_t *kc = static_cast<const uint16_t *>(a.k_cache) + hk * a.kc_head;
   const uint16_t *vc = static_cast<const uint16_t *>(a.v_cache) + hk * a.vc_head;
   Span s;
@@ -171,154 +297,53 @@ __global__ __launch_bounds__(AT_THREADS) void k_attn_few(sb_attention_args a, in
     span_rows(a, r0, FEW_ROWS, s);
     const int row = r0 + l16, i = row / G, p = s.n - s.m + i;
     const bool real = row < s.rows;
-    u4 q[KS];
+    // This part's tiles: `chunk` keys each, more where max_kv was too small.
+    const int tiles = (s.n_vis + FEW_KEYS - 1) / FEW_KEYS, per = max(chunk / FEW_KEYS, (tiles + splits - 1) / splits);
+    const int t_begin = min(split * per, tiles), t_end = min(t_begin + per, tiles);
+    if (t_begin < t_end) {
+      u4 q[KS];
 #pragma unroll
-    for (int x = 0; x < KS; ++x) {
-      const uint16_t *src = static_cast<const uint16_t *>(a.q) + (s.q0 + i) * a.q_token + (hk * G + row - i * G) * a.q_head;
-      q[x] = real ? *reinterpret_cast<const u4 *>(src + 32 * x + 8 * g4) : u4{0, 0, 0, 0};
+      for (int x = 0; x < KS; ++x) {
+        const uint16_t *src = static_cast<const uint16_t *>(a.q) + (s.q0 + i) * a.q_token + (hk * G + row - i * G) * a.q_head;
+        q[x] = real ? *reinterpret_cast<const u4 *>(src + 32 * x + 8 * g4) : u4{0, 0, 0, 0};
+      }
+      f4 o[DT16];
+      float mx, sum;
+      if (!few_keys<DT, D, false>(a, s, table, kc, vc, q, p, real, t_begin + w, t_end, &lds[w][0], o, mx, sum))
+        few_keys<DT, D, true>(a, s, table, kc, vc, q, p, real, t_begin + w, t_end, &lds[w][0], o, mx, sum);
+      sum += __shfl_xor(sum, 16, 64);
+      sum += __shfl_xor(sum, 32, 64);
+      // The four waves' parts: sums side by side where V was.
+      float *os = reinterpret_cast<float *>(&lds[w][0]);
+#pragma unroll
+      for (int x = 0; x < DT16; ++x) *reinterpret_cast<f4 *>(os + l16 * D + 16 * x + 4 * g4) = o[x];
+      if (g4 == 0) stats[w][l16] = make_float2(mx, sum);
     }
-    f4 o[DT16];
-#pragma unroll
-    for (int x = 0; x < DT16; ++x) o[x] = f4{0, 0, 0, 0};
-    float mx = -INFINITY, sum = 0.0f;
-    const int tiles = (s.n_vis + FEW_KEYS - 1) / FEW_KEYS, per = (tiles + splits - 1) / splits;
-    const int t_end = min(tiles, (split + 1) * per);
-    for (int t = split * per + w; t < t_end; t += AT_WAVES) {
-      // Where the tile's keys lie (lane l: key l % 32).
-      const int u = t * FEW_KEYS + (lane & 31);
-      int place = 0;
-      const int page = u < s.n_vis ? page_of(a, table, inv_page, s.key(u), place) : -1;
-      const uint32_t there = (uint32_t)__ballot(page >= 0);
-      const long long ko = page >= 0 ? page * a.kc_page + place * a.kc_slot : 0;
-      const long long vo = page >= 0 ? page * a.vc_page + place * a.vc_slot : -1;
-      u4 k[2][KS], v[NV];
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        const uint16_t *src = kc + __shfl(ko, hf * 16 + l16, 64) + 8 * g4;
-#pragma unroll
-        for (int x = 0; x < KS; ++x) k[hf][x] = *reinterpret_cast<const u4 *>(src + 32 * x);
-      }
-#pragma unroll
-      for (int x = 0; x < NV; ++x) {
-        const int piece = x * 64 + lane, kr = piece / (D / 8);
-        const long long off = __shfl(vo, kr, 64);
-        v[x] = u4{0, 0, 0, 0};
-        if (off >= 0) v[x] = *reinterpret_cast<const u4 *>(vc + off + (piece - kr * (D / 8)) * 8);
-      }
-      const int k_first = s.key(t * FEW_KEYS), k_last = s.key(t * FEW_KEYS + FEW_KEYS - 1);
-      const bool plain = there == 0xFFFFFFFFu && s.all_see(a, k_first, k_last);
-      f4 sc[2] = {f4{0, 0, 0, 0}, f4{0, 0, 0, 0}};
-#pragma unroll
-      for (int x = 0; x < KS; ++x)
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) sc[hf] = mfma16<DT>(k[hf][x], q[x], sc[hf]);
-      // Lane: keys 16 hf + 4 g4 + j of row l16.
-      float tm = -INFINITY;
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          sc[hf][j] *= c;
-          if (!plain) {
-            const int at = 16 * hf + 4 * g4 + j;
-            const bool on = real && ((there >> at) & 1u) && sees(a, p, s.key(t * FEW_KEYS + at));
-            sc[hf][j] = on ? sc[hf][j] : -INFINITY;
-          }
-          tm = fmaxf(tm, sc[hf][j]);
-        }
-      tm = fmaxf(tm, __shfl_xor(tm, 16, 64));
-      tm = fmaxf(tm, __shfl_xor(tm, 32, 64));
-      const float mn = fmaxf(mx, tm), base = mn == -INFINITY ? 0.0f : mn;
-      const float shrink = __builtin_amdgcn_exp2f(mx - base);
-      mx = mn;
-      float ts = 0.0f;
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          sc[hf][j] = __builtin_amdgcn_exp2f(sc[hf][j] - base);
-          ts += sc[hf][j];
-        }
-      sum = sum * shrink + ts;   // this lane's keys only; added up at the end
-      const u4 pk = {Half<DT>::pack(sc[0][0], sc[0][1]), Half<DT>::pack(sc[0][2], sc[0][3]),
-                     Half<DT>::pack(sc[1][0], sc[1][1]), Half<DT>::pack(sc[1][2], sc[1][3])};
-      auto put = [&] {
-#pragma unroll
-        for (int x = 0; x < NV; ++x) {
-          const int piece = x * 64 + lane, kr = piece / (D / 8);
-          *reinterpret_cast<u4 *>(&lds[w][kr * VS + (piece - kr * (D / 8)) * 16]) = v[x];
-        }
-        wave_lds_fence();
-      };
-      put();
-      f4 extra[DT16];
-      bool careful = false;
-      if (!plain) {
-        bool bad = false;
-        u4 vf[NV];
-#pragma unroll
-        for (int x = 0; x < NV; ++x) vf[x] = finite_only<DT>(v[x], bad);
-        careful = __any(bad);
-        if (careful) {
-#pragma unroll
-          for (int x = 0; x < DT16; ++x) extra[x] = f4{0, 0, 0, 0};
-          for (int kk = 0; kk < FEW_KEYS; ++kk) {
-            float wt = sc[0][0];
-#pragma unroll
-            for (int e = 1; e < 8; ++e) wt = e == (kk >> 4) * 4 + (kk & 3) ? sc[e >> 2][e & 3] : wt;
-            wt = __shfl(wt, ((kk & 15) >> 2) * 16 + l16, 64);
-#pragma unroll
-            for (int x = 0; x < DT16; ++x) extra[x] += not_finite<DT>(wt, &lds[w][kk * VS + 32 * x + 8 * g4]);
-          }
-          wave_lds_fence();
-#pragma unroll
-          for (int x = 0; x < NV; ++x) v[x] = vf[x];
-          put();
-        }
-      }
-      const unsigned char *vt = &lds[w][(4 * g4 + (l16 >> 2)) * VS + (l16 & 3) * 8];
-#pragma unroll
-      for (int x = 0; x < DT16; ++x) {
-        const u2 v0 = read_transposed(vt + 32 * x), v1 = read_transposed(vt + 16 * VS + 32 * x);
-        o[x] = mfma16<DT>(u4{v0[0], v0[1], v1[0], v1[1]}, pk, o[x] * shrink);
-      }
-      if (careful) {
-#pragma unroll
-        for (int x = 0; x < DT16; ++x) o[x] += extra[x];
-      }
-      wave_lds_fence();
-    }
-    sum += __shfl_xor(sum, 16, 64);
-    sum += __shfl_xor(sum, 32, 64);
-    // The four waves' parts: sums side by side where V was.
-    float *os = reinterpret_cast<float *>(&lds[w][0]);
-#pragma unroll
-    for (int x = 0; x < DT16; ++x) *reinterpret_cast<f4 *>(os + l16 * D + 16 * x + 4 * g4) = o[x];
-    if (g4 == 0) stats[w][l16] = make_float2(mx, sum);
     __syncthreads();
     for (int e = threadIdx.x; e < FEW_ROWS * D / 4; e += AT_THREADS) {
       const int rr = e / (D / 4), col = (e - rr * (D / 4)) * 4, rw = r0 + rr;
       if (rw >= s.rows) continue;
-      float m4 = -INFINITY;
-#pragma unroll
-      for (int x = 0; x < AT_WAVES; ++x) m4 = fmaxf(m4, stats[x][rr].x);
-      const float base = m4 == -INFINITY ? 0.0f : m4;
-      float l4 = 0.0f;
-      f4 acc = {0, 0, 0, 0};
-#pragma unroll
-      for (int x = 0; x < AT_WAVES; ++x) {
-        const float f = __builtin_amdgcn_exp2f(stats[x][rr].x - base);
-        l4 += f * stats[x][rr].y;
-        acc += f * *reinterpret_cast<const f4 *>(reinterpret_cast<const float *>(&lds[x][0]) + rr * D + col);
-      }
       const int qi = rw / G, tok = s.q0 + qi, h = hk * G + rw - qi * G;
+      const long long pr = (long long)tok * a.q_heads + h;
+      float m4 = -INFINITY, l4 = 0.0f;
+      f4 acc = {0, 0, 0, 0};
+      if (t_begin < t_end) {
+#pragma unroll
+        for (int x = 0; x < AT_WAVES; ++x) m4 = fmaxf(m4, stats[x][rr].x);
+        const float base = m4 == -INFINITY ? 0.0f : m4;
+#pragma unroll
+        for (int x = 0; x < AT_WAVES; ++x) {
+          const float f = __builtin_amdgcn_exp2f(stats[x][rr].x - base);
+          l4 += f * stats[x][rr].y;
+          acc += f * *reinterpret_cast<const f4 *>(reinterpret_cast<const float *>(&lds[x][0]) + rr * D + col);
+        }
+      }
       if (splits == 1) {
         const float inv = l4 == 0.0f ? 0.0f : 1.0f / l4;
         uint16_t *dst = static_cast<uint16_t *>(a.out) + tok * a.out_token + h * a.out_head + col;
         *reinterpret_cast<u2 *>(dst) = u2{Half<DT>::pack(acc[0] * inv, acc[1] * inv), Half<DT>::pack(acc[2] * inv, acc[3] * inv)};
-      } else {
-        const long long pr = (long long)tok * a.q_heads + h;
-        *reinterpret_cast<f4 *>(part_sums<D>(a, parts, split, pr) + col) = acc;
+      } else {   // (a part without keys: its statistics say so, and nobody reads its sums)
+        if (t_begin < t_end) *reinterpret_cast<f4 *>(part_sums<D>(a, parts, split, pr) + col) = acc;
         if (col == 0) *part_stats<D>(a, parts, splits, split, pr) = make_float2(m4, l4);
       }
     }
@@ -361,55 +386,38 @@ __global__ __launch_bounds__(AT_THREADS) void k_attn_join(sb_attention_args a, i
   }
 }
 
-template <int DT, int D>
-__global__ __launch_bounds__(AT_THREADS) void k_attn_many(sb_attention_args a) {
-  constexpr int KSTR = 2 * D + 16, VSTR = 2 * D + 32;   // bytes of a K and a V row in LDS
+// What the waves of k_attn_many share.
+template <int D>
+struct ManyShared {
+  static constexpr int KSTR = 2 * D + 16, VSTR = 2 * D + 32;   // bytes of a K and a V row
+  alignas(16) unsigned char k[MANY_KEYS * KSTR];
+  alignas(16) unsigned char v[MANY_KEYS * VSTR];
+  uint32_t there[2][2];   // [parity][half]: keys of the tile that have a page
+  int not_fin[2];         // [parity]: V of a tile that not all rows see has values that are not finite
+};
+
+// The workgroup's pass over its tiles: the lane's row's sums, and its keys'
+// share of the weights' sum. False where it stopped.
+template <int DT, int D, bool CAREFUL>
+__device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span &s, const int *table, const uint16_t *kc, const uint16_t *vc,
+                                          const u4 (&q)[D / 16], int p, bool real, ManyShared<D> &sh, f16v (&o)[D / 32], float &sum) {
+  constexpr int KSTR = ManyShared<D>::KSTR, VSTR = ManyShared<D>::VSTR;
   constexpr int PC = MANY_KEYS * (D / 8) / AT_THREADS;  // 16-byte pieces of K (and V) a thread brings
   constexpr int KS = D / 16, DB = D / 32;
-  __shared__ alignas(16) unsigned char lk[MANY_KEYS * KSTR];
-  __shared__ alignas(16) unsigned char lv[MANY_KEYS * VSTR];
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, h2 = lane >> 5;
-  const int G = a.q_heads / a.kv_heads, hk = blockIdx.y;
-  // The request of this tile: request b's tiles start at q_start[b] G / 128 + b,
-  // which leaves at least one place a tile; the last ones of some stay empty.
-  const int tile = (int)(gridDim.x - 1 - blockIdx.x);
-  int b = 0, bh = a.n_requests;
-  while (bh - b > 1) {
-    const int mid = (b + bh) >> 1;
-    if ((long long)a.q_start[mid] * G / MANY_ROWS + mid <= tile) b = mid;
-    else bh = mid;
-  }
-  Span s;
-  span_request(a, b, s);
-  const int r0 = (int)(tile - ((long long)a.q_start[b] * G / MANY_ROWS + b)) * MANY_ROWS;
-  if (r0 < 0 || r0 >= s.rows) return;
-  span_rows(a, r0, MANY_ROWS, s);
-  const int *table = a.table + b * a.table_stride;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, h2 = lane >> 5;
   const double inv_page = 1.0 / a.page_size;
-  const float c = (float)(a.scale * LOG2E);
-  const uint16_t *kc = static_cast<const uint16_t *>(a.k_cache) + hk * a.kc_head;
-  const uint16_t *vc = static_cast<const uint16_t *>(a.v_cache) + hk * a.vc_head;
-
-  const int row = r0 + 32 * w + l32, i = row / G, p = s.n - s.m + i;
-  const bool real = row < s.rows;
-  u4 q[KS];
-#pragma unroll
-  for (int x = 0; x < KS; ++x) {
-    const uint16_t *src = static_cast<const uint16_t *>(a.q) + (s.q0 + i) * a.q_token + (hk * G + row - i * G) * a.q_head;
-    q[x] = real ? *reinterpret_cast<const u4 *>(src + 16 * x + 8 * h2) : u4{0, 0, 0, 0};
-  }
-  f16v o[DB];
+  const float c = a.scale == 0.0f ? 1.0f : (float)(fabs((double)a.scale) * LOG2E);
 #pragma unroll
   for (int x = 0; x < DB; ++x)
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[x][e] = 0.0f;
-  float mx = -INFINITY, sum = 0.0f;
+  // `ref`: what the exponentials are taken against, a score the row has had. It
+  // moves to a larger one only when that would be over 2^GROW of it.
+  constexpr float GROW = 8.0f;
+  float ref = -INFINITY;
+  sum = 0.0f;
 
   u4 kr[PC], vr[PC];
-  __shared__ uint32_t there[2][2];   // [parity][half]: keys of the tile that have a page
-  __shared__ int not_fin[2];         // [parity]: V of a tile that not all rows see has values that are not finite
-  if (threadIdx.x < 2) not_fin[threadIdx.x] = 0;
-  __syncthreads();
   const int tiles = (s.n_vis + MANY_KEYS - 1) / MANY_KEYS;
   auto bring = [&](int t) {
 #pragma unroll
@@ -428,10 +436,13 @@ __global__ __launch_bounds__(AT_THREADS) void k_attn_many(sb_attention_args a) {
       const int u = t * MANY_KEYS + threadIdx.x;
       int place = 0;
       const unsigned long long m = __ballot(u < s.n_vis && page_of(a, table, inv_page, s.key(u), place) >= 0);
-      if (threadIdx.x < 2) there[t & 1][threadIdx.x] = (uint32_t)(m >> (32 * threadIdx.x));
+      if (threadIdx.x < 2) sh.there[t & 1][threadIdx.x] = (uint32_t)(m >> (32 * threadIdx.x));
     }
   };
+  __syncthreads();
+  if (threadIdx.x < 2) sh.not_fin[threadIdx.x] = 0;
   if (tiles > 0) bring(0);
+  __syncthreads();
   for (int t = 0; t < tiles; ++t) {
     const int u0 = t * MANY_KEYS;
     const bool shared = s.all_see(a, s.key(u0), s.key(u0 + MANY_KEYS - 1));
@@ -439,15 +450,15 @@ __global__ __launch_bounds__(AT_THREADS) void k_attn_many(sb_attention_args a) {
 #pragma unroll
     for (int x = 0; x < PC; ++x) {
       const int piece = x * AT_THREADS + threadIdx.x, kk = piece / (D / 8), col = (piece - kk * (D / 8)) * 16;
-      *reinterpret_cast<u4 *>(&lk[kk * KSTR + col]) = kr[x];
-      *reinterpret_cast<u4 *>(&lv[kk * VSTR + col]) = vr[x];
-      if (!shared) finite_only<DT>(vr[x], bad);
+      *reinterpret_cast<u4 *>(&sh.k[kk * KSTR + col]) = kr[x];
+      *reinterpret_cast<u4 *>(&sh.v[kk * VSTR + col]) = vr[x];
+      if (!CAREFUL && !shared) finite_only<DT>(vr[x], bad);
     }
-    if (bad) not_fin[t & 1] = 1;
+    if (bad) sh.not_fin[t & 1] = 1;
     __syncthreads();
-    const uint32_t on0 = there[t & 1][0], on1 = there[t & 1][1];
-    const bool careful = not_fin[t & 1];
-    if (threadIdx.x == 0) not_fin[(t + 1) & 1] = 0;
+    const uint32_t on0 = sh.there[t & 1][0], on1 = sh.there[t & 1][1];
+    if (!CAREFUL && sh.not_fin[t & 1]) return false;
+    if (threadIdx.x == 0) sh.not_fin[(t + 1) & 1] = 0;
     if (t + 1 < tiles) bring(t + 1);
     f16v sc[2];
 #pragma unroll
@@ -456,67 +467,70 @@ __global__ __launch_bounds__(AT_THREADS) void k_attn_many(sb_attention_args a) {
       for (int e = 0; e < 16; ++e) sc[kb][e] = 0.0f;
 #pragma unroll
       for (int x = 0; x < KS; ++x) {
-        const u4 kf = *reinterpret_cast<const u4 *>(&lk[(32 * kb + l32) * KSTR + 32 * x + 16 * h2]);
+        const u4 kf = *reinterpret_cast<const u4 *>(&sh.k[(32 * kb + l32) * KSTR + 32 * x + 16 * h2]);
         sc[kb] = mfma32<DT>(kf, q[x], sc[kb]);
       }
     }
     // Lane: keys 32 kb + 8 (e / 4) + 4 h2 + e % 4 of row l32.
-    const bool plain = (on0 & on1) == 0xFFFFFFFFu && shared;
+    if ((on0 & on1) != 0xFFFFFFFFu || !shared) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int at = 8 * (e >> 2) + 4 * h2 + (e & 3);
+          const bool on = real && (((kb ? on1 : on0) >> at) & 1u) && sees(a, p, s.key(u0 + 32 * kb + at));
+          sc[kb][e] = on ? sc[kb][e] : -INFINITY;
+        }
+    }
     float tm = -INFINITY;
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int at = 8 * (e >> 2) + 4 * h2 + (e & 3);
-        float x = sc[kb][e] * c;
-        if (!plain) {
-          const bool on = real && (((kb ? on1 : on0) >> at) & 1u) && sees(a, p, s.key(u0 + 32 * kb + at));
-          x = on ? x : -INFINITY;
-        }
-        sc[kb][e] = x;
-        tm = fmaxf(tm, x);
-      }
+      for (int e = 0; e < 16; ++e) tm = fmaxf(tm, sc[kb][e]);
     tm = fmaxf(tm, __shfl_xor(tm, 32, 64));
-    const float mn = fmaxf(mx, tm), base = mn == -INFINITY ? 0.0f : mn;
-    const float shrink = __builtin_amdgcn_exp2f(mx - base);
-    mx = mn;
-    float ts = 0.0f;
+    if (__any(tm > ref && !(c * (tm - ref) <= GROW))) {
+      const float mn = fmaxf(ref, tm);
+      const float shrink = ref == mn ? 1.0f : __builtin_amdgcn_exp2f(c * (ref - mn));
+      ref = mn;
+      sum *= shrink;
+#pragma unroll
+      for (int x = 0; x < DB; ++x) o[x] *= shrink;
+    }
+    const float base = ref == -INFINITY ? 0.0f : ref * c;
+    float ts[2] = {0.0f, 0.0f};
     u4 pk[4];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
       for (int e = 0; e < 16; e += 2) {
-        const float x = __builtin_amdgcn_exp2f(sc[kb][e] - base), y = __builtin_amdgcn_exp2f(sc[kb][e + 1] - base);
-        ts += x + y;
+        const float x = __builtin_amdgcn_exp2f(fmaf(sc[kb][e], c, -base)), y = __builtin_amdgcn_exp2f(fmaf(sc[kb][e + 1], c, -base));
+        ts[0] += x;
+        ts[1] += y;
         pk[2 * kb + (e >> 3)][(e & 7) >> 1] = Half<DT>::pack(x, y);
       }
-    sum = sum * shrink + ts;
+    sum += ts[0] + ts[1];
+    const unsigned char *vt = &sh.v[(4 * h2 + ((lane & 15) >> 2)) * VSTR + ((lane >> 4) & 1) * 32 + (lane & 3) * 8];
+    if (CAREFUL && !shared) {
 #pragma unroll
-    for (int x = 0; x < DB; ++x) o[x] *= shrink;
-    if (careful) {
-      for (int kk = 0; kk < MANY_KEYS; ++kk) {
-        const int e = ((kk >> 3) & 1) * 4 + (kk & 3), from = (kk >> 2) & 1;
-        uint32_t code = 0;
+      for (int x = 0; x < DB; ++x) {
+        f16v hit;
 #pragma unroll
-        for (int x = 0; x < 16; ++x) code = x == (kk >> 4) * 4 + (e >> 1) ? pk[x >> 2][x & 3] : code;
-        const float wt = __shfl(Half<DT>::to_float(e & 1 ? code >> 16 : code & 0xFFFFu), from * 32 + l32, 64);
+        for (int e = 0; e < 16; ++e) hit[e] = 0.0f;
 #pragma unroll
-        for (int x = 0; x < DB; ++x)
+        for (int ks = 0; ks < 4; ++ks) {
+          const u2 v0 = read_transposed(vt + 16 * ks * VSTR + 64 * x), v1 = read_transposed(vt + (16 * ks + 8) * VSTR + 64 * x);
+          hit = mfma32<DT>(not_finite<DT>(u4{v0[0], v0[1], v1[0], v1[1]}), not_zero<DT>(pk[ks]), hit);
+        }
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const f4 z = not_finite<DT>(wt, &lv[kk * VSTR + 64 * x + 16 * y + 8 * h2]);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[x][4 * y + j] += z[j];
-          }
+        for (int e = 0; e < 16; ++e) o[x][e] = hit[e] > 0.0f ? NAN : o[x][e];
       }
       __syncthreads();
       for (int piece = threadIdx.x; piece < MANY_KEYS * (D / 8); piece += AT_THREADS) {
-        u4 *at = reinterpret_cast<u4 *>(&lv[piece / (D / 8) * VSTR + piece % (D / 8) * 16]);
+        u4 *at = reinterpret_cast<u4 *>(&sh.v[piece / (D / 8) * VSTR + piece % (D / 8) * 16]);
         *at = finite_only<DT>(*at, bad);
       }
       __syncthreads();
     }
-    const unsigned char *vt = &lv[(4 * h2 + ((lane & 15) >> 2)) * VSTR + ((lane >> 4) & 1) * 32 + (lane & 3) * 8];
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
@@ -526,6 +540,48 @@ __global__ __launch_bounds__(AT_THREADS) void k_attn_many(sb_attention_args a) {
       }
     __syncthreads();
   }
+  return true;
+}
+
+template <int DT, int D>
+__global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : 2) void k_attn_many(sb_attention_args a) {
+  constexpr int KS = D / 16, DB = D / 32;
+  __shared__ ManyShared<D> sh;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, h2 = lane >> 5;
+  const int G = a.q_heads / a.kv_heads, hk = blockIdx.y;
+  // The request of this tile: request b's tiles start at q_start[b] G / 128 + b,
+  // which leaves at least one place a tile; the last ones of some stay empty.
+  const int tile = (int)(gridDim.x - 1 - blockIdx.x);
+  int b = 0, bh = a.n_requests;
+  while (bh - b > 1) {
+    const int mid = (b + bh) >> 1;
+    if ((long long)a.q_start[mid] * G / MANY_ROWS + mid <= tile) b = mid;
+    else bh = mid;
+  }
+  Span s;
+  span_request(a, b, s);
+  const int r0 = (int)(tile - ((long long)a.q_start[b] * G / MANY_ROWS + b)) * MANY_ROWS;
+  if (r0 < 0 || r0 >= s.rows) return;
+  span_rows(a, r0, MANY_ROWS, s);
+  const int *table = a.table + b * a.table_stride;
+  const uint16_t *kc = static_cast<const uint16_t *>(a.k_cache) + hk * a.kc_head;
+  const uint16_t *vc = static_cast<const uint16_t *>(a.v_cache) + hk * a.vc_head;
+  const int row = r0 + 32 * w + l32, i = row / G, p = s.n - s.m + i;
+  const bool real = row < s.rows;
+  // Scores stay as the products give them and are scaled where they go into
+  // the exponential, so the scale has to be positive: a negative one turns q's
+  // signs, and with 0 all scores are those of q = 0.
+  const uint32_t q_sign = a.scale < 0.0f ? 0x80008000u : 0u;
+  u4 q[KS];
+#pragma unroll
+  for (int x = 0; x < KS; ++x) {
+    const uint16_t *src = static_cast<const uint16_t *>(a.q) + (s.q0 + i) * a.q_token + (hk * G + row - i * G) * a.q_head;
+    q[x] = real && a.scale != 0.0f ? *reinterpret_cast<const u4 *>(src + 16 * x + 8 * h2) ^ q_sign : u4{0, 0, 0, 0};
+  }
+  f16v o[DB];
+  float sum;
+  if (!many_keys<DT, D, false>(a, s, table, kc, vc, q, p, real, sh, o, sum))
+    many_keys<DT, D, true>(a, s, table, kc, vc, q, p, real, sh, o, sum);
   sum += __shfl_xor(sum, 32, 64);
   if (!real) return;
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
@@ -542,6 +598,19 @@ __global__ __launch_bounds__(AT_THREADS) void k_attn_many(sb_attention_args a) {
 // would leave most of its products empty.
 bool many(const sb_attention_args &a) { return (long long)a.max_q * (a.q_heads / a.kv_heads) > 3 * FEW_ROWS; }
 
+// Keys a caller may expect a query to see at most.
+long long seen_keys(const sb_attention_args &a) {
+  return a.window > 0 ? std::min((long long)a.max_kv, (long long)a.window + a.sinks + a.max_q) : a.max_kv;
+}
+
+// Keys of one part: as many parts as there are (requests have caches of
+// different lengths, so that a part is a number of keys and not a share), at
+// least one tile a wave.
+int part_keys(const sb_attention_args &a, int splits) {
+  const long long step = FEW_KEYS * AT_WAVES;
+  return (int)std::max(step, ((seen_keys(a) + splits - 1) / splits + step - 1) / step * step);
+}
+
 template <int DT, int D>
 hipError_t launch(const sb_attention_args &a, int splits, float *parts, hipStream_t s) {
   if (many(a)) {
@@ -549,7 +618,8 @@ hipError_t launch(const sb_attention_args &a, int splits, float *parts, hipStrea
     hipLaunchKernelGGL((k_attn_many<DT, D>), dim3((unsigned)gx, a.kv_heads), dim3(AT_THREADS), 0, s, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((k_attn_few<DT, D>), dim3(a.n_requests, a.kv_heads, splits), dim3(AT_THREADS), 0, s, a, splits, parts);
+  hipLaunchKernelGGL((k_attn_few<DT, D>), dim3(a.n_requests, a.kv_heads, splits), dim3(AT_THREADS), 0, s, a, splits,
+                     part_keys(a, splits), parts);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || splits == 1) return e;
   const long long rows = (long long)a.n_tokens * a.q_heads;
@@ -561,9 +631,9 @@ hipError_t launch(const sb_attention_args &a, int splits, float *parts, hipStrea
 
 int attention_splits(const sb_attention_args &a, int n_cu) {
   if (many(a)) return 1;
-  const long long seen = a.window > 0 ? std::min((long long)a.max_kv, (long long)a.window + a.sinks + a.max_q) : a.max_kv;
-  const long long want = (4LL * n_cu + (long long)a.n_requests * a.kv_heads - 1) / ((long long)a.n_requests * a.kv_heads);
-  return (int)std::max(1LL, std::min({want, (seen + 255) / 256, 64LL}));
+  const long long groups = (long long)a.n_requests * a.kv_heads, step = FEW_KEYS * AT_WAVES;
+  const long long want = (6LL * n_cu + groups - 1) / groups;
+  return (int)std::max(1LL, std::min({want, (seen_keys(a) + step - 1) / step, 64LL}));
 }
 
 hipError_t launch_paged_attention(const sb_attention_args &a, int splits, float *parts, hipStream_t s) {
