@@ -4,173 +4,75 @@
 // where a released request's pages go on the free list, and how many tokens
 // and pages the requests before one take (a request is granted while both
 // sums, its own share included, stay within what there is, which is a prefix
-// of the requests). So one workgroup holds all requests, 8 a thread, and does
-// three scans; a step is bound by its latency, not by its bytes (20 a request,
-// 12 a token). The tokens' slots are written by a second, wide kernel, each
-// token finding its request by bisection of q_start.
+// of the requests). So one workgroup holds all requests and does one scan of
+// three sums; a step is bound by its latency - lengths, scan, free list, table,
+// each a trip to memory -, not by its bytes (20 a request, 12 a token). A step
+// of few tokens has its slots written by the same workgroup, each token finding
+// its request by bisection of q_start in LDS; more go to a second, wide kernel.
 #include "serve.h"
 
 namespace sb {
 namespace {
 
-constexpr int PLAN_THREADS = 1024;
-constexpr int PLAN_PER = SB_PLAN_MAX_REQUESTS / PLAN_THREADS;
+constexpr int PLAN_THREADS = 1024, PLAN_WAVES = PLAN_THREADS / 64;
+// Tokens that the planning workgroup writes itself: 4 a thread.
+constexpr int FUSED_TOKENS = 4 * PLAN_THREADS;
+
+struct Sums {
+  long long gone, tokens, pages;
+};
+
+struct PlanShared {
+  Sums wave[PLAN_WAVES];
+  unsigned long long granted_tokens, granted_pages;
+  int q_start[SB_PLAN_MAX_REQUESTS + 1];
+};
 
 // Exclusive prefix of v over the workgroup's threads; total: their sum.
-__device__ __forceinline__ long long scan_block(long long v, long long *wsum, long long &total) {
+__device__ __forceinline__ Sums scan_block(const Sums &v, PlanShared &sh, Sums &total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  long long x = v;
+  Sums x = v;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const long long y = __shfl_up(x, o, 64);
-    if (lane >= o) x += y;
+    const long long a = __shfl_up(x.gone, o, 64), b = __shfl_up(x.tokens, o, 64), c = __shfl_up(x.pages, o, 64);
+    if (lane >= o) {
+      x.gone += a;
+      x.tokens += b;
+      x.pages += c;
+    }
   }
-  __syncthreads();   // the last scan's sums have been read
-  if (lane == 63) wsum[w] = x;
+  if (lane == 63) sh.wave[w] = x;
   __syncthreads();
-  long long before = 0, all = 0;
+  Sums before = {0, 0, 0};
+  total = {0, 0, 0};
 #pragma unroll
-  for (int i = 0; i < PLAN_THREADS / 64; ++i) {
-    const long long s = wsum[i];
-    before += i < w ? s : 0;
-    all += s;
+  for (int i = 0; i < PLAN_WAVES; ++i) {
+    const Sums s = sh.wave[i];
+    if (i < w) {
+      before.gone += s.gone;
+      before.tokens += s.tokens;
+      before.pages += s.pages;
+    }
+    total.gone += s.gone;
+    total.tokens += s.tokens;
+    total.pages += s.pages;
   }
-  total = all;
-  return before + x - v;
+  return {before.gone + x.gone - v.gone, before.tokens + x.tokens - v.tokens, before.pages + x.pages - v.pages};
 }
 
-__global__ __launch_bounds__(PLAN_THREADS) void k_plan(sb_plan_args a) {
-  __shared__ long long wsum[PLAN_THREADS / 64];
-  __shared__ long long granted_sum[2];
-  const int B = a.n_requests, ps = a.page_size, lane = threadIdx.x & 63;
-  const int per = (B + PLAN_THREADS - 1) / PLAN_THREADS;
-  const long long room = (long long)a.max_pages * ps;
-  int len[PLAN_PER], want[PLAN_PER], held[PLAN_PER], at[PLAN_PER];
-  if (threadIdx.x < 2) granted_sum[threadIdx.x] = 0;
-
-  // Released pages, and their places on the free list.
-  long long mine = 0;
-#pragma unroll
-  for (int i = 0; i < PLAN_PER; ++i) {
-    const int b = threadIdx.x * per + i;
-    const bool on = i < per && b < B;
-    len[i] = on ? (int)min((long long)max(a.lens[b], 0), room) : 0;
-    want[i] = on ? a.add[b] : 0;
-    held[i] = (int)(((long long)len[i] + ps - 1) / ps);
-    at[i] = (int)mine;
-    mine += want[i] < 0 ? held[i] : 0;
-  }
-  const int free0 = min(max(*a.n_free, 0), a.n_pages);
-  long long gone;
-  long long base = scan_block(mine, wsum, gone);
-#pragma unroll
-  for (int i = 0; i < PLAN_PER; ++i) {
-    if (i >= per) break;
-    // The wave copies one released request after the other, 64 pages at once.
-    unsigned long long m = __ballot(want[i] < 0 && held[i] > 0);
-    while (m) {
-      const int src = __builtin_ctzll(m);
-      m &= m - 1;
-      const int b = (int)(threadIdx.x - lane + src) * per + i;
-      const int n = __shfl(held[i], src, 64);
-      const long long to = free0 + __shfl(base, src, 64) + __shfl(at[i], src, 64);
-      for (int c = lane; c < n; c += 64)
-        if (to + c < a.n_pages) a.free_list[to + c] = a.table[(long long)b * a.table_stride + c];
-    }
-  }
-  const int stack = (int)min((long long)free0 + gone, (long long)a.n_pages);
-
-  // Grants: prefix sums of the tokens and pages asked for.
-  int toks[PLAN_PER], need[PLAN_PER];
-  long long st = 0, sp = 0;
-#pragma unroll
-  for (int i = 0; i < PLAN_PER; ++i) {
-    toks[i] = want[i] > 0 && (long long)len[i] + want[i] <= room ? want[i] : 0;
-    need[i] = toks[i] ? (int)(((long long)len[i] + toks[i] + ps - 1) / ps) - held[i] : 0;
-    st += toks[i];
-    sp += need[i];
-  }
-  long long all;
-  long long bt = scan_block(st, wsum, all);   // its barriers also order the pushes before the pops
-  long long bp = scan_block(sp, wsum, all);
-  long long last_t = 0, last_p = 0;           // sums up to this thread's last request that is granted
-  int first[PLAN_PER];
-#pragma unroll
-  for (int i = 0; i < PLAN_PER; ++i) {
-    first[i] = 0;
-    const bool fits = bt + toks[i] <= a.token_cap && bp + need[i] <= stack;
-    bt += toks[i];
-    bp += need[i];
-    if (fits) {
-      first[i] = (int)(bp - need[i]);
-      last_t = bt;
-      last_p = bp;
-    } else {
-      toks[i] = need[i] = 0;
-    }
-  }
-  // (The sums only grow, so the largest granted one is everybody's total.)
-  atomicMax(&granted_sum[0], last_t);
-  atomicMax(&granted_sum[1], last_p);
-  __syncthreads();
-  const long long T = granted_sum[0];
-#pragma unroll
-  for (int i = 0; i < PLAN_PER; ++i) {
-    if (i >= per) break;
-    const int b = threadIdx.x * per + i;
-    const bool on = b < B;
-    if (!on) toks[i] = need[i] = 0;
-    unsigned long long m = __ballot(need[i] > 1);
-    if (on && need[i] == 1) {   // a step of single tokens: one page here and there
-      a.table[(long long)b * a.table_stride + held[i]] = a.free_list[stack - 1 - first[i]];
-    }
-    while (m) {
-      const int src = __builtin_ctzll(m);
-      m &= m - 1;
-      const int bb = (int)(threadIdx.x - lane + src) * per + i;
-      const int n = __shfl(need[i], src, 64), f = __shfl(first[i], src, 64), h = __shfl(held[i], src, 64);
-      for (int c = lane; c < n; c += 64)
-        a.table[(long long)bb * a.table_stride + h + c] = a.free_list[stack - 1 - f - c];
-    }
-  }
-  // First tokens: the sum before each request, or all of them behind the
-  // last granted one.
-  long long s0 = 0;
-#pragma unroll
-  for (int i = 0; i < PLAN_PER; ++i) s0 += toks[i];
-  s0 = scan_block(s0, wsum, all);
-#pragma unroll
-  for (int i = 0; i < PLAN_PER; ++i) {
-    const int b = threadIdx.x * per + i;
-    if (i < per && b < B) {
-      a.q_start[b] = (int)s0;
-      s0 += toks[i];
-      a.granted[b] = toks[i];
-      a.lens_out[b] = want[i] < 0 ? 0 : len[i] + toks[i];
-    }
-  }
-  if (threadIdx.x == 0) {
-    a.q_start[B] = (int)T;
-    *a.n_free_out = stack - (int)granted_sum[1];
-  }
-}
-
-constexpr int SLOT_THREADS = 256;
-
-__global__ __launch_bounds__(SLOT_THREADS) void k_slots(sb_plan_args a) {
-  const int t = blockIdx.x * SLOT_THREADS + threadIdx.x;
-  if (t >= a.token_cap) return;
+// Slot and position of new token t; start: q_start, in LDS.
+__device__ __forceinline__ void put_slot(const sb_plan_args &a, const int *start, int t) {
   const int B = a.n_requests;
   long long slot = -1;
   int pos = -1;
-  if (t < a.q_start[B]) {
-    int lo = 0, hi = B;   // q_start[lo] <= t < q_start[hi]
+  if (t < start[B]) {
+    int lo = 0, hi = B;   // start[lo] <= t < start[hi]
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (a.q_start[mid] <= t) lo = mid;
+      if (start[mid] <= t) lo = mid;
       else hi = mid;
     }
-    pos = a.lens_out[lo] - a.granted[lo] + t - a.q_start[lo];
+    pos = a.lens_out[lo] - (start[lo + 1] - t);
     const int c = pos / a.page_size;
     const int page = a.table[(long long)lo * a.table_stride + c];
     if (page >= 0 && page < a.n_pages) slot = (long long)page * a.page_size + (pos - c * a.page_size);
@@ -179,13 +81,135 @@ __global__ __launch_bounds__(SLOT_THREADS) void k_slots(sb_plan_args a) {
   a.positions[t] = pos;
 }
 
+// PER neighbouring requests a thread.
+template <int PER>
+__global__ __launch_bounds__(PLAN_THREADS) void k_plan(sb_plan_args a, int fused) {
+  __shared__ PlanShared sh;
+  const int B = a.n_requests, ps = a.page_size, lane = threadIdx.x & 63, b0 = threadIdx.x * PER;
+  const long long room = (long long)a.max_pages * ps;
+  int len[PER], want[PER], held[PER], toks[PER], need[PER];
+  if (threadIdx.x == 0) sh.granted_tokens = sh.granted_pages = 0;
+  const int free0 = min(max(*a.n_free, 0), a.n_pages);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    len[i] = b0 + i < B ? a.lens[b0 + i] : 0;
+    want[i] = b0 + i < B ? a.add[b0 + i] : 0;
+  }
+  Sums mine = {0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    len[i] = (int)min((long long)max(len[i], 0), room);
+    held[i] = (int)(((long long)len[i] + ps - 1) / ps);
+    toks[i] = want[i] > 0 && (long long)len[i] + want[i] <= room ? want[i] : 0;
+    need[i] = toks[i] ? (int)(((long long)len[i] + toks[i] + ps - 1) / ps) - held[i] : 0;
+    mine.gone += want[i] < 0 ? held[i] : 0;
+    mine.tokens += toks[i];
+    mine.pages += need[i];
+  }
+  Sums total, at = scan_block(mine, sh, total);
+  const int stack = (int)min((long long)free0 + total.gone, (long long)a.n_pages);
+
+  // Released pages onto the free list: the wave copies one request after the
+  // other, 64 pages at once.
+  if (total.gone > 0) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int n = want[i] < 0 ? held[i] : 0;
+      unsigned long long m = __ballot(n > 0);
+      while (m) {
+        const int src = __builtin_ctzll(m);
+        m &= m - 1;
+        const int b = (int)(threadIdx.x - lane + src) * PER + i, count = __shfl(n, src, 64);
+        const long long to = free0 + __shfl(at.gone, src, 64);
+        for (int c = lane; c < count; c += 64)
+          if (to + c < a.n_pages) a.free_list[to + c] = a.table[(long long)b * a.table_stride + c];
+      }
+      at.gone += n;
+    }
+  }
+  // Grants.
+  int first[PER];
+  long long start[PER], last_t = 0, last_p = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    start[i] = at.tokens;
+    first[i] = (int)min(at.pages, (long long)stack);
+    at.tokens += toks[i];
+    at.pages += need[i];
+    if (at.tokens <= a.token_cap && at.pages <= stack) {
+      last_t = at.tokens;   // sums up to the last request that is granted
+      last_p = at.pages;
+    } else {
+      toks[i] = need[i] = 0;
+    }
+  }
+  // (The sums only grow, so the largest granted ones are everybody's totals.)
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    last_t = max(last_t, __shfl_xor(last_t, o, 64));
+    last_p = max(last_p, __shfl_xor(last_p, o, 64));
+  }
+  if (lane == 0) {
+    atomicMax(&sh.granted_tokens, (unsigned long long)last_t);
+    atomicMax(&sh.granted_pages, (unsigned long long)last_p);
+  }
+  __syncthreads();   // also: the pushes are there before the pops
+  const long long T = (long long)sh.granted_tokens;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int b = b0 + i;
+    if (need[i] == 1)   // a step of single tokens: one page here and there
+      a.table[(long long)b * a.table_stride + held[i]] = a.free_list[stack - 1 - first[i]];
+    unsigned long long m = __ballot(need[i] > 1);
+    while (m) {
+      const int src = __builtin_ctzll(m);
+      m &= m - 1;
+      const int bb = (int)(threadIdx.x - lane + src) * PER + i;
+      const int n = __shfl(need[i], src, 64), f = __shfl(first[i], src, 64), h = __shfl(held[i], src, 64);
+      for (int c = lane; c < n; c += 64)
+        a.table[(long long)bb * a.table_stride + h + c] = a.free_list[stack - 1 - f - c];
+    }
+    if (b < B) {
+      // The tokens asked for before it, all of which are granted if it is, or
+      // all that are.
+      const int q = (int)min(start[i], T);
+      a.q_start[b] = q;
+      if (fused) sh.q_start[b] = q;
+      a.granted[b] = toks[i];
+      a.lens_out[b] = want[i] < 0 ? 0 : len[i] + toks[i];
+    }
+  }
+  if (threadIdx.x == 0) {
+    a.q_start[B] = (int)T;
+    sh.q_start[B] = (int)T;
+    *a.n_free_out = stack - (int)sh.granted_pages;
+  }
+  if (!fused) return;
+  __syncthreads();
+  for (int t = threadIdx.x; t < a.token_cap; t += PLAN_THREADS) put_slot(a, sh.q_start, t);
+}
+
+constexpr int SLOT_THREADS = 256;
+
+__global__ __launch_bounds__(SLOT_THREADS) void k_slots(sb_plan_args a) {
+  extern __shared__ int start[];
+  for (int b = threadIdx.x; b <= a.n_requests; b += SLOT_THREADS) start[b] = a.q_start[b];
+  __syncthreads();
+  const int t = blockIdx.x * SLOT_THREADS + threadIdx.x;
+  if (t < a.token_cap) put_slot(a, start, t);
+}
+
 }  // namespace
 
 hipError_t launch_plan(const sb_plan_args &a, hipStream_t s) {
-  hipLaunchKernelGGL(k_plan, dim3(1), dim3(PLAN_THREADS), 0, s, a);
+  const int fused = a.token_cap <= FUSED_TOKENS;
+  if (a.n_requests <= PLAN_THREADS) hipLaunchKernelGGL(k_plan<1>, dim3(1), dim3(PLAN_THREADS), 0, s, a, fused);
+  else if (a.n_requests <= 2 * PLAN_THREADS) hipLaunchKernelGGL(k_plan<2>, dim3(1), dim3(PLAN_THREADS), 0, s, a, fused);
+  else hipLaunchKernelGGL(k_plan<SB_PLAN_MAX_REQUESTS / PLAN_THREADS>, dim3(1), dim3(PLAN_THREADS), 0, s, a, fused);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.token_cap == 0) return e;
-  hipLaunchKernelGGL(k_slots, dim3((a.token_cap + SLOT_THREADS - 1) / SLOT_THREADS), dim3(SLOT_THREADS), 0, s, a);
+  if (e != hipSuccess || fused) return e;
+  hipLaunchKernelGGL(k_slots, dim3((a.token_cap + SLOT_THREADS - 1) / SLOT_THREADS), dim3(SLOT_THREADS),
+                     (a.n_requests + 1) * sizeof(int), s, a);
   return hipGetLastError();
 }
 
