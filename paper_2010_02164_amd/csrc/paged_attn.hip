@@ -146,7 +146,7 @@ __device__ __forceinline__ int page_of(const sb_attention_args &a, const int *ta
 }
 
 __device__ __forceinline__ bool sees(const sb_attention_args &a, int p, int key) {
-  return key <= p && (a.window == 0 || key > p - a.window || key < a.sinks);
+  return (key <= p) & ((a.window == 0) | (key > p - a.window) | (key < a.sinks));   // (no branches)
 }
 
 // Parts of a split: sums [splits][n_tokens q_heads][D], then (maximum, sum).
@@ -386,14 +386,16 @@ __global__ __launch_bounds__(AT_THREADS) void k_attn_join(sb_attention_args a, i
   }
 }
 
-// What the waves of k_attn_many share.
+// What the waves of k_attn_many share: two tiles of K and V, one worked on
+// while the other is filled.
 template <int D>
 struct ManyShared {
   static constexpr int KSTR = 2 * D + 16, VSTR = 2 * D + 32;   // bytes of a K and a V row
-  alignas(16) unsigned char k[MANY_KEYS * KSTR];
-  alignas(16) unsigned char v[MANY_KEYS * VSTR];
-  uint32_t there[2][2];   // [parity][half]: keys of the tile that have a page
-  int not_fin[2];         // [parity]: V of a tile that not all rows see has values that are not finite
+  alignas(16) unsigned char k[2][MANY_KEYS * KSTR];
+  alignas(16) unsigned char v[2][MANY_KEYS * VSTR];
+  unsigned char none[2][MANY_KEYS];   // 1: the key's page is outside the cache; looked at only if
+  int odd[2];                         // bit 0 says that there are such, bit 1: values that are not
+                                      // finite, in a tile that not all rows see
 };
 
 // The workgroup's pass over its tiles: the lane's row's sums, and its keys'
@@ -402,9 +404,11 @@ template <int DT, int D, bool CAREFUL>
 __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span &s, const int *table, const uint16_t *kc, const uint16_t *vc,
                                           const u4 (&q)[D / 16], int p, bool real, ManyShared<D> &sh, f16v (&o)[D / 32], float &sum) {
   constexpr int KSTR = ManyShared<D>::KSTR, VSTR = ManyShared<D>::VSTR;
-  constexpr int PC = MANY_KEYS * (D / 8) / AT_THREADS;  // 16-byte pieces of K (and V) a thread brings
+  constexpr int PC = MANY_KEYS * (D / 8) / AT_THREADS;   // 16-byte pieces of K (and V) a thread brings,
+  constexpr int RSTEP = AT_THREADS / (D / 8);            // their rows so far apart
   constexpr int KS = D / 16, DB = D / 32;
   const int lane = threadIdx.x & 63, l32 = lane & 31, h2 = lane >> 5;
+  const int row0 = threadIdx.x / (D / 8), col = threadIdx.x % (D / 8);
   const double inv_page = 1.0 / a.page_size;
   const float c = a.scale == 0.0f ? 1.0f : (float)(fabs((double)a.scale) * LOG2E);
 #pragma unroll
@@ -417,49 +421,73 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
   float ref = -INFINITY;
   sum = 0.0f;
 
+  // A tile's way: its pages are looked up two tiles ahead, its rows loaded one
+  // and a half ahead, written to LDS one ahead. Keys behind the last one are
+  // the last one again, which no row sees there.
   u4 kr[PC], vr[PC];
+  int page[PC], place[PC];
+  uint32_t gone = 0;   // bit x: piece x in the registers has no page
   const int tiles = (s.n_vis + MANY_KEYS - 1) / MANY_KEYS;
-  auto bring = [&](int t) {
+  auto look_up = [&](int t) {
+#pragma unroll
+    for (int x = 0; x < PC; ++x)
+      page[x] = page_of(a, table, inv_page, s.key(min(t * MANY_KEYS + row0 + x * RSTEP, s.n_vis - 1)), place[x]);
+  };
+  auto load = [&] {
+    gone = 0;
 #pragma unroll
     for (int x = 0; x < PC; ++x) {
-      const int piece = x * AT_THREADS + threadIdx.x, kk = piece / (D / 8), col = (piece - kk * (D / 8)) * 8;
-      const int u = t * MANY_KEYS + kk;
-      int place = 0;
-      const int page = u < s.n_vis ? page_of(a, table, inv_page, s.key(u), place) : -1;
-      kr[x] = vr[x] = u4{0, 0, 0, 0};
-      if (page >= 0) {
-        kr[x] = *reinterpret_cast<const u4 *>(kc + page * a.kc_page + place * a.kc_slot + col);
-        vr[x] = *reinterpret_cast<const u4 *>(vc + page * a.vc_page + place * a.vc_slot + col);
-      }
+      const int pg = max(page[x], 0);   // (any page for none)
+      kr[x] = *reinterpret_cast<const u4 *>(kc + pg * a.kc_page + place[x] * a.kc_slot + col * 8);
+      vr[x] = *reinterpret_cast<const u4 *>(vc + pg * a.vc_page + place[x] * a.vc_slot + col * 8);
+      gone |= (page[x] < 0 ? 1u : 0u) << x;
     }
-    if (threadIdx.x < MANY_KEYS) {
-      const int u = t * MANY_KEYS + threadIdx.x;
-      int place = 0;
-      const unsigned long long m = __ballot(u < s.n_vis && page_of(a, table, inv_page, s.key(u), place) >= 0);
-      if (threadIdx.x < 2) sh.there[t & 1][threadIdx.x] = (uint32_t)(m >> (32 * threadIdx.x));
+  };
+  auto write = [&](int t) {
+    const bool shared = s.all_see(a, s.key(t * MANY_KEYS), s.key(t * MANY_KEYS + MANY_KEYS - 1));
+    const int to = t & 1;
+    bool bad = false;
+    if (gone) {
+#pragma unroll
+      for (int x = 0; x < PC; ++x)
+        if ((gone >> x) & 1u) vr[x] = u4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int x = 0; x < PC; ++x) {
+      const int kk = row0 + x * RSTEP;
+      *reinterpret_cast<u4 *>(&sh.k[to][kk * KSTR + col * 16]) = kr[x];
+      *reinterpret_cast<u4 *>(&sh.v[to][kk * VSTR + col * 16]) = vr[x];
+      if (!CAREFUL && !shared) finite_only<DT>(vr[x], bad);
+    }
+    if (gone || bad) {
+#pragma unroll
+      for (int x = 0; x < PC; ++x) sh.none[to][row0 + x * RSTEP] = (gone >> x) & 1u;
+      atomicOr(&sh.odd[to], (gone ? 1 : 0) | (bad ? 2 : 0));
     }
   };
   __syncthreads();
-  if (threadIdx.x < 2) sh.not_fin[threadIdx.x] = 0;
-  if (tiles > 0) bring(0);
+  if (threadIdx.x < 2) sh.odd[threadIdx.x] = 0;
+  for (int x = threadIdx.x; x < 2 * MANY_KEYS; x += AT_THREADS) (&sh.none[0][0])[x] = 0;
   __syncthreads();
+  if (tiles > 0) {
+    look_up(0);
+    load();
+    look_up(1);
+    write(0);
+    load();
+    look_up(2);
+  }
   for (int t = 0; t < tiles; ++t) {
-    const int u0 = t * MANY_KEYS;
-    const bool shared = s.all_see(a, s.key(u0), s.key(u0 + MANY_KEYS - 1));
-    bool bad = false;
-#pragma unroll
-    for (int x = 0; x < PC; ++x) {
-      const int piece = x * AT_THREADS + threadIdx.x, kk = piece / (D / 8), col = (piece - kk * (D / 8)) * 16;
-      *reinterpret_cast<u4 *>(&sh.k[kk * KSTR + col]) = kr[x];
-      *reinterpret_cast<u4 *>(&sh.v[kk * VSTR + col]) = vr[x];
-      if (!CAREFUL && !shared) finite_only<DT>(vr[x], bad);
+    __syncthreads();   // tile t is there, and the other buffer has been read
+    const int odd = sh.odd[t & 1], u0 = t * MANY_KEYS;
+    if (!CAREFUL && (odd & 2)) return false;
+    if (t + 1 < tiles) {
+      write(t + 1);
+      load();
+      look_up(t + 3);
     }
-    if (bad) sh.not_fin[t & 1] = 1;
-    __syncthreads();
-    const uint32_t on0 = sh.there[t & 1][0], on1 = sh.there[t & 1][1];
-    if (!CAREFUL && sh.not_fin[t & 1]) return false;
-    if (threadIdx.x == 0) sh.not_fin[(t + 1) & 1] = 0;
-    if (t + 1 < tiles) bring(t + 1);
+    const unsigned char *sk = sh.k[t & 1], *sv = sh.v[t & 1];
+    const bool shared = s.all_see(a, s.key(u0), s.key(u0 + MANY_KEYS - 1));
     f16v sc[2];
 #pragma unroll
     for (int kb = 0; kb < 2; ++kb) {
@@ -467,20 +495,24 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
       for (int e = 0; e < 16; ++e) sc[kb][e] = 0.0f;
 #pragma unroll
       for (int x = 0; x < KS; ++x) {
-        const u4 kf = *reinterpret_cast<const u4 *>(&sh.k[(32 * kb + l32) * KSTR + 32 * x + 16 * h2]);
+        const u4 kf = *reinterpret_cast<const u4 *>(&sk[(32 * kb + l32) * KSTR + 32 * x + 16 * h2]);
         sc[kb] = mfma32<DT>(kf, q[x], sc[kb]);
       }
     }
     // Lane: keys 32 kb + 8 (e / 4) + 4 h2 + e % 4 of row l32.
-    if ((on0 & on1) != 0xFFFFFFFFu || !shared) {
+    if (!shared) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int at = 8 * (e >> 2) + 4 * h2 + (e & 3);
-          const bool on = real && (((kb ? on1 : on0) >> at) & 1u) && sees(a, p, s.key(u0 + 32 * kb + at));
-          sc[kb][e] = on ? sc[kb][e] : -INFINITY;
-        }
+        for (int e = 0; e < 16; ++e)
+          sc[kb][e] = sees(a, p, s.key(u0 + 32 * kb + 8 * (e >> 2) + 4 * h2 + (e & 3))) ? sc[kb][e] : -INFINITY;
+    }
+    if (odd & 1) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (sh.none[t & 1][32 * kb + 8 * (e >> 2) + 4 * h2 + (e & 3)]) sc[kb][e] = -INFINITY;
     }
     float tm = -INFINITY;
 #pragma unroll
@@ -509,7 +541,7 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
         pk[2 * kb + (e >> 3)][(e & 7) >> 1] = Half<DT>::pack(x, y);
       }
     sum += ts[0] + ts[1];
-    const unsigned char *vt = &sh.v[(4 * h2 + ((lane & 15) >> 2)) * VSTR + ((lane >> 4) & 1) * 32 + (lane & 3) * 8];
+    const unsigned char *vt = &sv[(4 * h2 + ((lane & 15) >> 2)) * VSTR + ((lane >> 4) & 1) * 32 + (lane & 3) * 8];
     if (CAREFUL && !shared) {
 #pragma unroll
       for (int x = 0; x < DB; ++x) {
@@ -524,9 +556,10 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[x][e] = hit[e] > 0.0f ? NAN : o[x][e];
       }
+      bool bad = false;
       __syncthreads();
       for (int piece = threadIdx.x; piece < MANY_KEYS * (D / 8); piece += AT_THREADS) {
-        u4 *at = reinterpret_cast<u4 *>(&sh.v[piece / (D / 8) * VSTR + piece % (D / 8) * 16]);
+        u4 *at = reinterpret_cast<u4 *>(&sh.v[t & 1][piece / (D / 8) * VSTR + piece % (D / 8) * 16]);
         *at = finite_only<DT>(*at, bad);
       }
       __syncthreads();
@@ -538,7 +571,11 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
         const u2 v0 = read_transposed(vt + 16 * ks * VSTR + 64 * x), v1 = read_transposed(vt + (16 * ks + 8) * VSTR + 64 * x);
         o[x] = mfma32<DT>(u4{v0[0], v0[1], v1[0], v1[1]}, pk[ks], o[x]);
       }
-    __syncthreads();
+    if (odd) {   // for the tile that comes into this buffer
+      __syncthreads();
+      for (int x = threadIdx.x; x < MANY_KEYS; x += AT_THREADS) sh.none[t & 1][x] = 0;
+      if (threadIdx.x == 0) sh.odd[t & 1] = 0;
+    }
   }
   return true;
 }
