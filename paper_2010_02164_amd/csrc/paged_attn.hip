@@ -393,6 +393,7 @@ struct ManyShared {
   static constexpr int KSTR = 2 * D + 16, VSTR = 2 * D + 32;   // bytes of a K and a V row
   alignas(16) unsigned char k[2][MANY_KEYS * KSTR];
   alignas(16) unsigned char v[2][MANY_KEYS * VSTR];
+  longlong2 at[2][MANY_KEYS];         // where a tile's rows of K and V lie; none (below 0): nowhere
   unsigned char none[2][MANY_KEYS];   // 1: the key's page is outside the cache; looked at only if
   int odd[2];                         // bit 0 says that there are such, bit 1: values that are not
                                       // finite, in a tile that not all rows see
@@ -421,26 +422,29 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
   float ref = -INFINITY;
   sum = 0.0f;
 
-  // A tile's way: its pages are looked up two tiles ahead, its rows loaded one
-  // and a half ahead, written to LDS one ahead. Keys behind the last one are
-  // the last one again, which no row sees there.
+  // A tile's way: its pages are looked up four tiles ahead, by one wave, a key
+  // a lane; the places of its rows are written to LDS three ahead, its rows
+  // loaded two ahead and written to LDS one ahead. Keys behind the last one
+  // are the last one again, which no row sees there.
   u4 kr[PC], vr[PC];
-  int page[PC], place[PC];
+  int page = 0, place = 0;
   uint32_t gone = 0;   // bit x: piece x in the registers has no page
-  const int tiles = (s.n_vis + MANY_KEYS - 1) / MANY_KEYS;
+  const int tiles = (s.n_vis + MANY_KEYS - 1) / MANY_KEYS, wave = threadIdx.x >> 6;
   auto look_up = [&](int t) {
-#pragma unroll
-    for (int x = 0; x < PC; ++x)
-      page[x] = page_of(a, table, inv_page, s.key(min(t * MANY_KEYS + row0 + x * RSTEP, s.n_vis - 1)), place[x]);
+    if (wave == (t & 3)) page = page_of(a, table, inv_page, s.key(min(t * MANY_KEYS + lane, s.n_vis - 1)), place);
   };
-  auto load = [&] {
+  auto put_at = [&](int t) {
+    if (wave == (t & 3))
+      sh.at[t & 1][lane] = page < 0 ? longlong2{-1, -1} : longlong2{page * a.kc_page + place * a.kc_slot, page * a.vc_page + place * a.vc_slot};
+  };
+  auto load = [&](int t) {
     gone = 0;
 #pragma unroll
     for (int x = 0; x < PC; ++x) {
-      const int pg = max(page[x], 0);   // (any page for none)
-      kr[x] = *reinterpret_cast<const u4 *>(kc + pg * a.kc_page + place[x] * a.kc_slot + col * 8);
-      vr[x] = *reinterpret_cast<const u4 *>(vc + pg * a.vc_page + place[x] * a.vc_slot + col * 8);
-      gone |= (page[x] < 0 ? 1u : 0u) << x;
+      const longlong2 at = sh.at[t & 1][row0 + x * RSTEP];
+      kr[x] = *reinterpret_cast<const u4 *>(kc + max(at.x, 0LL) + col * 8);   // (any row for none)
+      vr[x] = *reinterpret_cast<const u4 *>(vc + max(at.y, 0LL) + col * 8);
+      gone |= (at.x < 0 ? 1u : 0u) << x;
     }
   };
   auto write = [&](int t) {
@@ -470,21 +474,28 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
   for (int x = threadIdx.x; x < 2 * MANY_KEYS; x += AT_THREADS) (&sh.none[0][0])[x] = 0;
   __syncthreads();
   if (tiles > 0) {
-    look_up(0);
-    load();
-    look_up(1);
-    write(0);
-    load();
-    look_up(2);
+    for (int t = 0; t < 3; ++t) {   // the first three tiles' places; tile 0 all the way
+      if (t == 2) {
+        load(0);
+        write(0);
+        __syncthreads();
+      }
+      look_up(t);
+      put_at(t);
+      __syncthreads();
+    }
+    load(1);
+    look_up(3);
   }
   for (int t = 0; t < tiles; ++t) {
-    __syncthreads();   // tile t is there, and the other buffer has been read
+    __syncthreads();   // tile t is there, the places of tile t + 2 are, and the other buffer has been read
     const int odd = sh.odd[t & 1], u0 = t * MANY_KEYS;
     if (!CAREFUL && (odd & 2)) return false;
     if (t + 1 < tiles) {
       write(t + 1);
-      load();
-      look_up(t + 3);
+      load(t + 2);
+      put_at(t + 3);
+      look_up(t + 4);
     }
     const unsigned char *sk = sh.k[t & 1], *sv = sh.v[t & 1];
     const bool shared = s.all_see(a, s.key(u0), s.key(u0 + MANY_KEYS - 1));
