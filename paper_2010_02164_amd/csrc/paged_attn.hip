@@ -499,16 +499,33 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
     }
     const unsigned char *sk = sh.k[t & 1], *sv = sh.v[t & 1];
     const bool shared = s.all_see(a, s.key(u0), s.key(u0 + MANY_KEYS - 1));
+    // Operands come from LDS AHEAD products before they are needed.
+    constexpr int AHEAD = 4;
     f16v sc[2];
+    {
+      const unsigned char *kp = &sk[l32 * KSTR + 16 * h2];
+      u4 kf[AHEAD];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+      for (int x = 0; x < AHEAD; ++x) kf[x] = *reinterpret_cast<const u4 *>(kp + (x & 1) * 32 * KSTR + 32 * (x >> 1));
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sc[kb][e] = 0.0f;
+      for (int e = 0; e < 16; ++e) sc[0][e] = sc[1][e] = 0.0f;
 #pragma unroll
-      for (int x = 0; x < KS; ++x) {
-        const u4 kf = *reinterpret_cast<const u4 *>(&sk[(32 * kb + l32) * KSTR + 32 * x + 16 * h2]);
-        sc[kb] = mfma32<DT>(kf, q[x], sc[kb]);
+      for (int x = 0; x < 2 * KS; ++x) {
+        sc[x & 1] = mfma32<DT>(kf[x % AHEAD], q[x >> 1], sc[x & 1]);
+        const int y = x + AHEAD;
+        if (y < 2 * KS) kf[x % AHEAD] = *reinterpret_cast<const u4 *>(kp + (y & 1) * 32 * KSTR + 32 * (y >> 1));
       }
+    }
+    const unsigned char *vt = &sv[(4 * h2 + ((lane & 15) >> 2)) * VSTR + ((lane >> 4) & 1) * 32 + (lane & 3) * 8];
+    auto v_frag = [&](int x) {   // of product x: keys 16 (x / DB) .. + 15, values 32 (x % DB) .. + 31
+      const unsigned char *at = vt + 16 * (x / DB) * VSTR + 64 * (x % DB);
+      const u2 v0 = read_transposed(at), v1 = read_transposed(at + 8 * VSTR);
+      return u4{v0[0], v0[1], v1[0], v1[1]};
+    };
+    u4 vf[AHEAD];
+    if (!CAREFUL) {
+#pragma unroll
+      for (int x = 0; x < AHEAD; ++x) vf[x] = v_frag(x);
     }
     // Lane: keys 32 kb + 8 (e / 4) + 4 h2 + e % 4 of row l32.
     if (!shared) {
@@ -552,7 +569,6 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
         pk[2 * kb + (e >> 3)][(e & 7) >> 1] = Half<DT>::pack(x, y);
       }
     sum += ts[0] + ts[1];
-    const unsigned char *vt = &sv[(4 * h2 + ((lane & 15) >> 2)) * VSTR + ((lane >> 4) & 1) * 32 + (lane & 3) * 8];
     if (CAREFUL && !shared) {
 #pragma unroll
       for (int x = 0; x < DB; ++x) {
@@ -575,13 +591,15 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
       }
       __syncthreads();
     }
+    if (CAREFUL) {
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks)
+      for (int x = 0; x < AHEAD; ++x) vf[x] = v_frag(x);
+    }
 #pragma unroll
-      for (int x = 0; x < DB; ++x) {
-        const u2 v0 = read_transposed(vt + 16 * ks * VSTR + 64 * x), v1 = read_transposed(vt + (16 * ks + 8) * VSTR + 64 * x);
-        o[x] = mfma32<DT>(u4{v0[0], v0[1], v1[0], v1[1]}, pk[ks], o[x]);
-      }
+    for (int x = 0; x < 4 * DB; ++x) {
+      o[x % DB] = mfma32<DT>(vf[x % AHEAD], pk[x / DB], o[x % DB]);
+      if (x + AHEAD < 4 * DB) vf[x % AHEAD] = v_frag(x + AHEAD);
+    }
     if (odd) {   // for the tile that comes into this buffer
       __syncthreads();
       for (int x = threadIdx.x; x < MANY_KEYS; x += AT_THREADS) sh.none[t & 1][x] = 0;
@@ -596,10 +614,12 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : 2) void k_attn_many(sb_a
   constexpr int KS = D / 16, DB = D / 32;
   __shared__ ManyShared<D> sh;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, h2 = lane >> 5;
-  const int G = a.q_heads / a.kv_heads, hk = blockIdx.y;
+  // Heads side by side: workgroups go to the 8 XCDs in turn, so that tiles of
+  // one head, which read the same keys, share an L2.
+  const int G = a.q_heads / a.kv_heads, hk = (int)(blockIdx.x % a.kv_heads);
   // The request of this tile: request b's tiles start at q_start[b] G / 128 + b,
   // which leaves at least one place a tile; the last ones of some stay empty.
-  const int tile = (int)(gridDim.x - 1 - blockIdx.x);
+  const int tile = (int)((gridDim.x - 1 - blockIdx.x) / a.kv_heads);   // (long prompts' last tiles first)
   int b = 0, bh = a.n_requests;
   while (bh - b > 1) {
     const int mid = (b + bh) >> 1;
@@ -663,7 +683,7 @@ template <int DT, int D>
 hipError_t launch(const sb_attention_args &a, int splits, float *parts, hipStream_t s) {
   if (many(a)) {
     const long long gx = (long long)a.n_tokens * (a.q_heads / a.kv_heads) / MANY_ROWS + a.n_requests;
-    hipLaunchKernelGGL((k_attn_many<DT, D>), dim3((unsigned)gx, a.kv_heads), dim3(AT_THREADS), 0, s, a);
+    hipLaunchKernelGGL((k_attn_many<DT, D>), dim3((unsigned)(gx * a.kv_heads)), dim3(AT_THREADS), 0, s, a);
     return hipGetLastError();
   }
   hipLaunchKernelGGL((k_attn_few<DT, D>), dim3(a.n_requests, a.kv_heads, splits), dim3(AT_THREADS), 0, s, a, splits,
