@@ -218,20 +218,22 @@ __device__ __forceinline__ bool few_keys(const sb_attention_args &a, const Span 
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) sc[hf] = mfma16<DT>(k[hf][x], q[x], sc[hf]);
     load_v(v, page, place);
-    // Lane: keys 16 hf + 4 g4 + j of row l16.
-    float tm = -INFINITY;
+    // Lane: keys 16 hf + 4 g4 + j of row l16, as scalars from here on (masks
+    // written into the products' vectors have been compiled wrongly).
+    float e[8];
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
+    for (int x = 0; x < 8; ++x) e[x] = sc[x >> 2][x & 3] * c;
+    if (!plain) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        sc[hf][j] *= c;
-        if (!plain) {
-          const int at = 16 * hf + 4 * g4 + j;
-          const bool on = real && ((there >> at) & 1u) && sees(a, p, s.key(t * FEW_KEYS + at));
-          sc[hf][j] = on ? sc[hf][j] : -INFINITY;
-        }
-        tm = fmaxf(tm, sc[hf][j]);
+      for (int x = 0; x < 8; ++x) {
+        const int at = 16 * (x >> 2) + 4 * g4 + (x & 3);
+        const bool on = real & (((there >> at) & 1u) != 0) & sees(a, p, s.key(t * FEW_KEYS + at));
+        e[x] = on ? e[x] : -INFINITY;
       }
+    }
+    float tm = e[0];
+#pragma unroll
+    for (int x = 1; x < 8; ++x) tm = fmaxf(tm, e[x]);
     tm = fmaxf(tm, __shfl_xor(tm, 16, 64));
     tm = fmaxf(tm, __shfl_xor(tm, 32, 64));
     const float mn = fmaxf(mx, tm), base = mn == -INFINITY ? 0.0f : mn;
@@ -239,15 +241,12 @@ __device__ __forceinline__ bool few_keys(const sb_attention_args &a, const Span 
     mx = mn;
     float ts = 0.0f;
 #pragma unroll
-    for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        sc[hf][j] = __builtin_amdgcn_exp2f(sc[hf][j] - base);
-        ts += sc[hf][j];
-      }
+    for (int x = 0; x < 8; ++x) {
+      e[x] = __builtin_amdgcn_exp2f(e[x] - base);
+      ts += e[x];
+    }
     sum = sum * shrink + ts;
-    const u4 pk = {Half<DT>::pack(sc[0][0], sc[0][1]), Half<DT>::pack(sc[0][2], sc[0][3]),
-                   Half<DT>::pack(sc[1][0], sc[1][1]), Half<DT>::pack(sc[1][2], sc[1][3])};
+    const u4 pk = {Half<DT>::pack(e[0], e[1]), Half<DT>::pack(e[2], e[3]), Half<DT>::pack(e[4], e[5]), Half<DT>::pack(e[6], e[7])};
     bool bad = false;
 #pragma unroll
     for (int x = 0; x < NV; ++x) {
@@ -538,26 +537,25 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
 #pragma unroll
       for (int x = 0; x < AHEAD; ++x) vf[x] = v_frag(x);
     }
-    // Lane: keys 32 kb + 8 (e / 4) + 4 h2 + e % 4 of row l32.
+    // Lane: keys 32 (x / 16) + 8 (x % 16 / 4) + 4 h2 + x % 4 of row l32, as
+    // scalars from here on (masks written into the products' vectors have been
+    // compiled wrongly).
+    float e[32];
+#pragma unroll
+    for (int x = 0; x < 32; ++x) e[x] = sc[x >> 4][x & 15];
     if (!shared) {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          sc[kb][e] = sees(a, p, s.key(u0 + 32 * kb + 8 * (e >> 2) + 4 * h2 + (e & 3))) ? sc[kb][e] : -INFINITY;
+      for (int x = 0; x < 32; ++x)
+        e[x] = sees(a, p, s.key(u0 + 32 * (x >> 4) + 8 * ((x & 15) >> 2) + 4 * h2 + (x & 3))) ? e[x] : -INFINITY;
     }
     if (odd & 1) {
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (sh.none[t & 1][32 * kb + 8 * (e >> 2) + 4 * h2 + (e & 3)]) sc[kb][e] = -INFINITY;
+      for (int x = 0; x < 32; ++x)
+        e[x] = sh.none[t & 1][32 * (x >> 4) + 8 * ((x & 15) >> 2) + 4 * h2 + (x & 3)] ? -INFINITY : e[x];
     }
-    float tm = -INFINITY;
+    float tm = e[0];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) tm = fmaxf(tm, sc[kb][e]);
+    for (int x = 1; x < 32; ++x) tm = fmaxf(tm, e[x]);
     tm = fmaxf(tm, __shfl_xor(tm, 32, 64));
     if (__any(tm > ref && !(c * (tm - ref) <= GROW))) {
       const float mn = fmaxf(ref, tm);
@@ -571,14 +569,12 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
     float ts[2] = {0.0f, 0.0f};
     u4 pk[4];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int e = 0; e < 16; e += 2) {
-        const float x = __builtin_amdgcn_exp2f(fmaf(sc[kb][e], c, -base)), y = __builtin_amdgcn_exp2f(fmaf(sc[kb][e + 1], c, -base));
-        ts[0] += x;
-        ts[1] += y;
-        pk[2 * kb + (e >> 3)][(e & 7) >> 1] = Half<DT>::pack(x, y);
-      }
+    for (int x = 0; x < 32; x += 2) {
+      const float f = __builtin_amdgcn_exp2f(fmaf(e[x], c, -base)), g = __builtin_amdgcn_exp2f(fmaf(e[x + 1], c, -base));
+      ts[0] += f;
+      ts[1] += g;
+      pk[x >> 3][(x & 7) >> 1] = Half<DT>::pack(f, g);
+    }
     sum += ts[0] + ts[1];
     if (CAREFUL && !shared) {
 #pragma unroll
