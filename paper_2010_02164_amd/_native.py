@@ -120,7 +120,8 @@ def lib():
         "sb_rope_append": (c_int32, [c_char_p, c_void_p]),
         "sb_attention_workspace": (c_int64, [c_char_p]),
         "sb_paged_attention": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
-        "sb_sample_tokens": (c_int32, [c_char_p, c_void_p]),
+        "sb_sample_workspace": (c_int64, [c_char_p]),
+        "sb_sample_tokens": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
         "sb_destroy": (c_int32, [c_void_p]),
         "sb_last_error": (c_char_p, [c_void_p]),
         "sb_status_string": (c_char_p, [c_int32]),

@@ -12,9 +12,13 @@
 // the row lists the tokens from that bound on, a few hundred, and all searches
 // run on the list in registers and LDS; a list of fewer than k tokens sends the
 // row the other way. min-p alone bounds the tokens by the sample's largest.
-// top-p without top-k needs every weight: a second pass adds them up into bins
-// of equal ratio, which names the bin that the cut is in, a third lists that
-// bin, a fourth draws; they read caches.
+//
+// Rows without top-k but with top-p need every weight. A pass adds them up into
+// bins of equal ratio, which names the bin that the cut is in, a second lists
+// that bin, a third draws; they read caches, and are bound by the 22 fp64 and
+// integer operations of a weight. One workgroup took such a row 2 to 4 times as
+// long as the others; with a workspace the passes run as kernels of their own,
+// in chunks over all compute units.
 //
 // Weights are whole multiples of 2^-44 in 64-bit integers: up to 2^18 of them
 // add up without rounding or overflow, in any order, so that partial sums of
@@ -35,6 +39,9 @@ constexpr double ONE = 0x1p44;        // the weight of the largest logit
 constexpr int LIST_PER = 4, LIST_MAX = LIST_PER * SM_THREADS;
 constexpr int BIN_BITS = 9, BINS = 1 << BIN_BITS;
 constexpr int TAB_BITS = 9;           // 2^x by a table of 2^(i / 512) and a cubic
+constexpr int TAB = 1 << TAB_BITS;
+constexpr int CHUNK = 16384;          // tokens of a row that a workgroup of the wide kernels takes
+constexpr int CHUNKS_MAX = SB_SAMPLE_MAX_VOCAB / CHUNK;
 // The largest top-k that is read off the sample: the list then aims at twice
 // as many tokens, and 256 more.
 constexpr int SAMPLED_K = 1536;
@@ -112,7 +119,7 @@ struct Row {
 };
 
 struct Shared {
-  double tab[1 << TAB_BITS];   // 2^(i / 512)
+  double tab[TAB];             // 2^(44 + i / 512)
   u64 hist[BINS];
   u64 part[SM_WAVES], ends[2][8];
   uint32_t key[LIST_MAX];      // listed tokens: order bits
@@ -125,33 +132,30 @@ struct Shared {
 // A row's weights: 2^44 exp((z - top) / T), rounded.
 struct Weigher {
   const double *tab;
-  double top, c;   // c = log2(e) / T. With a largest logit of +inf: 2^128 and 1, far from all others
+  double top, c;   // c = 512 log2(e) / T. With a largest logit of +inf: 2^128 and 512, far from all others
   __device__ __forceinline__ Weigher(const double *t, float largest, float T)
-      : tab(t), top(largest == INFINITY ? 0x1p128 : (double)largest), c(largest == INFINITY ? 1.0 : 1.4426950408889634074 / (double)T) {}
-  // log2 of the weight (of the largest: 0). NaN, and -inf with T = inf: -64.
-  __device__ __forceinline__ double log2w(float z) const { return fmin(fmax(((double)z - top) * c, -64.0), 0.0); }
-  // x = n / 512 + r with |r| <= 2^-10: 2^x = 2^(n / 512) (1 + r ln 2 + ...);
-  // the cubic leaves out (2^-10 ln 2)^4 / 24 = 2^-46.7.
-  __device__ __forceinline__ u64 of(double x) const {
-    constexpr double MAGIC = 0x1.8p43;   // its last bit is worth 2^-9
+      : tab(t), top(largest == INFINITY ? 0x1p128 : (double)largest),
+        c(largest == INFINITY ? TAB : TAB * 1.4426950408889634074 / (double)T) {}
+  // 512 log2 of the weight (of the largest: 0). NaN, and -inf with T = inf: the lowest.
+  static constexpr double LOW = -64.0 * TAB;
+  __device__ __forceinline__ double log2w(float z) const { return fmin(fmax(((double)z - top) * c, LOW), 0.0); }
+  // x = n + r with |r| <= 1/2: 2^(x / 512) = 2^(n / 512) (1 + r ln 2 / 512 + ...);
+  // the cubic leaves out (2^-10 ln 2)^4 / 24 = 2^-46.7. The result as the bits of
+  // 2^52 + weight, whose last bits are the weight rounded to a whole number.
+  static constexpr u64 RAW = 0x4330000000000000ull;   // those of 2^52
+  __device__ __forceinline__ u64 raw(double x) const {
+    constexpr double MAGIC = 0x1.8p52, A = 0.69314718055994531 / TAB;
     const double t = x + MAGIC;
     const int n = __double2loint(t);
     const double r = x - (t - MAGIC);
-    const double y = fma(fma(fma(r, 0.055504108664821580, 0.24022650695910071), r, 0.69314718055994531), r, 1.0);
-    const double v = tab[n & ((1 << TAB_BITS) - 1)] * y;
-    // Its exponent raised by 44 + n / 512, between -20 and 44.
-    const double w = __hiloint2double(__double2hiint(v) + ((44 + (n >> TAB_BITS)) << 20), __double2loint(v));
-    return (u64)__double_as_longlong(w + 0x1p52) & 0xFFFFFFFFFFFFFull;   // w <= 2^44, rounded to a whole number
+    const double y = fma(fma(fma(r, A * A * A / 6.0, A * A / 2.0), r, A), r, 1.0);
+    return (u64)__double_as_longlong(ldexp(tab[n & (TAB - 1)] * y, n >> TAB_BITS) + 0x1p52);
   }
+  __device__ __forceinline__ u64 of(double x) const { return raw(x) - RAW; }
   __device__ __forceinline__ u64 operator()(float z) const { return of(log2w(z)); }
 };
-
-// x or 0, by a mask that the compiler does not turn into a branch around x:
-// the chains of operations of a piece's tokens are to run side by side.
-__device__ __forceinline__ u64 only_if(bool on, u64 x) {
-  uint32_t m = on ? 0xFFFFFFFFu : 0u;
-  asm("" : "+v"(m));
-  return (u64)((uint32_t)x & m) | ((u64)((uint32_t)(x >> 32) & m) << 32);
+__device__ __forceinline__ void fill_table(Shared &sh) {
+  if (threadIdx.x < TAB) sh.tab[threadIdx.x] = exp2(44.0 + threadIdx.x * (1.0 / TAB));
 }
 
 __device__ __forceinline__ u64 wave_scan(u64 v) {   // inclusive
@@ -276,7 +280,7 @@ __device__ __forceinline__ uint32_t row_search(const Row<DT> &row, u64 limit, F 
 }
 
 // The smallest index up to which the weights total more than limit(total),
-// which they do; weights(z, i0, w) gives those of a piece. Each wave adds up a
+// which they do; weights(z, i0, w) gives those of a piece, each + RAW. Each wave adds up a
 // stretch of pieces (the row's ends are stretches of their own), then all
 // threads share the stretch that passes the limit.
 template <int DT, typename F, typename L>
@@ -290,6 +294,7 @@ __device__ __forceinline__ int locate(const Row<DT> &row, F weights, L limit_of,
     weights(z, i0, x);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) s += x[e];
+    s -= VEC * Weigher::RAW;
   });
   s = wave_sum(s);
   __syncthreads();
@@ -303,7 +308,7 @@ __device__ __forceinline__ int locate(const Row<DT> &row, F weights, L limit_of,
 #pragma unroll
     for (int e = 1; e < VEC; ++e) z[e] = -INFINITY;
     weights(z, i0 + lane, x);
-    x[0] = wave_scan(x[0]);
+    x[0] = wave_scan(x[0] - Weigher::RAW);
     if (lane < 8) sh.ends[w][lane] = x[0];   // (up to 7 tokens)
   }
   __syncthreads();
@@ -338,8 +343,9 @@ __device__ __forceinline__ int locate(const Row<DT> &row, F weights, L limit_of,
       weights(z, row.head + j * VEC, y);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        if (turn == 1 && run <= limit && limit < run + y[e]) sh.token = row.head + j * VEC + e;
-        run += y[e];
+        const u64 x = y[e] - Weigher::RAW;
+        if (turn == 1 && run <= limit && limit < run + x) sh.token = row.head + j * VEC + e;
+        run += x;
       }
     }
     if (turn == 1) break;
@@ -379,20 +385,278 @@ __device__ __forceinline__ void list_token(uint32_t bits, int i, Shared &sh) {
 
 __device__ __forceinline__ int bits_of(uint32_t x) { return 32 - __clz((int)x); }   // x < 2^bits; 0 for 0
 
+// Leaves the listed tokens up to the cut at best - d, of its equals the first
+// before / each + 1 (`at`: what they total). Returns the last index of those
+// that stay, V if all do.
+__device__ __forceinline__ int cut_list(Items &it, uint32_t best, uint32_t d, u64 before, u64 each, u64 at, int V, Shared &sh) {
+  int last = V;
+  if (at > before + each) {   // not all of its equals stay
+    Items eq = it;
+#pragma unroll
+    for (int j = 0; j < LIST_PER; ++j) eq.w[j] = it.w[j] && best - it.key[j] == d;
+    u64 rest, a2;
+    last = (int)list_search(eq, [&](int j) { return (uint32_t)eq.idx[j]; }, bits_of(V - 1), 0, before / each, rest, a2, sh);
+  }
+#pragma unroll
+  for (int j = 0; j < LIST_PER; ++j) {
+    const uint32_t dj = best - it.key[j];
+    if (dj > d || (dj == d && it.idx[j] > last)) it.w[j] = 0;
+  }
+  return last;
+}
+
+struct Params {
+  float T, p, mp, u;   // p: 1 where it keeps all; mp: 0 likewise, at most 1
+  int k;               // 0 where it keeps all
+  bool greedy;
+  __device__ __forceinline__ Params(const sb_sample_args &a, int r) {
+    T = a.temperature ? a.temperature[r] : 1.0f;
+    k = a.top_k && a.top_k[r] > 0 && a.top_k[r] < a.vocab ? a.top_k[r] : 0;
+    p = a.top_p && a.top_p[r] < 1.0f ? a.top_p[r] : 1.0f;
+    mp = a.min_p && a.min_p[r] > 0.0f ? fminf(a.min_p[r], 1.0f) : 0.0f;
+    u = a.u[r] > 0.0f ? fminf(a.u[r], 1.0f) : 0.0f;
+    greedy = !(T > 0.0f);
+  }
+  __device__ __forceinline__ u64 draw_limit(u64 total) const { return min((u64)((double)u * (double)total), total - 1); }
+  // Kept where the weights ranked before total less than p z_k, so at most
+  // this: the cut is where they first total more.
+  __device__ __forceinline__ u64 top_p_limit(u64 z_k) const { return (u64)fmax(ceil((double)p * (double)z_k), 1.0) - 1; }
+  // Weights below (1 - p) / V of the largest total less than 1 - p of all: the
+  // cut is not among those further below it than this (two octaves to spare
+  // for rounding).
+  __device__ __forceinline__ double top_p_reach(int V) const {
+    return fmin(TAB * (2.0 + log2((double)V / fmax(1.0 - (double)p, 1e-9))), -Weigher::LOW);
+  }
+};
+
+// What is kept of a row: logits above `lo`, and those equal to it with an
+// index up to `last`. (Never NaN or -inf.)
+struct Cut {
+  static constexpr int ALL = 0x7FFFFFFF;
+  float lo = -3.4028234663852886e38f;
+  int last = ALL;
+  __device__ __forceinline__ float masked(float z, int i) const {
+    float y = z >= lo ? z : -INFINITY;
+    if (last != ALL) y = ((z == lo) & (i > last)) ? -INFINITY : y;
+    return y;
+  }
+  __device__ __forceinline__ void raise(float z) {
+    if (z > lo) {
+      lo = z;
+      last = ALL;
+    }
+  }
+};
+
+// The lowest order bits in [lo, hi] that pred holds for; from there on it
+// holds, at hi it does. The lanes of a wave try 64 at once.
+template <typename P>
+__device__ __forceinline__ uint32_t first_bits(uint32_t lo, uint32_t hi, P pred) {
+  while (lo < hi) {
+    const uint32_t step = (hi - lo) / 64 + 1, mid = lo + (threadIdx.x & 63) * step;
+    const u64 m = __ballot(pred(min(mid, hi)));
+    const int f = m ? __builtin_ctzll(m) : 64;
+    if (f < 64) hi = min(lo + f * step, hi);
+    if (f > 0) lo = min(lo + (f - 1) * step + 1, hi);
+    else hi = lo;
+  }
+  return lo;
+}
+
+// The lowest logit that min-p keeps.
+__device__ __forceinline__ float min_p_logit(const Params &pr, const Weigher &weigh, uint32_t best) {
+  const u64 floor_w = (u64)ceil((double)pr.mp * ONE);
+  return from_order(first_bits(LOWEST, best, [&](uint32_t b) { return weigh(from_order(b)) >= floor_w; }));
+}
+
+// Bins of equal ratio, from the largest weight down to the smallest one there
+// is, or that can matter; what is below in the last.
+struct Bins {
+  double scale;
+  __device__ __forceinline__ Bins(const Weigher &weigh, float low, double reach)
+      : scale((BINS - 2) / fmin(fmax(-weigh.log2w(low), 0.05), reach)) {}
+  __device__ __forceinline__ int of(double x) const { return min(__double2loint(fma(x, -scale, 0x1.8p52)), BINS - 1); }   // to the nearest
+  // The bin's logits lie in [first, last]: bins fall as logits rise.
+  __device__ __forceinline__ void range(const Weigher &weigh, int bin, uint32_t best, uint32_t &first, uint32_t &last) const {
+    auto from = [&](int most) { return first_bits(LOWEST, best, [&](uint32_t b) { return of(weigh.log2w(from_order(b))) <= most; }); };
+    first = max(from(bin), LOWEST + 1);
+    last = bin > 0 ? from(bin - 1) - 1 : best;
+  }
+};
+
+// A pass that adds a row's (or a chunk's) kept weights, or counts, into sh.hist;
+// all: their sum. i_off: the index of the row's first token.
 template <int DT>
-__global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a) {
+__device__ __forceinline__ void add_bins(const Row<DT> &row, int i_off, const Weigher &weigh, const Bins &bins, const Cut &cut, bool count,
+                                         u64 &all, Shared &sh) {
+  constexpr int VEC = Row<DT>::VEC;
+  clear_bins(sh);
+  u64 below = 0;
+  all = 0;
+  row.each([&](const float (&z)[VEC], int i0) {
+    u64 w[VEC];
+    int at[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {   // no branches here: the tokens' chains of operations run side by side
+      const float y = cut.masked(z[e], i_off + i0 + e);
+      const double x = weigh.log2w(y);
+      w[e] = count ? (u64)(y > -INFINITY) : weigh.of(x);
+      at[e] = bins.of(x);
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      all += w[e];
+      if (at[e] < BINS - 1) {
+        if (w[e]) atomicAdd(&sh.hist[at[e]], w[e]);
+      } else {
+        below += w[e];
+      }
+    }
+  });
+  below = block_sum(below, sh);
+  all = block_sum(all, sh);
+  if (threadIdx.x == 0) sh.hist[BINS - 1] = below;
+}
+
+// A pass that lists the kept tokens with logits from z_lo to z_hi in LDS;
+// returns how many there are.
+template <int DT>
+__device__ __forceinline__ int list_range(const Row<DT> &row, int i_off, float z_lo, float z_hi, const Cut &cut, Shared &sh) {
+  constexpr int VEC = Row<DT>::VEC;
+  if (threadIdx.x == 0) sh.n = 0;
+  __syncthreads();
+  row.each([&](const float (&z)[VEC], int i0) {
+    float m = z[0];
+#pragma unroll
+    for (int e = 1; e < VEC; ++e) m = fmaxf(m, z[e]);
+    if (!(m >= z_lo)) return;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const float y = cut.masked(z[e], i_off + i0 + e);
+      if (y >= z_lo && y <= z_hi) list_token(order_bits(y), i_off + i0 + e, sh);
+    }
+  });
+  __syncthreads();
+  return sh.n;
+}
+
+// A piece's kept weights, + RAW. A wave without kept tokens takes none.
+template <int VEC>
+__device__ __forceinline__ void kept_weights(const float (&z)[VEC], int i, const Weigher &weigh, const Cut &cut, u64 (&w)[VEC]) {
+  float m = z[0];
+#pragma unroll
+  for (int e = 1; e < VEC; ++e) m = fmaxf(m, z[e]);
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) w[e] = Weigher::RAW;
+  if (!(m >= cut.lo)) return;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) w[e] = weigh.raw(weigh.log2w(cut.masked(z[e], i + e)));
+}
+
+// A whole row by one workgroup, any filters: top-k by counts, top-p by weights,
+// then the draw; one code for all, its passes being much of the kernels'.
+template <int DT>
+__device__ __forceinline__ int wide_row(const Row<DT> &row, const Params &pr, const Weigher &weigh, uint32_t best, float low, u64 &total, Shared &sh) {
+  constexpr int VEC = Row<DT>::VEC;
+  Cut cut;
+  int token = 0;
+#pragma unroll 1
+  for (int stage = pr.greedy ? 2 : 0; stage < 3; ++stage) {
+    const bool count = stage == 0;
+    uint32_t bits = 0;
+    u64 limit = 0;
+    if (stage < 2) {
+      if (count ? pr.k == 0 : pr.p == 1.0f) continue;
+      const Bins bins(weigh, low, count ? -Weigher::LOW : pr.top_p_reach(row.V));
+      u64 all, rest, at;
+      add_bins<DT>(row, 0, weigh, bins, cut, count, all, sh);
+      limit = count ? (u64)(pr.k - 1) : pr.top_p_limit(all);
+      if (limit >= all) continue;
+      uint32_t first, last;
+      bins.range(weigh, (int)find_bin(limit, rest, at, sh), best, first, last);
+      const int m = list_range<DT>(row, 0, from_order(first), from_order(last), cut, sh);
+      if (m <= LIST_MAX) {
+        Items it;
+        take_list(it, m, [&](uint32_t b) { return count ? (u64)1 : weigh(from_order(b)); }, sh);
+        bits = best - list_search(it, [&](int j) { return best - it.key[j]; }, 32, 0, rest, rest, at, sh);
+      } else {   // (all equals of the cut: kept ones and others weigh the same, and the limit is among the kept)
+        bits = row_search<DT>(row, limit, [&](float z) { return z >= cut.lo ? count ? (u64)1 : weigh(z) : 0; }, rest, at, sh);
+      }
+      const u64 each = count ? 1 : weigh(from_order(bits));
+      const float z = from_order(bits);
+      if (at <= rest + each) {   // all of the cut's equals stay
+        cut.raise(z);
+        continue;
+      }
+      limit = rest / each;   // the first so many of them, and one
+    } else if (pr.greedy) {
+      bits = best;
+    } else if (pr.mp > 0.0f) {
+      cut.raise(min_p_logit(pr, weigh, best));
+    }
+    const int found = locate<DT>(
+        row,
+        [&](const float (&z)[VEC], int i0, u64 (&w)[VEC]) {
+          if (!bits) return kept_weights<VEC>(z, i0, weigh, cut, w);
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) w[e] = Weigher::RAW + (order_bits(z[e]) == bits);
+        },
+        [&](u64 t) { return bits ? limit : pr.draw_limit(t); }, total, sh);
+    if (stage == 2) {
+      token = found;
+    } else {
+      const float z = from_order(bits);
+      cut.last = z > cut.lo ? found : min(cut.last, found);
+      cut.lo = z;
+    }
+  }
+  if (pr.greedy) total = (u64)ONE;
+  return token;
+}
+
+__device__ __forceinline__ void put_token(const sb_sample_args &a, int r, int token, float z, float top, const Params &pr, u64 total) {
+  if (threadIdx.x != 0) return;
+  a.tokens[r] = token;
+  const double x = pr.greedy || top == INFINITY ? 0.0 : ((double)z - (double)top) / (double)pr.T;
+  if (a.logprobs) a.logprobs[r] = (float)(x - log((double)total / ONE));
+}
+
+// A row that the wide kernels take: in the workspace, one a row.
+struct WideRow {
+  int kind;                 // 0: not such a row, 1: top-p, 2: no cut but min-p's
+  int n;                    // listed tokens (more than LIST_MAX: not all of them are)
+  uint32_t best;            // order bits of the largest logit
+  float low;                // the smallest finite one
+  int cut;                  // top-p: 1 where it leaves tokens out
+  int pad;
+  u64 rest;                 // of its limit, within the listed bin
+  u64 totals[CHUNKS_MAX];   // kept weights of a chunk, without the listed ones
+  u64 hist[BINS];
+  uint32_t key[LIST_MAX];
+  int idx[LIST_MAX];
+};
+static_assert(sizeof(WideRow) % 16 == 0, "rows of the workspace stay aligned");
+
+template <int DT>
+__device__ __forceinline__ const unsigned char *row_at(const sb_sample_args &a, int r) {
+  return static_cast<const unsigned char *>(a.logits) + (size_t)r * a.row_stride * Row<DT>::ES;
+}
+
+template <int DT>
+__global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, WideRow *wide) {
   constexpr int VEC = Row<DT>::VEC;
   __shared__ Shared sh;
   const int r = blockIdx.x, V = a.vocab, tid = threadIdx.x;
-  const Row<DT> row(static_cast<const unsigned char *>(a.logits) + (size_t)r * a.row_stride * Row<DT>::ES, V);
-  const float T = a.temperature ? a.temperature[r] : 1.0f;
-  const int k = a.top_k && a.top_k[r] > 0 && a.top_k[r] < V ? a.top_k[r] : 0;
-  const float p = a.top_p && a.top_p[r] < 1.0f ? a.top_p[r] : 1.0f;
-  const float mp = a.min_p && a.min_p[r] > 0.0f ? fminf(a.min_p[r], 1.0f) : 0.0f;
-  const float u = a.u[r];
-  const bool greedy = !(T > 0.0f);
-  if (tid < (1 << TAB_BITS)) sh.tab[tid] = exp2(tid * (1.0 / (1 << TAB_BITS)));
-  if (tid == 0) sh.n = 0;
+  const Row<DT> row(row_at<DT>(a, r), V);
+  const Params pr(a, r);
+  const int k = pr.k;
+  const float p = pr.p, mp = pr.mp;
+  const bool greedy = pr.greedy;
+  fill_table(sh);
+  if (tid == 0) {
+    sh.n = 0;
+    if (wide) wide[r].kind = 0;
+  }
 
   // The sample: SAMPLE pieces a thread, from as many places of the row.
   const int apart = max((row.pieces + SAMPLE - 1) / SAMPLE, SM_THREADS);
@@ -409,7 +673,7 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a) {
       for (int e = 0; e < VEC; ++e) zm = fmaxf(zm, z[e]);
     }
   }
-  const uint32_t seen = block_max(order_bits(zm), sh);   // (its barriers also publish tab and n)
+  const uint32_t seen = block_max(order_bits(zm), sh);   // (its barriers also publish the table and n)
   // Whether the tokens that matter are read off the sample, and from which on.
   const bool sampled = greedy || (k > 0 && k <= SAMPLED_K) || (k == 0 && p == 1.0f && mp > 0.0f);
   float bound = -INFINITY;
@@ -436,7 +700,7 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a) {
     // min-p keeps z >= top + T ln(min_p), top at least the sample's (less a
     // little for the rounding here).
     if (p == 1.0f && mp > 0.0f && from_order(seen) < INFINITY) {
-      const double b = (double)from_order(seen) + (double)T * log((double)mp);
+      const double b = (double)from_order(seen) + (double)pr.T * log((double)mp);
       const float bf = (float)(b - 1e-6 * fabs(b) - 1e-30);
       sure |= bf >= bound;
       bound = fmaxf(bound, bf);
@@ -485,14 +749,7 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a) {
     return;
   }
   const float top = from_order(best);
-  const Weigher weigh(sh.tab, top, T);
-  const u64 floor_w = mp > 0.0f ? (u64)ceil((double)mp * ONE) : 0;
-  const float uc = u > 0.0f ? fminf(u, 1.0f) : 0.0f;
-  auto draw_limit = [=](u64 total) { return min((u64)((double)uc * (double)total), total - 1); };
-  // Kept where the weights ranked before total less than p z_k, so at most
-  // this: the cut is where they first total more.
-  auto top_p_limit = [=](u64 z_k) { return (u64)fmax(ceil((double)p * (double)z_k), 1.0) - 1; };
-
+  const Weigher weigh(sh.tab, top, pr.T);
   int token = 0;
   u64 total = 1;
   const int n = sh.n;
@@ -501,42 +758,26 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a) {
     take_list(it, n, [&](uint32_t b) { return greedy ? (u64)(b == best) : weigh(from_order(b)); }, sh);
     if (!greedy) {
       const int bits = bits_of(best - order_bits(bound));
-      // Leaves the weights of those up to the cut, of its equals the first
-      // `rest` / (what each adds) + 1.
-      auto cut_at = [&](uint32_t d, u64 before, u64 each, u64 at) {
-        int last = V;
-        if (at > before + each) {   // not all of its equals stay
-          Items eq = it;
-#pragma unroll
-          for (int j = 0; j < LIST_PER; ++j) eq.w[j] = it.w[j] && best - it.key[j] == d;
-          u64 rest, a2;
-          last = (int)list_search(eq, [&](int j) { return (uint32_t)eq.idx[j]; }, bits_of(V - 1), 0, before / each, rest, a2, sh);
-        }
-#pragma unroll
-        for (int j = 0; j < LIST_PER; ++j) {
-          const uint32_t dj = best - it.key[j];
-          if (dj > d || (dj == d && it.idx[j] > last)) it.w[j] = 0;
-        }
-      };
       if (k > 0 && k < n) {
         Items count = it;
 #pragma unroll
         for (int j = 0; j < LIST_PER; ++j) count.w[j] = j * SM_THREADS + tid < n;
         u64 rest, at;
         const uint32_t d = list_search(count, [&](int j) { return best - count.key[j]; }, bits, 0, (u64)(k - 1), rest, at, sh);
-        cut_at(d, rest, 1, at);
+        cut_list(it, best, d, rest, 1, at, V, sh);
       }
       if (p < 1.0f) {
         u64 s = 0;
 #pragma unroll
         for (int j = 0; j < LIST_PER; ++j) s += it.w[j];
-        const u64 z_k = block_sum(s, sh), limit = top_p_limit(z_k);
+        const u64 z_k = block_sum(s, sh), limit = pr.top_p_limit(z_k);
         if (limit < z_k) {
           u64 rest, at;
           const uint32_t d = list_search(it, [&](int j) { return best - it.key[j]; }, bits, 0, limit, rest, at, sh);
-          cut_at(d, rest, weigh(from_order(best - d)), at);
+          cut_list(it, best, d, rest, weigh(from_order(best - d)), at, V, sh);
         }
       }
+      const u64 floor_w = (u64)ceil((double)mp * ONE);
 #pragma unroll
       for (int j = 0; j < LIST_PER; ++j)
         if (it.w[j] < floor_w) it.w[j] = 0;
@@ -545,146 +786,195 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a) {
 #pragma unroll
     for (int j = 0; j < LIST_PER; ++j) s += it.w[j];
     total = block_sum(s, sh);
-    token = (int)list_search(it, [&](int j) { return (uint32_t)it.idx[j]; }, bits_of(V - 1), 0, greedy ? 0 : draw_limit(total), rest, at, sh);
+    token = (int)list_search(it, [&](int j) { return (uint32_t)it.idx[j]; }, bits_of(V - 1), 0, greedy ? 0 : pr.draw_limit(total), rest, at, sh);
     if (greedy) total = (u64)ONE;
   } else {
-    // Kept: order bits above `cut`, or equal to it with an index up to `cut_i`.
-    uint32_t cut = LOWEST;
-    float cut_z = -INFINITY;
-    int cut_i = -1;
-    const float low = sampled ? -INFINITY : -from_order(block_max(order_bits(-zl), sh));   // (the full list: not looked for)
-    auto kept = [&](int i, float z) { return (z > cut_z) | ((z == cut_z) & (i <= cut_i)); };   // (NaN: no)
-    // Top-k by counts, top-p by weights, then the draw: one code for all, its
-    // passes being much of the kernel's.
-#pragma unroll 1
-    for (int stage = greedy ? 2 : 0; stage < 3; ++stage) {
-      const bool count = stage == 0;
-      uint32_t bits = 0;
-      u64 limit = 0;
-      if (stage < 2) {
-        if (count ? k == 0 : p == 1.0f) continue;
-        // Bins of equal ratio, from the largest weight down to the smallest
-        // one there is, or that can matter; what is below in the last. Weights
-        // below (1 - p) / V of the largest total less than 1 - p of all: the
-        // cut is not among them (two octaves to spare for rounding).
-        const double reach = count ? 64.0 : fmin(2.0 + log2((double)V / fmax(1.0 - (double)p, 1e-9)), 64.0);
-        const double range = fmin(fmax(-weigh.log2w(low), 1e-4), reach), scale = (BINS - 2) / range;
-        auto bin = [&](double x) { return min(__double2loint(fma(x, -scale, 0x1.8p52)), BINS - 1); };   // to the nearest
-        clear_bins(sh);
-        u64 below = 0, all = 0;
-        row.each([&](const float (&z)[VEC], int i0) {
-          u64 w[VEC];
-          int at[VEC];
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) {   // no branches here: the tokens' chains of operations run side by side
-            const double xw = weigh.log2w(z[e]);
-            w[e] = only_if(kept(i0 + e, z[e]), count ? 1 : weigh.of(xw));
-            at[e] = bin(xw);
-          }
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            all += w[e];
-            if (at[e] < BINS - 1) {
-              if (w[e]) atomicAdd(&sh.hist[at[e]], w[e]);
-            } else {
-              below += w[e];
-            }
-          }
-        });
-        below = block_sum(below, sh);
-        all = block_sum(all, sh);
-        if (tid == 0) sh.hist[BINS - 1] = below;
-        limit = count ? (u64)(k - 1) : top_p_limit(all);
-        if (limit >= all) continue;
-        u64 rest, at;
-        const int target = (int)find_bin(limit, rest, at, sh);
-        if (tid == 0) sh.n = 0;
-        // The bin's logits: bins fall as logits rise, so each end is bisected.
-        auto first_in = [&](int most) {   // the lowest order bits with a bin up to `most`
-          uint32_t lo = LOWEST, hi = best;   // (best is in bin 0)
-          while (lo < hi) {
-            const uint32_t mid = lo + (hi - lo) / 2;
-            if (bin(weigh.log2w(from_order(mid))) <= most) hi = mid;
-            else lo = mid + 1;
-          }
-          return hi;
-        };
-        const float z_lo = from_order(max(first_in(target), max(cut, LOWEST + 1)));
-        const float z_hi = target > 0 ? from_order(first_in(target - 1) - 1) : top;
-        __syncthreads();
-        row.each([&](const float (&z)[VEC], int i0) {
-          float m = z[0];
-#pragma unroll
-          for (int e = 1; e < VEC; ++e) m = fmaxf(m, z[e]);
-          if (!(m >= z_lo)) return;
-#pragma unroll
-          for (int e = 0; e < VEC; ++e)
-            if (z[e] >= z_lo && z[e] <= z_hi && (z[e] != cut_z || i0 + e <= cut_i)) list_token(order_bits(z[e]), i0 + e, sh);
-        });
-        __syncthreads();
-        const int m = sh.n;
-        if (m <= LIST_MAX) {
-          Items it;
-          take_list(it, m, [&](uint32_t b) { return count ? (u64)1 : weigh(from_order(b)); }, sh);
-          bits = best - list_search(it, [&](int j) { return best - it.key[j]; }, 32, 0, rest, rest, at, sh);
-        } else {
-          bits = row_search<DT>(row, limit, [&](float z) { return z >= cut_z && z > -INFINITY ? count ? (u64)1 : weigh(z) : 0; }, rest, at, sh);
-        }
-        const u64 each = count ? 1 : weigh(from_order(bits));
-        if (at <= rest + each) {   // all of the cut's equals stay
-          if (bits > cut) cut_i = V;
-          cut = bits;
-          cut_z = from_order(cut);
-          continue;
-        }
-        limit = rest / each;   // the first so many of them, and one
-      } else if (greedy) {
-        bits = best;
+    const float low = sampled ? -INFINITY : -from_order(block_max(order_bits(-zl), sh));   // (sampled: not looked for)
+    if (wide && k == 0 && !greedy) {
+      WideRow &w = wide[r];
+      if (tid < BINS) w.hist[tid] = 0;
+      if (tid == 0) {
+        w.kind = p < 1.0f ? 1 : 2;
+        w.n = 0;
+        w.best = best;
+        w.low = low;
+        w.cut = 0;
       }
-      const int found = locate<DT>(
-          row,
-          [&](const float (&z)[VEC], int i0, u64 (&w)[VEC]) {
-            float m = z[0];
+      return;
+    }
+    token = wide_row<DT>(row, pr, weigh, best, low, total, sh);
+  }
+  put_token(a, r, token, row.one(token), top, pr, total);
+}
+
+// Of a wide row's chunk: its weights in bins (top-p), or their sum.
+template <int DT>
+__global__ __launch_bounds__(SM_THREADS, 4) void k_wide_bins(sb_sample_args a, WideRow *wide) {
+  __shared__ Shared sh;
+  const int r = blockIdx.y, i0 = blockIdx.x * CHUNK;
+  WideRow &w = wide[r];
+  if (w.kind == 0) return;
+  fill_table(sh);
+  __syncthreads();
+  const Row<DT> row(row_at<DT>(a, r) + (size_t)i0 * Row<DT>::ES, min(CHUNK, a.vocab - i0));
+  const Params pr(a, r);
+  const Weigher weigh(sh.tab, from_order(w.best), pr.T);
+  Cut cut;
+  u64 all;
+  if (w.kind == 1) {
+    add_bins<DT>(row, i0, weigh, Bins(weigh, w.low, pr.top_p_reach(a.vocab)), cut, false, all, sh);
+    __syncthreads();
+    if (threadIdx.x < BINS && sh.hist[threadIdx.x]) atomicAdd(&w.hist[threadIdx.x], sh.hist[threadIdx.x]);
+    return;
+  }
+  if (pr.mp > 0.0f) cut.raise(min_p_logit(pr, weigh, w.best));
+  all = 0;
+  row.each([&](const float (&z)[Row<DT>::VEC], int j0) {
+    u64 x[Row<DT>::VEC];
+    kept_weights<Row<DT>::VEC>(z, i0 + j0, weigh, cut, x);
 #pragma unroll
-            for (int e = 1; e < VEC; ++e) m = fmaxf(m, z[e]);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) w[e] = bits && order_bits(z[e]) == bits;
-            if (bits || m < cut_z) return;   // a wave without kept tokens takes no weights
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-              const u64 x = weigh(z[e]);
-              w[e] = only_if(kept(i0 + e, z[e]) & (x >= floor_w), x);
-            }
-          },
-          [&](u64 t) { return bits ? limit : draw_limit(t); }, total, sh);
-      if (stage == 2) {
-        token = found;
-      } else {
-        cut_i = bits > cut ? found : min(cut_i, found);
-        cut = bits;
-        cut_z = from_order(cut);
+    for (int e = 0; e < Row<DT>::VEC; ++e) all += x[e];
+    all -= Row<DT>::VEC * Weigher::RAW;
+  });
+  all = block_sum(all, sh);
+  if (threadIdx.x == 0) w.totals[blockIdx.x] = all;
+}
+
+// Of a top-p row's chunk: the tokens of the bin that the cut is in, and the
+// weights above it.
+template <int DT>
+__global__ __launch_bounds__(SM_THREADS, 4) void k_wide_list(sb_sample_args a, WideRow *wide) {
+  constexpr int VEC = Row<DT>::VEC;
+  __shared__ Shared sh;
+  __shared__ int base;
+  const int r = blockIdx.y, i0 = blockIdx.x * CHUNK, tid = threadIdx.x;
+  WideRow &w = wide[r];
+  if (w.kind != 1) return;
+  fill_table(sh);
+  const u64 mine = tid < BINS ? w.hist[tid] : 0;
+  if (tid < BINS) sh.hist[tid] = mine;
+  const u64 all = block_sum(mine, sh);
+  const Row<DT> row(row_at<DT>(a, r) + (size_t)i0 * Row<DT>::ES, min(CHUNK, a.vocab - i0));
+  const Params pr(a, r);
+  const Weigher weigh(sh.tab, from_order(w.best), pr.T);
+  const u64 limit = pr.top_p_limit(all);
+  Cut none, above;
+  if (limit < all) {
+    u64 rest, at;
+    uint32_t first, last;
+    const int bin = (int)find_bin(limit, rest, at, sh);
+    Bins(weigh, w.low, pr.top_p_reach(a.vocab)).range(weigh, bin, w.best, first, last);
+    const int m = list_range<DT>(row, i0, from_order(first), from_order(last), none, sh);
+    if (tid == 0) {
+      base = m ? atomicAdd(&w.n, m) : 0;
+      if (i0 == 0) {
+        w.cut = 1;
+        w.rest = rest;
       }
     }
-    if (greedy) total = (u64)ONE;
+    __syncthreads();
+    for (int j = tid; j < min(m, LIST_MAX); j += SM_THREADS)
+      if (base + j < LIST_MAX) {
+        w.key[base + j] = sh.key[j];
+        w.idx[base + j] = sh.idx[j];
+      }
+    above.raise(last < w.best ? from_order(last + 1) : INFINITY);
+    if (last == w.best) above.last = -1;   // nothing is above the bin (not +inf either)
   }
-  if (tid == 0) {
-    a.tokens[r] = token;
-    const double z = row.one(token);
-    const double xt = greedy || top == INFINITY ? 0.0 : (z - (double)top) / (double)T;
-    if (a.logprobs) a.logprobs[r] = (float)(xt - log((double)total / ONE));
+  if (pr.mp > 0.0f) above.raise(min_p_logit(pr, weigh, w.best));
+  u64 sum = 0;
+  row.each([&](const float (&z)[VEC], int j0) {
+    u64 x[VEC];
+    kept_weights<VEC>(z, i0 + j0, weigh, above, x);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) sum += x[e];
+    sum -= VEC * Weigher::RAW;
+  });
+  sum = block_sum(sum, sh);
+  if (tid == 0) w.totals[blockIdx.x] = sum;
+}
+
+// A wide row's cut and draw.
+template <int DT>
+__global__ __launch_bounds__(SM_THREADS, 4) void k_wide_draw(sb_sample_args a, WideRow *wide) {
+  constexpr int VEC = Row<DT>::VEC;
+  __shared__ Shared sh;
+  __shared__ u64 tot[CHUNKS_MAX];
+  const int r = blockIdx.x, V = a.vocab, tid = threadIdx.x, chunks = (V + CHUNK - 1) / CHUNK;
+  const WideRow &w = wide[r];
+  if (w.kind == 0) return;
+  fill_table(sh);
+  if (tid < chunks) tot[tid] = w.totals[tid];
+  __syncthreads();
+  const Params pr(a, r);
+  const uint32_t best = w.best;
+  const Weigher weigh(sh.tab, from_order(best), pr.T);
+  const unsigned char *at_row = row_at<DT>(a, r);
+  int token;
+  u64 total = 0;
+  if (w.cut && w.n > LIST_MAX) {
+    token = wide_row<DT>(Row<DT>(at_row, V), pr, weigh, best, w.low, total, sh);
+  } else {
+    Cut cut;
+    const float z_mp = pr.mp > 0.0f ? min_p_logit(pr, weigh, best) : -INFINITY;
+    if (w.cut) {
+      Items it;
+      for (int j = tid; j < w.n; j += SM_THREADS) {
+        sh.key[j] = w.key[j];
+        sh.idx[j] = w.idx[j];
+      }
+      __syncthreads();
+      take_list(it, w.n, [&](uint32_t b) { return weigh(from_order(b)); }, sh);
+      u64 rest, at;
+      const uint32_t d = list_search(it, [&](int j) { return best - it.key[j]; }, 32, 0, w.rest, rest, at, sh);
+      const int last = cut_list(it, best, d, rest, weigh(from_order(best - d)), at, V, sh);
+      cut.lo = from_order(best - d);
+      if (last < V) cut.last = last;
+#pragma unroll
+      for (int j = 0; j < LIST_PER; ++j)
+        if (it.w[j] && from_order(it.key[j]) >= z_mp) atomicAdd(&tot[it.idx[j] / CHUNK], it.w[j]);
+      __syncthreads();
+    }
+    cut.raise(z_mp);
+    for (int c = 0; c < chunks; ++c) total += tot[c];
+    u64 limit = pr.draw_limit(total);
+    int c = 0;
+    while (c < chunks - 1 && limit >= tot[c]) limit -= tot[c++];
+    u64 t;
+    token = c * CHUNK + locate<DT>(
+        Row<DT>(at_row + (size_t)c * CHUNK * Row<DT>::ES, min(CHUNK, V - c * CHUNK)),
+        [&](const float (&z)[VEC], int i0, u64 (&x)[VEC]) { kept_weights<VEC>(z, c * CHUNK + i0, weigh, cut, x); },
+        [&](u64) { return limit; }, t, sh);
   }
+  put_token(a, r, token, Row<DT>(at_row, V).one(token), from_order(best), pr, total);
+}
+
+template <int DT>
+hipError_t launch(const sb_sample_args &a, void *workspace, hipStream_t s) {
+  WideRow *wide = static_cast<WideRow *>(workspace);
+  hipLaunchKernelGGL(k_sample<DT>, dim3(a.rows), dim3(SM_THREADS), 0, s, a, wide);
+  if (wide) {
+    const dim3 grid((a.vocab + CHUNK - 1) / CHUNK, a.rows);
+    hipLaunchKernelGGL(k_wide_bins<DT>, grid, dim3(SM_THREADS), 0, s, a, wide);
+    if (a.top_p) hipLaunchKernelGGL(k_wide_list<DT>, grid, dim3(SM_THREADS), 0, s, a, wide);
+    hipLaunchKernelGGL(k_wide_draw<DT>, dim3(a.rows), dim3(SM_THREADS), 0, s, a, wide);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_sample(const sb_sample_args &a, hipStream_t s) {
+// Rows of the wide kernels' workspace. They are three launches more, which a
+// few rows, or rows that one workgroup is through with at once, would pay for
+// nothing.
+int64_t sample_workspace(const sb_sample_args &a) {
+  return a.rows >= 16 && a.vocab > CHUNK ? a.rows * (int64_t)sizeof(WideRow) : 0;
+}
+
+hipError_t launch_sample(const sb_sample_args &a, void *workspace, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
-  switch (a.dtype) {
-    case SB_F32: hipLaunchKernelGGL(k_sample<SB_F32>, dim3(a.rows), dim3(SM_THREADS), 0, s, a); break;
-    case SB_BF16: hipLaunchKernelGGL(k_sample<SB_BF16>, dim3(a.rows), dim3(SM_THREADS), 0, s, a); break;
-    default: hipLaunchKernelGGL(k_sample<SB_F16>, dim3(a.rows), dim3(SM_THREADS), 0, s, a); break;
-  }
-  return hipGetLastError();
+  if (a.dtype == SB_F32) return launch<SB_F32>(a, workspace, s);
+  return a.dtype == SB_BF16 ? launch<SB_BF16>(a, workspace, s) : launch<SB_F16>(a, workspace, s);
 }
 
 }  // namespace sb

@@ -75,6 +75,16 @@ sb_status check_attention(const sb_attention_args *a, const char *call, bool poi
   return SB_OK;
 }
 
+sb_status check_sample(const sb_sample_args *a, const char *call) {
+  REFUSE_IF(!a, SB_E_INVALID_ARG, "no arguments");
+  REFUSE_IF(a->struct_bytes != (int64_t)sizeof(*a) || a->reserved, SB_E_INVALID_ARG, "struct_bytes is not this library's");
+  REFUSE_IF(a->dtype != SB_F32 && a->dtype != SB_BF16 && a->dtype != SB_F16, SB_E_UNSUPPORTED, "unknown dtype");
+  REFUSE_IF(a->rows < 0 || a->vocab < 1, SB_E_INVALID_ARG, "rows < 0 or vocab < 1");
+  REFUSE_IF(a->vocab > SB_SAMPLE_MAX_VOCAB, SB_E_UNSUPPORTED, "vocab above SB_SAMPLE_MAX_VOCAB");
+  REFUSE_IF(a->row_stride < 0 || (a->rows > 1 && a->row_stride < a->vocab), SB_E_INVALID_ARG, "row_stride < vocab");
+  return SB_OK;
+}
+
 int64_t attention_bytes(const sb_attention_args &a, int splits) {
   return splits == 1 ? 0 : (int64_t)splits * a.n_tokens * a.q_heads * (a.head_dim + 2) * 4;
 }
@@ -161,21 +171,24 @@ sb_status sb_paged_attention(const sb_attention_args *a, void *workspace, size_t
   return launched(launch_paged_attention(*a, splits, static_cast<float *>(workspace), static_cast<hipStream_t>(stream)), call);
 }
 
-sb_status sb_sample_tokens(const sb_sample_args *a, void *stream) {
+int64_t sb_sample_workspace(const sb_sample_args *a) {
+  return check_sample(a, "sb_sample_workspace") == SB_OK ? sample_workspace(*a) : -1;
+}
+
+sb_status sb_sample_tokens(const sb_sample_args *a, void *workspace, size_t bytes, void *stream) {
   const char *call = "sb_sample_tokens";
-  REFUSE_IF(!a, SB_E_INVALID_ARG, "no arguments");
-  REFUSE_IF(a->struct_bytes != (int64_t)sizeof(*a) || a->reserved, SB_E_INVALID_ARG, "struct_bytes is not this library's");
-  REFUSE_IF(a->dtype != SB_F32 && a->dtype != SB_BF16 && a->dtype != SB_F16, SB_E_UNSUPPORTED, "unknown dtype");
-  REFUSE_IF(a->rows < 0 || a->vocab < 1, SB_E_INVALID_ARG, "rows < 0 or vocab < 1");
-  REFUSE_IF(a->vocab > SB_SAMPLE_MAX_VOCAB, SB_E_UNSUPPORTED, "vocab above SB_SAMPLE_MAX_VOCAB");
-  REFUSE_IF(a->row_stride < 0 || (a->rows > 1 && a->row_stride < a->vocab), SB_E_INVALID_ARG, "row_stride < vocab");
+  const sb_status st = check_sample(a, call);
+  if (st != SB_OK) return st;
   if (a->rows == 0) return SB_OK;
   REFUSE_IF(!a->logits || !a->u || !a->tokens, SB_E_INVALID_ARG, "a pointer is missing");
   REFUSE_IF(!aligned(a->logits, a->dtype == SB_F32 ? 4 : 2) || !aligned(a->u, 4) || !aligned(a->temperature, 4) ||
                 !aligned(a->top_k, 4) || !aligned(a->top_p, 4) || !aligned(a->min_p, 4) || !aligned(a->tokens, 4) ||
                 !aligned(a->logprobs, 4),
             SB_E_INVALID_ARG, "an array is not aligned to its type");
-  return launched(launch_sample(*a, static_cast<hipStream_t>(stream)), call);
+  const int64_t need = sample_workspace(*a);
+  REFUSE_IF(workspace && need && (!aligned(workspace, 256) || bytes < (size_t)need), SB_E_WORKSPACE,
+            "workspace misaligned or smaller than sb_sample_workspace");
+  return launched(launch_sample(*a, need ? workspace : nullptr, static_cast<hipStream_t>(stream)), call);
 }
 
 }  // extern "C"

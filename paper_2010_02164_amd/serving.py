@@ -296,5 +296,8 @@ def sample_tokens(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=
         0 if top_p is None else _whole(top_p, "top_p", f32, dev, (R,)),
         0 if min_p is None else _whole(min_p, "min_p", f32, dev, (R,)), _whole(tokens, "out tokens", torch.int32, dev, (R,)),
         _whole(logprobs, "out logprobs", f32, dev, (R,)), logits.stride(0) if R > 1 else V, R, V, _LOGITS[logits.dtype], 0)
-    _call(N.lib().sb_sample_tokens, "sb_sample_tokens", dev, args)
+    L = N.lib()
+    need = L.sb_sample_workspace(args)   # (below 0: refused by the call itself)
+    work = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
+    _call(L.sb_sample_tokens, "sb_sample_tokens", dev, args, None if work is None else work.data_ptr(), max(need, 0))
     return tokens, logprobs

@@ -431,6 +431,44 @@ def test_sample_flat_and_wide(gpu):
     check_sample(z, u, T=np.full(12, 100.0))
 
 
+@pytest.mark.parametrize("dtype,V", [(F32, 16385), (F32, 40003), (BF16, 50000), (F16, 131072), (BF16, 262144)])
+def test_sample_rows_by_kernels_of_their_own(gpu, dtype, V):
+    """Many wide rows, for whose passes the call brings a workspace: as the
+    oracle says (some rows), and every row as without it."""
+    r = rng(V)
+    rows = 36
+    z = r.standard_normal((rows, V)) * r.choice([0.01, 0.5, 1.0, 2.5, 6.0], (rows, 1))
+    z[np.arange(rows)[:, None], r.integers(0, V, (rows, 9))] += 12 * r.random((rows, 9))
+    z[5] = 1.0                                       # all equal
+    z[6] = np.where(np.arange(V) % 3, -1.0, 2.0)     # two values
+    z[7] = -np.inf
+    z[8, 1:] = -np.inf
+    z[9] = np.where(np.arange(V) % 7 == 0, z[9], -np.inf)
+    z[10, [3, V - 1]] = np.inf
+    z[11, ::2] = np.nan
+    u, T = r.random(rows), 0.4 + r.random(rows)
+    u[:4] = 0.0, 1.0, 0.5, 1 - 2.0 ** -24
+    T[12::9] = 0
+    k = np.where(np.arange(rows) % 4 == 0, np.exp(r.random(rows) * math.log(V)).astype(int), 0)
+    p, mp = np.where(np.arange(rows) % 6 == 1, 1.0, 0.3 + 0.7 * r.random(rows)), np.where(np.arange(rows) % 3, 0.0, 0.1 * r.random(rows))
+    f = lambda x: dev(np.asarray(x, np.float32))   # noqa: E731
+    zd = dev(z, F32).to(dtype)
+    kw = dict(u=f(u), temperature=f(T), top_k=i32(k), top_p=f(p), min_p=f(mp))
+    for leave in ((), ("top_k",), ("top_k", "top_p"), ("top_k", "min_p"), ("top_k", "top_p", "min_p", "temperature")):
+        left = {n: x for n, x in kw.items() if n not in leave}
+        tok, lp = sb.sample_tokens(zd, **left)
+        for a in range(0, rows, 9):
+            t, q = sb.sample_tokens(zd[a:a + 9], **{n: x[a:a + 9].clone() for n, x in left.items()})
+            assert torch.equal(t, tok[a:a + 9]) and torch.equal(q, lp[a:a + 9]), (leave, a)
+        if V < 60000:
+            for j in range(0, rows, 5):
+                want = oracle.sample(f64(zd[j]), float(np.float32(u[j])), float(np.float32(T[j])) if "temperature" in left else 1.0,
+                                     int(k[j]) if "top_k" in left else 0, float(np.float32(p[j])) if "top_p" in left else 1.0,
+                                     float(np.float32(mp[j])) if "min_p" in left else 0.0)
+                assert int(tok[j]) == want[0], (leave, j)
+                assert float(lp[j]) == pytest.approx(want[1], rel=2.0 ** -22, abs=2.0 ** -36)
+
+
 def test_sample_odd_values(gpu):
     """-inf, NaN, +inf, the largest and smallest numbers, -0; parameters out of
     their range."""

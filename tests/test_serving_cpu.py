@@ -58,7 +58,7 @@ def _refused(native_lib, call, base, over):
     assert not set(over) - set(base)
     args = packer.pack(*dict(base, **over).values())
     fn = getattr(native_lib, call)
-    status = fn(args, None, 0, None) if call == "sb_paged_attention" else fn(args, None)
+    status = fn(args, None, 0, None) if call in ("sb_paged_attention", "sb_sample_tokens") else fn(args, None)
     if status != N.SB_OK:
         assert call in native_lib.sb_last_error(None).decode()
     return status
@@ -111,12 +111,26 @@ def test_sample_refusals(native_lib, over, status):
     assert _refused(native_lib, "sb_sample_tokens", SAMPLE, over) == status
 
 
+def test_sample_workspace(native_lib):
+    """Only many wide rows are faster with one; one that is too small is refused."""
+    def ask(**over):
+        return native_lib.sb_sample_workspace(N.SAMPLE_ARGS.pack(*dict(SAMPLE, **over).values()))
+    wide = dict(rows=64, vocab=32000, row_stride=32000)
+    assert ask() == 0 and ask(**dict(wide, rows=1)) == 0 and ask(**dict(wide, rows=0)) == 0
+    need = ask(**wide)
+    assert 0 < need and ask(**dict(wide, rows=128)) == 2 * need and ask(dtype=9) == -1
+    args = N.SAMPLE_ARGS.pack(*dict(SAMPLE, **wide).values())
+    assert native_lib.sb_sample_tokens(args, PTR, need - 1, None) == N.SB_E_WORKSPACE
+    assert native_lib.sb_sample_tokens(args, PTR + 128, need, None) == N.SB_E_WORKSPACE
+
+
 def test_missing_arguments(native_lib):
     assert native_lib.sb_plan_pages(None, None) == INVALID
     assert native_lib.sb_rope_append(None, None) == INVALID
     assert native_lib.sb_attention_workspace(None) == -1
     assert native_lib.sb_paged_attention(None, None, 0, None) == INVALID
-    assert native_lib.sb_sample_tokens(None, None) == INVALID
+    assert native_lib.sb_sample_workspace(None) == -1
+    assert native_lib.sb_sample_tokens(None, None, 0, None) == INVALID
 
 
 def test_nothing_to_do_needs_no_gpu(native_lib):
