@@ -18,13 +18,17 @@
 // that bin, a third draws; they read caches, and are bound by the 22 fp64 and
 // integer operations of a weight. One workgroup took such a row 2 to 4 times as
 // long as the others; with a workspace the passes run as kernels of their own,
-// in chunks over all compute units.
+// in chunks over all compute units. (Kernels: a row's last chunk taking the next
+// step in the same launch made 188 us into 1021, the fences between the XCDs'
+// caches costing more than launches.)
 //
 // Weights are whole multiples of 2^-44 in 64-bit integers: up to 2^18 of them
 // add up without rounding or overflow, in any order, so that partial sums of
 // waves and LDS atomics give one result. 44 bits below the largest weight
 // keep the sum of 2^18 roundings under 2^-27 of it in the worst case and near
 // 2^-36 in practice, below what u (24 bits) tells apart.
+#include <algorithm>
+
 #include "serve.h"
 
 namespace sb {
@@ -625,11 +629,15 @@ __device__ __forceinline__ void put_token(const sb_sample_args &a, int r, int to
 struct WideRow {
   int kind;                 // 0: not such a row, 1: top-p, 2: no cut but min-p's
   int n;                    // listed tokens (more than LIST_MAX: not all of them are)
+  int pad[2];
   uint32_t best;            // order bits of the largest logit
   float low;                // the smallest finite one
-  int cut;                  // top-p: 1 where it leaves tokens out
-  int pad;
-  u64 rest;                 // of its limit, within the listed bin
+  // Top-p, from k_wide_cut on: whether the cut leaves tokens out, the order bits
+  // of the bin that it is in, and what of its limit is left there.
+  int cut;
+  uint32_t first, last;
+  float z_mp;               // the lowest logit that min-p keeps
+  u64 rest;
   u64 totals[CHUNKS_MAX];   // kept weights of a chunk, without the listed ones
   u64 hist[BINS];
   uint32_t key[LIST_MAX];
@@ -807,70 +815,163 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
   put_token(a, r, token, row.one(token), top, pr, total);
 }
 
-// Of a wide row's chunk: its weights in bins (top-p), or their sum.
+// The wide kernels' workgroups share the chunks of all wide rows: item(r, c) for
+// each of this workgroup's.
+template <typename F>
+__device__ __forceinline__ void each_chunk(const sb_sample_args &a, const WideRow *wide, int kinds, F item) {
+  __shared__ int found[SM_THREADS];
+  __shared__ int counts[SM_WAVES];
+  const int chunks = (a.vocab + CHUNK - 1) / CHUNK, tid = threadIdx.x, w = tid >> 6;
+  int before = 0;   // items of the rows before this thousand
+  for (int r0 = 0; r0 < a.rows; r0 += SM_THREADS) {
+    const bool on = r0 + tid < a.rows && ((kinds >> wide[min(r0 + tid, a.rows - 1)].kind) & 1);
+    const u64 m = __ballot(on);
+    __syncthreads();
+    if ((tid & 63) == 0) counts[w] = __popcll(m);
+    __syncthreads();
+    int at = __popcll(m & ((1ull << (tid & 63)) - 1)), n = 0;
+    for (int i = 0; i < SM_WAVES; ++i) {
+      at += i < w ? counts[i] : 0;
+      n += counts[i];
+    }
+    if (on) found[at] = r0 + tid;
+    __syncthreads();
+    const int items = n * chunks;
+    // Item i of all belongs to workgroup i % gridDim.
+    int i = (int)blockIdx.x - before % (int)gridDim.x;
+    if (i < 0) i += gridDim.x;
+    for (; i < items; i += gridDim.x) item(found[i / chunks], i % chunks);
+    before += items;
+  }
+}
+
+// The draw, from the chunks' totals in sh.tot.
+template <int DT>
+__device__ __forceinline__ void draw_wide(const sb_sample_args &a, int r, const Params &pr, const Weigher &weigh, const Cut &cut, uint32_t best,
+                                          const u64 *tot, Shared &sh) {
+  constexpr int VEC = Row<DT>::VEC;
+  const int chunks = (a.vocab + CHUNK - 1) / CHUNK;
+  u64 total = 0, t;
+  for (int c = 0; c < chunks; ++c) total += tot[c];
+  u64 limit = pr.draw_limit(total);
+  int c = 0;
+  while (c < chunks - 1 && limit >= tot[c]) limit -= tot[c++];
+  const unsigned char *row = row_at<DT>(a, r);
+  const int token = c * CHUNK + locate<DT>(
+      Row<DT>(row + (size_t)c * CHUNK * Row<DT>::ES, min(CHUNK, a.vocab - c * CHUNK)),
+      [&](const float (&z)[VEC], int i0, u64 (&x)[VEC]) { kept_weights<VEC>(z, c * CHUNK + i0, weigh, cut, x); },
+      [&](u64) { return limit; }, t, sh);
+  put_token(a, r, token, Row<DT>(row, a.vocab).one(token), from_order(best), pr, total);
+}
+
+// First, of a top-p row's chunk: its weights into the row's bins. Of a row
+// without: their sum.
 template <int DT>
 __global__ __launch_bounds__(SM_THREADS, 4) void k_wide_bins(sb_sample_args a, WideRow *wide) {
+  constexpr int VEC = Row<DT>::VEC;
   __shared__ Shared sh;
-  const int r = blockIdx.y, i0 = blockIdx.x * CHUNK;
+  const int tid = threadIdx.x;
+  fill_table(sh);
+  each_chunk(a, wide, 1 << 1 | 1 << 2, [&](int r, int c) {
+    WideRow &w = wide[r];
+    const int i0 = c * CHUNK;
+    const Row<DT> row(row_at<DT>(a, r) + (size_t)i0 * Row<DT>::ES, min(CHUNK, a.vocab - i0));
+    const Params pr(a, r);
+    const Weigher weigh(sh.tab, from_order(w.best), pr.T);
+    Cut cut;
+    u64 all;
+    if (w.kind == 1) {
+      add_bins<DT>(row, i0, weigh, Bins(weigh, w.low, pr.top_p_reach(a.vocab)), cut, false, all, sh);
+      __syncthreads();
+      if (tid < BINS && sh.hist[tid]) atomicAdd(&w.hist[tid], sh.hist[tid]);
+      return;
+    }
+    if (pr.mp > 0.0f) cut.raise(min_p_logit(pr, weigh, w.best));
+    all = 0;
+    row.each([&](const float (&z)[VEC], int j0) {
+      u64 x[VEC];
+      kept_weights<VEC>(z, i0 + j0, weigh, cut, x);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) all += x[e];
+      all -= VEC * Weigher::RAW;
+    });
+    all = block_sum(all, sh);
+    if (tid == 0) w.totals[c] = all;
+  });
+}
+
+// Then, of a top-p row: the bin that the cut is in.
+template <int DT>
+__global__ __launch_bounds__(SM_THREADS, 4) void k_wide_cut(sb_sample_args a, WideRow *wide) {
+  __shared__ Shared sh;
+  const int r = blockIdx.x, tid = threadIdx.x;
   WideRow &w = wide[r];
   if (w.kind == 0) return;
   fill_table(sh);
-  __syncthreads();
-  const Row<DT> row(row_at<DT>(a, r) + (size_t)i0 * Row<DT>::ES, min(CHUNK, a.vocab - i0));
+  const u64 mine = tid < BINS ? w.hist[tid] : 0;
+  if (tid < BINS) sh.hist[tid] = mine;
+  const u64 all = block_sum(mine, sh);
   const Params pr(a, r);
   const Weigher weigh(sh.tab, from_order(w.best), pr.T);
-  Cut cut;
-  u64 all;
-  if (w.kind == 1) {
-    add_bins<DT>(row, i0, weigh, Bins(weigh, w.low, pr.top_p_reach(a.vocab)), cut, false, all, sh);
-    __syncthreads();
-    if (threadIdx.x < BINS && sh.hist[threadIdx.x]) atomicAdd(&w.hist[threadIdx.x], sh.hist[threadIdx.x]);
-    return;
+  const u64 limit = w.kind == 1 ? pr.top_p_limit(all) : 0;
+  uint32_t first = 0, last = 0;
+  u64 rest = 0, at;
+  const bool cuts = limit < all;   // (without top-p there are no bins: all is 0)
+  if (cuts) Bins(weigh, w.low, pr.top_p_reach(a.vocab)).range(weigh, (int)find_bin(limit, rest, at, sh), w.best, first, last);
+  const float z_mp = pr.mp > 0.0f ? min_p_logit(pr, weigh, w.best) : -INFINITY;
+  if (tid == 0) {
+    w.cut = cuts;
+    w.first = first;
+    w.last = last;
+    w.rest = rest;
+    w.z_mp = z_mp;
   }
-  if (pr.mp > 0.0f) cut.raise(min_p_logit(pr, weigh, w.best));
-  all = 0;
-  row.each([&](const float (&z)[Row<DT>::VEC], int j0) {
-    u64 x[Row<DT>::VEC];
-    kept_weights<Row<DT>::VEC>(z, i0 + j0, weigh, cut, x);
-#pragma unroll
-    for (int e = 0; e < Row<DT>::VEC; ++e) all += x[e];
-    all -= Row<DT>::VEC * Weigher::RAW;
-  });
-  all = block_sum(all, sh);
-  if (threadIdx.x == 0) w.totals[blockIdx.x] = all;
 }
 
-// Of a top-p row's chunk: the tokens of the bin that the cut is in, and the
-// weights above it.
+// Then, of a top-p row's chunk: the tokens of that bin, and the weights above it.
 template <int DT>
 __global__ __launch_bounds__(SM_THREADS, 4) void k_wide_list(sb_sample_args a, WideRow *wide) {
   constexpr int VEC = Row<DT>::VEC;
   __shared__ Shared sh;
   __shared__ int base;
-  const int r = blockIdx.y, i0 = blockIdx.x * CHUNK, tid = threadIdx.x;
-  WideRow &w = wide[r];
-  if (w.kind != 1) return;
+  const int tid = threadIdx.x;
   fill_table(sh);
-  const u64 mine = tid < BINS ? w.hist[tid] : 0;
-  if (tid < BINS) sh.hist[tid] = mine;
-  const u64 all = block_sum(mine, sh);
-  const Row<DT> row(row_at<DT>(a, r) + (size_t)i0 * Row<DT>::ES, min(CHUNK, a.vocab - i0));
-  const Params pr(a, r);
-  const Weigher weigh(sh.tab, from_order(w.best), pr.T);
-  const u64 limit = pr.top_p_limit(all);
-  Cut none, above;
-  if (limit < all) {
-    u64 rest, at;
-    uint32_t first, last;
-    const int bin = (int)find_bin(limit, rest, at, sh);
-    Bins(weigh, w.low, pr.top_p_reach(a.vocab)).range(weigh, bin, w.best, first, last);
-    const int m = list_range<DT>(row, i0, from_order(first), from_order(last), none, sh);
+  each_chunk(a, wide, 1 << 1, [&](int r, int c) {
+    WideRow &w = wide[r];
+    const int i0 = c * CHUNK;
+    const Row<DT> row(row_at<DT>(a, r) + (size_t)i0 * Row<DT>::ES, min(CHUNK, a.vocab - i0));
+    const Params pr(a, r);
+    const Weigher weigh(sh.tab, from_order(w.best), pr.T);
+    const bool cuts = w.cut, any_above = !cuts || w.last < w.best;
+    // Logits from z_lo to z_hi are listed, those above weighed.
+    const float z_lo = cuts ? from_order(w.first) : INFINITY, z_hi = cuts ? from_order(w.last) : -INFINITY;
+    Cut above;
+    if (cuts) above.raise(from_order(min(w.last + 1, w.best)));
+    above.raise(w.z_mp);
+    const float from = any_above ? fminf(z_lo, above.lo) : z_lo;
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    u64 sum = 0;
+    row.each([&](const float (&z)[VEC], int j0) {
+      float m = z[0];
+#pragma unroll
+      for (int e = 1; e < VEC; ++e) m = fmaxf(m, z[e]);
+      if (!(m >= from)) return;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (z[e] >= z_lo && z[e] <= z_hi) list_token(order_bits(z[e]), i0 + j0 + e, sh);
+      if (!any_above) return;
+      u64 x[VEC];
+      kept_weights<VEC>(z, i0 + j0, weigh, above, x);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sum += x[e];
+      sum -= VEC * Weigher::RAW;
+    });
+    sum = block_sum(sum, sh);
+    const int m = sh.n;
     if (tid == 0) {
+      w.totals[c] = sum;
       base = m ? atomicAdd(&w.n, m) : 0;
-      if (i0 == 0) {
-        w.cut = 1;
-        w.rest = rest;
-      }
     }
     __syncthreads();
     for (int j = tid; j < min(m, LIST_MAX); j += SM_THREADS)
@@ -878,84 +979,62 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_wide_list(sb_sample_args a, W
         w.key[base + j] = sh.key[j];
         w.idx[base + j] = sh.idx[j];
       }
-    above.raise(last < w.best ? from_order(last + 1) : INFINITY);
-    if (last == w.best) above.last = -1;   // nothing is above the bin (not +inf either)
-  }
-  if (pr.mp > 0.0f) above.raise(min_p_logit(pr, weigh, w.best));
-  u64 sum = 0;
-  row.each([&](const float (&z)[VEC], int j0) {
-    u64 x[VEC];
-    kept_weights<VEC>(z, i0 + j0, weigh, above, x);
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) sum += x[e];
-    sum -= VEC * Weigher::RAW;
   });
-  sum = block_sum(sum, sh);
-  if (tid == 0) w.totals[blockIdx.x] = sum;
 }
 
-// A wide row's cut and draw.
+// Last, of a wide row: its cut and its draw.
 template <int DT>
 __global__ __launch_bounds__(SM_THREADS, 4) void k_wide_draw(sb_sample_args a, WideRow *wide) {
-  constexpr int VEC = Row<DT>::VEC;
   __shared__ Shared sh;
   __shared__ u64 tot[CHUNKS_MAX];
-  const int r = blockIdx.x, V = a.vocab, tid = threadIdx.x, chunks = (V + CHUNK - 1) / CHUNK;
+  const int r = blockIdx.x, tid = threadIdx.x, V = a.vocab, chunks = (V + CHUNK - 1) / CHUNK;
   const WideRow &w = wide[r];
   if (w.kind == 0) return;
   fill_table(sh);
   if (tid < chunks) tot[tid] = w.totals[tid];
-  __syncthreads();
   const Params pr(a, r);
-  const uint32_t best = w.best;
+  const uint32_t best = w.best, last = w.last;
   const Weigher weigh(sh.tab, from_order(best), pr.T);
-  const unsigned char *at_row = row_at<DT>(a, r);
-  int token;
-  u64 total = 0;
+  Cut cut;
   if (w.cut && w.n > LIST_MAX) {
-    token = wide_row<DT>(Row<DT>(at_row, V), pr, weigh, best, w.low, total, sh);
-  } else {
-    Cut cut;
-    const float z_mp = pr.mp > 0.0f ? min_p_logit(pr, weigh, best) : -INFINITY;
-    if (w.cut) {
-      Items it;
-      for (int j = tid; j < w.n; j += SM_THREADS) {
-        sh.key[j] = w.key[j];
-        sh.idx[j] = w.idx[j];
-      }
-      __syncthreads();
-      take_list(it, w.n, [&](uint32_t b) { return weigh(from_order(b)); }, sh);
-      u64 rest, at;
-      const uint32_t d = list_search(it, [&](int j) { return best - it.key[j]; }, 32, 0, w.rest, rest, at, sh);
-      const int last = cut_list(it, best, d, rest, weigh(from_order(best - d)), at, V, sh);
-      cut.lo = from_order(best - d);
-      if (last < V) cut.last = last;
-#pragma unroll
-      for (int j = 0; j < LIST_PER; ++j)
-        if (it.w[j] && from_order(it.key[j]) >= z_mp) atomicAdd(&tot[it.idx[j] / CHUNK], it.w[j]);
-      __syncthreads();
-    }
-    cut.raise(z_mp);
-    for (int c = 0; c < chunks; ++c) total += tot[c];
-    u64 limit = pr.draw_limit(total);
-    int c = 0;
-    while (c < chunks - 1 && limit >= tot[c]) limit -= tot[c++];
-    u64 t;
-    token = c * CHUNK + locate<DT>(
-        Row<DT>(at_row + (size_t)c * CHUNK * Row<DT>::ES, min(CHUNK, V - c * CHUNK)),
-        [&](const float (&z)[VEC], int i0, u64 (&x)[VEC]) { kept_weights<VEC>(z, c * CHUNK + i0, weigh, cut, x); },
-        [&](u64) { return limit; }, t, sh);
+    __syncthreads();
+    u64 total;
+    const Row<DT> whole(row_at<DT>(a, r), V);
+    const int token = wide_row<DT>(whole, pr, weigh, best, w.low, total, sh);
+    put_token(a, r, token, whole.one(token), from_order(best), pr, total);
+    return;
   }
-  put_token(a, r, token, Row<DT>(at_row, V).one(token), from_order(best), pr, total);
+  if (w.cut) {
+    Items it;
+    for (int j = tid; j < w.n; j += SM_THREADS) {
+      sh.key[j] = w.key[j];
+      sh.idx[j] = w.idx[j];
+    }
+    __syncthreads();
+    take_list(it, w.n, [&](uint32_t b) { return weigh(from_order(b)); }, sh);
+    u64 rest, at;
+    const uint32_t d = list_search(it, [&](int j) { return last - it.key[j]; }, bits_of(last - w.first), 0, w.rest, rest, at, sh);
+    const int end = cut_list(it, last, d, rest, weigh(from_order(last - d)), at, V, sh);
+    cut.lo = from_order(last - d);
+    if (end < V) cut.last = end;
+#pragma unroll
+    for (int j = 0; j < LIST_PER; ++j)
+      if (it.w[j] && from_order(it.key[j]) >= w.z_mp) atomicAdd(&tot[it.idx[j] / CHUNK], it.w[j]);
+  }
+  __syncthreads();
+  cut.raise(w.z_mp);
+  draw_wide<DT>(a, r, pr, weigh, cut, best, tot, sh);
 }
 
 template <int DT>
-hipError_t launch(const sb_sample_args &a, void *workspace, hipStream_t s) {
+hipError_t launch(const sb_sample_args &a, void *workspace, int n_cu, hipStream_t s) {
   WideRow *wide = static_cast<WideRow *>(workspace);
   hipLaunchKernelGGL(k_sample<DT>, dim3(a.rows), dim3(SM_THREADS), 0, s, a, wide);
   if (wide) {
-    const dim3 grid((a.vocab + CHUNK - 1) / CHUNK, a.rows);
+    const long long chunks = (long long)((a.vocab + CHUNK - 1) / CHUNK) * a.rows;
+    const dim3 grid((unsigned)std::min(chunks, (long long)n_cu));
     hipLaunchKernelGGL(k_wide_bins<DT>, grid, dim3(SM_THREADS), 0, s, a, wide);
+    hipLaunchKernelGGL(k_wide_cut<DT>, dim3(a.rows), dim3(SM_THREADS), 0, s, a, wide);
     if (a.top_p) hipLaunchKernelGGL(k_wide_list<DT>, grid, dim3(SM_THREADS), 0, s, a, wide);
     hipLaunchKernelGGL(k_wide_draw<DT>, dim3(a.rows), dim3(SM_THREADS), 0, s, a, wide);
   }
@@ -964,17 +1043,16 @@ hipError_t launch(const sb_sample_args &a, void *workspace, hipStream_t s) {
 
 }  // namespace
 
-// Rows of the wide kernels' workspace. They are three launches more, which a
+// Rows of the wide kernels' workspace. They are four launches more, which a
 // few rows, or rows that one workgroup is through with at once, would pay for
 // nothing.
 int64_t sample_workspace(const sb_sample_args &a) {
   return a.rows >= 16 && a.vocab > CHUNK ? a.rows * (int64_t)sizeof(WideRow) : 0;
 }
 
-hipError_t launch_sample(const sb_sample_args &a, void *workspace, hipStream_t s) {
-  if (a.rows == 0) return hipSuccess;
-  if (a.dtype == SB_F32) return launch<SB_F32>(a, workspace, s);
-  return a.dtype == SB_BF16 ? launch<SB_BF16>(a, workspace, s) : launch<SB_F16>(a, workspace, s);
+hipError_t launch_sample(const sb_sample_args &a, void *workspace, int n_cu, hipStream_t s) {
+  if (a.dtype == SB_F32) return launch<SB_F32>(a, workspace, n_cu, s);
+  return a.dtype == SB_BF16 ? launch<SB_BF16>(a, workspace, n_cu, s) : launch<SB_F16>(a, workspace, n_cu, s);
 }
 
 }  // namespace sb

@@ -16,7 +16,7 @@ void set_call_error(const char *msg);
 hipError_t launch_plan(const sb_plan_args &a, hipStream_t s);
 hipError_t launch_rope(const sb_rope_args &a, int n_cu, hipStream_t s);
 hipError_t launch_paged_attention(const sb_attention_args &a, int splits, float *parts, hipStream_t s);
-hipError_t launch_sample(const sb_sample_args &a, void *workspace, hipStream_t s);   // workspace: may be null
+hipError_t launch_sample(const sb_sample_args &a, void *workspace, int n_cu, hipStream_t s);   // workspace: may be null
 
 // Parts that the keys of a request are split into (1: no workspace).
 int attention_splits(const sb_attention_args &a, int n_cu);

@@ -188,7 +188,10 @@ sb_status sb_sample_tokens(const sb_sample_args *a, void *workspace, size_t byte
   const int64_t need = sample_workspace(*a);
   REFUSE_IF(workspace && need && (!aligned(workspace, 256) || bytes < (size_t)need), SB_E_WORKSPACE,
             "workspace misaligned or smaller than sb_sample_workspace");
-  return launched(launch_sample(*a, need ? workspace : nullptr, static_cast<hipStream_t>(stream)), call);
+  int n_cu = 0;
+  const hipError_t e = compute_units(n_cu);
+  if (e != hipSuccess) return launched(e, call);
+  return launched(launch_sample(*a, need ? workspace : nullptr, n_cu, static_cast<hipStream_t>(stream)), call);
 }
 
 }  // extern "C"
