@@ -30,6 +30,7 @@
 #include <algorithm>
 
 #include "serve.h"
+#include "wave.h"
 
 namespace sb {
 namespace {
@@ -51,7 +52,7 @@ constexpr int CHUNKS_MAX = SB_SAMPLE_MAX_VOCAB / CHUNK;
 constexpr int SAMPLED_K = 1536;
 // 16-byte pieces a thread loads at once: of the sample, and of a pass (4 there
 // made the code of the passes larger than the instruction cache).
-constexpr int SAMPLE = 4, BATCH = 2;
+constexpr int SAMPLE = 4, PASS = 2;
 
 // The bits of z in an order that ascends with it; NaN counts as -inf.
 __device__ __forceinline__ uint32_t order_bits(float z) {
@@ -85,7 +86,7 @@ struct Row {
     }
   }
   // f(z, i0) for pieces first, first + step, ... of [first, end): values i0 .. i0 + VEC - 1.
-  template <typename F>
+  template <int BATCH, typename F>
   __device__ __forceinline__ void each_piece(int first, int end, int step, F f) const {
 #pragma unroll 1
     for (int j0 = first; j0 < end; j0 += BATCH * step) {
@@ -115,9 +116,9 @@ struct Row {
       f(z, i);
     }
   }
-  template <typename F>
+  template <int BATCH = PASS, typename F>
   __device__ __forceinline__ void each(F f) const {
-    each_piece(threadIdx.x, pieces, SM_THREADS, f);
+    each_piece<BATCH>(threadIdx.x, pieces, SM_THREADS, f);
     each_end(f);
   }
 };
@@ -162,18 +163,40 @@ __device__ __forceinline__ void fill_table(Shared &sh) {
   if (threadIdx.x < TAB) sh.tab[threadIdx.x] = exp2(44.0 + threadIdx.x * (1.0 / TAB));
 }
 
+// Sums and maxima over a wave through the lanes' own paths (a shuffle through
+// LDS takes about 130 cycles, and a search has dozens of steps).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 shifted(u64 v) {   // 0 where nothing comes
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xF, false);
+  return ((u64)hi << 32) | lo;
+}
 __device__ __forceinline__ u64 wave_scan(u64 v) {   // inclusive
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const u64 y = __shfl_up(v, o, 64);
-    if ((int)(threadIdx.x & 63) >= o) v += y;
-  }
+  v += shifted<0x111, 0xF>(v);   // within 16 lanes: from 1, 2, 4, 8 before
+  v += shifted<0x112, 0xF>(v);
+  v += shifted<0x114, 0xF>(v);
+  v += shifted<0x118, 0xF>(v);
+  v += shifted<0x142, 0xA>(v);   // the last of the first and third 16 to the next
+  v += shifted<0x143, 0xC>(v);   // the last of the first 32 to the others
   return v;
 }
+template <int S>
+__device__ __forceinline__ u64 sum_stage(u64 v) {
+  u64 a, b;
+  stage64<S>(v, a, b);
+  return a + b;
+}
 __device__ __forceinline__ u64 wave_sum(u64 v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  return sum_stage<5>(sum_stage<4>(sum_stage<3>(sum_stage<2>(sum_stage<1>(sum_stage<0>(v))))));
+}
+template <int S>
+__device__ __forceinline__ uint32_t max_stage(uint32_t v) {
+  uint32_t a, b;
+  stage32<S>(v, a, b);
+  return max(a, b);
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  return max_stage<5>(max_stage<4>(max_stage<3>(max_stage<2>(max_stage<1>(max_stage<0>(v))))));
 }
 __device__ __forceinline__ u64 block_sum(u64 v, Shared &sh) {
   v = wave_sum(v);
@@ -186,8 +209,7 @@ __device__ __forceinline__ u64 block_sum(u64 v, Shared &sh) {
   return s;
 }
 __device__ __forceinline__ uint32_t block_max(uint32_t v, Shared &sh) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, o, 64));
+  v = wave_max(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = v;
   __syncthreads();
@@ -293,7 +315,7 @@ __device__ __forceinline__ int locate(const Row<DT> &row, F weights, L limit_of,
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int len = (row.pieces + SM_WAVES - 1) / SM_WAVES;   // pieces a wave
   u64 s = 0;
-  row.each_piece(min(w * len, row.pieces) + lane, min((w + 1) * len, row.pieces), 64, [&](const float (&z)[VEC], int i0) {
+  row.template each_piece<PASS>(min(w * len, row.pieces) + lane, min((w + 1) * len, row.pieces), 64, [&](const float (&z)[VEC], int i0) {
     u64 x[VEC];
     weights(z, i0, x);
 #pragma unroll
@@ -639,11 +661,16 @@ struct WideRow {
   float z_mp;               // the lowest logit that min-p keeps
   u64 rest;
   u64 totals[CHUNKS_MAX];   // kept weights of a chunk, without the listed ones
-  u64 hist[BINS];
   uint32_t key[LIST_MAX];
   int idx[LIST_MAX];
 };
 static_assert(sizeof(WideRow) % 16 == 0, "rows of the workspace stay aligned");
+__host__ __device__ __forceinline__ int chunks_of(int V) { return (V + CHUNK - 1) / CHUNK; }
+// Behind them: a chunk's bins. (Atomics on one set of a row's took as long as
+// the weights.)
+__device__ __forceinline__ u64 *bins_at(const sb_sample_args &a, WideRow *wide, int r, int c) {
+  return reinterpret_cast<u64 *>(wide + a.rows) + ((size_t)r * chunks_of(a.vocab) + c) * BINS;
+}
 
 template <int DT>
 __device__ __forceinline__ const unsigned char *row_at(const sb_sample_args &a, int r) {
@@ -660,11 +687,6 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
   const int k = pr.k;
   const float p = pr.p, mp = pr.mp;
   const bool greedy = pr.greedy;
-  fill_table(sh);
-  if (tid == 0) {
-    sh.n = 0;
-    if (wide) wide[r].kind = 0;
-  }
 
   // The sample: SAMPLE pieces a thread, from as many places of the row.
   const int apart = max((row.pieces + SAMPLE - 1) / SAMPLE, SM_THREADS);
@@ -673,13 +695,22 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
 #pragma unroll
   for (int b = 0; b < SAMPLE; ++b) {
     const int j = b * apart + tid;
+    if (j < row.pieces) x[b] = row.piece(j);
+  }
+  fill_table(sh);   // while they are on their way
+#pragma unroll
+  for (int b = 0; b < SAMPLE; ++b) {
+    const int j = b * apart + tid;
     if (j < row.pieces) {
-      x[b] = row.piece(j);
       float z[VEC];
       Row<DT>::unpack(x[b], z);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) zm = fmaxf(zm, z[e]);
     }
+  }
+  if (tid == 0) {
+    sh.n = 0;
+    if (wide) wide[r].kind = 0;
   }
   const uint32_t seen = block_max(order_bits(zm), sh);   // (its barriers also publish the table and n)
   // Whether the tokens that matter are read off the sample, and from which on.
@@ -746,7 +777,7 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
   }
   if (apart > SM_THREADS)
 #pragma unroll 1
-    for (int b = 0; b < SAMPLE; ++b) row.each_piece(b * apart + SM_THREADS + tid, min((b + 1) * apart, row.pieces), SM_THREADS, look);
+    for (int b = 0; b < SAMPLE; ++b) row.template each_piece<PASS>(b * apart + SM_THREADS + tid, min((b + 1) * apart, row.pieces), SM_THREADS, look);
   row.each_end(look);
   const uint32_t best = block_max(order_bits(zm), sh);
   if (best == LOWEST) {
@@ -800,7 +831,6 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
     const float low = sampled ? -INFINITY : -from_order(block_max(order_bits(-zl), sh));   // (sampled: not looked for)
     if (wide && k == 0 && !greedy) {
       WideRow &w = wide[r];
-      if (tid < BINS) w.hist[tid] = 0;
       if (tid == 0) {
         w.kind = p < 1.0f ? 1 : 2;
         w.n = 0;
@@ -821,7 +851,7 @@ template <typename F>
 __device__ __forceinline__ void each_chunk(const sb_sample_args &a, const WideRow *wide, int kinds, F item) {
   __shared__ int found[SM_THREADS];
   __shared__ int counts[SM_WAVES];
-  const int chunks = (a.vocab + CHUNK - 1) / CHUNK, tid = threadIdx.x, w = tid >> 6;
+  const int chunks = chunks_of(a.vocab), tid = threadIdx.x, w = tid >> 6;
   int before = 0;   // items of the rows before this thousand
   for (int r0 = 0; r0 < a.rows; r0 += SM_THREADS) {
     const bool on = r0 + tid < a.rows && ((kinds >> wide[min(r0 + tid, a.rows - 1)].kind) & 1);
@@ -850,7 +880,7 @@ template <int DT>
 __device__ __forceinline__ void draw_wide(const sb_sample_args &a, int r, const Params &pr, const Weigher &weigh, const Cut &cut, uint32_t best,
                                           const u64 *tot, Shared &sh) {
   constexpr int VEC = Row<DT>::VEC;
-  const int chunks = (a.vocab + CHUNK - 1) / CHUNK;
+  const int chunks = chunks_of(a.vocab);
   u64 total = 0, t;
   for (int c = 0; c < chunks; ++c) total += tot[c];
   u64 limit = pr.draw_limit(total);
@@ -883,7 +913,7 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_wide_bins(sb_sample_args a, W
     if (w.kind == 1) {
       add_bins<DT>(row, i0, weigh, Bins(weigh, w.low, pr.top_p_reach(a.vocab)), cut, false, all, sh);
       __syncthreads();
-      if (tid < BINS && sh.hist[tid]) atomicAdd(&w.hist[tid], sh.hist[tid]);
+      if (tid < BINS) bins_at(a, wide, r, c)[tid] = sh.hist[tid];
       return;
     }
     if (pr.mp > 0.0f) cut.raise(min_p_logit(pr, weigh, w.best));
@@ -908,15 +938,19 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_wide_cut(sb_sample_args a, Wi
   WideRow &w = wide[r];
   if (w.kind == 0) return;
   fill_table(sh);
-  const u64 mine = tid < BINS ? w.hist[tid] : 0;
-  if (tid < BINS) sh.hist[tid] = mine;
+  u64 mine = 0;
+  if (w.kind == 1 && tid < BINS) {
+#pragma unroll 4
+    for (int c = 0; c < chunks_of(a.vocab); ++c) mine += bins_at(a, wide, r, c)[tid];
+    sh.hist[tid] = mine;
+  }
   const u64 all = block_sum(mine, sh);
   const Params pr(a, r);
   const Weigher weigh(sh.tab, from_order(w.best), pr.T);
   const u64 limit = w.kind == 1 ? pr.top_p_limit(all) : 0;
   uint32_t first = 0, last = 0;
   u64 rest = 0, at;
-  const bool cuts = limit < all;   // (without top-p there are no bins: all is 0)
+  const bool cuts = limit < all;   // (without top-p all is 0)
   if (cuts) Bins(weigh, w.low, pr.top_p_reach(a.vocab)).range(weigh, (int)find_bin(limit, rest, at, sh), w.best, first, last);
   const float z_mp = pr.mp > 0.0f ? min_p_logit(pr, weigh, w.best) : -INFINITY;
   if (tid == 0) {
@@ -930,7 +964,7 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_wide_cut(sb_sample_args a, Wi
 
 // Then, of a top-p row's chunk: the tokens of that bin, and the weights above it.
 template <int DT>
-__global__ __launch_bounds__(SM_THREADS, 4) void k_wide_list(sb_sample_args a, WideRow *wide) {
+__global__ __launch_bounds__(SM_THREADS, 8) void k_wide_list(sb_sample_args a, WideRow *wide) {
   constexpr int VEC = Row<DT>::VEC;
   __shared__ Shared sh;
   __shared__ int base;
@@ -987,7 +1021,7 @@ template <int DT>
 __global__ __launch_bounds__(SM_THREADS, 4) void k_wide_draw(sb_sample_args a, WideRow *wide) {
   __shared__ Shared sh;
   __shared__ u64 tot[CHUNKS_MAX];
-  const int r = blockIdx.x, tid = threadIdx.x, V = a.vocab, chunks = (V + CHUNK - 1) / CHUNK;
+  const int r = blockIdx.x, tid = threadIdx.x, V = a.vocab, chunks = chunks_of(V);
   const WideRow &w = wide[r];
   if (w.kind == 0) return;
   fill_table(sh);
@@ -1031,11 +1065,10 @@ hipError_t launch(const sb_sample_args &a, void *workspace, int n_cu, hipStream_
   WideRow *wide = static_cast<WideRow *>(workspace);
   hipLaunchKernelGGL(k_sample<DT>, dim3(a.rows), dim3(SM_THREADS), 0, s, a, wide);
   if (wide) {
-    const long long chunks = (long long)((a.vocab + CHUNK - 1) / CHUNK) * a.rows;
-    const dim3 grid((unsigned)std::min(chunks, (long long)n_cu));
-    hipLaunchKernelGGL(k_wide_bins<DT>, grid, dim3(SM_THREADS), 0, s, a, wide);
+    const long long chunks = (long long)chunks_of(a.vocab) * a.rows;
+    hipLaunchKernelGGL(k_wide_bins<DT>, dim3((unsigned)std::min(chunks, (long long)n_cu)), dim3(SM_THREADS), 0, s, a, wide);
     hipLaunchKernelGGL(k_wide_cut<DT>, dim3(a.rows), dim3(SM_THREADS), 0, s, a, wide);
-    if (a.top_p) hipLaunchKernelGGL(k_wide_list<DT>, grid, dim3(SM_THREADS), 0, s, a, wide);
+    if (a.top_p) hipLaunchKernelGGL(k_wide_list<DT>, dim3((unsigned)std::min(chunks, 2LL * n_cu)), dim3(SM_THREADS), 0, s, a, wide);
     hipLaunchKernelGGL(k_wide_draw<DT>, dim3(a.rows), dim3(SM_THREADS), 0, s, a, wide);
   }
   return hipGetLastError();
@@ -1047,7 +1080,7 @@ hipError_t launch(const sb_sample_args &a, void *workspace, int n_cu, hipStream_
 // few rows, or rows that one workgroup is through with at once, would pay for
 // nothing.
 int64_t sample_workspace(const sb_sample_args &a) {
-  return a.rows >= 16 && a.vocab > CHUNK ? a.rows * (int64_t)sizeof(WideRow) : 0;
+  return a.rows >= 16 && a.vocab > CHUNK ? a.rows * (int64_t)(sizeof(WideRow) + (size_t)chunks_of(a.vocab) * BINS * 8) : 0;
 }
 
 hipError_t launch_sample(const sb_sample_args &a, void *workspace, int n_cu, hipStream_t s) {
