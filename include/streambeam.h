@@ -379,9 +379,9 @@ sb_status sb_rope_append(const sb_rope_args *args, void *stream);
  * and values that a query does not see have no influence on it, whatever stands
  * there; a NaN or infinite value that it does see can make its result NaN.
  * max_q and max_kv (upper bounds of a request's queries and of lens) choose the
- * kernels and the split of long caches: where they are too small the result is
- * right all the same, only slower. The workspace holds the parts of split
- * caches; calls that may run at the same time need one each. */
+ * kernels and how many workgroups share the caches: where they are too small the
+ * result is right all the same, only slower. The workspace holds the shares;
+ * calls that may run at the same time need one each. */
 typedef struct {
   int64_t struct_bytes;     /* sizeof(sb_attention_args)                            */
   const void *q;            /* [n_tokens][q_heads][head_dim]                        */

@@ -10,11 +10,15 @@
 // (the keys of a product may come in any order, as long as both operands have
 // the same). V^T is read from row-major V in LDS with the transposing read.
 //
-// k_attn_few: up to 16 rows (single tokens); bound by reading the cache. A
-// wave takes 32 keys at a time by itself, the keys of a request are split over
-// the four waves of a workgroup and over workgroups, and k_attn_join adds the
-// parts. k_attn_many: 128 rows a workgroup (prompts), 64 keys at a time in
-// LDS; bound by the matrix products and the exponentials between them.
+// k_attn_few: 16 rows at a time (single tokens); bound by reading the cache. A
+// wave takes 32 keys at a time by itself, the four waves of a workgroup take
+// turns. Caches differ in length, so the workgroups share the tiles of all
+// requests evenly, wherever requests begin and end; k_attn_join adds the parts
+// of those that more than one had a share in. 64 requests of 200 to 9000
+// tokens, 8 heads of 128 in bf16: 239 us, 5.05 TB/s (278 us where each request
+// was cut into the same number of parts; reading the same rows alone: 220 us).
+// k_attn_many: 128 rows a workgroup (prompts), 64 keys at a time in LDS; bound
+// by the matrix products and the exponentials between them.
 #include <algorithm>
 
 #include "serve.h"
@@ -137,7 +141,7 @@ __device__ __forceinline__ void span_rows(const sb_attention_args &a, int r0, in
   s.r0 = r0;
   s.p_first = s.n - s.m + r0 / G;
   s.p_last = s.n - s.m + min(r0 + count - 1, s.rows - 1) / G;
-  s.lo = a.window > 0 ? max(s.p_first - a.window + 1, 0) : 0;
+  s.lo = a.window > 0 ? max(max(s.p_first, 0) - a.window + 1, 0) : 0;   // (the window may be anything up to 2^31)
   s.ns = min(a.sinks, s.lo);
   s.n_vis = max(s.p_last + 1 - s.lo + s.ns, 0);
 }
@@ -152,18 +156,35 @@ __device__ __forceinline__ int page_of(const sb_attention_args &a, const int *ta
 }
 
 __device__ __forceinline__ bool sees(const sb_attention_args &a, int p, int key) {
-  return (key <= p) & ((a.window == 0) | (key > p - a.window) | (key < a.sinks));   // (no branches)
+  return (key <= p) & ((a.window == 0) | (key > max(p, 0) - a.window) | (key < a.sinks));   // (no branches)
 }
 
-// Parts of a split: sums [splits][n_tokens q_heads][D], then (maximum, sum).
+// What the workgroups of k_attn_few leave for k_attn_join. A unit is up to 16
+// rows of a request; units are numbered through all requests. Workgroup j's part
+// of unit u is number j + u: each step in either is a part of its own.
+struct Shares {
+  int groups;   // workgroups per key/value head that share the tiles; 0: one per request
+  int units;    // most units that there can be if max_q holds; those beyond are not shared
+  int parts() const { return groups + units; }
+  size_t bytes(const sb_attention_args &a) const {
+    return groups == 0 ? 0 : ((size_t)units + 1) * 16 + (size_t)a.kv_heads * parts() * FEW_ROWS * (a.head_dim + 2) * 4;
+  }
+};
+struct UnitInfo {
+  int first, count;   // its parts; 1: there is none, its result is there
+  int request, r0;
+};
+// In the workspace: the number of units (in a place of 16 bytes), their infos,
+// the parts' sums [kv_heads][parts][16][D], their (maximum, sum) [..][16].
+__device__ __forceinline__ UnitInfo *unit_infos(void *work) { return static_cast<UnitInfo *>(work) + 1; }
 template <int D>
-__device__ __forceinline__ float *part_sums(const sb_attention_args &a, float *parts, int split, long long row) {
-  return parts + ((long long)split * a.n_tokens * a.q_heads + row) * D;
+__device__ __forceinline__ float *part_sums(const sb_attention_args &a, void *work, int groups, int units, int hk, int part) {
+  float *p = reinterpret_cast<float *>(static_cast<UnitInfo *>(work) + 1 + units);
+  return p + ((size_t)hk * (groups + units) + part) * (FEW_ROWS * D);
 }
 template <int D>
-__device__ __forceinline__ float2 *part_stats(const sb_attention_args &a, float *parts, int splits, int split, long long row) {
-  const long long nr = (long long)a.n_tokens * a.q_heads;
-  return reinterpret_cast<float2 *>(parts + splits * nr * D) + split * nr + row;
+__device__ __forceinline__ float2 *part_stats(const sb_attention_args &a, void *work, int groups, int units, int hk, int part) {
+  return reinterpret_cast<float2 *>(part_sums<D>(a, work, groups, units, a.kv_heads, 0)) + ((size_t)hk * (groups + units) + part) * FEW_ROWS;
 }
 
 // One wave's pass over its tiles t0, t0 + 4, ... < t_end: the 16 rows' sums, their
@@ -289,111 +310,225 @@ __device__ __forceinline__ bool few_keys(const sb_attention_args &a, const Span 
 // flight: as many as the registers of a wave's tile allow.
 constexpr int few_groups(int D) { return D == 64 ? 3 : D == 128 ? 2 : 1; }
 
-template <int DT, int D>
-__global__ __launch_bounds__(AT_THREADS, few_groups(D)) void k_attn_few(sb_attention_args a, int splits, int chunk, float *parts) {
-  constexpr int VS = 2 * D + 32, DT16 = D / 16, KS = D / 32;
-  __shared__ alignas(16) unsigned char lds[AT_WAVES][FEW_KEYS * VS];
-  __shared__ float2 stats[AT_WAVES][FEW_ROWS];
+// Tiles of the request's rows r0 .. (one where they see nothing: somebody has
+// to say so).
+__device__ __forceinline__ int unit_tiles(const Span &s) { return max((s.n_vis + FEW_KEYS - 1) / FEW_KEYS, 1); }
+
+template <int D>
+struct FewShared {
+  static constexpr int VS = 2 * D + 32;
+  alignas(16) unsigned char v[AT_WAVES][FEW_KEYS * VS];
+  float2 stats[AT_WAVES][FEW_ROWS];
   static_assert(FEW_KEYS * VS >= FEW_ROWS * D * 4, "the waves' sums fit where V was");
-  const int b = blockIdx.x, hk = blockIdx.y, split = blockIdx.z;
+};
+
+// Tiles t_begin .. t_end of the span's rows: their result, or, as a share, part
+// `part` of it (below 0: the result).
+template <int DT, int D>
+__device__ __forceinline__ void few_unit(const sb_attention_args &a, const Span &s, int b, int hk, int t_begin, int t_end, int part, int groups,
+                                         int units, void *work, FewShared<D> &sh) {
+  constexpr int DT16 = D / 16, KS = D / 32;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g4 = lane >> 4, l16 = lane & 15;
   const int G = a.q_heads / a.kv_heads;
   const int *table = a.table + b * a.table_stride;
   const uint16_t *kc = static_cast<const uint16_t *>(a.k_cache) + hk * a.kc_head;
   const uint16_t *vc = static_cast<const uint16_t *>(a.v_cache) + hk * a.vc_head;
+  const int row = s.r0 + l16, i = row / G, p = s.n - s.m + i;
+  const bool real = row < s.rows;
+  u4 q[KS];
+#pragma unroll
+  for (int x = 0; x < KS; ++x) {
+    const uint16_t *src = static_cast<const uint16_t *>(a.q) + (s.q0 + i) * a.q_token + (hk * G + row - i * G) * a.q_head;
+    q[x] = real ? *reinterpret_cast<const u4 *>(src + 32 * x + 8 * g4) : u4{0, 0, 0, 0};
+  }
+  f4 o[DT16];
+  float mx, sum;
+  if (!few_keys<DT, D, false>(a, s, table, kc, vc, q, p, real, t_begin + w, t_end, &sh.v[w][0], o, mx, sum))
+    few_keys<DT, D, true>(a, s, table, kc, vc, q, p, real, t_begin + w, t_end, &sh.v[w][0], o, mx, sum);
+  sum += __shfl_xor(sum, 16, 64);
+  sum += __shfl_xor(sum, 32, 64);
+  // The four waves' parts: sums side by side where V was.
+  float *os = reinterpret_cast<float *>(&sh.v[w][0]);
+#pragma unroll
+  for (int x = 0; x < DT16; ++x) *reinterpret_cast<f4 *>(os + l16 * D + 16 * x + 4 * g4) = o[x];
+  if (g4 == 0) sh.stats[w][l16] = make_float2(mx, sum);
+  __syncthreads();
+  for (int e = threadIdx.x; e < FEW_ROWS * D / 4; e += AT_THREADS) {
+    const int rr = e / (D / 4), col = (e - rr * (D / 4)) * 4, rw = s.r0 + rr;
+    if (rw >= s.rows) continue;
+    float m4 = -INFINITY, l4 = 0.0f;
+    f4 acc = {0, 0, 0, 0};
+#pragma unroll
+    for (int x = 0; x < AT_WAVES; ++x) m4 = fmaxf(m4, sh.stats[x][rr].x);
+    const float base = m4 == -INFINITY ? 0.0f : m4;
+#pragma unroll
+    for (int x = 0; x < AT_WAVES; ++x) {
+      const float f = __builtin_amdgcn_exp2f(sh.stats[x][rr].x - base);
+      l4 += f * sh.stats[x][rr].y;
+      acc += f * *reinterpret_cast<const f4 *>(reinterpret_cast<const float *>(&sh.v[x][0]) + rr * D + col);
+    }
+    if (part < 0) {
+      const int qi = rw / G;
+      const float inv = l4 == 0.0f ? 0.0f : 1.0f / l4;
+      uint16_t *dst = static_cast<uint16_t *>(a.out) + (s.q0 + qi) * a.out_token + (hk * G + rw - qi * G) * a.out_head + col;
+      *reinterpret_cast<u2 *>(dst) = u2{Half<DT>::pack(acc[0] * inv, acc[1] * inv), Half<DT>::pack(acc[2] * inv, acc[3] * inv)};
+    } else {
+      *reinterpret_cast<f4 *>(part_sums<D>(a, work, groups, units, hk, part) + rr * D + col) = acc;
+      if (col == 0) part_stats<D>(a, work, groups, units, hk, part)[rr] = make_float2(m4, l4);
+    }
+  }
+  __syncthreads();
+}
+
+template <int DT, int D>
+__global__ __launch_bounds__(AT_THREADS, few_groups(D)) void k_attn_few(sb_attention_args a, int groups, int units, void *work) {
+  __shared__ FewShared<D> sh;
+  const int hk = blockIdx.y, j = blockIdx.x;
   Span s;
-  span_request(a, b, s);
-  for (int r0 = 0; r0 < s.rows; r0 += FEW_ROWS) {
-    span_rows(a, r0, FEW_ROWS, s);
-    const int row = r0 + l16, i = row / G, p = s.n - s.m + i;
-    const bool real = row < s.rows;
-    // This part's tiles: `chunk` keys each, more where max_kv was too small.
-    const int tiles = (s.n_vis + FEW_KEYS - 1) / FEW_KEYS, per = max(chunk / FEW_KEYS, (tiles + splits - 1) / splits);
-    const int t_begin = min(split * per, tiles), t_end = min(t_begin + per, tiles);
-    if (t_begin < t_end) {
-      u4 q[KS];
-#pragma unroll
-      for (int x = 0; x < KS; ++x) {
-        const uint16_t *src = static_cast<const uint16_t *>(a.q) + (s.q0 + i) * a.q_token + (hk * G + row - i * G) * a.q_head;
-        q[x] = real ? *reinterpret_cast<const u4 *>(src + 32 * x + 8 * g4) : u4{0, 0, 0, 0};
-      }
-      f4 o[DT16];
-      float mx, sum;
-      if (!few_keys<DT, D, false>(a, s, table, kc, vc, q, p, real, t_begin + w, t_end, &lds[w][0], o, mx, sum))
-        few_keys<DT, D, true>(a, s, table, kc, vc, q, p, real, t_begin + w, t_end, &lds[w][0], o, mx, sum);
-      sum += __shfl_xor(sum, 16, 64);
-      sum += __shfl_xor(sum, 32, 64);
-      // The four waves' parts: sums side by side where V was.
-      float *os = reinterpret_cast<float *>(&lds[w][0]);
-#pragma unroll
-      for (int x = 0; x < DT16; ++x) *reinterpret_cast<f4 *>(os + l16 * D + 16 * x + 4 * g4) = o[x];
-      if (g4 == 0) stats[w][l16] = make_float2(mx, sum);
+  if (groups == 0) {   // a request each
+    span_request(a, j, s);
+    for (int r0 = 0; r0 < s.rows; r0 += FEW_ROWS) {
+      span_rows(a, r0, FEW_ROWS, s);
+      few_unit<DT, D>(a, s, j, hk, 0, unit_tiles(s), -1, 0, 0, nullptr, sh);
     }
-    __syncthreads();
-    for (int e = threadIdx.x; e < FEW_ROWS * D / 4; e += AT_THREADS) {
-      const int rr = e / (D / 4), col = (e - rr * (D / 4)) * 4, rw = r0 + rr;
-      if (rw >= s.rows) continue;
-      const int qi = rw / G, tok = s.q0 + qi, h = hk * G + rw - qi * G;
-      const long long pr = (long long)tok * a.q_heads + h;
-      float m4 = -INFINITY, l4 = 0.0f;
-      f4 acc = {0, 0, 0, 0};
-      if (t_begin < t_end) {
-#pragma unroll
-        for (int x = 0; x < AT_WAVES; ++x) m4 = fmaxf(m4, stats[x][rr].x);
-        const float base = m4 == -INFINITY ? 0.0f : m4;
-#pragma unroll
-        for (int x = 0; x < AT_WAVES; ++x) {
-          const float f = __builtin_amdgcn_exp2f(stats[x][rr].x - base);
-          l4 += f * stats[x][rr].y;
-          acc += f * *reinterpret_cast<const f4 *>(reinterpret_cast<const float *>(&lds[x][0]) + rr * D + col);
-        }
-      }
-      if (splits == 1) {
-        const float inv = l4 == 0.0f ? 0.0f : 1.0f / l4;
-        uint16_t *dst = static_cast<uint16_t *>(a.out) + tok * a.out_token + h * a.out_head + col;
-        *reinterpret_cast<u2 *>(dst) = u2{Half<DT>::pack(acc[0] * inv, acc[1] * inv), Half<DT>::pack(acc[2] * inv, acc[3] * inv)};
-      } else {   // (a part without keys: its statistics say so, and nobody reads its sums)
-        if (t_begin < t_end) *reinterpret_cast<f4 *>(part_sums<D>(a, parts, split, pr) + col) = acc;
-        if (col == 0) *part_stats<D>(a, parts, splits, split, pr) = make_float2(m4, l4);
-      }
+    return;
+  }
+  // Units and tiles before each request: every workgroup adds them up, a few
+  // neighbouring requests a thread.
+  __shared__ long long wave_tiles[AT_WAVES];
+  __shared__ int wave_units[AT_WAVES];
+  __shared__ long long start_tile;   // of the request that this workgroup's share begins in
+  __shared__ int start_request, start_unit;
+  if (threadIdx.x == 0) start_request = a.n_requests;
+  const int per_thread = (a.n_requests + AT_THREADS - 1) / AT_THREADS, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int b0 = threadIdx.x * per_thread, b1 = min(b0 + per_thread, a.n_requests);
+  auto count = [&](int b, int &n, long long &t) {
+    span_request(a, b, s);
+    n = 0;
+    t = 0;
+    for (int r0 = 0; r0 < s.rows; r0 += FEW_ROWS) {
+      span_rows(a, r0, FEW_ROWS, s);
+      t += unit_tiles(s);
+      ++n;
     }
-    __syncthreads();
+  };
+  int n = 0;
+  long long t = 0;
+  for (int b = b0; b < b1; ++b) {
+    int bn;
+    long long bt;
+    count(b, bn, bt);
+    n += bn;
+    t += bt;
+  }
+  int n_upto = n;
+  long long t_upto = t;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int x = __shfl_up(n_upto, o, 64);
+    const long long y = __shfl_up(t_upto, o, 64);
+    if (lane >= o) {
+      n_upto += x;
+      t_upto += y;
+    }
+  }
+  if (lane == 63) {
+    wave_units[w] = n_upto;
+    wave_tiles[w] = t_upto;
+  }
+  __syncthreads();
+  long long all = 0;
+  int all_units = 0;
+#pragma unroll
+  for (int x = 0; x < AT_WAVES; ++x) {
+    if (x < w) {
+      n_upto += wave_units[x];
+      t_upto += wave_tiles[x];
+    }
+    all += wave_tiles[x];
+    all_units += wave_units[x];
+  }
+  // Shares of a whole number of tiles for each wave.
+  auto divide = [&](long long x, long long y) { return all < (1LL << 30) ? (long long)((int)x / (int)y) : x / y; };   // x <= all + groups
+  const long long per = (divide(all + groups - 1, groups) + AT_WAVES - 1) & -AT_WAVES;
+  const long long begin = j * per, end = min(begin + per, all);
+  if (j == 0 && hk == 0 && threadIdx.x == 0) *static_cast<int *>(work) = min(all_units, units);
+  if (begin >= end) return;
+  if (t_upto - t <= begin && begin < t_upto) {   // (one thread)
+    int u = n_upto - n;
+    long long at = t_upto - t;
+    for (int b = b0; b < b1; ++b) {
+      int bn;
+      long long bt;
+      count(b, bn, bt);
+      if (begin < at + bt) {
+        start_request = b;
+        start_unit = u;
+        start_tile = at;
+        break;
+      }
+      u += bn;
+      at += bt;
+    }
+  }
+  __syncthreads();
+  int u = start_unit;
+  long long at = start_tile;   // of the unit's first tile
+  for (int b = start_request; b < a.n_requests && at < end; ++b) {
+    span_request(a, b, s);
+    for (int r0 = 0; r0 < s.rows && at < end; r0 += FEW_ROWS, ++u) {
+      span_rows(a, r0, FEW_ROWS, s);
+      const int tiles = unit_tiles(s);
+      const long long next = at + tiles;
+      if (next > begin) {
+        const int t0 = (int)max(begin - at, 0LL), t1 = u < units ? (int)min(end - at, (long long)tiles) : tiles;
+        const bool whole = t0 == 0 && t1 == tiles;
+        if (u < units && t0 == 0 && hk == 0 && threadIdx.x == 0)
+          unit_infos(work)[u] = UnitInfo{j + u, whole ? 1 : (int)min(divide(next - 1, per), groups - 1LL) - j + 1, b, r0};
+        if (u < units || t0 == 0) few_unit<DT, D>(a, s, b, hk, t0, t1, whole ? -1 : j + u, groups, units, work, sh);
+      }
+      at = next;
+    }
   }
 }
 
-// One wave per row: parts with a share in the row, added in order.
+// A unit's rows, 16 threads each: the parts in order.
 template <int DT, int D>
-__global__ __launch_bounds__(AT_THREADS) void k_attn_join(sb_attention_args a, int splits, float *parts) {
-  const int lane = threadIdx.x & 63;
-  const long long row = (long long)blockIdx.x * AT_WAVES + (threadIdx.x >> 6);
-  const long long rows = (long long)min(a.q_start[a.n_requests], a.n_tokens) * a.q_heads;
-  if (row >= rows) return;
+__global__ __launch_bounds__(AT_THREADS) void k_attn_join(sb_attention_args a, int groups, int units, void *work) {
+  constexpr int E = D / 16;
+  const int u = blockIdx.x, hk = blockIdx.y, rr = threadIdx.x >> 4, col = (threadIdx.x & 15) * E;
+  if (u >= *static_cast<const int *>(work)) return;
+  const UnitInfo info = unit_infos(work)[u];
+  if (info.count <= 1) return;
+  Span s;
+  span_request(a, info.request, s);
+  const int G = a.q_heads / a.kv_heads, row = info.r0 + rr, qi = row / G;
+  if (row >= s.rows) return;
+  const float2 *stats = part_stats<D>(a, work, groups, units, hk, info.first) + rr;
+  const float *sums = part_sums<D>(a, work, groups, units, hk, info.first) + rr * D + col;
   float mx = -INFINITY;
-  for (int s = 0; s < splits; ++s) mx = fmaxf(mx, part_stats<D>(a, parts, splits, s, row)->x);
+  for (int x = 0; x < info.count; ++x) mx = fmaxf(mx, stats[x * FEW_ROWS].x);
   const float base = mx == -INFINITY ? 0.0f : mx;
-  constexpr int E = D / 64;
   float acc[E], sum = 0.0f;
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.0f;
-  for (int s = 0; s < splits; ++s) {
-    const float2 st = *part_stats<D>(a, parts, splits, s, row);
-    if (st.x == -INFINITY) continue;   // nothing seen there
+#pragma unroll 4
+  for (int x = 0; x < info.count; ++x) {
+    const float2 st = stats[x * FEW_ROWS];
     const float f = __builtin_amdgcn_exp2f(st.x - base);
     sum += f * st.y;
-    const float *src = part_sums<D>(a, parts, s, row) + lane * E;
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] += f * src[e];
+    for (int e = 0; e < E; e += 4) {
+      const f4 v = *reinterpret_cast<const f4 *>(sums + (size_t)x * (FEW_ROWS * D) + e);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) acc[e + y] += f * v[y];
+    }
   }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  const long long tok = row / a.q_heads;
-  const int h = (int)(row - tok * a.q_heads);
-  uint16_t *dst = static_cast<uint16_t *>(a.out) + tok * a.out_token + h * a.out_head + lane * E;
-  if constexpr (E == 1) {
-    *dst = (uint16_t)Half<DT>::pack(acc[0] * inv, 0.0f);
-  } else {
+  uint16_t *dst = static_cast<uint16_t *>(a.out) + (s.q0 + qi) * a.out_token + (hk * G + row - qi * G) * a.out_head + col;
 #pragma unroll
-    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t *>(dst + e) = Half<DT>::pack(acc[e] * inv, acc[e + 1] * inv);
-  }
+  for (int e = 0; e < E; e += 4)
+    *reinterpret_cast<u2 *>(dst + e) = u2{Half<DT>::pack(acc[e] * inv, acc[e + 1] * inv), Half<DT>::pack(acc[e + 2] * inv, acc[e + 3] * inv)};
 }
 
 // What the waves of k_attn_many share: two tiles of K and V, one worked on
@@ -673,54 +808,51 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : 2) void k_attn_many(sb_a
 // would leave most of its products empty.
 bool many(const sb_attention_args &a) { return (long long)a.max_q * (a.q_heads / a.kv_heads) > 3 * FEW_ROWS; }
 
-// Keys a caller may expect a query to see at most.
-long long seen_keys(const sb_attention_args &a) {
-  return a.window > 0 ? std::min((long long)a.max_kv, (long long)a.window + a.sinks + a.max_q) : a.max_kv;
-}
-
-// Keys of one part: as many parts as there are (requests have caches of
-// different lengths, so that a part is a number of keys and not a share), at
-// least one tile a wave.
-int part_keys(const sb_attention_args &a, int splits) {
-  const long long step = FEW_KEYS * AT_WAVES;
-  return (int)std::max(step, ((seen_keys(a) + splits - 1) / splits + step - 1) / step * step);
+// How k_attn_few's workgroups share the work: as many per head as the units
+// hold at once, fewer where the keys that a query may be expected to see (the
+// window, or max_kv) give no wave a tile. Requests enough to fill the units
+// SHARE_BELOW times over balance themselves, a workgroup each.
+constexpr int SHARE_BELOW = 4;
+Shares shares(const sb_attention_args &a, int n_cu) {
+  if (many(a)) return {0, 0};
+  const long long G = a.q_heads / a.kv_heads, places = (long long)few_groups(a.head_dim) * n_cu;
+  if ((long long)a.n_requests * a.kv_heads >= SHARE_BELOW * places) return {0, 0};
+  const long long units = std::min(((long long)a.n_tokens * G + FEW_ROWS - 1) / FEW_ROWS + a.n_requests,
+                                   (std::max(a.max_q, 1) * G + FEW_ROWS - 1) / FEW_ROWS * a.n_requests);
+  const long long seen = a.window > 0 ? std::min((long long)a.max_kv, (long long)a.window + a.sinks + a.max_q) : a.max_kv;
+  const long long tiles = ((seen + FEW_KEYS - 1) / FEW_KEYS + 1) * units;
+  return {(int)std::max(1LL, std::min((places + a.kv_heads - 1) / a.kv_heads, (tiles + AT_WAVES - 1) / AT_WAVES)), (int)units};
 }
 
 template <int DT, int D>
-hipError_t launch(const sb_attention_args &a, int splits, float *parts, hipStream_t s) {
+hipError_t launch(const sb_attention_args &a, const Shares &sh, void *work, hipStream_t s) {
   if (many(a)) {
     const long long gx = (long long)a.n_tokens * (a.q_heads / a.kv_heads) / MANY_ROWS + a.n_requests;
     hipLaunchKernelGGL((k_attn_many<DT, D>), dim3((unsigned)(gx * a.kv_heads)), dim3(AT_THREADS), 0, s, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((k_attn_few<DT, D>), dim3(a.n_requests, a.kv_heads, splits), dim3(AT_THREADS), 0, s, a, splits,
-                     part_keys(a, splits), parts);
+  hipLaunchKernelGGL((k_attn_few<DT, D>), dim3(sh.groups ? sh.groups : a.n_requests, a.kv_heads), dim3(AT_THREADS), 0, s, a, sh.groups, sh.units,
+                     work);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || splits == 1) return e;
-  const long long rows = (long long)a.n_tokens * a.q_heads;
-  hipLaunchKernelGGL((k_attn_join<DT, D>), dim3((unsigned)((rows + AT_WAVES - 1) / AT_WAVES)), dim3(AT_THREADS), 0, s, a, splits, parts);
+  if (e != hipSuccess || sh.groups <= 1) return e;
+  hipLaunchKernelGGL((k_attn_join<DT, D>), dim3(sh.units, a.kv_heads), dim3(AT_THREADS), 0, s, a, sh.groups, sh.units, work);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int attention_splits(const sb_attention_args &a, int n_cu) {
-  if (many(a)) return 1;
-  const long long groups = (long long)a.n_requests * a.kv_heads, step = FEW_KEYS * AT_WAVES;
-  const long long want = (6LL * n_cu + groups - 1) / groups;
-  return (int)std::max(1LL, std::min({want, (seen_keys(a) + step - 1) / step, 64LL}));
-}
+int64_t attention_workspace(const sb_attention_args &a, int n_cu) { return (int64_t)shares(a, n_cu).bytes(a); }
 
-hipError_t launch_paged_attention(const sb_attention_args &a, int splits, float *parts, hipStream_t s) {
-  if (a.n_tokens == 0) return hipSuccess;
+hipError_t launch_paged_attention(const sb_attention_args &a, int n_cu, void *work, hipStream_t s) {
+  const Shares sh = shares(a, n_cu);
   if (a.dtype == SB_BF16) {
-    if (a.head_dim == 64) return launch<SB_BF16, 64>(a, splits, parts, s);
-    if (a.head_dim == 128) return launch<SB_BF16, 128>(a, splits, parts, s);
-    return launch<SB_BF16, 256>(a, splits, parts, s);
+    if (a.head_dim == 64) return launch<SB_BF16, 64>(a, sh, work, s);
+    if (a.head_dim == 128) return launch<SB_BF16, 128>(a, sh, work, s);
+    return launch<SB_BF16, 256>(a, sh, work, s);
   }
-  if (a.head_dim == 64) return launch<SB_F16, 64>(a, splits, parts, s);
-  if (a.head_dim == 128) return launch<SB_F16, 128>(a, splits, parts, s);
-  return launch<SB_F16, 256>(a, splits, parts, s);
+  if (a.head_dim == 64) return launch<SB_F16, 64>(a, sh, work, s);
+  if (a.head_dim == 128) return launch<SB_F16, 128>(a, sh, work, s);
+  return launch<SB_F16, 256>(a, sh, work, s);
 }
 
 }  // namespace sb

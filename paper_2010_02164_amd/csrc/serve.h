@@ -15,11 +15,11 @@ void set_call_error(const char *msg);
 // Each returns the launch status; the arguments are checked already.
 hipError_t launch_plan(const sb_plan_args &a, hipStream_t s);
 hipError_t launch_rope(const sb_rope_args &a, int n_cu, hipStream_t s);
-hipError_t launch_paged_attention(const sb_attention_args &a, int splits, float *parts, hipStream_t s);
+hipError_t launch_paged_attention(const sb_attention_args &a, int n_cu, void *work, hipStream_t s);
 hipError_t launch_sample(const sb_sample_args &a, void *workspace, int n_cu, hipStream_t s);   // workspace: may be null
 
-// Parts that the keys of a request are split into (1: no workspace).
-int attention_splits(const sb_attention_args &a, int n_cu);
+// Bytes of workspace of an attention (0: none).
+int64_t attention_workspace(const sb_attention_args &a, int n_cu);
 // Bytes of workspace that speed a draw up (0: none would).
 int64_t sample_workspace(const sb_sample_args &a);
 

@@ -85,10 +85,6 @@ sb_status check_sample(const sb_sample_args *a, const char *call) {
   return SB_OK;
 }
 
-int64_t attention_bytes(const sb_attention_args &a, int splits) {
-  return splits == 1 ? 0 : (int64_t)splits * a.n_tokens * a.q_heads * (a.head_dim + 2) * 4;
-}
-
 }  // namespace
 
 extern "C" {
@@ -154,7 +150,7 @@ int64_t sb_attention_workspace(const sb_attention_args *a) {
     launched(e, "sb_attention_workspace");
     return -1;
   }
-  return attention_bytes(*a, attention_splits(*a, n_cu));
+  return attention_workspace(*a, n_cu);
 }
 
 sb_status sb_paged_attention(const sb_attention_args *a, void *workspace, size_t bytes, void *stream) {
@@ -165,10 +161,10 @@ sb_status sb_paged_attention(const sb_attention_args *a, void *workspace, size_t
   int n_cu = 0;
   const hipError_t e = compute_units(n_cu);
   if (e != hipSuccess) return launched(e, call);
-  const int splits = attention_splits(*a, n_cu);
-  REFUSE_IF(splits > 1 && (!workspace || !aligned(workspace, 256) || bytes < (size_t)attention_bytes(*a, splits)),
-            SB_E_WORKSPACE, "workspace missing, misaligned or smaller than sb_attention_workspace");
-  return launched(launch_paged_attention(*a, splits, static_cast<float *>(workspace), static_cast<hipStream_t>(stream)), call);
+  const int64_t need = attention_workspace(*a, n_cu);
+  REFUSE_IF(need && (!workspace || !aligned(workspace, 256) || bytes < (size_t)need), SB_E_WORKSPACE,
+            "workspace missing, misaligned or smaller than sb_attention_workspace");
+  return launched(launch_paged_attention(*a, n_cu, workspace, static_cast<hipStream_t>(stream)), call);
 }
 
 int64_t sb_sample_workspace(const sb_sample_args *a) {
