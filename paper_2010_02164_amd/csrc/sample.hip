@@ -8,10 +8,14 @@
 // and the draw is the same search over the kept tokens' indexes.
 //
 // Most rows are read once: a sample of the row (four 16-byte pieces a thread)
-// gives a bound that the k-th largest logit hardly ever is below, the pass over
-// the row lists the tokens from that bound on, a few hundred, and all searches
-// run on the list in registers and LDS; a list of fewer than k tokens sends the
-// row the other way. min-p alone bounds the tokens by the sample's largest.
+// gives a bound that the k-th largest logit hardly ever is below, and the pass
+// over the row lists the tokens from that bound on; a list of fewer than k sends
+// the row the other way. min-p alone bounds the tokens by the sample's largest.
+// A list of up to 512 is sorted, where every filter keeps a prefix; a longer one
+// (up to 4096) is searched in registers and LDS. A row of 32000 logits in fp32
+// takes 10.5 us, of which launching and reading it takes 6 (17.6 us where short
+// lists were searched, too). 512 threads: two rows share a unit, and 320 rows
+// run at once (1024 threads: 38 instead of 34 us).
 //
 // Rows without top-k but with top-p need every weight. A pass adds them up into
 // bins of equal ratio, which names the bin that the cut is in, a second lists
@@ -38,17 +42,18 @@ namespace {
 typedef unsigned long long u64;
 typedef unsigned int u4 __attribute__((ext_vector_type(4)));
 
-constexpr int SM_THREADS = 1024;
+constexpr int SM_THREADS = 512;
 constexpr int SM_WAVES = SM_THREADS / 64;
 constexpr double ONE = 0x1p44;        // the weight of the largest logit
-constexpr int LIST_PER = 4, LIST_MAX = LIST_PER * SM_THREADS;
+constexpr int LIST_PER = 8, LIST_MAX = LIST_PER * SM_THREADS;
+constexpr int RANKED = SM_THREADS;   // a list up to this is sorted
+constexpr int DIRECT = 128;          // tokens left of it that are drawn from by comparing their indexes
 constexpr int BIN_BITS = 9, BINS = 1 << BIN_BITS;
 constexpr int TAB_BITS = 9;           // 2^x by a table of 2^(i / 512) and a cubic
 constexpr int TAB = 1 << TAB_BITS;
 constexpr int CHUNK = 16384;          // tokens of a row that a workgroup of the wide kernels takes
 constexpr int CHUNKS_MAX = SB_SAMPLE_MAX_VOCAB / CHUNK;
-// The largest top-k that is read off the sample: the list then aims at twice
-// as many tokens, and 256 more.
+// The largest top-k that is read off the sample.
 constexpr int SAMPLED_K = 1536;
 // 16-byte pieces a thread loads at once: of the sample, and of a pass (4 there
 // made the code of the passes larger than the instruction cache).
@@ -127,8 +132,8 @@ struct Shared {
   double tab[TAB];             // 2^(44 + i / 512)
   u64 hist[BINS];
   u64 part[SM_WAVES], ends[2][8];
-  uint32_t key[LIST_MAX];      // listed tokens: order bits
-  int idx[LIST_MAX];           // and indexes
+  alignas(16) uint32_t key[LIST_MAX];   // listed tokens: order bits
+  int idx[LIST_MAX];                    // and indexes
   u64 rest, at_cut;
   uint32_t digit;
   int n, token;
@@ -159,7 +164,8 @@ struct Weigher {
   __device__ __forceinline__ u64 of(double x) const { return raw(x) - RAW; }
   __device__ __forceinline__ u64 operator()(float z) const { return of(log2w(z)); }
 };
-__device__ __forceinline__ void fill_table(Shared &sh) {
+template <typename S>
+__device__ __forceinline__ void fill_table(S &sh) {
   if (threadIdx.x < TAB) sh.tab[threadIdx.x] = exp2(44.0 + threadIdx.x * (1.0 / TAB));
 }
 
@@ -198,7 +204,8 @@ __device__ __forceinline__ uint32_t max_stage(uint32_t v) {
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   return max_stage<5>(max_stage<4>(max_stage<3>(max_stage<2>(max_stage<1>(max_stage<0>(v))))));
 }
-__device__ __forceinline__ u64 block_sum(u64 v, Shared &sh) {
+template <typename S>
+__device__ __forceinline__ u64 block_sum(u64 v, S &sh) {
   v = wave_sum(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sh.part[threadIdx.x >> 6] = v;
@@ -409,6 +416,62 @@ __device__ __forceinline__ void list_token(uint32_t bits, int i, Shared &sh) {
   }
 }
 
+// A short list sorted by (-z, index): each token counts those before it (a search
+// would pass four barriers for each of its digits).
+struct Ranked {   // the token of rank threadIdx.x
+  uint32_t key;
+  int idx;
+  u64 w, before;   // its weight (0: not there), and what those before it total
+};
+template <typename F>
+__device__ __forceinline__ Ranked rank_list(int n, F weight, Shared &sh) {
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  // Behind the list: keys by rank, equals in any order and then by their indexes.
+  uint32_t *keys = sh.key + 2 * RANKED, *sharing = sh.key + 3 * RANKED;
+  int *any_order = sh.idx + 2 * RANKED, *sorted = sh.idx + 3 * RANKED;
+  if (tid < 4) sh.key[n + tid] = 0;   // before none
+  sharing[tid] = 0;
+  if (tid == 0) sh.at_cut = 0, sh.digit = 0;
+  __syncthreads();
+  int rank = 0;
+  const uint32_t key = sh.key[tid];
+  const int idx = sh.idx[tid];
+  if (tid < n) {
+#pragma unroll 4
+    for (int x = 0; x < n; x += 4) {
+      const u4 k = *reinterpret_cast<const u4 *>(&sh.key[x]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) rank += k[e] > key;
+    }
+    const int at = rank + (int)atomicAdd(&sharing[rank], 1u);
+    keys[at] = key;
+    any_order[at] = idx;
+  }
+  __syncthreads();
+  if (tid < n) {
+    const int equals = (int)sharing[rank];
+    int at = rank;
+    if (equals > 1)
+#pragma unroll 4
+      for (int x = 0; x < equals; ++x) at += any_order[rank + x] < idx;
+    sorted[at] = idx;
+  }
+  __syncthreads();
+  Ranked me = {0, 0, 0, 0};
+  if (tid < n) {
+    me.key = keys[tid];
+    me.idx = sorted[tid];
+    me.w = weight(me.key);
+  }
+  const u64 upto = wave_scan(me.w);
+  if (lane == 63) sh.part[wv] = upto;
+  __syncthreads();
+  me.before = upto - me.w;
+#pragma unroll
+  for (int i = 0; i < SM_WAVES; ++i) me.before += i < wv ? sh.part[i] : 0;
+  return me;
+}
+
 __device__ __forceinline__ int bits_of(uint32_t x) { return 32 - __clz((int)x); }   // x < 2^bits; 0 for 0
 
 // Leaves the listed tokens up to the cut at best - d, of its equals the first
@@ -454,6 +517,54 @@ struct Params {
     return fmin(TAB * (2.0 + log2((double)V / fmax(1.0 - (double)p, 1e-9))), -Weigher::LOW);
   }
 };
+
+// The draw from a short list that holds every token that may be kept.
+__device__ __forceinline__ int draw_ranked(int n, const Params &pr, const Weigher &weigh, int V, u64 &total, Shared &sh) {
+  const Ranked me = rank_list(n, [&](uint32_t b) { return weigh(from_order(b)); }, sh);
+  if (pr.greedy) {
+    total = (u64)ONE;
+    if (threadIdx.x == 0) sh.token = me.idx;
+    __syncthreads();
+    return sh.token;
+  }
+  const int keep = pr.k > 0 ? min(pr.k, n) : n;
+  u64 limit = ~0ull;
+  if (pr.p < 1.0f) {
+    if ((int)threadIdx.x == keep - 1) sh.rest = me.before + me.w;
+    __syncthreads();
+    limit = pr.top_p_limit(sh.rest);
+  }
+  // Every filter leaves the first so many.
+  const bool kept = (int)threadIdx.x < keep && me.before <= limit && me.w >= (u64)ceil((double)pr.mp * ONE) && me.w > 0;
+  const u64 on = __ballot(kept);
+  if (on && (int)(threadIdx.x & 63) == 63 - __builtin_clzll(on)) {   // the wave's last
+    atomicAdd(&sh.digit, (uint32_t)__popcll(on));
+    atomicMax(&sh.at_cut, me.before + me.w);
+  }
+  sh.hist[threadIdx.x] = kept ? me.w : 0;
+  __syncthreads();
+  const int m = (int)sh.digit;
+  total = sh.at_cut;
+  limit = pr.draw_limit(total);
+  if (m > DIRECT) {
+    Items it;
+#pragma unroll
+    for (int j = 1; j < LIST_PER; ++j) it.w[j] = 0, it.idx[j] = 0;
+    it.idx[0] = me.idx;
+    it.w[0] = kept ? me.w : 0;
+    u64 rest, at;
+    return (int)list_search(it, [&](int j) { return (uint32_t)it.idx[j]; }, bits_of(V - 1), 0, limit, rest, at, sh);
+  }
+  if (kept) {   // what the kept tokens of lower indexes total
+    const int *sorted = sh.idx + 3 * RANKED;
+    u64 before = 0;
+#pragma unroll 4
+    for (int x = 0; x < m; ++x) before += sorted[x] < me.idx ? sh.hist[x] : 0;
+    if (before <= limit && limit < before + me.w) sh.token = me.idx;
+  }
+  __syncthreads();
+  return sh.token;
+}
 
 // What is kept of a row: logits above `lo`, and those equal to it with an
 // index up to `last`. (Never NaN or -inf.)
@@ -664,6 +775,7 @@ struct WideRow {
   uint32_t key[LIST_MAX];
   int idx[LIST_MAX];
 };
+static_assert(RANKED <= BINS && LIST_MAX >= 4 * RANKED, "room for what is sorted behind the list, and for its weights");
 static_assert(sizeof(WideRow) % 16 == 0, "rows of the workspace stay aligned");
 __host__ __device__ __forceinline__ int chunks_of(int V) { return (V + CHUNK - 1) / CHUNK; }
 // Behind them: a chunk's bins. (Atomics on one set of a row's took as long as
@@ -691,7 +803,7 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
   // The sample: SAMPLE pieces a thread, from as many places of the row.
   const int apart = max((row.pieces + SAMPLE - 1) / SAMPLE, SM_THREADS);
   u4 x[SAMPLE];
-  float zm = -INFINITY;
+  float zs[2] = {-INFINITY, -INFINITY};   // the largest of each half of this thread's
 #pragma unroll
   for (int b = 0; b < SAMPLE; ++b) {
     const int j = b * apart + tid;
@@ -705,14 +817,14 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
       float z[VEC];
       Row<DT>::unpack(x[b], z);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) zm = fmaxf(zm, z[e]);
+      for (int e = 0; e < VEC; ++e) zs[b & 1] = fmaxf(zs[b & 1], z[e]);
     }
   }
   if (tid == 0) {
     sh.n = 0;
     if (wide) wide[r].kind = 0;
   }
-  const uint32_t seen = block_max(order_bits(zm), sh);   // (its barriers also publish the table and n)
+  const uint32_t seen = block_max(order_bits(fmaxf(zs[0], zs[1])), sh);   // (its barriers also publish the table and n)
   // Whether the tokens that matter are read off the sample, and from which on.
   const bool sampled = greedy || (k > 0 && k <= SAMPLED_K) || (k == 0 && p == 1.0f && mp > 0.0f);
   float bound = -INFINITY;
@@ -721,20 +833,24 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
     bound = from_order(seen);
   } else if (sampled) {
     if (k > 0) {
-      Items it;
-      it.key[0] = seen - order_bits(zm);
-      it.w[0] = 1;
-#pragma unroll
-      for (int j = 1; j < LIST_PER; ++j) it.w[j] = 0, it.key[j] = 0;
       // Read off the sample as the k-th largest is off the row, or a lower
-      // one than that (2 k + 256 tokens in the row by the sample's share) where
-      // that lists fewer: no bound in itself, so the list is counted.
-      const int want = min(k, (int)((float)(2 * k + 256) * (float)(min(SAMPLE * SM_THREADS, row.pieces) * VEC) / (float)V) + 1);
+      // one (of k tokens, the sample's share and five times its spread, and 6)
+      // where that lists fewer: no bound in itself, so the list is counted.
+      const float share = (float)(min(SAMPLE * SM_THREADS, row.pieces) * VEC) / (float)V, kf = (float)k * share;
+      const int want = min(k, (int)(kf + 5.0f * sqrtf(kf)) + 6);
       sure = want == k;
-      // 18 bits of it: rounded away from the largest, which keeps it a bound.
+      // To a sixteenth of its distance (in order bits) from the largest, away
+      // from that, which keeps it a bound: bins of four bits and an exponent.
+      clear_bins(sh);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t d = seen - order_bits(zs[j]), e = 31 - __clz((int)(d | 16));   // e >= 4
+        atomicAdd(&sh.hist[(e - 4) * 16 + (d >> (e - 4))], 1ull);
+      }
       u64 rest, at;
-      const uint32_t d = list_search(it, [&](int j) { return it.key[j]; }, 32, 14, (u64)(want - 1), rest, at, sh) | 0x3FFFu;
-      bound = from_order(seen - min(d, seen - LOWEST));
+      const uint32_t bin = find_bin((u64)(want - 1), rest, at, sh), e4 = bin < 32 ? 0 : bin / 16 - 1;
+      const u64 d = ((u64)(bin - e4 * 16) + 1 << e4) - 1;   // the furthest of the bin
+      bound = from_order(seen - (uint32_t)min(d, (u64)(seen - LOWEST)));
     }
     // min-p keeps z >= top + T ln(min_p), top at least the sample's (less a
     // little for the rounding here).
@@ -748,8 +864,7 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
 
   // The pass over the row: its largest logit, its smallest finite one, and
   // the tokens from the bound on.
-  zm = -INFINITY;
-  float zl = INFINITY;
+  float zm = -INFINITY, zl = INFINITY;
   auto look = [&](const float (&z)[VEC], int i0) {
     float m = z[0];
 #pragma unroll
@@ -792,7 +907,10 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
   int token = 0;
   u64 total = 1;
   const int n = sh.n;
-  if (sampled && n <= LIST_MAX && (sure || n >= k)) {
+  const bool listed = sampled && (sure || n >= k);
+  if (listed && n <= RANKED) {
+    token = draw_ranked(n, pr, weigh, V, total, sh);
+  } else if (listed && n <= LIST_MAX) {
     Items it;
     take_list(it, n, [&](uint32_t b) { return greedy ? (u64)(b == best) : weigh(from_order(b)); }, sh);
     if (!greedy) {
@@ -852,7 +970,7 @@ __device__ __forceinline__ void each_chunk(const sb_sample_args &a, const WideRo
   __shared__ int found[SM_THREADS];
   __shared__ int counts[SM_WAVES];
   const int chunks = chunks_of(a.vocab), tid = threadIdx.x, w = tid >> 6;
-  int before = 0;   // items of the rows before this thousand
+  int before = 0;   // items of the rows before these
   for (int r0 = 0; r0 < a.rows; r0 += SM_THREADS) {
     const bool on = r0 + tid < a.rows && ((kinds >> wide[min(r0 + tid, a.rows - 1)].kind) & 1);
     const u64 m = __ballot(on);
@@ -963,10 +1081,18 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_wide_cut(sb_sample_args a, Wi
 }
 
 // Then, of a top-p row's chunk: the tokens of that bin, and the weights above it.
+struct ListShared {   // (room for four workgroups a unit)
+  double tab[TAB];
+  u64 part[SM_WAVES];
+  uint32_t key[LIST_MAX];
+  uint16_t idx[LIST_MAX];   // within the chunk
+  int n;
+};
+static_assert(CHUNK <= 1 << 16, "a chunk's indexes in 16 bits");
 template <int DT>
 __global__ __launch_bounds__(SM_THREADS, 8) void k_wide_list(sb_sample_args a, WideRow *wide) {
   constexpr int VEC = Row<DT>::VEC;
-  __shared__ Shared sh;
+  __shared__ ListShared sh;
   __shared__ int base;
   const int tid = threadIdx.x;
   fill_table(sh);
@@ -993,7 +1119,13 @@ __global__ __launch_bounds__(SM_THREADS, 8) void k_wide_list(sb_sample_args a, W
       if (!(m >= from)) return;
 #pragma unroll
       for (int e = 0; e < VEC; ++e)
-        if (z[e] >= z_lo && z[e] <= z_hi) list_token(order_bits(z[e]), i0 + j0 + e, sh);
+        if (z[e] >= z_lo && z[e] <= z_hi) {
+          const int at = atomicAdd(&sh.n, 1);
+          if (at < LIST_MAX) {
+            sh.key[at] = order_bits(z[e]);
+            sh.idx[at] = (uint16_t)(j0 + e);
+          }
+        }
       if (!any_above) return;
       u64 x[VEC];
       kept_weights<VEC>(z, i0 + j0, weigh, above, x);
@@ -1011,7 +1143,7 @@ __global__ __launch_bounds__(SM_THREADS, 8) void k_wide_list(sb_sample_args a, W
     for (int j = tid; j < min(m, LIST_MAX); j += SM_THREADS)
       if (base + j < LIST_MAX) {
         w.key[base + j] = sh.key[j];
-        w.idx[base + j] = sh.idx[j];
+        w.idx[base + j] = i0 + sh.idx[j];
       }
   });
 }
@@ -1045,6 +1177,19 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_wide_draw(sb_sample_args a, W
       sh.idx[j] = w.idx[j];
     }
     __syncthreads();
+    if (w.n <= RANKED) {
+      const Ranked me = rank_list(w.n, [&](uint32_t b) { return weigh(from_order(b)); }, sh);
+      if (me.w && me.before <= w.rest) {
+        if (from_order(me.key) >= w.z_mp) atomicAdd(&tot[me.idx / CHUNK], me.w);
+        if (w.rest < me.before + me.w) {
+          sh.digit = me.key;
+          sh.token = me.idx;
+        }
+      }
+      __syncthreads();
+      cut.lo = from_order(sh.digit);
+      cut.last = sh.token;
+    } else {
     take_list(it, w.n, [&](uint32_t b) { return weigh(from_order(b)); }, sh);
     u64 rest, at;
     const uint32_t d = list_search(it, [&](int j) { return last - it.key[j]; }, bits_of(last - w.first), 0, w.rest, rest, at, sh);
@@ -1054,6 +1199,7 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_wide_draw(sb_sample_args a, W
 #pragma unroll
     for (int j = 0; j < LIST_PER; ++j)
       if (it.w[j] && from_order(it.key[j]) >= w.z_mp) atomicAdd(&tot[it.idx[j] / CHUNK], it.w[j]);
+    }
   }
   __syncthreads();
   cut.raise(w.z_mp);
@@ -1066,9 +1212,9 @@ hipError_t launch(const sb_sample_args &a, void *workspace, int n_cu, hipStream_
   hipLaunchKernelGGL(k_sample<DT>, dim3(a.rows), dim3(SM_THREADS), 0, s, a, wide);
   if (wide) {
     const long long chunks = (long long)chunks_of(a.vocab) * a.rows;
-    hipLaunchKernelGGL(k_wide_bins<DT>, dim3((unsigned)std::min(chunks, (long long)n_cu)), dim3(SM_THREADS), 0, s, a, wide);
+    hipLaunchKernelGGL(k_wide_bins<DT>, dim3((unsigned)std::min(chunks, 2LL * n_cu)), dim3(SM_THREADS), 0, s, a, wide);
     hipLaunchKernelGGL(k_wide_cut<DT>, dim3(a.rows), dim3(SM_THREADS), 0, s, a, wide);
-    if (a.top_p) hipLaunchKernelGGL(k_wide_list<DT>, dim3((unsigned)std::min(chunks, 2LL * n_cu)), dim3(SM_THREADS), 0, s, a, wide);
+    if (a.top_p) hipLaunchKernelGGL(k_wide_list<DT>, dim3((unsigned)std::min(chunks, 4LL * n_cu)), dim3(SM_THREADS), 0, s, a, wide);
     hipLaunchKernelGGL(k_wide_draw<DT>, dim3(a.rows), dim3(SM_THREADS), 0, s, a, wide);
   }
   return hipGetLastError();
