@@ -7,9 +7,11 @@
 // of the requests). So one workgroup holds all requests and does one scan of
 // three sums; a step is bound by its latency - lengths, scan, free list, table,
 // each a trip to memory -, not by its bytes (20 a request, 12 a token). A step
-// of few tokens has its slots written by the same workgroup, each token finding
-// its request by bisection of q_start in LDS; more go to a second, wide kernel.
+// of few tokens has its slots written by the same workgroup: where each request
+// has one new token by the request's thread, else each token finds its request
+// by bisection of q_start in LDS; more tokens go to a second, wide kernel.
 #include "serve.h"
+#include "wave.h"
 
 namespace sb {
 namespace {
@@ -25,6 +27,7 @@ struct Sums {
 struct PlanShared {
   Sums wave[PLAN_WAVES];
   unsigned long long granted_tokens, granted_pages;
+  int more;   // whether a request was granted more than one token
   int q_start[SB_PLAN_MAX_REQUESTS + 1];
 };
 
@@ -32,15 +35,9 @@ struct PlanShared {
 __device__ __forceinline__ Sums scan_block(const Sums &v, PlanShared &sh, Sums &total) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   Sums x = v;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const long long a = __shfl_up(x.gone, o, 64), b = __shfl_up(x.tokens, o, 64), c = __shfl_up(x.pages, o, 64);
-    if (lane >= o) {
-      x.gone += a;
-      x.tokens += b;
-      x.pages += c;
-    }
-  }
+  x.gone = (long long)wave_scan((unsigned long long)x.gone);
+  x.tokens = (long long)wave_scan((unsigned long long)x.tokens);
+  x.pages = (long long)wave_scan((unsigned long long)x.pages);
   if (lane == 63) sh.wave[w] = x;
   __syncthreads();
   Sums before = {0, 0, 0};
@@ -88,7 +85,11 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan(sb_plan_args a, int fused
   const int B = a.n_requests, ps = a.page_size, lane = threadIdx.x & 63, b0 = threadIdx.x * PER;
   const long long room = (long long)a.max_pages * ps;
   int len[PER], want[PER], held[PER], toks[PER], need[PER];
-  if (threadIdx.x == 0) sh.granted_tokens = sh.granted_pages = 0;
+  int page[PER];   // that a request's next token goes to, as far as it has one
+  if (threadIdx.x == 0) {
+    sh.granted_tokens = sh.granted_pages = 0;
+    sh.more = 0;
+  }
   const int free0 = min(max(*a.n_free, 0), a.n_pages);
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
@@ -99,9 +100,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan(sb_plan_args a, int fused
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     len[i] = (int)min((long long)max(len[i], 0), room);
-    held[i] = (int)(((long long)len[i] + ps - 1) / ps);
+    held[i] = (int)(((unsigned)len[i] + (unsigned)ps - 1u) / (unsigned)ps);
     toks[i] = want[i] > 0 && (long long)len[i] + want[i] <= room ? want[i] : 0;
-    need[i] = toks[i] ? (int)(((long long)len[i] + toks[i] + ps - 1) / ps) - held[i] : 0;
+    need[i] = toks[i] ? (int)(((unsigned)len[i] + (unsigned)toks[i] + (unsigned)ps - 1u) / (unsigned)ps) - held[i] : 0;
+    page[i] = toks[i] && held[i] * (long long)ps > len[i] ? a.table[(long long)(b0 + i) * a.table_stride + held[i] - 1] : -1;
     mine.gone += want[i] < 0 ? held[i] : 0;
     mine.tokens += toks[i];
     mine.pages += need[i];
@@ -143,23 +145,26 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan(sb_plan_args a, int fused
       toks[i] = need[i] = 0;
     }
   }
-  // (The sums only grow, so the largest granted ones are everybody's totals.)
+  // (The sums only grow, so the last granted one's are everybody's totals.)
+  const unsigned long long granted = __ballot(last_t > 0);
+  bool several = false;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    last_t = max(last_t, __shfl_xor(last_t, o, 64));
-    last_p = max(last_p, __shfl_xor(last_p, o, 64));
-  }
-  if (lane == 0) {
+  for (int i = 0; i < PER; ++i) several |= toks[i] > 1;
+  if (granted && lane == 63 - __builtin_clzll(granted)) {
     atomicMax(&sh.granted_tokens, (unsigned long long)last_t);
     atomicMax(&sh.granted_pages, (unsigned long long)last_p);
   }
+  if (several) sh.more = 1;
   __syncthreads();   // also: the pushes are there before the pops
   const long long T = (long long)sh.granted_tokens;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     const int b = b0 + i;
-    if (need[i] == 1)   // a step of single tokens: one page here and there
-      a.table[(long long)b * a.table_stride + held[i]] = a.free_list[stack - 1 - first[i]];
+    if (need[i] == 1) {   // a step of single tokens: one page here and there
+      const int fresh = a.free_list[stack - 1 - first[i]];
+      a.table[(long long)b * a.table_stride + held[i]] = fresh;
+      if (page[i] < 0) page[i] = fresh;
+    }
     unsigned long long m = __ballot(need[i] > 1);
     while (m) {
       const int src = __builtin_ctzll(m);
@@ -175,6 +180,11 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan(sb_plan_args a, int fused
       const int q = (int)min(start[i], T);
       a.q_start[b] = q;
       if (fused) sh.q_start[b] = q;
+      if (fused && !sh.more && toks[i]) {
+        const bool there = page[i] >= 0 && page[i] < a.n_pages;
+        a.slots[q] = there ? (long long)page[i] * ps + (unsigned)len[i] % (unsigned)ps : -1;
+        a.positions[q] = len[i];
+      }
       a.granted[b] = toks[i];
       a.lens_out[b] = want[i] < 0 ? 0 : len[i] + toks[i];
     }
@@ -186,7 +196,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void k_plan(sb_plan_args a, int fused
   }
   if (!fused) return;
   __syncthreads();
-  for (int t = threadIdx.x; t < a.token_cap; t += PLAN_THREADS) put_slot(a, sh.q_start, t);
+  for (int t = threadIdx.x + (sh.more ? 0 : (int)T); t < a.token_cap; t += PLAN_THREADS) put_slot(a, sh.q_start, t);
 }
 
 constexpr int SLOT_THREADS = 256;

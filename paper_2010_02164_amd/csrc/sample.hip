@@ -171,21 +171,6 @@ __device__ __forceinline__ void fill_table(S &sh) {
 
 // Sums and maxima over a wave through the lanes' own paths (a shuffle through
 // LDS takes about 130 cycles, and a search has dozens of steps).
-template <int CTRL, int ROWS>
-__device__ __forceinline__ u64 shifted(u64 v) {   // 0 where nothing comes
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xF, false);
-  return ((u64)hi << 32) | lo;
-}
-__device__ __forceinline__ u64 wave_scan(u64 v) {   // inclusive
-  v += shifted<0x111, 0xF>(v);   // within 16 lanes: from 1, 2, 4, 8 before
-  v += shifted<0x112, 0xF>(v);
-  v += shifted<0x114, 0xF>(v);
-  v += shifted<0x118, 0xF>(v);
-  v += shifted<0x142, 0xA>(v);   // the last of the first and third 16 to the next
-  v += shifted<0x143, 0xC>(v);   // the last of the first 32 to the others
-  return v;
-}
 template <int S>
 __device__ __forceinline__ u64 sum_stage(u64 v) {
   u64 a, b;

@@ -38,22 +38,23 @@ def _check(status: int, where: str):
 _raw_stream, _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
 
 
-def _call(fn, where, dev, *args):
-    """fn(*args, stream) on the tensors' device and its current stream."""
-    i = dev.index
+def _call(fn, where, i, *args):
+    """fn(*args, stream) on device i and its current stream."""
     if i == _current():
         status = fn(*args, _raw_stream(i))
     else:
-        with torch.cuda.device(dev):
+        with torch.cuda.device(i):
             status = fn(*args, _raw_stream(i))
     if status != N.SB_OK:
         _check(status, where)
 
 
-def _whole(t, name, dtype, dev, shape):
+# The checks read each property of a tensor once: a read takes 0.1 us, a call
+# with single tokens 10 to 15.
+def _whole(t, name, dtype, i, shape):
     """A contiguous array of whole numbers or parameters."""
-    if t.dtype != dtype or t.device != dev or t.shape != shape or not t.is_contiguous():
-        _refuse(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {dev}")
+    if t.dtype != dtype or t.get_device() != i or t.shape != shape or not t.is_contiguous():
+        _refuse(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{i}")
     return t.data_ptr()
 
 
@@ -69,29 +70,46 @@ def _apart(t, name):
 
 
 def _no_grad(*tensors):
-    if torch.is_grad_enabled() and any(t.requires_grad for t in tensors):
-        _refuse("there is no backward pass: call it under torch.no_grad()")
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t.requires_grad:
+                _refuse("there is no backward pass: call it under torch.no_grad()")
 
 
 def _device(t, name):
-    if not t.is_cuda:
+    i = t.get_device() if t.is_cuda else -1
+    if i < 0:
         _refuse(f"{name} must be on a GPU")
-    return t.device
+    return i
 
 
-def _heads(t, name, dtype, dev, tokens=None, dim=None):
-    if t.dim() != 3 or t.dtype != dtype or t.device != dev or (t.shape[2] > 1 and t.stride(2) != 1):
-        _refuse(f"{name} must be a {dtype} tensor [tokens, heads, head_dim] on {dev} with contiguous heads")
-    if (tokens is not None and t.shape[0] != tokens) or (dim is not None and t.shape[2] != dim):
+def _heads(t, name, dtype, i, tokens=None, dim=None):
+    """Its shape and strides."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 3 or t.dtype != dtype or t.get_device() != i or (strides[2] != 1 and shape[2] > 1):
+        _refuse(f"{name} must be a {dtype} tensor [tokens, heads, head_dim] on cuda:{i} with contiguous heads")
+    if dim is not None and (shape[0] != tokens or shape[2] != dim):
         _refuse(f"{name} has another number of tokens or another head_dim")
+    return shape, strides
 
 
-def _caches(k_cache, v_cache, dtype, dev, heads, dim):
-    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
-        if t.dim() != 4 or t.dtype != dtype or t.device != dev or t.stride(3) != 1:
-            _refuse(f"{name} must be a {dtype} tensor [pages, page_size, heads, head_dim] on {dev} with contiguous heads")
-    if k_cache.shape != v_cache.shape or k_cache.shape[3] != dim or (heads is not None and k_cache.shape[2] != heads):
+def _caches(k_cache, v_cache, dtype, i, heads, dim):
+    """Their shape, and the strides of each."""
+    shape, kc, vc = k_cache.shape, k_cache.stride(), v_cache.stride()
+    for t, name, strides in ((k_cache, "k_cache", kc), (v_cache, "v_cache", vc)):
+        if len(strides) != 4 or t.dtype != dtype or t.get_device() != i or strides[3] != 1:
+            _refuse(f"{name} must be a {dtype} tensor [pages, page_size, heads, head_dim] on cuda:{i} with contiguous heads")
+    if shape != v_cache.shape or shape[3] != dim or (heads is not None and shape[2] != heads):
         _refuse("the caches must have one shape, with the keys' heads and head_dim")
+    return shape, kc, vc
+
+
+def _table(t, i):
+    """Its shape and row stride."""
+    shape = t.shape
+    if len(shape) != 2 or t.dtype != torch.int32 or t.get_device() != i or (shape[1] > 1 and t.stride(1) != 1):
+        _refuse(f"table must be an int32 tensor [requests, max_pages] on cuda:{i} with contiguous rows")
+    return shape, t.stride(0) if shape[0] > 1 else shape[1]
 
 
 class PagePlan(NamedTuple):
@@ -115,28 +133,29 @@ def plan_pages(lens, add, free_list, n_free, table, *, page_size: int, token_cap
     free_list are updated in place, the rest of the new state is returned, in
     new tensors or in `out`'s, which may be lens and n_free themselves. token_cap:
     the most tokens a step takes."""
-    dev = _device(lens, "lens")
-    if lens.dim() != 1 or table.dim() != 2 or table.dtype != torch.int32 or table.device != dev or (table.shape[1] > 1 and table.stride(1) != 1):
-        _refuse(f"table must be an int32 tensor [requests, max_pages] on {dev} with contiguous rows")
-    B, width, cap = lens.shape[0], table.shape[1], int(token_cap)
-    if table.shape[0] != B or free_list.dim() != 1:
-        _refuse("table needs a row per request, free_list one dimension")
+    i = _device(lens, "lens")
+    (B, width), row = _table(table, i)
+    cap = int(token_cap)
+    if free_list.dim() != 1:
+        _refuse("free_list must have one dimension")
     if cap < 0:
         _refuse("token_cap must not be negative")
     _apart(table, "table")
-    i32 = torch.int32
+    i32, i64 = torch.int32, torch.int64
     if out is None:
-        q_start, after, granted, left = torch.empty(3 * B + 2, dtype=i32, device=dev).split((B + 1, B, B, 1))
-        out = PagePlan(q_start, after, granted, torch.empty(cap, dtype=torch.int64, device=dev),
-                       torch.empty(cap, dtype=i32, device=dev), left)
+        q_start, after, granted, left = torch.empty(3 * B + 2, dtype=i32, device=i).split((B + 1, B, B, 1))
+        out = PagePlan(q_start, after, granted, torch.empty(cap, dtype=i64, device=i), torch.empty(cap, dtype=i32, device=i), left)
+        at = q_start.data_ptr()
+        to = at + 4 * (B + 1), at + 4 * (3 * B + 1), at, at + 4 * (2 * B + 1), out.slots.data_ptr(), out.positions.data_ptr()
+    else:
+        to = (_whole(out.lens, "out.lens", i32, i, (B,)), _whole(out.n_free, "out.n_free", i32, i, (1,)),
+              _whole(out.q_start, "out.q_start", i32, i, (B + 1,)), _whole(out.granted, "out.granted", i32, i, (B,)),
+              _whole(out.slots, "out.slots", i64, i, (cap,)), _whole(out.positions, "out.positions", i32, i, (cap,)))
     args = N.PLAN_ARGS.pack(
-        N.PLAN_ARGS.size, _whole(lens, "lens", i32, dev, (B,)), _whole(add, "add", i32, dev, (B,)),
-        _whole(n_free, "n_free", i32, dev, (1,)), _whole(free_list, "free_list", i32, dev, free_list.shape), table.data_ptr(),
-        _whole(out.lens, "out.lens", i32, dev, (B,)), _whole(out.n_free, "out.n_free", i32, dev, (1,)),
-        _whole(out.q_start, "out.q_start", i32, dev, (B + 1,)), _whole(out.granted, "out.granted", i32, dev, (B,)),
-        _whole(out.slots, "out.slots", torch.int64, dev, (cap,)), _whole(out.positions, "out.positions", i32, dev, (cap,)),
-        table.stride(0) if B > 1 else width, B, free_list.shape[0], int(page_size), width, cap, 0)
-    _call(N.lib().sb_plan_pages, "sb_plan_pages", dev, args)
+        N.PLAN_ARGS.size, _whole(lens, "lens", i32, i, (B,)), _whole(add, "add", i32, i, (B,)), _whole(n_free, "n_free", i32, i, (1,)),
+        _whole(free_list, "free_list", i32, i, free_list.shape), table.data_ptr(), *to,
+        row, B, free_list.shape[0], int(page_size), width, cap, 0)
+    _call(N.lib().sb_plan_pages, "sb_plan_pages", i, args)
     return out
 
 
@@ -184,39 +203,36 @@ def rope_append(q, k, v, positions, slots, k_cache, v_cache, inv_freq, *, layout
     [tokens], slots: int64 [tokens] (plan_pages gives both; tokens with slots
     outside the cache are skipped); inv_freq: float64, one per pair
     (rope_frequencies). out: where the queries go, q itself for in place."""
-    dev, dtype = _device(q, "q"), q.dtype
+    i, dtype = _device(q, "q"), q.dtype
     if dtype not in _HALVES:
         _refuse("q must be bfloat16 or float16")
     _no_grad(q, k, v)
-    _heads(q, "q", dtype, dev)
-    T, Hq, D = q.shape
-    _heads(k, "k", dtype, dev, T, D)
-    _heads(v, "v", dtype, dev, T, D)
-    Hkv = k.shape[1]
-    if v.shape[1] != Hkv:
+    (T, Hq, D), qs = _heads(q, "q", dtype, i)
+    (_, Hkv, _), ks = _heads(k, "k", dtype, i, T, D)
+    (_, Hv, _), vs = _heads(v, "v", dtype, i, T, D)
+    if Hv != Hkv:
         _refuse("k and v must have the same heads")
-    _caches(k_cache, v_cache, dtype, dev, Hkv, D)
+    (pages, page_size, _, _), kc, vc = _caches(k_cache, v_cache, dtype, i, Hkv, D)
     _apart(k_cache, "k_cache"), _apart(v_cache, "v_cache")
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=dtype, device=dev)
+        out = torch.empty((T, Hq, D), dtype=dtype, device=i)
+        os_ = (Hq * D, D)
     else:
-        _heads(out, "out", dtype, dev, T, D)
-        if out.shape[1] != Hq:
+        (_, Ho, _), os_ = _heads(out, "out", dtype, i, T, D)
+        if Ho != Hq:
             _refuse("out must have q's heads")
         _apart(out, "out")
     if layout not in _LAYOUTS:
         _refuse(f"unknown layout {layout!r}")
     if inv_freq.dim() != 1:
         _refuse("inv_freq must have one dimension")
-    np_ = inv_freq.shape[0]
-    qs, ks, vs, os_, kc, vc = q.stride(), k.stride(), v.stride(), out.stride(), k_cache.stride(), v_cache.stride()
+    pairs = inv_freq.shape[0]
     args = N.ROPE_ARGS.pack(
         N.ROPE_ARGS.size, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-        _whole(positions, "positions", torch.int32, dev, (T,)), _whole(slots, "slots", torch.int64, dev, (T,)),
-        _whole(inv_freq, "inv_freq", torch.float64, dev, (np_,)), qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], os_[0], os_[1],
-        kc[0], kc[1], kc[2], vc[0], vc[1], vc[2], T, Hq, Hkv, D, np_, _LAYOUTS[layout], _HALVES[dtype], k_cache.shape[0],
-        k_cache.shape[1], mscale)
-    _call(N.lib().sb_rope_append, "sb_rope_append", dev, args)
+        _whole(positions, "positions", torch.int32, i, (T,)), _whole(slots, "slots", torch.int64, i, (T,)),
+        _whole(inv_freq, "inv_freq", torch.float64, i, (pairs,)), qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], os_[0], os_[1],
+        kc[0], kc[1], kc[2], vc[0], vc[1], vc[2], T, Hq, Hkv, D, pairs, _LAYOUTS[layout], _HALVES[dtype], pages, page_size, mscale)
+    _call(N.lib().sb_rope_append, "sb_rope_append", i, args)
     return out
 
 
@@ -233,41 +249,37 @@ def paged_attention(q, k_cache, v_cache, table, lens, q_start, *, max_q: int, ma
     scale: 1 / sqrt(head_dim) by default. max_q, max_kv: upper bounds of a request's queries
     and of lens, for the choice of kernels only. Rows of the result behind
     the last request's are left as they are in `out` (undefined without it)."""
-    dev, dtype = _device(q, "q"), q.dtype
+    i, dtype = _device(q, "q"), q.dtype
     if dtype not in _HALVES:
         _refuse("q must be bfloat16 or float16")
     _no_grad(q, k_cache, v_cache)
-    _heads(q, "q", dtype, dev)
-    T, Hq, D = q.shape
-    _caches(k_cache, v_cache, dtype, dev, None, D)
-    if table.dim() != 2 or table.dtype != torch.int32 or table.device != dev or (table.shape[1] > 1 and table.stride(1) != 1):
-        _refuse(f"table must be an int32 tensor [requests, max_pages] on {dev} with contiguous rows")
-    B, width = table.shape
+    (T, Hq, D), qs = _heads(q, "q", dtype, i)
+    (pages, page_size, Hkv, _), kc, vc = _caches(k_cache, v_cache, dtype, i, None, D)
+    (B, width), row = _table(table, i)
     if out is None:
-        out = torch.empty((T, Hq, D), dtype=dtype, device=dev)
+        out = torch.empty((T, Hq, D), dtype=dtype, device=i)
+        os_ = (Hq * D, D)
     else:
-        _heads(out, "out", dtype, dev, T, D)
-        if out.shape[1] != Hq:
+        (_, Ho, _), os_ = _heads(out, "out", dtype, i, T, D)
+        if Ho != Hq:
             _refuse("out must have q's heads")
         _apart(out, "out")
-    pages, page, Hkv, _ = k_cache.shape
-    qs, os_, kc, vc = q.stride(), out.stride(), k_cache.stride(), v_cache.stride()
     args = N.ATTENTION_ARGS.pack(
         N.ATTENTION_ARGS.size, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table.data_ptr(),
-        _whole(lens, "lens", torch.int32, dev, (B,)), _whole(q_start, "q_start", torch.int32, dev, (B + 1,)), out.data_ptr(),
-        qs[0], qs[1], os_[0], os_[1], kc[0], kc[1], kc[2], vc[0], vc[1], vc[2], table.stride(0) if B > 1 else width,
-        T, B, Hq, Hkv, D, _HALVES[dtype], pages, page, width, window, sinks, max_q, max_kv,
+        _whole(lens, "lens", torch.int32, i, (B,)), _whole(q_start, "q_start", torch.int32, i, (B + 1,)), out.data_ptr(),
+        qs[0], qs[1], os_[0], os_[1], kc[0], kc[1], kc[2], vc[0], vc[1], vc[2], row,
+        T, B, Hq, Hkv, D, _HALVES[dtype], pages, page_size, width, window, sinks, max_q, max_kv,
         1.0 / math.sqrt(D) if scale is None else scale)
     L = N.lib()
-    if dev.index == _current():
+    if i == _current():
         need = L.sb_attention_workspace(args)
     else:
-        with torch.cuda.device(dev):
+        with torch.cuda.device(i):
             need = L.sb_attention_workspace(args)
     if need < 0:
         _check(N.SB_E_INVALID_ARG, "sb_paged_attention")
-    parts = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
-    _call(L.sb_paged_attention, "sb_paged_attention", dev, args, parts.data_ptr() if need else None, need)
+    work = torch.empty(need, dtype=torch.uint8, device=i) if need else None
+    _call(L.sb_paged_attention, "sb_paged_attention", i, args, work.data_ptr() if need else None, need)
     return out
 
 
@@ -280,24 +292,24 @@ def sample_tokens(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=
     (int32): one per row, or None to leave that filter out (temperature: 1; 0
     takes the largest logit). logprobs: of the drawn token among the kept
     ones. out: (tokens, logprobs) to write to."""
-    dev = _device(logits, "logits")
+    i = _device(logits, "logits")
     if logits.dim() != 2 or logits.dtype not in _LOGITS or (logits.shape[1] > 1 and logits.stride(1) != 1):
         _refuse("logits must be a float32, bfloat16 or float16 tensor [rows, vocab] with contiguous rows")
     _no_grad(logits)
     R, V = logits.shape
     f32 = torch.float32
     if out is None:
-        out = torch.empty(R, dtype=torch.int32, device=dev), torch.empty(R, dtype=f32, device=dev)
+        out = torch.empty(R, dtype=torch.int32, device=i), torch.empty(R, dtype=f32, device=i)
     tokens, logprobs = out
     args = N.SAMPLE_ARGS.pack(
-        N.SAMPLE_ARGS.size, logits.data_ptr(), _whole(u, "u", f32, dev, (R,)),
-        0 if temperature is None else _whole(temperature, "temperature", f32, dev, (R,)),
-        0 if top_k is None else _whole(top_k, "top_k", torch.int32, dev, (R,)),
-        0 if top_p is None else _whole(top_p, "top_p", f32, dev, (R,)),
-        0 if min_p is None else _whole(min_p, "min_p", f32, dev, (R,)), _whole(tokens, "out tokens", torch.int32, dev, (R,)),
-        _whole(logprobs, "out logprobs", f32, dev, (R,)), logits.stride(0) if R > 1 else V, R, V, _LOGITS[logits.dtype], 0)
+        N.SAMPLE_ARGS.size, logits.data_ptr(), _whole(u, "u", f32, i, (R,)),
+        0 if temperature is None else _whole(temperature, "temperature", f32, i, (R,)),
+        0 if top_k is None else _whole(top_k, "top_k", torch.int32, i, (R,)),
+        0 if top_p is None else _whole(top_p, "top_p", f32, i, (R,)),
+        0 if min_p is None else _whole(min_p, "min_p", f32, i, (R,)), _whole(tokens, "out tokens", torch.int32, i, (R,)),
+        _whole(logprobs, "out logprobs", f32, i, (R,)), logits.stride(0) if R > 1 else V, R, V, _LOGITS[logits.dtype], 0)
     L = N.lib()
     need = L.sb_sample_workspace(args)   # (below 0: refused by the call itself)
-    work = torch.empty(need, dtype=torch.uint8, device=dev) if need > 0 else None
-    _call(L.sb_sample_tokens, "sb_sample_tokens", dev, args, None if work is None else work.data_ptr(), max(need, 0))
+    work = torch.empty(need, dtype=torch.uint8, device=i) if need > 0 else None
+    _call(L.sb_sample_tokens, "sb_sample_tokens", i, args, None if work is None else work.data_ptr(), max(need, 0))
     return tokens, logprobs
