@@ -66,10 +66,18 @@ class SbStats(ctypes.Structure):
 # Arguments of the serving calls, in the order of their structs' fields
 # (struct_bytes first): packed rather than kept as ctypes structures, whose
 # assignments take longer than a single-token call.
-PLAN_ARGS = struct.Struct("q11Pq6i")
-ROPE_ARGS = struct.Struct("q9P14q9if")
-ATTENTION_ARGS = struct.Struct("q7P11q13if")
-SAMPLE_ARGS = struct.Struct("q8Pq4i")
+class _Args(struct.Struct):
+    def pack(self, *fields) -> bytes:
+        try:
+            return super().pack(*fields)
+        except struct.error as e:
+            raise ValueError(f"an argument does not fit its field: {e}") from None
+
+
+PLAN_ARGS = _Args("q11Pq6i")
+ROPE_ARGS = _Args("q9P14q9if")
+ATTENTION_ARGS = _Args("q7P11q13if")
+SAMPLE_ARGS = _Args("q8Pq4i")
 
 
 class StreambeamError(RuntimeError):

@@ -115,6 +115,29 @@ def test_plan_in_place_and_repeated(gpu):
         assert cur.lens.tolist() == lens and cur.slots.tolist() == slots and fl[:int(cur.n_free)].tolist() == free
 
 
+@pytest.mark.parametrize("B,page", [(1, 16), (65, 4), (1024, 16), (1030, 3)])
+def test_plan_of_single_tokens(gpu, B, page):
+    """Steps in which requests take a token, none, or end; of entries of the
+    table that are no pages the slots are -1."""
+    r = rng(B + 1)
+    lens, add = r.integers(0, 5 * page, B), r.integers(-1, 2, B)
+    add[0] = 1
+    held = -(-lens // page)
+    n_pages = int(held.sum()) + B
+    ids = r.permutation(n_pages)
+    table = np.full((B, 6), -1)
+    table[np.arange(6) < held[:, None]] = ids[:held.sum()]
+    free = ids[held.sum():].tolist()
+    for cap, some in ((B, free), (B // 2, free), (B + 70, free[:B // 8])):
+        check_plan(lens, add, some, n_pages, table, page, cap)
+    lens[0], add[:] = 2 * page - 1, 1
+    for bad in (-1, -2 ** 31, n_pages, 2 ** 31 - 1):
+        table[0, 1] = bad
+        p, _, _ = run_plan(lens, add, free, n_pages, table, page, B)
+        assert int(p.slots[0]) == -1 and int(p.positions[0]) == 2 * page - 1
+        assert bool((p.slots[1:] >= 0).all())
+
+
 # -- rotary positions and the cache's write --------------------------------------------
 
 def rope_case(T, Hq, Hkv, D, pairs, dtype, seed, page=16, far=10 ** 6):
@@ -270,6 +293,31 @@ def test_attention_wrong_bounds_only_cost_time(gpu):
             check_attention(c, got, 300, 2)
 
 
+@pytest.mark.parametrize("max_q", [0, 1, 3, 1000])
+def test_attention_of_many_requests(gpu, max_q):
+    """More requests than threads, of 0 to 3 queries, some over no tokens; with
+    many heads so many that each has a workgroup."""
+    for B, Hq, Hkv, D, dtype in ((300, 4, 1, 64, BF16), (700, 20, 1, 64, F16), (1100, 8, 8, 128, BF16)):
+        r = rng(B)
+        c = attention_case(B, Hq, Hkv, D, 16, r.integers(0, 4, B), r.integers(0, 120, B) * (r.random(B) > 0.1).astype(int), dtype, B)
+        for window, sinks in ((0, 0), (20, 2)):
+            check_attention(c, sb.paged_attention(**c, max_q=max_q, max_kv=120, window=window, sinks=sinks), window, sinks)
+
+
+@pytest.mark.parametrize("max_q", [1, 1000])
+def test_attention_windows_of_any_size(gpu, max_q):
+    """Up to 2^31 - 1, also for queries before the first cached token."""
+    c = attention_case(4, 8, 2, 64, 16, [5, 1, 40, 3], [2, 300, 17, 0], BF16, 14)
+    want = sb.paged_attention(**c, max_q=max_q, max_kv=300)
+    check_attention(c, want)
+    for window in (301, 10 ** 9, 2 ** 31 - 40, 2 ** 31 - 2, 2 ** 31 - 1):
+        for sinks in (0, 3, 2 ** 31 - 1):
+            got = sb.paged_attention(**c, max_q=max_q, max_kv=300, window=window, sinks=sinks)
+            assert torch.equal(got, want), (window, sinks)
+    got = sb.paged_attention(**c, max_q=max_q, max_kv=300, window=1, sinks=2 ** 31 - 1)
+    check_attention(c, got, 1, 2 ** 31 - 1)
+
+
 @pytest.mark.parametrize("max_q", [1, 1000])
 def test_attention_empty_rows(gpu, max_q):
     """Requests without queries or tokens, queries before the first position,
@@ -418,6 +466,41 @@ def test_sample_ties(gpu, V):
         check_sample(z, u, top_p=np.arange(16) / 14)
         check_sample(z, u, top_k=np.full(16, V // 2 + 1), top_p=np.arange(16) / 14)
         check_sample(z, u, T=np.full(16, math.log2(math.e)), min_p=np.arange(16) / 14)
+
+
+@pytest.mark.parametrize("dtype,V", [(F32, 3000), (BF16, 3000), (F32, 9000), (F16, 40000)])
+def test_sample_kept_numbers(gpu, dtype, V):
+    """top-k around the sizes at which lists are handled another way, without and
+    with equal logits across the cut."""
+    k = [1, 2, 63, 64, 65, 127, 128, 129, 130, 255, 400, 511, 512, 513, 514, 700]
+    r = rng(V)
+    z = 2 * r.standard_normal((16, V))
+    u = r.random(16)
+    for x in (z, np.round(2 * z) / 2):
+        check_sample(x, u, top_k=k, dtype=dtype)
+        check_sample(x, u, T=np.full(16, 1.5), top_k=k, top_p=np.linspace(0.2, 1, 16), dtype=dtype)
+        check_sample(x, u, T=np.linspace(0.3, 3, 16), min_p=np.geomspace(1, 1e-3, 16), dtype=dtype)
+
+
+def test_sample_captured_with_a_workspace(gpu):
+    """Many wide rows captured once; replayed with other logits and filters."""
+    r = rng(21)
+    rows, V = 40, 20011
+    z, u, top_p = (torch.zeros(s, device="cuda") for s in ((rows, V), (rows,), (rows,)))
+    top_k = i32([0] * rows)
+    graph = torch.cuda.CUDAGraph()
+    sb.sample_tokens(z, u, top_k=top_k, top_p=top_p)
+    with torch.cuda.graph(graph):
+        tok, lp = sb.sample_tokens(z, u, top_k=top_k, top_p=top_p)
+    for t in range(6):
+        z.copy_(torch.as_tensor(r.standard_normal((rows, V)) * (1 + t)))
+        u.copy_(torch.as_tensor(r.random(rows)))
+        top_p.copy_(torch.as_tensor(r.random(rows)))
+        top_k.copy_(torch.as_tensor(np.where(np.arange(rows) % (t + 2), 0, 40)))
+        graph.replay()
+        want = sb.sample_tokens(z, u, top_k=top_k, top_p=top_p)
+        assert torch.equal(tok, want[0]) and torch.equal(lp, want[1]), t
+        torch.cuda.synchronize()
 
 
 def test_sample_flat_and_wide(gpu):
@@ -664,6 +747,8 @@ def test_python_refusals(gpu):
         sb.paged_attention(**c, **kw, out=c["q"][:1].expand(2, 4, 64))
     with pytest.raises(ValueError, match="backward"):
         sb.paged_attention(**dict(c, q=c["q"].clone().requires_grad_()), **kw)
+    with pytest.raises(ValueError, match="argument"):
+        sb.paged_attention(**c, **dict(kw, max_kv=2 ** 31))
     for over in (dict(window=-1), dict(max_kv=-1), dict(scale=math.nan)):
         with pytest.raises(sb.decoder.N.StreambeamError):
             sb.paged_attention(**c, **dict(kw, **over))
