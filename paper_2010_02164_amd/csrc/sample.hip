@@ -57,7 +57,9 @@ constexpr int CHUNKS_MAX = SB_SAMPLE_MAX_VOCAB / CHUNK;
 constexpr int SAMPLED_K = 1536;
 // 16-byte pieces a thread loads at once: of the sample, and of a pass (4 there
 // made the code of the passes larger than the instruction cache).
-constexpr int SAMPLE = 4, PASS = 2;
+constexpr int SAMPLE = 4, PASS = 2, LOOK = 4;
+constexpr int QUEUE = SAMPLE;   // pieces of a thread that its list takes after the pass
+static_assert(SM_THREADS * QUEUE * 2 <= BINS * 8 && SB_SAMPLE_MAX_VOCAB / 4 <= 1 << 16, "the pieces' numbers fit the bins' place");
 
 // The bits of z in an order that ascends with it; NaN counts as -inf.
 __device__ __forceinline__ uint32_t order_bits(float z) {
@@ -850,6 +852,13 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
   // The pass over the row: its largest logit, its smallest finite one, and
   // the tokens from the bound on.
   float zm = -INFINITY, zl = INFINITY;
+  uint16_t *mine = reinterpret_cast<uint16_t *>(sh.hist) + tid * QUEUE;   // pieces of this thread with such tokens: listed
+  int queued = 0;                                                         // behind the pass, which waits for nothing so
+  auto list_piece = [&](const float (&z)[VEC], int i0) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if (z[e] >= bound && z[e] > -INFINITY) list_token(order_bits(z[e]), i0 + e, sh);
+  };
   auto look = [&](const float (&z)[VEC], int i0) {
     float m = z[0];
 #pragma unroll
@@ -857,9 +866,8 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
     zm = fmaxf(zm, m);
     if (sampled) {
       if (m >= bound && m > -INFINITY) {
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          if (z[e] >= bound && z[e] > -INFINITY) list_token(order_bits(z[e]), i0 + e, sh);
+        if (queued < QUEUE) mine[queued++] = (uint16_t)((i0 - row.head) / VEC);
+        else list_piece(z, i0);
       }
     } else {
 #pragma unroll
@@ -877,8 +885,42 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
   }
   if (apart > SM_THREADS)
 #pragma unroll 1
-    for (int b = 0; b < SAMPLE; ++b) row.template each_piece<PASS>(b * apart + SM_THREADS + tid, min((b + 1) * apart, row.pieces), SM_THREADS, look);
-  row.each_end(look);
+    for (int b = 0; b < SAMPLE; ++b) row.template each_piece<LOOK>(b * apart + SM_THREADS + tid, min((b + 1) * apart, row.pieces), SM_THREADS, look);
+  if (sampled) {
+#pragma unroll
+    for (int b = 0; b < QUEUE; ++b)
+      if (b < queued) x[b] = row.piece(mine[b]);
+    int hits = 0;
+#pragma unroll
+    for (int b = 0; b < QUEUE; ++b) {
+      if (b >= queued) break;
+      float z[VEC];
+      Row<DT>::unpack(x[b], z);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) hits += z[e] >= bound && z[e] > -INFINITY;
+    }
+    int at = hits ? atomicAdd(&sh.n, hits) : 0;
+#pragma unroll
+    for (int b = 0; b < QUEUE; ++b) {
+      if (b >= queued) break;
+      float z[VEC];
+      Row<DT>::unpack(x[b], z);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (z[e] >= bound && z[e] > -INFINITY) {
+          if (at < LIST_MAX) {
+            sh.key[at] = order_bits(z[e]);
+            sh.idx[at] = row.head + mine[b] * VEC + e;
+          }
+          ++at;
+        }
+    }
+  }
+  row.each_end([&](const float (&z)[VEC], int i) {
+    zm = fmaxf(zm, z[0]);
+    if (sampled) list_piece(z, i);
+    else zl = fminf(zl, z[0] > -INFINITY ? z[0] : INFINITY);
+  });
   const uint32_t best = block_max(order_bits(zm), sh);
   if (best == LOWEST) {
     if (tid == 0) {
