@@ -20,6 +20,7 @@
 // k_attn_many: 128 rows a workgroup (prompts), 64 keys at a time in LDS; bound
 // by the matrix products and the exponentials between them.
 #include <algorithm>
+#include <cmath>
 
 #include "serve.h"
 
@@ -804,33 +805,57 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : 2) void k_attn_many(sb_a
           u2{Half<DT>::pack(o[x][e] * inv, o[x][e + 1] * inv), Half<DT>::pack(o[x][e + 2] * inv, o[x][e + 3] * inv)};
 }
 
-// Prompts go to k_attn_many, which keeps 128 rows on its keys; a few rows
-// would leave most of its products empty.
-bool many(const sb_attention_args &a) { return (long long)a.max_q * (a.q_heads / a.kv_heads) > 3 * FEW_ROWS; }
+// Rows of each request, and workgroups of k_attn_few (16 rows) and k_attn_many
+// (128), that the bounds allow.
+struct Load {
+  long long G, keys, few, many;
+  Load(const sb_attention_args &a) : G(a.q_heads / a.kv_heads) {
+    const long long rows = std::max(a.max_q, 1) * G, all = a.n_tokens * G;
+    keys = std::max(a.max_kv, 1);
+    if (a.window > 0) keys = std::min(keys, (long long)a.window + a.sinks + a.max_q);
+    few = std::min(all / FEW_ROWS + a.n_requests, (rows + FEW_ROWS - 1) / FEW_ROWS * a.n_requests);
+    many = std::min(all / MANY_ROWS + a.n_requests, (rows + MANY_ROWS - 1) / MANY_ROWS * a.n_requests);
+  }
+};
+
+// k_attn_many reads keys once for 128 rows, but gives a request's rows to one
+// workgroup each; k_attn_few spreads their keys over the card, 16 rows at a time.
+// Up to 16 rows it is always taken, else by what both took (8 heads of 128; in
+// ns): 6000 and 0.083 for each key of each 16 rows, and 34 for each key as often
+// as the workgroups of 128 rows go round the units. 16 requests over 3000 keys:
+// 32 rows 74 against 103 us, 48 rows 103 and 103, 64 rows 131 and 103; one
+// request, 64 rows over 8000 keys: 39 and 243; 64 requests, 32 rows over 1000
+// keys: 88 and 62.
+bool many(const sb_attention_args &a, int n_cu) {
+  const Load l(a);
+  if (std::max(a.max_q, 1) * l.G <= FEW_ROWS) return false;
+  const double keys = (double)l.keys, rounds = std::ceil((double)l.many * a.kv_heads / n_cu);
+  return 6000.0 + 0.083 * l.few * a.kv_heads * keys > 34.0 * rounds * keys;
+}
 
 // How k_attn_few's workgroups share the work: as many per head as the units
-// hold at once, fewer where the keys that a query may be expected to see (the
-// window, or max_kv) give no wave a tile. Requests enough to fill the units
-// SHARE_BELOW times over balance themselves, a workgroup each.
+// hold at once, fewer where the keys that a query may be expected to see give no
+// wave a tile. Requests enough to fill the units SHARE_BELOW times over balance
+// themselves, a workgroup each (8 heads of 128; 128 requests of 200 to 6000
+// tokens: shared 203 us, not shared 252; 260 of 200 to 4000: 274 and 280; 300 of
+// 100 to 1000: 123 and 103; 2000 of 20 to 300: 309 and 266).
 constexpr int SHARE_BELOW = 4;
 Shares shares(const sb_attention_args &a, int n_cu) {
-  if (many(a)) return {0, 0};
-  const long long G = a.q_heads / a.kv_heads, places = (long long)few_groups(a.head_dim) * n_cu;
-  if ((long long)a.n_requests * a.kv_heads >= SHARE_BELOW * places) return {0, 0};
-  const long long units = std::min(((long long)a.n_tokens * G + FEW_ROWS - 1) / FEW_ROWS + a.n_requests,
-                                   (std::max(a.max_q, 1) * G + FEW_ROWS - 1) / FEW_ROWS * a.n_requests);
-  const long long seen = a.window > 0 ? std::min((long long)a.max_kv, (long long)a.window + a.sinks + a.max_q) : a.max_kv;
-  const long long tiles = ((seen + FEW_KEYS - 1) / FEW_KEYS + 1) * units;
-  return {(int)std::max(1LL, std::min((places + a.kv_heads - 1) / a.kv_heads, (tiles + AT_WAVES - 1) / AT_WAVES)), (int)units};
+  const Load l(a);
+  const long long places = (long long)few_groups(a.head_dim) * n_cu;
+  if (many(a, n_cu) || (long long)a.n_requests * a.kv_heads >= SHARE_BELOW * places) return {0, 0};
+  const long long tiles = ((l.keys + FEW_KEYS - 1) / FEW_KEYS + 1) * l.few;
+  return {(int)std::max(1LL, std::min((places + a.kv_heads - 1) / a.kv_heads, (tiles + AT_WAVES - 1) / AT_WAVES)), (int)l.few};
 }
 
 template <int DT, int D>
-hipError_t launch(const sb_attention_args &a, const Shares &sh, void *work, hipStream_t s) {
-  if (many(a)) {
+hipError_t launch(const sb_attention_args &a, int n_cu, void *work, hipStream_t s) {
+  if (many(a, n_cu)) {
     const long long gx = (long long)a.n_tokens * (a.q_heads / a.kv_heads) / MANY_ROWS + a.n_requests;
     hipLaunchKernelGGL((k_attn_many<DT, D>), dim3((unsigned)(gx * a.kv_heads)), dim3(AT_THREADS), 0, s, a);
     return hipGetLastError();
   }
+  const Shares sh = shares(a, n_cu);
   hipLaunchKernelGGL((k_attn_few<DT, D>), dim3(sh.groups ? sh.groups : a.n_requests, a.kv_heads), dim3(AT_THREADS), 0, s, a, sh.groups, sh.units,
                      work);
   const hipError_t e = hipGetLastError();
@@ -844,15 +869,14 @@ hipError_t launch(const sb_attention_args &a, const Shares &sh, void *work, hipS
 int64_t attention_workspace(const sb_attention_args &a, int n_cu) { return (int64_t)shares(a, n_cu).bytes(a); }
 
 hipError_t launch_paged_attention(const sb_attention_args &a, int n_cu, void *work, hipStream_t s) {
-  const Shares sh = shares(a, n_cu);
   if (a.dtype == SB_BF16) {
-    if (a.head_dim == 64) return launch<SB_BF16, 64>(a, sh, work, s);
-    if (a.head_dim == 128) return launch<SB_BF16, 128>(a, sh, work, s);
-    return launch<SB_BF16, 256>(a, sh, work, s);
+    if (a.head_dim == 64) return launch<SB_BF16, 64>(a, n_cu, work, s);
+    if (a.head_dim == 128) return launch<SB_BF16, 128>(a, n_cu, work, s);
+    return launch<SB_BF16, 256>(a, n_cu, work, s);
   }
-  if (a.head_dim == 64) return launch<SB_F16, 64>(a, sh, work, s);
-  if (a.head_dim == 128) return launch<SB_F16, 128>(a, sh, work, s);
-  return launch<SB_F16, 256>(a, sh, work, s);
+  if (a.head_dim == 64) return launch<SB_F16, 64>(a, n_cu, work, s);
+  if (a.head_dim == 128) return launch<SB_F16, 128>(a, n_cu, work, s);
+  return launch<SB_F16, 256>(a, n_cu, work, s);
 }
 
 }  // namespace sb
