@@ -440,8 +440,9 @@ typedef struct {
   int32_t reserved;         /* 0                                                    */
 } sb_sample_args;
 #define SB_SAMPLE_MAX_VOCAB 262144
-/* Bytes of workspace that sb_sample_tokens is faster with (pointers are not
- * looked at); 0 where none helps, -1 if the sizes are invalid. */
+/* Bytes of workspace that sb_sample_tokens is faster with (of the arrays only
+ * whether they are NULL is looked at); 0 where none helps, -1 if the sizes are
+ * invalid. */
 int64_t sb_sample_workspace(const sb_sample_args *args);
 /* workspace: 256-byte aligned, at least sb_sample_workspace bytes, or NULL:
  * every row is then left to one workgroup, with the same result. Calls that may

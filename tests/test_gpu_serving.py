@@ -245,6 +245,12 @@ def bounds(c, max_q=None, max_kv=None):
     return dict(max_q=int(q) if max_q is None else max_q, max_kv=int(c["lens"].max()) if max_kv is None else max_kv)
 
 
+def kv_bound(max_q, max_kv):
+    """With a large max_q a bound of 1 token takes the kernel for prompts, and
+    max_kv may take either."""
+    return 1 if max_q == 1000 else max_kv
+
+
 def check_attention(c, got, window=0, sinks=0, scale=None, only=None):
     """only: queries to look at (the oracle runs on those requests' rows)."""
     D = got.shape[2]
@@ -273,6 +279,10 @@ def test_attention(gpu, form, dtype, D):
     for window, sinks in ((0, 0), (17, 0), (17, 4), (1, 0), (1, 100), (64, 33)):
         got = sb.paged_attention(**c, **bounds(c), window=window, sinks=sinks)
         check_attention(c, got, window, sinks)
+        if form < 2 or form > 5:   # by the other kernel: of prompts, or of single tokens
+            for max_q, max_kv in ((1000, 1), (0, 1)):
+                got = sb.paged_attention(**c, max_q=max_q, max_kv=max_kv, window=window, sinks=sinks)
+                check_attention(c, got, window, sinks)
 
 
 @pytest.mark.parametrize("dtype,D,Hq,Hkv", [(BF16, 128, 4, 1), (F16, 64, 8, 1), (BF16, 256, 2, 1)])
@@ -280,8 +290,9 @@ def test_attention_long_cache_in_parts(gpu, dtype, D, Hq, Hkv):
     """Caches long enough to be split over workgroups, short ones beside."""
     c = attention_case(3, Hq, Hkv, D, 16, [1, 2, 1], [6000, 9, 2500], dtype, 5)
     for window, sinks in ((0, 0), (2000, 5)):
-        got = sb.paged_attention(**c, **bounds(c), window=window, sinks=sinks)
-        check_attention(c, got, window, sinks)
+        for over in ({}, dict(max_q=1000, max_kv=1)):
+            got = sb.paged_attention(**c, **bounds(c, **over), window=window, sinks=sinks)
+            check_attention(c, got, window, sinks)
 
 
 def test_attention_wrong_bounds_only_cost_time(gpu):
@@ -301,20 +312,20 @@ def test_attention_of_many_requests(gpu, max_q):
         r = rng(B)
         c = attention_case(B, Hq, Hkv, D, 16, r.integers(0, 4, B), r.integers(0, 120, B) * (r.random(B) > 0.1).astype(int), dtype, B)
         for window, sinks in ((0, 0), (20, 2)):
-            check_attention(c, sb.paged_attention(**c, max_q=max_q, max_kv=120, window=window, sinks=sinks), window, sinks)
+            check_attention(c, sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 120), window=window, sinks=sinks), window, sinks)
 
 
 @pytest.mark.parametrize("max_q", [1, 1000])
 def test_attention_windows_of_any_size(gpu, max_q):
     """Up to 2^31 - 1, also for queries before the first cached token."""
     c = attention_case(4, 8, 2, 64, 16, [5, 1, 40, 3], [2, 300, 17, 0], BF16, 14)
-    want = sb.paged_attention(**c, max_q=max_q, max_kv=300)
+    want = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 300))
     check_attention(c, want)
     for window in (301, 10 ** 9, 2 ** 31 - 40, 2 ** 31 - 2, 2 ** 31 - 1):
         for sinks in (0, 3, 2 ** 31 - 1):
-            got = sb.paged_attention(**c, max_q=max_q, max_kv=300, window=window, sinks=sinks)
+            got = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 300), window=window, sinks=sinks)
             assert torch.equal(got, want), (window, sinks)
-    got = sb.paged_attention(**c, max_q=max_q, max_kv=300, window=1, sinks=2 ** 31 - 1)
+    got = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 300), window=1, sinks=2 ** 31 - 1)
     check_attention(c, got, 1, 2 ** 31 - 1)
 
 
@@ -324,13 +335,13 @@ def test_attention_empty_rows(gpu, max_q):
     rows behind the last request."""
     c = attention_case(6, 4, 2, 64, 8, [0, 2, 1, 0, 5, 1], [9, 2, 0, 0, 3, 6], BF16, 7, pad=4)
     out = dev(np.full(c["q"].shape, 3.0), BF16)
-    assert sb.paged_attention(**c, max_q=max_q, max_kv=9, out=out) is out
+    assert sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 9), out=out) is out
     check_attention(c, out)
     assert bool((out[2] == 0).all()) and bool((out[3:5] == 0).all())   # of a request of 0 tokens; positions -2 and -1
     assert bool((out[-4:] == 3).all())
     out.fill_(3)
     nobody = dict(c, q_start=i32([0] * 7))
-    sb.paged_attention(**nobody, max_q=max_q, max_kv=9, out=out)
+    sb.paged_attention(**nobody, max_q=max_q, max_kv=kv_bound(max_q, 9), out=out)
     assert bool((out == 3).all())
 
 
@@ -339,11 +350,11 @@ def test_attention_pages_outside_the_cache_are_skipped(gpu, max_q):
     c = attention_case(3, 4, 2, 128, 4, [2, 1, 1], [30, 21, 8], BF16, 8)
     c["table"][0, 3], c["table"][0, 5], c["table"][1, 0] = 10 ** 6, -9, 2 ** 31 - 1
     c["table"][2, :2] = -1
-    got = sb.paged_attention(**c, max_q=max_q, max_kv=30)
+    got = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 30))
     check_attention(c, got)
     assert bool((got[3] == 0).all())
     c["lens"][1] = 2 ** 31 - 1   # longer than its table row: cut there, whose places behind are -1
-    got = sb.paged_attention(**c, max_q=max_q, max_kv=30)
+    got = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 30))
     assert bool(torch.isfinite(got).all())
 
 
@@ -353,7 +364,7 @@ def test_attention_what_is_hidden_does_not_matter(gpu, max_q, dtype):
     window, and at positions that other rows of the tile do see."""
     for q, kv, window, sinks in (([1], [50, 77], 20, 3), ([6, 3], [50, 77], 9, 2), ([6, 3], [50, 77], 0, 0)):
         c = attention_case(2, 4, 1, 64, 16, q, kv, dtype, 9)
-        clean = sb.paged_attention(**c, max_q=max_q, max_kv=77, window=window, sinks=sinks)
+        clean = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 77), window=window, sinks=sinks)
         used = torch.zeros(c["k_cache"].shape[:2], dtype=torch.bool, device="cuda")
         m = c["q_start"][1:] - c["q_start"][:-1]
         for b, n in enumerate(kv):
@@ -363,15 +374,15 @@ def test_attention_what_is_hidden_does_not_matter(gpu, max_q, dtype):
         for bad in (math.nan, math.inf, -math.inf):
             c["k_cache"][~used] = bad
             c["v_cache"][~used] = bad
-            assert torch.equal(sb.paged_attention(**c, max_q=max_q, max_kv=77, window=window, sinks=sinks), clean)
+            assert torch.equal(sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 77), window=window, sinks=sinks), clean)
         if q[0] > 1:   # the last position is seen by the last query alone
             at = int(c["table"][0, 49 // 16]), 49 % 16
             c["k_cache"][at], c["v_cache"][at] = 0.0, math.nan
-            got = sb.paged_attention(**c, max_q=max_q, max_kv=77, window=window, sinks=sinks)
+            got = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 77), window=window, sinks=sinks)
             assert torch.equal(got[:5], clean[:5]) and bool(got[5].isnan().all()) and torch.equal(got[6:], clean[6:])
             c["v_cache"][at] = math.inf
             c["k_cache"][at] = math.nan
-            got = sb.paged_attention(**c, max_q=max_q, max_kv=77, window=window, sinks=sinks)
+            got = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 77), window=window, sinks=sinks)
             assert torch.equal(got[:5], clean[:5]) and bool(got[5].isnan().all()) and torch.equal(got[6:], clean[6:])
 
 
@@ -381,7 +392,7 @@ def test_attention_large_scores(gpu, max_q):
     own, also negative and zero."""
     c = attention_case(2, 4, 2, 128, 16, [9, 1], [300, 140], BF16, 10, spread=60.0)
     for scale in (None, -0.02, 0.0):
-        got = sb.paged_attention(**c, max_q=max_q, max_kv=300, scale=scale)
+        got = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 300), scale=scale)
         check_attention(c, got, scale=scale)
 
 
@@ -390,7 +401,7 @@ def test_attention_strides(gpu, max_q):
     """q a slice of a wider projection, caches with heads before tokens in one
     allocation, a table that is part of a wider one, out into a slice."""
     c = attention_case(3, 6, 2, 64, 8, [4, 1, 2], [20, 33, 2], F16, 11)
-    want = sb.paged_attention(**c, max_q=max_q, max_kv=33, window=9, sinks=1)
+    want = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 33), window=9, sinks=1)
     T, P = c["q"].shape[0], c["k_cache"].shape[0]
     wide = torch.randn(T, 10, 64, device="cuda").half()
     wide[:, 2:8] = c["q"]
@@ -400,7 +411,7 @@ def test_attention_strides(gpu, max_q):
     tab[:, :-5] = c["table"]
     out = torch.zeros(6, T, 72, dtype=F16, device="cuda")
     got = sb.paged_attention(wide[:, 2:8], pool[:, 0].transpose(1, 2), pool[:, 1].transpose(1, 2), tab[:, :-5], c["lens"], c["q_start"],
-                             max_q=max_q, max_kv=33, window=9, sinks=1, out=out[:, :, :64].transpose(0, 1))
+                             max_q=max_q, max_kv=kv_bound(max_q, 33), window=9, sinks=1, out=out[:, :, :64].transpose(0, 1))
     assert torch.equal(got, want) and bool((out[:, :, 64:] == 0).all())
 
 
@@ -411,11 +422,11 @@ def test_attention_offsets_beyond_32_bits(gpu):
     k, v = (torch.zeros(n_pages, page, Hkv, D, dtype=BF16, device="cuda") for _ in range(2))
     c = attention_case(1, 16, Hkv, D, page, [1], [150], BF16, 12)
     for max_q in (1, 1000):
-        want = sb.paged_attention(**c, max_q=max_q, max_kv=150)
+        want = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 150))
         tail = n_pages - c["k_cache"].shape[0]
         k[tail:], v[tail:] = c["k_cache"], c["v_cache"]
         got = sb.paged_attention(c["q"], k, v, torch.where(c["table"] >= 0, c["table"] + tail, -1), c["lens"], c["q_start"],
-                                 max_q=max_q, max_kv=150)
+                                 max_q=max_q, max_kv=kv_bound(max_q, 150))
         assert torch.equal(got, want)
 
 
@@ -485,7 +496,7 @@ def test_sample_kept_numbers(gpu, dtype, V):
 def test_sample_captured_with_a_workspace(gpu):
     """Many wide rows captured once; replayed with other logits and filters."""
     r = rng(21)
-    rows, V = 40, 20011
+    rows, V = 40, 50021
     z, u, top_p = (torch.zeros(s, device="cuda") for s in ((rows, V), (rows,), (rows,)))
     top_k = i32([0] * rows)
     graph = torch.cuda.CUDAGraph()
@@ -514,7 +525,8 @@ def test_sample_flat_and_wide(gpu):
     check_sample(z, u, T=np.full(12, 100.0))
 
 
-@pytest.mark.parametrize("dtype,V", [(F32, 16385), (F32, 40003), (BF16, 50000), (F16, 131072), (BF16, 262144)])
+@pytest.mark.parametrize("dtype,V", [(F32, 16385), (F32, 40003), (F32, 50001), (BF16, 50000), (F16, 131072), (BF16, 262144),
+                                     (F32, 262144)])
 def test_sample_rows_by_kernels_of_their_own(gpu, dtype, V):
     """Many wide rows, for whose passes the call brings a workspace: as the
     oracle says (some rows), and every row as without it."""
@@ -529,6 +541,7 @@ def test_sample_rows_by_kernels_of_their_own(gpu, dtype, V):
     z[9] = np.where(np.arange(V) % 7 == 0, z[9], -np.inf)
     z[10, [3, V - 1]] = np.inf
     z[11, ::2] = np.nan
+    z[13] = np.where(np.arange(V) < 5000, 2.0 + 1e-4 * r.random(V), -1.0)   # more in one place than a list takes
     u, T = r.random(rows), 0.4 + r.random(rows)
     u[:4] = 0.0, 1.0, 0.5, 1 - 2.0 ** -24
     T[12::9] = 0
@@ -541,7 +554,9 @@ def test_sample_rows_by_kernels_of_their_own(gpu, dtype, V):
         left = {n: x for n, x in kw.items() if n not in leave}
         tok, lp = sb.sample_tokens(zd, **left)
         for a in range(0, rows, 9):
-            t, q = sb.sample_tokens(zd[a:a + 9], **{n: x[a:a + 9].clone() for n, x in left.items()})
+            few = {n: x[a:a + 9].clone() for n, x in left.items()}
+            few.setdefault("top_k", i32([0] * 9))   # (without any top-k these rows would have one, too)
+            t, q = sb.sample_tokens(zd[a:a + 9], **few)
             assert torch.equal(t, tok[a:a + 9]) and torch.equal(q, lp[a:a + 9]), (leave, a)
         if V < 60000:
             for j in range(0, rows, 5):
@@ -549,6 +564,8 @@ def test_sample_rows_by_kernels_of_their_own(gpu, dtype, V):
                                      int(k[j]) if "top_k" in left else 0, float(np.float32(p[j])) if "top_p" in left else 1.0,
                                      float(np.float32(mp[j])) if "min_p" in left else 0.0)
                 assert int(tok[j]) == want[0], (leave, j)
+                one = sb.sample_tokens(zd[j:j + 1], **{n: x[j:j + 1].clone() for n, x in left.items()})
+                assert int(one[0]) == want[0] and float(one[1]) == float(lp[j])
                 assert float(lp[j]) == pytest.approx(want[1], rel=2.0 ** -22, abs=2.0 ** -36)
 
 
