@@ -18,7 +18,10 @@
 // tokens, 8 heads of 128 in bf16: 239 us, 5.05 TB/s (278 us where each request
 // was cut into the same number of parts; reading the same rows alone: 220 us).
 // k_attn_many: 128 rows a workgroup (prompts), 64 keys at a time in LDS; bound
-// by the matrix products and the exponentials between them.
+// by the matrix products and the exponentials between them: three prompts of 1500
+// to 4100 tokens over up to 8200, window 2048, 32 heads of 128: 400 us, 705
+// TFLOP/s (a library product of 8192^3: 1250), the matrix unit busy 32, the vector
+// unit 41, LDS 35 percent of the time.
 #include <algorithm>
 #include <cmath>
 
@@ -493,7 +496,8 @@ __global__ __launch_bounds__(AT_THREADS, few_groups(D)) void k_attn_few(sb_atten
   }
 }
 
-// A unit's rows, 16 threads each: the parts in order.
+// A unit's rows, 16 threads each: the parts in order. (5 us: a launch, and three
+// reads one after the other.)
 template <int DT, int D>
 __global__ __launch_bounds__(AT_THREADS) void k_attn_join(sb_attention_args a, int groups, int units, void *work) {
   constexpr int E = D / 16;

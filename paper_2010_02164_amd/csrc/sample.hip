@@ -3,7 +3,7 @@
 //
 // Every filter keeps a prefix of the tokens ranked by (-z, index), so the kept
 // tokens are those above one cut (a logit and, among its equals, an index),
-// and nothing is sorted: a radix search over the ordered bits of the logits
+// and no row is sorted: a radix search over the ordered bits of the logits
 // finds where a sum of counts (top-k) or of weights (top-p) passes its limit,
 // and the draw is the same search over the kept tokens' indexes.
 //
@@ -11,20 +11,22 @@
 // gives a bound that the k-th largest logit hardly ever is below, and the pass
 // over the row lists the tokens from that bound on; a list of fewer than k sends
 // the row the other way. min-p alone bounds the tokens by the sample's largest.
-// A list of up to 512 is sorted, where every filter keeps a prefix; a longer one
+// A short list is sorted, where every filter keeps a prefix; a longer one
 // (up to 4096) is searched in registers and LDS. A row of 32000 logits in fp32
 // takes 10.5 us, of which launching and reading it takes 6 (17.6 us where short
 // lists were searched, too). 512 threads: two rows share a unit, and 320 rows
-// run at once (1024 threads: 38 instead of 34 us).
+// run at once (1024 threads: 38 instead of 34 us; 29 since tokens are listed
+// behind the pass instead of within it).
 //
 // Rows without top-k but with top-p need every weight. A pass adds them up into
 // bins of equal ratio, which names the bin that the cut is in, a second lists
 // that bin, a third draws; they read caches, and are bound by the 22 fp64 and
 // integer operations of a weight. One workgroup took such a row 2 to 4 times as
 // long as the others; with a workspace the passes run as kernels of their own,
-// in chunks over all compute units. (Kernels: a row's last chunk taking the next
-// step in the same launch made 188 us into 1021, the fences between the XCDs'
-// caches costing more than launches.)
+// in chunks over all compute units: 512 rows of 128000 in fp32, part of them
+// with top-k, 57 us in k_sample, 32, 8, 19 and 18 in the others. (A row's last
+// chunk taking the next step in the same launch made 188 us into 1021: fences
+// between the XCDs' caches cost more than launches.)
 //
 // Weights are whole multiples of 2^-44 in 64-bit integers: up to 2^18 of them
 // add up without rounding or overflow, in any order, so that partial sums of
@@ -46,8 +48,12 @@ constexpr int SM_THREADS = 512;
 constexpr int SM_WAVES = SM_THREADS / 64;
 constexpr double ONE = 0x1p44;        // the weight of the largest logit
 constexpr int LIST_PER = 8, LIST_MAX = LIST_PER * SM_THREADS;
-constexpr int RANKED = SM_THREADS;   // a list up to this is sorted
-constexpr int DIRECT = 128;          // tokens left of it that are drawn from by comparing their indexes
+// Lists up to RANKED are sorted for top-p, up to half of it else (a row of 32000;
+// top-k 20, a list of about 80: 12.6 us, searched 14.0, with top-p 12.8 and 17.2; 100,
+// about 250: 16.1 and 15.5, with top-p 16.3 and 18.6; 200, 430: 19.5 and 16.3, 19.6
+// and 19.4). From up to DIRECT kept tokens the draw compares indexes (5 kept: 10.3
+// us, searched 11.2; 20: 12.6 and 12.6; 60: 16.6 and 14.3).
+constexpr int RANKED = SM_THREADS, DIRECT = 24;
 constexpr int BIN_BITS = 9, BINS = 1 << BIN_BITS;
 constexpr int TAB_BITS = 9;           // 2^x by a table of 2^(i / 512) and a cubic
 constexpr int TAB = 1 << TAB_BITS;
@@ -935,7 +941,7 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
   u64 total = 1;
   const int n = sh.n;
   const bool listed = sampled && (sure || n >= k);
-  if (listed && n <= RANKED) {
+  if (listed && n <= (p < 1.0f ? RANKED : RANKED / 2)) {
     token = draw_ranked(n, pr, weigh, V, total, sh);
   } else if (listed && n <= LIST_MAX) {
     Items it;

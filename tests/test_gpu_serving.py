@@ -483,7 +483,7 @@ def test_sample_ties(gpu, V):
 def test_sample_kept_numbers(gpu, dtype, V):
     """top-k around the sizes at which lists are handled another way, without and
     with equal logits across the cut."""
-    k = [1, 2, 63, 64, 65, 127, 128, 129, 130, 255, 400, 511, 512, 513, 514, 700]
+    k = [1, 23, 24, 25, 64, 127, 128, 129, 255, 256, 257, 400, 511, 512, 513, 700]
     r = rng(V)
     z = 2 * r.standard_normal((16, V))
     u = r.random(16)
