@@ -12,7 +12,6 @@
 // by bisection of q_start in LDS; more tokens go to a second, wide kernel. 1024
 // requests with a token each: 10.9 us; 37 with 300 to 2900: 9 and 3.
 #include "serve.h"
-#include "wave.h"
 
 namespace sb {
 namespace {

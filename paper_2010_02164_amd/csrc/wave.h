@@ -67,22 +67,4 @@ __device__ __forceinline__ void stage32(uint32_t x, uint32_t &a, uint32_t &b) {
   }
 }
 
-// Sums over the lanes up to each, through the lanes' own paths (a shuffle
-// through LDS takes about 130 cycles).
-template <int CTRL, int ROWS>
-__device__ __forceinline__ unsigned long long from_before(unsigned long long v) {   // 0 where nothing comes
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false);
-  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xF, false);
-  return ((unsigned long long)hi << 32) | lo;
-}
-__device__ __forceinline__ unsigned long long wave_scan(unsigned long long v) {   // inclusive
-  v += from_before<0x111, 0xF>(v);   // within 16 lanes: from 1, 2, 4, 8 before
-  v += from_before<0x112, 0xF>(v);
-  v += from_before<0x114, 0xF>(v);
-  v += from_before<0x118, 0xF>(v);
-  v += from_before<0x142, 0xA>(v);   // the last of the first and third 16 to the next
-  v += from_before<0x143, 0xC>(v);   // the last of the first 32 to the others
-  return v;
-}
-
 }  // namespace sb
