@@ -549,11 +549,13 @@ struct ManyShared {
                                       // finite, in a tile that not all rows see
 };
 
-// The workgroup's pass over its tiles: the lane's row's sums, and its keys'
-// share of the weights' sum. False where it stopped.
+// The workgroup's pass over `tiles` tiles from t_first on: the lane's row's sums,
+// what its exponentials are taken against, and its keys' share of the weights'
+// sum. False where it stopped.
 template <int DT, int D, bool CAREFUL>
 __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span &s, const int *table, const uint16_t *kc, const uint16_t *vc,
-                                          const u4 (&q)[D / 16], int p, bool real, ManyShared<D> &sh, f16v (&o)[D / 32], float &sum) {
+                                          const u4 (&q)[D / 16], int p, bool real, int t_first, int tiles, ManyShared<D> &sh,
+                                          f16v (&o)[D / 32], float &ref, float &sum) {
   constexpr int KSTR = ManyShared<D>::KSTR, VSTR = ManyShared<D>::VSTR;
   constexpr int PC = MANY_KEYS * (D / 8) / AT_THREADS;   // 16-byte pieces of K (and V) a thread brings,
   constexpr int RSTEP = AT_THREADS / (D / 8);            // their rows so far apart
@@ -569,7 +571,7 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
   // `ref`: what the exponentials are taken against, a score the row has had. It
   // moves to a larger one only when that would be over 2^GROW of it.
   constexpr float GROW = 8.0f;
-  float ref = -INFINITY;
+  ref = -INFINITY;
   sum = 0.0f;
 
   // A tile's way: its pages are looked up four tiles ahead, by one wave, a key
@@ -579,9 +581,9 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
   u4 kr[PC], vr[PC];
   int page = 0, place = 0;
   uint32_t gone = 0;   // bit x: piece x in the registers has no page
-  const int tiles = (s.n_vis + MANY_KEYS - 1) / MANY_KEYS, wave = threadIdx.x >> 6;
+  const int base_u = t_first * MANY_KEYS, wave = threadIdx.x >> 6;
   auto look_up = [&](int t) {
-    if (wave == (t & 3)) page = page_of(a, table, inv_page, s.key(min(t * MANY_KEYS + lane, s.n_vis - 1)), place);
+    if (wave == (t & 3)) page = page_of(a, table, inv_page, s.key(min(base_u + t * MANY_KEYS + lane, s.n_vis - 1)), place);
   };
   auto put_at = [&](int t) {
     if (wave == (t & 3))
@@ -598,7 +600,7 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
     }
   };
   auto write = [&](int t) {
-    const bool shared = s.all_see(a, s.key(t * MANY_KEYS), s.key(t * MANY_KEYS + MANY_KEYS - 1));
+    const bool shared = s.all_see(a, s.key(base_u + t * MANY_KEYS), s.key(base_u + t * MANY_KEYS + MANY_KEYS - 1));
     const int to = t & 1;
     bool bad = false;
     if (gone) {
@@ -639,7 +641,7 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
   }
   for (int t = 0; t < tiles; ++t) {
     __syncthreads();   // tile t is there, the places of tile t + 2 are, and the other buffer has been read
-    const int odd = sh.odd[t & 1], u0 = t * MANY_KEYS;
+    const int odd = sh.odd[t & 1], u0 = base_u + t * MANY_KEYS;
     if (!CAREFUL && (odd & 2)) return false;
     if (t + 1 < tiles) {
       write(t + 1);
@@ -756,28 +758,38 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
   return true;
 }
 
-template <int DT, int D>
-__global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : 2) void k_attn_many(sb_attention_args a) {
-  constexpr int KS = D / 16, DB = D / 32;
-  __shared__ ManyShared<D> sh;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, h2 = lane >> 5;
-  // Heads side by side: workgroups go to the 8 XCDs in turn, so that tiles of
-  // one head, which read the same keys, share an L2.
-  const int G = a.q_heads / a.kv_heads, hk = (int)(blockIdx.x % a.kv_heads);
-  // The request of this tile: request b's tiles start at q_start[b] G / 128 + b,
-  // which leaves at least one place a tile; the last ones of some stay empty.
-  const int tile = (int)((gridDim.x - 1 - blockIdx.x) / a.kv_heads);   // (long prompts' last tiles first)
+// The rows of place `tile` of the grid: request b's tiles start at
+// q_start[b] G / 128 + b, which leaves at least one place a tile. Returns the
+// request, -1 where the place is empty.
+__device__ __forceinline__ int span_tile(const sb_attention_args &a, int tile, Span &s) {
+  const int G = a.q_heads / a.kv_heads;
   int b = 0, bh = a.n_requests;
   while (bh - b > 1) {
     const int mid = (b + bh) >> 1;
     if ((long long)a.q_start[mid] * G / MANY_ROWS + mid <= tile) b = mid;
     else bh = mid;
   }
-  Span s;
   span_request(a, b, s);
-  const int r0 = (int)(tile - ((long long)a.q_start[b] * G / MANY_ROWS + b)) * MANY_ROWS;
-  if (r0 < 0 || r0 >= s.rows) return;
-  span_rows(a, r0, MANY_ROWS, s);
+  const long long r0 = (tile - ((long long)a.q_start[b] * G / MANY_ROWS + b)) * MANY_ROWS;
+  if (r0 < 0 || r0 >= s.rows) return -1;
+  span_rows(a, (int)r0, MANY_ROWS, s);
+  return b;
+}
+
+// Few long prompts leave units without work: their keys are then split, too, and
+// the parts [grid place][key/value head][128][D] added up by k_attn_many_join.
+template <int DT, int D>
+__global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : 2) void k_attn_many(sb_attention_args a, int splits, void *work) {
+  constexpr int KS = D / 16, DB = D / 32;
+  __shared__ ManyShared<D> sh;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, h2 = lane >> 5;
+  // Heads side by side: workgroups go to the 8 XCDs in turn, so that tiles of
+  // one head, which read the same keys, share an L2.
+  const int G = a.q_heads / a.kv_heads, hk = (int)(blockIdx.x % a.kv_heads);
+  const int part = (int)((gridDim.x - 1 - blockIdx.x) / a.kv_heads);   // (long prompts' last tiles first)
+  Span s;
+  const int b = span_tile(a, part / splits, s), r0 = s.r0;
+  if (b < 0) return;
   const int *table = a.table + b * a.table_stride;
   const uint16_t *kc = static_cast<const uint16_t *>(a.k_cache) + hk * a.kc_head;
   const uint16_t *vc = static_cast<const uint16_t *>(a.v_cache) + hk * a.vc_head;
@@ -794,11 +806,25 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : 2) void k_attn_many(sb_a
     q[x] = real && a.scale != 0.0f ? *reinterpret_cast<const u4 *>(src + 16 * x + 8 * h2) ^ q_sign : u4{0, 0, 0, 0};
   }
   f16v o[DB];
-  float sum;
-  if (!many_keys<DT, D, false>(a, s, table, kc, vc, q, p, real, sh, o, sum))
-    many_keys<DT, D, true>(a, s, table, kc, vc, q, p, real, sh, o, sum);
+  float ref, sum;
+  const int tiles = (s.n_vis + MANY_KEYS - 1) / MANY_KEYS, each = (tiles + splits - 1) / splits;
+  const int t0 = min(part % splits * each, tiles), count = min(each, tiles - t0);
+  if (!many_keys<DT, D, false>(a, s, table, kc, vc, q, p, real, t0, count, sh, o, ref, sum))
+    many_keys<DT, D, true>(a, s, table, kc, vc, q, p, real, t0, count, sh, o, ref, sum);
   sum += __shfl_xor(sum, 32, 64);
   if (!real) return;
+  if (splits > 1) {
+    const long long at = (long long)part * a.kv_heads + hk;
+    float *sums = static_cast<float *>(work) + (at * MANY_ROWS + 32 * w + l32) * D;
+    float2 *stats = reinterpret_cast<float2 *>(static_cast<float *>(work) + (long long)gridDim.x * MANY_ROWS * D);
+    const float c = a.scale == 0.0f ? 1.0f : (float)(fabs((double)a.scale) * LOG2E);
+    if (h2 == 0) stats[at * MANY_ROWS + 32 * w + l32] = make_float2(ref == -INFINITY ? -INFINITY : ref * c, sum);
+#pragma unroll
+    for (int x = 0; x < DB; ++x)
+#pragma unroll
+      for (int e = 0; e < 16; e += 4) *reinterpret_cast<f4 *>(sums + 32 * x + 2 * e + 4 * h2) = f4{o[x][e], o[x][e + 1], o[x][e + 2], o[x][e + 3]};
+    return;
+  }
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   uint16_t *dst = static_cast<uint16_t *>(a.out) + (s.q0 + i) * a.out_token + (hk * G + row - i * G) * a.out_head;
 #pragma unroll
@@ -809,16 +835,65 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : 2) void k_attn_many(sb_a
           u2{Half<DT>::pack(o[x][e] * inv, o[x][e + 1] * inv), Half<DT>::pack(o[x][e + 2] * inv, o[x][e + 3] * inv)};
 }
 
+// 16 rows of a tile, 16 threads each: the parts in order.
+template <int DT, int D>
+__global__ __launch_bounds__(AT_THREADS) void k_attn_many_join(sb_attention_args a, int splits, const void *work) {
+  constexpr int E = D / 16;
+  const int tile = blockIdx.x, hk = blockIdx.y, rr = blockIdx.z * 16 + (threadIdx.x >> 4), col = (threadIdx.x & 15) * E;
+  Span s;
+  const int b = span_tile(a, tile, s);
+  if (b < 0) return;
+  const int G = a.q_heads / a.kv_heads, row = s.r0 + rr, qi = row / G;
+  if (row >= s.rows) return;
+  const long long parts = (long long)gridDim.x * splits * a.kv_heads, at = (long long)tile * splits * a.kv_heads + hk;
+  const float *sums = static_cast<const float *>(work) + (at * MANY_ROWS + rr) * D + col;
+  const float2 *stats = reinterpret_cast<const float2 *>(static_cast<const float *>(work) + parts * MANY_ROWS * D) + at * MANY_ROWS + rr;
+  const long long step = (long long)a.kv_heads * MANY_ROWS;
+  float mx = -INFINITY;
+  for (int x = 0; x < splits; ++x) mx = fmaxf(mx, stats[x * step].x);
+  const float base = mx == -INFINITY ? 0.0f : mx;
+  float acc[E], sum = 0.0f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+#pragma unroll 4
+  for (int x = 0; x < splits; ++x) {
+    const float2 st = stats[x * step];
+    const float f = __builtin_amdgcn_exp2f(st.x - base);
+    sum += f * st.y;
+#pragma unroll
+    for (int e = 0; e < E; e += 4) {
+      const f4 v = *reinterpret_cast<const f4 *>(sums + x * step * D + e);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) acc[e + y] += f * v[y];
+    }
+  }
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+  uint16_t *dst = static_cast<uint16_t *>(a.out) + (s.q0 + qi) * a.out_token + (hk * G + row - qi * G) * a.out_head + col;
+#pragma unroll
+  for (int e = 0; e < E; e += 4)
+    *reinterpret_cast<u2 *>(dst + e) = u2{Half<DT>::pack(acc[e] * inv, acc[e + 1] * inv), Half<DT>::pack(acc[e + 2] * inv, acc[e + 3] * inv)};
+}
+
 // Rows of each request, and workgroups of k_attn_few (16 rows) and k_attn_many
 // (128), that the bounds allow.
+constexpr int SPLIT_TILES = 8;
 struct Load {
-  long long G, keys, few, many;
-  Load(const sb_attention_args &a) : G(a.q_heads / a.kv_heads) {
+  long long G, keys, few, many, grid;   // grid: places of k_attn_many for each head
+  int splits;                           // parts that it splits the keys into
+  Load(const sb_attention_args &a, int n_cu) : G(a.q_heads / a.kv_heads) {
     const long long rows = std::max(a.max_q, 1) * G, all = a.n_tokens * G;
     keys = std::max(a.max_kv, 1);
     if (a.window > 0) keys = std::min(keys, (long long)a.window + a.sinks + a.max_q);
     few = std::min(all / FEW_ROWS + a.n_requests, (rows + FEW_ROWS - 1) / FEW_ROWS * a.n_requests);
     many = std::min(all / MANY_ROWS + a.n_requests, (rows + MANY_ROWS - 1) / MANY_ROWS * a.n_requests);
+    grid = all / MANY_ROWS + a.n_requests;
+    // As many as fill the units, of SPLIT_TILES tiles at least; the parts of up to
+    // twice as many places (some may be empty) have room.
+    const long long places = (a.head_dim == 256 ? 1 : 2) * (long long)n_cu;
+    splits = (int)std::max(1LL, std::min({places / (many * a.kv_heads), 2 * places / (grid * a.kv_heads), keys / (SPLIT_TILES * MANY_KEYS)}));
+  }
+  size_t parts_bytes(const sb_attention_args &a) const {
+    return splits == 1 ? 0 : (size_t)grid * a.kv_heads * splits * MANY_ROWS * (a.head_dim + 2) * 4;
   }
 };
 
@@ -830,11 +905,10 @@ struct Load {
 // 32 rows 74 against 103 us, 48 rows 103 and 103, 64 rows 131 and 103; one
 // request, 64 rows over 8000 keys: 39 and 243; 64 requests, 32 rows over 1000
 // keys: 88 and 62.
-bool many(const sb_attention_args &a, int n_cu) {
-  const Load l(a);
+bool many(const sb_attention_args &a, const Load &l, int n_cu) {
   if (std::max(a.max_q, 1) * l.G <= FEW_ROWS) return false;
   const double keys = (double)l.keys, rounds = std::ceil((double)l.many * a.kv_heads / n_cu);
-  return 6000.0 + 0.083 * l.few * a.kv_heads * keys > 34.0 * rounds * keys;
+  return 6000.0 + 0.083 * l.few * a.kv_heads * keys > 34.0 * rounds * keys / l.splits + (l.splits > 1 ? 6000.0 : 0.0);
 }
 
 // How k_attn_few's workgroups share the work: as many per head as the units
@@ -844,22 +918,24 @@ bool many(const sb_attention_args &a, int n_cu) {
 // tokens: shared 203 us, not shared 252; 260 of 200 to 4000: 274 and 280; 300 of
 // 100 to 1000: 123 and 103; 2000 of 20 to 300: 309 and 266).
 constexpr int SHARE_BELOW = 4;
-Shares shares(const sb_attention_args &a, int n_cu) {
-  const Load l(a);
+Shares shares(const sb_attention_args &a, const Load &l, int n_cu) {
   const long long places = (long long)few_groups(a.head_dim) * n_cu;
-  if (many(a, n_cu) || (long long)a.n_requests * a.kv_heads >= SHARE_BELOW * places) return {0, 0};
+  if ((long long)a.n_requests * a.kv_heads >= SHARE_BELOW * places) return {0, 0};
   const long long tiles = ((l.keys + FEW_KEYS - 1) / FEW_KEYS + 1) * l.few;
   return {(int)std::max(1LL, std::min((places + a.kv_heads - 1) / a.kv_heads, (tiles + AT_WAVES - 1) / AT_WAVES)), (int)l.few};
 }
 
 template <int DT, int D>
 hipError_t launch(const sb_attention_args &a, int n_cu, void *work, hipStream_t s) {
-  if (many(a, n_cu)) {
-    const long long gx = (long long)a.n_tokens * (a.q_heads / a.kv_heads) / MANY_ROWS + a.n_requests;
-    hipLaunchKernelGGL((k_attn_many<DT, D>), dim3((unsigned)(gx * a.kv_heads)), dim3(AT_THREADS), 0, s, a);
+  const Load l(a, n_cu);
+  if (many(a, l, n_cu)) {
+    hipLaunchKernelGGL((k_attn_many<DT, D>), dim3((unsigned)(l.grid * a.kv_heads * l.splits)), dim3(AT_THREADS), 0, s, a, l.splits, work);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || l.splits == 1) return e;
+    hipLaunchKernelGGL((k_attn_many_join<DT, D>), dim3((unsigned)l.grid, a.kv_heads, MANY_ROWS / 16), dim3(AT_THREADS), 0, s, a, l.splits, work);
     return hipGetLastError();
   }
-  const Shares sh = shares(a, n_cu);
+  const Shares sh = shares(a, l, n_cu);
   hipLaunchKernelGGL((k_attn_few<DT, D>), dim3(sh.groups ? sh.groups : a.n_requests, a.kv_heads), dim3(AT_THREADS), 0, s, a, sh.groups, sh.units,
                      work);
   const hipError_t e = hipGetLastError();
@@ -870,7 +946,10 @@ hipError_t launch(const sb_attention_args &a, int n_cu, void *work, hipStream_t 
 
 }  // namespace
 
-int64_t attention_workspace(const sb_attention_args &a, int n_cu) { return (int64_t)shares(a, n_cu).bytes(a); }
+int64_t attention_workspace(const sb_attention_args &a, int n_cu) {
+  const Load l(a, n_cu);
+  return (int64_t)(many(a, l, n_cu) ? l.parts_bytes(a) : shares(a, l, n_cu).bytes(a));
+}
 
 hipError_t launch_paged_attention(const sb_attention_args &a, int n_cu, void *work, hipStream_t s) {
   if (a.dtype == SB_BF16) {

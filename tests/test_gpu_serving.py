@@ -315,6 +315,35 @@ def test_attention_of_many_requests(gpu, max_q):
             check_attention(c, sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 120), window=window, sinks=sinks), window, sinks)
 
 
+@pytest.mark.parametrize("dtype,D,Hq,Hkv,page,q,kv", [
+    (BF16, 128, 8, 2, 16, [200], [5000]), (F16, 64, 6, 1, 32, [150, 1, 333], [2600, 900, 4000]), (BF16, 256, 4, 2, 64, [100, 260], [3000, 2000]),
+    (F16, 128, 32, 8, 16, [64], [4100])])
+def test_attention_prompts_with_split_keys(gpu, dtype, D, Hq, Hkv, page, q, kv):
+    """Few long prompts, whose keys are split over workgroups: with windows, pages
+    that are none, values that are not finite behind the last key, and rows
+    behind the last request."""
+    c = attention_case(len(q), Hq, Hkv, D, page, q, kv, dtype, D + len(q), pad=5)
+    kw = bounds(c)
+    for window, sinks in ((0, 0), (1500, 3), (40, 0)):
+        check_attention(c, sb.paged_attention(**c, **kw, window=window, sinks=sinks), window, sinks)
+    out = dev(np.full(c["q"].shape, 3.0), dtype)
+    clean = sb.paged_attention(**c, **kw)
+    last = int(c["lens"][0]) - 1   # a key that the first request's last query alone sees
+    at = int(c["table"][0, last // page]), last % page
+    held = c["v_cache"][at].clone()
+    c["v_cache"][at] = math.nan
+    sb.paged_attention(**c, **kw, out=out)
+    first, rows = int(c["q_start"][1]) - 1, int(c["q_start"][-1])
+    assert torch.equal(out[:first], clean[:first]) and bool(out[first].isnan().all()) and bool((out[rows:] == 3).all())
+    c["v_cache"][at] = held
+    c["table"][0, 20], c["table"][0, 33] = -1, 10 ** 6
+    check_attention(c, sb.paged_attention(**c, **kw))
+    c["lens"][0] = 3   # fewer tokens than queries: those before the first see nothing
+    got = sb.paged_attention(**c, **kw)
+    check_attention(c, got)
+    assert bool((got[:int(c["q_start"][1]) - 3] == 0).all())
+
+
 @pytest.mark.parametrize("max_q", [1, 1000])
 def test_attention_windows_of_any_size(gpu, max_q):
     """Up to 2^31 - 1, also for queries before the first cached token."""
