@@ -17,7 +17,8 @@
 // of those that more than one had a share in. 64 requests of 200 to 9000
 // tokens, 8 heads of 128 in bf16: 239 us, 5.05 TB/s (278 us where each request
 // was cut into the same number of parts; reading the same rows alone: 220 us).
-// k_attn_many: 128 rows a workgroup (prompts), 64 keys at a time in LDS; bound
+// k_attn_many: 128 rows a workgroup (prompts), 64 keys at a time in LDS, the keys
+// of few prompts split over workgroups (k_attn_many_join); bound
 // by the matrix products and the exponentials between them: three prompts of 1500
 // to 4100 tokens over up to 8200, window 2048, 32 heads of 128: 400 us, 705
 // TFLOP/s (a library product of 8192^3: 1250), the matrix unit busy 32, the vector
@@ -874,42 +875,35 @@ __global__ __launch_bounds__(AT_THREADS) void k_attn_many_join(sb_attention_args
     *reinterpret_cast<u2 *>(dst + e) = u2{Half<DT>::pack(acc[e] * inv, acc[e + 1] * inv), Half<DT>::pack(acc[e + 2] * inv, acc[e + 3] * inv)};
 }
 
-// Rows of each request, and workgroups of k_attn_few (16 rows) and k_attn_many
-// (128), that the bounds allow.
+// The work that the bounds allow. Keys: that a query sees. Units of 16 rows; tiles
+// of 128 rows, and places for them in the grid, for each key/value head.
+// k_attn_many splits keys into as many parts as fill the units, of SPLIT_TILES
+// tiles at least (8 heads of 128, 4 query heads each; one prompt of 512 tokens
+// over 8000: 109 us, in one piece 250; over 1000: 37 and 38; 2048 over 8000, which
+// fill the units: 301 and 301).
 constexpr int SPLIT_TILES = 8;
 struct Load {
-  long long G, keys, few, many, grid;   // grid: places of k_attn_many for each head
-  int splits;                           // parts that it splits the keys into
+  long long G, keys, units, tiles, grid;
+  int splits;
   Load(const sb_attention_args &a, int n_cu) : G(a.q_heads / a.kv_heads) {
     const long long rows = std::max(a.max_q, 1) * G, all = a.n_tokens * G;
     keys = std::max(a.max_kv, 1);
     if (a.window > 0) keys = std::min(keys, (long long)a.window + a.sinks + a.max_q);
-    few = std::min(all / FEW_ROWS + a.n_requests, (rows + FEW_ROWS - 1) / FEW_ROWS * a.n_requests);
-    many = std::min(all / MANY_ROWS + a.n_requests, (rows + MANY_ROWS - 1) / MANY_ROWS * a.n_requests);
+    units = std::min(all / FEW_ROWS + a.n_requests, (rows + FEW_ROWS - 1) / FEW_ROWS * a.n_requests);
+    tiles = std::min(all / MANY_ROWS + a.n_requests, (rows + MANY_ROWS - 1) / MANY_ROWS * a.n_requests);
     grid = all / MANY_ROWS + a.n_requests;
-    // As many as fill the units, of SPLIT_TILES tiles at least; the parts of up to
-    // twice as many places (some may be empty) have room.
-    const long long places = (a.head_dim == 256 ? 1 : 2) * (long long)n_cu;
-    splits = (int)std::max(1LL, std::min({places / (many * a.kv_heads), 2 * places / (grid * a.kv_heads), keys / (SPLIT_TILES * MANY_KEYS)}));
+    const long long room = (a.head_dim == 256 ? 1 : 2) * (long long)n_cu;   // workgroups that the units hold at once
+    splits = (int)std::max(1LL, std::min({room / (tiles * a.kv_heads), 2 * room / (grid * a.kv_heads), keys / (SPLIT_TILES * MANY_KEYS)}));
   }
   size_t parts_bytes(const sb_attention_args &a) const {
     return splits == 1 ? 0 : (size_t)grid * a.kv_heads * splits * MANY_ROWS * (a.head_dim + 2) * 4;
   }
 };
 
-// k_attn_many reads keys once for 128 rows, but gives a request's rows to one
-// workgroup each; k_attn_few spreads their keys over the card, 16 rows at a time.
-// Up to 16 rows it is always taken, else by what both took (8 heads of 128; in
-// ns): 6000 and 0.083 for each key of each 16 rows, and 34 for each key as often
-// as the workgroups of 128 rows go round the units. 16 requests over 3000 keys:
-// 32 rows 74 against 103 us, 48 rows 103 and 103, 64 rows 131 and 103; one
-// request, 64 rows over 8000 keys: 39 and 243; 64 requests, 32 rows over 1000
-// keys: 88 and 62.
-bool many(const sb_attention_args &a, const Load &l, int n_cu) {
-  if (std::max(a.max_q, 1) * l.G <= FEW_ROWS) return false;
-  const double keys = (double)l.keys, rounds = std::ceil((double)l.many * a.kv_heads / n_cu);
-  return 6000.0 + 0.083 * l.few * a.kv_heads * keys > 34.0 * rounds * keys / l.splits + (l.splits > 1 ? 6000.0 : 0.0);
-}
+// More than 16 rows of a request read its keys once in k_attn_many, in k_attn_few
+// every 16 of them again (16 requests over 3000 keys, 32 rows: 49 and 75 us, 64
+// rows: 53 and 133; one request over 8000 keys, 32 rows: 32 and 36).
+bool many(const sb_attention_args &a) { return std::max(a.max_q, 1) * (long long)(a.q_heads / a.kv_heads) > FEW_ROWS; }
 
 // How k_attn_few's workgroups share the work: as many per head as the units
 // hold at once, fewer where the keys that a query may be expected to see give no
@@ -921,14 +915,14 @@ constexpr int SHARE_BELOW = 4;
 Shares shares(const sb_attention_args &a, const Load &l, int n_cu) {
   const long long places = (long long)few_groups(a.head_dim) * n_cu;
   if ((long long)a.n_requests * a.kv_heads >= SHARE_BELOW * places) return {0, 0};
-  const long long tiles = ((l.keys + FEW_KEYS - 1) / FEW_KEYS + 1) * l.few;
-  return {(int)std::max(1LL, std::min((places + a.kv_heads - 1) / a.kv_heads, (tiles + AT_WAVES - 1) / AT_WAVES)), (int)l.few};
+  const long long tiles = ((l.keys + FEW_KEYS - 1) / FEW_KEYS + 1) * l.units;
+  return {(int)std::max(1LL, std::min((places + a.kv_heads - 1) / a.kv_heads, (tiles + AT_WAVES - 1) / AT_WAVES)), (int)l.units};
 }
 
 template <int DT, int D>
 hipError_t launch(const sb_attention_args &a, int n_cu, void *work, hipStream_t s) {
   const Load l(a, n_cu);
-  if (many(a, l, n_cu)) {
+  if (many(a)) {
     hipLaunchKernelGGL((k_attn_many<DT, D>), dim3((unsigned)(l.grid * a.kv_heads * l.splits)), dim3(AT_THREADS), 0, s, a, l.splits, work);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || l.splits == 1) return e;
@@ -948,7 +942,7 @@ hipError_t launch(const sb_attention_args &a, int n_cu, void *work, hipStream_t 
 
 int64_t attention_workspace(const sb_attention_args &a, int n_cu) {
   const Load l(a, n_cu);
-  return (int64_t)(many(a, l, n_cu) ? l.parts_bytes(a) : shares(a, l, n_cu).bytes(a));
+  return (int64_t)(many(a) ? l.parts_bytes(a) : shares(a, l, n_cu).bytes(a));
 }
 
 hipError_t launch_paged_attention(const sb_attention_args &a, int n_cu, void *work, hipStream_t s) {

@@ -246,8 +246,8 @@ def bounds(c, max_q=None, max_kv=None):
 
 
 def kv_bound(max_q, max_kv):
-    """With a large max_q a bound of 1 token takes the kernel for prompts, and
-    max_kv may take either."""
+    """The kernel for prompts, which a large max_q takes, splits no keys where
+    there may be 1."""
     return 1 if max_q == 1000 else max_kv
 
 
