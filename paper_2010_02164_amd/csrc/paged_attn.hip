@@ -497,12 +497,14 @@ __global__ __launch_bounds__(AT_THREADS, few_groups(D)) void k_attn_few(sb_atten
   }
 }
 
-// A unit's rows, 16 threads each: the parts in order. (5 us: a launch, and three
-// reads one after the other.)
+// A wave a row of the unit: every fourth part in each 16 lanes, in order, then the
+// four sums. (4 to 5 us, a launch and three reads one after the other; with all
+// parts in turn the 128 of one request of 16000 tokens took 15.)
 template <int DT, int D>
 __global__ __launch_bounds__(AT_THREADS) void k_attn_join(sb_attention_args a, int groups, int units, void *work) {
   constexpr int E = D / 16;
-  const int u = blockIdx.x, hk = blockIdx.y, rr = threadIdx.x >> 4, col = (threadIdx.x & 15) * E;
+  const int u = blockIdx.x, hk = blockIdx.y, lane = threadIdx.x & 63;
+  const int rr = blockIdx.z * AT_WAVES + (threadIdx.x >> 6), col = (lane & 15) * E, turn = lane >> 4;
   if (u >= *static_cast<const int *>(work)) return;
   const UnitInfo info = unit_infos(work)[u];
   if (info.count <= 1) return;
@@ -513,13 +515,16 @@ __global__ __launch_bounds__(AT_THREADS) void k_attn_join(sb_attention_args a, i
   const float2 *stats = part_stats<D>(a, work, groups, units, hk, info.first) + rr;
   const float *sums = part_sums<D>(a, work, groups, units, hk, info.first) + rr * D + col;
   float mx = -INFINITY;
-  for (int x = 0; x < info.count; ++x) mx = fmaxf(mx, stats[x * FEW_ROWS].x);
+#pragma unroll 4
+  for (int x = turn; x < info.count; x += 4) mx = fmaxf(mx, stats[x * FEW_ROWS].x);
+  mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+  mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
   const float base = mx == -INFINITY ? 0.0f : mx;
   float acc[E], sum = 0.0f;
 #pragma unroll
   for (int e = 0; e < E; ++e) acc[e] = 0.0f;
 #pragma unroll 4
-  for (int x = 0; x < info.count; ++x) {
+  for (int x = turn; x < info.count; x += 4) {
     const float2 st = stats[x * FEW_ROWS];
     const float f = __builtin_amdgcn_exp2f(st.x - base);
     sum += f * st.y;
@@ -530,6 +535,13 @@ __global__ __launch_bounds__(AT_THREADS) void k_attn_join(sb_attention_args a, i
       for (int y = 0; y < 4; ++y) acc[e + y] += f * v[y];
     }
   }
+#pragma unroll
+  for (int o = 16; o < 64; o <<= 1) {
+    sum += __shfl_xor(sum, o, 64);
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+  }
+  if (turn != 0) return;
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
   uint16_t *dst = static_cast<uint16_t *>(a.out) + (s.q0 + qi) * a.out_token + (hk * G + row - qi * G) * a.out_head + col;
 #pragma unroll
@@ -911,10 +923,13 @@ bool many(const sb_attention_args &a) { return std::max(a.max_q, 1) * (long long
 // themselves, a workgroup each (8 heads of 128; 128 requests of 200 to 6000
 // tokens: shared 203 us, not shared 252; 260 of 200 to 4000: 274 and 280; 300 of
 // 100 to 1000: 123 and 103; 2000 of 20 to 300: 309 and 266).
-constexpr int SHARE_BELOW = 4;
+// So do short caches: 500 tokens, 1 request of 4 heads: 12.9 and 12.0 us, 100 of
+// 8: 45 and 38; 1000 tokens, 1 of 4: 12.6 and 18.8, 8 of 8: 16 and 21.
+constexpr int SHARE_BELOW = 4, SHARE_KEYS = 512;
 Shares shares(const sb_attention_args &a, const Load &l, int n_cu) {
   const long long places = (long long)few_groups(a.head_dim) * n_cu;
   if ((long long)a.n_requests * a.kv_heads >= SHARE_BELOW * places) return {0, 0};
+  if (l.keys <= SHARE_KEYS) return {0, 0};
   const long long tiles = ((l.keys + FEW_KEYS - 1) / FEW_KEYS + 1) * l.units;
   return {(int)std::max(1LL, std::min((places + a.kv_heads - 1) / a.kv_heads, (tiles + AT_WAVES - 1) / AT_WAVES)), (int)l.units};
 }
@@ -934,7 +949,7 @@ hipError_t launch(const sb_attention_args &a, int n_cu, void *work, hipStream_t 
                      work);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || sh.groups <= 1) return e;
-  hipLaunchKernelGGL((k_attn_join<DT, D>), dim3(sh.units, a.kv_heads), dim3(AT_THREADS), 0, s, a, sh.groups, sh.units, work);
+  hipLaunchKernelGGL((k_attn_join<DT, D>), dim3(sh.units, a.kv_heads, FEW_ROWS / AT_WAVES), dim3(AT_THREADS), 0, s, a, sh.groups, sh.units, work);
   return hipGetLastError();
 }
 

@@ -143,7 +143,7 @@ def plan_pages(lens, add, free_list, n_free, table, *, page_size: int, token_cap
     _apart(table, "table")
     i32, i64 = torch.int32, torch.int64
     if out is None:
-        q_start, after, granted, left = torch.empty(3 * B + 2, dtype=i32, device=i).split((B + 1, B, B, 1))
+        q_start, after, granted, left = torch.empty(3 * B + 2, dtype=i32, device=i).split_with_sizes((B + 1, B, B, 1))
         out = PagePlan(q_start, after, granted, torch.empty(cap, dtype=i64, device=i), torch.empty(cap, dtype=i32, device=i), left)
         at = q_start.data_ptr()
         to = at + 4 * (B + 1), at + 4 * (3 * B + 1), at, at + 4 * (2 * B + 1), out.slots.data_ptr(), out.positions.data_ptr()
