@@ -246,9 +246,9 @@ def bounds(c, max_q=None, max_kv=None):
 
 
 def kv_bound(max_q, max_kv):
-    """The kernel for prompts, which a large max_q takes, splits no keys where
-    there may be 1."""
-    return 1 if max_q == 1000 else max_kv
+    """A bound with which the kernel for prompts, which a large max_q takes, splits
+    no keys, and workgroups of the other one share them."""
+    return 1 if max_q == 1000 else max(max_kv, 5000)
 
 
 def check_attention(c, got, window=0, sinks=0, scale=None, only=None):
@@ -280,9 +280,11 @@ def test_attention(gpu, form, dtype, D):
         got = sb.paged_attention(**c, **bounds(c), window=window, sinks=sinks)
         check_attention(c, got, window, sinks)
         if form < 2 or form > 5:   # by the other kernel: of prompts, or of single tokens
-            for max_q, max_kv in ((1000, 1), (0, 1)):
+            for max_q, max_kv in ((1000, 1), (0, 1), (0, 5000)):
                 got = sb.paged_attention(**c, max_q=max_q, max_kv=max_kv, window=window, sinks=sinks)
                 check_attention(c, got, window, sinks)
+        got = sb.paged_attention(**c, **bounds(c, max_kv=5000), window=window, sinks=sinks)   # (shared, or split)
+        check_attention(c, got, window, sinks)
 
 
 @pytest.mark.parametrize("dtype,D,Hq,Hkv", [(BF16, 128, 4, 1), (F16, 64, 8, 1), (BF16, 256, 2, 1)])
@@ -348,12 +350,15 @@ def test_attention_prompts_with_split_keys(gpu, dtype, D, Hq, Hkv, page, q, kv):
 def test_attention_windows_of_any_size(gpu, max_q):
     """Up to 2^31 - 1, also for queries before the first cached token."""
     c = attention_case(4, 8, 2, 64, 16, [5, 1, 40, 3], [2, 300, 17, 0], BF16, 14)
-    want = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 300))
-    check_attention(c, want)
-    for window in (301, 10 ** 9, 2 ** 31 - 40, 2 ** 31 - 2, 2 ** 31 - 1):
-        for sinks in (0, 3, 2 ** 31 - 1):
-            got = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 300), window=window, sinks=sinks)
-            assert torch.equal(got, want), (window, sinks)
+    for max_kv in (1, 300, 5000):
+        want = sb.paged_attention(**c, max_q=max_q, max_kv=max_kv)
+        check_attention(c, want)
+        for window in (301, 10 ** 9, 2 ** 31 - 40, 2 ** 31 - 2, 2 ** 31 - 1):
+            for sinks in (0, 3, 2 ** 31 - 1):
+                got = sb.paged_attention(**c, max_q=max_q, max_kv=max_kv, window=window, sinks=sinks)
+                if window > 301:   # (that one may bring another split)
+                    assert torch.equal(got, want), (window, sinks)
+                check_attention(c, got)
     got = sb.paged_attention(**c, max_q=max_q, max_kv=kv_bound(max_q, 300), window=1, sinks=2 ** 31 - 1)
     check_attention(c, got, 1, 2 ** 31 - 1)
 
