@@ -20,7 +20,7 @@
 // k_attn_many: 128 rows a workgroup (prompts), 64 keys at a time in LDS, the keys
 // of few prompts split over workgroups (k_attn_many_join); bound
 // by the matrix products and the exponentials between them: three prompts of 1500
-// to 4100 tokens over up to 8200, window 2048, 32 heads of 128: 400 us, 705
+// to 4100 tokens over up to 8200, window 2048, 32 heads of 128: 391 us, 722
 // TFLOP/s (a library product of 8192^3: 1250), the matrix unit busy 32, the vector
 // unit 41, LDS 35 percent of the time.
 #include <algorithm>

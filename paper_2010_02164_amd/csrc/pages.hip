@@ -10,7 +10,7 @@
 // of few tokens has its slots written by the same workgroup: where each request
 // has one new token by the request's thread, else each token finds its request
 // by bisection of q_start in LDS; more tokens go to a second, wide kernel. 1024
-// requests with a token each: 10.9 us; 37 with 300 to 2900: 9 and 3.
+// requests with a token each: 11 us; 37 with 300 to 2900: 6 and 3.
 #include "serve.h"
 
 namespace sb {
