@@ -1259,10 +1259,11 @@ hipError_t launch(const sb_sample_args &a, void *workspace, int n_cu, hipStream_
 // where one workgroup would pass over a long row three times while others have
 // nothing left to do. Rows of which a part has top-k, without and with them:
 // 320 of 32000 logits 52 and 68 us, 64 of 64000 79 and 63, 512 of 64000 99 and
-// 96, 512 of 128000 195 and 138. Of a few rows most have top-k, unless there is
-// none at all: one row with top-p, 32000: 45 and 40, 128000: 140 and 50.
+// 96, 512 of 128000 195 and 138. One row of 128000 with top-p: 140 and 50, with
+// top-k, too, 20 and 27: of a few rows, which may all have top-k, only those of
+// calls with top-p bring it.
 int64_t sample_workspace(const sb_sample_args &a) {
-  if (a.vocab <= 3 * CHUNK || a.rows < 1 || (a.rows < 16 && (a.top_k || !a.top_p))) return 0;
+  if (a.vocab <= 3 * CHUNK || a.rows < 1 || (a.rows < 16 && !a.top_p)) return 0;
   return a.rows * (int64_t)(sizeof(WideRow) + (size_t)chunks_of(a.vocab) * BINS * 8);
 }
 

@@ -112,13 +112,13 @@ def test_sample_refusals(native_lib, over, status):
 
 
 def test_sample_workspace(native_lib):
-    """Only many wide rows, or some with top-p and no top-k, are faster with one;
-    one that is too small is refused."""
+    """Only many wide rows, or some with top-p, are faster with one; one that is
+    too small is refused."""
     def ask(**over):
         return native_lib.sb_sample_workspace(N.SAMPLE_ARGS.pack(*dict(SAMPLE, **over).values()))
     wide = dict(rows=64, vocab=64000, row_stride=64000)
-    assert ask() == 0 and ask(**dict(wide, rows=1)) == 0 and ask(**dict(wide, rows=0)) == 0 and ask(**dict(wide, vocab=32000)) == 0
-    assert ask(**dict(wide, rows=1, top_k=0)) > 0 and ask(**dict(wide, rows=1, top_k=0, top_p=0)) == 0
+    assert ask() == 0 and ask(**dict(wide, rows=0)) == 0 and ask(**dict(wide, vocab=32000)) == 0
+    assert ask(**dict(wide, rows=1)) > 0 and ask(**dict(wide, rows=1, top_p=0)) == 0
     need = ask(**wide)
     assert 0 < need and ask(**dict(wide, rows=128)) == 2 * need and ask(dtype=9) == -1
     args = N.SAMPLE_ARGS.pack(*dict(SAMPLE, **wide).values())
