@@ -120,6 +120,16 @@ __device__ __forceinline__ u4 not_zero(const u4 &x) {
   return y;
 }
 
+// Weights go into the second product in the cache's type, as multiples of
+// 2^-raise of the largest (the sums likewise, so that it cancels): fp16 has
+// nothing between 0 and 2^-24, and 100000 keys of 2^-25 each total 0.003 of one
+// large one. `most`: how far above 1 (as a power of 2) a weight may be; the
+// largest stays below fp16's 65504. bf16 has fp32's exponents.
+template <int DT>
+constexpr float raise(int most) {
+  return DT == SB_F16 ? 15.0f - most : 0.0f;
+}
+
 // The rows and keys of one workgroup's pass. The keys its rows see are the
 // first `ns` of the request and those from `lo` on, n_vis in all.
 struct Span {
@@ -262,8 +272,8 @@ __device__ __forceinline__ bool few_keys(const sb_attention_args &a, const Span 
     for (int x = 1; x < 8; ++x) tm = fmaxf(tm, e[x]);
     tm = fmaxf(tm, __shfl_xor(tm, 16, 64));
     tm = fmaxf(tm, __shfl_xor(tm, 32, 64));
-    const float mn = fmaxf(mx, tm), base = mn == -INFINITY ? 0.0f : mn;
-    const float shrink = __builtin_amdgcn_exp2f(mx - base);
+    const float mn = fmaxf(mx, tm), top = mn == -INFINITY ? 0.0f : mn, base = top - raise<DT>(0);
+    const float shrink = __builtin_amdgcn_exp2f(mx - top);
     mx = mn;
     float ts = 0.0f;
 #pragma unroll
@@ -583,7 +593,7 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
     for (int e = 0; e < 16; ++e) o[x][e] = 0.0f;
   // `ref`: what the exponentials are taken against, a score the row has had. It
   // moves to a larger one only when that would be over 2^GROW of it.
-  constexpr float GROW = 8.0f;
+  constexpr int GROW = 8;
   ref = -INFINITY;
   sum = 0.0f;
 
@@ -720,7 +730,7 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
 #pragma unroll
       for (int x = 0; x < DB; ++x) o[x] *= shrink;
     }
-    const float base = ref == -INFINITY ? 0.0f : ref * c;
+    const float base = ref == -INFINITY ? 0.0f : fmaf(ref, c, -raise<DT>(GROW));
     float ts[2] = {0.0f, 0.0f};
     u4 pk[4];
 #pragma unroll

@@ -430,6 +430,25 @@ def test_attention_large_scores(gpu, max_q):
         check_attention(c, got, scale=scale)
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("max_q", [1, 1000])
+def test_attention_many_small_weights(gpu, max_q, dtype):
+    """Very many keys of weights around fp16's smallest number (2^-24 of the
+    largest one's) next to a large one, which comes first, last, or in between:
+    together they are 0.002 to 0.004 of it."""
+    n, D = 100_000, 64
+    far = [24.4, 24.9, 25.1, 25.6]   # powers of two below the large one's
+    for at in (0, n // 2, n - 1):
+        c = attention_case(1, 4, 1, D, 128, [1], [n], dtype, 15)
+        c["q"].zero_(), c["k_cache"].zero_()
+        for h, x in enumerate(far):
+            c["q"][0, h, h] = x / 4 * math.log(2)   # in halves: rounded to the type, which both sides take
+        c["k_cache"][int(c["table"][0, at // 128]), at % 128, 0, :4] = 4.0
+        c["v_cache"] += 1.0
+        for max_kv in (1, n):
+            check_attention(c, sb.paged_attention(**c, max_q=max_q, max_kv=max_kv, scale=1.0), scale=1.0)
+
+
 @pytest.mark.parametrize("max_q", [1, 1000])
 def test_attention_strides(gpu, max_q):
     """q a slice of a wider projection, caches with heads before tokens in one
