@@ -375,8 +375,10 @@ sb_status sb_rope_append(const sb_rope_args *args, void *stream);
  * h / (q_heads / kv_heads). A query with p < 0 gets 0; so does one whose keys all
  * lie in pages outside the cache, which are skipped. Rows of out behind
  * q_start[n_requests] stay as they were. fp32 scores, statistics and sums; the
- * weights are rounded to the cache's type for the product with the values (fp16:
- * to 2^-12 of themselves, or 2^-32 of the row's largest where that is more). Keys
+ * weights go into the product with the values in two parts of the cache's type (off
+ * by 2^-16 of themselves in bf16, 2^-22 in fp16), or, where max_q queries times
+ * q_heads / kv_heads are more than 16, rounded to it once (2^-8; in fp16 2^-11, or
+ * 2^-32 of the row's largest where that is more). Keys
  * and values that a query does not see have no influence on it, whatever stands
  * there; a NaN or infinite value that it does see can make its result NaN.
  * max_q and max_kv (upper bounds of a request's queries and of lens) choose the

@@ -449,6 +449,28 @@ def test_attention_many_small_weights(gpu, max_q, dtype):
             check_attention(c, sb.paged_attention(**c, max_q=max_q, max_kv=max_kv, scale=1.0), scale=1.0)
 
 
+@pytest.mark.parametrize("dtype,D", [(BF16, 64), (BF16, 128), (BF16, 256), (F16, 64), (F16, 128), (F16, 256)])
+@pytest.mark.parametrize("n", [2, 700, 6000])
+def test_attention_weights_in_two_parts(gpu, n, dtype, D):
+    """Up to 16 rows a request: a weight is off by (eps / 2)^2 of itself. Every
+    other key is a little less likely and its value the negative one, so that
+    weights rounded once would show (their errors add up, the values do not)."""
+    c = attention_case(1, 16, 1, D, 16, [1], [n], dtype, n)
+    c["q"].zero_(), c["k_cache"].zero_()
+    c["q"][0, :, 0] = torch.linspace(0.005, 0.4, 16, device="cuda")
+    for j in range(n):
+        at = int(c["table"][0, j // 16]), j % 16
+        c["v_cache"][at] = 1.0 if j % 2 else -1.0
+        c["k_cache"][at][0, 0] = -float(j % 2)
+    eps = torch.finfo(dtype).eps
+    want, size, big = oracle.attention(f64(c["q"]), f64(c["k_cache"]), f64(c["v_cache"]), c["table"].tolist(), [n], [0, 1], 0, 0, 1.0)
+    score = big * (D * 2.0 ** -24 + 2.0 ** -22)
+    tol = eps / 2 * np.abs(want) + ((eps / 2) ** 2 + 2 * score + 2.0 ** -20) * size
+    for max_kv in (1, 10000):
+        d = np.abs(f64(sb.paged_attention(**c, max_q=1, max_kv=max_kv, scale=1.0)) - want)
+        assert np.all(d <= tol), np.max(d / tol)
+
+
 @pytest.mark.parametrize("max_q", [1, 1000])
 def test_attention_strides(gpu, max_q):
     """q a slice of a wider projection, caches with heads before tokens in one
