@@ -374,7 +374,8 @@ sb_status sb_rope_append(const sb_rope_args *args, void *stream);
  * j > p - window, or j < sinks (window 0: all). Query head h reads key/value head
  * h / (q_heads / kv_heads). A query with p < 0 gets 0; so does one whose keys all
  * lie in pages outside the cache, which are skipped. Rows of out behind
- * q_start[n_requests] stay as they were. fp32 scores, statistics and sums; the
+ * q_start[n_requests] stay as they were; q_start is clipped to 0 .. n_tokens, and
+ * a request whose start lies behind the next one's has no queries. fp32 scores, statistics and sums; the
  * weights go into the product with the values in two parts of the cache's type (off
  * by 2^-16 of themselves in bf16, 2^-22 in fp16), or, where max_q queries times
  * q_heads / kv_heads are more than 16, rounded to it once (2^-8; in fp16 2^-11, or

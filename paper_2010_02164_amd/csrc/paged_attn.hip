@@ -145,8 +145,10 @@ struct Span {
 };
 
 __device__ __forceinline__ void span_request(const sb_attention_args &a, int b, Span &s) {
-  s.q0 = max(a.q_start[b], 0);
-  s.m = min(a.q_start[b + 1], a.n_tokens) - s.q0;
+  // Starts outside q, or behind the next one, leave the request no rows. (A
+  // difference of unclipped ones, or G times a negative m, could pass 2^31.)
+  s.q0 = min(max(a.q_start[b], 0), a.n_tokens);
+  s.m = min(max(a.q_start[b + 1], s.q0), a.n_tokens) - s.q0;
   s.n = (int)min((long long)max(a.lens[b], 0), (long long)a.max_pages * a.page_size);
   s.rows = s.m * (a.q_heads / a.kv_heads);
 }

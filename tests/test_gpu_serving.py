@@ -392,6 +392,25 @@ def test_attention_pages_outside_the_cache_are_skipped(gpu, max_q):
     assert bool(torch.isfinite(got).all())
 
 
+@pytest.mark.parametrize("max_q", [1, 1000])
+@pytest.mark.parametrize("Hq", [2, 3, 6])
+def test_attention_wrong_starts_stay_in_bounds(gpu, max_q, Hq):
+    """Starts that are none: clipped to the rows there are, and a request that
+    starts behind the next has none. (m = -1.5e9 queries of 2 heads are 1.29e9
+    rows in 32 bits.)"""
+    c = attention_case(4, Hq, 1, 64, 8, [2, 0, 3, 0], [9, 5, 20, 7], BF16, 16, pad=3)
+    T, kw = 8, dict(max_q=max_q, max_kv=kv_bound(max_q, 20))
+    want = sb.paged_attention(**dict(c, q_start=i32([0, 2, 2, T, T])), **kw)
+    for last in (0, -5, -2 ** 31, 1_500_000_000):
+        for q_start in ([0, 2, 2, 1_500_000_000, last], [-7, 2, 2, 2 ** 31 - 1, last], [0, 2, 2, T, last]):
+            out = torch.full_like(want, 3.0)
+            sb.paged_attention(**dict(c, q_start=i32(q_start)), **kw, out=out)
+            assert torch.equal(out[2:], want[2:]) and (q_start[0] < 0 or torch.equal(out, want)), q_start
+    for q_start in ([-2 ** 31, -1, 2 ** 31 - 1, -2 ** 31, 5], [2 ** 31 - 1, 2 ** 31 - 2, -3, 2 ** 30, -2 ** 30]):
+        sb.paged_attention(**dict(c, q_start=i32(q_start)), **kw, out=torch.full_like(want, 3.0))
+    torch.cuda.synchronize()
+
+
 @pytest.mark.parametrize("max_q,dtype", [(1, BF16), (1000, BF16), (1000, F16)])
 def test_attention_what_is_hidden_does_not_matter(gpu, max_q, dtype):
     """NaN and infinities on pages of nobody, behind the last token, before the
