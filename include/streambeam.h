@@ -405,6 +405,7 @@ typedef struct {
   int32_t max_q, max_kv;    /* >= 0                                                 */
   float scale;
 } sb_attention_args;
+#define SB_ATTENTION_MAX_KEYS (INT32_MAX - 1023)   /* max_pages times page_size, at most */
 /* Bytes of workspace sb_paged_attention needs on the current device for these
  * sizes (pointers are not looked at); -1 if they are invalid. */
 int64_t sb_attention_workspace(const sb_attention_args *args);

@@ -58,6 +58,9 @@ sb_status check_attention(const sb_attention_args *a, const char *call, bool poi
             "n_pages, max_pages < 1 or page_size outside 1 .. 4096");
   REFUSE_IF((int64_t)a->n_pages * a->page_size > INT32_MAX || (int64_t)a->max_pages * a->page_size > INT32_MAX,
             SB_E_UNSUPPORTED, "n_pages or max_pages times page_size is not below 2^31");
+  // The kernels look a few tiles of keys behind a request's last one, in 32 bits.
+  REFUSE_IF((int64_t)a->max_pages * a->page_size > SB_ATTENTION_MAX_KEYS, SB_E_UNSUPPORTED,
+            "max_pages times page_size is above SB_ATTENTION_MAX_KEYS");
   REFUSE_IF((int64_t)a->n_tokens * a->q_heads > INT32_MAX, SB_E_UNSUPPORTED, "n_tokens times q_heads is not below 2^31");
   REFUSE_IF(a->window < 0 || a->sinks < 0 || a->max_q < 0 || a->max_kv < 0, SB_E_INVALID_ARG,
             "window, sinks, max_q or max_kv < 0");

@@ -111,6 +111,19 @@ def test_sample_refusals(native_lib, over, status):
     assert _refused(native_lib, "sb_sample_tokens", SAMPLE, over) == status
 
 
+def test_attention_keys_stay_below_32_bits(native_lib):
+    """Tiles of up to 64 keys are looked up four ahead of the last one, numbered in
+    32 bits: a table that ends within 320 keys of 2^31 cannot be taken."""
+    most = 2 ** 31 - 1024
+    for page, fits in ((1, most), (16, most // 16), (4096, most // 4096)):
+        for pages in (fits, fits + 1, (2 ** 31 - 1) // page):
+            status = N.SB_OK if pages * page <= most else UNSUPPORTED
+            over = dict(page_size=page, max_pages=pages, table_stride=pages, n_pages=8)
+            assert _refused(native_lib, "sb_paged_attention", ATTN, dict(over, n_tokens=0)) == status, over
+            if status != N.SB_OK and pages * page < 2 ** 31:
+                assert "MAX_KEYS" in native_lib.sb_last_error(None).decode()
+
+
 def test_sample_workspace(native_lib):
     """Only many wide rows, or some with top-p, are faster with one; one that is
     too small is refused."""
