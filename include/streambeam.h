@@ -424,10 +424,10 @@ sb_status sb_paged_attention(const sb_attention_args *args, void *workspace, siz
  * temperature <= 0 or NaN it is the largest logit, of equal ones the first.
  * logprobs: ln of the drawn token's share of the kept weights. Logits -inf and
  * NaN are never drawn; those of +inf share the draw evenly; a row with nothing
- * to draw gives token -1 and -inf. Weights are whole multiples of 2^-44 (of the
- * row's largest), summed as integers: the result does not depend on the order
- * of sums, and a token more than 44 powers of two below the largest is not
- * drawn. */
+ * to draw gives token -1 and -inf. Weights are taken as the nearest whole multiples
+ * of 2^-44 (of the row's largest), by every filter, and summed as integers: the
+ * result does not depend on the order of sums, a token more than 45 powers of two
+ * below the largest is not drawn, and min_p keeps what rounds to it or more. */
 typedef struct {
   int64_t struct_bytes;     /* sizeof(sb_sample_args)                               */
   const void *logits;       /* [rows][row_stride], the first vocab of each row      */

@@ -845,11 +845,12 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
       const u64 d = ((u64)(bin - e4 * 16) + 1 << e4) - 1;   // the furthest of the bin
       bound = from_order(seen - (uint32_t)min(d, (u64)(seen - LOWEST)));
     }
-    // min-p keeps z >= top + T ln(min_p), top at least the sample's (less a
-    // little for the rounding here).
+    // min-p keeps the weights that round to min_p or more, half a step of theirs
+    // below it (at least half a step): z >= top + T ln(min_p - 2^-45), top at least
+    // the sample's (less a little for the rounding here).
     if (p == 1.0f && mp > 0.0f && from_order(seen) < INFINITY) {
-      const double b = (double)from_order(seen) + (double)pr.T * log((double)mp);
-      const float bf = (float)(b - 1e-6 * fabs(b) - 1e-30);
+      const double m = from_order(seen), t = (double)pr.T * log(fmax((double)mp - 0x1p-45, 0x1p-45));
+      const float bf = (float)(m + t - 1e-6 * (fabs(m) + fabs(t)) - 1e-30);
       sure |= bf >= bound;
       bound = fmaxf(bound, bf);
     }

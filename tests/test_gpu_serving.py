@@ -686,6 +686,24 @@ def test_sample_odd_values(gpu):
     assert int(tok) == 2
 
 
+@pytest.mark.parametrize("V", [40, 3000, 40000])
+def test_sample_weights_of_one_step(gpu, V):
+    """Weights around 2^-44 of the largest, which is one: min-p goes by the rounded
+    ones. With u = 1 the last kept token is drawn."""
+    steps = [2.6, 2.3, 1.55, 1.45, 1.2, 0.95, 0.7, 0.55, 0.45]     # their weights in steps: the last kept is the least
+    rows, mins = [], []
+    for T in (1.0, 0.5, 3.0):
+        for top in (0.0, 21.5, -3.25):
+            for mp in (2.0 ** -60, 2.0 ** -45, 2.0 ** -44, 1.4 * 2.0 ** -44, 2.0 ** -43, 2.6 * 2.0 ** -44):
+                z = np.full(V, -np.inf)
+                z[V // 3] = top
+                z[V // 2:V // 2 + len(steps)] = top + T * np.log(np.array(steps) * 2.0 ** -44)
+                rows.append((z, T))
+                mins.append(mp)
+    check_sample([z for z, _ in rows], [1.0] * len(rows), T=[T for _, T in rows], min_p=mins)
+    check_sample([z for z, _ in rows], [1.0] * len(rows), T=[T for _, T in rows], min_p=mins, top_k=[7] * len(rows))
+
+
 def test_sample_views(gpu):
     """Rows of a wider array, at addresses of no alignment, and out tensors."""
     r = rng(6)
