@@ -186,7 +186,7 @@ def rope_frequencies(rot_dim: int, *, base: float = 10000.0, scaling: str = "non
         def pair_of(turns):   # the pair (as a real number) that turns so often over original_length
             return rot_dim * math.log(original_length / (2 * math.pi * turns)) / (2 * math.log(base))
         lo = max(math.floor(pair_of(beta_fast)), 0)
-        hi = min(math.ceil(pair_of(beta_slow)), rot_dim // 2 - 1)
+        hi = min(math.ceil(pair_of(beta_slow)), rot_dim - 1)   # (may lie behind the last pair, which is then slowed in part)
         slowed = ((i - lo) / max(hi - lo, 1e-3)).clamp(0, 1)
         inv = inv * (1 - slowed) + inv / factor * slowed
         mscale = 1.0 + 0.1 * math.log(factor)

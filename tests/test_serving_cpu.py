@@ -195,6 +195,24 @@ def test_rope_frequencies():
             sb.rope_frequencies(device="cpu", **bad)
 
 
+@pytest.mark.parametrize("rot,base,length,factor", [(128, 10000.0, 131072, 8.0), (64, 10000.0, 65536, 4.0), (128, 500000.0, 8192, 8.0),
+                                                    (8, 10000.0, 10 ** 9, 2.0)])
+def test_rope_frequencies_in_parts(rot, base, length, factor):
+    """Pair i turns length base^(-2 i / rot) / 2 pi times over the original length.
+    The blend runs evenly from the whole number below the pair that turns 32 times
+    to that above the one that turns once, which may lie behind the last pair:
+    none that turns more than once is slowed by the whole factor."""
+    got, _ = sb.rope_frequencies(rot, base=base, scaling="parts", factor=factor, original_length=length, device="cpu")
+    ends = [rot / 2 * math.log(length / (2 * math.pi * n)) / math.log(base) for n in (32.0, 1.0)]
+    lo, hi = max(math.floor(ends[0]), 0), min(math.ceil(ends[1]), rot - 1)
+    for i in range(rot // 2):
+        plain = base ** (-2 * i / rot)
+        slowed = min(max((i - lo) / max(hi - lo, 1e-3), 0.0), 1.0)
+        assert math.isclose(float(got[i]), plain * (1 - slowed) + plain / factor * slowed, rel_tol=1e-12), i
+        if length * plain / (2 * math.pi) > 1:
+            assert float(got[i]) > plain / factor * (1 + 1e-9), i
+
+
 # -- pins of the oracle ------------------------------------------------------------
 
 def test_oracle_plan_by_hand():
