@@ -15,6 +15,7 @@ import math
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _native as N
 
@@ -70,10 +71,16 @@ def _apart(t, name):
 
 
 def _no_grad(*tensors):
+    """Refuses what a backward pass, or a tangent of forward mode, would have to go
+    through: inputs, and what is written (None: left out)."""
     if torch.is_grad_enabled():
         for t in tensors:
-            if t.requires_grad:
+            if t is not None and t.requires_grad:
                 _refuse("there is no backward pass: call it under torch.no_grad()")
+    if forward_ad._current_level >= 0:   # (a dual tensor does not require a gradient)
+        for t in tensors:
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                _refuse("there is no forward-mode derivative: unpack the dual tensors")
 
 
 def _device(t, name):
@@ -206,7 +213,7 @@ def rope_append(q, k, v, positions, slots, k_cache, v_cache, inv_freq, *, layout
     i, dtype = _device(q, "q"), q.dtype
     if dtype not in _HALVES:
         _refuse("q must be bfloat16 or float16")
-    _no_grad(q, k, v)
+    _no_grad(q, k, v, k_cache, v_cache, inv_freq, out)
     (T, Hq, D), qs = _heads(q, "q", dtype, i)
     (_, Hkv, _), ks = _heads(k, "k", dtype, i, T, D)
     (_, Hv, _), vs = _heads(v, "v", dtype, i, T, D)
@@ -252,7 +259,7 @@ def paged_attention(q, k_cache, v_cache, table, lens, q_start, *, max_q: int, ma
     i, dtype = _device(q, "q"), q.dtype
     if dtype not in _HALVES:
         _refuse("q must be bfloat16 or float16")
-    _no_grad(q, k_cache, v_cache)
+    _no_grad(q, k_cache, v_cache, out)
     (T, Hq, D), qs = _heads(q, "q", dtype, i)
     (pages, page_size, Hkv, _), kc, vc = _caches(k_cache, v_cache, dtype, i, None, D)
     (B, width), row = _table(table, i)
@@ -295,7 +302,7 @@ def sample_tokens(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=
     i = _device(logits, "logits")
     if logits.dim() != 2 or logits.dtype not in _LOGITS or (logits.shape[1] > 1 and logits.stride(1) != 1):
         _refuse("logits must be a float32, bfloat16 or float16 tensor [rows, vocab] with contiguous rows")
-    _no_grad(logits)
+    _no_grad(logits, u, temperature, top_p, min_p, *(out or ()))
     R, V = logits.shape
     f32 = torch.float32
     if out is None:

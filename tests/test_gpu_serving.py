@@ -901,3 +901,27 @@ def test_python_refusals(gpu):
         sb.sample_tokens(torch.zeros(1, 262145, device="cuda"), u[:1])
     with pytest.raises(ValueError, match="token_cap"):
         sb.plan_pages(i32([1]), i32([1]), i32([1]), i32([1]), i32([[1]]), page_size=4, token_cap=-1)
+
+
+def test_no_derivative_is_dropped(gpu):
+    """Every floating tensor that a call reads or writes is looked at: those that
+    require a gradient, and dual ones of forward mode."""
+    from torch.autograd import forward_ad
+    a, r = attention_case(2, 4, 2, 64, 16, [1], [30, 40], BF16, 1), rope_case(3, 4, 2, 64, 32, BF16, 1)
+    a["out"], r["out"] = torch.empty_like(a["q"]), torch.empty_like(r["q"])
+    one = lambda: torch.ones(3, device="cuda")   # noqa: E731
+    s = dict(logits=torch.zeros(3, 10, device="cuda"), u=0 * one(), temperature=one(), top_p=one(), min_p=0 * one())
+    calls = ((lambda **kw: sb.paged_attention(**kw, **bounds(a)), a), (sb.rope_append, r), (sb.sample_tokens, s))
+    for call, args in calls:
+        call(**args)
+        for name, t in args.items():
+            if not t.is_floating_point():
+                continue
+            with pytest.raises(ValueError, match="backward"):
+                call(**dict(args, **{name: t.clone().requires_grad_()}))
+            with torch.no_grad():
+                call(**dict(args, **{name: t.clone().requires_grad_()}))
+            with forward_ad.dual_level(), pytest.raises(ValueError, match="forward"):
+                call(**dict(args, **{name: forward_ad.make_dual(t, torch.ones_like(t))}))
+    with pytest.raises(ValueError, match="backward"):
+        sb.sample_tokens(**s, out=(torch.zeros(3, dtype=torch.int32, device="cuda"), one().requires_grad_()))

@@ -177,6 +177,25 @@ def test_overlapping_outputs_are_found():
             _apart(t, "x")
 
 
+def test_gradients_and_tangents_are_refused():
+    from torch.autograd import forward_ad
+
+    from paper_2010_02164_amd.serving import _no_grad
+    x, y = torch.zeros(3), torch.zeros(3, requires_grad=True)
+    _no_grad(x, None)
+    with pytest.raises(ValueError, match="backward"):
+        _no_grad(x, y)
+    with torch.no_grad():
+        _no_grad(x, y)
+    with forward_ad.dual_level():
+        _no_grad(x, None)
+        dual = forward_ad.make_dual(x, torch.ones(3))
+        for mode in (torch.no_grad(), torch.enable_grad()):
+            with mode, pytest.raises(ValueError, match="forward"):
+                _no_grad(None, dual)
+        _no_grad(forward_ad.unpack_dual(dual).primal)
+
+
 def test_rope_frequencies():
     f, m = sb.rope_frequencies(8, base=100.0, device="cpu")
     assert f.dtype == torch.float64 and m == 1.0
