@@ -83,6 +83,11 @@ def _no_grad(*tensors):
                 _refuse("there is no forward-mode derivative: unpack the dual tensors")
 
 
+# Tells autograd that tensors were written: one that it has saved is then found
+# to have changed, as with torch's own in-place operations. (0.2 us.)
+_written = torch._C._increment_version
+
+
 def _device(t, name):
     i = t.get_device() if t.is_cuda else -1
     if i < 0:
@@ -149,7 +154,8 @@ def plan_pages(lens, add, free_list, n_free, table, *, page_size: int, token_cap
         _refuse("token_cap must not be negative")
     _apart(table, "table")
     i32, i64 = torch.int32, torch.int64
-    if out is None:
+    fresh = out is None
+    if fresh:
         q_start, after, granted, left = torch.empty(3 * B + 2, dtype=i32, device=i).split_with_sizes((B + 1, B, B, 1))
         out = PagePlan(q_start, after, granted, torch.empty(cap, dtype=i64, device=i), torch.empty(cap, dtype=i32, device=i), left)
         at = q_start.data_ptr()
@@ -163,6 +169,7 @@ def plan_pages(lens, add, free_list, n_free, table, *, page_size: int, token_cap
         _whole(free_list, "free_list", i32, i, free_list.shape), table.data_ptr(), *to,
         row, B, free_list.shape[0], int(page_size), width, cap, 0)
     _call(N.lib().sb_plan_pages, "sb_plan_pages", i, args)
+    _written((table, free_list) if fresh else (table, free_list, *out))
     return out
 
 
@@ -240,6 +247,7 @@ def rope_append(q, k, v, positions, slots, k_cache, v_cache, inv_freq, *, layout
         _whole(inv_freq, "inv_freq", torch.float64, i, (pairs,)), qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], os_[0], os_[1],
         kc[0], kc[1], kc[2], vc[0], vc[1], vc[2], T, Hq, Hkv, D, pairs, _LAYOUTS[layout], _HALVES[dtype], pages, page_size, mscale)
     _call(N.lib().sb_rope_append, "sb_rope_append", i, args)
+    _written((k_cache, v_cache, out))
     return out
 
 
@@ -287,6 +295,7 @@ def paged_attention(q, k_cache, v_cache, table, lens, q_start, *, max_q: int, ma
         _check(N.SB_E_INVALID_ARG, "sb_paged_attention")
     work = torch.empty(need, dtype=torch.uint8, device=i) if need else None
     _call(L.sb_paged_attention, "sb_paged_attention", i, args, work.data_ptr() if need else None, need)
+    _written((out,))
     return out
 
 
@@ -319,4 +328,5 @@ def sample_tokens(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=
     need = L.sb_sample_workspace(args)   # (below 0: refused by the call itself)
     work = torch.empty(need, dtype=torch.uint8, device=i) if need > 0 else None
     _call(L.sb_sample_tokens, "sb_sample_tokens", i, args, None if work is None else work.data_ptr(), max(need, 0))
+    _written((tokens, logprobs))
     return tokens, logprobs

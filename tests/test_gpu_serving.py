@@ -925,3 +925,34 @@ def test_no_derivative_is_dropped(gpu):
                 call(**dict(args, **{name: forward_ad.make_dual(t, torch.ones_like(t))}))
     with pytest.raises(ValueError, match="backward"):
         sb.sample_tokens(**s, out=(torch.zeros(3, dtype=torch.int32, device="cuda"), one().requires_grad_()))
+
+
+def test_writes_are_known_to_autograd(gpu):
+    """What a call writes counts as written in place: saved for a backward pass
+    before, it is found to have changed."""
+    r, a = rope_case(3, 4, 2, 64, 32, BF16, 1), attention_case(2, 4, 2, 64, 16, [1], [30, 40], BF16, 1)
+    a["out"] = torch.empty_like(a["q"])
+    out = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.zeros(3, device="cuda")
+    table, fl, n_free = i32([[0, -1]]), i32([1, 2, 3]), i32([3])
+    plan = sb.PagePlan(i32([0, 0]), i32([3]), i32([0]), dev(np.zeros(4, np.int64)), i32([0] * 4), n_free)
+
+    def written(call, *tensors):
+        before = [t._version for t in tensors]
+        call()
+        return all(t._version > v for t, v in zip(tensors, before))
+
+    assert written(lambda: sb.rope_append(**r, out=r["q"]), r["q"], r["k_cache"], r["v_cache"])
+    assert written(lambda: sb.rope_append(**r), r["k_cache"], r["v_cache"])
+    assert written(lambda: sb.paged_attention(**a, **bounds(a)), a["out"])
+    assert written(lambda: sb.sample_tokens(torch.zeros(3, 10, device="cuda"), out[1].clone(), out=out), *out)
+    assert written(lambda: sb.plan_pages(plan.lens, i32([2]), fl, n_free, table, page_size=4, token_cap=4, out=plan), table, fl, *plan)
+    assert written(lambda: sb.plan_pages(plan.lens, i32([2]), fl, n_free, table, page_size=4, token_cap=4), table, fl)
+    w = torch.ones(r["q"].shape, device="cuda", requires_grad=True)
+    product = (w * r["q"]).sum()
+    with torch.no_grad():
+        sb.rope_append(**r, out=r["q"])
+    with pytest.raises(RuntimeError, match="in-?place"):
+        product.backward()
+    with torch.inference_mode():   # tensors without a version
+        sb.rope_append(**r)
+        sb.paged_attention(**dict(a, out=torch.empty_like(a["q"])), **bounds(a))
