@@ -291,7 +291,8 @@ const char *sb_status_string(sb_status s);
  * elements, rows contiguous). Request b's token at position p lies in page
  * table[b][p / page_size], place p % page_size; its slot is
  * page * page_size + place. SB_BF16 or SB_F16. Addresses of q, k, v, out and
- * the caches are 16-byte aligned and their strides multiples of 8 elements.
+ * the caches are 16-byte aligned and their strides multiples of 8 elements
+ * (but those of a single token, head, page or slot, which are not looked at).
  * ------------------------------------------------------------------------ */
 
 /* IEEE half precision, for these calls only (next to sb_dtype's two). */

@@ -3,6 +3,8 @@
 #include <math.h>
 #include <stdio.h>
 
+#include <initializer_list>
+
 #include "serve.h"
 
 using namespace sb;
@@ -37,10 +39,15 @@ hipError_t compute_units(int &n) {
 
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
-// 16-byte loads of rows: strides that keep every row's address a multiple.
-template <typename... S>
-bool strides_fit(S... s) {
-  return ((s >= 0 && s % 8 == 0) && ...);
+// 16-byte loads of rows: strides that keep every row's address a multiple. One
+// that has a single place is never stepped along, and may be anything.
+struct Stride {
+  int64_t step, places;
+};
+bool strides_fit(std::initializer_list<Stride> all) {
+  for (const Stride &s : all)
+    if (s.places > 1 && (s.step < 0 || s.step % 8)) return false;
+  return true;
 }
 
 #define REFUSE_IF(cond, status, why) \
@@ -66,8 +73,9 @@ sb_status check_attention(const sb_attention_args *a, const char *call, bool poi
             "window, sinks, max_q or max_kv < 0");
   REFUSE_IF(!isfinite(a->scale), SB_E_INVALID_ARG, "scale is not finite");
   REFUSE_IF(a->table_stride < a->max_pages, SB_E_INVALID_ARG, "table_stride < max_pages");
-  REFUSE_IF(!strides_fit(a->q_token, a->q_head, a->out_token, a->out_head, a->kc_page, a->kc_slot, a->kc_head, a->vc_page,
-                         a->vc_slot, a->vc_head),
+  REFUSE_IF(!strides_fit({{a->q_token, a->n_tokens}, {a->q_head, a->q_heads}, {a->out_token, a->n_tokens}, {a->out_head, a->q_heads},
+                          {a->kc_page, a->n_pages}, {a->kc_slot, a->page_size}, {a->kc_head, a->kv_heads}, {a->vc_page, a->n_pages},
+                          {a->vc_slot, a->page_size}, {a->vc_head, a->kv_heads}}),
             SB_E_UNSUPPORTED, "a stride is negative or no multiple of 8");
   if (!pointers) return SB_OK;
   REFUSE_IF(!a->table || !a->lens || !a->q_start || !a->k_cache || !a->v_cache || (a->n_tokens && (!a->q || !a->out)),
@@ -129,8 +137,10 @@ sb_status sb_rope_append(const sb_rope_args *a, void *stream) {
   REFUSE_IF(a->n_pages < 1 || a->page_size < 1 || a->page_size > 4096, SB_E_INVALID_ARG, "n_pages < 1 or page_size outside 1 .. 4096");
   REFUSE_IF((int64_t)a->n_pages * a->page_size > INT32_MAX, SB_E_UNSUPPORTED, "n_pages times page_size is not below 2^31");
   REFUSE_IF(!isfinite(a->mscale), SB_E_INVALID_ARG, "mscale is not finite");
-  REFUSE_IF(!strides_fit(a->q_token, a->q_head, a->k_token, a->k_head, a->v_token, a->v_head, a->out_token, a->out_head, a->kc_page,
-                         a->kc_slot, a->kc_head, a->vc_page, a->vc_slot, a->vc_head),
+  REFUSE_IF(!strides_fit({{a->q_token, a->n_tokens}, {a->q_head, a->q_heads}, {a->k_token, a->n_tokens}, {a->k_head, a->kv_heads},
+                          {a->v_token, a->n_tokens}, {a->v_head, a->kv_heads}, {a->out_token, a->n_tokens}, {a->out_head, a->q_heads},
+                          {a->kc_page, a->n_pages}, {a->kc_slot, a->page_size}, {a->kc_head, a->kv_heads}, {a->vc_page, a->n_pages},
+                          {a->vc_slot, a->page_size}, {a->vc_head, a->kv_heads}}),
             SB_E_UNSUPPORTED, "a stride is negative or no multiple of 8");
   if (a->n_tokens == 0) return SB_OK;
   REFUSE_IF(!a->q || !a->k || !a->v || !a->q_out || !a->k_cache || !a->v_cache || !a->positions || !a->slots ||

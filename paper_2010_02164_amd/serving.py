@@ -212,8 +212,9 @@ def rope_append(q, k, v, positions, slots, k_cache, v_cache, inv_freq, *, layout
     (sb_rope_append).
 
     q: [tokens, q_heads, head_dim], k, v: [tokens, kv_heads, head_dim], caches:
-    [pages, page_size, kv_heads, head_dim], one type (bfloat16 or float16);
-    their token, head, page and slot strides are free. positions: int32
+    [pages, page_size, kv_heads, head_dim], one type (bfloat16 or float16); of
+    any strides that are multiples of 8, heads contiguous, at addresses that are
+    multiples of 16. positions: int32
     [tokens], slots: int64 [tokens] (plan_pages gives both; tokens with slots
     outside the cache are skipped); inv_freq: float64, one per pair
     (rope_frequencies). out: where the queries go, q itself for in place."""

@@ -956,3 +956,26 @@ def test_writes_are_known_to_autograd(gpu):
     with torch.inference_mode():   # tensors without a version
         sb.rope_append(**r)
         sb.paged_attention(**dict(a, out=torch.empty_like(a["q"])), **bounds(a))
+
+
+def test_strides_of_one_place(gpu):
+    """One token, head, page or slot cut out of arrays of odd strides."""
+    def cut(t):   # the same values, in rows of an odd stride where there is one
+        shape, stride = t.shape, [s if n > 1 else s + 13 for n, s in zip(t.shape, t.stride())]
+        flat = torch.zeros(t.numel() + 64, dtype=t.dtype, device="cuda")
+        got = flat.as_strided(shape, stride)
+        got.copy_(t)
+        return got
+
+    for Hq, Hkv, page in ((4, 2, 16), (1, 1, 16), (3, 1, 1)):
+        a = attention_case(1, Hq, Hkv, 64, page, [1], [1], BF16, 3)
+        a["k_cache"], a["v_cache"], a["table"] = a["k_cache"][:1].contiguous(), a["v_cache"][:1].contiguous(), i32([[0]])
+        want = sb.paged_attention(**a, max_q=1, max_kv=1)
+        odd = dict(a, **{n: cut(a[n]) for n in ("q", "k_cache", "v_cache")})
+        for max_q in (1, 1000):
+            assert torch.equal(sb.paged_attention(**odd, max_q=max_q, max_kv=1, out=cut(torch.zeros_like(want))), want)
+        r = rope_case(1, Hq, Hkv, 64, 32, F16, 2, page)
+        r["k_cache"], r["v_cache"], r["slots"] = r["k_cache"][:1].contiguous(), r["v_cache"][:1].contiguous(), dev(np.zeros(1, np.int64))
+        odd = dict(r, **{n: cut(r[n]) for n in ("q", "k", "v", "k_cache", "v_cache")})
+        assert torch.equal(sb.rope_append(**odd, out=cut(r["q"])), sb.rope_append(**r))
+        assert torch.equal(odd["k_cache"], r["k_cache"]) and torch.equal(odd["v_cache"], r["v_cache"])

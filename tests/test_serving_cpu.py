@@ -124,6 +124,20 @@ def test_attention_keys_stay_below_32_bits(native_lib):
                 assert "MAX_KEYS" in native_lib.sb_last_error(None).decode()
 
 
+def test_strides_of_one_place_are_not_looked_at(native_lib):
+    one = dict(n_tokens=0, q_heads=1, kv_heads=1, n_pages=1, page_size=1)
+    names = [n for n in ATTN if n.split("_")[-1] in ("token", "head", "page", "slot")]
+    assert len(names) == 10
+    odd = {n: 13 for n in names}
+    assert _refused(native_lib, "sb_paged_attention", ATTN, dict(one, **odd)) == N.SB_OK
+    for n in names:   # but those of several are
+        places = dict(one, n_tokens=3, q_heads=2, kv_heads=2, n_pages=2, page_size=2)
+        args = N.ATTENTION_ARGS.pack(*dict(ATTN, **places, **{n: 13}).values())
+        assert native_lib.sb_attention_workspace(args) == -1 and "stride" in native_lib.sb_last_error(None).decode()
+    # (What rope does with its tokens' strides needs a launch: in the tests on a GPU.)
+    assert _refused(native_lib, "sb_rope_append", ROPE, dict(one, **odd, k_token=13, k_head=13, v_token=13, v_head=-7)) == N.SB_OK
+
+
 def test_sample_workspace(native_lib):
     """Only many wide rows, or some with top-p, are faster with one; one that is
     too small is refused."""
