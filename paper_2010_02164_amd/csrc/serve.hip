@@ -71,7 +71,7 @@ sb_status check_attention(const sb_attention_args *a, const char *call, bool poi
   REFUSE_IF((int64_t)a->n_tokens * a->q_heads > INT32_MAX, SB_E_UNSUPPORTED, "n_tokens times q_heads is not below 2^31");
   REFUSE_IF(a->window < 0 || a->sinks < 0 || a->max_q < 0 || a->max_kv < 0, SB_E_INVALID_ARG,
             "window, sinks, max_q or max_kv < 0");
-  REFUSE_IF(!isfinite(a->scale), SB_E_INVALID_ARG, "scale is not finite");
+  REFUSE_IF(!isfinite((float)(a->scale * 1.4426950408889634)), SB_E_INVALID_ARG, "scale, in powers of two, is not finite");
   REFUSE_IF(a->table_stride < a->max_pages, SB_E_INVALID_ARG, "table_stride < max_pages");
   REFUSE_IF(!strides_fit({{a->q_token, a->n_tokens}, {a->q_head, a->q_heads}, {a->out_token, a->n_tokens}, {a->out_head, a->q_heads},
                           {a->kc_page, a->n_pages}, {a->kc_slot, a->page_size}, {a->kc_head, a->kv_heads}, {a->vc_page, a->n_pages},

@@ -12,6 +12,7 @@ and every call can be captured into a graph. There are no backward passes.
 from __future__ import annotations
 
 import math
+import operator
 from typing import NamedTuple, Optional
 
 import torch
@@ -147,7 +148,10 @@ def plan_pages(lens, add, free_list, n_free, table, *, page_size: int, token_cap
     the most tokens a step takes."""
     i = _device(lens, "lens")
     (B, width), row = _table(table, i)
-    cap = int(token_cap)
+    try:
+        cap = operator.index(token_cap)
+    except TypeError:
+        _refuse("token_cap must be a whole number")
     if free_list.dim() != 1:
         _refuse("free_list must have one dimension")
     if cap < 0:
@@ -167,7 +171,7 @@ def plan_pages(lens, add, free_list, n_free, table, *, page_size: int, token_cap
     args = N.PLAN_ARGS.pack(
         N.PLAN_ARGS.size, _whole(lens, "lens", i32, i, (B,)), _whole(add, "add", i32, i, (B,)), _whole(n_free, "n_free", i32, i, (1,)),
         _whole(free_list, "free_list", i32, i, free_list.shape), table.data_ptr(), *to,
-        row, B, free_list.shape[0], int(page_size), width, cap, 0)
+        row, B, free_list.shape[0], page_size, width, cap, 0)
     _call(N.lib().sb_plan_pages, "sb_plan_pages", i, args)
     _written((table, free_list) if fresh else (table, free_list, *out))
     return out

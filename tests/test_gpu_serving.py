@@ -979,3 +979,11 @@ def test_strides_of_one_place(gpu):
         odd = dict(r, **{n: cut(r[n]) for n in ("q", "k", "v", "k_cache", "v_cache")})
         assert torch.equal(sb.rope_append(**odd, out=cut(r["q"])), sb.rope_append(**r))
         assert torch.equal(odd["k_cache"], r["k_cache"]) and torch.equal(odd["v_cache"], r["v_cache"])
+
+
+def test_plan_takes_whole_numbers_only(gpu):
+    args = lambda: (i32([1]), i32([1]), i32([1]), i32([1]), i32([[1]]))   # noqa: E731
+    for bad in (dict(page_size=4.5, token_cap=2), dict(page_size=4, token_cap=2.5), dict(page_size=2 ** 40, token_cap=2)):
+        with pytest.raises(ValueError):
+            sb.plan_pages(*args(), **bad)
+    assert sb.plan_pages(*args(), page_size=np.int64(4), token_cap=np.int32(2)).granted.tolist() == [1]

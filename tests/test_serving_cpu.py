@@ -138,6 +138,17 @@ def test_strides_of_one_place_are_not_looked_at(native_lib):
     assert _refused(native_lib, "sb_rope_append", ROPE, dict(one, **odd, k_token=13, k_head=13, v_token=13, v_head=-7)) == N.SB_OK
 
 
+def test_numbers_that_do_not_fit(native_lib):
+    """A scale has to fit fp32 as the power of two that the kernels take; fields of
+    whole numbers take no others."""
+    for packer, base, over in ((N.PLAN_ARGS, PLAN, dict(page_size=16.5)), (N.SAMPLE_ARGS, SAMPLE, dict(rows=2 ** 31))):
+        with pytest.raises(ValueError, match="does not fit"):
+            packer.pack(*dict(base, **over).values())
+    assert _refused(native_lib, "sb_rope_append", ROPE, dict(mscale=-1e39)) == INVALID
+    for scale, status in ((2.35e38, N.SB_OK), (2.4e38, INVALID), (-3.4e38, INVALID), (1e300, INVALID), (0.0, N.SB_OK)):
+        assert _refused(native_lib, "sb_paged_attention", ATTN, dict(scale=scale, n_tokens=0)) == status
+
+
 def test_sample_workspace(native_lib):
     """Only many wide rows, or some with top-p, are faster with one; one that is
     too small is refused."""
