@@ -343,8 +343,9 @@ sb_status sb_plan_pages(const sb_plan_args *args, void *stream);
  * is copied. Pairs are (i, i + n_pairs) (SB_ROPE_HALF) or (2i, 2i + 1)
  * (SB_ROPE_INTERLEAVED). Rotated queries go to q_out (which may be q), rotated
  * keys and the values to slot slots[t] of the caches. A token whose slot lies
- * outside the cache is skipped: its q_out row stays as it was. Two tokens of
- * one slot leave either's key and value there. */
+ * outside the cache is skipped: its q_out row stays as it was. Slots have to be
+ * distinct: of two tokens of one slot, each piece of 8 values of its key and its
+ * value may be either's. */
 enum { SB_ROPE_HALF = 0, SB_ROPE_INTERLEAVED = 1 };
 typedef struct {
   int64_t struct_bytes;     /* sizeof(sb_rope_args)                                 */

@@ -220,7 +220,8 @@ def rope_append(q, k, v, positions, slots, k_cache, v_cache, inv_freq, *, layout
     any strides that are multiples of 8, heads contiguous, at addresses that are
     multiples of 16. positions: int32
     [tokens], slots: int64 [tokens] (plan_pages gives both; tokens with slots
-    outside the cache are skipped); inv_freq: float64, one per pair
+    outside the cache are skipped, those of the others have to be distinct);
+    inv_freq: float64, one per pair
     (rope_frequencies). out: where the queries go, q itself for in place."""
     i, dtype = _device(q, "q"), q.dtype
     if dtype not in _HALVES:

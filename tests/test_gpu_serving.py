@@ -217,6 +217,27 @@ def test_rope_views_in_place(gpu):
     check_rope(dict(plain, k_cache=c["k_cache"], v_cache=c["v_cache"]), "half", 1.0, q, before)
 
 
+def test_rope_slots_given_twice(gpu):
+    """The queries are right, and every piece of 8 values in the cache is one of
+    the tokens'; nothing else is written."""
+    T, D = 600, 64
+    c = rope_case(T, 2, 2, D, 32, BF16, 13)
+    apart = dict(c, k_cache=c["k_cache"].clone(), v_cache=c["v_cache"].clone())
+    want = sb.rope_append(**apart)
+    at = [(int(s) // 16, int(s) % 16) for s in c["slots"][:3]]
+    own = c["slots"].clone()
+    c["slots"] = own[torch.arange(T, device="cuda") % 3]
+    before = c["k_cache"].clone(), c["v_cache"].clone()
+    assert torch.equal(sb.rope_append(**c), want)
+    for cache, held, given in ((c["k_cache"], before[0], apart["k_cache"]), (c["v_cache"], before[1], apart["v_cache"])):
+        mine = given.view(-1, 2, D // 8, 8)[own]   # what each token writes
+        for i, (page, place) in enumerate(at):
+            got = cache[page, place].view(2, D // 8, 8)
+            assert bool((mine[i::3] == got).all(-1).any(0).all())
+            cache[page, place] = held[page, place]
+        assert torch.equal(cache, held)
+
+
 def test_rope_far_positions(gpu):
     """Positions up to 2^31 - 1: an fp32 angle would be off by whole turns."""
     c = rope_case(4, 1, 1, 64, 32, F16, 11)
