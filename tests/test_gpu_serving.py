@@ -308,6 +308,32 @@ def test_attention(gpu, form, dtype, D):
         check_attention(c, got, window, sinks)
 
 
+@pytest.mark.parametrize("form", range(len(FORMS)))
+def test_attention_fp16_heads_of_256(gpu, form):
+    """Both kernels, whole, shared and split, with and without windows."""
+    test_attention(gpu, form, F16, 256)
+
+
+@pytest.mark.parametrize("q,kv", [([1, 2, 1], [6000, 9, 2500]), ([90, 260, 1], [3000, 2000, 700])])
+def test_attention_fp16_heads_of_256_long(gpu, q, kv):
+    """Keys in parts, what is hidden not finite, and a key that the last query
+    alone sees not a number."""
+    c = attention_case(3, 4, 2, 256, 16, q, kv, F16, 17, pad=3)
+    for window, sinks in ((0, 0), (1100, 3)):
+        check_attention(c, sb.paged_attention(**c, **bounds(c), window=window, sinks=sinks), window, sinks)
+    want = sb.paged_attention(**c, **bounds(c))
+    last = kv[0] - 1
+    at = int(c["table"][0, last // 16]), last % 16
+    for j in range(last % 16 + 1, 16):   # behind the first request's last token
+        c["k_cache"][at[0], j], c["v_cache"][at[0], j] = math.nan, math.inf
+    rows, first = int(c["q_start"][-1]), int(c["q_start"][1]) - 1
+    assert torch.equal(sb.paged_attention(**c, **bounds(c))[:rows], want[:rows])
+    c["v_cache"][at] = math.nan
+    got = sb.paged_attention(**c, **bounds(c))[:rows]
+    assert bool(got[first].isnan().all())
+    assert torch.equal(got[:first], want[:first]) and torch.equal(got[first + 1:], want[first + 1:rows])
+
+
 @pytest.mark.parametrize("dtype,D,Hq,Hkv", [(BF16, 128, 4, 1), (F16, 64, 8, 1), (BF16, 256, 2, 1)])
 def test_attention_long_cache_in_parts(gpu, dtype, D, Hq, Hkv):
     """Caches long enough to be split over workgroups, short ones beside."""
