@@ -710,6 +710,44 @@ def test_sample_rows_by_kernels_of_their_own(gpu, dtype, V, monkeypatch):
                 assert float(lp[j]) == pytest.approx(want[1], rel=2.0 ** -22, abs=2.0 ** -36)
 
 
+@pytest.mark.parametrize("dtype,V", [(F32, 49153), (BF16, 49153), (F32, 49159), (F16, 49159), (BF16, 65537)])
+def test_sample_last_chunk_of_a_wide_row(gpu, dtype, V, monkeypatch):
+    """Rows just long enough for a workspace, the last chunk of 1 or 7 tokens (less
+    than 16 bytes): as the oracle says, and as without a workspace."""
+    r = rng(V)
+    rows = 20
+    z = 2 * r.standard_normal((rows, V))
+    z[1, -1] = 30.0                                   # the largest last
+    z[2, -1] = -np.inf
+    z[3] = 1.0                                        # cuts among equals up to the last
+    z[4], z[4, -1] = -40.0, 0.0                       # alone
+    z[5, -7:] = z[5].max() + 1.0                      # equals at the end
+    z[6, :-1] = np.minimum(z[6, :-1], 3.0)
+    z[6, -1] = 3.0                                    # equal to the largest of the others
+    z[7, -1] = np.nan
+    z[8, -1] = np.inf
+    u, T = r.random(rows), 0.5 + r.random(rows)
+    u[[3, 4, 5, 6, 9]] = 1.0, 0.5, 1.0, 1 - 2.0 ** -24, 1.0
+    p, mp = np.where(np.arange(rows) % 5 == 4, 1.0, 0.5 + 0.5 * r.random(rows)), np.where(np.arange(rows) % 3, 0.0, 0.05 * r.random(rows))
+    p[[3, 6]] = 0.9999, 0.999
+    f = lambda x: dev(np.asarray(x, np.float32))   # noqa: E731
+    zd, L = dev(z, F32).to(dtype), sb.decoder.N.lib()
+    zz, need = f64(zd), L.sb_sample_workspace
+    for kw in (dict(temperature=f(T), top_p=f(p), min_p=f(mp)), dict(temperature=f(T)), dict(top_p=f(p))):
+        asked = []
+        with monkeypatch.context() as m:
+            m.setattr(L, "sb_sample_workspace", lambda args: asked.append(need(args)) or asked[-1])
+            tok, lp = sb.sample_tokens(zd, f(u), **kw)
+            assert asked[0] > 0
+            m.setattr(L, "sb_sample_workspace", lambda args: 0)
+            alone = sb.sample_tokens(zd, f(u), **kw)
+        assert torch.equal(tok, alone[0]) and torch.equal(lp, alone[1])
+        for j in range(rows):
+            at = lambda n, d: float(kw[n][j]) if n in kw else d   # noqa: E731
+            want = oracle.sample(zz[j], float(np.float32(u[j])), at("temperature", 1.0), 0, at("top_p", 1.0), at("min_p", 0.0))
+            assert int(tok[j]) == want[0] and float(lp[j]) == pytest.approx(want[1], rel=2.0 ** -22, abs=2.0 ** -36), j
+
+
 def test_sample_odd_values(gpu):
     """-inf, NaN, +inf, the largest and smallest numbers, -0; parameters out of
     their range."""
