@@ -887,6 +887,39 @@ def test_a_run_of_them_together(gpu, window, sinks):
     assert plan.lens.tolist() == [37 + 11, 0, 20 + 11]
 
 
+@pytest.mark.parametrize("window,sinks", [(0, 0), (24, 3)])
+def test_a_batch_goes_by_its_own_draws(gpu, window, sinks):
+    """Every token drawn is the oracle's for that row's logits, and the next step's
+    input; at every step each page is in one live request's row or on the free
+    list; a released request's row and pages serve the next one."""
+    layer, page, width, n_pages, cap = Layer(3), 8, 16, 40, 64
+    r = rng(4)
+    cache, free, table, plan = fresh(n_pages, page, layer, 3, width, cap)
+    top_p, T = dev(np.full(3, 0.8, np.float32)), dev(np.full(3, 1.1, np.float32))
+    lens, add, new = [0, 0, 0], [37, 1, 20], [r.integers(0, 500, n).tolist() for n in (37, 1, 20)]
+    for t in range(14):
+        tokens = torch.tensor(sum(new, []) + [0] * (cap - sum(map(len, new)))).cuda()
+        plan = sb.plan_pages(plan.lens, i32(add), free, plan.n_free, table, page_size=page, token_cap=cap, out=plan)
+        lens = [0 if n < 0 else x + n for x, n in zip(lens, add)]
+        held = [-(-x // page) for x in lens]
+        assert plan.lens.tolist() == lens and int(plan.n_free) == n_pages - sum(held), t
+        ids = free[:int(plan.n_free)].tolist() + sum((table[b, :n].tolist() for b, n in enumerate(held)), [])
+        assert sorted(ids) == list(range(n_pages)), t
+        logits = layer.step(tokens, plan, cache, table, max_q=max(add), max_kv=width * page, window=window, sinks=sinks)
+        live = [b for b in range(3) if add[b] > 0]
+        last = logits[(plan.q_start[1:].long() - 1).clamp(min=0)].float()
+        u = r.random(3).astype(np.float32)
+        drawn = sb.sample_tokens(last, dev(u), temperature=T, top_p=top_p)[0]
+        z = f64(last)
+        assert np.isfinite(z[live]).all()
+        for b in live:
+            assert int(drawn[b]) == oracle.sample(z[b], float(u[b]), float(np.float32(1.1)), 0, float(np.float32(0.8)))[0], (t, b)
+        # Request 1 ends after its sixth token; its row stands idle for a step and
+        # then takes a prompt of 12.
+        add = [1, -1 if t == 5 else 0 if t == 6 else 12 if t == 7 else 1, 1]
+        new = [[int(drawn[b])] if add[b] == 1 else r.integers(0, 500, max(add[b], 0)).tolist() for b in range(3)]
+
+
 def test_captured_steps(gpu):
     """A whole step captured once and replayed, with eager work between: as the
     same steps taken eagerly. Two graphs live at once, each with its workspace."""
