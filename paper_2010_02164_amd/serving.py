@@ -29,12 +29,6 @@ def _refuse(what):
     raise ValueError(what)
 
 
-def _check(status: int, where: str):
-    if status != N.SB_OK:
-        msg = N.lib().sb_last_error(None)
-        raise N.StreambeamError(status, where, msg.decode() if msg else "")
-
-
 # The current stream's handle and the current device by torch's direct calls:
 # the public ones build objects, 3 of a single-token call's 15 microseconds.
 _raw_stream, _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
@@ -48,7 +42,8 @@ def _call(fn, where, i, *args):
         with torch.cuda.device(i):
             status = fn(*args, _raw_stream(i))
     if status != N.SB_OK:
-        _check(status, where)
+        msg = N.lib().sb_last_error(None)
+        raise N.StreambeamError(status, where, msg.decode() if msg else "")
 
 
 # The checks read each property of a tensor once: a read takes 0.1 us, a call
@@ -297,10 +292,8 @@ def paged_attention(q, k_cache, v_cache, table, lens, q_start, *, max_q: int, ma
     else:
         with torch.cuda.device(i):
             need = L.sb_attention_workspace(args)
-    if need < 0:
-        _check(N.SB_E_INVALID_ARG, "sb_paged_attention")
-    work = torch.empty(need, dtype=torch.uint8, device=i) if need else None
-    _call(L.sb_paged_attention, "sb_paged_attention", i, args, work.data_ptr() if need else None, need)
+    work = torch.empty(need, dtype=torch.uint8, device=i) if need > 0 else None   # (below 0: refused by the call itself)
+    _call(L.sb_paged_attention, "sb_paged_attention", i, args, None if work is None else work.data_ptr(), max(need, 0))
     _written((out,))
     return out
 

@@ -1105,3 +1105,18 @@ def test_plan_takes_whole_numbers_only(gpu):
         with pytest.raises(ValueError):
             sb.plan_pages(*args(), **bad)
     assert sb.plan_pages(*args(), page_size=np.int64(4), token_cap=np.int32(2)).granted.tolist() == [1]
+
+
+def test_refusals_keep_their_status(gpu):
+    """The library's own status, of calls that ask for a workspace first, too."""
+    N = sb.decoder.N
+    a = attention_case(1, 4, 2, 64, 16, [1], [30], BF16, 1)
+    cut = dict(a, q=a["q"][..., :40].contiguous(), k_cache=a["k_cache"][..., :40].contiguous(), v_cache=a["v_cache"][..., :40].contiguous())
+    wide, u = torch.zeros(1, 262145, device="cuda"), torch.zeros(1, device="cuda")
+    for call, status in ((lambda: sb.paged_attention(**cut, **bounds(a)), N.SB_E_UNSUPPORTED),
+                         (lambda: sb.paged_attention(**a, **bounds(a), window=-1), N.SB_E_INVALID_ARG),
+                         (lambda: sb.sample_tokens(wide, u), N.SB_E_UNSUPPORTED),
+                         (lambda: sb.sample_tokens(wide[:, :0], u), N.SB_E_INVALID_ARG)):
+        with pytest.raises(N.StreambeamError) as e:
+            call()
+        assert e.value.status == status
