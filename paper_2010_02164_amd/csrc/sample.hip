@@ -259,14 +259,13 @@ struct Items {
 };
 
 // The key at which the items' weights, in ascending order of their keys, first
-// total more than `limit`, which they do. keys < 2^bits; `drop` low bits are
-// left out of the search (and of the result).
+// total more than `limit`, which they do. keys < 2^bits.
 template <typename K>
-__device__ __forceinline__ uint32_t list_search(const Items &it, K key, int bits, int drop, u64 limit, u64 &rest, u64 &at, Shared &sh) {
+__device__ __forceinline__ uint32_t list_search(const Items &it, K key, int bits, u64 limit, u64 &rest, u64 &at, Shared &sh) {
   uint32_t prefix = 0;
   int shift = bits;
   do {
-    const int take = min(BIN_BITS, shift - drop);
+    const int take = min(BIN_BITS, shift);
     shift -= take;
     clear_bins(sh);
 #pragma unroll
@@ -276,8 +275,8 @@ __device__ __forceinline__ uint32_t list_search(const Items &it, K key, int bits
     }
     prefix = (prefix << take) | find_bin(limit, rest, at, sh);
     limit = rest;
-  } while (shift > drop);
-  return prefix << drop;
+  } while (shift > 0);
+  return prefix;
 }
 
 // Likewise over the row's tokens, from the largest logit down, 8 bits a pass;
@@ -477,7 +476,7 @@ __device__ __forceinline__ int cut_list(Items &it, uint32_t best, uint32_t d, u6
 #pragma unroll
     for (int j = 0; j < LIST_PER; ++j) eq.w[j] = it.w[j] && best - it.key[j] == d;
     u64 rest, a2;
-    last = (int)list_search(eq, [&](int j) { return (uint32_t)eq.idx[j]; }, bits_of(V - 1), 0, before / each, rest, a2, sh);
+    last = (int)list_search(eq, [&](int j) { return (uint32_t)eq.idx[j]; }, bits_of(V - 1), before / each, rest, a2, sh);
   }
 #pragma unroll
   for (int j = 0; j < LIST_PER; ++j) {
@@ -546,7 +545,7 @@ __device__ __forceinline__ int draw_ranked(int n, const Params &pr, const Weighe
     it.idx[0] = me.idx;
     it.w[0] = kept ? me.w : 0;
     u64 rest, at;
-    return (int)list_search(it, [&](int j) { return (uint32_t)it.idx[j]; }, bits_of(V - 1), 0, limit, rest, at, sh);
+    return (int)list_search(it, [&](int j) { return (uint32_t)it.idx[j]; }, bits_of(V - 1), limit, rest, at, sh);
   }
   if (kept) {   // what the kept tokens of lower indexes total
     const int *sorted = sh.idx + 3 * RANKED;
@@ -708,7 +707,7 @@ __device__ __forceinline__ int wide_row(const Row<DT> &row, const Params &pr, co
       if (m <= LIST_MAX) {
         Items it;
         take_list(it, m, [&](uint32_t b) { return count ? (u64)1 : weigh(from_order(b)); }, sh);
-        bits = best - list_search(it, [&](int j) { return best - it.key[j]; }, 32, 0, rest, rest, at, sh);
+        bits = best - list_search(it, [&](int j) { return best - it.key[j]; }, 32, rest, rest, at, sh);
       } else {   // (all equals of the cut: kept ones and others weigh the same, and the limit is among the kept)
         bits = row_search<DT>(row, limit, [&](float z) { return z >= cut.lo ? count ? (u64)1 : weigh(z) : 0; }, rest, at, sh);
       }
@@ -954,7 +953,7 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
 #pragma unroll
         for (int j = 0; j < LIST_PER; ++j) count.w[j] = j * SM_THREADS + tid < n;
         u64 rest, at;
-        const uint32_t d = list_search(count, [&](int j) { return best - count.key[j]; }, bits, 0, (u64)(k - 1), rest, at, sh);
+        const uint32_t d = list_search(count, [&](int j) { return best - count.key[j]; }, bits, (u64)(k - 1), rest, at, sh);
         cut_list(it, best, d, rest, 1, at, V, sh);
       }
       if (p < 1.0f) {
@@ -964,7 +963,7 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
         const u64 z_k = block_sum(s, sh), limit = pr.top_p_limit(z_k);
         if (limit < z_k) {
           u64 rest, at;
-          const uint32_t d = list_search(it, [&](int j) { return best - it.key[j]; }, bits, 0, limit, rest, at, sh);
+          const uint32_t d = list_search(it, [&](int j) { return best - it.key[j]; }, bits, limit, rest, at, sh);
           cut_list(it, best, d, rest, weigh(from_order(best - d)), at, V, sh);
         }
       }
@@ -977,7 +976,7 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_sample(sb_sample_args a, Wide
 #pragma unroll
     for (int j = 0; j < LIST_PER; ++j) s += it.w[j];
     total = block_sum(s, sh);
-    token = (int)list_search(it, [&](int j) { return (uint32_t)it.idx[j]; }, bits_of(V - 1), 0, greedy ? 0 : pr.draw_limit(total), rest, at, sh);
+    token = (int)list_search(it, [&](int j) { return (uint32_t)it.idx[j]; }, bits_of(V - 1), greedy ? 0 : pr.draw_limit(total), rest, at, sh);
     if (greedy) total = (u64)ONE;
   } else {
     const float low = sampled ? -INFINITY : -from_order(block_max(order_bits(-zl), sh));   // (sampled: not looked for)
@@ -1224,15 +1223,15 @@ __global__ __launch_bounds__(SM_THREADS, 4) void k_wide_draw(sb_sample_args a, W
       cut.lo = from_order(sh.digit);
       cut.last = sh.token;
     } else {
-    take_list(it, w.n, [&](uint32_t b) { return weigh(from_order(b)); }, sh);
-    u64 rest, at;
-    const uint32_t d = list_search(it, [&](int j) { return last - it.key[j]; }, bits_of(last - w.first), 0, w.rest, rest, at, sh);
-    const int end = cut_list(it, last, d, rest, weigh(from_order(last - d)), at, V, sh);
-    cut.lo = from_order(last - d);
-    if (end < V) cut.last = end;
+      take_list(it, w.n, [&](uint32_t b) { return weigh(from_order(b)); }, sh);
+      u64 rest, at;
+      const uint32_t d = list_search(it, [&](int j) { return last - it.key[j]; }, bits_of(last - w.first), w.rest, rest, at, sh);
+      const int end = cut_list(it, last, d, rest, weigh(from_order(last - d)), at, V, sh);
+      cut.lo = from_order(last - d);
+      if (end < V) cut.last = end;
 #pragma unroll
-    for (int j = 0; j < LIST_PER; ++j)
-      if (it.w[j] && from_order(it.key[j]) >= w.z_mp) atomicAdd(&tot[it.idx[j] / CHUNK], it.w[j]);
+      for (int j = 0; j < LIST_PER; ++j)
+        if (it.w[j] && from_order(it.key[j]) >= w.z_mp) atomicAdd(&tot[it.idx[j] / CHUNK], it.w[j]);
     }
   }
   __syncthreads();
