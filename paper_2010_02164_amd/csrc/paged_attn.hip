@@ -15,14 +15,14 @@
 // turns. Caches differ in length, so the workgroups share the tiles of all
 // requests evenly, wherever requests begin and end; k_attn_join adds the parts
 // of those that more than one had a share in. 64 requests of 200 to 9000
-// tokens, 8 heads of 128 in bf16: 239 us, 5.05 TB/s (278 us where each request
+// tokens, 8 heads of 128 in bf16: 238 us, 5.07 TB/s (278 us where each request
 // was cut into the same number of parts; reading the same rows alone: 220 us).
 // k_attn_many: 128 rows a workgroup (prompts), 64 keys at a time in LDS, the keys
 // of few prompts split over workgroups (k_attn_many_join); bound
 // by the matrix products and the exponentials between them: three prompts of 1500
 // to 4100 tokens over up to 8200, window 2048, 32 heads of 128: 391 us, 722
-// TFLOP/s (a library product of 8192^3: 1250), the matrix unit busy 32, the vector
-// unit 41, LDS 35 percent of the time.
+// TFLOP/s (a library product of 8192^3: 1250), the matrix unit busy 35, the vector
+// unit 45, LDS 38 percent of a compute unit's busy cycles.
 #include <algorithm>
 #include <cmath>
 
@@ -98,7 +98,8 @@ __device__ __forceinline__ u4 finite_only(const u4 &x, bool &bad) {
 // indicators (ones where V is not finite, ones where a weight is not 0) says
 // which results become NaN instead. That code is apart: the loops over the
 // keys stop at such a tile and are run again with it from the start, so that
-// it takes no registers from them.
+// it takes no registers from them (at heads of 256 the one for prompts is out of
+// registers all the same and reloads about 8 a tile).
 template <int DT>
 __device__ __forceinline__ uint32_t ones_where(bool lo, bool hi) {
   constexpr uint32_t ONE16 = DT == SB_BF16 ? 0x3F80u : 0x3C00u;

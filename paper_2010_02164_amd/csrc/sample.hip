@@ -7,10 +7,13 @@
 // finds where a sum of counts (top-k) or of weights (top-p) passes its limit,
 // and the draw is the same search over the kept tokens' indexes.
 //
-// Most rows are read once: a sample of the row (four 16-byte pieces a thread)
-// gives a bound that the k-th largest logit hardly ever is below, and the pass
-// over the row lists the tokens from that bound on; a list of fewer than k sends
-// the row the other way. min-p alone bounds the tokens by the sample's largest.
+// Rows with top-k, or min-p alone, are read once where their likely tokens are spread
+// over the vocabulary: a sample of the row (four runs of 512 neighbouring 16-byte
+// pieces) gives a bound that the k-th largest logit then hardly ever is below, and
+// the pass over the row lists the tokens from that bound on. A list of fewer than k
+// sends the row the other way. So do likely tokens that gather in one of the runs
+// (top-k 50 of 128000 in fp32: 30 us; with logits that fall as ln(1 + i / 100)
+// with the index i 96). min-p alone bounds the tokens by the sample's largest.
 // A short list is sorted, where every filter keeps a prefix; a longer one
 // (up to 4096) is searched in registers and LDS. A row of 32000 logits in fp32
 // takes 10.5 us, of which launching and reading it takes 6 (17.6 us where short
