@@ -69,3 +69,20 @@ def test_projection_registers(kernels):
     assert len(proj) == 7
     for name, (vgprs, spills) in proj.items():
         assert vgprs <= 256 and spills == 0, (name, vgprs, spills)
+
+
+def test_serving_registers(kernels):
+    """The workgroups a compute unit is to hold: three, two and one of single
+    tokens' attention at heads of 64, 128 and 256, two of prompts' up to 128, four
+    waves a SIMD of the sampler (eight where it lists wide rows). Spills only where
+    they are known: prompts from heads of 128 on, plans of more than 2048 requests."""
+    most = {"k_attn_fewILi.ELi64E": 168, "k_attn_fewILi.ELi128E": 256, "k_attn_fewILi.ELi256E": 512, "k_attn_manyILi.ELi64E": 256,
+            "k_attn_joinILi": 128, "k_attn_many_joinILi": 128, "k_ropeILi": 128, "k_slotsE": 128, "k_planILi[12]E": 128, "k_sampleILi": 128,
+            "k_wide_binsILi": 128, "k_wide_cutILi": 128, "k_wide_drawILi": 128, "k_wide_listILi": 64}
+    for pattern, vgprs in most.items():
+        found = {k: v for k, v in kernels.items() if re.search(pattern, k)}
+        assert found, pattern
+        for name, (used, spills) in found.items():
+            assert used <= vgprs and spills == 0, (name, used, spills)
+    for pattern in ("k_attn_manyILi.ELi128E", "k_attn_manyILi.ELi256E", "k_planILi8E"):
+        assert any(re.search(pattern, k) for k in kernels), pattern
