@@ -135,8 +135,8 @@ def plan_pages(lens, add, free_list, n_free, table, *, page_size: int, token_cap
     """Pages, slots and positions of a step's new tokens, from the requests'
     lengths (sb_plan_pages).
 
-    lens, add: int32 [requests] (add: new tokens wanted, 0 none, negative
-    releases the request); free_list: int32 [pages], its first n_free (int32
+    lens, add: int32 [requests], one at least (add: new tokens wanted, 0 none,
+    negative releases the request); free_list: int32 [pages], its first n_free (int32
     [1]) entries free page ids; table: int32 [requests, max_pages]. table and
     free_list are updated in place, the rest of the new state is returned, in
     new tensors or in `out`'s, which may be lens and n_free themselves. token_cap:
@@ -258,8 +258,9 @@ def paged_attention(q, k_cache, v_cache, table, lens, q_start, *, max_q: int, ma
     (sb_paged_attention).
 
     q: [tokens, q_heads, head_dim] (rotated), caches: [pages, page_size, kv_heads,
-    head_dim], one type (bfloat16 or float16), head_dim 64, 128 or 256; table:
-    int32 [requests, max_pages]; lens: int32 [requests], the new tokens included;
+    head_dim], one type (bfloat16 or float16), head_dim 64, 128 or 256, strides and
+    addresses as in rope_append; table: int32 [requests, max_pages], one request at
+    least; lens: int32 [requests], the new tokens included;
     q_start: int32 [requests + 1]. A query sees the last `window` positions up
     to its own and the request's first `sinks` (window 0: all up to its own).
     scale: 1 / sqrt(head_dim) by default. max_q, max_kv: upper bounds of a request's queries
