@@ -456,6 +456,56 @@ int64_t sb_sample_workspace(const sb_sample_args *args);
  * run at the same time need one each. */
 sb_status sb_sample_tokens(const sb_sample_args *args, void *workspace, size_t bytes, void *stream);
 
+/* Rows in 8-bit integers, each with a scale of its own:
+ *   scales[r] = max_i |x[r][i]| / 127 (rounded to fp32),
+ *   codes[r][i] = the whole number next to x[r][i] / scales[r] (of two that are
+ * equally near the even one, the quotient taken exactly; -127 .. 127). Columns
+ * from cols up to the next multiple of 16 become 0, so that rows can be
+ * multiplied in pieces of 16. A row of zeros gets the scale 0 and codes 0; one
+ * that holds NaN or an infinity gets the scale NaN and codes 0, and is NaN in
+ * every product. */
+typedef struct {
+  int64_t struct_bytes;     /* sizeof(sb_quantize_args)                             */
+  const void *x;            /* [rows][x_row], the first cols of each row            */
+  void *codes;              /* int8 [rows][codes_row], cols rounded up to 16        */
+  float *scales;            /* [rows]                                               */
+  int64_t x_row, codes_row; /* elements; codes_row a multiple of 16                 */
+  int32_t rows;             /* 0 .. SB_LINEAR_MAX_ROWS                              */
+  int32_t cols;             /* 1 .. SB_LINEAR_MAX_DEPTH                             */
+  int32_t dtype;            /* of x: SB_F32, SB_BF16 or SB_F16                      */
+  int32_t reserved;         /* 0                                                    */
+} sb_quantize_args;
+sb_status sb_quantize_rows(const sb_quantize_args *args, void *stream);
+
+/* The product of quantised rows with quantised weights:
+ *   out[r][n] = x_scale[r] w_scale[n] sum_i x[r][i] w[n][i] + bias[n].
+ * The sums are exact (32-bit integers); the scales are applied in fp32 (fp32
+ * results: fp64) and the result is rounded once to its type. Codes may be
+ * any int8. */
+typedef struct {
+  int64_t struct_bytes;     /* sizeof(sb_linear_args)                               */
+  const void *x;            /* int8 [rows][x_row]                                   */
+  const void *w;            /* int8 [channels][w_row]                               */
+  const float *x_scale;     /* [rows]                                               */
+  const float *w_scale;     /* [channels]                                           */
+  const float *bias;        /* [channels], or NULL: none                            */
+  void *out;                /* [rows][out_row], the first channels of each row      */
+  int64_t x_row, w_row;     /* multiples of 16                                      */
+  int64_t out_row;          /* elements                                             */
+  int32_t rows;             /* 0 .. SB_LINEAR_MAX_ROWS                              */
+  int32_t channels;         /* 1 .. SB_LINEAR_MAX_ROWS                              */
+  int32_t depth;            /* a multiple of 16, up to SB_LINEAR_MAX_DEPTH          */
+  int32_t dtype;            /* of out: SB_F32, SB_BF16 or SB_F16                    */
+} sb_linear_args;
+#define SB_LINEAR_MAX_DEPTH 131056   /* 128 * 128 times it stays below 2^31 */
+#define SB_LINEAR_MAX_ROWS 4194240   /* of x and of w, at most */
+/* Bytes of workspace sb_quantized_linear needs on the current device for these
+ * sizes (pointers are not looked at); -1 if they are invalid. */
+int64_t sb_linear_workspace(const sb_linear_args *args);
+/* workspace: 256-byte aligned, at least sb_linear_workspace bytes (NULL where
+ * that is 0). Calls that may run at the same time need one each. */
+sb_status sb_quantized_linear(const sb_linear_args *args, void *workspace, size_t bytes, void *stream);
+
 /* ------------------------------------------------------------------------
  * Test support. Not part of the decoding interface: these calls expose one
  * decoder step and one candidate slot so that tests can compare them with

@@ -116,3 +116,26 @@ def sample(z, u, T=1.0, top_k=0, top_p=1.0, min_p=0.0):
         if mass > float(u) * float(total):
             break
     return int(i), float(x[i] / T - math.log(total / 2.0 ** 44)) if x[i] < 0 else -math.log(total / 2.0 ** 44)
+
+
+def quantize_rows(x):
+    """(codes [rows, cols rounded up to 16], scales [rows]) of fp64 rows that
+    hold values of at most 24 bits: their quotients with an fp32 scale are no
+    nearer to a border than 2^-33 unless they are on it, and fp64 tells them apart."""
+    x = np.asarray(x, np.float64)
+    codes, scales = np.zeros((x.shape[0], -(-x.shape[1] // 16) * 16), np.int64), np.zeros(x.shape[0], np.float32)
+    for r, row in enumerate(x):
+        if not np.all(np.isfinite(row)):
+            scales[r] = np.nan
+            continue
+        scales[r] = np.float32(np.max(np.abs(row)) / 127)
+        if scales[r] > 0:
+            codes[r, :len(row)] = np.clip(np.rint(row / np.float64(scales[r])), -127, 127)
+    return codes, scales
+
+
+def linear(x, x_scale, w, w_scale, bias=None):
+    """(out, the size of the product alone) in fp64; the sums as whole numbers."""
+    sums = np.asarray(x, np.float64) @ np.asarray(w, np.float64).T   # (below 2^53: exact)
+    out = sums * np.asarray(x_scale, np.float64)[:, None] * np.asarray(w_scale, np.float64)
+    return out + (0 if bias is None else np.asarray(bias, np.float64)), np.abs(out)

@@ -9,7 +9,8 @@ binding and the build script; PyTorch only provides device memory and streams.
 from .decoder import (Decoder, Hypothesis, decoder_for_workload, group_by_input, inputs_to_device,
                       weights_to_device)
 
-_SERVING = ("PagePlan", "paged_attention", "plan_pages", "rope_append", "rope_frequencies", "sample_tokens")
+_SERVING = ("PagePlan", "int8_linear", "paged_attention", "plan_pages", "quantize_rows", "rope_append", "rope_frequencies",
+            "sample_tokens")
 
 __all__ = ["Decoder", "Hypothesis", "decoder_for_workload", "group_by_input", "inputs_to_device",
            "weights_to_device", *_SERVING]

@@ -27,6 +27,7 @@ SB_RULE_PAPER, SB_RULE_FAIRSEQ = 0, 1
 SB_F32, SB_BF16, SB_F16 = 0, 1, 2
 SB_ROPE_HALF, SB_ROPE_INTERLEAVED = 0, 1
 SB_PLAN_MAX_REQUESTS, SB_SAMPLE_MAX_VOCAB = 8192, 262144
+SB_LINEAR_MAX_DEPTH, SB_LINEAR_MAX_ROWS = 131056, 4194240
 SCHEDULERS = {"fixed": SB_FIXED, "var_batch": SB_VAR_BATCH, "var_stream": SB_VAR_STREAM,
               "var_fifo": SB_VAR_FIFO, "fixed_stream": SB_FIXED_STREAM, "var_cap": SB_VAR_CAP}
 # Scheduler names that also pick the Fairseq finalization rule.
@@ -78,6 +79,8 @@ PLAN_ARGS = _Args("q11Pq6i")
 ROPE_ARGS = _Args("q9P14q9if")
 ATTENTION_ARGS = _Args("q7P11q13if")
 SAMPLE_ARGS = _Args("q8Pq4i")
+QUANTIZE_ARGS = _Args("q3P2q4i")
+LINEAR_ARGS = _Args("q6P3q4i")
 
 
 class StreambeamError(RuntimeError):
@@ -130,6 +133,9 @@ def lib():
         "sb_paged_attention": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
         "sb_sample_workspace": (c_int64, [c_char_p]),
         "sb_sample_tokens": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
+        "sb_quantize_rows": (c_int32, [c_char_p, c_void_p]),
+        "sb_linear_workspace": (c_int64, [c_char_p]),
+        "sb_quantized_linear": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
         "sb_destroy": (c_int32, [c_void_p]),
         "sb_last_error": (c_char_p, [c_void_p]),
         "sb_status_string": (c_char_p, [c_int32]),

@@ -96,6 +96,20 @@ sb_status check_sample(const sb_sample_args *a, const char *call) {
   return SB_OK;
 }
 
+sb_status check_linear(const sb_linear_args *a, const char *call) {
+  REFUSE_IF(!a, SB_E_INVALID_ARG, "no arguments");
+  REFUSE_IF(a->struct_bytes != (int64_t)sizeof(*a), SB_E_INVALID_ARG, "struct_bytes is not this library's");
+  REFUSE_IF(a->dtype != SB_F32 && a->dtype != SB_BF16 && a->dtype != SB_F16, SB_E_UNSUPPORTED, "unknown dtype");
+  REFUSE_IF(a->rows < 0 || a->channels < 1 || a->depth < 1, SB_E_INVALID_ARG, "rows < 0, channels < 1 or depth < 1");
+  REFUSE_IF(a->rows > SB_LINEAR_MAX_ROWS || a->channels > SB_LINEAR_MAX_ROWS || a->depth > SB_LINEAR_MAX_DEPTH, SB_E_UNSUPPORTED,
+            "rows or channels above SB_LINEAR_MAX_ROWS, or depth above SB_LINEAR_MAX_DEPTH");
+  REFUSE_IF(a->depth % 16, SB_E_UNSUPPORTED, "depth is no multiple of 16");
+  REFUSE_IF((a->rows > 1 && (a->x_row < a->depth || a->out_row < a->channels)) || (a->channels > 1 && a->w_row < a->depth),
+            SB_E_INVALID_ARG, "rows of x, w or out overlap");
+  REFUSE_IF((a->rows > 1 && a->x_row % 16) || (a->channels > 1 && a->w_row % 16), SB_E_UNSUPPORTED, "a row stride is no multiple of 16");
+  return SB_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -201,6 +215,54 @@ sb_status sb_sample_tokens(const sb_sample_args *a, void *workspace, size_t byte
   const hipError_t e = compute_units(n_cu);
   if (e != hipSuccess) return launched(e, call);
   return launched(launch_sample(*a, need ? workspace : nullptr, n_cu, static_cast<hipStream_t>(stream)), call);
+}
+
+sb_status sb_quantize_rows(const sb_quantize_args *a, void *stream) {
+  const char *call = "sb_quantize_rows";
+  REFUSE_IF(!a, SB_E_INVALID_ARG, "no arguments");
+  REFUSE_IF(a->struct_bytes != (int64_t)sizeof(*a) || a->reserved, SB_E_INVALID_ARG, "struct_bytes is not this library's");
+  REFUSE_IF(a->dtype != SB_F32 && a->dtype != SB_BF16 && a->dtype != SB_F16, SB_E_UNSUPPORTED, "unknown dtype");
+  REFUSE_IF(a->rows < 0 || a->cols < 1, SB_E_INVALID_ARG, "rows < 0 or cols < 1");
+  REFUSE_IF(a->rows > SB_LINEAR_MAX_ROWS || a->cols > SB_LINEAR_MAX_DEPTH, SB_E_UNSUPPORTED,
+            "rows above SB_LINEAR_MAX_ROWS or cols above SB_LINEAR_MAX_DEPTH");
+  REFUSE_IF(a->rows > 1 && a->x_row < 0, SB_E_INVALID_ARG, "x_row < 0");
+  REFUSE_IF(a->rows > 1 && a->codes_row < (a->cols + 15) / 16 * 16, SB_E_INVALID_ARG, "codes_row < cols rounded up to 16");
+  REFUSE_IF(a->rows > 1 && a->codes_row % 16, SB_E_UNSUPPORTED, "codes_row is no multiple of 16");
+  if (a->rows == 0) return SB_OK;
+  REFUSE_IF(!a->x || !a->codes || !a->scales, SB_E_INVALID_ARG, "a pointer is missing");
+  REFUSE_IF(!aligned(a->x, a->dtype == SB_F32 ? 4 : 2) || !aligned(a->scales, 4), SB_E_INVALID_ARG, "an array is not aligned to its type");
+  REFUSE_IF(!aligned(a->codes, 16), SB_E_UNSUPPORTED, "codes are not 16-byte aligned");
+  return launched(launch_quantize(*a, static_cast<hipStream_t>(stream)), call);
+}
+
+int64_t sb_linear_workspace(const sb_linear_args *a) {
+  const char *call = "sb_linear_workspace";
+  if (check_linear(a, call) != SB_OK) return -1;
+  int n_cu = 0;
+  const hipError_t e = compute_units(n_cu);
+  if (e != hipSuccess) {
+    launched(e, call);
+    return -1;
+  }
+  return linear_workspace(*a, n_cu);
+}
+
+sb_status sb_quantized_linear(const sb_linear_args *a, void *workspace, size_t bytes, void *stream) {
+  const char *call = "sb_quantized_linear";
+  const sb_status st = check_linear(a, call);
+  if (st != SB_OK) return st;
+  if (a->rows == 0) return SB_OK;
+  REFUSE_IF(!a->x || !a->w || !a->x_scale || !a->w_scale || !a->out, SB_E_INVALID_ARG, "a pointer is missing");
+  REFUSE_IF(!aligned(a->x_scale, 4) || !aligned(a->w_scale, 4) || !aligned(a->bias, 4) || !aligned(a->out, a->dtype == SB_F32 ? 4 : 2),
+            SB_E_INVALID_ARG, "an array is not aligned to its type");
+  REFUSE_IF(!aligned(a->x, 16) || !aligned(a->w, 16), SB_E_UNSUPPORTED, "x or w is not 16-byte aligned");
+  int n_cu = 0;
+  const hipError_t e = compute_units(n_cu);
+  if (e != hipSuccess) return launched(e, call);
+  const int64_t need = linear_workspace(*a, n_cu);
+  REFUSE_IF(need && (!workspace || !aligned(workspace, 256) || bytes < (size_t)need), SB_E_WORKSPACE,
+            "workspace missing, misaligned or smaller than sb_linear_workspace");
+  return launched(launch_linear(*a, n_cu, workspace, static_cast<hipStream_t>(stream)), call);
 }
 
 }  // extern "C"

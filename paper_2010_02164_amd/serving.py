@@ -330,3 +330,81 @@ def sample_tokens(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=
     _call(L.sb_sample_tokens, "sb_sample_tokens", i, args, None if work is None else work.data_ptr(), max(need, 0))
     _written((tokens, logprobs))
     return tokens, logprobs
+
+
+def _rows(t, name, i, types, cols=None):
+    """A matrix with contiguous rows: its shape and row stride."""
+    shape = t.shape
+    if len(shape) != 2 or t.dtype not in types or t.get_device() != i or (shape[1] > 1 and t.stride(1) != 1):
+        _refuse(f"{name} must be a matrix of {' or '.join(str(x) for x in types)} on cuda:{i} with contiguous rows")
+    if cols is not None and shape[1] != cols:
+        _refuse(f"{name} must have {cols} columns")
+    return shape, t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def quantize_rows(x, *, out=None):
+    """(codes int8 [rows, cols rounded up to 16], scales float32 [rows]): rows in
+    8-bit integers (sb_quantize_rows).
+
+    x: [rows, cols], float32, bfloat16 or float16, contiguous rows. A row's scale
+    is its largest size / 127, its codes are the whole numbers next to x / scale,
+    and 0 behind the last column. A row with a value that is not finite gets the
+    scale NaN. Tokens are quantised so for int8_linear, and the rows of a weight
+    matrix [channels, depth]. out: (codes, scales) to write to."""
+    i = _device(x, "x")
+    (R, C), row = _rows(x, "x", i, _LOGITS)
+    if C < 1:
+        _refuse("x must have a column")
+    _no_grad(x, *(out or ()))
+    wide = (C + 15) // 16 * 16
+    if out is None:
+        codes, scales = torch.empty((R, wide), dtype=torch.int8, device=i), torch.empty(R, dtype=torch.float32, device=i)
+        crow = wide
+    else:
+        codes, scales = out
+        (Rc, _), crow = _rows(codes, "out codes", i, (torch.int8,), wide)
+        if Rc != R:
+            _refuse("out codes must have x's rows")
+        _apart(codes, "out codes")
+    args = N.QUANTIZE_ARGS.pack(N.QUANTIZE_ARGS.size, x.data_ptr(), codes.data_ptr(), _whole(scales, "scales", torch.float32, i, (R,)),
+                                row, crow, R, C, _LOGITS[x.dtype], 0)
+    _call(N.lib().sb_quantize_rows, "sb_quantize_rows", i, args)
+    _written((codes, scales))
+    return codes, scales
+
+
+def int8_linear(x, x_scale, w, w_scale, *, bias=None, dtype=torch.bfloat16, out=None):
+    """x_scale[:, None] * (x @ w.T) * w_scale + bias of quantised rows
+    (sb_quantized_linear): [rows, channels].
+
+    x: int8 [rows, depth], w: int8 [channels, depth], contiguous rows at
+    addresses and strides that are multiples of 16, depth a multiple of 16
+    (quantize_rows gives such); x_scale: float32 [rows]; w_scale, bias: float32
+    [channels]. The sums are exact; the result is float32, bfloat16 or float16
+    (dtype, or out's)."""
+    i, int8, f32 = _device(x, "x"), (torch.int8,), torch.float32
+    (R, K), x_row = _rows(x, "x", i, int8)
+    (C, _), w_row = _rows(w, "w", i, int8, K)
+    _no_grad(x_scale, w_scale, bias, out)
+    if out is None:
+        if dtype not in _LOGITS:
+            _refuse("dtype must be float32, bfloat16 or float16")
+        out, out_row = torch.empty((R, C), dtype=dtype, device=i), C
+    else:
+        (Ro, _), out_row = _rows(out, "out", i, _LOGITS, C)
+        if Ro != R:
+            _refuse("out must have x's rows")
+        _apart(out, "out")
+    args = N.LINEAR_ARGS.pack(
+        N.LINEAR_ARGS.size, x.data_ptr(), w.data_ptr(), _whole(x_scale, "x_scale", f32, i, (R,)), _whole(w_scale, "w_scale", f32, i, (C,)),
+        0 if bias is None else _whole(bias, "bias", f32, i, (C,)), out.data_ptr(), x_row, w_row, out_row, R, C, K, _LOGITS[out.dtype])
+    L = N.lib()
+    if i == _current():
+        need = L.sb_linear_workspace(args)
+    else:
+        with torch.cuda.device(i):
+            need = L.sb_linear_workspace(args)
+    work = torch.empty(need, dtype=torch.uint8, device=i) if need > 0 else None   # (below 0: refused by the call itself)
+    _call(L.sb_quantized_linear, "sb_quantized_linear", i, args, None if work is None else work.data_ptr(), max(need, 0))
+    _written((out,))
+    return out
