@@ -506,6 +506,38 @@ int64_t sb_linear_workspace(const sb_linear_args *args);
  * that is 0). Calls that may run at the same time need one each. */
 sb_status sb_quantized_linear(const sb_linear_args *args, void *workspace, size_t bytes, void *stream);
 
+/* Attention of new tokens over a prefix that the requests of a group share, and
+ * over each request's own tokens behind it:
+ *   out[t] = sum_j softmax_j(scale q[t] . k_j) v_j
+ * over the keys of the prefix of t's group, which every query of the group sees,
+ * and those of its request's own cache as in sb_paged_attention without a
+ * window: own.lens, own.table, own.q_start count and place the tokens behind the
+ * prefix alone. Requests group_start[g] .. group_start[g + 1] - 1 are those of
+ * group g; requests of no group have no prefix (group_start is clipped to
+ * 0 .. n_requests). A query that sees no key gets 0. Each prefix is read once for
+ * all queries of its group. fp32 scores, statistics and sums; weights go into
+ * the product with the values as sb_paged_attention says, by the number of rows
+ * that read the same keys. max_prefix (an upper bound of prefix_lens) chooses
+ * kernels and splits as max_q and max_kv do. own.window and own.sinks are 0. */
+typedef struct {
+  int64_t struct_bytes;          /* sizeof(sb_shared_args)                               */
+  sb_attention_args own;         /* the step's queries and the requests' own tokens      */
+  const int32_t *prefix_table;   /* [n_groups][prefix_stride]                            */
+  const int32_t *prefix_lens;    /* [n_groups]                                           */
+  const int32_t *group_start;    /* [n_groups + 1], ascending from 0                     */
+  int64_t prefix_stride;         /* >= prefix_pages                                      */
+  int32_t n_groups;              /* >= 1                                                 */
+  int32_t prefix_pages;          /* columns of prefix_table in use, >= 1                 */
+  int32_t max_prefix;            /* >= 0                                                 */
+  int32_t reserved;              /* 0                                                    */
+} sb_shared_args;
+/* Bytes of workspace sb_shared_attention needs on the current device for these
+ * sizes (pointers but own are not looked at); -1 if they are invalid. */
+int64_t sb_shared_workspace(const sb_shared_args *args);
+/* workspace: 256-byte aligned, at least sb_shared_workspace bytes. Calls that may
+ * run at the same time need one each. */
+sb_status sb_shared_attention(const sb_shared_args *args, void *workspace, size_t bytes, void *stream);
+
 /* ------------------------------------------------------------------------
  * Test support. Not part of the decoding interface: these calls expose one
  * decoder step and one candidate slot so that tests can compare them with

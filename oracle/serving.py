@@ -80,6 +80,37 @@ def attention(q, k_cache, v_cache, table, lens, q_start, window, sinks, scale):
     return out, size, big
 
 
+def shared_attention(q, k_cache, v_cache, prefix_table, prefix_lens, group_start, table, lens, q_start, scale):
+    """As attention, over the group's prefix and the request's own tokens."""
+    q, k_cache, v_cache = (np.asarray(t, np.float64) for t in (q, k_cache, v_cache))
+    T, Hq, D = q.shape
+    pages, page, Hkv, _ = k_cache.shape
+    out, size, big = (np.full(q.shape, np.nan) for _ in range(3))
+    for b, n in enumerate(lens):
+        m = q_start[b + 1] - q_start[b]
+        ahead = []
+        for g, length in enumerate(prefix_lens):
+            if group_start[g] <= b < group_start[g + 1]:
+                ahead = [(prefix_table[g][j // page], j % page) for j in range(length)]
+        for t in range(q_start[b], q_start[b + 1]):
+            p = n - m + t - q_start[b]
+            out[t] = size[t] = big[t] = 0
+            at = [i for i in ahead + [(table[b][j // page], j % page) for j in range(p + 1)] if 0 <= i[0] < pages]
+            if not at:
+                continue
+            i, j = np.array(at).T
+            K, V = k_cache[i, j], v_cache[i, j]   # [keys, Hkv, D]
+            for h in range(Hq):
+                hk = h // (Hq // Hkv)
+                s = K[:, hk] @ q[t, h] * scale
+                w = np.exp(s - s.max())
+                w /= w.sum()
+                out[t, h] = w @ V[:, hk]
+                size[t, h] = w @ np.abs(V[:, hk])
+                big[t, h] = np.max(np.abs(K[:, hk]) @ np.abs(q[t, h]))
+    return out, size, big
+
+
 def sample(z, u, T=1.0, top_k=0, top_p=1.0, min_p=0.0):
     """(token, logprob) of one row."""
     z = np.asarray(z, np.float64).copy()

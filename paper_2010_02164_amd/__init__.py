@@ -10,7 +10,7 @@ from .decoder import (Decoder, Hypothesis, decoder_for_workload, group_by_input,
                       weights_to_device)
 
 _SERVING = ("PagePlan", "int8_linear", "paged_attention", "plan_pages", "quantize_rows", "rope_append", "rope_frequencies",
-            "sample_tokens")
+            "sample_tokens", "shared_attention")
 
 __all__ = ["Decoder", "Hypothesis", "decoder_for_workload", "group_by_input", "inputs_to_device",
            "weights_to_device", *_SERVING]

@@ -79,6 +79,7 @@ PLAN_ARGS = _Args("q11Pq6i")
 ROPE_ARGS = _Args("q9P14q9if")
 ATTENTION_ARGS = _Args("q7P11q13if")
 SAMPLE_ARGS = _Args("q8Pq4i")
+SHARED_ARGS = _Args("q" + ATTENTION_ARGS.format + "3Pq4i")
 QUANTIZE_ARGS = _Args("q3P2q4i")
 LINEAR_ARGS = _Args("q6P3q4i")
 
@@ -133,6 +134,8 @@ def lib():
         "sb_paged_attention": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
         "sb_sample_workspace": (c_int64, [c_char_p]),
         "sb_sample_tokens": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
+        "sb_shared_workspace": (c_int64, [c_char_p]),
+        "sb_shared_attention": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
         "sb_quantize_rows": (c_int32, [c_char_p, c_void_p]),
         "sb_linear_workspace": (c_int64, [c_char_p]),
         "sb_quantized_linear": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),

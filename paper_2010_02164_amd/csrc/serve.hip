@@ -86,6 +86,26 @@ sb_status check_attention(const sb_attention_args *a, const char *call, bool poi
   return SB_OK;
 }
 
+sb_status check_shared(const sb_shared_args *x, const char *call, bool pointers) {
+  REFUSE_IF(!x, SB_E_INVALID_ARG, "no arguments");
+  REFUSE_IF(x->struct_bytes != (int64_t)sizeof(*x) || x->reserved, SB_E_INVALID_ARG, "struct_bytes is not this library's");
+  const sb_status st = check_attention(&x->own, call, pointers);
+  if (st != SB_OK) return st;
+  const sb_attention_args *a = &x->own;
+  REFUSE_IF(a->window || a->sinks, SB_E_INVALID_ARG, "window or sinks is not 0");
+  REFUSE_IF(x->n_groups < 1 || x->prefix_pages < 1 || x->max_prefix < 0, SB_E_INVALID_ARG, "n_groups, prefix_pages < 1 or max_prefix < 0");
+  REFUSE_IF((int64_t)x->prefix_pages * a->page_size > SB_ATTENTION_MAX_KEYS, SB_E_UNSUPPORTED,
+            "prefix_pages times page_size is above SB_ATTENTION_MAX_KEYS");
+  REFUSE_IF(x->prefix_stride < x->prefix_pages, SB_E_INVALID_ARG, "prefix_stride < prefix_pages");
+  REFUSE_IF((int64_t)a->n_tokens * a->q_heads / 8 + ((int64_t)x->n_groups + a->n_requests) * a->kv_heads > (1 << 23), SB_E_UNSUPPORTED,
+            "n_tokens times q_heads / 8 and groups and requests times kv_heads are more than 2^23");
+  if (!pointers) return SB_OK;
+  REFUSE_IF(!x->prefix_table || !x->prefix_lens || !x->group_start, SB_E_INVALID_ARG, "a pointer is missing");
+  REFUSE_IF(!aligned(x->prefix_table, 4) || !aligned(x->prefix_lens, 4) || !aligned(x->group_start, 4), SB_E_INVALID_ARG,
+            "an array is not aligned to its type");
+  return SB_OK;
+}
+
 sb_status check_sample(const sb_sample_args *a, const char *call) {
   REFUSE_IF(!a, SB_E_INVALID_ARG, "no arguments");
   REFUSE_IF(a->struct_bytes != (int64_t)sizeof(*a) || a->reserved, SB_E_INVALID_ARG, "struct_bytes is not this library's");
@@ -192,6 +212,31 @@ sb_status sb_paged_attention(const sb_attention_args *a, void *workspace, size_t
   REFUSE_IF(need && (!workspace || !aligned(workspace, 256) || bytes < (size_t)need), SB_E_WORKSPACE,
             "workspace missing, misaligned or smaller than sb_attention_workspace");
   return launched(launch_paged_attention(*a, n_cu, workspace, static_cast<hipStream_t>(stream)), call);
+}
+
+int64_t sb_shared_workspace(const sb_shared_args *a) {
+  const char *call = "sb_shared_workspace";
+  if (check_shared(a, call, false) != SB_OK) return -1;
+  int n_cu = 0;
+  const hipError_t e = compute_units(n_cu);
+  if (e != hipSuccess) {
+    launched(e, call);
+    return -1;
+  }
+  return shared_workspace(*a, n_cu);
+}
+
+sb_status sb_shared_attention(const sb_shared_args *a, void *workspace, size_t bytes, void *stream) {
+  const char *call = "sb_shared_attention";
+  const sb_status st = check_shared(a, call, true);
+  if (st != SB_OK) return st;
+  if (a->own.n_tokens == 0) return SB_OK;
+  int n_cu = 0;
+  const hipError_t e = compute_units(n_cu);
+  if (e != hipSuccess) return launched(e, call);
+  REFUSE_IF(!workspace || !aligned(workspace, 256) || bytes < (size_t)shared_workspace(*a, n_cu), SB_E_WORKSPACE,
+            "workspace missing, misaligned or smaller than sb_shared_workspace");
+  return launched(launch_shared_attention(*a, n_cu, workspace, static_cast<hipStream_t>(stream)), call);
 }
 
 int64_t sb_sample_workspace(const sb_sample_args *a) {

@@ -46,6 +46,17 @@ def _call(fn, where, i, *args):
         raise N.StreambeamError(status, where, msg.decode() if msg else "")
 
 
+def _call_with_workspace(fn, ask, where, i, args):
+    """fn(args, workspace, bytes, stream) with the workspace that ask(args) says."""
+    if i == _current():
+        need = ask(args)
+    else:
+        with torch.cuda.device(i):
+            need = ask(args)
+    work = torch.empty(need, dtype=torch.uint8, device=i) if need > 0 else None   # (below 0: refused by the call itself)
+    _call(fn, where, i, args, None if work is None else work.data_ptr(), max(need, 0))
+
+
 # The checks read each property of a tensor once: a read takes 0.1 us, a call
 # with single tokens 10 to 15.
 def _whole(t, name, dtype, i, shape):
@@ -118,6 +129,16 @@ def _table(t, i):
     if len(shape) != 2 or t.dtype != torch.int32 or t.get_device() != i or (shape[1] > 1 and t.stride(1) != 1):
         _refuse(f"table must be an int32 tensor [requests, max_pages] on cuda:{i} with contiguous rows")
     return shape, t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _attended(out, dtype, i, T, Hq, D):
+    """Where an attention's result goes: out, or a new tensor, and its strides."""
+    if out is None:
+        return torch.empty((T, Hq, D), dtype=dtype, device=i), (Hq * D, D)
+    (_, Ho, _), strides = _heads(out, "out", dtype, i, T, D)
+    if Ho != Hq:
+        _refuse("out must have q's heads")
+    return _apart(out, "out"), strides
 
 
 class PagePlan(NamedTuple):
@@ -299,6 +320,42 @@ def paged_attention(q, k_cache, v_cache, table, lens, q_start, *, max_q: int, ma
     return out
 
 
+def shared_attention(q, k_cache, v_cache, prefix_table, prefix_lens, group_start, table, lens, q_start, *, max_q: int, max_kv: int,
+                     max_prefix: int, scale: Optional[float] = None, out=None):
+    """Causal attention of a step's queries over a prefix that the requests of a
+    group share, read once for all of them, and over their own tokens behind it
+    (sb_shared_attention).
+
+    prefix_table: int32 [groups, max_pages], one group at least; prefix_lens: int32
+    [groups]; group_start: int32 [groups + 1]: requests group_start[g] ..
+    group_start[g + 1] follow prefix g (the hypotheses of one source, the requests
+    behind one instruction), requests of no group follow none. The others as in
+    paged_attention, with lens and table of the tokens behind the prefix alone.
+    max_q, max_kv, max_prefix: upper bounds of a request's queries, of lens and of
+    prefix_lens, for the choice of kernels and splits only."""
+    i, dtype = _device(q, "q"), q.dtype
+    if dtype not in _HALVES:
+        _refuse("q must be bfloat16 or float16")
+    _no_grad(q, k_cache, v_cache, out)
+    (T, Hq, D), qs = _heads(q, "q", dtype, i)
+    (pages, page_size, Hkv, _), kc, vc = _caches(k_cache, v_cache, dtype, i, None, D)
+    (B, width), row = _table(table, i)
+    (G, prefix_width), prefix_row = _table(prefix_table, i)
+    out, os_ = _attended(out, dtype, i, T, Hq, D)
+    i32 = torch.int32
+    args = N.SHARED_ARGS.pack(
+        N.SHARED_ARGS.size, N.ATTENTION_ARGS.size, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table.data_ptr(),
+        _whole(lens, "lens", i32, i, (B,)), _whole(q_start, "q_start", i32, i, (B + 1,)), out.data_ptr(),
+        qs[0], qs[1], os_[0], os_[1], kc[0], kc[1], kc[2], vc[0], vc[1], vc[2], row,
+        T, B, Hq, Hkv, D, _HALVES[dtype], pages, page_size, width, 0, 0, max_q, max_kv, 1.0 / math.sqrt(D) if scale is None else scale,
+        prefix_table.data_ptr(), _whole(prefix_lens, "prefix_lens", i32, i, (G,)), _whole(group_start, "group_start", i32, i, (G + 1,)),
+        prefix_row, G, prefix_width, max_prefix, 0)
+    L = N.lib()
+    _call_with_workspace(L.sb_shared_attention, L.sb_shared_workspace, "sb_shared_attention", i, args)
+    _written((out,))
+    return out
+
+
 def sample_tokens(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, out=None):
     """(tokens int32 [rows], logprobs float32 [rows]): one token per row of
     logits, drawn with the given numbers (sb_sample_tokens).
@@ -399,12 +456,6 @@ def int8_linear(x, x_scale, w, w_scale, *, bias=None, dtype=torch.bfloat16, out=
         N.LINEAR_ARGS.size, x.data_ptr(), w.data_ptr(), _whole(x_scale, "x_scale", f32, i, (R,)), _whole(w_scale, "w_scale", f32, i, (C,)),
         0 if bias is None else _whole(bias, "bias", f32, i, (C,)), out.data_ptr(), x_row, w_row, out_row, R, C, K, _LOGITS[out.dtype])
     L = N.lib()
-    if i == _current():
-        need = L.sb_linear_workspace(args)
-    else:
-        with torch.cuda.device(i):
-            need = L.sb_linear_workspace(args)
-    work = torch.empty(need, dtype=torch.uint8, device=i) if need > 0 else None   # (below 0: refused by the call itself)
-    _call(L.sb_quantized_linear, "sb_quantized_linear", i, args, None if work is None else work.data_ptr(), max(need, 0))
+    _call_with_workspace(L.sb_quantized_linear, L.sb_linear_workspace, "sb_quantized_linear", i, args)
     _written((out,))
     return out

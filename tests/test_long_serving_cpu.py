@@ -19,7 +19,14 @@ QUANTIZE = dict(bytes=N.QUANTIZE_ARGS.size, x=PTR, codes=PTR, scales=PTR, x_row=
                 reserved=0)
 LINEAR = dict(bytes=N.LINEAR_ARGS.size, x=PTR, w=PTR, x_scale=PTR, w_scale=PTR, bias=PTR, out=PTR, x_row=112, w_row=128, out_row=50, rows=3,
               channels=50, depth=112, dtype=N.SB_BF16)
+ATTN = dict(own_bytes=N.ATTENTION_ARGS.size, q=PTR, k_cache=PTR, v_cache=PTR, table=PTR, lens=PTR, q_start=PTR, out=PTR, q_token=512, q_head=128,
+            out_token=512, out_head=128, kc_page=4096, kc_slot=256, kc_head=128, vc_page=4096, vc_slot=256, vc_head=128, table_stride=8,
+            n_tokens=3, n_requests=2, q_heads=4, kv_heads=2, head_dim=128, dtype=N.SB_BF16, n_pages=32, page_size=16, max_pages=8, window=0,
+            sinks=0, max_q=2, max_kv=100, scale=0.1)
+SHARED = dict(bytes=N.SHARED_ARGS.size, **ATTN, prefix_table=PTR, prefix_lens=PTR, group_start=PTR, prefix_stride=9, n_groups=2, prefix_pages=8,
+              max_prefix=100, reserved=0)
 CALLS = {   # call -> (its struct, the packer, the call's arguments, whether it takes a workspace)
+    "sb_shared_attention": ("sb_shared_args", N.SHARED_ARGS, SHARED, True),
     "sb_quantize_rows": ("sb_quantize_args", N.QUANTIZE_ARGS, QUANTIZE, False),
     "sb_quantized_linear": ("sb_linear_args", N.LINEAR_ARGS, LINEAR, True),
 }
@@ -27,12 +34,15 @@ CALLS = {   # call -> (its struct, the packer, the call's arguments, whether it 
 
 @pytest.mark.parametrize("call", sorted(CALLS))
 def test_packed_arguments_follow_the_header(call):
-    """The fields of the header's struct, in their order and types."""
+    """The fields of the header's struct, in their order and types (of a struct
+    within it, its fields)."""
     name, packer, values, _ = CALLS[call]
     with open(N.HEADER) as f:
-        body = re.search(r"typedef struct \{([^}]*)\} " + name + ";", f.read()).group(1)
+        text = re.sub(r"/\*.*?\*/", "", f.read(), flags=re.S)
+    structs = {m.group(2): m.group(1) for m in re.finditer(r"typedef struct \{([^}]*)\} (\w+);", text)}
+    body = re.sub(r"sb_attention_args own;", structs["sb_attention_args"].replace("struct_bytes", "own_bytes"), structs[name])
     fields, codes = [], ""
-    for decl in re.sub(r"/\*.*?\*/", "", body, flags=re.S).split(";"):
+    for decl in body.split(";"):
         decl = decl.strip()
         if not decl:
             continue
@@ -52,6 +62,21 @@ def run(L, call, over):
     if status != N.SB_OK:
         assert call in L.sb_last_error(None).decode()
     return status
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(bytes=8), INVALID), (dict(own_bytes=8), INVALID), (dict(reserved=1), INVALID), (dict(dtype=N.SB_F32), UNSUPPORTED),
+    (dict(head_dim=96), UNSUPPORTED), (dict(n_requests=0), INVALID), (dict(n_tokens=-1), INVALID), (dict(q_heads=5), INVALID),
+    (dict(page_size=0), INVALID), (dict(window=1), INVALID), (dict(sinks=1), INVALID), (dict(max_q=-1), INVALID), (dict(scale=math.inf), INVALID),
+    (dict(n_groups=0), INVALID), (dict(prefix_pages=0), INVALID), (dict(max_prefix=-1), INVALID), (dict(prefix_stride=7), INVALID),
+    (dict(prefix_pages=1 << 27, prefix_stride=1 << 27), UNSUPPORTED), (dict(n_tokens=1 << 25), UNSUPPORTED), (dict(n_groups=1 << 23), UNSUPPORTED),
+    (dict(n_requests=1 << 23), UNSUPPORTED), (dict(q_head=124), UNSUPPORTED), (dict(lens=0), INVALID), (dict(prefix_table=0), INVALID),
+    (dict(prefix_lens=0), INVALID), (dict(group_start=0), INVALID), (dict(prefix_table=PTR + 2), INVALID), (dict(out=PTR + 8), UNSUPPORTED),
+    (dict(group_start=PTR + 1), INVALID)])
+def test_shared_attention_refusals(native_lib, over, status):
+    assert run(native_lib, "sb_shared_attention", over) == status
+    if not {"lens", "out", "prefix_table", "prefix_lens", "group_start"} & set(over):
+        assert native_lib.sb_shared_workspace(N.SHARED_ARGS.pack(*dict(SHARED, **over).values())) == -1
 
 
 @pytest.mark.parametrize("over,status", [
@@ -80,11 +105,14 @@ def test_linear_refusals(native_lib, over, status):
 def test_nothing_to_do_needs_no_gpu(native_lib):
     assert run(native_lib, "sb_quantize_rows", dict(rows=0, x=0, codes=0, scales=0)) == N.SB_OK
     assert run(native_lib, "sb_quantized_linear", dict(rows=0, x=0, out=0)) == N.SB_OK
+    assert run(native_lib, "sb_shared_attention", dict(n_tokens=0, q=0, out=0)) == N.SB_OK
     # Strides of a single row are not looked at.
     assert run(native_lib, "sb_quantized_linear", dict(rows=0, x_row=7, out_row=1)) == N.SB_OK
 
 
 def test_missing_arguments(native_lib):
+    assert native_lib.sb_shared_workspace(None) == -1
+    assert native_lib.sb_shared_attention(None, None, 0, None) == INVALID
     assert native_lib.sb_quantize_rows(None, None) == INVALID
     assert native_lib.sb_linear_workspace(None) == -1
     assert native_lib.sb_quantized_linear(None, None, 0, None) == INVALID
@@ -92,6 +120,9 @@ def test_missing_arguments(native_lib):
 
 def test_tensors_must_be_on_a_gpu():
     x, f = torch.zeros(2, 16, dtype=torch.int8), torch.zeros(2)
+    h, i = torch.zeros(2, 1, 64, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(ValueError, match="GPU"):
+        sb.shared_attention(h, h[None], h[None], i[None], i, i, i[None], i, i, max_q=1, max_kv=1, max_prefix=1)
     with pytest.raises(ValueError, match="GPU"):
         sb.quantize_rows(torch.zeros(2, 5))
     with pytest.raises(ValueError, match="GPU"):
@@ -105,6 +136,19 @@ def test_oracle_quantize_by_hand():
     assert codes.shape == (4, 16) and np.array_equal(scales[:3], [1, 0, 2]) and np.isnan(scales[3])
     assert codes[0, :6].tolist() == [127, -64, 0, 2, -2, 0] and not codes[1].any() and not codes[3].any()
     assert codes[2, :5].tolist() == [-127, 0, 2, 3, 1]   # halves to the even one
+
+
+def test_oracle_shared_attention_by_hand():
+    # One head of one value, pages of 2: a prefix of one token on page 2 before
+    # requests 0 and 1, whose own tokens are on pages 0 and 1; 2 has no prefix.
+    k = np.zeros((3, 2, 1, 1))
+    k[0, 1] = math.log(3)
+    v = np.array([[8.0, 1.0], [4.0, 9.0], [2.0, 7.0]]).reshape(3, 2, 1, 1)
+    args = (np.ones((4, 1, 1)), k, v, [[2, 9]], [1], [0, 2], [[0], [1], [1]], [2, 1, 1], [0, 2, 3, 4], 1.0)
+    out, *_ = oracle.shared_attention(*args)
+    assert np.allclose(out[:, 0, 0], [(2 + 8) / 2, (2 + 8 + 3) / 5, (2 + 4) / 2, 4])
+    out, *_ = oracle.shared_attention(*args[:7], [1, 0, 0], *args[8:])   # fewer tokens than queries
+    assert np.allclose(out[:, 0, 0], [2, (2 + 8) / 2, 2, 0])
 
 
 def test_oracle_linear_by_hand():
