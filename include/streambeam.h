@@ -538,6 +538,98 @@ int64_t sb_shared_workspace(const sb_shared_args *args);
  * run at the same time need one each. */
 sb_status sb_shared_attention(const sb_shared_args *args, void *workspace, size_t bytes, void *stream);
 
+/* Bounds of cached keys by page: for every page that holds one of a request's
+ * new tokens (its last q_start[b + 1] - q_start[b] positions of lens[b]),
+ *   bounds[page][0][h][i] = the smallest, bounds[page][1][h][i] = the largest
+ * of value i of head h over the page's positions below lens[b]; NaN where one of
+ * them is. Other pages' bounds stay as they are. Pages outside the cache are
+ * skipped; one that two requests' new tokens went to is either's. max_q (an
+ * upper bound of a request's new tokens) only chooses the grid. */
+typedef struct {
+  int64_t struct_bytes;     /* sizeof(sb_bounds_args)                               */
+  const void *k_cache;      /* [n_pages][page_size][kv_heads][head_dim]             */
+  const int32_t *table;     /* [n_requests][table_stride]                           */
+  const int32_t *lens;      /* [n_requests] tokens cached, the new ones included    */
+  const int32_t *q_start;   /* [n_requests + 1]                                     */
+  void *bounds;             /* [n_pages][2][kv_heads][head_dim], contiguous         */
+  int64_t kc_page, kc_slot, kc_head, table_stride;
+  int32_t n_requests;       /* >= 1                                                 */
+  int32_t kv_heads;         /* 1 .. 1024                                            */
+  int32_t head_dim;         /* 64, 128 or 256                                       */
+  int32_t dtype;            /* SB_BF16 or SB_F16                                    */
+  int32_t n_pages, page_size, max_pages;
+  int32_t max_q;            /* >= 0                                                 */
+} sb_bounds_args;
+sb_status sb_page_bounds(const sb_bounds_args *args, void *stream);
+
+/* The pages that each query attends to, for every key/value head: of the pages
+ * 0 .. p / page_size of its request, p its position as in sb_paged_attention, the
+ * first `first`, the last `last` and, of those between, the `top` of the largest
+ *   sum_i  max(bounds[1][i] Q+_i) + bounds[0][i] Q-_i,
+ *   Q+_i, Q-_i = the sums of max(q_i, 0) and min(q_i, 0) over the head's group,
+ * the largest sum of the group's scores that keys within the bounds can have.
+ * Sums are fp64; of equal ones the lower page is taken, NaN counts as the largest,
+ * and pages outside the cache come last. pages[t][h] lists them in the order of
+ * the cache, -1 behind the last; kept[t] is how many keys they hold up to p. Where
+ * a query's pages are no more than first + top + last, all are listed. A query
+ * with p < 0 gets no pages and kept 0, rows behind the last request's and of no
+ * request get no pages and kept -1. max_kv (an upper bound of lens) only chooses
+ * the grid. */
+typedef struct {
+  int64_t struct_bytes;     /* sizeof(sb_select_args)                               */
+  const void *q;            /* [n_tokens][q_heads][head_dim]                        */
+  const void *bounds;       /* [n_pages][2][kv_heads][head_dim], contiguous         */
+  const int32_t *table;     /* [n_requests][table_stride]                           */
+  const int32_t *lens;      /* [n_requests] tokens cached, the new ones included    */
+  const int32_t *q_start;   /* [n_requests + 1]                                     */
+  int32_t *pages;           /* [n_tokens][kv_heads][first + top + last]             */
+  int32_t *kept;            /* [n_tokens]                                           */
+  int64_t q_token, q_head, table_stride;
+  int32_t n_tokens;         /* >= 0                                                 */
+  int32_t n_requests;       /* >= 1                                                 */
+  int32_t q_heads, kv_heads;/* 1 .. 1024, q_heads a multiple of kv_heads            */
+  int32_t head_dim;         /* 64, 128 or 256                                       */
+  int32_t dtype;            /* SB_BF16 or SB_F16                                    */
+  int32_t n_pages, page_size, max_pages;
+  int32_t top, first, last; /* >= 0, last >= 1                                      */
+  int32_t max_kv;           /* >= 0                                                 */
+  int32_t reserved;         /* 0                                                    */
+} sb_select_args;
+/* Bytes of workspace sb_select_pages needs for these sizes (pointers are not
+ * looked at); -1 if they are invalid. */
+int64_t sb_select_workspace(const sb_select_args *args);
+/* workspace: 256-byte aligned, at least sb_select_workspace bytes. Calls that may
+ * run at the same time need one each. */
+sb_status sb_select_pages(const sb_select_args *args, void *workspace, size_t bytes, void *stream);
+
+/* Attention of every token over pages of its own, given for each key/value head:
+ * out[t] as in sb_paged_attention, over the first kept[t] keys of the pages
+ * pages[t][h][0], pages[t][h][1], .. in turn (at most width pages); pages outside
+ * the cache are skipped. A token with kept 0, or whose keys all lie in pages
+ * outside the cache, gets 0; rows with kept below 0 stay as they are. */
+typedef struct {
+  int64_t struct_bytes;     /* sizeof(sb_selected_args)                             */
+  const void *q;            /* [n_tokens][q_heads][head_dim]                        */
+  const void *k_cache, *v_cache;
+  const int32_t *pages;     /* [n_tokens][kv_heads][width]                          */
+  const int32_t *kept;      /* [n_tokens]                                           */
+  void *out;                /* [n_tokens][q_heads][head_dim]; not q                 */
+  int64_t q_token, q_head, out_token, out_head, kc_page, kc_slot, kc_head, vc_page, vc_slot, vc_head;
+  int32_t n_tokens;         /* >= 0                                                 */
+  int32_t q_heads, kv_heads;/* 1 .. 1024, q_heads a multiple of kv_heads            */
+  int32_t head_dim;         /* 64, 128 or 256                                       */
+  int32_t dtype;            /* SB_BF16 or SB_F16                                    */
+  int32_t n_pages, page_size, width;
+  float scale;
+  int32_t reserved;         /* 0                                                    */
+} sb_selected_args;
+/* Bytes of workspace sb_selected_attention needs on the current device for these
+ * sizes (pointers are not looked at); -1 if they are invalid. */
+int64_t sb_selected_workspace(const sb_selected_args *args);
+/* workspace: 256-byte aligned, at least sb_selected_workspace bytes (NULL where
+ * that is 0). Calls that may run at the same time need one each. */
+sb_status sb_selected_attention(const sb_selected_args *args, void *workspace, size_t bytes, void *stream);
+
 /* ------------------------------------------------------------------------
  * Test support. Not part of the decoding interface: these calls expose one
  * decoder step and one candidate slot so that tests can compare them with

@@ -111,6 +111,76 @@ def shared_attention(q, k_cache, v_cache, prefix_table, prefix_lens, group_start
     return out, size, big
 
 
+def page_bounds(k_cache, table, lens, q_start, bounds):
+    """bounds [pages, 2, kv_heads, D] after the step."""
+    k_cache, bounds = np.asarray(k_cache, np.float64), np.array(bounds, np.float64)
+    pages, page = k_cache.shape[:2]
+    for b, n in enumerate(lens):
+        m = q_start[b + 1] - q_start[b]
+        for c in sorted({j // page for j in range(max(n - m, 0), n)}):
+            at = table[b][c]
+            if 0 <= at < pages:
+                keys = k_cache[at, :min(page, n - c * page)]
+                bounds[at, 0], bounds[at, 1] = keys.min(0), keys.max(0)   # (NaN where one is)
+    return bounds
+
+
+def select_pages(q, bounds, table, lens, q_start, page_size, top, first, last):
+    """(pages [tokens, kv_heads, first + top + last], kept [tokens])."""
+    q, bounds = np.asarray(q, np.float64), np.asarray(bounds, np.float64)
+    T, Hq, D = q.shape
+    n_pages, _, Hkv, _ = bounds.shape
+    width = first + top + last
+    pages, kept = np.full((T, Hkv, width), -1), np.full(T, -1)
+    for b, n in enumerate(lens):
+        m = q_start[b + 1] - q_start[b]
+        for t in range(q_start[b], q_start[b + 1]):
+            p = n - m + t - q_start[b]
+            seen = p // page_size + 1 if p >= 0 else 0
+            kept[t] = max(p + 1, 0) if seen <= width else (width - 1) * page_size + p % page_size + 1
+            for h in range(Hkv):
+                cols = list(range(seen))
+                if seen > width:
+                    mine = q[t, h * (Hq // Hkv):(h + 1) * (Hq // Hkv)]
+                    up, down = np.where(mine < 0, 0, mine).sum(0), np.where(mine > 0, 0, mine).sum(0)   # (NaN stays)
+                    score = {}
+                    for c in range(first, seen - last):
+                        at = table[b][c]
+                        with np.errstate(invalid="ignore"):
+                            s = float(np.sum(bounds[at, 1, h] * up + bounds[at, 0, h] * down)) if 0 <= at < n_pages else -math.inf
+                        score[c] = (1, 0.0) if math.isnan(s) else (0, s)
+                    best = sorted(score, key=lambda c: (score[c][0], score[c][1]), reverse=True)   # (stable: of equal ones the first)
+                    cols = sorted(cols[:first] + best[:top] + cols[seen - last:])
+                pages[t, h, :len(cols)] = [table[b][c] for c in cols]
+    return pages, kept
+
+
+def selected_attention(q, k_cache, v_cache, pages, kept, scale):
+    """As attention, over the first kept[t] keys of pages[t][h]; rows with kept
+    below 0 are NaN."""
+    q, k_cache, v_cache = (np.asarray(t, np.float64) for t in (q, k_cache, v_cache))
+    T, Hq, D = q.shape
+    n_pages, page, Hkv, _ = k_cache.shape
+    out, size, big = (np.full(q.shape, np.nan) for _ in range(3))
+    for t in range(T):
+        if kept[t] < 0:
+            continue
+        out[t] = size[t] = big[t] = 0
+        for hk in range(Hkv):
+            n = min(kept[t], page * len(pages[t][hk]))
+            at = [(pages[t][hk][j // page], j % page) for j in range(n) if 0 <= pages[t][hk][j // page] < n_pages]
+            if not at:
+                continue
+            i, j = np.array(at).T
+            K, V = k_cache[i, j, hk], v_cache[i, j, hk]
+            for h in range(hk * (Hq // Hkv), (hk + 1) * (Hq // Hkv)):
+                s = K @ q[t, h] * scale
+                w = np.exp(s - s.max())
+                w /= w.sum()
+                out[t, h], size[t, h], big[t, h] = w @ V, w @ np.abs(V), np.max(np.abs(K) @ np.abs(q[t, h]))
+    return out, size, big
+
+
 def sample(z, u, T=1.0, top_k=0, top_p=1.0, min_p=0.0):
     """(token, logprob) of one row."""
     z = np.asarray(z, np.float64).copy()

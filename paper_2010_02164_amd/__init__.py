@@ -9,8 +9,8 @@ binding and the build script; PyTorch only provides device memory and streams.
 from .decoder import (Decoder, Hypothesis, decoder_for_workload, group_by_input, inputs_to_device,
                       weights_to_device)
 
-_SERVING = ("PagePlan", "int8_linear", "paged_attention", "plan_pages", "quantize_rows", "rope_append", "rope_frequencies",
-            "sample_tokens", "shared_attention")
+_SERVING = ("PagePlan", "int8_linear", "page_bounds", "paged_attention", "plan_pages", "quantize_rows", "rope_append",
+            "rope_frequencies", "sample_tokens", "select_pages", "selected_attention", "shared_attention")
 
 __all__ = ["Decoder", "Hypothesis", "decoder_for_workload", "group_by_input", "inputs_to_device",
            "weights_to_device", *_SERVING]

@@ -80,6 +80,9 @@ ROPE_ARGS = _Args("q9P14q9if")
 ATTENTION_ARGS = _Args("q7P11q13if")
 SAMPLE_ARGS = _Args("q8Pq4i")
 SHARED_ARGS = _Args("q" + ATTENTION_ARGS.format + "3Pq4i")
+BOUNDS_ARGS = _Args("q5P4q8i")
+SELECT_ARGS = _Args("q7P3q14i")
+SELECTED_ARGS = _Args("q6P10q8ifi")
 QUANTIZE_ARGS = _Args("q3P2q4i")
 LINEAR_ARGS = _Args("q6P3q4i")
 
@@ -136,6 +139,11 @@ def lib():
         "sb_sample_tokens": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
         "sb_shared_workspace": (c_int64, [c_char_p]),
         "sb_shared_attention": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
+        "sb_page_bounds": (c_int32, [c_char_p, c_void_p]),
+        "sb_select_workspace": (c_int64, [c_char_p]),
+        "sb_select_pages": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
+        "sb_selected_workspace": (c_int64, [c_char_p]),
+        "sb_selected_attention": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),
         "sb_quantize_rows": (c_int32, [c_char_p, c_void_p]),
         "sb_linear_workspace": (c_int64, [c_char_p]),
         "sb_quantized_linear": (c_int32, [c_char_p, c_void_p, c_size_t, c_void_p]),

@@ -16,7 +16,7 @@ OUTDIR = os.path.join(HERE, "_lib")
 LIB = os.path.join(OUTDIR, "libstreambeam.so")
 SOURCES = ["api.hip", "sched.hip", "rec.hip", "proj.hip", "proj_f32.hip", "beam.hip", "attn.hip",
            "serve.hip", "pages.hip", "rope.hip", "paged_attn.hip", "sample.hip", "linear.hip",
-           "shared_attn.hip"]
+           "shared_attn.hip", "select.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 

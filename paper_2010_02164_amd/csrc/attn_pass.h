@@ -615,5 +615,48 @@ __device__ __forceinline__ int span_tile(const sb_attention_args &a, int tile, S
   return b;
 }
 
+// One row's parts added up by a wave: every fourth in each 16 lanes, in order, then
+// the four sums; part x is at row place(x) of the sums [..][D] and of their
+// (reference, sum). The result goes to dst.
+template <int DT, int D, class Place>
+__device__ __forceinline__ void join_row(const float *sums, const float2 *stats, int count, const Place &place, uint16_t *dst) {
+  constexpr int E = D / 16;
+  const int lane = threadIdx.x & 63, col = (lane & 15) * E, turn = lane >> 4;
+  float mx = -INFINITY;
+#pragma unroll 4
+  for (int x = turn; x < count; x += 4) mx = fmaxf(mx, stats[place(x)].x);
+  mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+  mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+  const float base = mx == -INFINITY ? 0.0f : mx;
+  float acc[E], sum = 0.0f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+#pragma unroll 4
+  for (int x = turn; x < count; x += 4) {
+    const long long at = place(x);
+    const float2 st = stats[at];
+    const float f = __builtin_amdgcn_exp2f(st.x - base);
+    sum += f * st.y;
+#pragma unroll
+    for (int e = 0; e < E; e += 4) {
+      const f4 v = *reinterpret_cast<const f4 *>(sums + at * D + col + e);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) acc[e + y] += f * v[y];
+    }
+  }
+#pragma unroll
+  for (int o = 16; o < 64; o <<= 1) {
+    sum += __shfl_xor(sum, o, 64);
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+  }
+  if (turn != 0) return;
+  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+  for (int e = 0; e < E; e += 4)
+    *reinterpret_cast<u2 *>(dst + col + e) =
+        u2{Half<DT>::pack(acc[e] * inv, acc[e + 1] * inv), Half<DT>::pack(acc[e + 2] * inv, acc[e + 3] * inv)};
+}
+
 }  // namespace
 }  // namespace sb

@@ -1,0 +1,427 @@
+// Selected pages of a paged cache: the bounds of their keys, the pages that each
+// query attends to by them, and the attention over those.
+//
+// With the smallest and largest of each value over a page's keys, the largest score
+// that one of its keys can have with a query is sum max(q_i lo_i, q_i hi_i) =
+// sum max(q_i, 0) hi_i + min(q_i, 0) lo_i: linear in the bounds, so that a group's
+// heads are added up before, and one product of 2 D values ranks a page for all
+// of them. Sums are fp64, where products of 16-bit values are exact and their sums
+// nearly always: the order of the pages does not depend on that of the sums.
+#include <algorithm>
+
+#include "attn_pass.h"
+#include "wave.h"
+
+namespace sb {
+namespace {
+
+typedef unsigned long long u64;
+
+// -- bounds ------------------------------------------------------------------------
+
+constexpr int BD_THREADS = 256;
+
+// A wave takes 128 values of a page (a lane 8 of them, of every fourth key).
+template <int DT>
+__global__ __launch_bounds__(BD_THREADS) void k_bounds(sb_bounds_args a) {
+  const int b = blockIdx.x, lane = threadIdx.x & 63, turn = lane >> 4;
+  const int n = (int)min((long long)max(a.lens[b], 0), (long long)a.max_pages * a.page_size);
+  const int m = (int)min(max((long long)a.q_start[b + 1] - a.q_start[b], 0LL), (long long)n);
+  if (m == 0) return;
+  const int first = (n - m) / a.page_size, values = a.kv_heads * a.head_dim, blocks = (values + 127) / 128;
+  const long long units = (long long)((n - 1) / a.page_size - first + 1) * blocks;
+  for (long long u = blockIdx.y * (BD_THREADS / 64) + (threadIdx.x >> 6); u < units; u += gridDim.y * (BD_THREADS / 64)) {
+    const int c = first + (int)(u / blocks), at = (int)(u % blocks) * 128 + (lane & 15) * 8;
+    const int page = a.table[b * a.table_stride + c];
+    if ((unsigned)page >= (unsigned)a.n_pages) continue;
+    const bool real = at < values;
+    const int keys = min(a.page_size, n - c * a.page_size), head = real ? at / a.head_dim : 0;
+    const uint16_t *src = static_cast<const uint16_t *>(a.k_cache) + page * a.kc_page + head * a.kc_head + (real ? at - head * a.head_dim : 0);
+    float lo[8], hi[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      lo[x] = INFINITY;
+      hi[x] = -INFINITY;
+    }
+    // (A NaN stays: nothing is smaller or larger.)
+    auto take = [&](int x, float l, float h) {
+      lo[x] = l < lo[x] || l != l ? l : lo[x];
+      hi[x] = h > hi[x] || h != h ? h : hi[x];
+    };
+#pragma unroll 4
+    for (int k = turn; k < keys; k += 4) {
+      const u4 v = *reinterpret_cast<const u4 *>(src + k * a.kc_slot);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const float f = Half<DT>::to_float(x & 1 ? v[x >> 1] >> 16 : v[x >> 1] & 0xFFFFu);
+        take(x, f, f);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o < 64; o <<= 1)
+#pragma unroll
+      for (int x = 0; x < 8; ++x) take(x, __shfl_xor(lo[x], o, 64), __shfl_xor(hi[x], o, 64));
+    if (turn < 2 && real) {
+      u4 out;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) out[x] = turn ? Half<DT>::pack(hi[2 * x], hi[2 * x + 1]) : Half<DT>::pack(lo[2 * x], lo[2 * x + 1]);
+      *reinterpret_cast<u4 *>(static_cast<uint16_t *>(a.bounds) + ((long long)page * 2 + turn) * values + at) = out;
+    }
+  }
+}
+
+// -- selection -----------------------------------------------------------------------
+
+constexpr int SL_THREADS = 256, SL_WAVES = 4;
+
+// Of token t: its position and how many pages there are up to it. position -1:
+// before the request's first; no request: false. (Called by all threads; `found` in LDS.)
+struct Query {
+  int b, p, n;
+};
+__device__ __forceinline__ bool query_of(const sb_select_args &a, int t, int *found, Query &q) {
+  if (threadIdx.x == 0) *found = -1;
+  __syncthreads();
+  for (int b = threadIdx.x; b < a.n_requests; b += SL_THREADS)
+    if (a.q_start[b] <= t && t < a.q_start[b + 1]) atomicMax(found, b);
+  __syncthreads();
+  q.b = *found;
+  if (q.b < 0) return false;
+  const long long len = min((long long)max(a.lens[q.b], 0), (long long)a.max_pages * a.page_size);
+  q.p = (int)max(len - a.q_start[q.b + 1] + t, -1LL);
+  q.n = q.p < 0 ? 0 : q.p / a.page_size + 1;
+  return true;
+}
+
+// A score as a number whose order is the scores': NaN last.
+__device__ __forceinline__ u64 order_of(double score) {
+  const u64 bits = (u64)__double_as_longlong(score + 0.0);   // (of -0 and 0 one)
+  return score != score ? ~0ULL : bits ^ (bits >> 63 ? ~0ULL : 1ULL << 63);
+}
+
+// Scores of the pages first .. n - last - 1 of token t0 + blockIdx.z, head
+// blockIdx.y, those of `chunk` pages a workgroup, to keys [tokens][kv_heads][max_pages].
+template <int DT, int D>
+__global__ __launch_bounds__(SL_THREADS) void k_scores(sb_select_args a, int t0, int chunk, u64 *keys) {
+  constexpr int L = D / 8, P = 64 / L;   // lanes of a page, pages a wave takes at once
+  __shared__ int found;
+  const int t = t0 + blockIdx.z, hk = blockIdx.y, G = a.q_heads / a.kv_heads, lane = threadIdx.x & 63, col = lane % L;
+  Query q;
+  if (!query_of(a, t, &found, q) || q.n <= (long long)a.first + a.top + a.last) return;
+  double up[8], down[8];
+#pragma unroll
+  for (int x = 0; x < 8; ++x) up[x] = down[x] = 0.0;
+  for (int g = 0; g < G; ++g) {
+    const u4 v = *reinterpret_cast<const u4 *>(static_cast<const uint16_t *>(a.q) + t * a.q_token + (hk * G + g) * a.q_head + 8 * col);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const float f = Half<DT>::to_float(x & 1 ? v[x >> 1] >> 16 : v[x >> 1] & 0xFFFFu);
+      if (f != f) up[x] = f;   // (NaN: neither above nor below 0)
+      up[x] += f > 0.0f ? f : 0.0f;
+      down[x] += f < 0.0f ? f : 0.0f;
+    }
+  }
+  const int *table = a.table + q.b * a.table_stride;
+  const long long row = (long long)a.kv_heads * D;
+  const uint16_t *bounds = static_cast<const uint16_t *>(a.bounds) + (long long)hk * D + 8 * col;
+  u64 *out = keys + ((long long)blockIdx.z * a.kv_heads + hk) * a.max_pages;
+  const int end = q.n - a.last;
+  for (int at = blockIdx.x * chunk + a.first; at < end; at += gridDim.x * chunk) {
+    const int stop = min(at + chunk, end);
+    for (int c0 = at + (threadIdx.x >> 6) * P; c0 < stop; c0 += SL_WAVES * P) {
+      const int c = c0 + lane / L, page = c < stop ? table[c] : -1;
+      const bool there = (unsigned)page < (unsigned)a.n_pages;
+      const uint16_t *src = bounds + (there ? 2LL * page * row : 0);
+      const u4 lo = *reinterpret_cast<const u4 *>(src), hi = *reinterpret_cast<const u4 *>(src + row);
+      double s = 0.0;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        s = fma((double)Half<DT>::to_float(x & 1 ? hi[x >> 1] >> 16 : hi[x >> 1] & 0xFFFFu), up[x], s);
+        s = fma((double)Half<DT>::to_float(x & 1 ? lo[x >> 1] >> 16 : lo[x >> 1] & 0xFFFFu), down[x], s);
+      }
+#pragma unroll
+      for (int o = 1; o < L; o <<= 1) s += __shfl_xor(s, o, 64);
+      if (col == 0 && c < stop) out[c] = there ? order_of(s) : order_of(-INFINITY);
+    }
+  }
+}
+
+constexpr int BINS = 2048, LIST = SL_THREADS;
+
+// The list of token t0 + blockIdx.x, head blockIdx.y: the key of the last page
+// taken is found by counting keys in bins, ever finer, until those of its bin fit
+// a list; then all pages are looked through in order.
+__global__ __launch_bounds__(SL_THREADS) void k_pick(sb_select_args a, int t0, const u64 *all_keys) {
+  __shared__ int found, bins[BINS], wave_sums[2][SL_WAVES][2], listed, bin_at, bin_before;
+  __shared__ u64 list[LIST], ends[SL_WAVES][2], cut_key;
+  __shared__ int cut_equal;
+  const int t = t0 + blockIdx.x, hk = blockIdx.y, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int width = a.first + a.top + a.last;
+  int *out = a.pages + ((long long)t * a.kv_heads + hk) * width;
+  Query q;
+  const bool real = query_of(a, t, &found, q);
+  if (hk == 0 && threadIdx.x == 0)
+    a.kept[t] = !real ? -1 : q.n <= width ? q.p + 1 : (width - 1) * a.page_size + q.p % a.page_size + 1;
+  if (!real || q.n <= width) {
+    for (int x = threadIdx.x; x < width; x += SL_THREADS) out[x] = real && x < q.n ? a.table[q.b * a.table_stride + x] : -1;
+    return;
+  }
+  const int *table = a.table + q.b * a.table_stride;
+  for (int x = threadIdx.x; x < a.first; x += SL_THREADS) out[x] = table[x];
+  for (int x = threadIdx.x; x < a.last; x += SL_THREADS) out[a.first + a.top + x] = table[q.n - a.last + x];
+  if (a.top == 0) return;
+  const u64 *keys = all_keys + ((long long)blockIdx.x * a.kv_heads + hk) * a.max_pages;
+  const int begin = a.first, end = q.n - a.last;
+  u64 lo = ~0ULL, hi = 0;
+  for (int c = begin + threadIdx.x; c < end; c += SL_THREADS) {
+    lo = min(lo, keys[c]);
+    hi = max(hi, keys[c]);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    lo = min(lo, (u64)__shfl_xor((long long)lo, o, 64));
+    hi = max(hi, (u64)__shfl_xor((long long)hi, o, 64));
+  }
+  if (lane == 0) {
+    ends[w][0] = lo;
+    ends[w][1] = hi;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int x = 0; x < SL_WAVES; ++x) {
+    lo = min(lo, ends[x][0]);
+    hi = max(hi, ends[x][1]);
+  }
+  int want = a.top;   // the want'th largest of the keys from lo to hi is the last one taken
+  for (;;) {
+    if (lo == hi) {
+      if (threadIdx.x == 0) {
+        cut_key = lo;
+        cut_equal = want;
+      }
+      break;
+    }
+    const int shift = max(64 - __clzll((long long)(hi - lo)) - 11, 0);   // bins of 2^shift keys
+    for (int x = threadIdx.x; x < BINS; x += SL_THREADS) bins[x] = 0;
+    if (threadIdx.x == 0) listed = 0;
+    __syncthreads();
+    for (int c = begin + threadIdx.x; c < end; c += SL_THREADS) {
+      const u64 k = keys[c];
+      if (k >= lo && k <= hi) atomicAdd(&bins[(hi - k) >> shift], 1);   // (bin 0: the largest)
+    }
+    __syncthreads();
+    // 8 bins a thread: where their sum passes want.
+    int mine = 0;
+#pragma unroll
+    for (int x = 0; x < BINS / SL_THREADS; ++x) mine += bins[threadIdx.x * (BINS / SL_THREADS) + x];
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += y;
+    }
+    if (lane == 63) wave_sums[0][w][0] = upto;
+    __syncthreads();
+    for (int x = 0; x < w; ++x) upto += wave_sums[0][x][0];
+    if (upto - mine < want && want <= upto) {   // (one thread)
+      int before = upto - mine, x = threadIdx.x * (BINS / SL_THREADS);
+      while (before + bins[x] < want) before += bins[x++];
+      bin_at = x;
+      bin_before = before;
+    }
+    __syncthreads();
+    const int bin = bin_at, count = bins[bin];
+    want -= bin_before;
+    const u64 top = hi - ((u64)bin << shift), width_of = (1ULL << shift) - 1;
+    hi = top;
+    lo = top - lo > width_of ? top - width_of : lo;
+    if (count <= LIST) {
+      for (int c = begin + threadIdx.x; c < end; c += SL_THREADS) {
+        const u64 k = keys[c];
+        if (k >= lo && k <= hi) list[atomicAdd(&listed, 1)] = k;
+      }
+      __syncthreads();
+      if (threadIdx.x < count) {
+        const u64 k = list[threadIdx.x];
+        int above = 0, equal = 0;
+        for (int x = 0; x < count; ++x) {
+          above += list[x] > k;
+          equal += list[x] == k;
+        }
+        if (above < want && want <= above + equal) {   // (equal keys write the same)
+          cut_key = k;
+          cut_equal = want - above;
+        }
+      }
+      break;
+    }
+    __syncthreads();
+  }
+  __syncthreads();
+  const u64 cut = cut_key;
+  const int equal_taken = cut_equal;
+  // Pages above the cut, and the first of those on it, in the cache's order.
+  int above_before = 0, equal_before = 0;
+  for (int c0 = begin, turn = 0; c0 < end; c0 += SL_THREADS, turn ^= 1) {
+    const int c = c0 + threadIdx.x;
+    const u64 k = c < end ? keys[c] : 0;
+    const bool above = c < end && k > cut, equal = c < end && k == cut;
+    const u64 ma = __ballot(above), me = __ballot(equal), below = (1ULL << lane) - 1;
+    if (lane == 0) {
+      wave_sums[turn][w][0] = __popcll(ma);
+      wave_sums[turn][w][1] = __popcll(me);
+    }
+    __syncthreads();
+    int na = above_before + __popcll(ma & below), ne = equal_before + __popcll(me & below);
+#pragma unroll
+    for (int x = 0; x < SL_WAVES; ++x) {
+      if (x < w) {
+        na += wave_sums[turn][x][0];
+        ne += wave_sums[turn][x][1];
+      }
+      above_before += wave_sums[turn][x][0];
+      equal_before += wave_sums[turn][x][1];
+    }
+    if (above || (equal && ne < equal_taken)) out[a.first + na + min(ne, equal_taken)] = table[c];
+  }
+}
+
+// -- attention over the selected pages -----------------------------------------------
+
+// In the workspace: the parts' sums [splits][n_tokens][q_heads][D] and their
+// (reference, sum).
+template <int DT, int D>
+__global__ __launch_bounds__(AT_THREADS, D == 64 ? 3 : D == 128 ? 2 : 1) void k_selected(sb_attention_args a, const int *kept, int splits,
+                                                                                        void *work) {
+  __shared__ FewShared<D> sh;
+  const int G = a.q_heads / a.kv_heads, hk = (int)(blockIdx.x % a.kv_heads), j = (int)(blockIdx.x / a.kv_heads);
+  const int t = j / splits, split = j % splits, n = kept[t];
+  if (n < 0) return;
+  const long long rows = (long long)a.n_tokens * a.q_heads;
+  float *sums = static_cast<float *>(work);
+  float2 *stats = reinterpret_cast<float2 *>(sums + rows * splits * D);
+  Span s;
+  s.q0 = t;
+  s.m = 1;
+  s.n = s.n_vis = (int)min((long long)n, (long long)a.max_pages * a.page_size);
+  s.rows = G;
+  s.ns = s.lo = 0;
+  s.p_first = s.p_last = s.n - 1;
+  s.all = true;
+  const int *table = a.table + ((long long)t * a.kv_heads + hk) * a.table_stride;
+  const int tiles = few_tiles(s), each = (tiles + splits - 1) / splits, t0 = min(split * each, tiles), t1 = min(t0 + each, tiles);
+  for (int r0 = 0; r0 < G; r0 += FEW_ROWS) {
+    s.r0 = r0;
+    few_unit<DT, D>(a, s, hk, table, t0, t1, sh, [&](int rw, int col, float top, float sum, const f4 &acc) {
+      if (splits == 1) {
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        uint16_t *dst = static_cast<uint16_t *>(a.out) + t * a.out_token + (hk * G + rw) * a.out_head + col;
+        *reinterpret_cast<u2 *>(dst) = u2{Half<DT>::pack(acc[0] * inv, acc[1] * inv), Half<DT>::pack(acc[2] * inv, acc[3] * inv)};
+        return;
+      }
+      const long long at = split * rows + (long long)t * a.q_heads + hk * G + rw;
+      *reinterpret_cast<f4 *>(sums + at * D + col) = acc;
+      if (col == 0) stats[at] = make_float2(top, sum);
+    });
+  }
+}
+
+template <int DT, int D>
+__global__ __launch_bounds__(AT_THREADS) void k_selected_join(sb_attention_args a, const int *kept, int splits, const void *work) {
+  const long long rows = (long long)a.n_tokens * a.q_heads, at = (long long)blockIdx.x * AT_WAVES + (threadIdx.x >> 6);
+  if (at >= rows || kept[at / a.q_heads] < 0) return;
+  const float *sums = static_cast<const float *>(work);
+  join_row<DT, D>(sums, reinterpret_cast<const float2 *>(sums + rows * splits * D), splits, [&](int x) { return x * rows + at; },
+                  static_cast<uint16_t *>(a.out) + at / a.q_heads * a.out_token + at % a.q_heads * a.out_head);
+}
+
+// Splits where tokens and heads are too few for the units, of SPLIT_KEYS keys at
+// least.
+constexpr int SPLIT_KEYS = 128;
+int splits_of(const sb_selected_args &x, int n_cu) {
+  const long long room = (x.head_dim == 64 ? 3 : x.head_dim == 128 ? 2 : 1) * (long long)n_cu;
+  return (int)std::max(1LL, std::min(room / ((long long)x.n_tokens * x.kv_heads), (long long)x.width * x.page_size / SPLIT_KEYS));
+}
+
+template <int DT, int D>
+hipError_t attend(const sb_selected_args &x, int n_cu, void *work, hipStream_t s) {
+  sb_attention_args a = {};
+  a.q = x.q, a.k_cache = x.k_cache, a.v_cache = x.v_cache, a.table = x.pages, a.out = x.out;
+  a.q_token = x.q_token, a.q_head = x.q_head, a.out_token = x.out_token, a.out_head = x.out_head;
+  a.kc_page = x.kc_page, a.kc_slot = x.kc_slot, a.kc_head = x.kc_head, a.vc_page = x.vc_page, a.vc_slot = x.vc_slot, a.vc_head = x.vc_head;
+  a.table_stride = a.max_pages = x.width;
+  a.n_tokens = x.n_tokens, a.q_heads = x.q_heads, a.kv_heads = x.kv_heads, a.head_dim = D, a.n_pages = x.n_pages, a.page_size = x.page_size;
+  a.scale = x.scale;
+  const int splits = splits_of(x, n_cu);
+  hipLaunchKernelGGL((k_selected<DT, D>), dim3((unsigned)((long long)x.n_tokens * splits * x.kv_heads)), dim3(AT_THREADS), 0, s, a, x.kept,
+                     splits, work);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || splits == 1) return e;
+  const long long rows = (long long)x.n_tokens * x.q_heads;
+  hipLaunchKernelGGL((k_selected_join<DT, D>), dim3((unsigned)((rows + AT_WAVES - 1) / AT_WAVES)), dim3(AT_THREADS), 0, s, a, x.kept, splits, work);
+  return hipGetLastError();
+}
+
+// Tokens whose scores are kept at a time.
+constexpr long long SCORE_BYTES = 256 << 20;
+long long tokens_at_once(const sb_select_args &a) {
+  return std::max(1LL, std::min({(long long)a.n_tokens, SCORE_BYTES / ((long long)a.kv_heads * a.max_pages * 8), 65535LL}));
+}
+
+template <int DT, int D>
+hipError_t select(const sb_select_args &a, int n_cu, void *work, hipStream_t s) {
+  const long long step = tokens_at_once(a);
+  const long long between = std::max(1LL, (std::max(a.max_kv, 1) + a.page_size - 1LL) / a.page_size - a.first - a.last);
+  for (long long t0 = 0; t0 < a.n_tokens; t0 += step) {
+    const unsigned tokens = (unsigned)std::min(step, a.n_tokens - t0);
+    if (a.top > 0) {
+      // Pages enough for a workgroup that reading the queries is a small part.
+      constexpr long long LEAST = 32, MOST = 512;
+      const long long chunk = std::min(MOST, std::max(LEAST, between * tokens * a.kv_heads / (8 * n_cu) / LEAST * LEAST));
+      const unsigned chunks = (unsigned)std::min(65535LL, (between + chunk - 1) / chunk);
+      hipLaunchKernelGGL((k_scores<DT, D>), dim3(chunks, a.kv_heads, tokens), dim3(SL_THREADS), 0, s, a, (int)t0, (int)chunk,
+                         static_cast<u64 *>(work));
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(k_pick, dim3(tokens, a.kv_heads), dim3(SL_THREADS), 0, s, a, (int)t0, static_cast<const u64 *>(work));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_bounds(const sb_bounds_args &a, hipStream_t s) {
+  const long long pages = std::max(a.max_q, 1) / a.page_size + 2LL, units = pages * ((a.kv_heads * a.head_dim + 127) / 128);
+  const dim3 grid((unsigned)a.n_requests, (unsigned)std::min((units + BD_THREADS / 64 - 1) / (BD_THREADS / 64), 1024LL));
+  if (a.dtype == SB_BF16) hipLaunchKernelGGL((k_bounds<SB_BF16>), grid, dim3(BD_THREADS), 0, s, a);
+  else hipLaunchKernelGGL((k_bounds<SB_F16>), grid, dim3(BD_THREADS), 0, s, a);
+  return hipGetLastError();
+}
+
+int64_t select_workspace(const sb_select_args &a) { return tokens_at_once(a) * a.kv_heads * a.max_pages * 8; }
+
+int64_t selected_workspace(const sb_selected_args &a, int n_cu) {
+  if (a.n_tokens == 0) return 0;
+  const int splits = splits_of(a, n_cu);
+  return splits == 1 ? 0 : (int64_t)splits * a.n_tokens * a.q_heads * (a.head_dim + 2) * 4;
+}
+
+#define BY_TYPE_AND_SIZE(fn, a, ...)                                              \
+  if (a.dtype == SB_BF16) {                                                       \
+    if (a.head_dim == 64) return fn<SB_BF16, 64>(a, __VA_ARGS__);                 \
+    if (a.head_dim == 128) return fn<SB_BF16, 128>(a, __VA_ARGS__);               \
+    return fn<SB_BF16, 256>(a, __VA_ARGS__);                                      \
+  }                                                                               \
+  if (a.head_dim == 64) return fn<SB_F16, 64>(a, __VA_ARGS__);                    \
+  if (a.head_dim == 128) return fn<SB_F16, 128>(a, __VA_ARGS__);                  \
+  return fn<SB_F16, 256>(a, __VA_ARGS__)
+
+hipError_t launch_select(const sb_select_args &a, int n_cu, void *work, hipStream_t s) { BY_TYPE_AND_SIZE(select, a, n_cu, work, s); }
+hipError_t launch_selected_attention(const sb_selected_args &a, int n_cu, void *work, hipStream_t s) {
+  BY_TYPE_AND_SIZE(attend, a, n_cu, work, s);
+}
+
+}  // namespace sb

@@ -19,14 +19,20 @@ hipError_t launch_paged_attention(const sb_attention_args &a, int n_cu, void *wo
 hipError_t launch_sample(const sb_sample_args &a, void *workspace, int n_cu, hipStream_t s);   // workspace: may be null
 
 hipError_t launch_shared_attention(const sb_shared_args &a, int n_cu, void *work, hipStream_t s);
+hipError_t launch_bounds(const sb_bounds_args &a, hipStream_t s);
+hipError_t launch_select(const sb_select_args &a, int n_cu, void *work, hipStream_t s);
+hipError_t launch_selected_attention(const sb_selected_args &a, int n_cu, void *work, hipStream_t s);
 hipError_t launch_quantize(const sb_quantize_args &a, hipStream_t s);
 hipError_t launch_linear(const sb_linear_args &a, int n_cu, void *work, hipStream_t s);
 
 // Bytes of workspace of an attention (0: none).
 int64_t attention_workspace(const sb_attention_args &a, int n_cu);
 int64_t shared_workspace(const sb_shared_args &a, int n_cu);
+int64_t selected_workspace(const sb_selected_args &a, int n_cu);
 // Bytes of workspace that speed a draw up (0: none would).
 int64_t sample_workspace(const sb_sample_args &a);
+// Bytes of workspace of a selection.
+int64_t select_workspace(const sb_select_args &a);
 // Bytes of workspace of a product (0: none).
 int64_t linear_workspace(const sb_linear_args &a, int n_cu);
 

@@ -106,6 +106,46 @@ sb_status check_shared(const sb_shared_args *x, const char *call, bool pointers)
   return SB_OK;
 }
 
+sb_status check_select(const sb_select_args *a, const char *call) {
+  REFUSE_IF(!a, SB_E_INVALID_ARG, "no arguments");
+  REFUSE_IF(a->struct_bytes != (int64_t)sizeof(*a) || a->reserved, SB_E_INVALID_ARG, "struct_bytes is not this library's");
+  REFUSE_IF(a->dtype != SB_BF16 && a->dtype != SB_F16, SB_E_UNSUPPORTED, "dtype is not SB_BF16 or SB_F16");
+  REFUSE_IF(a->head_dim != 64 && a->head_dim != 128 && a->head_dim != 256, SB_E_UNSUPPORTED, "head_dim is not 64, 128 or 256");
+  REFUSE_IF(a->n_tokens < 0 || a->n_requests < 1, SB_E_INVALID_ARG, "n_tokens < 0 or n_requests < 1");
+  REFUSE_IF(a->kv_heads < 1 || a->kv_heads > 1024 || a->q_heads < 1 || a->q_heads > 1024 || a->q_heads % a->kv_heads,
+            SB_E_INVALID_ARG, "q_heads is not a multiple of kv_heads, or outside 1 .. 1024");
+  REFUSE_IF(a->n_pages < 1 || a->page_size < 1 || a->page_size > 4096 || a->max_pages < 1, SB_E_INVALID_ARG,
+            "n_pages, max_pages < 1 or page_size outside 1 .. 4096");
+  REFUSE_IF(a->top < 0 || a->first < 0 || a->last < 1 || a->max_kv < 0, SB_E_INVALID_ARG, "top, first or max_kv < 0, or last < 1");
+  REFUSE_IF(((int64_t)a->top + a->first + a->last) * a->page_size > SB_ATTENTION_MAX_KEYS ||
+                (int64_t)a->max_pages * a->page_size > SB_ATTENTION_MAX_KEYS || (int64_t)a->n_pages * a->page_size > INT32_MAX,
+            SB_E_UNSUPPORTED, "pages (of the cache, a table's row, or selected) times page_size are above SB_ATTENTION_MAX_KEYS");
+  REFUSE_IF(a->table_stride < a->max_pages, SB_E_INVALID_ARG, "table_stride < max_pages");
+  REFUSE_IF(!strides_fit({{a->q_token, a->n_tokens}, {a->q_head, a->q_heads}}), SB_E_UNSUPPORTED, "a stride is negative or no multiple of 8");
+  return SB_OK;
+}
+
+sb_status check_selected(const sb_selected_args *a, const char *call) {
+  REFUSE_IF(!a, SB_E_INVALID_ARG, "no arguments");
+  REFUSE_IF(a->struct_bytes != (int64_t)sizeof(*a) || a->reserved, SB_E_INVALID_ARG, "struct_bytes is not this library's");
+  REFUSE_IF(a->dtype != SB_BF16 && a->dtype != SB_F16, SB_E_UNSUPPORTED, "dtype is not SB_BF16 or SB_F16");
+  REFUSE_IF(a->head_dim != 64 && a->head_dim != 128 && a->head_dim != 256, SB_E_UNSUPPORTED, "head_dim is not 64, 128 or 256");
+  REFUSE_IF(a->n_tokens < 0, SB_E_INVALID_ARG, "n_tokens < 0");
+  REFUSE_IF(a->kv_heads < 1 || a->kv_heads > 1024 || a->q_heads < 1 || a->q_heads > 1024 || a->q_heads % a->kv_heads,
+            SB_E_INVALID_ARG, "q_heads is not a multiple of kv_heads, or outside 1 .. 1024");
+  REFUSE_IF(a->n_pages < 1 || a->page_size < 1 || a->page_size > 4096 || a->width < 1, SB_E_INVALID_ARG,
+            "n_pages, width < 1 or page_size outside 1 .. 4096");
+  REFUSE_IF((int64_t)a->n_pages * a->page_size > INT32_MAX || (int64_t)a->width * a->page_size > SB_ATTENTION_MAX_KEYS, SB_E_UNSUPPORTED,
+            "n_pages times page_size is not below 2^31, or width times page_size above SB_ATTENTION_MAX_KEYS");
+  REFUSE_IF((int64_t)a->n_tokens * a->q_heads > (1 << 23), SB_E_UNSUPPORTED, "n_tokens times q_heads is above 2^23");
+  REFUSE_IF(!isfinite((float)(a->scale * 1.4426950408889634)), SB_E_INVALID_ARG, "scale, in powers of two, is not finite");
+  REFUSE_IF(!strides_fit({{a->q_token, a->n_tokens}, {a->q_head, a->q_heads}, {a->out_token, a->n_tokens}, {a->out_head, a->q_heads},
+                          {a->kc_page, a->n_pages}, {a->kc_slot, a->page_size}, {a->kc_head, a->kv_heads}, {a->vc_page, a->n_pages},
+                          {a->vc_slot, a->page_size}, {a->vc_head, a->kv_heads}}),
+            SB_E_UNSUPPORTED, "a stride is negative or no multiple of 8");
+  return SB_OK;
+}
+
 sb_status check_sample(const sb_sample_args *a, const char *call) {
   REFUSE_IF(!a, SB_E_INVALID_ARG, "no arguments");
   REFUSE_IF(a->struct_bytes != (int64_t)sizeof(*a) || a->reserved, SB_E_INVALID_ARG, "struct_bytes is not this library's");
@@ -237,6 +277,79 @@ sb_status sb_shared_attention(const sb_shared_args *a, void *workspace, size_t b
   REFUSE_IF(!workspace || !aligned(workspace, 256) || bytes < (size_t)shared_workspace(*a, n_cu), SB_E_WORKSPACE,
             "workspace missing, misaligned or smaller than sb_shared_workspace");
   return launched(launch_shared_attention(*a, n_cu, workspace, static_cast<hipStream_t>(stream)), call);
+}
+
+sb_status sb_page_bounds(const sb_bounds_args *a, void *stream) {
+  const char *call = "sb_page_bounds";
+  REFUSE_IF(!a, SB_E_INVALID_ARG, "no arguments");
+  REFUSE_IF(a->struct_bytes != (int64_t)sizeof(*a), SB_E_INVALID_ARG, "struct_bytes is not this library's");
+  REFUSE_IF(a->dtype != SB_BF16 && a->dtype != SB_F16, SB_E_UNSUPPORTED, "dtype is not SB_BF16 or SB_F16");
+  REFUSE_IF(a->head_dim != 64 && a->head_dim != 128 && a->head_dim != 256, SB_E_UNSUPPORTED, "head_dim is not 64, 128 or 256");
+  REFUSE_IF(a->n_requests < 1 || a->kv_heads < 1 || a->kv_heads > 1024 || a->max_q < 0, SB_E_INVALID_ARG,
+            "n_requests < 1, kv_heads outside 1 .. 1024 or max_q < 0");
+  REFUSE_IF(a->n_requests > (1 << 23), SB_E_UNSUPPORTED, "more than 2^23 requests");
+  REFUSE_IF(a->n_pages < 1 || a->page_size < 1 || a->page_size > 4096 || a->max_pages < 1, SB_E_INVALID_ARG,
+            "n_pages, max_pages < 1 or page_size outside 1 .. 4096");
+  REFUSE_IF((int64_t)a->n_pages * a->page_size > INT32_MAX || (int64_t)a->max_pages * a->page_size > INT32_MAX, SB_E_UNSUPPORTED,
+            "n_pages or max_pages times page_size is not below 2^31");
+  REFUSE_IF(a->table_stride < a->max_pages, SB_E_INVALID_ARG, "table_stride < max_pages");
+  REFUSE_IF(!strides_fit({{a->kc_page, a->n_pages}, {a->kc_slot, a->page_size}, {a->kc_head, a->kv_heads}}), SB_E_UNSUPPORTED,
+            "a stride is negative or no multiple of 8");
+  REFUSE_IF(!a->k_cache || !a->table || !a->lens || !a->q_start || !a->bounds, SB_E_INVALID_ARG, "a pointer is missing");
+  REFUSE_IF(!aligned(a->table, 4) || !aligned(a->lens, 4) || !aligned(a->q_start, 4), SB_E_INVALID_ARG, "an array is not aligned to its type");
+  REFUSE_IF(!aligned(a->k_cache, 16) || !aligned(a->bounds, 16), SB_E_UNSUPPORTED, "k_cache or bounds is not 16-byte aligned");
+  return launched(launch_bounds(*a, static_cast<hipStream_t>(stream)), call);
+}
+
+int64_t sb_select_workspace(const sb_select_args *a) {
+  return check_select(a, "sb_select_workspace") == SB_OK ? (a->n_tokens ? select_workspace(*a) : 0) : -1;
+}
+
+sb_status sb_select_pages(const sb_select_args *a, void *workspace, size_t bytes, void *stream) {
+  const char *call = "sb_select_pages";
+  const sb_status st = check_select(a, call);
+  if (st != SB_OK) return st;
+  if (a->n_tokens == 0) return SB_OK;
+  REFUSE_IF(!a->q || !a->bounds || !a->table || !a->lens || !a->q_start || !a->pages || !a->kept, SB_E_INVALID_ARG, "a pointer is missing");
+  REFUSE_IF(!aligned(a->table, 4) || !aligned(a->lens, 4) || !aligned(a->q_start, 4) || !aligned(a->pages, 4) || !aligned(a->kept, 4),
+            SB_E_INVALID_ARG, "an array is not aligned to its type");
+  REFUSE_IF(!aligned(a->q, 16) || !aligned(a->bounds, 16), SB_E_UNSUPPORTED, "q or bounds is not 16-byte aligned");
+  REFUSE_IF(!workspace || !aligned(workspace, 256) || bytes < (size_t)select_workspace(*a), SB_E_WORKSPACE,
+            "workspace missing, misaligned or smaller than sb_select_workspace");
+  int n_cu = 0;
+  const hipError_t e = compute_units(n_cu);
+  if (e != hipSuccess) return launched(e, call);
+  return launched(launch_select(*a, n_cu, workspace, static_cast<hipStream_t>(stream)), call);
+}
+
+int64_t sb_selected_workspace(const sb_selected_args *a) {
+  const char *call = "sb_selected_workspace";
+  if (check_selected(a, call) != SB_OK) return -1;
+  int n_cu = 0;
+  const hipError_t e = compute_units(n_cu);
+  if (e != hipSuccess) {
+    launched(e, call);
+    return -1;
+  }
+  return selected_workspace(*a, n_cu);
+}
+
+sb_status sb_selected_attention(const sb_selected_args *a, void *workspace, size_t bytes, void *stream) {
+  const char *call = "sb_selected_attention";
+  const sb_status st = check_selected(a, call);
+  if (st != SB_OK) return st;
+  if (a->n_tokens == 0) return SB_OK;
+  REFUSE_IF(!a->q || !a->k_cache || !a->v_cache || !a->pages || !a->kept || !a->out, SB_E_INVALID_ARG, "a pointer is missing");
+  REFUSE_IF(!aligned(a->pages, 4) || !aligned(a->kept, 4), SB_E_INVALID_ARG, "an array is not aligned to its type");
+  REFUSE_IF(!aligned(a->q, 16) || !aligned(a->k_cache, 16) || !aligned(a->v_cache, 16) || !aligned(a->out, 16), SB_E_UNSUPPORTED,
+            "q, out or the caches are not 16-byte aligned");
+  int n_cu = 0;
+  const hipError_t e = compute_units(n_cu);
+  if (e != hipSuccess) return launched(e, call);
+  const int64_t need = selected_workspace(*a, n_cu);
+  REFUSE_IF(need && (!workspace || !aligned(workspace, 256) || bytes < (size_t)need), SB_E_WORKSPACE,
+            "workspace missing, misaligned or smaller than sb_selected_workspace");
+  return launched(launch_selected_attention(*a, n_cu, workspace, static_cast<hipStream_t>(stream)), call);
 }
 
 int64_t sb_sample_workspace(const sb_sample_args *a) {

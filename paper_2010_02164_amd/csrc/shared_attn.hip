@@ -170,53 +170,20 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : 2) void k_shared(sb_atte
   }
 }
 
-// A wave a row: every fourth part in each 16 lanes, in order, then the four sums.
+// A wave a row.
 template <int DT, int D>
 __global__ __launch_bounds__(AT_THREADS) void k_shared_join(sb_attention_args a, Cut c, void *work) {
-  constexpr int E = D / 16;
   const Parts in(a, c, work);
-  const int b = blockIdx.x, lane = threadIdx.x & 63, col = (lane & 15) * E, turn = lane >> 4;
+  const int b = blockIdx.x;
   Span s;
   span_request(a, b, s);
   if (s.m == 0) return;
-  const int ahead = min(max(in.ahead[b], 0), c.prefix_splits);
+  const int ahead = min(max(in.ahead[b], 0), c.prefix_splits), gap = c.prefix_splits - ahead;
   const long long rows = (long long)s.m * a.q_heads, step = (long long)gridDim.y * AT_WAVES;
   for (long long r = (long long)blockIdx.y * AT_WAVES + (threadIdx.x >> 6); r < rows; r += step) {
     const long long at = (long long)s.q0 * a.q_heads + r;
-    const int first = c.prefix_splits - ahead, count = ahead + c.own_splits;
-    float mx = -INFINITY;
-    for (int x = turn; x < count; x += 4) mx = fmaxf(mx, in.stats[(x < ahead ? x : x + first) * in.rows + at].x);
-    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float base = mx == -INFINITY ? 0.0f : mx;
-    float acc[E], sum = 0.0f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.0f;
-#pragma unroll 4
-    for (int x = turn; x < count; x += 4) {
-      const long long place = (x < ahead ? x : x + first) * in.rows + at;
-      const float2 st = in.stats[place];
-      const float f = __builtin_amdgcn_exp2f(st.x - base);
-      sum += f * st.y;
-#pragma unroll
-      for (int e = 0; e < E; e += 4) {
-        const f4 v = *reinterpret_cast<const f4 *>(in.sums + place * D + col + e);
-#pragma unroll
-        for (int y = 0; y < 4; ++y) acc[e + y] += f * v[y];
-      }
-    }
-#pragma unroll
-    for (int o = 16; o < 64; o <<= 1) {
-      sum += __shfl_xor(sum, o, 64);
-#pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
-    }
-    if (turn != 0) continue;
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    uint16_t *dst = static_cast<uint16_t *>(a.out) + (s.q0 + r / a.q_heads) * a.out_token + (r % a.q_heads) * a.out_head + col;
-#pragma unroll
-    for (int e = 0; e < E; e += 4)
-      *reinterpret_cast<u2 *>(dst + e) = u2{Half<DT>::pack(acc[e] * inv, acc[e + 1] * inv), Half<DT>::pack(acc[e + 2] * inv, acc[e + 3] * inv)};
+    join_row<DT, D>(in.sums, in.stats, ahead + c.own_splits, [&](int x) { return (x < ahead ? x : x + gap) * in.rows + at; },
+                    static_cast<uint16_t *>(a.out) + (s.q0 + r / a.q_heads) * a.out_token + (r % a.q_heads) * a.out_head);
   }
 }
 

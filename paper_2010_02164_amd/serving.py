@@ -356,6 +356,110 @@ def shared_attention(q, k_cache, v_cache, prefix_table, prefix_lens, group_start
     return out
 
 
+def _bounds(t, dtype, i, pages=None, heads=None, dim=None):
+    """Its shape."""
+    shape = t.shape
+    if len(shape) != 4 or shape[1] != 2 or t.dtype != dtype or t.get_device() != i or not t.is_contiguous():
+        _refuse(f"bounds must be a contiguous {dtype} tensor [pages, 2, kv_heads, head_dim] on cuda:{i}")
+    if pages is not None and (shape[0], shape[2]) != (pages, heads):
+        _refuse("bounds must have the cache's pages and heads")
+    if dim is not None and shape[3] != dim:
+        _refuse("bounds have another head_dim")
+    return shape
+
+
+def page_bounds(k_cache, table, lens, q_start, bounds, *, max_q: int):
+    """The smallest and largest of each value over the keys of the pages that a
+    step's new tokens went to (sb_page_bounds), for select_pages.
+
+    k_cache, table, lens, q_start as in paged_attention; bounds: [pages, 2, kv_heads,
+    head_dim] of the cache's type, contiguous, of which those pages' are written:
+    called with every step's tokens, a prompt's and the single ones behind it, it
+    keeps the bounds of all cached keys. max_q: an upper bound of a request's new
+    tokens, for the grid only. Returns bounds."""
+    i, dtype = _device(k_cache, "k_cache"), k_cache.dtype
+    if dtype not in _HALVES:
+        _refuse("k_cache must be bfloat16 or float16")
+    _no_grad(k_cache, bounds)
+    (pages, page_size, Hkv, D), kc, _ = _caches(k_cache, k_cache, dtype, i, None, k_cache.shape[-1] if k_cache.dim() else 0)
+    (B, width), row = _table(table, i)
+    _bounds(bounds, dtype, i, pages, Hkv, D)
+    args = N.BOUNDS_ARGS.pack(
+        N.BOUNDS_ARGS.size, k_cache.data_ptr(), table.data_ptr(), _whole(lens, "lens", torch.int32, i, (B,)),
+        _whole(q_start, "q_start", torch.int32, i, (B + 1,)), bounds.data_ptr(), kc[0], kc[1], kc[2], row,
+        B, Hkv, D, _HALVES[dtype], pages, page_size, width, max_q)
+    _call(N.lib().sb_page_bounds, "sb_page_bounds", i, args)
+    _written((bounds,))
+    return bounds
+
+
+def select_pages(q, bounds, table, lens, q_start, *, page_size: int, top: int, first: int = 1, last: int = 1, max_kv: int, out=None):
+    """(pages int32 [tokens, kv_heads, first + top + last], kept int32 [tokens]): the
+    pages that each query attends to (sb_select_pages).
+
+    q: [tokens, q_heads, head_dim] (rotated), bfloat16 or float16; bounds: as
+    page_bounds keeps them; table, lens, q_start as in paged_attention. Listed
+    are the first pages of the request, the last ones up to the query's, and of
+    those between the `top` whose keys may score highest, summed over the heads
+    of a group; in the cache's order, -1 behind the last. kept: how many keys they
+    hold up to the query, 0 without any, -1 for rows of no request. max_kv: an
+    upper bound of lens, for the grid only. out: (pages, kept) to write to. A
+    selection may serve several layers' selected_attention."""
+    i, dtype, i32 = _device(q, "q"), q.dtype, torch.int32
+    if dtype not in _HALVES:
+        _refuse("q must be bfloat16 or float16")
+    _no_grad(q, bounds)
+    (T, Hq, D), qs = _heads(q, "q", dtype, i)
+    n_pages, _, Hkv, _ = _bounds(bounds, dtype, i, dim=D)
+    (B, table_width), row = _table(table, i)
+    try:
+        width = operator.index(top) + operator.index(first) + operator.index(last)
+    except TypeError:
+        _refuse("top, first and last must be whole numbers")
+    if min(top, first) < 0 or last < 1:
+        _refuse("top and first must not be negative, last at least 1")
+    if out is None:
+        out = torch.empty((T, Hkv, width), dtype=i32, device=i), torch.empty(T, dtype=i32, device=i)
+    pages, kept = out
+    args = N.SELECT_ARGS.pack(
+        N.SELECT_ARGS.size, q.data_ptr(), bounds.data_ptr(), table.data_ptr(), _whole(lens, "lens", i32, i, (B,)),
+        _whole(q_start, "q_start", i32, i, (B + 1,)), _whole(pages, "out pages", i32, i, (T, Hkv, width)), _whole(kept, "out kept", i32, i, (T,)),
+        qs[0], qs[1], row, T, B, Hq, Hkv, D, _HALVES[dtype], n_pages, page_size, table_width, top, first, last, max_kv, 0)
+    L = N.lib()
+    need = L.sb_select_workspace(args)   # (below 0: refused by the call itself)
+    work = torch.empty(need, dtype=torch.uint8, device=i) if need > 0 else None
+    _call(L.sb_select_pages, "sb_select_pages", i, args, None if work is None else work.data_ptr(), max(need, 0))
+    _written((pages, kept))
+    return pages, kept
+
+
+def selected_attention(q, k_cache, v_cache, pages, kept, *, scale: Optional[float] = None, out=None):
+    """Attention of every token over pages of its own (sb_selected_attention).
+
+    q and the caches as in paged_attention; pages: int32 [tokens, kv_heads, width],
+    kept: int32 [tokens], as select_pages gives them: a token sees the first kept
+    keys of its pages, one after the other. Rows with kept below 0 are left as
+    they are in `out` (undefined without it)."""
+    i, dtype, i32 = _device(q, "q"), q.dtype, torch.int32
+    if dtype not in _HALVES:
+        _refuse("q must be bfloat16 or float16")
+    _no_grad(q, k_cache, v_cache, out)
+    (T, Hq, D), qs = _heads(q, "q", dtype, i)
+    (n_pages, page_size, Hkv, _), kc, vc = _caches(k_cache, v_cache, dtype, i, None, D)
+    if pages.dim() != 3:
+        _refuse("pages must be [tokens, kv_heads, width]")
+    width = pages.shape[2]
+    out, os_ = _attended(out, dtype, i, T, Hq, D)
+    args = N.SELECTED_ARGS.pack(
+        N.SELECTED_ARGS.size, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), _whole(pages, "pages", i32, i, (T, Hkv, width)),
+        _whole(kept, "kept", i32, i, (T,)), out.data_ptr(), qs[0], qs[1], os_[0], os_[1], kc[0], kc[1], kc[2], vc[0], vc[1], vc[2],
+        T, Hq, Hkv, D, _HALVES[dtype], n_pages, page_size, width, 1.0 / math.sqrt(D) if scale is None else scale, 0)
+    L = N.lib()
+    _call_with_workspace(L.sb_selected_attention, L.sb_selected_workspace, "sb_selected_attention", i, args)
+    _written((out,))
+    return out
+
+
 def sample_tokens(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, out=None):
     """(tokens int32 [rows], logprobs float32 [rows]): one token per row of
     logits, drawn with the given numbers (sb_sample_tokens).

@@ -25,8 +25,19 @@ ATTN = dict(own_bytes=N.ATTENTION_ARGS.size, q=PTR, k_cache=PTR, v_cache=PTR, ta
             sinks=0, max_q=2, max_kv=100, scale=0.1)
 SHARED = dict(bytes=N.SHARED_ARGS.size, **ATTN, prefix_table=PTR, prefix_lens=PTR, group_start=PTR, prefix_stride=9, n_groups=2, prefix_pages=8,
               max_prefix=100, reserved=0)
+BOUNDS = dict(bytes=N.BOUNDS_ARGS.size, k_cache=PTR, table=PTR, lens=PTR, q_start=PTR, bounds=PTR, kc_page=4096, kc_slot=256, kc_head=128,
+              table_stride=8, n_requests=2, kv_heads=2, head_dim=128, dtype=N.SB_BF16, n_pages=32, page_size=16, max_pages=8, max_q=1)
+SELECT = dict(bytes=N.SELECT_ARGS.size, q=PTR, bounds=PTR, table=PTR, lens=PTR, q_start=PTR, pages=PTR, kept=PTR, q_token=512, q_head=128,
+              table_stride=8, n_tokens=3, n_requests=2, q_heads=4, kv_heads=2, head_dim=128, dtype=N.SB_BF16, n_pages=32, page_size=16,
+              max_pages=8, top=3, first=1, last=2, max_kv=100, reserved=0)
+SELECTED = dict(bytes=N.SELECTED_ARGS.size, q=PTR, k_cache=PTR, v_cache=PTR, pages=PTR, kept=PTR, out=PTR, q_token=512, q_head=128,
+                out_token=512, out_head=128, kc_page=4096, kc_slot=256, kc_head=128, vc_page=4096, vc_slot=256, vc_head=128, n_tokens=3,
+                q_heads=4, kv_heads=2, head_dim=128, dtype=N.SB_BF16, n_pages=32, page_size=16, width=6, scale=0.1, reserved=0)
 CALLS = {   # call -> (its struct, the packer, the call's arguments, whether it takes a workspace)
     "sb_shared_attention": ("sb_shared_args", N.SHARED_ARGS, SHARED, True),
+    "sb_page_bounds": ("sb_bounds_args", N.BOUNDS_ARGS, BOUNDS, False),
+    "sb_select_pages": ("sb_select_args", N.SELECT_ARGS, SELECT, True),
+    "sb_selected_attention": ("sb_selected_args", N.SELECTED_ARGS, SELECTED, True),
     "sb_quantize_rows": ("sb_quantize_args", N.QUANTIZE_ARGS, QUANTIZE, False),
     "sb_quantized_linear": ("sb_linear_args", N.LINEAR_ARGS, LINEAR, True),
 }
@@ -102,10 +113,58 @@ def test_linear_refusals(native_lib, over, status):
         assert native_lib.sb_linear_workspace(N.LINEAR_ARGS.pack(*dict(LINEAR, **over).values())) == -1
 
 
+PAGED = [(dict(bytes=8), INVALID), (dict(dtype=N.SB_F32), UNSUPPORTED), (dict(head_dim=96), UNSUPPORTED), (dict(kv_heads=0), INVALID),
+         (dict(page_size=0), INVALID), (dict(page_size=4097), INVALID), (dict(n_pages=0), INVALID), (dict(n_pages=1 << 28), UNSUPPORTED)]
+
+
+@pytest.mark.parametrize("over,status", PAGED + [
+    (dict(n_requests=0), INVALID), (dict(n_requests=(1 << 23) + 1), UNSUPPORTED), (dict(max_q=-1), INVALID), (dict(max_pages=0), INVALID),
+    (dict(max_pages=1 << 27, table_stride=1 << 27), UNSUPPORTED), (dict(table_stride=7), INVALID), (dict(kc_head=124), UNSUPPORTED),
+    (dict(kc_page=-8), UNSUPPORTED), (dict(k_cache=0), INVALID), (dict(bounds=0), INVALID), (dict(lens=PTR + 2), INVALID),
+    (dict(k_cache=PTR + 8), UNSUPPORTED), (dict(bounds=PTR + 8), UNSUPPORTED)])
+def test_bounds_refusals(native_lib, over, status):
+    assert run(native_lib, "sb_page_bounds", over) == status
+
+
+@pytest.mark.parametrize("over,status", PAGED + [
+    (dict(reserved=1), INVALID), (dict(n_requests=0), INVALID), (dict(n_tokens=-1), INVALID), (dict(q_heads=5), INVALID),
+    (dict(max_pages=0), INVALID), (dict(top=-1), INVALID), (dict(first=-1), INVALID), (dict(last=0), INVALID), (dict(max_kv=-1), INVALID),
+    (dict(top=1 << 27), UNSUPPORTED), (dict(max_pages=1 << 27, table_stride=1 << 27), UNSUPPORTED), (dict(table_stride=7), INVALID),
+    (dict(q_token=516), UNSUPPORTED), (dict(q=0), INVALID), (dict(pages=0), INVALID), (dict(kept=0), INVALID), (dict(pages=PTR + 2), INVALID),
+    (dict(q=PTR + 8), UNSUPPORTED), (dict(bounds=PTR + 2), UNSUPPORTED), ({}, N.SB_E_WORKSPACE)])
+def test_select_refusals(native_lib, over, status):
+    assert run(native_lib, "sb_select_pages", over) == status
+    need = native_lib.sb_select_workspace(N.SELECT_ARGS.pack(*dict(SELECT, **over).values()))
+    assert (need == -1) == (status != N.SB_E_WORKSPACE and not {"q", "pages", "kept", "bounds"} & set(over))
+
+
+@pytest.mark.parametrize("over,status", PAGED + [
+    (dict(reserved=1), INVALID), (dict(n_tokens=-1), INVALID), (dict(q_heads=5), INVALID), (dict(width=0), INVALID), (dict(width=1 << 27), UNSUPPORTED),
+    (dict(n_tokens=1 << 22), UNSUPPORTED), (dict(scale=math.nan), INVALID), (dict(out_head=4), UNSUPPORTED), (dict(vc_slot=-8), UNSUPPORTED),
+    (dict(q=0), INVALID), (dict(pages=0), INVALID), (dict(kept=0), INVALID), (dict(out=0), INVALID), (dict(kept=PTR + 1), INVALID),
+    (dict(out=PTR + 8), UNSUPPORTED), (dict(v_cache=PTR + 4), UNSUPPORTED)])
+def test_selected_attention_refusals(native_lib, over, status):
+    assert run(native_lib, "sb_selected_attention", over) == status
+    if not {"q", "pages", "kept", "out", "v_cache"} & set(over):
+        assert native_lib.sb_selected_workspace(N.SELECTED_ARGS.pack(*dict(SELECTED, **over).values())) == -1
+
+
+def test_select_workspace_is_bounded(native_lib):
+    """Scores of some tokens at a time, of one at least."""
+    def ask(**over):
+        return native_lib.sb_select_workspace(N.SELECT_ARGS.pack(*dict(SELECT, **over).values()))
+    assert ask() == 3 * 2 * 8 * 8 and ask(n_tokens=0) == 0
+    wide = dict(max_pages=1 << 20, table_stride=1 << 20)
+    assert ask(**wide, n_tokens=100) == ask(**wide, n_tokens=16) == 16 * 2 * 8 << 20
+    assert ask(max_pages=1 << 24, table_stride=1 << 24, n_tokens=9) == 2 * 8 << 24
+
+
 def test_nothing_to_do_needs_no_gpu(native_lib):
     assert run(native_lib, "sb_quantize_rows", dict(rows=0, x=0, codes=0, scales=0)) == N.SB_OK
     assert run(native_lib, "sb_quantized_linear", dict(rows=0, x=0, out=0)) == N.SB_OK
     assert run(native_lib, "sb_shared_attention", dict(n_tokens=0, q=0, out=0)) == N.SB_OK
+    assert run(native_lib, "sb_select_pages", dict(n_tokens=0, q=0, pages=0, kept=0)) == N.SB_OK
+    assert run(native_lib, "sb_selected_attention", dict(n_tokens=0, q=0, pages=0, kept=0, out=0)) == N.SB_OK
     # Strides of a single row are not looked at.
     assert run(native_lib, "sb_quantized_linear", dict(rows=0, x_row=7, out_row=1)) == N.SB_OK
 
@@ -113,6 +172,9 @@ def test_nothing_to_do_needs_no_gpu(native_lib):
 def test_missing_arguments(native_lib):
     assert native_lib.sb_shared_workspace(None) == -1
     assert native_lib.sb_shared_attention(None, None, 0, None) == INVALID
+    assert native_lib.sb_page_bounds(None, None) == INVALID
+    assert native_lib.sb_select_workspace(None) == native_lib.sb_selected_workspace(None) == -1
+    assert native_lib.sb_select_pages(None, None, 0, None) == native_lib.sb_selected_attention(None, None, 0, None) == INVALID
     assert native_lib.sb_quantize_rows(None, None) == INVALID
     assert native_lib.sb_linear_workspace(None) == -1
     assert native_lib.sb_quantized_linear(None, None, 0, None) == INVALID
@@ -123,6 +185,12 @@ def test_tensors_must_be_on_a_gpu():
     h, i = torch.zeros(2, 1, 64, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
     with pytest.raises(ValueError, match="GPU"):
         sb.shared_attention(h, h[None], h[None], i[None], i, i, i[None], i, i, max_q=1, max_kv=1, max_prefix=1)
+    with pytest.raises(ValueError, match="GPU"):
+        sb.page_bounds(h[None], i[None], i, i, h[None], max_q=1)
+    with pytest.raises(ValueError, match="GPU"):
+        sb.select_pages(h, h[None], i[None], i, i, page_size=4, top=1, max_kv=1)
+    with pytest.raises(ValueError, match="GPU"):
+        sb.selected_attention(h, h[None], h[None], i[None, None], i)
     with pytest.raises(ValueError, match="GPU"):
         sb.quantize_rows(torch.zeros(2, 5))
     with pytest.raises(ValueError, match="GPU"):
@@ -149,6 +217,27 @@ def test_oracle_shared_attention_by_hand():
     assert np.allclose(out[:, 0, 0], [(2 + 8) / 2, (2 + 8 + 3) / 5, (2 + 4) / 2, 4])
     out, *_ = oracle.shared_attention(*args[:7], [1, 0, 0], *args[8:])   # fewer tokens than queries
     assert np.allclose(out[:, 0, 0], [2, (2 + 8) / 2, 2, 0])
+
+
+def test_oracle_selection_by_hand():
+    # Pages of 2, one head of two values; request 0 has 9 tokens on pages 4 0 1 2 3.
+    k = np.array([[[1, 0], [3, -1]], [[0, 0], [2, 5]], [[-4, 4], [0, 0]], [[9, 9], [9, 9]], [[1, 1], [1, 1]]], float)[:, :, None]
+    table = [[4, 0, 1, 2, 3]]
+    bounds = oracle.page_bounds(k, table, [9], [0, 9], np.zeros((5, 2, 1, 2)))
+    assert bounds[0, :, 0].tolist() == [[1, -1], [3, 0]] and bounds[2, :, 0].tolist() == [[-4, 0], [0, 4]]
+    assert bounds[3, :, 0].tolist() == [[9, 9], [9, 9]]
+    one = oracle.page_bounds(k, table, [3], [0, 1], np.zeros((5, 2, 1, 2)))   # page 0 alone, its first key
+    assert one[0, :, 0].tolist() == [[1, 0], [1, 0]] and not one[[1, 2, 3, 4]].any()
+    # Two heads of a group: up (2, 0), down (0, -1): pages 0, 1, 2 score 6 + 1, 4 + 0, 0 + 0.
+    q = np.array([[[2.0, 0.0], [0.0, -1.0]]])
+    pages, kept = oracle.select_pages(q, bounds, table, [9], [0, 1], 2, 1, 1, 1)
+    assert pages.tolist() == [[[4, 0, 3]]] and kept.tolist() == [5]
+    pages, kept = oracle.select_pages(-q, bounds, table, [9], [0, 1], 2, 2, 0, 1)   # -2 + 0, 0 + 5, 8 + 4, and -2 + 1 of page 4
+    assert pages.tolist() == [[[1, 2, 3]]] and kept.tolist() == [5]
+    pages, kept = oracle.select_pages(q, bounds, table, [8], [0, 1], 2, 3, 1, 1)
+    assert pages.tolist() == [[[4, 0, 1, 2, -1]]] and kept.tolist() == [8]
+    out, *_ = oracle.selected_attention(np.zeros((2, 1, 2)), k, k, [[[0, 9, 2]], [[1, 1, 1]]], [5, 0], 1.0)
+    assert np.allclose(out[:, 0], [[0, 1], [0, 0]])   # keys (1, 0), (3, -1) and (-4, 4)
 
 
 def test_oracle_linear_by_hand():
