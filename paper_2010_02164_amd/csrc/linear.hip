@@ -8,12 +8,15 @@
 // so that they may be split and joined in any order.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "serve.h"
 
 namespace sb {
 namespace {
 
 typedef unsigned int u4 __attribute__((ext_vector_type(4)));
+typedef float f4 __attribute__((ext_vector_type(4)));
 typedef int i4 __attribute__((ext_vector_type(4)));
 typedef int i16v __attribute__((ext_vector_type(16)));
 
@@ -194,8 +197,206 @@ __global__ __launch_bounds__(256) void k_linear(sb_linear_args a) {
   }
 }
 
+// 8 channels of a row side by side, those that there are.
+template <int DT>
+__device__ __forceinline__ void store8(const sb_linear_args &a, int m, int n, const float (&v)[8], bool wide) {
+  const long long at = m * a.out_row + n;
+  if (wide && n + 8 <= a.channels) {
+    if constexpr (DT == SB_F32) {
+      float *dst = static_cast<float *>(a.out) + at;
+      *reinterpret_cast<f4 *>(dst) = f4{v[0], v[1], v[2], v[3]};
+      *reinterpret_cast<f4 *>(dst + 4) = f4{v[4], v[5], v[6], v[7]};
+    } else {
+      *reinterpret_cast<u4 *>(static_cast<uint16_t *>(a.out) + at) =
+          u4{Half<DT>::pack(v[0], v[1]), Half<DT>::pack(v[2], v[3]), Half<DT>::pack(v[4], v[5]), Half<DT>::pack(v[6], v[7])};
+    }
+    return;
+  }
+#pragma unroll
+  for (int y = 0; y < 8; ++y) {
+    if (n + y >= a.channels) continue;
+    if constexpr (DT == SB_F32) static_cast<float *>(a.out)[at + y] = v[y];
+    else static_cast<uint16_t *>(a.out)[at + y] = (uint16_t)Half<DT>::pack(v[y], v[y]);
+  }
+}
+
+// -- many rows: tiles in LDS -----------------------------------------------------
+//
+// A workgroup of 2 x 2 waves makes 64 MT rows of x by 64 NT channels, 128 values of
+// the depth at a time. LDS has two such tiles of both operands, one worked on
+// while the other is filled from registers that were loaded a tile before. In
+// LDS a row is 128 bytes, its 16-byte pieces at place piece ^ (a number of the
+// row), so that the lanes of an operand's read, which take one piece of rows that
+// follow each other, use all banks. The matrix unit's rows are channels: a lane
+// then has 4 channels of one row of x side by side, and 8 with the next product's,
+// since the channels are dealt out to products in turns of 4.
+
+constexpr int TILE_K = 128;   // bytes of a row in LDS
+
+template <int MT, int NT>
+struct TileShared {
+  alignas(16) unsigned char x[2][64 * MT * TILE_K];
+  alignas(16) unsigned char w[2][64 * NT * TILE_K];
+};
+
+__device__ __forceinline__ int x_place(int row, int piece) { return row * TILE_K + ((piece ^ (row & 7)) << 4); }
+__device__ __forceinline__ int w_place(int row, int piece) { return row * TILE_K + ((piece ^ ((row & 3) | ((row >> 1) & 4))) << 4); }
+
+// Spreads READS reads and WRITES writes of LDS and LOADS loads over PRODUCTS products
+// of the matrix unit, which all came before it.
+template <int PRODUCTS, int READS, int WRITES, int LOADS, int X = 0>
+__device__ __forceinline__ void interleave() {
+  if constexpr (X < PRODUCTS) {
+    constexpr int r = READS * (X + 1) / PRODUCTS - READS * X / PRODUCTS, w = WRITES * (X + 1) / PRODUCTS - WRITES * X / PRODUCTS;
+    constexpr int l = LOADS * (X + 1) / PRODUCTS - LOADS * X / PRODUCTS;
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
+    if constexpr (w > 0) __builtin_amdgcn_sched_group_barrier(0x200, w, 0);
+    if constexpr (l > 0) __builtin_amdgcn_sched_group_barrier(0x020, l, 0);
+    interleave<PRODUCTS, READS, WRITES, LOADS, X + 1>();
+  } else {
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
+
+template <int DT, int MT, int NT>
+__global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_linear_args a, int tiles_m, int tiles_n) {
+  constexpr int BM = 64 * MT, BN = 64 * NT, KS = TILE_K / 32;
+  constexpr int XP = BM * 8 / 256, WP = BN * 8 / 256;   // 16-byte pieces of a tile that a thread brings
+  __shared__ TileShared<MT, NT> sh;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, h2 = lane >> 5;
+  // Workgroups go to the 8 XCDs in turn: each gets tiles that follow each other, in
+  // blocks of GROUP tiles of rows by all of channels, which share operands in its L2.
+  constexpr int GROUP = 4;
+  const int tiles = tiles_m * tiles_n, xcd = blockIdx.x & 7, per = tiles >> 3, more = tiles & 7;
+  const int p = xcd * per + min(xcd, more) + (int)(blockIdx.x >> 3);
+  const int g = p / (GROUP * tiles_n), in = p - g * (GROUP * tiles_n), high = min(tiles_m - g * GROUP, GROUP);
+  const int m0 = (g * GROUP + in % high) * BM, n0 = in / high * BN;
+  const int row0 = threadIdx.x >> 3, piece = threadIdx.x & 7;
+  const unsigned char *xs[XP], *ws[WP];
+#pragma unroll
+  for (int i = 0; i < XP; ++i) xs[i] = static_cast<const unsigned char *>(a.x) + min(m0 + row0 + 32 * i, a.rows - 1) * a.x_row + 16 * piece;
+#pragma unroll
+  for (int i = 0; i < WP; ++i) ws[i] = static_cast<const unsigned char *>(a.w) + min(n0 + row0 + 32 * i, a.channels - 1) * a.w_row + 16 * piece;
+  u4 xr[XP], wr[WP];
+  auto load_x = [&](int k) {
+    const int at = min(k, a.depth - 16 - 16 * piece);   // (behind the last value: any that is)
+#pragma unroll
+    for (int i = 0; i < XP; ++i) xr[i] = *reinterpret_cast<const u4 *>(xs[i] + at);
+  };
+  auto load_w = [&](int k) {
+    const int at = min(k, a.depth - 16 - 16 * piece);
+#pragma unroll
+    for (int i = 0; i < WP; ++i) wr[i] = *reinterpret_cast<const u4 *>(ws[i] + at);
+  };
+  auto write_x = [&](int k, int to, auto last) {   // of the last tile, zeros behind the last value
+    const unsigned int keep = !decltype(last)::value || k + 16 * piece < a.depth ? ~0u : 0u;
+#pragma unroll
+    for (int i = 0; i < XP; ++i) *reinterpret_cast<u4 *>(&sh.x[to][x_place(row0 + 32 * i, piece)]) = xr[i] & keep;
+  };
+  auto write_w = [&](int to) {
+#pragma unroll
+    for (int i = 0; i < WP; ++i) *reinterpret_cast<u4 *>(&sh.w[to][w_place(row0 + 32 * i, piece)]) = wr[i];
+  };
+  const int xrow = (w >> 1) * 32 * MT + l32, wrow = (w & 1) * 32 * NT + (l32 >> 2) * 8 + (l32 & 3);
+  i4 xf[2][MT], wf[2][NT];
+  auto fetch = [&](int from, int ks, int to) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i) xf[to][i] = *reinterpret_cast<const i4 *>(&sh.x[from][x_place(xrow + 32 * i, 2 * ks + h2)]);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) wf[to][j] = *reinterpret_cast<const i4 *>(&sh.w[from][w_place(wrow + 64 * (j >> 1) + 4 * (j & 1), 2 * ks + h2)]);
+  };
+  i16v c[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) c[i][j][e] = 0;
+  auto multiply = [&](int from) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int j = 0; j < NT; ++j) c[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[from][j], xf[from][i], c[i][j], 0, 0, 0);
+  };
+  // A tile's work: operands come from LDS a step of 32 before their products; in
+  // between the next tile goes to LDS (WRITE) and the one after it is loaded (LOAD).
+  auto tile = [&](int t, auto write_next, auto load_next) {
+    constexpr bool WRITE = decltype(write_next)::value, LOAD = decltype(load_next)::value;
+    const int cur = t & 1, next = cur ^ 1;
+    fetch(cur, 1, 1);
+    if constexpr (WRITE) write_x((t + 1) * TILE_K, next, std::bool_constant<!LOAD>());
+    multiply(0);
+    interleave<MT * NT, MT + NT, WRITE ? XP : 0, 0>();
+    fetch(cur, 2, 0);
+    if constexpr (LOAD) load_x((t + 2) * TILE_K);
+    if constexpr (WRITE) write_w(next);
+    multiply(1);
+    interleave<MT * NT, MT + NT, WRITE ? WP : 0, LOAD ? XP : 0>();
+    fetch(cur, 3, 1);
+    if constexpr (LOAD) load_w((t + 2) * TILE_K);
+    multiply(0);
+    interleave<MT * NT, MT + NT, 0, LOAD ? WP : 0>();
+    if constexpr (WRITE) {   // all of this tile is in registers, the next one in LDS
+      __syncthreads();
+      fetch(next, 0, 0);
+    }
+    multiply(1);
+    interleave<MT * NT, WRITE ? MT + NT : 0, 0, 0>();
+  };
+  const int steps = (a.depth + TILE_K - 1) / TILE_K;
+  load_x(0);
+  load_w(0);
+  write_x(0, 0, std::true_type());
+  write_w(0);
+  load_x(TILE_K);
+  load_w(TILE_K);
+  __syncthreads();
+  fetch(0, 0, 0);
+  int t = 0;
+  for (; t + 2 < steps; ++t) tile(t, std::true_type(), std::true_type());
+  if (t + 1 < steps) tile(t++, std::true_type(), std::false_type());
+  tile(t, std::false_type(), std::false_type());
+  // Lane: row m, of products j and j + 1 channels 8 (2 (e / 4) + h2) + 4 (j % 2) + e % 4.
+  const bool wide = (a.out_row * (DT == SB_F32 ? 4 : 2)) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
+#pragma unroll
+  for (int j = 0; j < NT; j += 2) {
+#pragma unroll
+    for (int e = 0; e < 16; e += 4) {
+      const int n = n0 + (w & 1) * 32 * NT + 64 * (j >> 1) + 8 * (2 * (e >> 2) + h2);
+      float sw[8], bias[8];
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        const int at = min(n + y, a.channels - 1);
+        sw[y] = a.w_scale[at];
+        bias[y] = a.bias ? a.bias[at] : 0.0f;
+      }
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int m = m0 + (w >> 1) * 32 * MT + 32 * i + l32;
+        if (m >= a.rows) continue;
+        const float sx = a.x_scale[m];
+        float v[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) v[y] = scaled<DT>(c[i][j + (y >> 2)][e + (y & 3)], sx, sw[y], bias[y]);
+        store8<DT>(a, m, n, v, wide);
+      }
+    }
+  }
+}
+
 template <int DT>
 hipError_t linear(const sb_linear_args &a, int n_cu, void *work, hipStream_t s) {
+  const auto tiles = [&](auto kernel, int bm, int bn) {
+    const int tm = (a.rows + bm - 1) / bm, tn = (a.channels + bn - 1) / bn;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tm * tn)), dim3(256), 0, s, a, tm, tn);
+    return hipGetLastError();
+  };
+  if (a.rows > 64) {
+    const long long large = ((a.rows + 255LL) / 256) * ((a.channels + 255LL) / 256);
+    if (large >= n_cu) return tiles(k_linear_tiles<DT, 4, 4>, 256, 256);
+    return tiles(k_linear_tiles<DT, 2, 2>, 128, 128);
+  }
   hipLaunchKernelGGL((k_linear<DT>), dim3((unsigned)((a.channels + 63LL) / 64), (unsigned)((a.rows + 63LL) / 64)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
