@@ -11,10 +11,12 @@
 #include <type_traits>
 
 #include "serve.h"
+#include "wave.h"
 
 namespace sb {
 namespace {
 
+typedef unsigned int u2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u4 __attribute__((ext_vector_type(4)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef int i4 __attribute__((ext_vector_type(4)));
@@ -57,16 +59,59 @@ __device__ __forceinline__ void load_values(const void *row, int at, int cols, f
   }
 }
 
-// The whole number next to y / s, |y| <= 127.5 s. The product with the rounded
+// The whole number next to y / s, |y| <= 190 s. The product with the rounded
 // reciprocal is off by less than one; which side of the borders (n +- 1/2) s y
 // lies on is the sign of one fused operation, which rounding does not change.
 __device__ __forceinline__ int nearest(float y, float s, float inv) {
-  float n = rintf(y * inv);
-  const float above = fmaf(-(n + 0.5f), s, y), below = fmaf(-(n - 0.5f), s, y);
-  const bool odd = ((int)n & 1) != 0;
-  if (above > 0.0f || (above == 0.0f && odd)) n += 1.0f;
-  else if (below < 0.0f || (below == 0.0f && odd)) n -= 1.0f;
-  return (int)fminf(fmaxf(n, -127.0f), 127.0f);
+  const float n = rintf(y * inv), above = fmaf(-(n + 0.5f), s, y), below = fmaf(-(n - 0.5f), s, y);
+  const int odd = (int)n & 1;
+  int c = (int)n;
+  c += (above > 0.0f) | ((above == 0.0f) & odd);
+  c -= (below < 0.0f) | ((below == 0.0f) & odd);
+  return min(max(c, -127), 127);
+}
+
+// The codes of 16 values. With the product plus 1.5 2^23, whose last place is 1, a
+// sum's low byte is the code; the product is off by at most 190 2^-22 < 2^-14, and
+// only where it comes so near to a border are the codes found the long way (one
+// of 1000 values in 30 does in a wave: 82 us for 8000 rows of 4096 where all went
+// the long way).
+__device__ __forceinline__ u4 codes_of(const float (&v)[QT_PIECE], float up, float s, float inv) {
+  constexpr float SHIFT = 12582912.0f;
+  u4 out;
+  float far = 0.0f;
+#pragma unroll
+  for (int x = 0; x < QT_PIECE; x += 4) {
+    uint32_t bits[4];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const float value = v[x + y] * up, sum = fmaf(value, inv, SHIFT);
+      far = fmaxf(far, fabsf(fmaf(value, inv, SHIFT - sum)));
+      bits[y] = __float_as_uint(sum);
+    }
+    const uint32_t lo = __builtin_amdgcn_perm(bits[1], bits[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(bits[3], bits[2], 0x0C0C0400u);
+    out[x >> 2] = lo | hi << 16;
+  }
+  if (far > 0.5f - 0x1p-14f) {
+#pragma unroll
+    for (int x = 0; x < QT_PIECE; x += 4) {
+      __builtin_amdgcn_sched_barrier(0);   // (4 at a time: few registers)
+      out[x >> 2] = 0;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) out[x >> 2] |= ((uint32_t)nearest(v[x + y] * up, s, inv) & 0xFFu) << (8 * y);
+    }
+  }
+  return out;
+}
+
+template <int S>
+__device__ __forceinline__ uint32_t max_stage(uint32_t v) {
+  uint32_t x, y;
+  stage32<S>(v, x, y);
+  return max(x, y);
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  return max_stage<5>(max_stage<4>(max_stage<3>(max_stage<2>(max_stage<1>(max_stage<0>(v))))));
 }
 
 // ROWS rows a workgroup; PIECES pieces a thread stay in registers, those of longer
@@ -102,8 +147,7 @@ __global__ __launch_bounds__(QT_THREADS) void k_quantize(sb_quantize_args a, int
     load(piece, w);
     look(w);
   }
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o, 64));
+  top = wave_max(top);
   if (T > 64) {
     if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
     __syncthreads();
@@ -121,12 +165,7 @@ __global__ __launch_bounds__(QT_THREADS) void k_quantize(sb_quantize_args a, int
   const float inv = none ? 0.0f : 1.0f / s;
   u4 *dst = reinterpret_cast<u4 *>(static_cast<int8_t *>(a.codes) + r * a.codes_row);
   auto store = [&](int piece, const float (&from)[QT_PIECE]) {
-    u4 out = {0, 0, 0, 0};
-    if (!none) {
-#pragma unroll
-      for (int x = 0; x < QT_PIECE; ++x) out[x >> 2] |= ((uint32_t)nearest(from[x] * up, s, inv) & 0xFFu) << (8 * (x & 3));
-    }
-    dst[piece] = out;
+    dst[piece] = none ? u4{0, 0, 0, 0} : codes_of(from, up, s, inv);
   };
 #pragma unroll
   for (int p = 0; p < PIECES; ++p)
@@ -142,10 +181,16 @@ template <int DT>
 hipError_t quantize(const sb_quantize_args &a, hipStream_t s) {
   const int unit = DT == SB_F32 ? 4 : 8;
   const int wide = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && (a.rows == 1 || a.x_row % unit == 0);
-  if (a.cols <= 64 * QT_PIECE)
+  // Rows enough to fill the card go by waves, which do not wait for each other.
+  const int wave = 64 * QT_PIECE;
+  if (a.cols <= wave)
     hipLaunchKernelGGL((k_quantize<DT, 4, 1>), dim3((unsigned)((a.rows + 3LL) / 4)), dim3(QT_THREADS), 0, s, a, wide);
+  else if (a.rows >= 2048 && a.cols <= 4 * wave)
+    hipLaunchKernelGGL((k_quantize<DT, 4, 4>), dim3((unsigned)((a.rows + 3LL) / 4)), dim3(QT_THREADS), 0, s, a, wide);
+  else if (a.cols <= 4 * wave)
+    hipLaunchKernelGGL((k_quantize<DT, 1, 1>), dim3((unsigned)a.rows), dim3(QT_THREADS), 0, s, a, wide);
   else
-    hipLaunchKernelGGL((k_quantize<DT, 1, 2>), dim3((unsigned)a.rows), dim3(QT_THREADS), 0, s, a, wide);
+    hipLaunchKernelGGL((k_quantize<DT, 1, 4>), dim3((unsigned)a.rows), dim3(QT_THREADS), 0, s, a, wide);
   return hipGetLastError();
 }
 
@@ -166,58 +211,109 @@ __device__ __forceinline__ float scaled(int sum, float sx, float sw, float bias)
   return __builtin_amdgcn_ldexpf((float)sum * (x.part * w.part), x.power + w.power) + bias;
 }
 
-// 64 x 64 results a workgroup, 32 x 32 a wave, straight from memory.
-template <int DT>
-__global__ __launch_bounds__(256) void k_linear(sb_linear_args a) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, h2 = lane >> 5;
-  const int n0 = blockIdx.x * 64 + (w & 1) * 32, m0 = blockIdx.y * 64 + (w >> 1) * 32;
-  const int n = min(n0 + l32, a.channels - 1), m = min(m0 + l32, a.rows - 1);
-  const char *wr = static_cast<const char *>(a.w) + n * a.w_row, *xr = static_cast<const char *>(a.x) + m * a.x_row;
-  i16v c;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) c[e] = 0;
-  for (int k = 16 * h2; k < a.depth + 16 * h2; k += 32) {
-    i4 x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
-    if (k < a.depth) {
-      x = *reinterpret_cast<const i4 *>(wr + k);
-      y = *reinterpret_cast<const i4 *>(xr + k);
-    }
-    c = __builtin_amdgcn_mfma_i32_32x32x32_i8(x, y, c, 0, 0, 0);
-  }
-  const int row = m0 + l32;
-  if (row >= a.rows) return;
-  const float sx = a.x_scale[row];
-#pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const int col = n0 + 8 * (e >> 2) + 4 * h2 + (e & 3);
-    if (col >= a.channels) continue;
-    const float v = scaled<DT>(c[e], sx, a.w_scale[col], a.bias ? a.bias[col] : 0.0f);
-    if constexpr (DT == SB_F32) static_cast<float *>(a.out)[row * a.out_row + col] = v;
-    else static_cast<uint16_t *>(a.out)[row * a.out_row + col] = (uint16_t)Half<DT>::pack(v, v);
-  }
-}
-
-// 8 channels of a row side by side, those that there are.
-template <int DT>
-__device__ __forceinline__ void store8(const sb_linear_args &a, int m, int n, const float (&v)[8], bool wide) {
+// W channels of a row side by side, those that there are. wide: rows of 16 bytes
+// and more start at multiples of 16.
+template <int DT, int W>
+__device__ __forceinline__ void store_side_by_side(const sb_linear_args &a, int m, int n, const float (&v)[W], bool wide) {
   const long long at = m * a.out_row + n;
-  if (wide && n + 8 <= a.channels) {
+  if (wide && n + W <= a.channels) {
     if constexpr (DT == SB_F32) {
-      float *dst = static_cast<float *>(a.out) + at;
-      *reinterpret_cast<f4 *>(dst) = f4{v[0], v[1], v[2], v[3]};
-      *reinterpret_cast<f4 *>(dst + 4) = f4{v[4], v[5], v[6], v[7]};
+#pragma unroll
+      for (int y = 0; y < W; y += 4) *reinterpret_cast<f4 *>(static_cast<float *>(a.out) + at + y) = f4{v[y], v[y + 1], v[y + 2], v[y + 3]};
     } else {
-      *reinterpret_cast<u4 *>(static_cast<uint16_t *>(a.out) + at) =
-          u4{Half<DT>::pack(v[0], v[1]), Half<DT>::pack(v[2], v[3]), Half<DT>::pack(v[4], v[5]), Half<DT>::pack(v[6], v[7])};
+      uint32_t p[W / 2];
+#pragma unroll
+      for (int y = 0; y < W; y += 2) p[y >> 1] = Half<DT>::pack(v[y], v[y + 1]);
+      if constexpr (W == 8) *reinterpret_cast<u4 *>(static_cast<uint16_t *>(a.out) + at) = u4{p[0], p[1], p[2], p[3]};
+      else *reinterpret_cast<u2 *>(static_cast<uint16_t *>(a.out) + at) = u2{p[0], p[1]};
     }
     return;
   }
 #pragma unroll
-  for (int y = 0; y < 8; ++y) {
+  for (int y = 0; y < W; ++y) {
     if (n + y >= a.channels) continue;
     if constexpr (DT == SB_F32) static_cast<float *>(a.out)[at + y] = v[y];
     else static_cast<uint16_t *>(a.out)[at + y] = (uint16_t)Half<DT>::pack(v[y], v[y]);
   }
+}
+
+// -- few rows: the weights straight to the matrix unit ---------------------------
+//
+// Up to 64 rows of x: reading the weights binds. A workgroup takes 16 channels, its
+// waves a stretch of the depth each, in pieces of 64 that are loaded as the matrix
+// unit wants them (lane: channel l % 16, values 16 (l / 16) .. + 15); the waves'
+// sums meet in LDS.
+
+constexpr int FEW_WAVES = 8, FEW_STEP = 64;
+
+template <int DT, int MT, int NT>
+__global__ __launch_bounds__(64 * FEW_WAVES) void k_linear_few(sb_linear_args a, bool wide) {
+  constexpr int BATCH = MT == 1 ? 8 : 4;   // pieces in flight
+  static_assert(FEW_WAVES >= MT * NT, "a thread for every 4 results");
+  __shared__ alignas(16) int sums[FEW_WAVES][16 * MT][16 * NT];   // [wave][row of x][channel]
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l16 = lane & 15, g4 = lane >> 4, n0 = blockIdx.x * (16 * NT);
+  const unsigned char *wp[NT], *xp[MT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) wp[j] = static_cast<const unsigned char *>(a.w) + min(n0 + 16 * j + l16, a.channels - 1) * a.w_row;
+#pragma unroll
+  for (int i = 0; i < MT; ++i) xp[i] = static_cast<const unsigned char *>(a.x) + min(16 * i + l16, a.rows - 1) * a.x_row;
+  // What the results are scaled by is loaded ahead.
+  const int m = threadIdx.x / (4 * NT), at4 = threadIdx.x % (4 * NT) * 4, n = n0 + at4;
+  const bool mine = m < min(a.rows, 16 * MT);
+  float sx = 0.0f, sw[4], bias[4];
+  if (mine) {
+    sx = a.x_scale[m];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) {
+      const int at = min(n + y, a.channels - 1);
+      sw[y] = a.w_scale[at];
+      bias[y] = a.bias ? a.bias[at] : 0.0f;
+    }
+  }
+  i4 c[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) c[i][j] = i4{0, 0, 0, 0};
+  const int steps = (a.depth + FEW_STEP - 1) / FEW_STEP, each = (steps + FEW_WAVES - 1) / FEW_WAVES;
+  const int end = min(min(w * each + each, steps) * FEW_STEP, a.depth);
+  auto batch = [&](int k0, auto whole) {   // BATCH pieces; not whole: those before the end
+    i4 wv[BATCH][NT], xv[BATCH][MT];
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u) {
+      const int k = k0 + u * FEW_STEP + 16 * g4, at = decltype(whole)::value ? k : min(k, a.depth - 16);
+#pragma unroll
+      for (int j = 0; j < NT; ++j) wv[u][j] = *reinterpret_cast<const i4 *>(wp[j] + at);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) xv[u][i] = *reinterpret_cast<const i4 *>(xp[i] + at);
+    }
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u) {
+      const int k = k0 + u * FEW_STEP + 16 * g4;
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        if (!decltype(whole)::value && k >= end) wv[u][j] = i4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < MT; ++i) c[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv[u][j], xv[u][i], c[i][j], 0, 0, 0);
+      }
+    }
+  };
+  int k = w * each * FEW_STEP;
+  for (; k + BATCH * FEW_STEP <= end; k += BATCH * FEW_STEP) batch(k, std::true_type());
+  if (k < end) batch(k, std::false_type());
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) *reinterpret_cast<i4 *>(&sums[w][16 * i + l16][16 * j + 4 * g4]) = c[i][j];
+  __syncthreads();
+  if (!mine) return;
+  i4 total = {0, 0, 0, 0};
+#pragma unroll
+  for (int x = 0; x < FEW_WAVES; ++x) total += *reinterpret_cast<const i4 *>(&sums[x][m][at4]);
+  float v[4];
+#pragma unroll
+  for (int y = 0; y < 4; ++y) v[y] = scaled<DT>(total[y], sx, sw[y], bias[y]);
+  store_side_by_side<DT, 4>(a, m, n, v, wide);
 }
 
 // -- many rows: tiles in LDS -----------------------------------------------------
@@ -260,7 +356,7 @@ __device__ __forceinline__ void interleave() {
 }
 
 template <int DT, int MT, int NT>
-__global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_linear_args a, int tiles_m, int tiles_n) {
+__global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_linear_args a, int tiles_m, int tiles_n, bool wide) {
   constexpr int BM = 64 * MT, BN = 64 * NT, KS = TILE_K / 32;
   constexpr int XP = BM * 8 / 256, WP = BN * 8 / 256;   // 16-byte pieces of a tile that a thread brings
   __shared__ TileShared<MT, NT> sh;
@@ -358,7 +454,6 @@ __global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_l
   if (t + 1 < steps) tile(t++, std::true_type(), std::false_type());
   tile(t, std::false_type(), std::false_type());
   // Lane: row m, of products j and j + 1 channels 8 (2 (e / 4) + h2) + 4 (j % 2) + e % 4.
-  const bool wide = (a.out_row * (DT == SB_F32 ? 4 : 2)) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
 #pragma unroll
   for (int j = 0; j < NT; j += 2) {
 #pragma unroll
@@ -379,7 +474,7 @@ __global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_l
         float v[8];
 #pragma unroll
         for (int y = 0; y < 8; ++y) v[y] = scaled<DT>(c[i][j + (y >> 2)][e + (y & 3)], sx, sw[y], bias[y]);
-        store8<DT>(a, m, n, v, wide);
+        store_side_by_side<DT, 8>(a, m, n, v, wide);
       }
     }
   }
@@ -387,18 +482,24 @@ __global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_l
 
 template <int DT>
 hipError_t linear(const sb_linear_args &a, int n_cu, void *work, hipStream_t s) {
+  const bool wide = (a.out_row * (DT == SB_F32 ? 4 : 2)) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
   const auto tiles = [&](auto kernel, int bm, int bn) {
     const int tm = (a.rows + bm - 1) / bm, tn = (a.channels + bn - 1) / bn;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(tm * tn)), dim3(256), 0, s, a, tm, tn);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tm * tn)), dim3(256), 0, s, a, tm, tn, wide);
     return hipGetLastError();
   };
-  if (a.rows > 64) {
-    const long long large = ((a.rows + 255LL) / 256) * ((a.channels + 255LL) / 256);
-    if (large >= n_cu) return tiles(k_linear_tiles<DT, 4, 4>, 256, 256);
-    return tiles(k_linear_tiles<DT, 2, 2>, 128, 128);
+  if (a.rows <= 64) {
+    const auto few = [&](auto kernel, int channels) {
+      hipLaunchKernelGGL(kernel, dim3((unsigned)((a.channels + channels - 1) / channels)), dim3(64 * FEW_WAVES), 0, s, a, wide);
+      return hipGetLastError();
+    };
+    if (a.rows <= 16) return few(k_linear_few<DT, 1, 1>, 16);
+    if (a.rows <= 32) return few(k_linear_few<DT, 2, 2>, 32);
+    return few(k_linear_few<DT, 4, 2>, 32);
   }
-  hipLaunchKernelGGL((k_linear<DT>), dim3((unsigned)((a.channels + 63LL) / 64), (unsigned)((a.rows + 63LL) / 64)), dim3(256), 0, s, a);
-  return hipGetLastError();
+  const long long large = ((a.rows + 255LL) / 256) * ((a.channels + 255LL) / 256);
+  if (large >= n_cu) return tiles(k_linear_tiles<DT, 4, 4>, 256, 256);
+  return tiles(k_linear_tiles<DT, 2, 2>, 128, 128);
 }
 
 }  // namespace
