@@ -333,6 +333,7 @@ template <int MT, int NT>
 struct TileShared {
   alignas(16) unsigned char x[2][64 * MT * TILE_K];
   alignas(16) unsigned char w[2][64 * NT * TILE_K];
+  alignas(16) float x_scale[64 * MT], w_scale[64 * NT], bias[64 * NT];   // (read from memory at the end they took a quarter of the time)
 };
 
 __device__ __forceinline__ int x_place(int row, int piece) { return row * TILE_K + ((piece ^ (row & 7)) << 4); }
@@ -343,10 +344,12 @@ __device__ __forceinline__ int w_place(int row, int piece) { return row * TILE_K
 template <int PRODUCTS, int READS, int WRITES, int LOADS, int X = 0>
 __device__ __forceinline__ void interleave() {
   if constexpr (X < PRODUCTS) {
-    constexpr int r = READS * (X + 1) / PRODUCTS - READS * X / PRODUCTS, w = WRITES * (X + 1) / PRODUCTS - WRITES * X / PRODUCTS;
+    // (Reads in the first half: the products behind them wait for them.)
+    constexpr int H = (PRODUCTS + 1) / 2, Y = X < H ? X + 1 : H;
+    constexpr int r = READS * Y / H - READS * (X < H ? X : H) / H, w = WRITES * (X + 1) / PRODUCTS - WRITES * X / PRODUCTS;
     constexpr int l = LOADS * (X + 1) / PRODUCTS - LOADS * X / PRODUCTS;
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
     if constexpr (r > 0) __builtin_amdgcn_sched_group_barrier(0x100, r, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
     if constexpr (w > 0) __builtin_amdgcn_sched_group_barrier(0x200, w, 0);
     if constexpr (l > 0) __builtin_amdgcn_sched_group_barrier(0x020, l, 0);
     interleave<PRODUCTS, READS, WRITES, LOADS, X + 1>();
@@ -355,7 +358,7 @@ __device__ __forceinline__ void interleave() {
   }
 }
 
-template <int DT, int MT, int NT>
+template <int DT, int MT, int NT, int R>
 __global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_linear_args a, int tiles_m, int tiles_n, bool wide) {
   constexpr int BM = 64 * MT, BN = 64 * NT, KS = TILE_K / 32;
   constexpr int XP = BM * 8 / 256, WP = BN * 8 / 256;   // 16-byte pieces of a tile that a thread brings
@@ -369,30 +372,36 @@ __global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_l
   const int g = p / (GROUP * tiles_n), in = p - g * (GROUP * tiles_n), high = min(tiles_m - g * GROUP, GROUP);
   const int m0 = (g * GROUP + in % high) * BM, n0 = in / high * BN;
   const int row0 = threadIdx.x >> 3, piece = threadIdx.x & 7;
+  if (threadIdx.x < BM) sh.x_scale[threadIdx.x] = a.x_scale[min(m0 + (int)threadIdx.x, a.rows - 1)];
+  if (threadIdx.x < BN) {
+    const int n = min(n0 + (int)threadIdx.x, a.channels - 1);
+    sh.w_scale[threadIdx.x] = a.w_scale[n];
+    sh.bias[threadIdx.x] = a.bias ? a.bias[n] : 0.0f;
+  }
   const unsigned char *xs[XP], *ws[WP];
 #pragma unroll
   for (int i = 0; i < XP; ++i) xs[i] = static_cast<const unsigned char *>(a.x) + min(m0 + row0 + 32 * i, a.rows - 1) * a.x_row + 16 * piece;
 #pragma unroll
   for (int i = 0; i < WP; ++i) ws[i] = static_cast<const unsigned char *>(a.w) + min(n0 + row0 + 32 * i, a.channels - 1) * a.w_row + 16 * piece;
-  u4 xr[XP], wr[WP];
-  auto load_x = [&](int k) {
+  u4 xr[R][XP], wr[R][WP];
+  auto load_x = [&](int k, int r) {
     const int at = min(k, a.depth - 16 - 16 * piece);   // (behind the last value: any that is)
 #pragma unroll
-    for (int i = 0; i < XP; ++i) xr[i] = *reinterpret_cast<const u4 *>(xs[i] + at);
+    for (int i = 0; i < XP; ++i) xr[r][i] = *reinterpret_cast<const u4 *>(xs[i] + at);
   };
-  auto load_w = [&](int k) {
+  auto load_w = [&](int k, int r) {
     const int at = min(k, a.depth - 16 - 16 * piece);
 #pragma unroll
-    for (int i = 0; i < WP; ++i) wr[i] = *reinterpret_cast<const u4 *>(ws[i] + at);
+    for (int i = 0; i < WP; ++i) wr[r][i] = *reinterpret_cast<const u4 *>(ws[i] + at);
   };
-  auto write_x = [&](int k, int to, auto last) {   // of the last tile, zeros behind the last value
+  auto write_x = [&](int k, int r, int to, auto last) {   // of the last tile, zeros behind the last value
     const unsigned int keep = !decltype(last)::value || k + 16 * piece < a.depth ? ~0u : 0u;
 #pragma unroll
-    for (int i = 0; i < XP; ++i) *reinterpret_cast<u4 *>(&sh.x[to][x_place(row0 + 32 * i, piece)]) = xr[i] & keep;
+    for (int i = 0; i < XP; ++i) *reinterpret_cast<u4 *>(&sh.x[to][x_place(row0 + 32 * i, piece)]) = xr[r][i] & keep;
   };
-  auto write_w = [&](int to) {
+  auto write_w = [&](int r, int to) {
 #pragma unroll
-    for (int i = 0; i < WP; ++i) *reinterpret_cast<u4 *>(&sh.w[to][w_place(row0 + 32 * i, piece)]) = wr[i];
+    for (int i = 0; i < WP; ++i) *reinterpret_cast<u4 *>(&sh.w[to][w_place(row0 + 32 * i, piece)]) = wr[r][i];
   };
   const int xrow = (w >> 1) * 32 * MT + l32, wrow = (w & 1) * 32 * NT + (l32 >> 2) * 8 + (l32 & 3);
   i4 xf[2][MT], wf[2][NT];
@@ -416,21 +425,22 @@ __global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_l
       for (int j = 0; j < NT; ++j) c[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[from][j], xf[from][i], c[i][j], 0, 0, 0);
   };
   // A tile's work: operands come from LDS a step of 32 before their products; in
-  // between the next tile goes to LDS (WRITE) and the one after it is loaded (LOAD).
-  auto tile = [&](int t, auto write_next, auto load_next) {
+  // between the next tile goes to LDS (WRITE) from registers r, into which the tile
+  // R after it is loaded (LOAD).
+  auto tile = [&](int t, int r, auto write_next, auto load_next, auto mask) {
     constexpr bool WRITE = decltype(write_next)::value, LOAD = decltype(load_next)::value;
     const int cur = t & 1, next = cur ^ 1;
     fetch(cur, 1, 1);
-    if constexpr (WRITE) write_x((t + 1) * TILE_K, next, std::bool_constant<!LOAD>());
+    if constexpr (WRITE) write_x((t + 1) * TILE_K, r, next, mask);
     multiply(0);
     interleave<MT * NT, MT + NT, WRITE ? XP : 0, 0>();
     fetch(cur, 2, 0);
-    if constexpr (LOAD) load_x((t + 2) * TILE_K);
-    if constexpr (WRITE) write_w(next);
+    if constexpr (LOAD) load_x((t + 1 + R) * TILE_K, r);
+    if constexpr (WRITE) write_w(r, next);
     multiply(1);
     interleave<MT * NT, MT + NT, WRITE ? WP : 0, LOAD ? XP : 0>();
     fetch(cur, 3, 1);
-    if constexpr (LOAD) load_w((t + 2) * TILE_K);
+    if constexpr (LOAD) load_w((t + 1 + R) * TILE_K, r);
     multiply(0);
     interleave<MT * NT, MT + NT, 0, LOAD ? WP : 0>();
     if constexpr (WRITE) {   // all of this tile is in registers, the next one in LDS
@@ -440,37 +450,59 @@ __global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_l
     multiply(1);
     interleave<MT * NT, WRITE ? MT + NT : 0, 0, 0>();
   };
+  const std::true_type yes;
+  const std::false_type no;
   const int steps = (a.depth + TILE_K - 1) / TILE_K;
-  load_x(0);
-  load_w(0);
-  write_x(0, 0, std::true_type());
-  write_w(0);
-  load_x(TILE_K);
-  load_w(TILE_K);
+  load_x(0, 0);
+  load_w(0, 0);
+  write_x(0, 0, 0, yes);
+  write_w(0, 0);
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    __builtin_amdgcn_sched_barrier(0);   // (in this order: waits are for all loads up to one)
+    load_x((r + 1) * TILE_K, r);
+    __builtin_amdgcn_sched_barrier(0);
+    load_w((r + 1) * TILE_K, r);
+  }
   __syncthreads();
   fetch(0, 0, 0);
   int t = 0;
-  for (; t + 2 < steps; ++t) tile(t, std::true_type(), std::true_type());
-  if (t + 1 < steps) tile(t++, std::true_type(), std::false_type());
-  tile(t, std::false_type(), std::false_type());
+  if constexpr (R == 1) {
+    for (; t + 2 < steps; ++t) tile(t, 0, yes, yes, no);
+    if (t + 1 < steps) tile(t++, 0, yes, no, yes);
+    tile(t, 0, no, no, no);
+  } else {   // (tiles behind the last one are loaded from its end, and zeros)
+    // (One way out of the loop, at its end: no way then leads from one tile to any
+    // but the next, and the compiler knows what has to be waited for.)
+    for (; t + R <= steps; t += R) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) tile(t + r, r, yes, yes, yes);
+    }
+#pragma unroll
+    for (int r = 0; r + 1 < R; ++r)
+      if (t + r < steps) tile(t + r, r, yes, yes, yes);
+  }
   // Lane: row m, of products j and j + 1 channels 8 (2 (e / 4) + h2) + 4 (j % 2) + e % 4.
 #pragma unroll
   for (int j = 0; j < NT; j += 2) {
 #pragma unroll
     for (int e = 0; e < 16; e += 4) {
-      const int n = n0 + (w & 1) * 32 * NT + 64 * (j >> 1) + 8 * (2 * (e >> 2) + h2);
+      const int at = (w & 1) * 32 * NT + 64 * (j >> 1) + 8 * (2 * (e >> 2) + h2), n = n0 + at;
       float sw[8], bias[8];
 #pragma unroll
-      for (int y = 0; y < 8; ++y) {
-        const int at = min(n + y, a.channels - 1);
-        sw[y] = a.w_scale[at];
-        bias[y] = a.bias ? a.bias[at] : 0.0f;
+      for (int y = 0; y < 8; y += 4) {
+        const f4 s4 = *reinterpret_cast<const f4 *>(&sh.w_scale[at + y]), b4 = *reinterpret_cast<const f4 *>(&sh.bias[at + y]);
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          sw[y + z] = s4[z];
+          bias[y + z] = b4[z];
+        }
       }
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        const int m = m0 + (w >> 1) * 32 * MT + 32 * i + l32;
+        const int row = (w >> 1) * 32 * MT + 32 * i + l32, m = m0 + row;
         if (m >= a.rows) continue;
-        const float sx = a.x_scale[m];
+        const float sx = sh.x_scale[row];
         float v[8];
 #pragma unroll
         for (int y = 0; y < 8; ++y) v[y] = scaled<DT>(c[i][j + (y >> 2)][e + (y & 3)], sx, sw[y], bias[y]);
@@ -498,8 +530,8 @@ hipError_t linear(const sb_linear_args &a, int n_cu, void *work, hipStream_t s) 
     return few(k_linear_few<DT, 4, 2>, 32);
   }
   const long long large = ((a.rows + 255LL) / 256) * ((a.channels + 255LL) / 256);
-  if (large >= n_cu) return tiles(k_linear_tiles<DT, 4, 4>, 256, 256);
-  return tiles(k_linear_tiles<DT, 2, 2>, 128, 128);
+  if (large >= n_cu) return tiles(k_linear_tiles<DT, 4, 4, 1>, 256, 256);
+  return tiles(k_linear_tiles<DT, 2, 2, 1>, 128, 128);
 }
 
 }  // namespace
