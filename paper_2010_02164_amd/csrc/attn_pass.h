@@ -167,12 +167,12 @@ __device__ __forceinline__ bool sees(const sb_attention_args &a, int p, int key)
   return (key <= p) & ((a.window == 0) | (key > max(p, 0) - a.window) | (key < a.sinks));   // (no branches)
 }
 
-// One wave's pass over its tiles t0, t0 + 4, ... < t_end: the 16 rows' sums, their
+// One wave's pass over its tiles t0, t0 + 4, ... < t_end: the 16 RT rows' sums, their
 // maxima and this lane's share of the weights' sums. False where it stopped.
-template <int DT, int D, bool CAREFUL>
+template <int DT, int D, int RT, bool CAREFUL>
 __device__ __forceinline__ bool few_keys(const sb_attention_args &a, const Span &s, const int *table, const uint16_t *kc, const uint16_t *vc,
-                                         const u4 (&q)[D / 32], int p, bool real, int t0, int t_end, unsigned char *lds, f4 (&o)[D / 16],
-                                         float &mx, float &sum) {
+                                         const u4 (&q)[RT][D / 32], const int (&p)[RT], const bool (&real)[RT], int t0, int t_end,
+                                         unsigned char *lds, f4 (&o)[RT][D / 16], float (&mx)[RT], float (&sum)[RT]) {
   constexpr int VS = 2 * D + 32;            // bytes of a V row in LDS: 8 rows of 32 bytes in different banks
   constexpr int KS = D / 32, NV = D / 16;   // products per score, 16-byte pieces of V per lane
   constexpr int DT16 = D / 16;
@@ -180,10 +180,13 @@ __device__ __forceinline__ bool few_keys(const sb_attention_args &a, const Span 
   const int lane = threadIdx.x & 63, g4 = lane >> 4, l16 = lane & 15, v_row = lane / (D / 8), v_col = lane % (D / 8);
   const double inv_page = 1.0 / a.page_size;
   const float c = (float)(a.scale * LOG2E);
-  mx = -INFINITY;
-  sum = 0.0f;
 #pragma unroll
-  for (int x = 0; x < DT16; ++x) o[x] = f4{0, 0, 0, 0};
+  for (int r = 0; r < RT; ++r) {
+    mx[r] = -INFINITY;
+    sum[r] = 0.0f;
+#pragma unroll
+    for (int x = 0; x < DT16; ++x) o[r][x] = f4{0, 0, 0, 0};
+  }
   // Where a tile's keys lie (lane l: key l % 32), looked up a tile ahead. Its
   // rows are loaded when they are needed: few registers, and so many waves to
   // have loads in flight, did better than loads ahead (286 against 306 us).
@@ -213,48 +216,56 @@ __device__ __forceinline__ bool few_keys(const sb_attention_args &a, const Span 
     load_k(k, page, place);
     next = find(t + AT_WAVES, next_place);
     const bool plain = there == 0xFFFFFFFFu && s.all_see(a, s.key(t * FEW_KEYS), s.key(t * FEW_KEYS + FEW_KEYS - 1));
-    f4 sc[2] = {f4{0, 0, 0, 0}, f4{0, 0, 0, 0}};
+    f4 sc[RT][2];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) sc[r][0] = sc[r][1] = f4{0, 0, 0, 0};
 #pragma unroll
     for (int x = 0; x < KS; ++x)
 #pragma unroll
-      for (int hf = 0; hf < 2; ++hf) sc[hf] = mfma16<DT>(k[hf][x], q[x], sc[hf]);
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) sc[r][hf] = mfma16<DT>(k[hf][x], q[r][x], sc[r][hf]);
     load_v(v, page, place);
-    // Lane: keys 16 hf + 4 g4 + j of row l16, as scalars from here on (masks
-    // written into the products' vectors have been compiled wrongly).
-    float e[8];
-#pragma unroll
-    for (int x = 0; x < 8; ++x) e[x] = sc[x >> 2][x & 3] * c;
-    if (!plain) {
-#pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        const int at = 16 * (x >> 2) + 4 * g4 + (x & 3);
-        const bool on = real & (((there >> at) & 1u) != 0) & sees(a, p, s.key(t * FEW_KEYS + at));
-        e[x] = on ? e[x] : -INFINITY;
-      }
-    }
-    float tm = e[0];
-#pragma unroll
-    for (int x = 1; x < 8; ++x) tm = fmaxf(tm, e[x]);
-    tm = fmaxf(tm, __shfl_xor(tm, 16, 64));
-    tm = fmaxf(tm, __shfl_xor(tm, 32, 64));
-    const float mn = fmaxf(mx, tm), top = mn == -INFINITY ? 0.0f : mn, base = top - raise<DT>(0);
-    const float shrink = __builtin_amdgcn_exp2f(mx - top);
-    mx = mn;
-    float ts = 0.0f;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      e[x] = __builtin_amdgcn_exp2f(e[x] - base);
-      ts += e[x];
-    }
-    sum = sum * shrink + ts;
     // Each weight in two parts, the rounded one and what that leaves: reading the
     // cache binds here, and the second product costs nothing (238.3 us a batch's
     // step, without 238.4).
-    u4 pk, pl;
+    u4 pk[RT], pl[RT];
+    float shrink[RT];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      pk[x] = Half<DT>::pack(e[2 * x], e[2 * x + 1]);
-      pl[x] = Half<DT>::pack(e[2 * x] - Half<DT>::to_float(pk[x] & 0xFFFFu), e[2 * x + 1] - Half<DT>::to_float(pk[x] >> 16));
+    for (int r = 0; r < RT; ++r) {
+      // Lane: keys 16 hf + 4 g4 + j of row l16, as scalars from here on (masks
+      // written into the products' vectors have been compiled wrongly).
+      float e[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) e[x] = sc[r][x >> 2][x & 3] * c;
+      if (!plain) {
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const int at = 16 * (x >> 2) + 4 * g4 + (x & 3);
+          const bool on = real[r] & (((there >> at) & 1u) != 0) & sees(a, p[r], s.key(t * FEW_KEYS + at));
+          e[x] = on ? e[x] : -INFINITY;
+        }
+      }
+      float tm = e[0];
+#pragma unroll
+      for (int x = 1; x < 8; ++x) tm = fmaxf(tm, e[x]);
+      tm = fmaxf(tm, __shfl_xor(tm, 16, 64));
+      tm = fmaxf(tm, __shfl_xor(tm, 32, 64));
+      const float mn = fmaxf(mx[r], tm), top = mn == -INFINITY ? 0.0f : mn, base = top - raise<DT>(0);
+      shrink[r] = __builtin_amdgcn_exp2f(mx[r] - top);
+      mx[r] = mn;
+      float ts = 0.0f;
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        e[x] = __builtin_amdgcn_exp2f(e[x] - base);
+        ts += e[x];
+      }
+      sum[r] = sum[r] * shrink[r] + ts;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        pk[r][x] = Half<DT>::pack(e[2 * x], e[2 * x + 1]);
+        pl[r][x] = Half<DT>::pack(e[2 * x] - Half<DT>::to_float(pk[r][x] & 0xFFFFu), e[2 * x + 1] - Half<DT>::to_float(pk[r][x] >> 16));
+      }
     }
     bool bad = false;
 #pragma unroll
@@ -269,13 +280,15 @@ __device__ __forceinline__ bool few_keys(const sb_attention_args &a, const Span 
     wave_lds_fence();
     const unsigned char *vt = lds + (4 * g4 + (l16 >> 2)) * VS + (l16 & 3) * 8;
     if (CAREFUL && !plain) {
-      const u4 pn = not_zero<DT>(pk);
 #pragma unroll
       for (int x = 0; x < DT16; ++x) {
         const u2 v0 = read_transposed(vt + 32 * x), v1 = read_transposed(vt + 16 * VS + 32 * x);
-        const f4 hit = mfma16<DT>(not_finite<DT>(u4{v0[0], v0[1], v1[0], v1[1]}), pn, f4{0, 0, 0, 0});
 #pragma unroll
-        for (int j = 0; j < 4; ++j) o[x][j] = hit[j] > 0.0f ? NAN : o[x][j];
+        for (int r = 0; r < RT; ++r) {
+          const f4 hit = mfma16<DT>(not_finite<DT>(u4{v0[0], v0[1], v1[0], v1[1]}), not_zero<DT>(pk[r]), f4{0, 0, 0, 0});
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[r][x][j] = hit[j] > 0.0f ? NAN : o[r][x][j];
+        }
       }
       wave_lds_fence();
       for (int piece = lane; piece < FEW_KEYS * (D / 8); piece += 64) {
@@ -288,7 +301,8 @@ __device__ __forceinline__ bool few_keys(const sb_attention_args &a, const Span 
     for (int x = 0; x < DT16; ++x) {
       const u2 v0 = read_transposed(vt + 32 * x), v1 = read_transposed(vt + 16 * VS + 32 * x);
       const u4 vv = {v0[0], v0[1], v1[0], v1[1]};
-      o[x] = mfma16<DT>(vv, pl, mfma16<DT>(vv, pk, o[x] * shrink));
+#pragma unroll
+      for (int r = 0; r < RT; ++r) o[r][x] = mfma16<DT>(vv, pl[r], mfma16<DT>(vv, pk[r], o[r][x] * shrink[r]));
     }
     wave_lds_fence();
   }
@@ -303,62 +317,74 @@ constexpr int few_groups(int D) { return D == 64 ? 3 : D == 128 ? 2 : 1; }
 // to say so).
 __device__ __forceinline__ int few_tiles(const Span &s) { return max((s.n_vis + FEW_KEYS - 1) / FEW_KEYS, 1); }
 
-template <int D>
+template <int D, int RT = 1>
 struct FewShared {
   static constexpr int VS = 2 * D + 32;
   alignas(16) unsigned char v[AT_WAVES][FEW_KEYS * VS];
-  float2 stats[AT_WAVES][FEW_ROWS];
+  float2 stats[AT_WAVES][RT * FEW_ROWS];
   static_assert(FEW_KEYS * VS >= FEW_ROWS * D * 4, "the waves' sums fit where V was");
 };
 
-// Tiles t_begin .. t_end of the span's rows, by all waves of a workgroup: put gets
-// each row's number, 4 values' place and their sums, and the row's maximum and sum
-// of weights.
-template <int DT, int D, class Put>
+// Tiles t_begin .. t_end of the span's 16 RT rows, by all waves of a workgroup: put
+// gets each row's number, 4 values' place and their sums, and the row's maximum and
+// sum of weights.
+template <int DT, int D, int RT = 1, class Put>
 __device__ __forceinline__ void few_unit(const sb_attention_args &a, const Span &s, int hk, const int *table, int t_begin, int t_end,
-                                         FewShared<D> &sh, const Put &put) {
+                                         FewShared<D, RT> &sh, const Put &put) {
   constexpr int DT16 = D / 16, KS = D / 32;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, g4 = lane >> 4, l16 = lane & 15;
   const int G = a.q_heads / a.kv_heads;
   const uint16_t *kc = static_cast<const uint16_t *>(a.k_cache) + hk * a.kc_head;
   const uint16_t *vc = static_cast<const uint16_t *>(a.v_cache) + hk * a.vc_head;
-  const int row = s.r0 + l16, i = row / G, p = s.position(i);
-  const bool real = row < s.rows;
-  u4 q[KS];
+  int p[RT];
+  bool real[RT];
+  u4 q[RT][KS];
 #pragma unroll
-  for (int x = 0; x < KS; ++x) {
-    const uint16_t *src = static_cast<const uint16_t *>(a.q) + (s.q0 + i) * a.q_token + (hk * G + row - i * G) * a.q_head;
-    q[x] = real ? *reinterpret_cast<const u4 *>(src + 32 * x + 8 * g4) : u4{0, 0, 0, 0};
+  for (int r = 0; r < RT; ++r) {
+    const int row = s.r0 + FEW_ROWS * r + l16, i = row / G;
+    p[r] = s.position(i);
+    real[r] = row < s.rows;
+#pragma unroll
+    for (int x = 0; x < KS; ++x) {
+      const uint16_t *src = static_cast<const uint16_t *>(a.q) + (s.q0 + i) * a.q_token + (hk * G + row - i * G) * a.q_head;
+      q[r][x] = real[r] ? *reinterpret_cast<const u4 *>(src + 32 * x + 8 * g4) : u4{0, 0, 0, 0};
+    }
   }
-  f4 o[DT16];
-  float mx, sum;
-  if (!few_keys<DT, D, false>(a, s, table, kc, vc, q, p, real, t_begin + w, t_end, &sh.v[w][0], o, mx, sum))
-    few_keys<DT, D, true>(a, s, table, kc, vc, q, p, real, t_begin + w, t_end, &sh.v[w][0], o, mx, sum);
-  sum += __shfl_xor(sum, 16, 64);
-  sum += __shfl_xor(sum, 32, 64);
-  // The four waves' parts: sums side by side where V was.
+  f4 o[RT][DT16];
+  float mx[RT], sum[RT];
+  if (!few_keys<DT, D, RT, false>(a, s, table, kc, vc, q, p, real, t_begin + w, t_end, &sh.v[w][0], o, mx, sum))
+    few_keys<DT, D, RT, true>(a, s, table, kc, vc, q, p, real, t_begin + w, t_end, &sh.v[w][0], o, mx, sum);
   float *os = reinterpret_cast<float *>(&sh.v[w][0]);
 #pragma unroll
-  for (int x = 0; x < DT16; ++x) *reinterpret_cast<f4 *>(os + l16 * D + 16 * x + 4 * g4) = o[x];
-  if (g4 == 0) sh.stats[w][l16] = make_float2(mx, sum);
-  __syncthreads();
-  for (int e = threadIdx.x; e < FEW_ROWS * D / 4; e += AT_THREADS) {
-    const int rr = e / (D / 4), col = (e - rr * (D / 4)) * 4, rw = s.r0 + rr;
-    if (rw >= s.rows) continue;
-    float m4 = -INFINITY, l4 = 0.0f;
-    f4 acc = {0, 0, 0, 0};
-#pragma unroll
-    for (int x = 0; x < AT_WAVES; ++x) m4 = fmaxf(m4, sh.stats[x][rr].x);
-    const float base = m4 == -INFINITY ? 0.0f : m4;
-#pragma unroll
-    for (int x = 0; x < AT_WAVES; ++x) {
-      const float f = __builtin_amdgcn_exp2f(sh.stats[x][rr].x - base);
-      l4 += f * sh.stats[x][rr].y;
-      acc += f * *reinterpret_cast<const f4 *>(reinterpret_cast<const float *>(&sh.v[x][0]) + rr * D + col);
-    }
-    put(rw, col, m4, l4, acc);
+  for (int r = 0; r < RT; ++r) {
+    sum[r] += __shfl_xor(sum[r], 16, 64);
+    sum[r] += __shfl_xor(sum[r], 32, 64);
+    if (g4 == 0) sh.stats[w][FEW_ROWS * r + l16] = make_float2(mx[r], sum[r]);
   }
-  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    // The four waves' parts of 16 rows: sums side by side where V was.
+#pragma unroll
+    for (int x = 0; x < DT16; ++x) *reinterpret_cast<f4 *>(os + l16 * D + 16 * x + 4 * g4) = o[r][x];
+    __syncthreads();
+    for (int e = threadIdx.x; e < FEW_ROWS * D / 4; e += AT_THREADS) {
+      const int rr = e / (D / 4), col = (e - rr * (D / 4)) * 4, sr = FEW_ROWS * r + rr, rw = s.r0 + sr;
+      if (rw >= s.rows) continue;
+      float m4 = -INFINITY, l4 = 0.0f;
+      f4 acc = {0, 0, 0, 0};
+#pragma unroll
+      for (int x = 0; x < AT_WAVES; ++x) m4 = fmaxf(m4, sh.stats[x][sr].x);
+      const float base = m4 == -INFINITY ? 0.0f : m4;
+#pragma unroll
+      for (int x = 0; x < AT_WAVES; ++x) {
+        const float f = __builtin_amdgcn_exp2f(sh.stats[x][sr].x - base);
+        l4 += f * sh.stats[x][sr].y;
+        acc += f * *reinterpret_cast<const f4 *>(reinterpret_cast<const float *>(&sh.v[x][0]) + rr * D + col);
+      }
+      put(rw, col, m4, l4, acc);
+    }
+    __syncthreads();
+  }
 }
 
 // What the waves of k_attn_many share: two tiles of K and V, one worked on
