@@ -74,23 +74,36 @@ __global__ __launch_bounds__(BD_THREADS) void k_bounds(sb_bounds_args a) {
 
 constexpr int SL_THREADS = 256, SL_WAVES = 4;
 
-// Of token t: its position and how many pages there are up to it. position -1:
-// before the request's first; no request: false. (Called by all threads; `found` in LDS.)
+// Of token t: its request, its position (-1: before the request's first token) and
+// how many pages there are up to it. False where it is of no request. (Called by all
+// threads; `found` in LDS, 0 before. Starts and lengths are loaded together: each
+// wait for memory is a microsecond of a small call's.)
 struct Query {
   int b, p, n;
 };
-__device__ __forceinline__ bool query_of(const sb_select_args &a, int t, int *found, Query &q) {
-  if (threadIdx.x == 0) *found = -1;
+__device__ __forceinline__ bool query_of(const sb_select_args &a, int t, u64 *found, Query &q) {
+  for (int b = threadIdx.x; b < a.n_requests; b += blockDim.x) {
+    const int from = a.q_start[b], to = a.q_start[b + 1], len = a.lens[b];
+    if (from <= t && t < to) {
+      const long long p = max(min((long long)max(len, 0), (long long)a.max_pages * a.page_size) - to + t, -1LL);
+      atomicMax(found, (u64)b << 32 | (u64)(p + 2));
+    }
+  }
   __syncthreads();
-  for (int b = threadIdx.x; b < a.n_requests; b += SL_THREADS)
-    if (a.q_start[b] <= t && t < a.q_start[b + 1]) atomicMax(found, b);
-  __syncthreads();
-  q.b = *found;
-  if (q.b < 0) return false;
-  const long long len = min((long long)max(a.lens[q.b], 0), (long long)a.max_pages * a.page_size);
-  q.p = (int)max(len - a.q_start[q.b + 1] + t, -1LL);
+  const u64 at = *found;
+  if (at == 0) return false;
+  q.b = (int)(at >> 32);
+  q.p = (int)(uint32_t)at - 2;
   q.n = q.p < 0 ? 0 : q.p / a.page_size + 1;
   return true;
+}
+
+// Sums over neighbouring lanes (wave.h's stages).
+template <int S>
+__device__ __forceinline__ double add_stage(double v) {
+  u64 x, y;
+  stage64<S>((u64)__double_as_longlong(v), x, y);
+  return __longlong_as_double((long long)x) + __longlong_as_double((long long)y);
 }
 
 // A score as a number whose order is the scores': NaN last.
@@ -101,13 +114,16 @@ __device__ __forceinline__ u64 order_of(double score) {
 
 // Scores of the pages first .. n - last - 1 of token t0 + blockIdx.z, head
 // blockIdx.y, those of `chunk` pages a workgroup, to keys [tokens][kv_heads][max_pages].
+// Bound by reading the bounds: 48 requests of 5000 to 50000 tokens, pages of 16, 8
+// heads of 128: 84 us, 4.0 TB/s (heads side by side in the grid: 89; 2 or 8 loads of
+// each bound in flight: 90, 87; a load at a time: 96); where they come from L2, a
+// prompt's, 11 TB/s.
 template <int DT, int D>
 __global__ __launch_bounds__(SL_THREADS) void k_scores(sb_select_args a, int t0, int chunk, u64 *keys) {
   constexpr int L = D / 8, P = 64 / L;   // lanes of a page, pages a wave takes at once
-  __shared__ int found;
+  __shared__ u64 found;
   const int t = t0 + blockIdx.z, hk = blockIdx.y, G = a.q_heads / a.kv_heads, lane = threadIdx.x & 63, col = lane % L;
-  Query q;
-  if (!query_of(a, t, &found, q) || q.n <= (long long)a.first + a.top + a.last) return;
+  if (threadIdx.x == 0) found = 0;
   double up[8], down[8];
 #pragma unroll
   for (int x = 0; x < 8; ++x) up[x] = down[x] = 0.0;
@@ -121,6 +137,9 @@ __global__ __launch_bounds__(SL_THREADS) void k_scores(sb_select_args a, int t0,
       down[x] += f < 0.0f ? f : 0.0f;
     }
   }
+  __syncthreads();
+  Query q;
+  if (!query_of(a, t, &found, q) || q.n <= (long long)a.first + a.top + a.last) return;
   const int *table = a.table + q.b * a.table_stride;
   const long long row = (long long)a.kv_heads * D;
   const uint16_t *bounds = static_cast<const uint16_t *>(a.bounds) + (long long)hk * D + 8 * col;
@@ -128,55 +147,95 @@ __global__ __launch_bounds__(SL_THREADS) void k_scores(sb_select_args a, int t0,
   const int end = q.n - a.last;
   for (int at = blockIdx.x * chunk + a.first; at < end; at += gridDim.x * chunk) {
     const int stop = min(at + chunk, end);
-    for (int c0 = at + (threadIdx.x >> 6) * P; c0 < stop; c0 += SL_WAVES * P) {
-      const int c = c0 + lane / L, page = c < stop ? table[c] : -1;
-      const bool there = (unsigned)page < (unsigned)a.n_pages;
-      const uint16_t *src = bounds + (there ? 2LL * page * row : 0);
-      const u4 lo = *reinterpret_cast<const u4 *>(src), hi = *reinterpret_cast<const u4 *>(src + row);
-      double s = 0.0;
+    // A wave's pages are looked up together, then taken a few at a time, with their
+    // loads in flight together.
+    constexpr int BATCH = 4;
+    const int each = chunk / SL_WAVES, wave_stop = min(at + ((int)(threadIdx.x >> 6) + 1) * each, stop);   // (each: 16 to 128)
+    for (int c0 = at + (int)(threadIdx.x >> 6) * each; c0 < wave_stop; c0 += 64) {
+      const int page = c0 + lane < wave_stop ? table[c0 + lane] : -1;
+      for (int s0 = 0; s0 < 64 && c0 + s0 < wave_stop; s0 += BATCH * P) {
+        u4 lo[BATCH], hi[BATCH];
+        bool there[BATCH];
 #pragma unroll
-      for (int x = 0; x < 8; ++x) {
-        s = fma((double)Half<DT>::to_float(x & 1 ? hi[x >> 1] >> 16 : hi[x >> 1] & 0xFFFFu), up[x], s);
-        s = fma((double)Half<DT>::to_float(x & 1 ? lo[x >> 1] >> 16 : lo[x >> 1] & 0xFFFFu), down[x], s);
+        for (int x = 0; x < BATCH; ++x) {
+          const int mine = __shfl(page, s0 + x * P + lane / L, 64);
+          there[x] = (unsigned)mine < (unsigned)a.n_pages;
+          const uint16_t *src = bounds + (there[x] ? 2LL * mine * row : 0);
+          lo[x] = *reinterpret_cast<const u4 *>(src);
+          hi[x] = *reinterpret_cast<const u4 *>(src + row);
+        }
+#pragma unroll
+        for (int x = 0; x < BATCH; ++x) {
+          double s = 0.0;
+#pragma unroll
+          for (int y = 0; y < 8; ++y) {
+            s = fma((double)Half<DT>::to_float(y & 1 ? hi[x][y >> 1] >> 16 : hi[x][y >> 1] & 0xFFFFu), up[y], s);
+            s = fma((double)Half<DT>::to_float(y & 1 ? lo[x][y >> 1] >> 16 : lo[x][y >> 1] & 0xFFFFu), down[y], s);
+          }
+          s = add_stage<2>(add_stage<1>(add_stage<0>(s)));
+          if constexpr (L >= 16) s = add_stage<3>(s);
+          if constexpr (L >= 32) s = add_stage<4>(s);
+          const int c = c0 + s0 + x * P + lane / L;
+          if (col == 0 && c < wave_stop) out[c] = order_of(there[x] ? s : -INFINITY);
+        }
       }
-#pragma unroll
-      for (int o = 1; o < L; o <<= 1) s += __shfl_xor(s, o, 64);
-      if (col == 0 && c < stop) out[c] = there ? order_of(s) : order_of(-INFINITY);
     }
   }
 }
 
-constexpr int BINS = 2048, LIST = SL_THREADS;
+constexpr int BINS = 2048, LIST = 256;
 
 // The list of token t0 + blockIdx.x, head blockIdx.y: the key of the last page
 // taken is found by counting keys in bins, ever finer, until those of its bin fit
-// a list; then all pages are looked through in order.
-__global__ __launch_bounds__(SL_THREADS) void k_pick(sb_select_args a, int t0, const u64 *all_keys) {
-  __shared__ int found, bins[BINS], wave_sums[2][SL_WAVES][2], listed, bin_at, bin_before;
-  __shared__ u64 list[LIST], ends[SL_WAVES][2], cut_key;
+// a list; then the pages above it are written in order. A thread has PER keys that
+// follow each other in registers; where there are more pages than that, the passes
+// read them from memory again (48 requests of 5000 to 50000 tokens in pages of 16:
+// 20 us where all did).
+template <int THREADS, int PER>
+__global__ __launch_bounds__(THREADS) void k_pick(sb_select_args a, int t0, const u64 *all_keys) {
+  constexpr int WAVES = THREADS / 64;
+  __shared__ int bins[BINS], wave_sums[2][WAVES][2], listed, bin_at, bin_before;
+  __shared__ u64 found, list[LIST], ends[WAVES][2], cut_key;
   __shared__ int cut_equal;
   const int t = t0 + blockIdx.x, hk = blockIdx.y, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int width = a.first + a.top + a.last;
   int *out = a.pages + ((long long)t * a.kv_heads + hk) * width;
   Query q;
+  if (threadIdx.x == 0) found = 0;
+  __syncthreads();
   const bool real = query_of(a, t, &found, q);
   if (hk == 0 && threadIdx.x == 0)
     a.kept[t] = !real ? -1 : q.n <= width ? q.p + 1 : (width - 1) * a.page_size + q.p % a.page_size + 1;
   if (!real || q.n <= width) {
-    for (int x = threadIdx.x; x < width; x += SL_THREADS) out[x] = real && x < q.n ? a.table[q.b * a.table_stride + x] : -1;
+    for (int x = threadIdx.x; x < width; x += THREADS) out[x] = real && x < q.n ? a.table[q.b * a.table_stride + x] : -1;
     return;
   }
   const int *table = a.table + q.b * a.table_stride;
-  for (int x = threadIdx.x; x < a.first; x += SL_THREADS) out[x] = table[x];
-  for (int x = threadIdx.x; x < a.last; x += SL_THREADS) out[a.first + a.top + x] = table[q.n - a.last + x];
-  if (a.top == 0) return;
   const u64 *keys = all_keys + ((long long)blockIdx.x * a.kv_heads + hk) * a.max_pages;
-  const int begin = a.first, end = q.n - a.last;
-  u64 lo = ~0ULL, hi = 0;
-  for (int c = begin + threadIdx.x; c < end; c += SL_THREADS) {
-    lo = min(lo, keys[c]);
-    hi = max(hi, keys[c]);
+  const int begin = a.first, end = q.n - a.last, mine = begin + threadIdx.x * PER;
+  const bool held = end - begin <= THREADS * PER;   // all keys in registers
+  u64 k[PER];
+  if (held && a.top > 0) {
+#pragma unroll
+    for (int x = 0; x < PER; ++x) k[x] = mine + x < end ? keys[mine + x] : 0;
   }
+  for (int x = threadIdx.x; x < a.first; x += THREADS) out[x] = table[x];
+  for (int x = threadIdx.x; x < a.last; x += THREADS) out[a.first + a.top + x] = table[q.n - a.last + x];
+  if (a.top == 0) return;
+  const auto each = [&](const auto &f) {
+    if (held) {
+#pragma unroll
+      for (int x = 0; x < PER; ++x)
+        if (mine + x < end) f(k[x]);
+    } else {
+      for (int c = begin + threadIdx.x; c < end; c += THREADS) f(keys[c]);
+    }
+  };
+  u64 lo = ~0ULL, hi = 0;
+  each([&](u64 key) {
+    lo = min(lo, key);
+    hi = max(hi, key);
+  });
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     lo = min(lo, (u64)__shfl_xor((long long)lo, o, 64));
@@ -188,7 +247,7 @@ __global__ __launch_bounds__(SL_THREADS) void k_pick(sb_select_args a, int t0, c
   }
   __syncthreads();
 #pragma unroll
-  for (int x = 0; x < SL_WAVES; ++x) {
+  for (int x = 0; x < WAVES; ++x) {
     lo = min(lo, ends[x][0]);
     hi = max(hi, ends[x][1]);
   }
@@ -202,19 +261,19 @@ __global__ __launch_bounds__(SL_THREADS) void k_pick(sb_select_args a, int t0, c
       break;
     }
     const int shift = max(64 - __clzll((long long)(hi - lo)) - 11, 0);   // bins of 2^shift keys
-    for (int x = threadIdx.x; x < BINS; x += SL_THREADS) bins[x] = 0;
+    for (int x = threadIdx.x; x < BINS; x += THREADS) bins[x] = 0;
     if (threadIdx.x == 0) listed = 0;
     __syncthreads();
-    for (int c = begin + threadIdx.x; c < end; c += SL_THREADS) {
-      const u64 k = keys[c];
-      if (k >= lo && k <= hi) atomicAdd(&bins[(hi - k) >> shift], 1);   // (bin 0: the largest)
-    }
+    each([&](u64 key) {
+      if (key >= lo && key <= hi) atomicAdd(&bins[(hi - key) >> shift], 1);   // (bin 0: the largest)
+    });
     __syncthreads();
-    // 8 bins a thread: where their sum passes want.
-    int mine = 0;
+    // Some bins a thread: where their sum passes want.
+    constexpr int OWN = BINS / THREADS;
+    int sum = 0;
 #pragma unroll
-    for (int x = 0; x < BINS / SL_THREADS; ++x) mine += bins[threadIdx.x * (BINS / SL_THREADS) + x];
-    int upto = mine;
+    for (int x = 0; x < OWN; ++x) sum += bins[threadIdx.x * OWN + x];
+    int upto = sum;
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
       const int y = __shfl_up(upto, o, 64);
@@ -223,8 +282,8 @@ __global__ __launch_bounds__(SL_THREADS) void k_pick(sb_select_args a, int t0, c
     if (lane == 63) wave_sums[0][w][0] = upto;
     __syncthreads();
     for (int x = 0; x < w; ++x) upto += wave_sums[0][x][0];
-    if (upto - mine < want && want <= upto) {   // (one thread)
-      int before = upto - mine, x = threadIdx.x * (BINS / SL_THREADS);
+    if (upto - sum < want && want <= upto) {   // (one thread)
+      int before = upto - sum, x = threadIdx.x * OWN;
       while (before + bins[x] < want) before += bins[x++];
       bin_at = x;
       bin_before = before;
@@ -236,20 +295,19 @@ __global__ __launch_bounds__(SL_THREADS) void k_pick(sb_select_args a, int t0, c
     hi = top;
     lo = top - lo > width_of ? top - width_of : lo;
     if (count <= LIST) {
-      for (int c = begin + threadIdx.x; c < end; c += SL_THREADS) {
-        const u64 k = keys[c];
-        if (k >= lo && k <= hi) list[atomicAdd(&listed, 1)] = k;
-      }
+      each([&](u64 key) {
+        if (key >= lo && key <= hi) list[atomicAdd(&listed, 1)] = key;
+      });
       __syncthreads();
       if (threadIdx.x < count) {
-        const u64 k = list[threadIdx.x];
+        const u64 key = list[threadIdx.x];
         int above = 0, equal = 0;
         for (int x = 0; x < count; ++x) {
-          above += list[x] > k;
-          equal += list[x] == k;
+          above += list[x] > key;
+          equal += list[x] == key;
         }
         if (above < want && want <= above + equal) {   // (equal keys write the same)
-          cut_key = k;
+          cut_key = key;
           cut_equal = want - above;
         }
       }
@@ -261,11 +319,47 @@ __global__ __launch_bounds__(SL_THREADS) void k_pick(sb_select_args a, int t0, c
   const u64 cut = cut_key;
   const int equal_taken = cut_equal;
   // Pages above the cut, and the first of those on it, in the cache's order.
+  if (held) {
+    int above = 0, equal = 0;
+    each([&](u64 key) {
+      above += key > cut;
+      equal += key == cut;
+    });
+    int na = above, ne = equal;   // up to this thread
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int x = __shfl_up(na, o, 64), y = __shfl_up(ne, o, 64);
+      if (lane >= o) {
+        na += x;
+        ne += y;
+      }
+    }
+    if (lane == 63) {
+      wave_sums[1][w][0] = na;
+      wave_sums[1][w][1] = ne;
+    }
+    __syncthreads();
+    na -= above;
+    ne -= equal;
+    for (int x = 0; x < w; ++x) {
+      na += wave_sums[1][x][0];
+      ne += wave_sums[1][x][1];
+    }
+    if (above + equal == 0) return;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      const bool there = mine + x < end, over = there && k[x] > cut, on = there && k[x] == cut;
+      if (over || (on && ne < equal_taken)) out[a.first + na + min(ne, equal_taken)] = table[mine + x];
+      na += over;
+      ne += on;
+    }
+    return;
+  }
   int above_before = 0, equal_before = 0;
-  for (int c0 = begin, turn = 0; c0 < end; c0 += SL_THREADS, turn ^= 1) {
+  for (int c0 = begin, turn = 0; c0 < end; c0 += THREADS, turn ^= 1) {
     const int c = c0 + threadIdx.x;
-    const u64 k = c < end ? keys[c] : 0;
-    const bool above = c < end && k > cut, equal = c < end && k == cut;
+    const u64 key = c < end ? keys[c] : 0;
+    const bool above = c < end && key > cut, equal = c < end && key == cut;
     const u64 ma = __ballot(above), me = __ballot(equal), below = (1ULL << lane) - 1;
     if (lane == 0) {
       wave_sums[turn][w][0] = __popcll(ma);
@@ -274,7 +368,7 @@ __global__ __launch_bounds__(SL_THREADS) void k_pick(sb_select_args a, int t0, c
     __syncthreads();
     int na = above_before + __popcll(ma & below), ne = equal_before + __popcll(me & below);
 #pragma unroll
-    for (int x = 0; x < SL_WAVES; ++x) {
+    for (int x = 0; x < WAVES; ++x) {
       if (x < w) {
         na += wave_sums[turn][x][0];
         ne += wave_sums[turn][x][1];
@@ -376,7 +470,7 @@ hipError_t select(const sb_select_args &a, int n_cu, void *work, hipStream_t s) 
     const unsigned tokens = (unsigned)std::min(step, a.n_tokens - t0);
     if (a.top > 0) {
       // Pages enough for a workgroup that reading the queries is a small part.
-      constexpr long long LEAST = 32, MOST = 512;
+      constexpr long long LEAST = 64, MOST = 512;
       const long long chunk = std::min(MOST, std::max(LEAST, between * tokens * a.kv_heads / (8 * n_cu) / LEAST * LEAST));
       const unsigned chunks = (unsigned)std::min(65535LL, (between + chunk - 1) / chunk);
       hipLaunchKernelGGL((k_scores<DT, D>), dim3(chunks, a.kv_heads, tokens), dim3(SL_THREADS), 0, s, a, (int)t0, (int)chunk,
@@ -384,7 +478,15 @@ hipError_t select(const sb_select_args &a, int n_cu, void *work, hipStream_t s) 
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(k_pick, dim3(tokens, a.kv_heads), dim3(SL_THREADS), 0, s, a, (int)t0, static_cast<const u64 *>(work));
+    const auto pick = [&](auto kernel, int threads) {
+      hipLaunchKernelGGL(kernel, dim3(tokens, a.kv_heads), dim3(threads), 0, s, a, (int)t0, static_cast<const u64 *>(work));
+    };
+    // (Of 1250 pages, 4 lists: 256 threads 9.9 us, 1024 8.5; of up to 3125, 384 lists: 15.0
+    // and 16.9.)
+    if (between <= 1024) pick(k_pick<256, 4>, 256);
+    else if (between <= 4096 && (long long)tokens * a.kv_heads >= n_cu) pick(k_pick<256, 16>, 256);
+    else if (between <= 4096) pick(k_pick<1024, 4>, 1024);
+    else pick(k_pick<1024, 16>, 1024);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
