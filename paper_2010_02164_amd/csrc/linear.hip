@@ -8,6 +8,8 @@
 // so that they may be split and joined in any order.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "serve.h"
@@ -25,23 +27,25 @@ typedef int i16v __attribute__((ext_vector_type(16)));
 constexpr int QT_THREADS = 256;
 constexpr int QT_PIECE = 16;   // codes a thread makes at a time
 
-// 16 values of a row from column at, 0 behind the last one.
-template <int DT, bool WIDE>
+typedef uint32_t at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t at4 __attribute__((ext_vector_type(4), aligned(4)));
+
+// 16 values of a row from column at, 0 behind the last one. Loads of 16 bytes need
+// no more than their values' alignment.
+template <int DT>
 __device__ __forceinline__ void load_values(const void *row, int at, int cols, float (&v)[QT_PIECE]) {
-  if (WIDE && at + QT_PIECE <= cols) {
-    if constexpr (DT == SB_F32) {
+  typedef typename std::conditional<DT == SB_F32, at4, at2>::type any4;
+  constexpr int SIZE = DT == SB_F32 ? 4 : 2;
+  if (at + QT_PIECE <= cols) {
+    const any4 *src = reinterpret_cast<const any4 *>(static_cast<const char *>(row) + (long long)at * SIZE);
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const u4 p = *reinterpret_cast<const u4 *>(static_cast<const float *>(row) + at + 4 * x);
+    for (int x = 0; x < SIZE; ++x) {
+      const any4 p = src[x];
 #pragma unroll
-        for (int y = 0; y < 4; ++y) v[4 * x + y] = __uint_as_float(p[y]);
-      }
-    } else {
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const u4 p = *reinterpret_cast<const u4 *>(static_cast<const uint16_t *>(row) + at + 8 * x);
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
+      for (int y = 0; y < 4; ++y) {
+        if constexpr (DT == SB_F32) {
+          v[4 * x + y] = __uint_as_float(p[y]);
+        } else {
           v[8 * x + 2 * y] = Half<DT>::to_float(p[y] & 0xFFFFu);
           v[8 * x + 2 * y + 1] = Half<DT>::to_float(p[y] >> 16);
         }
@@ -51,11 +55,11 @@ __device__ __forceinline__ void load_values(const void *row, int at, int cols, f
   }
 #pragma unroll
   for (int x = 0; x < QT_PIECE; ++x) {
-    v[x] = 0.0f;
-    if (at + x < cols) {
-      if constexpr (DT == SB_F32) v[x] = static_cast<const float *>(row)[at + x];
-      else v[x] = Half<DT>::to_float(static_cast<const uint16_t *>(row)[at + x]);
-    }
+    const int i = min(at + x, cols - 1);   // (no branches: all loads at once)
+    float f;
+    if constexpr (DT == SB_F32) f = static_cast<const float *>(row)[i];
+    else f = Half<DT>::to_float(static_cast<const uint16_t *>(row)[i]);
+    v[x] = at + x < cols ? f : 0.0f;
   }
 }
 
@@ -117,7 +121,7 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
 // ROWS rows a workgroup; PIECES pieces a thread stay in registers, those of longer
 // rows are read twice.
 template <int DT, int ROWS, int PIECES>
-__global__ __launch_bounds__(QT_THREADS) void k_quantize(sb_quantize_args a, int wide) {
+__global__ __launch_bounds__(QT_THREADS) void k_quantize(sb_quantize_args a) {
   constexpr int T = QT_THREADS / ROWS;   // threads a row
   __shared__ uint32_t tops[QT_THREADS / 64];
   const int t = threadIdx.x % T;
@@ -127,10 +131,7 @@ __global__ __launch_bounds__(QT_THREADS) void k_quantize(sb_quantize_args a, int
   const char *row = static_cast<const char *>(a.x) + (real ? r : 0) * a.x_row * (DT == SB_F32 ? 4 : 2);
   float v[PIECES][QT_PIECE];
   uint32_t top = 0;   // sizes compare as their codes do, NaN above infinity above all numbers
-  auto load = [&](int piece, float (&to)[QT_PIECE]) {
-    if (wide) load_values<DT, true>(row, piece * QT_PIECE, a.cols, to);
-    else load_values<DT, false>(row, piece * QT_PIECE, a.cols, to);
-  };
+  auto load = [&](int piece, float (&to)[QT_PIECE]) { load_values<DT>(row, piece * QT_PIECE, a.cols, to); };
   auto look = [&](const float (&from)[QT_PIECE]) {
 #pragma unroll
     for (int x = 0; x < QT_PIECE; ++x) top = max(top, __float_as_uint(from[x]) & 0x7FFFFFFFu);
@@ -179,18 +180,16 @@ __global__ __launch_bounds__(QT_THREADS) void k_quantize(sb_quantize_args a, int
 
 template <int DT>
 hipError_t quantize(const sb_quantize_args &a, hipStream_t s) {
-  const int unit = DT == SB_F32 ? 4 : 8;
-  const int wide = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && (a.rows == 1 || a.x_row % unit == 0);
   // Rows enough to fill the card go by waves, which do not wait for each other.
   const int wave = 64 * QT_PIECE;
   if (a.cols <= wave)
-    hipLaunchKernelGGL((k_quantize<DT, 4, 1>), dim3((unsigned)((a.rows + 3LL) / 4)), dim3(QT_THREADS), 0, s, a, wide);
+    hipLaunchKernelGGL((k_quantize<DT, 4, 1>), dim3((unsigned)((a.rows + 3LL) / 4)), dim3(QT_THREADS), 0, s, a);
   else if (a.rows >= 2048 && a.cols <= 4 * wave)
-    hipLaunchKernelGGL((k_quantize<DT, 4, 4>), dim3((unsigned)((a.rows + 3LL) / 4)), dim3(QT_THREADS), 0, s, a, wide);
+    hipLaunchKernelGGL((k_quantize<DT, 4, 4>), dim3((unsigned)((a.rows + 3LL) / 4)), dim3(QT_THREADS), 0, s, a);
   else if (a.cols <= 4 * wave)
-    hipLaunchKernelGGL((k_quantize<DT, 1, 1>), dim3((unsigned)a.rows), dim3(QT_THREADS), 0, s, a, wide);
+    hipLaunchKernelGGL((k_quantize<DT, 1, 1>), dim3((unsigned)a.rows), dim3(QT_THREADS), 0, s, a);
   else
-    hipLaunchKernelGGL((k_quantize<DT, 1, 4>), dim3((unsigned)a.rows), dim3(QT_THREADS), 0, s, a, wide);
+    hipLaunchKernelGGL((k_quantize<DT, 1, 4>), dim3((unsigned)a.rows), dim3(QT_THREADS), 0, s, a);
   return hipGetLastError();
 }
 
@@ -358,19 +357,30 @@ __device__ __forceinline__ void interleave() {
   }
 }
 
-template <int DT, int MT, int NT, int R>
-__global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_linear_args a, int tiles_m, int tiles_n, bool wide) {
+// Which tile is number p: blocks of GROUP tiles of rows by all of channels, so that
+// those that follow each other share operands.
+__device__ __forceinline__ void tile_place(int p, int tiles_m, int tiles_n, int &m, int &n) {
+  constexpr int GROUP = 4;
+  const int g = p / (GROUP * tiles_n), in = p - g * (GROUP * tiles_n), high = min(tiles_m - g * GROUP, GROUP);
+  m = g * GROUP + in % high;
+  n = in / high;
+}
+
+template <int DT, int MT, int NT, bool SPLIT>
+__global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_linear_args a, int tiles_m, int tiles_n, bool wide, int split_into,
+                                                                            void *work) {
   constexpr int BM = 64 * MT, BN = 64 * NT, KS = TILE_K / 32;
   constexpr int XP = BM * 8 / 256, WP = BN * 8 / 256;   // 16-byte pieces of a tile that a thread brings
   __shared__ TileShared<MT, NT> sh;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, h2 = lane >> 5;
-  // Workgroups go to the 8 XCDs in turn: each gets tiles that follow each other, in
-  // blocks of GROUP tiles of rows by all of channels, which share operands in its L2.
-  constexpr int GROUP = 4;
-  const int tiles = tiles_m * tiles_n, xcd = blockIdx.x & 7, per = tiles >> 3, more = tiles & 7;
-  const int p = xcd * per + min(xcd, more) + (int)(blockIdx.x >> 3);
-  const int g = p / (GROUP * tiles_n), in = p - g * (GROUP * tiles_n), high = min(tiles_m - g * GROUP, GROUP);
-  const int m0 = (g * GROUP + in % high) * BM, n0 = in / high * BN;
+  // Workgroups go to the 8 XCDs in turn: each gets tiles that follow each other (or all
+  // splits of few).
+  const int splits = SPLIT ? split_into : 1, all = tiles_m * tiles_n * splits, xcd = blockIdx.x & 7, per = all >> 3, more = all & 7;
+  const int y = xcd * per + min(xcd, more) + (int)(blockIdx.x >> 3), p = y / splits, split = y - p * splits;
+  int m0, n0;
+  tile_place(p, tiles_m, tiles_n, m0, n0);
+  m0 *= BM;
+  n0 *= BN;
   const int row0 = threadIdx.x >> 3, piece = threadIdx.x & 7;
   if (threadIdx.x < BM) sh.x_scale[threadIdx.x] = a.x_scale[min(m0 + (int)threadIdx.x, a.rows - 1)];
   if (threadIdx.x < BN) {
@@ -383,25 +393,27 @@ __global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_l
   for (int i = 0; i < XP; ++i) xs[i] = static_cast<const unsigned char *>(a.x) + min(m0 + row0 + 32 * i, a.rows - 1) * a.x_row + 16 * piece;
 #pragma unroll
   for (int i = 0; i < WP; ++i) ws[i] = static_cast<const unsigned char *>(a.w) + min(n0 + row0 + 32 * i, a.channels - 1) * a.w_row + 16 * piece;
-  u4 xr[R][XP], wr[R][WP];
-  auto load_x = [&](int k, int r) {
-    const int at = min(k, a.depth - 16 - 16 * piece);   // (behind the last value: any that is)
+  u4 xr[XP], wr[WP];
+  const int all_steps = (a.depth + TILE_K - 1) / TILE_K, each = (all_steps + splits - 1) / splits;
+  const int step0 = min(split * each, all_steps), steps = min(each, all_steps - step0), k0 = step0 * TILE_K;   // (steps 0: nothing is left)
+  auto load_x = [&](int k) {
+    const int at = min(k0 + k, a.depth - 16 - 16 * piece);   // (behind the last value: any that is)
 #pragma unroll
-    for (int i = 0; i < XP; ++i) xr[r][i] = *reinterpret_cast<const u4 *>(xs[i] + at);
+    for (int i = 0; i < XP; ++i) xr[i] = *reinterpret_cast<const u4 *>(xs[i] + at);
   };
-  auto load_w = [&](int k, int r) {
-    const int at = min(k, a.depth - 16 - 16 * piece);
+  auto load_w = [&](int k) {
+    const int at = min(k0 + k, a.depth - 16 - 16 * piece);
 #pragma unroll
-    for (int i = 0; i < WP; ++i) wr[r][i] = *reinterpret_cast<const u4 *>(ws[i] + at);
+    for (int i = 0; i < WP; ++i) wr[i] = *reinterpret_cast<const u4 *>(ws[i] + at);
   };
-  auto write_x = [&](int k, int r, int to, auto last) {   // of the last tile, zeros behind the last value
-    const unsigned int keep = !decltype(last)::value || k + 16 * piece < a.depth ? ~0u : 0u;
+  auto write_x = [&](int k, int to, auto last) {   // of the last tile, zeros behind the last value
+    const unsigned int keep = !decltype(last)::value || k0 + k + 16 * piece < a.depth ? ~0u : 0u;
 #pragma unroll
-    for (int i = 0; i < XP; ++i) *reinterpret_cast<u4 *>(&sh.x[to][x_place(row0 + 32 * i, piece)]) = xr[r][i] & keep;
+    for (int i = 0; i < XP; ++i) *reinterpret_cast<u4 *>(&sh.x[to][x_place(row0 + 32 * i, piece)]) = xr[i] & keep;
   };
-  auto write_w = [&](int r, int to) {
+  auto write_w = [&](int to) {
 #pragma unroll
-    for (int i = 0; i < WP; ++i) *reinterpret_cast<u4 *>(&sh.w[to][w_place(row0 + 32 * i, piece)]) = wr[r][i];
+    for (int i = 0; i < WP; ++i) *reinterpret_cast<u4 *>(&sh.w[to][w_place(row0 + 32 * i, piece)]) = wr[i];
   };
   const int xrow = (w >> 1) * 32 * MT + l32, wrow = (w & 1) * 32 * NT + (l32 >> 2) * 8 + (l32 & 3);
   i4 xf[2][MT], wf[2][NT];
@@ -424,26 +436,25 @@ __global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_l
 #pragma unroll
       for (int j = 0; j < NT; ++j) c[i][j] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[from][j], xf[from][i], c[i][j], 0, 0, 0);
   };
-  // A tile's work: operands come from LDS a step of 32 before their products; in
-  // between the next tile goes to LDS (WRITE) from registers r, into which the tile
-  // R after it is loaded (LOAD).
-  auto tile = [&](int t, int r, auto write_next, auto load_next, auto mask) {
+  // A step's work: operands come from LDS 32 values before their products; in between
+  // the next step's go to LDS (WRITE) and those of the one after it are loaded (LOAD).
+  auto tile = [&](int t, auto write_next, auto load_next) {
     constexpr bool WRITE = decltype(write_next)::value, LOAD = decltype(load_next)::value;
     const int cur = t & 1, next = cur ^ 1;
     fetch(cur, 1, 1);
-    if constexpr (WRITE) write_x((t + 1) * TILE_K, r, next, mask);
+    if constexpr (WRITE) write_x((t + 1) * TILE_K, next, std::bool_constant<!LOAD>());
     multiply(0);
     interleave<MT * NT, MT + NT, WRITE ? XP : 0, 0>();
     fetch(cur, 2, 0);
-    if constexpr (LOAD) load_x((t + 1 + R) * TILE_K, r);
-    if constexpr (WRITE) write_w(r, next);
+    if constexpr (LOAD) load_x((t + 2) * TILE_K);
+    if constexpr (WRITE) write_w(next);
     multiply(1);
     interleave<MT * NT, MT + NT, WRITE ? WP : 0, LOAD ? XP : 0>();
     fetch(cur, 3, 1);
-    if constexpr (LOAD) load_w((t + 1 + R) * TILE_K, r);
+    if constexpr (LOAD) load_w((t + 2) * TILE_K);
     multiply(0);
     interleave<MT * NT, MT + NT, 0, LOAD ? WP : 0>();
-    if constexpr (WRITE) {   // all of this tile is in registers, the next one in LDS
+    if constexpr (WRITE) {   // all of this step's is in registers, the next one's in LDS
       __syncthreads();
       fetch(next, 0, 0);
     }
@@ -452,35 +463,27 @@ __global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_l
   };
   const std::true_type yes;
   const std::false_type no;
-  const int steps = (a.depth + TILE_K - 1) / TILE_K;
-  load_x(0, 0);
-  load_w(0, 0);
-  write_x(0, 0, 0, yes);
-  write_w(0, 0);
-#pragma unroll
-  for (int r = 0; r < R; ++r) {
-    __builtin_amdgcn_sched_barrier(0);   // (in this order: waits are for all loads up to one)
-    load_x((r + 1) * TILE_K, r);
-    __builtin_amdgcn_sched_barrier(0);
-    load_w((r + 1) * TILE_K, r);
-  }
+  load_x(0);
+  load_w(0);
+  write_x(0, 0, yes);
+  write_w(0);
+  load_x(TILE_K);
+  load_w(TILE_K);
   __syncthreads();
   fetch(0, 0, 0);
   int t = 0;
-  if constexpr (R == 1) {
-    for (; t + 2 < steps; ++t) tile(t, 0, yes, yes, no);
-    if (t + 1 < steps) tile(t++, 0, yes, no, yes);
-    tile(t, 0, no, no, no);
-  } else {   // (tiles behind the last one are loaded from its end, and zeros)
-    // (One way out of the loop, at its end: no way then leads from one tile to any
-    // but the next, and the compiler knows what has to be waited for.)
-    for (; t + R <= steps; t += R) {
+  for (; t + 2 < steps; ++t) tile(t, yes, yes);
+  if (t + 1 < steps) tile(t++, yes, no);
+  tile(t, no, no);
+  if constexpr (SPLIT) {   // sums as the threads hold them; k_linear_join adds them up
+    i4 *dst = static_cast<i4 *>(work) + ((long long)p * splits + split) * (MT * NT * 4) * 256 + threadIdx.x;
 #pragma unroll
-      for (int r = 0; r < R; ++r) tile(t + r, r, yes, yes, yes);
-    }
+    for (int i = 0; i < MT; ++i)
 #pragma unroll
-    for (int r = 0; r + 1 < R; ++r)
-      if (t + r < steps) tile(t + r, r, yes, yes, yes);
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) dst[((i * NT + j) * 4 + (e >> 2)) * 256] = i4{c[i][j][e], c[i][j][e + 1], c[i][j][e + 2], c[i][j][e + 3]};
+    return;
   }
   // Lane: row m, of products j and j + 1 channels 8 (2 (e / 4) + h2) + 4 (j % 2) + e % 4.
 #pragma unroll
@@ -512,15 +515,74 @@ __global__ __launch_bounds__(256, MT * NT <= 4 ? 2 : 1) void k_linear_tiles(sb_l
   }
 }
 
+// The sums of a tile's splits, scaled: a workgroup 8 of each thread's.
+template <int DT, int MT, int NT>
+__global__ __launch_bounds__(256) void k_linear_join(sb_linear_args a, int tiles_m, int tiles_n, bool wide, int splits, const void *work) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, l32 = lane & 31, h2 = lane >> 5, p = blockIdx.x;
+  const int e = (int)blockIdx.y & 3, i = (int)(blockIdx.y >> 2) % MT, j = (int)(blockIdx.y >> 2) / MT * 2;
+  int m0, n0;
+  tile_place(p, tiles_m, tiles_n, m0, n0);
+  const int m = m0 * 64 * MT + (w >> 1) * 32 * MT + 32 * i + l32, n = n0 * 64 * NT + (w & 1) * 32 * NT + 64 * (j >> 1) + 8 * (2 * e + h2);
+  const float sx = a.x_scale[min(m, a.rows - 1)];
+  float sw[8], bias[8];
+#pragma unroll
+  for (int y = 0; y < 8; ++y) {
+    const int at = min(n + y, a.channels - 1);
+    sw[y] = a.w_scale[at];
+    bias[y] = a.bias ? a.bias[at] : 0.0f;
+  }
+  i4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+  const i4 *src = static_cast<const i4 *>(work) + (long long)p * splits * (MT * NT * 4) * 256 + ((i * NT + j) * 4 + e) * 256 + threadIdx.x;
+#pragma unroll 8
+  for (int x = 0; x < splits; ++x, src += MT * NT * 4 * 256) {
+    lo += src[0];
+    hi += src[4 * 256];
+  }
+  if (m >= a.rows) return;
+  float v[8];
+#pragma unroll
+  for (int y = 0; y < 8; ++y) v[y] = scaled<DT>(y < 4 ? lo[y & 3] : hi[y & 3], sx, sw[y], bias[y]);
+  store_side_by_side<DT, 8>(a, m, n, v, wide);
+}
+
+// How a product is cut up: by few rows, or by tiles, whose depth is split where they
+// leave units without work. Times in microseconds, as measured: what a step of 128
+// of the depth takes (a tile of 256 x 256: 2; of 128 x 128: 0.75, two in a unit 1.3),
+// a launch and its ends 4, a join 4 and its bytes at 4 TB/s; few rows: 4 pieces of a
+// wave 3.3 (up to 32 rows) or 5.2.
+struct Plan {
+  int tile;   // 0: few rows
+  int m, n, splits;
+};
+Plan plan(const sb_linear_args &a, int n_cu) {
+  if (a.rows <= 16) return {0, 0, 0, 1};
+  const auto up = [](long long x, long long y) { return (int)((x + y - 1) / y); };
+  const int steps = up(a.depth, TILE_K), m = up(a.rows, 128), n = up(a.channels, 128);
+  const double tiles = (double)m * n;
+  Plan best = {128, m, n, 1};
+  double least = 1e30;
+  for (int s = 1; s <= 16 && (s == 1 || steps >= 4 * s); ++s) {
+    const double groups = tiles * s, step = groups <= n_cu ? 0.75 : 1.3 * std::ceil(groups / (2 * n_cu));
+    const double time = 4 + up(steps, s) * step + (s > 1 ? 4 + groups * 128 * 128 * 8 / 4e6 : 0);
+    if (time < least) {
+      least = time;
+      best.splits = up(steps, up(steps, s));   // (none without a step)
+    }
+  }
+  const int m2 = up(a.rows, 256), n2 = up(a.channels, 256);
+  if (4 + steps * 2.0 * std::ceil((double)m2 * n2 / n_cu) < least) best = {256, m2, n2, 1};
+  if (a.rows <= 64) {
+    const double batches = up(up(a.depth, FEW_STEP), 4 * FEW_WAVES), rounds = std::ceil((double)up(a.channels, 32) / n_cu);
+    if (3.5 + rounds * batches * (a.rows <= 32 ? 3.3 : 5.2) < least) best = {0, 0, 0, 1};
+  }
+  return best;
+}
+
 template <int DT>
 hipError_t linear(const sb_linear_args &a, int n_cu, void *work, hipStream_t s) {
   const bool wide = (a.out_row * (DT == SB_F32 ? 4 : 2)) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
-  const auto tiles = [&](auto kernel, int bm, int bn) {
-    const int tm = (a.rows + bm - 1) / bm, tn = (a.channels + bn - 1) / bn;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(tm * tn)), dim3(256), 0, s, a, tm, tn, wide);
-    return hipGetLastError();
-  };
-  if (a.rows <= 64) {
+  const Plan p = plan(a, n_cu);
+  if (p.tile == 0) {
     const auto few = [&](auto kernel, int channels) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)((a.channels + channels - 1) / channels)), dim3(64 * FEW_WAVES), 0, s, a, wide);
       return hipGetLastError();
@@ -529,9 +591,17 @@ hipError_t linear(const sb_linear_args &a, int n_cu, void *work, hipStream_t s) 
     if (a.rows <= 32) return few(k_linear_few<DT, 2, 2>, 32);
     return few(k_linear_few<DT, 4, 2>, 32);
   }
-  const long long large = ((a.rows + 255LL) / 256) * ((a.channels + 255LL) / 256);
-  if (large >= n_cu) return tiles(k_linear_tiles<DT, 4, 4, 1>, 256, 256);
-  return tiles(k_linear_tiles<DT, 2, 2, 1>, 128, 128);
+  const dim3 grid((unsigned)((long long)p.m * p.n * p.splits));
+  const auto tiles = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, p.m, p.n, wide, p.splits, work);
+    return hipGetLastError();
+  };
+  if (p.tile == 256) return tiles(k_linear_tiles<DT, 4, 4, false>);
+  if (p.splits == 1) return tiles(k_linear_tiles<DT, 2, 2, false>);
+  const hipError_t e = tiles(k_linear_tiles<DT, 2, 2, true>);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_linear_join<DT, 2, 2>), dim3((unsigned)(p.m * p.n), 8), dim3(256), 0, s, a, p.m, p.n, wide, p.splits, work);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -540,7 +610,11 @@ hipError_t launch_quantize(const sb_quantize_args &a, hipStream_t s) {
   return a.dtype == SB_F32 ? quantize<SB_F32>(a, s) : a.dtype == SB_BF16 ? quantize<SB_BF16>(a, s) : quantize<SB_F16>(a, s);
 }
 
-int64_t linear_workspace(const sb_linear_args &a, int n_cu) { return 0; }
+int64_t linear_workspace(const sb_linear_args &a, int n_cu) {
+  if (a.rows == 0) return 0;
+  const Plan p = plan(a, n_cu);
+  return p.splits == 1 ? 0 : (int64_t)p.m * p.n * p.splits * 128 * 128 * 4;
+}
 
 hipError_t launch_linear(const sb_linear_args &a, int n_cu, void *work, hipStream_t s) {
   return a.dtype == SB_F32 ? linear<SB_F32>(a, n_cu, work, s)

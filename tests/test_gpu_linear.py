@@ -111,7 +111,10 @@ def test_quantize_strides_and_out(gpu):
 
 SHAPES = [(1, 1, 16), (1, 5, 48), (1, 4096, 4096), (2, 64, 100), (7, 33, 1000), (16, 129, 64), (17, 640, 4096), (31, 100, 272), (33, 65, 500),
           (64, 300, 2064), (65, 257, 128), (100, 96, 5000), (130, 130, 130), (200, 1000, 1000), (257, 513, 1040), (600, 255, 320), (1000, 31, 4000),
-          (300, 2200, 96), (1025, 1025, 112)]
+          (300, 2200, 96), (1025, 1025, 112),
+          # tiles whose depth is split (several rows and channels behind the last), many rounds of steps
+          (90, 130, 2048), (31, 200, 8000), (64, 999, 8192), (129, 257, 6160), (931, 313, 6263), (20, 100, 40000), (300, 260, 1030),
+          (2000, 4500, 640), (4100, 4200, 272)]
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
@@ -150,7 +153,7 @@ def test_linear_scales_of_all_sizes(gpu, M):
     assert bool((y[0, 9] == math.inf)) and int((~torch.isfinite(y[0])).sum()) == 2
 
 
-@pytest.mark.parametrize("M,N,K", [(5, 70, 160), (50, 131, 1024), (140, 150, 336)])
+@pytest.mark.parametrize("M,N,K", [(5, 70, 160), (50, 131, 1024), (140, 150, 336), (100, 150, 4112)])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_linear_strides(gpu, M, N, K, dtype):
     """Rows within wider ones, which hold other codes behind their ends, into a
@@ -165,6 +168,27 @@ def test_linear_strides(gpu, M, N, K, dtype):
         got = sb.int8_linear(wx[:, 16:16 + K], xs, ww[:, 32:], ws, bias=bias, out=out[:, at:at + N])
         assert torch.equal(got, want)
         assert bool((out[:, :at] == 5).all()) and bool((out[:, at + N:] == 5).all())
+
+
+def test_linear_workspace(gpu):
+    """Asked for where the depth is split, refused where it is too small; what stands
+    in it before the call does not matter."""
+    N = sb.decoder.N
+    x, xs, w, ws, _ = operands(100, 150, 4112, 5)
+    out = torch.empty(100, 150, device="cuda")
+    args = N.LINEAR_ARGS.pack(N.LINEAR_ARGS.size, x.data_ptr(), w.data_ptr(), xs.data_ptr(), ws.data_ptr(), 0, out.data_ptr(), 4112, 4112, 150,
+                              100, 150, 4112, N.SB_F32)
+    L = N.lib()
+    need = L.sb_linear_workspace(args)
+    assert need > 0
+    work = torch.full((need + 256,), 0x7F, dtype=torch.uint8, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    assert L.sb_quantized_linear(args, None, 0, stream) == N.SB_E_WORKSPACE
+    assert L.sb_quantized_linear(args, work.data_ptr(), need - 1, stream) == N.SB_E_WORKSPACE
+    assert L.sb_quantized_linear(args, work.data_ptr() + 64, need, stream) == N.SB_E_WORKSPACE
+    assert L.sb_quantized_linear(args, work.data_ptr(), need, stream) == N.SB_OK
+    check_linear(x, xs, w, ws, None, out)
+    assert bool((work[need:] == 0x7F).all())
 
 
 def test_linear_refusals(gpu):
