@@ -116,8 +116,7 @@ __device__ __forceinline__ u64 order_of(double score) {
 // blockIdx.y, those of `chunk` pages a workgroup, to keys [tokens][kv_heads][max_pages].
 // Bound by reading the bounds: 48 requests of 5000 to 50000 tokens, pages of 16, 8
 // heads of 128: 84 us, 4.0 TB/s (heads side by side in the grid: 89; 2 or 8 loads of
-// each bound in flight: 90, 87; a load at a time: 96); where they come from L2, a
-// prompt's, 11 TB/s.
+// each bound in flight: 90, 87; a load at a time: 96).
 template <int DT, int D>
 __global__ __launch_bounds__(SL_THREADS) void k_scores(sb_select_args a, int t0, int chunk, u64 *keys) {
   constexpr int L = D / 8, P = 64 / L;   // lanes of a page, pages a wave takes at once
@@ -178,6 +177,112 @@ __global__ __launch_bounds__(SL_THREADS) void k_scores(sb_select_args a, int t0,
           const int c = c0 + s0 + x * P + lane / L;
           if (col == 0 && c < wave_stop) out[c] = order_of(there[x] ? s : -INFINITY);
         }
+      }
+    }
+  }
+}
+
+// The same for prompts, 16 tokens a workgroup, by the matrix unit in fp64: its rows are
+// the tokens' sums, in LDS as its lanes take them, its columns 16 pages a wave. Lane l
+// has values l / 16 D / 4 .. of a bound (which value stands for which k of a product
+// does not matter, as long as both operands have the same). Tokens of several requests
+// take a turn each. 900 tokens over 24000 to 30000, pages of 32, 4 heads of 128: 66 us,
+// by k_scores 157, most of it conversions and sums (four tokens a workgroup there: 156).
+constexpr int SP_TOKENS = 16;
+typedef double d4 __attribute__((ext_vector_type(4)));
+template <int DT, int D>
+__global__ __launch_bounds__(SL_THREADS) void k_scores_many(sb_select_args a, int t0, int t_end, int chunk, u64 *keys) {
+  constexpr int Q = D / 4, PIECES = Q / 8;   // values and 16-byte pieces of a lane
+  __shared__ double sums[2 * Q][64];          // [product][lane]: the first Q with the larger bounds, the others with the smaller
+  __shared__ u64 found[SP_TOKENS];
+  const int z = blockIdx.z * SP_TOKENS, t = t0 + z, hk = blockIdx.y, G = a.q_heads / a.kv_heads;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, g4 = lane >> 4;
+  if (threadIdx.x < SP_TOKENS) found[threadIdx.x] = 0;
+  for (int x = threadIdx.x; x < SP_TOKENS * (D / 8); x += SL_THREADS) {
+    const int token = x & (SP_TOKENS - 1), d = x / SP_TOKENS * 8;
+    const uint16_t *src = static_cast<const uint16_t *>(a.q) + min(t + token, t_end - 1) * a.q_token + hk * G * a.q_head + d;
+    double up[8], down[8];
+#pragma unroll
+    for (int y = 0; y < 8; ++y) up[y] = down[y] = 0.0;
+    for (int g = 0; g < G; ++g) {
+      const u4 v = *reinterpret_cast<const u4 *>(src + g * a.q_head);
+#pragma unroll
+      for (int y = 0; y < 8; ++y) {
+        const float f = Half<DT>::to_float(y & 1 ? v[y >> 1] >> 16 : v[y >> 1] & 0xFFFFu);
+        if (f != f) up[y] = f;
+        up[y] += f > 0.0f ? f : 0.0f;
+        down[y] += f < 0.0f ? f : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int y = 0; y < 8; ++y) {
+      sums[(d + y) % Q][(d + y) / Q * 16 + token] = up[y];
+      sums[Q + (d + y) % Q][(d + y) / Q * 16 + token] = down[y];
+    }
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < a.n_requests; b += SL_THREADS) {
+    const int from = max(a.q_start[b], t), to = min(a.q_start[b + 1], min(t + SP_TOKENS, t_end));
+    const long long len = min((long long)max(a.lens[b], 0), (long long)a.max_pages * a.page_size);
+    for (int x = from; x < to; ++x) {
+      const long long p = max(len - a.q_start[b + 1] + x, -1LL);
+      atomicMax(&found[x - t], (u64)b << 32 | (u64)(p + 2));
+    }
+  }
+  __syncthreads();
+  // The lane's four tokens (rows g4 + 4 i of a product's result) and the ends of their pages.
+  const auto request_of = [&](int token, int &end) {
+    const u64 at = found[token];
+    const int p = (int)(uint32_t)at - 2, n = at == 0 || p < 0 ? 0 : p / a.page_size + 1;
+    end = n - a.last;
+    return n > (long long)a.first + a.top + a.last ? (int)(at >> 32) : -1;
+  };
+  const long long row = (long long)a.kv_heads * D, next = (long long)a.kv_heads * a.max_pages;
+  const uint16_t *bounds = static_cast<const uint16_t *>(a.bounds) + (long long)hk * D + g4 * Q;
+  u64 *out = keys + ((long long)z * a.kv_heads + hk) * a.max_pages;
+  int before = -1;
+  for (int turn = 0; turn < SP_TOKENS; ++turn) {   // a request a turn (those that follow each other are one)
+    int end;
+    const int b = request_of(turn, end);
+    if (b < 0 || b == before) continue;
+    before = b;
+    end = 0;
+    int ends[4];
+    for (int x = 0; x < SP_TOKENS; ++x) {
+      int e;
+      if (request_of(x, e) == b) end = max(end, e);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      int e;
+      ends[i] = request_of(g4 + 4 * i, e) == b ? e : 0;
+    }
+    const int *table = a.table + b * a.table_stride;
+    for (int at = blockIdx.x * chunk + a.first; at < end; at += gridDim.x * chunk) {
+      const int stop = min(at + chunk, end);
+      for (int c0 = at + (int)(threadIdx.x >> 6) * 16; c0 < stop; c0 += SL_WAVES * 16) {
+        const int c = c0 + l16, page = c < stop ? table[c] : -1;
+        const bool there = (unsigned)page < (unsigned)a.n_pages;
+        const uint16_t *src = bounds + (there ? 2LL * page * row : 0);
+        u4 hi[PIECES], lo[PIECES];
+#pragma unroll
+        for (int x = 0; x < PIECES; ++x) {
+          hi[x] = *reinterpret_cast<const u4 *>(src + row + 8 * x);
+          lo[x] = *reinterpret_cast<const u4 *>(src + 8 * x);
+        }
+        d4 s[2] = {d4{0, 0, 0, 0}, d4{0, 0, 0, 0}};
+#pragma unroll
+        for (int x = 0; x < PIECES; ++x)
+#pragma unroll
+          for (int y = 0; y < 8; ++y) {
+            const double h = Half<DT>::to_float(y & 1 ? hi[x][y >> 1] >> 16 : hi[x][y >> 1] & 0xFFFFu);
+            const double l = Half<DT>::to_float(y & 1 ? lo[x][y >> 1] >> 16 : lo[x][y >> 1] & 0xFFFFu);
+            s[0] = __builtin_amdgcn_mfma_f64_16x16x4f64(sums[8 * x + y][lane], h, s[0], 0, 0, 0);
+            s[1] = __builtin_amdgcn_mfma_f64_16x16x4f64(sums[Q + 8 * x + y][lane], l, s[1], 0, 0, 0);
+          }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (c < min(stop, ends[i])) out[(g4 + 4 * i) * next + c] = order_of(there ? s[0][i] + s[1][i] : -INFINITY);
       }
     }
   }
@@ -466,15 +571,22 @@ template <int DT, int D>
 hipError_t select(const sb_select_args &a, int n_cu, void *work, hipStream_t s) {
   const long long step = tokens_at_once(a);
   const long long between = std::max(1LL, (std::max(a.max_kv, 1) + a.page_size - 1LL) / a.page_size - a.first - a.last);
+  const bool many = a.n_tokens >= 8LL * a.n_requests;   // several tokens of a request in 16
   for (long long t0 = 0; t0 < a.n_tokens; t0 += step) {
     const unsigned tokens = (unsigned)std::min(step, a.n_tokens - t0);
     if (a.top > 0) {
       // Pages enough for a workgroup that reading the queries is a small part.
       constexpr long long LEAST = 64, MOST = 512;
-      const long long chunk = std::min(MOST, std::max(LEAST, between * tokens * a.kv_heads / (8 * n_cu) / LEAST * LEAST));
+      const long long rows = (many ? (tokens + SP_TOKENS - 1) / SP_TOKENS : tokens) * (long long)a.kv_heads;
+      const long long chunk = std::min(MOST, std::max(LEAST, between * rows / ((many ? 3 : 8) * n_cu) / LEAST * LEAST));
       const unsigned chunks = (unsigned)std::min(65535LL, (between + chunk - 1) / chunk);
-      hipLaunchKernelGGL((k_scores<DT, D>), dim3(chunks, a.kv_heads, tokens), dim3(SL_THREADS), 0, s, a, (int)t0, (int)chunk,
-                         static_cast<u64 *>(work));
+      if (many) {
+        hipLaunchKernelGGL((k_scores_many<DT, D>), dim3(chunks, a.kv_heads, (tokens + SP_TOKENS - 1) / SP_TOKENS), dim3(SL_THREADS), 0, s, a,
+                           (int)t0, (int)(t0 + tokens), (int)chunk, static_cast<u64 *>(work));
+      } else {
+        hipLaunchKernelGGL((k_scores<DT, D>), dim3(chunks, a.kv_heads, tokens), dim3(SL_THREADS), 0, s, a, (int)t0, (int)chunk,
+                           static_cast<u64 *>(work));
+      }
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }

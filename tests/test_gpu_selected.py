@@ -133,8 +133,21 @@ def test_bounds_grow_with_the_cache(gpu):
 
 FORMS = [   # B, Hq, Hkv, page, queries, cached
     (1, 4, 1, 16, [1], [1]), (3, 8, 2, 16, [1], [900, 33, 300]), (2, 5, 5, 7, [3, 1], [150, 70]), (2, 16, 1, 1, [2], [600, 97]),
-    (2, 6, 2, 24, [1, 4], [1300, 500]), (5, 2, 2, 8, [1, 0, 2, 9, 1], [400, 90, 64, 65, 0]), (1, 40, 4, 4, [3], [3000]),
+    (2, 6, 2, 24, [1, 4], [1300, 500]), (3, 4, 2, 8, [20, 3, 33], [500, 40, 333]), (1, 3, 1, 4, [17], [300]), (5, 2, 2, 8, [1, 0, 2, 9, 1], [400, 90, 64, 65, 0]), (1, 40, 4, 4, [3], [3000]),
 ]
+
+
+def test_select_is_the_same_by_either_unit(gpu):
+    """A prompt's tokens at once (scored by the matrix unit) and one by one."""
+    c = case(2, 8, 2, 128, 16, [70, 45], [3000, 2000], BF16, 15)
+    bounds = all_bounds(c)
+    pages, kept = select(c, bounds, 20, 1, 2)
+    for t in range(0, 115, 7):
+        b = 0 if t < 70 else 1
+        p = (3000 - 70 + t) if b == 0 else (2000 - 45 + t - 70)
+        one = sb.select_pages(c["q"][t:t + 1], bounds, c["table"][b:b + 1], i32([p + 1]), i32([0, 1]), page_size=16, top=20, first=1, last=2,
+                              max_kv=3000)
+        assert torch.equal(one[0][0], pages[t]) and int(one[1]) == int(kept[t])
 
 
 @pytest.mark.parametrize("dtype,D", [(BF16, 128), (F16, 64), (BF16, 256), (F16, 256)])
@@ -169,10 +182,11 @@ def test_select_equal_scores(gpu):
         check_select(c, bounds, top, 0, 1, select(c, bounds, top, 0, 1))
 
 
-def test_select_odd_values(gpu):
+@pytest.mark.parametrize("q", [[1, 2], [30, 21]])
+def test_select_odd_values(gpu, q):
     """Bounds and queries that are not finite, pages outside the cache, zeros of
-    both signs."""
-    c = case(2, 4, 2, 64, 4, [1, 2], [400, 200], F16, 2)
+    both signs; single tokens, and so many that the matrix unit scores them."""
+    c = case(2, 4, 2, 64, 4, q, [400, 200], F16, 2)
     bounds = all_bounds(c)
     row = c["table"][0].tolist()
     bounds[row[20], 1, 0, 3], bounds[row[30], 0, 0], bounds[row[40], 1] = math.nan, -math.inf, math.inf
