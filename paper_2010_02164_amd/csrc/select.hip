@@ -21,7 +21,8 @@ typedef unsigned long long u64;
 
 constexpr int BD_THREADS = 256;
 
-// A wave takes 128 values of a page (a lane 8 of them, of every fourth key).
+// A wave takes 128 values of a page (a lane 8 of them, of every fourth key). Bound by
+// its chain of waits (lengths, table, keys): 4 us for one request, 7 for 48.
 template <int DT>
 __global__ __launch_bounds__(BD_THREADS) void k_bounds(sb_bounds_args a) {
   const int b = blockIdx.x, lane = threadIdx.x & 63, turn = lane >> 4;
@@ -487,11 +488,15 @@ __global__ __launch_bounds__(THREADS) void k_pick(sb_select_args a, int t0, cons
 
 // -- attention over the selected pages -----------------------------------------------
 
+// A token's heads of a group are up to 16 rows of one pass over its selected keys
+// (attn_pass.h), which all of them see. Bound by reading the keys: 48 tokens, 8 heads of
+// 128, 2048 keys each: 86 us, 4.7 TB/s; a prompt's, where pages come from the caches,
+// by the waits for them: 900 tokens, 4 heads, 2080 keys: 304 us, 12.6 TB/s (two
+// workgroups a compute unit, not three: 340, and the 48 tokens 86 to 89).
 // In the workspace: the parts' sums [splits][n_tokens][q_heads][D] and their
 // (reference, sum).
 template <int DT, int D>
-__global__ __launch_bounds__(AT_THREADS, D == 64 ? 3 : D == 128 ? 2 : 1) void k_selected(sb_attention_args a, const int *kept, int splits,
-                                                                                        void *work) {
+__global__ __launch_bounds__(AT_THREADS, D <= 128 ? 3 : 1) void k_selected(sb_attention_args a, const int *kept, int splits, void *work) {
   __shared__ FewShared<D> sh;
   const int G = a.q_heads / a.kv_heads, hk = (int)(blockIdx.x % a.kv_heads), j = (int)(blockIdx.x / a.kv_heads);
   const int t = j / splits, split = j % splits, n = kept[t];
@@ -538,7 +543,7 @@ __global__ __launch_bounds__(AT_THREADS) void k_selected_join(sb_attention_args 
 // least.
 constexpr int SPLIT_KEYS = 128;
 int splits_of(const sb_selected_args &x, int n_cu) {
-  const long long room = (x.head_dim == 64 ? 3 : x.head_dim == 128 ? 2 : 1) * (long long)n_cu;
+  const long long room = (x.head_dim <= 128 ? 3 : 1) * (long long)n_cu;
   return (int)std::max(1LL, std::min(room / ((long long)x.n_tokens * x.kv_heads), (long long)x.width * x.page_size / SPLIT_KEYS));
 }
 

@@ -1,10 +1,14 @@
 """Operators of a serving step: paged caches, rotary positions, attention with
-a sliding window and sinks, sampled tokens.
+a sliding window and sinks, over a shared prefix or over selected pages, products
+in 8-bit integers, sampled tokens.
 
 A step of a cached decoder takes them in this order: plan_pages finds pages
-and slots for the step's new tokens, rope_append turns their queries and keys
-and writes keys and values to the slots (per layer), paged_attention reads
-the cache (per layer), sample_tokens draws the next token of every request.
+and slots for the step's new tokens; per layer, quantize_rows and int8_linear make
+the projections, rope_append turns queries and keys and writes keys and
+values to the slots, and an attention reads the cache: paged_attention all of
+it, shared_attention once for all requests that share a prefix, or page_bounds,
+select_pages and selected_attention the pages that matter to a query;
+sample_tokens draws the next token of every request.
 Each is one call of the C ABI (include/streambeam.h, which defines what it
 computes) on torch's current stream of its tensors' device; nothing waits,
 and every call can be captured into a graph. There are no backward passes.
