@@ -89,7 +89,7 @@ __device__ __forceinline__ int nearest(float y, float s, float inv) {
 __device__ __forceinline__ u4 codes_of(const float (&v)[QT_PIECE], float up, float s, float inv) {
   constexpr float SHIFT = 12582912.0f;
   u4 out;
-  float far = 0.0f;
+  float far = up > 1.0f ? 1.0f : 0.0f;   // (small scales may be rounded to few bits: quotients pass 127)
 #pragma unroll
   for (int x = 0; x < QT_PIECE; x += 4) {
     uint32_t bits[4];

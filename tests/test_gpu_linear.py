@@ -80,6 +80,19 @@ def test_quantize_borders(gpu, dtype):
     check_quantize(least.cuda(), sb.quantize_rows(least.cuda()))
 
 
+@pytest.mark.parametrize("cols", [40, 1500, 5000])
+def test_quantize_rows_of_coarse_scales(gpu, cols):
+    """fp32 rows whose largest value is a few of the smallest steps: the scale is
+    rounded to whole steps, so that quotients lie up to half above 127 and are cut
+    off there."""
+    tops = torch.cat([torch.arange(60, 260), torch.arange(300, 13000, 97)])
+    x = torch.zeros(len(tops), cols, dtype=torch.float64)
+    for i, part in enumerate((1.0, -1.0, 0.5, -0.97, 0.9, 0.01)):
+        x[:, i * (cols // 7)] = (tops * part).trunc() * 2.0 ** -149
+    x = x.float().cuda()
+    check_quantize(x, sb.quantize_rows(x))
+
+
 @pytest.mark.parametrize("dtype", [BF16, F16, F32])
 @pytest.mark.parametrize("cols", [50, 3000, 9000])
 def test_quantize_rows_that_are_not_finite(gpu, cols, dtype):
