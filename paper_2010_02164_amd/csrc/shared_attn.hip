@@ -107,8 +107,9 @@ union SharedLds {
 
 // What a workgroup looks its piece up with.
 struct Scan {
-  long long tiles[AT_WAVES];
-  int units[AT_WAVES], pieces[AT_WAVES], item, before;
+  unsigned long long tiles[AT_WAVES];
+  unsigned units[AT_WAVES], pieces[AT_WAVES], at;
+  int item;
 };
 
 template <int DT, int D>
@@ -143,10 +144,10 @@ __device__ __forceinline__ void part_many(const sb_attention_args &a, const Span
     for (int e = 0; e < 16; e += 4) *reinterpret_cast<f4 *>(sums + 32 * x + 2 * e + 4 * h2) = f4{o[x][e], o[x][e + 1], o[x][e + 2], o[x][e + 3]};
 }
 
-__device__ __forceinline__ int scan_up(int v) {   // of the lanes up to this one
+__device__ __forceinline__ unsigned scan_up(unsigned v) {   // of the lanes up to this one
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(v, o, 64);
+    const unsigned y = __shfl_up(v, o, 64);
     if ((int)(threadIdx.x & 63) >= o) v += y;
   }
   return v;
@@ -190,11 +191,14 @@ __device__ __forceinline__ void run_prefix(const sb_attention_args &a, const Pre
     t = (tiles_of<KIND>(s) + ROUND - 1) & -ROUND;
   };
   const int per_thread = (p.n_groups + AT_THREADS - 1) / AT_THREADS, g0 = threadIdx.x * per_thread, g1 = min(g0 + per_thread, p.n_groups);
-  long long tiles = 0;
-  int units = 0, n = 0, t = 0;   // (of the last group looked at: the only one, nearly always)
+  // (Groups that lie over each other have any number of units, and counts may pass
+  // 2^32: a unit that its group does not have is left out at the end.)
+  unsigned long long tiles = 0;
+  unsigned units = 0;
+  int n = 0, t = 0;   // (of the last group looked at: the only one, nearly always)
   for (int g = g0; g < g1; ++g) {
     units_of(g, n, t);
-    tiles += (long long)t * n;
+    tiles += (unsigned long long)t * n;
     units += n;
   }
 #pragma unroll
@@ -218,38 +222,40 @@ __device__ __forceinline__ void run_prefix(const sb_attention_args &a, const Pre
   // Tiles of a piece: every unit may leave one that is not full, so that there are at
   // most `room` and the units pieces. (fp32's rounding makes less than the one
   // workgroup more that there is.)
-  const int room = max(pass.fill - units, (pass.fill + 1) / 2);
+  const int half = (pass.fill + 1) / 2, room = units < (unsigned)pass.fill ? max(pass.fill - (int)units, half) : half;
   const float want = (float)tiles / (float)room;
   const int per = ((want < 1e9f ? max((int)ceilf(want), LEAST) : 1 << 30) + ROUND - 1) & -ROUND;
   const auto pieces_of = [&](int t) { return (t + per - 1) / per; };
-  int mine = 0;
+  unsigned mine = 0;
   for (int g = g0; g < g1; ++g) {
     if (per_thread > 1) units_of(g, n, t);
-    mine += pieces_of(t) * n;
+    mine += (unsigned)pieces_of(t) * n;
   }
-  int upto = scan_up(mine);
+  unsigned upto = scan_up(mine);
   if (lane == 63) scan.pieces[w] = upto;
   __syncthreads();
 #pragma unroll
   for (int x = 0; x < AT_WAVES; ++x)
     if (x < w) upto += scan.pieces[x];
-  if (upto - mine <= j && j < upto) {   // (one thread at most)
-    int before = upto - mine;
+  unsigned rest = j - (upto - mine);
+  if (rest < mine) {   // (one thread)
     for (int g = g0; g < g1; ++g) {
       if (per_thread > 1) units_of(g, n, t);
-      if (j < before + pieces_of(t) * n) {
+      const unsigned here = (unsigned)pieces_of(t) * n;
+      if (rest < here) {
         scan.item = g;
-        scan.before = before;
+        scan.at = rest;
         break;
       }
-      before += pieces_of(t) * n;
+      rest -= here;
     }
   }
   __syncthreads();
   const int g = scan.item;
   if (g < 0) return;
   units_of(g, n, t);
-  const int pieces = pieces_of(t), at = j - scan.before, unit = at / pieces, x = at - unit * pieces;
+  const int pieces = pieces_of(t), unit = (int)(scan.at / (unsigned)pieces), x = (int)(scan.at - (unsigned)(unit * pieces));
+  if (unit >= n) return;
   s.r0 = unit * ROWS;
   if (x == 0 && hk == 0 && threadIdx.x == 0) out.infos[(int)((long long)s.q0 * G / ROWS) + g + unit] = Info{j, pieces};
   run_piece<DT, D, KIND>(a, s, pass, out.sums[0], out.stats[0], hk, p.table + g * p.stride, x * per, min(x * per + per, t), j, sh);

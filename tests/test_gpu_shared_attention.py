@@ -203,6 +203,26 @@ def test_shared_attention_wrong_state_stays_in_bounds(gpu, max_q):
     assert torch.equal(sb.shared_attention(**dict(c, group_start=i32([0, 2, 9])), **kw)[:rows], want[:rows])
 
 
+def test_shared_attention_groups_over_each_other(gpu):
+    """Starts that go back: every other group has all requests, 2^25 units where there
+    is room for 2^14. Nothing is written outside the result, and the next call is
+    right."""
+    c = case([2, 2], 6, 2, 64, 8, [30, 9], [2, 0, 3, 1], [9, 5, 20, 7], BF16, 16)
+    want = sb.shared_attention(**c, **bounds(c))
+    n, groups = 8192, 8192
+    q = torch.randn(n, 16, 64, device="cuda").bfloat16()
+    cache = torch.randn(4, 16, 1, 64, device="cuda").bfloat16()
+    table, prefix_table = torch.zeros(n, 1, dtype=torch.int32, device="cuda"), torch.zeros(groups, 4096, dtype=torch.int32, device="cuda")
+    starts = torch.zeros(groups + 1, dtype=torch.int32, device="cuda")
+    starts[1::2] = n
+    lens, q_start = torch.ones(n, dtype=torch.int32, device="cuda"), torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    long = torch.full((groups,), 65536, dtype=torch.int32, device="cuda")
+    held = torch.full((n + 64, 16, 64), 3.0, dtype=BF16, device="cuda")
+    sb.shared_attention(q, cache, cache, prefix_table, long, starts, table, lens, q_start, max_q=1, max_kv=1, max_prefix=16, out=held[32:-32])
+    assert bool((held[:32] == 3).all()) and bool((held[-32:] == 3).all())
+    assert torch.equal(sb.shared_attention(**c, **bounds(c)), want)
+
+
 @pytest.mark.parametrize("max_q", [1, 1000])
 def test_shared_attention_strides(gpu, max_q):
     c = case([2, 1], 6, 2, 64, 8, [40, 21], [4, 1, 2], [20, 33, 2], F16, 11)
