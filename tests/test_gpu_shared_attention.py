@@ -136,8 +136,8 @@ def test_shared_attention_is_paged_attention_without_a_prefix(gpu, max_q):
     both = np.full((5, 20), -1)
     for b in range(5):
         g = 0 if b < 3 else 1
-        both[b, :ahead[b]] = c["prefix_table"][g, :ahead[b]].cpu()
-        both[b, ahead[b]:ahead[b] + c["table"].shape[1]] = c["table"][b].cpu()
+        both[b, :ahead[b]] = c["prefix_table"][g, :ahead[b]].cpu().numpy()
+        both[b, ahead[b]:ahead[b] + c["table"].shape[1]] = c["table"][b].cpu().numpy()
     want = sb.paged_attention(**dict(own, lens=c["lens"] + i32(ahead) * 16), table=i32(both), max_q=max_q, max_kv=300)
     got = sb.shared_attention(**c, **bounds(c, max_q=max_q))
     assert torch.allclose(got.float(), want.float(), rtol=2 * 2.0 ** -8, atol=2.0 ** -8)
