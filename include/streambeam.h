@@ -516,12 +516,11 @@ sb_status sb_quantized_linear(const sb_linear_args *args, void *workspace, size_
  * group g; requests of no group have no prefix (group_start is clipped to
  * 0 .. n_requests). A query that sees no key gets 0. Each prefix is read once for
  * all queries of its group, 32 or 128 rows (queries times q_heads / kv_heads) at a
- * time. fp32 scores, statistics and sums. Weights go into the product with the
- * values in two parts of the cache's type, as in sb_paged_attention; they are
- * rounded to it once, for the prefixes, where the groups have more than 32 rows on
- * average, and everywhere, where max_q queries have more than 64. max_prefix (an
- * upper bound of prefix_lens) chooses kernels and splits as max_q and max_kv do.
- * own.window and own.sinks are 0. */
+ * time. fp32 scores, statistics and sums. All weights go into the product with the
+ * values in two parts of the cache's type (off by the square of its rounding),
+ * whatever the groups' sizes and the bounds. max_prefix (an upper bound of
+ * prefix_lens) chooses kernels and splits as max_q and max_kv do. own.window and
+ * own.sinks are 0. */
 typedef struct {
   int64_t struct_bytes;          /* sizeof(sb_shared_args)                               */
   sb_attention_args own;         /* the step's queries and the requests' own tokens      */

@@ -414,8 +414,9 @@ __device__ __forceinline__ float many_reference(const sb_attention_args &a, floa
 
 // The workgroup's pass over `tiles` tiles from t_first on: the lane's row's sums,
 // what its exponentials are taken against, and its keys' share of the weights'
-// sum. False where it stopped.
-template <int DT, int D, bool CAREFUL>
+// sum. False where it stopped. TWO: each weight goes into the second product in two
+// parts, the rounded one and what that leaves.
+template <int DT, int D, bool CAREFUL, bool TWO>
 __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span &s, const int *table, const uint16_t *kc, const uint16_t *vc,
                                           const u4 (&q)[D / 16], int p, bool real, int t_first, int tiles, ManyShared<D> &sh,
                                           f16v (&o)[D / 32], float &ref, float &sum) {
@@ -570,17 +571,19 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
 #pragma unroll
       for (int x = 0; x < DB; ++x) o[x] *= shrink;
     }
-    // (One part a weight: a second product with what its rounding leaves made the
-    // three prompts' 391 us into 483.)
+    // (One part a weight in paged_attention's prompts: a second product with what its
+    // rounding leaves made the three prompts' 391 us into 483.)
     const float base = ref == -INFINITY ? 0.0f : fmaf(ref, c, -raise<DT>(GROW));
     float ts[2] = {0.0f, 0.0f};
-    u4 pk[4];
+    u4 pk[4], pl[TWO ? 4 : 1];
 #pragma unroll
     for (int x = 0; x < 32; x += 2) {
       const float f = __builtin_amdgcn_exp2f(fmaf(e[x], c, -base)), g = __builtin_amdgcn_exp2f(fmaf(e[x + 1], c, -base));
       ts[0] += f;
       ts[1] += g;
-      pk[x >> 3][(x & 7) >> 1] = Half<DT>::pack(f, g);
+      const uint32_t both = Half<DT>::pack(f, g);
+      pk[x >> 3][(x & 7) >> 1] = both;
+      if constexpr (TWO) pl[x >> 3][(x & 7) >> 1] = Half<DT>::pack(f - Half<DT>::to_float(both & 0xFFFFu), g - Half<DT>::to_float(both >> 16));
     }
     sum += ts[0] + ts[1];
     if (CAREFUL && !shared) {
@@ -612,6 +615,7 @@ __device__ __forceinline__ bool many_keys(const sb_attention_args &a, const Span
 #pragma unroll
     for (int x = 0; x < 4 * DB; ++x) {
       o[x % DB] = mfma32<DT>(vf[x % AHEAD], pk[x / DB], o[x % DB]);
+      if constexpr (TWO) o[x % DB] = mfma32<DT>(vf[x % AHEAD], pl[x / DB], o[x % DB]);
       if (x + AHEAD < 4 * DB) vf[x % AHEAD] = v_frag(x + AHEAD);
     }
     if (odd) {   // for the tile that comes into this buffer

@@ -268,8 +268,8 @@ __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : 2) void k_attn_many(sb_a
   float ref, sum;
   const int tiles = (s.n_vis + MANY_KEYS - 1) / MANY_KEYS, each = (tiles + splits - 1) / splits;
   const int t0 = min(part % splits * each, tiles), count = min(each, tiles - t0);
-  if (!many_keys<DT, D, false>(a, s, table, kc, vc, q, p, real, t0, count, sh, o, ref, sum))
-    many_keys<DT, D, true>(a, s, table, kc, vc, q, p, real, t0, count, sh, o, ref, sum);
+  if (!many_keys<DT, D, false, false>(a, s, table, kc, vc, q, p, real, t0, count, sh, o, ref, sum))
+    many_keys<DT, D, true, false>(a, s, table, kc, vc, q, p, real, t0, count, sh, o, ref, sum);
   sum += __shfl_xor(sum, 32, 64);
   if (!real) return;
   if (splits > 1) {

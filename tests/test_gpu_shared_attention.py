@@ -305,3 +305,31 @@ def test_shared_attention_captured_and_on_other_streams(gpu):
             got += [step() for _ in range(3)]
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for run in got for a, b in zip(run, want))
+
+
+@pytest.mark.parametrize("dtype,D", [(BF16, 64), (BF16, 128), (BF16, 256), (F16, 64), (F16, 128), (F16, 256)])
+@pytest.mark.parametrize("members,q,prefix,own", [
+    ([1], [1], [700], [300, 2]), ([2], [1], [700], [30]), ([3], [1], [6000], [2, 70]), ([1, 9], [1], [130, 700], [40]), ([2], [3], [700], [40, 90]),
+    ([1], [9], [700], [300])])
+def test_shared_attention_weights_in_two_parts(gpu, members, q, prefix, own, dtype, D):
+    """By every kind of pass (rows by waves and by workgroups, of the prefix and of
+    the own tokens): a weight is off by (eps / 2)^2 of itself, whatever the
+    group's size and the bounds that the kernels are chosen by. Every other key is a
+    little less likely and its value the negative one, so that weights rounded once
+    would show."""
+    c = case(members, 16, 1, D, 16, prefix, q, own, dtype, len(members) + D)
+    c["q"].zero_()
+    c["q"][:, :, 0] = torch.linspace(0.005, 0.4, 16, device="cuda")
+    odd = torch.arange(16, device="cuda") % 2   # (pages of 16: a place's parity is its position's)
+    c["v_cache"][:] = (2.0 * odd - 1)[:, None, None]
+    c["k_cache"].zero_()
+    c["k_cache"][..., 0] = -odd[:, None].to(dtype)
+    eps = torch.finfo(dtype).eps
+    args = [f64(c[n]) for n in ("q", "k_cache", "v_cache")]
+    args += [c[n].tolist() for n in ("prefix_table", "prefix_lens", "group_start", "table", "lens", "q_start")]
+    want, size, big = oracle.shared_attention(*args, 1.0)
+    score = big * (D * 2.0 ** -24 + 2.0 ** -22)
+    tol = eps / 2 * np.abs(want) + ((eps / 2) ** 2 + 2 * score[..., :1] + 2.0 ** -20) * size
+    for over in HINTS:
+        d = np.abs(f64(sb.shared_attention(**c, **bounds(c, **over), scale=1.0)) - want)
+        assert np.all(d <= tol), (over, np.max(d / tol))
