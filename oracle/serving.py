@@ -146,8 +146,11 @@ def select_pages(q, bounds, table, lens, q_start, page_size, top, first, last):
                     score = {}
                     for c in range(first, seen - last):
                         at = table[b][c]
+                        if not 0 <= at < n_pages:
+                            score[c] = (-1, 0.0)
+                            continue
                         with np.errstate(invalid="ignore"):
-                            s = float(np.sum(bounds[at, 1, h] * up + bounds[at, 0, h] * down)) if 0 <= at < n_pages else -math.inf
+                            s = float(np.sum(bounds[at, 1, h] * up + bounds[at, 0, h] * down))
                         score[c] = (1, 0.0) if math.isnan(s) else (0, s)
                     best = sorted(score, key=lambda c: (score[c][0], score[c][1]), reverse=True)   # (stable: of equal ones the first)
                     cols = sorted(cols[:first] + best[:top] + cols[seen - last:])

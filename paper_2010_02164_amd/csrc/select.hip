@@ -107,7 +107,9 @@ __device__ __forceinline__ double add_stage(double v) {
   return __longlong_as_double((long long)x) + __longlong_as_double((long long)y);
 }
 
-// A score as a number whose order is the scores': NaN last.
+// A score as a number whose order is the scores': NaN last, and all of them above
+// NOT_THERE, which pages outside the cache have.
+constexpr u64 NOT_THERE = 0;
 __device__ __forceinline__ u64 order_of(double score) {
   const u64 bits = (u64)__double_as_longlong(score + 0.0);   // (of -0 and 0 one)
   return score != score ? ~0ULL : bits ^ (bits >> 63 ? ~0ULL : 1ULL << 63);
@@ -176,7 +178,7 @@ __global__ __launch_bounds__(SL_THREADS) void k_scores(sb_select_args a, int t0,
           if constexpr (L >= 16) s = add_stage<3>(s);
           if constexpr (L >= 32) s = add_stage<4>(s);
           const int c = c0 + s0 + x * P + lane / L;
-          if (col == 0 && c < wave_stop) out[c] = order_of(there[x] ? s : -INFINITY);
+          if (col == 0 && c < wave_stop) out[c] = there[x] ? order_of(s) : NOT_THERE;
         }
       }
     }
@@ -283,7 +285,7 @@ __global__ __launch_bounds__(SL_THREADS) void k_scores_many(sb_select_args a, in
           }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (c < min(stop, ends[i])) out[(g4 + 4 * i) * next + c] = order_of(there ? s[0][i] + s[1][i] : -INFINITY);
+          if (c < min(stop, ends[i])) out[(g4 + 4 * i) * next + c] = there ? order_of(s[0][i] + s[1][i]) : NOT_THERE;
       }
     }
   }

@@ -203,6 +203,24 @@ def test_select_odd_values(gpu, q):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("q", [[1, 2], [30, 21]])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_select_pages_outside_the_cache_come_last(gpu, dtype, q):
+    """Behind pages that score minus infinity, too, which stand after them in the table."""
+    c = case(2, 4, 2, 64, 4, q, [400, 200], dtype, 5)
+    c["q"][:, :, 7] = c["q"][:, :, 7].abs() + 1.0
+    bounds = all_bounds(c)
+    row = c["table"][0].tolist()
+    c["table"][0, 10], c["table"][0, 25], c["table"][0, 40] = -1, 10 ** 6, -2 ** 31
+    for col in (20, 30, 55, 90):
+        bounds[row[col], 1, :, 7] = -math.inf
+    for top in (89, 90, 91, 92, 94, 95, 96):   # of 97 between for request 0's last token, 3 of them not there
+        got = select(c, bounds, top, 1, 2)
+        check_select(c, bounds, top, 1, 2, got)
+        last = got[0][int(c["q_start"][1]) - 1]
+        assert int(((last < 0) | (last >= 10 ** 6)).sum()) == 2 * max(0, top - 94)
+
+
 def test_select_some_tokens_at_a_time(gpu):
     """A table so wide that the scores of all tokens do not fit the workspace."""
     c = case(3, 2, 2, 64, 4, [100, 1, 60], [500, 90, 300], BF16, 6, pad=2)

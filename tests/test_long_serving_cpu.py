@@ -240,6 +240,15 @@ def test_oracle_selection_by_hand():
     assert np.allclose(out[:, 0], [[0, 1], [0, 0]])   # keys (1, 0), (3, -1) and (-4, 4)
 
 
+def test_oracle_selection_takes_missing_pages_last():
+    # Pages of 1, one head of one value; between page 0 and the last: one that is not
+    # there, one of minus infinity, one of -5.
+    bounds = np.array([[0.0, 0.0], [-9.0, -math.inf], [-5.0, -5.0]]).reshape(3, 2, 1, 1)
+    for top, want in ((1, [0, 2, 0]), (2, [0, 1, 2, 0]), (3, [0, 7, 1, 2, 0])):
+        pages, kept = oracle.select_pages(np.ones((1, 1, 1)), bounds, [[0, 7, 1, 2, 0]], [5], [0, 1], 1, top, 1, 1)
+        assert pages[0, 0].tolist() == want and kept.tolist() == [len(want)]
+
+
 def test_oracle_linear_by_hand():
     out, size = oracle.linear([[1, 2], [3, -4]], [0.5, 2.0], [[5, 6], [-7, 8], [0, 1]], [1.0, 10.0, 0.25], [0, 1, 2])
     assert out.tolist() == [[8.5, 46.0, 2.25], [-18.0, -1059.0, 0.0]] and size.tolist() == [[8.5, 45.0, 0.25], [18.0, 1060.0, 2.0]]
