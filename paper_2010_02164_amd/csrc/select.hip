@@ -107,6 +107,10 @@ __device__ __forceinline__ double add_stage(double v) {
   return __longlong_as_double((long long)x) + __longlong_as_double((long long)y);
 }
 
+// The place a grid's step behind `at`, or `end`: with rows of nearly 2^31 pages the sum
+// would pass an int.
+__device__ __forceinline__ int step_on(int at, int step, int end) { return end - at > step ? at + step : end; }
+
 // A score as a number whose order is the scores': NaN last, and all of them above
 // NOT_THERE, which pages outside the cache have.
 constexpr u64 NOT_THERE = 0;
@@ -147,7 +151,7 @@ __global__ __launch_bounds__(SL_THREADS) void k_scores(sb_select_args a, int t0,
   const uint16_t *bounds = static_cast<const uint16_t *>(a.bounds) + (long long)hk * D + 8 * col;
   u64 *out = keys + ((long long)blockIdx.z * a.kv_heads + hk) * a.max_pages;
   const int end = q.n - a.last;
-  for (int at = blockIdx.x * chunk + a.first; at < end; at += gridDim.x * chunk) {
+  for (int at = blockIdx.x * chunk + a.first; at < end; at = step_on(at, gridDim.x * chunk, end)) {
     const int stop = min(at + chunk, end);
     // A wave's pages are looked up together, then taken a few at a time, with their
     // loads in flight together.
@@ -261,7 +265,7 @@ __global__ __launch_bounds__(SL_THREADS) void k_scores_many(sb_select_args a, in
       ends[i] = request_of(g4 + 4 * i, e) == b ? e : 0;
     }
     const int *table = a.table + b * a.table_stride;
-    for (int at = blockIdx.x * chunk + a.first; at < end; at += gridDim.x * chunk) {
+    for (int at = blockIdx.x * chunk + a.first; at < end; at = step_on(at, gridDim.x * chunk, end)) {
       const int stop = min(at + chunk, end);
       for (int c0 = at + (int)(threadIdx.x >> 6) * 16; c0 < stop; c0 += SL_WAVES * 16) {
         const int c = c0 + l16, page = c < stop ? table[c] : -1;
@@ -320,7 +324,7 @@ __global__ __launch_bounds__(THREADS) void k_pick(sb_select_args a, int t0, cons
   }
   const int *table = a.table + q.b * a.table_stride;
   const u64 *keys = all_keys + ((long long)blockIdx.x * a.kv_heads + hk) * a.max_pages;
-  const int begin = a.first, end = q.n - a.last, mine = begin + threadIdx.x * PER;
+  const int begin = a.first, end = q.n - a.last, mine = begin + min((int)threadIdx.x * PER, end - begin);
   const bool held = end - begin <= THREADS * PER;   // all keys in registers
   u64 k[PER];
   if (held && a.top > 0) {

@@ -231,6 +231,27 @@ def test_select_some_tokens_at_a_time(gpu):
     check_select(c, bounds, 9, 1, 2, got)
 
 
+def test_select_longest_row(gpu):
+    """A row of as many pages as there may be, 2^31 - 1024 of one key: a grid's step
+    behind the last ones passes 2^31. All pages score the same but three, the last of
+    them next to the row's end. And with all but 1100 of them the first ones: so do
+    the places of threads behind the last."""
+    n = 2 ** 31 - 1024
+    q = torch.ones(1, 1, 64, dtype=BF16, device="cuda")
+    bounds = torch.zeros(2, 2, 1, 64, dtype=BF16, device="cuda")
+    bounds[1, 1] = 1.0
+    table = torch.zeros(1, n, dtype=torch.int32, device="cuda")
+    table[0, 40], table[0, 2 ** 30], table[0, n - 2] = 1, 1, 1
+    torch.cuda.synchronize()
+    pages, kept = sb.select_pages(q, bounds, table, i32([n]), i32([0, 1]), page_size=1, top=5, first=1, last=1, max_kv=n)
+    assert pages.tolist() == [[[0, 0, 0, 1, 1, 1, 0]]] and int(kept) == 7
+    first = n - 1101
+    table[0, n - 500:n - 480], table[0, 7] = 1, 1
+    pages, kept = sb.select_pages(q, bounds, table, i32([n]), i32([0, 1]), page_size=1, top=22, first=first, last=1, max_kv=n)
+    assert torch.equal(pages[0, 0, :first], table[0, :first]) and int(kept) == first + 23
+    assert pages[0, 0, first:].tolist() == [0] + [1] * 21 + [0]
+
+
 def test_select_out_and_strides(gpu):
     c = case(2, 4, 2, 64, 8, [2, 1], [300, 200], BF16, 8, pad=2)
     bounds = all_bounds(c)
