@@ -14,11 +14,10 @@
 // sums of tiles whose depth was split.
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
-#include <cmath>
 #include <type_traits>
 
 #include "serve.h"
+#include "serve_plan.h"
 #include "wave.h"
 
 namespace sb {
@@ -249,8 +248,6 @@ __device__ __forceinline__ void store_side_by_side(const sb_linear_args &a, int 
 // unit wants them (lane: channel l % 16, values 16 (l / 16) .. + 15); the waves'
 // sums meet in LDS.
 
-constexpr int FEW_WAVES = 8, FEW_STEP = 64;
-
 template <int DT, int MT, int NT>
 __global__ __launch_bounds__(64 * FEW_WAVES) void k_linear_few(sb_linear_args a, bool wide) {
   constexpr int BATCH = MT == 1 ? 8 : 4;   // pieces in flight
@@ -331,8 +328,6 @@ __global__ __launch_bounds__(64 * FEW_WAVES) void k_linear_few(sb_linear_args a,
 // follow each other, use all banks. The matrix unit's rows are channels: a lane
 // then has 4 channels of one row of x side by side, and 8 with the next product's,
 // since the channels are dealt out to products in turns of 4.
-
-constexpr int TILE_K = 128;   // bytes of a row in LDS
 
 template <int MT, int NT>
 struct TileShared {
@@ -551,43 +546,10 @@ __global__ __launch_bounds__(256) void k_linear_join(sb_linear_args a, int tiles
   store_side_by_side<DT, 8>(a, m, n, v, wide);
 }
 
-// How a product is cut up: by few rows, or by tiles, whose depth is split where they
-// leave units without work. Times in microseconds, as measured: what a step of 128
-// of the depth takes (a tile of 256 x 256: 2; of 128 x 128: 0.75, two in a unit 1.3),
-// a launch and its ends 4, a join 4 and its bytes at 4 TB/s; few rows: 4 pieces of a
-// wave 3.3 (up to 32 rows) or 5.2.
-struct Plan {
-  int tile;   // 0: few rows
-  int m, n, splits;
-};
-Plan plan(const sb_linear_args &a, int n_cu) {
-  if (a.rows <= 16) return {0, 0, 0, 1};
-  const auto up = [](long long x, long long y) { return (int)((x + y - 1) / y); };
-  const int steps = up(a.depth, TILE_K), m = up(a.rows, 128), n = up(a.channels, 128);
-  const double tiles = (double)m * n;
-  Plan best = {128, m, n, 1};
-  double least = 1e30;
-  for (int s = 1; s <= 16 && (s == 1 || steps >= 4 * s); ++s) {
-    const double groups = tiles * s, step = groups <= n_cu ? 0.75 : 1.3 * std::ceil(groups / (2 * n_cu));
-    const double time = 4 + up(steps, s) * step + (s > 1 ? 4 + groups * 128 * 128 * 8 / 4e6 : 0);
-    if (time < least) {
-      least = time;
-      best.splits = up(steps, up(steps, s));   // (none without a step)
-    }
-  }
-  const int m2 = up(a.rows, 256), n2 = up(a.channels, 256);
-  if (4 + steps * 2.0 * std::ceil((double)m2 * n2 / n_cu) < least) best = {256, m2, n2, 1};
-  if (a.rows <= 64) {
-    const double batches = up(up(a.depth, FEW_STEP), 4 * FEW_WAVES), rounds = std::ceil((double)up(a.channels, 32) / n_cu);
-    if (3.5 + rounds * batches * (a.rows <= 32 ? 3.3 : 5.2) < least) best = {0, 0, 0, 1};
-  }
-  return best;
-}
-
 template <int DT>
 hipError_t linear(const sb_linear_args &a, int n_cu, void *work, hipStream_t s) {
   const bool wide = (a.out_row * (DT == SB_F32 ? 4 : 2)) % 16 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0;
-  const Plan p = plan(a, n_cu);
+  const LinearPlan p = linear_plan(a, n_cu);
   if (p.tile == 0) {
     const auto few = [&](auto kernel, int channels) {
       hipLaunchKernelGGL(kernel, dim3((unsigned)((a.channels + channels - 1) / channels)), dim3(64 * FEW_WAVES), 0, s, a, wide);
@@ -618,7 +580,7 @@ hipError_t launch_quantize(const sb_quantize_args &a, hipStream_t s) {
 
 int64_t linear_workspace(const sb_linear_args &a, int n_cu) {
   if (a.rows == 0) return 0;
-  const Plan p = plan(a, n_cu);
+  const LinearPlan p = linear_plan(a, n_cu);
   return p.splits == 1 ? 0 : (int64_t)p.m * p.n * p.splits * 128 * 128 * 4;
 }
 

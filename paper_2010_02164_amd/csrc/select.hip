@@ -10,6 +10,7 @@
 #include <algorithm>
 
 #include "attn_pass.h"
+#include "serve_plan.h"
 #include "wave.h"
 
 namespace sb {
@@ -582,8 +583,8 @@ long long tokens_at_once(const sb_select_args &a) {
 template <int DT, int D>
 hipError_t select(const sb_select_args &a, int n_cu, void *work, hipStream_t s) {
   const long long step = tokens_at_once(a);
-  const long long between = std::max(1LL, (std::max(a.max_kv, 1) + a.page_size - 1LL) / a.page_size - a.first - a.last);
-  const bool many = a.n_tokens >= 8LL * a.n_requests;   // several tokens of a request in 16
+  const long long between = pages_between(a);
+  const bool many = many_scores(a);
   for (long long t0 = 0; t0 < a.n_tokens; t0 += step) {
     const unsigned tokens = (unsigned)std::min(step, a.n_tokens - t0);
     if (a.top > 0) {
@@ -605,12 +606,14 @@ hipError_t select(const sb_select_args &a, int n_cu, void *work, hipStream_t s) 
     const auto pick = [&](auto kernel, int threads) {
       hipLaunchKernelGGL(kernel, dim3(tokens, a.kv_heads), dim3(threads), 0, s, a, (int)t0, static_cast<const u64 *>(work));
     };
-    // (Of 1250 pages, 4 lists: 256 threads 9.9 us, 1024 8.5; of up to 3125, 384 lists: 15.0
-    // and 16.9.)
-    if (between <= 1024) pick(k_pick<256, 4>, 256);
-    else if (between <= 4096 && (long long)tokens * a.kv_heads >= n_cu) pick(k_pick<256, 16>, 256);
-    else if (between <= 4096) pick(k_pick<1024, 4>, 1024);
-    else pick(k_pick<1024, 16>, 1024);
+    const PickPlan p = pick_plan(between, (long long)tokens * a.kv_heads, n_cu);
+    if (p.threads == 256) {
+      if (p.per == 4) pick(k_pick<256, 4>, 256);
+      else pick(k_pick<256, 16>, 256);
+    } else {
+      if (p.per == 4) pick(k_pick<1024, 4>, 1024);
+      else pick(k_pick<1024, 16>, 1024);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -11,6 +11,7 @@
 #include <algorithm>
 
 #include "attn_pass.h"
+#include "serve_plan.h"
 
 namespace sb {
 namespace {
@@ -86,9 +87,6 @@ __device__ __forceinline__ void span_group(const sb_attention_args &a, const Pre
   s.p_first = s.p_last = s.n - 1;
 }
 
-// Kinds of a pass: 1 and 2, 16 and 32 rows by waves that take 32 keys each; MANY,
-// 128 rows by workgroups that take 64.
-constexpr int MANY = 8;
 __host__ __device__ constexpr int rows_of(int kind) { return kind == MANY ? MANY_ROWS : FEW_ROWS * kind; }
 
 template <int D, int KIND>
@@ -346,21 +344,9 @@ __global__ __launch_bounds__(AT_THREADS) void k_shared_join(sb_attention_args a,
   }
 }
 
-// The kinds of the passes go by the rows that read the same keys: 16 or 32 by waves,
-// more by workgroups.
-struct Kinds {
-  int prefix, own;
-};
-Kinds kinds(const sb_shared_args &x) {
-  const sb_attention_args &a = x.own;
-  const long long G = a.q_heads / a.kv_heads, group_rows = (a.n_tokens * G + x.n_groups - 1) / x.n_groups, request_rows = std::max(a.max_q, 1) * G;
-  const int own = request_rows <= FEW_ROWS ? 1 : request_rows <= 4 * FEW_ROWS ? 2 : MANY;
-  const int prefix = group_rows <= FEW_ROWS ? 1 : group_rows <= 2 * FEW_ROWS ? 2 : MANY;
-  return {own == MANY ? MANY : std::max(prefix, own), own};
-}
 Cut cut(const sb_shared_args &x, int n_cu) {
   const sb_attention_args &a = x.own;
-  const Kinds k = kinds(x);
+  const SharedKinds k = shared_kinds(x);
   const long long G = a.q_heads / a.kv_heads, all = a.n_tokens * G, room = (a.head_dim == 256 ? 1 : 2) * (long long)n_cu;
   Cut c = {};
   {   // workgroups: as many as the units hold at once, fewer where the bounds let expect no more tiles
@@ -393,7 +379,7 @@ template <int DT, int D>
 hipError_t launch(const sb_shared_args &x, int n_cu, void *work, hipStream_t s) {
   const sb_attention_args &a = x.own;
   const Cut c = cut(x, n_cu);
-  const Kinds k = kinds(x);
+  const SharedKinds k = shared_kinds(x);
   const Prefix p = {x.prefix_table, x.prefix_lens, x.group_start, x.prefix_stride, x.n_groups, x.prefix_pages};
   const long long own = (k.own == MANY ? c.own.places : a.n_requests) * (long long)c.own.splits;
   const dim3 grid((unsigned)((c.prefix.groups() + own) * a.kv_heads));
