@@ -85,7 +85,7 @@ struct Query {
 };
 __device__ __forceinline__ bool query_of(const sb_select_args &a, int t, u64 *found, Query &q) {
   for (int b = threadIdx.x; b < a.n_requests; b += blockDim.x) {
-    const int from = a.q_start[b], to = a.q_start[b + 1], len = a.lens[b];
+    const int from = a.q_start[b], to = min(a.q_start[b + 1], a.n_tokens), len = a.lens[b];
     if (from <= t && t < to) {
       const long long p = max(min((long long)max(len, 0), (long long)a.max_pages * a.page_size) - to + t, -1LL);
       atomicMax(found, (u64)b << 32 | (u64)(p + 2));
@@ -230,10 +230,10 @@ __global__ __launch_bounds__(SL_THREADS) void k_scores_many(sb_select_args a, in
   }
   __syncthreads();
   for (int b = threadIdx.x; b < a.n_requests; b += SL_THREADS) {
-    const int from = max(a.q_start[b], t), to = min(a.q_start[b + 1], min(t + SP_TOKENS, t_end));
+    const int next = min(a.q_start[b + 1], a.n_tokens), from = max(a.q_start[b], t), to = min(next, min(t + SP_TOKENS, t_end));
     const long long len = min((long long)max(a.lens[b], 0), (long long)a.max_pages * a.page_size);
     for (int x = from; x < to; ++x) {
-      const long long p = max(len - a.q_start[b + 1] + x, -1LL);
+      const long long p = max(len - next + x, -1LL);
       atomicMax(&found[x - t], (u64)b << 32 | (u64)(p + 2));
     }
   }

@@ -221,6 +221,19 @@ def test_select_pages_outside_the_cache_come_last(gpu, dtype, q):
         assert int(((last < 0) | (last >= 10 ** 6)).sum()) == 2 * max(0, top - 94)
 
 
+@pytest.mark.parametrize("q", [[2, 5], [9, 31]])
+def test_select_starts_behind_the_tokens(gpu, q):
+    """A last start behind n_tokens counts as n_tokens, as in paged_attention: the
+    request's queries are its last positions."""
+    c = case(2, 4, 2, 64, 4, q, [400, 301], BF16, 23)
+    bounds = all_bounds(c)
+    want = select(c, bounds, 9, 1, 2)
+    check_select(c, bounds, 9, 1, 2, want)
+    for behind in (1, 6, 400, 2 ** 31 - 1 - sum(q)):
+        got = select(dict(c, q_start=i32([0, q[0], sum(q) + behind])), bounds, 9, 1, 2)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), behind
+
+
 def test_select_some_tokens_at_a_time(gpu):
     """A table so wide that the scores of all tokens do not fit the workspace."""
     c = case(3, 2, 2, 64, 4, [100, 1, 60], [500, 90, 300], BF16, 6, pad=2)
