@@ -514,13 +514,14 @@ sb_status sb_quantized_linear(const sb_linear_args *args, void *workspace, size_
  * window: own.lens, own.table, own.q_start count and place the tokens behind the
  * prefix alone. Requests group_start[g] .. group_start[g + 1] - 1 are those of
  * group g; requests of no group have no prefix (group_start is clipped to
- * 0 .. n_requests). A query that sees no key gets 0. Each prefix is read once for
- * all queries of its group, 32 or 128 rows (queries times q_heads / kv_heads) at a
- * time. fp32 scores, statistics and sums. All weights go into the product with the
+ * 0 .. n_requests). A query that sees no key gets 0. A prefix is read once for
+ * every 16, 32 or 128 rows (queries times q_heads / kv_heads) of its group. fp32
+ * scores, statistics and sums. All weights go into the product with the
  * values in two parts of the cache's type (off by the square of its rounding),
  * whatever the groups' sizes and the bounds. max_prefix (an upper bound of
  * prefix_lens) chooses kernels and splits as max_q and max_kv do. own.window and
- * own.sinks are 0. */
+ * own.sinks are 0. n_tokens q_heads / 8 + (n_groups + n_requests) kv_heads may be up
+ * to 2^23. */
 typedef struct {
   int64_t struct_bytes;          /* sizeof(sb_shared_args)                               */
   sb_attention_args own;         /* the step's queries and the requests' own tokens      */
@@ -567,7 +568,7 @@ sb_status sb_page_bounds(const sb_bounds_args *args, void *stream);
 /* The pages that each query attends to, for every key/value head: of the pages
  * 0 .. p / page_size of its request, p its position as in sb_paged_attention, the
  * first `first`, the last `last` and, of those between, the `top` of the largest
- *   sum_i  max(bounds[1][i] Q+_i) + bounds[0][i] Q-_i,
+ *   sum_i  bounds[1][i] Q+_i + bounds[0][i] Q-_i,
  *   Q+_i, Q-_i = the sums of max(q_i, 0) and min(q_i, 0) over the head's group,
  * the largest sum of the group's scores that keys within the bounds can have.
  * Sums are fp64; of equal ones the lower page is taken, NaN counts as the largest,
@@ -608,7 +609,8 @@ sb_status sb_select_pages(const sb_select_args *args, void *workspace, size_t by
  * out[t] as in sb_paged_attention, over the first kept[t] keys of the pages
  * pages[t][h][0], pages[t][h][1], .. in turn (at most width pages); pages outside
  * the cache are skipped. A token with kept 0, or whose keys all lie in pages
- * outside the cache, gets 0; rows with kept below 0 stay as they are. */
+ * outside the cache, gets 0; rows with kept below 0 stay as they are. n_tokens q_heads
+ * may be up to 2^23. */
 typedef struct {
   int64_t struct_bytes;     /* sizeof(sb_selected_args)                             */
   const void *q;            /* [n_tokens][q_heads][head_dim]                        */

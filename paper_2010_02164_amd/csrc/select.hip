@@ -498,9 +498,10 @@ __global__ __launch_bounds__(THREADS) void k_pick(sb_select_args a, int t0, cons
 // A token's heads of a group are up to 16 rows of one pass over its selected keys
 // (attn_pass.h), which all of them see. Bound by reading the keys: 48 tokens, 8 heads of
 // 128, 2048 keys each: 86 us, 4.7 TB/s; a prompt's, where pages come from the caches,
-// by the waits for them: 900 tokens, 4 heads, 2080 keys: 304 us, 12.6 TB/s (two
-// workgroups a compute unit, not three: 340, and the 48 tokens 86 to 89; values asked
-// for together with the keys: 323 and 99, out of registers, by two workgroups 348 and 93).
+// by the waits for them: 900 tokens, 4 heads, 2080 keys: 297 to 304 us in a series of
+// them, 322 between a step's other kernels, 12.6 TB/s (two workgroups a compute unit,
+// not three: 340, and the 48 tokens 86 to 89; values asked for together with the keys:
+// 323 and 99, out of registers, by two workgroups 348 and 93).
 // In the workspace: the parts' sums [splits][n_tokens][q_heads][D] and their
 // (reference, sum).
 template <int DT, int D>

@@ -68,8 +68,15 @@ inline SharedKinds shared_kinds(const sb_shared_args &x) {
 
 // -- selection of pages -------------------------------------------------------------
 
-// Whether scores are made 16 tokens at a time by the matrix unit.
-inline bool many_scores(const sb_select_args &a) { return a.n_tokens >= 8LL * a.n_requests; }   // several tokens of a request in 16
+// Whether scores are made 16 tokens at a time by the matrix unit, by how many tokens a
+// request has on average. Scores and lists in us, a token at a time and 16, at 1, 4, 8
+// and 16 tokens a request: 12 requests of 5000 to 50000 tokens, pages of 16, 8 heads of
+// 128: 35 and 91, 64 and 85, 98 and 78, 172 and 92; 12 of 20000 to 120000, pages of 64,
+// 4 of 64: 28 and 51, 38 and 38, 46 and 38, 67 and 50; 48 of 2000 to 20000, pages of 32,
+// 8 of 128: 35 and 84, 65 and 71, 127 and 75, 234 and 91; one of 20000, pages of 16, 4
+// of 128: 17 and 22, 19 and 23, 21 and 24, 24 and 25. (One prompt of 300 among 15
+// single tokens, 20 on average: 154 and 332.)
+inline bool many_scores(const sb_select_args &a) { return a.n_tokens >= 8LL * a.n_requests; }
 
 // Pages that are ranked, as max_kv lets expect.
 inline long long pages_between(const sb_select_args &a) {

@@ -112,7 +112,7 @@ struct Scan {
 
 // 128 rows by a workgroup. (Each weight in two parts, as by waves, so that what a
 // request gets does not go by how many others there are: 64 requests behind 8000
-// tokens take 79 us for 76, 120 behind two of 24000 and 33000 500 for 444.)
+// tokens take 79 to 82 us for 76, 120 behind two of 24000 and 33000 484 to 500 for 444.)
 template <int DT, int D>
 __device__ __forceinline__ void part_many(const sb_attention_args &a, const Span &s, int hk, const int *table, int t0, int count, float *sums,
                                           float2 *stats, ManyShared<D> &sh) {
@@ -295,7 +295,10 @@ __device__ __forceinline__ void run_own(const sb_attention_args &a, const Prefix
 }
 
 // Workgroups of one pass, then those of the other; of each the key/value heads side
-// by side, so that those of one head, which read the same keys, share an XCD's L2.
+// by side, so that those of one head, which read the same keys, share an XCD's L2. Both
+// passes in one kernel take the registers and the LDS of the larger one: at heads of 128
+// a pass of 128 rows lets two workgroups into a compute unit, and 61 (with 16 own rows),
+// 100 (32) and 173 (128) registers are spilled, 40 with two passes of 32.
 template <int DT, int D, int P, int O>
 __global__ __launch_bounds__(AT_THREADS, D == 256 ? 1 : 2) void k_shared(sb_attention_args a, Prefix p, Cut c, void *work) {
   __shared__ SharedLds<D, P, O> sh;

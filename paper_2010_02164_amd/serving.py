@@ -336,7 +336,9 @@ def shared_attention(q, k_cache, v_cache, prefix_table, prefix_lens, group_start
     behind one instruction), requests of no group follow none. The others as in
     paged_attention, with lens and table of the tokens behind the prefix alone.
     max_q, max_kv, max_prefix: upper bounds of a request's queries, of lens and of
-    prefix_lens, for the choice of kernels and splits only."""
+    prefix_lens, for the choice of kernels and splits only (the groups'
+    sizes count there, too): weights are off by the square of the type's rounding in
+    all of them."""
     i, dtype = _device(q, "q"), q.dtype
     if dtype not in _HALVES:
         _refuse("q must be bfloat16 or float16")

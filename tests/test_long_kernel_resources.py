@@ -23,3 +23,17 @@ def test_registers(kernels):  # noqa: F811
     for name, (used, spills) in kernels.items():
         if re.search("k_selectedILi.ELi128E", name):
             assert used <= 168 and spills <= 8, (name, used, spills)
+
+
+def test_shared_passes_registers(kernels):  # noqa: F811
+    """Every pair of passes of the attention over a shared prefix. Both are in one
+    kernel, at two workgroups a compute unit (one at heads of 256): with passes of 128
+    rows, and two of 32, registers are spilled, no more than here."""
+    spilled = {   # head_dim: {(prefix's rows, own rows): registers}
+        64: {}, 128: {(2, 2): 48, (8, 1): 72, (8, 2): 112, (8, 8): 184}, 256: {(2, 2): 48, (8, 1): 136, (8, 2): 176, (8, 8): 304}}
+    for D, known in spilled.items():
+        for pair in ((1, 1), (2, 1), (8, 1), (2, 2), (8, 2), (8, 8)):
+            found = {k: v for k, v in kernels.items() if re.search(f"k_sharedILi.ELi{D}ELi{pair[0]}ELi{pair[1]}E", k)}
+            assert len(found) == 2   # both types
+            for name, (used, spills) in found.items():
+                assert used <= (512 if D == 256 else 256) and spills <= known.get(pair, 0), (name, used, spills)
